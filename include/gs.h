@@ -547,6 +547,84 @@ GS_API gs_status gs_release_workspace(void);
  */
 GS_API gs_status gs_tune_node2vec_group(int32_t lanes);
 
+/* ---------------------------------------------------------------- sequence models over walks */
+/*
+ * Attention over the positions of a walk, or of any sequence, and its gradient (the training step
+ * of a sequence model on the nodes that gs_random_walks visits; GraphScale itself trains pairs).
+ * For sequence b, query head h and its key/value head g = h / (q_heads / kv_heads):
+ *   s_ij = scale * q_i . k_j,  lse_i = log sum_j exp(s_ij),  out_i = sum_j exp(s_ij - lse_i) v_j
+ * over the visible keys j of row i.  With n_q = d_q_lens[b] (q_len if NULL), n_k = d_k_lens[b]
+ * (k_len if NULL), key j is visible to query i iff i < n_q, j < n_k and
+ *   -window_left <= j - (i + n_k - n_q) <= window_right,
+ * a negative bound meaning none: (-1, -1) everything, (-1, 0) causal with the last query at the last
+ * key, (w, w) the window of the skip-gram pairs.  A row that sees nothing has out = 0,
+ * lse = -infinity and gives no gradient.  Positions at or beyond n_q and n_k are never read (they may
+ * hold anything, NaN included); their outputs and gradients are written as zeros.  Lengths
+ * outside [0, q_len] and [0, k_len] are clamped to it.
+ *
+ * Tensors are [batch][position][head][head_dim] with any strides (in elements) over the first three
+ * and contiguous head_dim values; dtype GS_TABLE_F32, GS_TABLE_F16 or GS_TABLE_BF16 for all of them.
+ * d_lse is float [batch][q_heads][q_len], contiguous.  Inputs may have zero strides (broadcast
+ * values); outputs may not, and no output may overlap an input.  Sums, maxima and gradients are kept
+ * in fp32; 16-bit tensors multiply on the tensor cores with the probabilities and score gradients rounded
+ * to the tensors' type.  Results do not depend on scheduling: no value is summed with atomics.
+ * Supported: head_dim 1..128, lengths below 2^29.  No library scratch: calls on several streams may overlap.
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED, GS_ERR_CUDA.
+ */
+typedef struct gs_attention_config {
+    int32_t dtype;
+    int32_t head_dim;
+    int32_t q_heads, kv_heads;            /* q_heads a multiple of kv_heads                */
+    int64_t batch;
+    int32_t q_len, k_len;
+    int32_t window_left, window_right;
+    float   scale;                        /* positive; usually 1 / sqrt(head_dim)          */
+    int32_t reserved;                     /* 0                                             */
+    const int32_t *d_q_lens, *d_k_lens;   /* [batch] or NULL                               */
+    int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];       /* batch, position, head */
+    int64_t dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];   /* backward only         */
+} gs_attention_config;
+
+GS_API gs_status gs_attention_forward(const gs_attention_config *cfg, const void *d_q, const void *d_k,
+                               const void *d_v, void *d_out, float *d_lse, void *stream);
+
+/*
+ * d_out and d_lse are the forward call's results, d_dout the gradient of d_out.  With
+ * p_ij = exp(s_ij - lse_i) computed again and delta_i = dout_i . out_i:
+ *   ds_ij = p_ij (dout_i . v_j - delta_i),  dq_i = scale sum_j ds_ij k_j,
+ *   dk_j = scale sum_{h of the group, i} ds_ij q_i,  dv_j = sum_{h of the group, i} p_ij dout_i.
+ * d_work: batch * q_heads * q_len floats of the caller's, written by the call.
+ */
+GS_API gs_status gs_attention_backward(const gs_attention_config *cfg, const void *d_dout, const void *d_q,
+                                const void *d_k, const void *d_v, const void *d_out, const float *d_lse,
+                                float *d_work, void *d_dq, void *d_dk, void *d_dv, void *stream);
+
+/*
+ * Norm of the gradients of many tensors taken as one vector, and clipping by it (the bound on an
+ * update's length before it reaches a table).  *d_norm = sqrt(sum of all squares); squares are
+ * taken in fp32 (an element beyond 1.8e19 in magnitude makes the norm infinite), summed in fp32 over 32
+ * elements of a tensor and in fp64 from there, in an order that the sizes alone fix.
+ * gs_clip_gradients writes out = g * factor, rounded once to the output's type, with factor =
+ * max_norm / norm if the norm is finite and greater than max_norm, else 1 (a norm that is not finite leaves
+ * the gradients as they are for the caller to drop the step).  h_out NULL: in place.  An output may be
+ * its own gradient's buffer only if both have one type, and must not overlap another tensor.
+ *   h_grads, h_out : HOST arrays, read during the call; empty tensors (numel 0) are allowed
+ *   d_work         : gs_gradient_norm_work(n_tensors) doubles of the caller's, written by the call
+ * Errors: GS_ERR_INVALID_ARG (bad type, size, pointer or max_norm), GS_ERR_CUDA.
+ */
+typedef struct gs_tensor {
+    void   *d_data;                       /* contiguous, aligned to its element size */
+    int64_t numel;
+    int32_t dtype;                        /* GS_TABLE_F32, GS_TABLE_F16, GS_TABLE_BF16 */
+    int32_t reserved;
+} gs_tensor;
+
+GS_API int64_t gs_gradient_norm_work(int64_t n_tensors);
+GS_API gs_status gs_gradient_norm(const gs_tensor *h_grads, int64_t n_tensors, double *d_work, float *d_norm,
+                           void *stream);
+GS_API gs_status gs_clip_gradients(const gs_tensor *h_grads, const gs_tensor *h_out, int64_t n_tensors,
+                            float max_norm, double *d_work, float *d_norm, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,6 +35,8 @@ EXPORTS = [
     "gs_init_embeddings_f16", "gs_sgns_step_f16", "gs_sgns_step_adam", "gs_build_keep_thresholds",
     "gs_subsample_walks", "gs_shuffled_starts", "gs_refused_ids",
     "gs_init_embeddings_bf16", "gs_sgns_step_bf16",
+    "gs_attention_forward", "gs_attention_backward",
+    "gs_gradient_norm_work", "gs_gradient_norm", "gs_clip_gradients",
 ]
 
 
@@ -58,6 +60,21 @@ class SgnsConfig(ctypes.Structure):
         ("d_m_in", ctypes.c_void_p), ("d_m_out", ctypes.c_void_p), ("d_v_in", ctypes.c_void_p),
         ("d_v_out", ctypes.c_void_p), ("d_last_in", ctypes.c_void_p), ("d_last_out", ctypes.c_void_p),
     ]
+
+
+class AttentionConfig(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32), ("batch", ctypes.c_int64), ("q_len", ctypes.c_int32),
+        ("k_len", ctypes.c_int32), ("window_left", ctypes.c_int32), ("window_right", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+        ("d_q_lens", ctypes.c_void_p), ("d_k_lens", ctypes.c_void_p),
+    ] + [(f"{t}_stride", ctypes.c_int64 * 3) for t in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+
+
+class TensorEntry(ctypes.Structure):
+    _fields_ = [("d_data", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class EpochStats(ctypes.Structure):
@@ -87,6 +104,7 @@ def lib():
         for name in EXPORTS:
             if name not in ("gs_last_error", "gs_graph_free"):
                 getattr(L, name).restype = ctypes.c_int32
+        L.gs_gradient_norm_work.restype = ctypes.c_int64
         _lib = L
     return _lib
 
@@ -424,3 +442,133 @@ def gs_release_workspace():
 
 def gs_tune_node2vec_group(lanes: int):
     _check(lib().gs_tune_node2vec_group(ctypes.c_int32(lanes)))
+
+
+# ---------------------------------------------------------------- sequence models over walks
+_TABLE_DTYPE = {torch.float32: GS_TABLE_F32, torch.float16: GS_TABLE_F16, torch.bfloat16: GS_TABLE_BF16}
+
+
+def _heads(t, like, shape, name):
+    """Checks one [batch, position, head, head_dim] tensor; returns its address."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == like.dtype and t.device == like.device):
+        raise TypeError(f"{name} must be a CUDA tensor of {like.dtype} on {like.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.stride(3) != 1 and shape[3] > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return t.data_ptr()
+
+
+def _lens(t, batch, like, name):
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.device == like.device and t.dtype == torch.int32
+            and t.is_contiguous() and t.shape == (batch,)):
+        raise TypeError(f"{name} must be a contiguous int32 tensor of {batch} lengths on {like.device}")
+    return t.data_ptr()
+
+
+def _attention_config(q, k, v, scale, window, q_lens, k_lens):
+    if not (isinstance(q, torch.Tensor) and q.is_cuda and q.dim() == 4 and q.dtype in _TABLE_DTYPE):
+        raise TypeError("q must be a CUDA tensor [batch, position, head, head_dim] of float32, float16 or bfloat16")
+    if not (isinstance(k, torch.Tensor) and k.dim() == 4):
+        raise TypeError("k must be a tensor [batch, position, head, head_dim]")
+    if q.device.index != torch.cuda.current_device():
+        raise ValueError(f"q is on {q.device}, which is not the current device")
+    b, n, hq, d = q.shape
+    m, hk = k.shape[1], k.shape[2]
+    if scale is None:
+        scale = d ** -0.5 if d else 1.0
+    kv = (b, m, hk, d)
+    cfg = AttentionConfig(_TABLE_DTYPE[q.dtype], d, hq, hk, b, n, m, window[0], window[1], scale, 0,
+                          _lens(q_lens, b, q, "q_lens"), _lens(k_lens, b, q, "k_lens"))
+    cfg.q_stride[:] = q.stride()[:3]
+    cfg.k_stride[:] = k.stride()[:3]
+    cfg.v_stride[:] = v.stride()[:3]
+    return cfg, _heads(q, q, q.shape, "q"), _heads(k, q, kv, "k"), _heads(v, q, kv, "v")
+
+
+def _ptr(address) -> ctypes.c_void_p:
+    return ctypes.c_void_p(address)
+
+
+def gs_attention_forward(q, k, v, scale=None, window=(-1, -1), q_lens=None, k_lens=None, out=None, lse=None):
+    """Attention of q[batch, q_len, q_heads, head_dim] over k, v[batch, k_len, kv_heads, head_dim]
+    (see gs.h for the visible keys).  Returns (out like q, lse float32[batch, q_heads, q_len])."""
+    cfg, pq, pk, pv = _attention_config(q, k, v, scale, window, q_lens, k_lens)
+    b, n, hq, _ = q.shape
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((b, hq, n), dtype=torch.float32, device=q.device)
+    elif lse.shape != (b, hq, n):
+        raise ValueError(f"lse has shape {tuple(lse.shape)}, expected {(b, hq, n)}")
+    po = _heads(out, q, q.shape, "out")
+    cfg.out_stride[:] = out.stride()[:3]
+    _check(lib().gs_attention_forward(ctypes.byref(cfg), _ptr(pq), _ptr(pk), _ptr(pv), _ptr(po),
+                                      _dev(lse, torch.float32, "lse"), _stream()))
+    return out, lse
+
+
+def gs_attention_backward(dout, q, k, v, out, lse, scale=None, window=(-1, -1), q_lens=None, k_lens=None,
+                          dq=None, dk=None, dv=None):
+    """Gradients of gs_attention_forward: returns (dq, dk, dv), shaped like q, k, v.  out and lse are
+    the forward call's results, dout the gradient of out."""
+    cfg, pq, pk, pv = _attention_config(q, k, v, scale, window, q_lens, k_lens)
+    b, n, hq, _ = q.shape
+    if not (isinstance(lse, torch.Tensor) and lse.shape == (b, hq, n)):
+        raise ValueError(f"lse must be a tensor of shape {(b, hq, n)}")
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
+    dv = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dv is None else dv
+    at = {}
+    for name, t, like in (("dout", dout, q), ("out", out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+        at[name] = _ptr(_heads(t, q, like.shape, name))
+        getattr(cfg, f"{name}_stride")[:] = t.stride()[:3]
+    work = torch.empty(b * hq * n, dtype=torch.float32, device=q.device)
+    _check(lib().gs_attention_backward(ctypes.byref(cfg), at["dout"], _ptr(pq), _ptr(pk), _ptr(pv), at["out"],
+                                       _dev(lse, torch.float32, "lse"), _ptr(work.data_ptr()), at["dq"], at["dk"],
+                                       at["dv"], _stream()))
+    return dq, dk, dv
+
+
+def _tensor_list(tensors, name):
+    device = torch.cuda.current_device()
+    entries = (TensorEntry * len(tensors))()
+    for e, t in zip(entries, tensors):
+        code = _TABLE_DTYPE.get(t.dtype)
+        if code is None or not t.is_cuda or t.device.index != device or not t.is_contiguous():
+            raise TypeError(f"{name} must be contiguous float32, float16 or bfloat16 tensors on the current CUDA device")
+        e.d_data, e.numel, e.dtype = t.data_ptr(), t.numel(), code
+    return entries
+
+
+def _norm_buffers(n):
+    words = lib().gs_gradient_norm_work(ctypes.c_int64(n))
+    device = torch.cuda.current_device()
+    return (torch.empty(words, dtype=torch.float64, device=device),
+            torch.empty(1, dtype=torch.float32, device=device))
+
+
+def gs_gradient_norm(grads):
+    """Euclidean norm of all tensors of `grads` taken as one vector: float32[1] on the device."""
+    entries = _tensor_list(grads, "grads")
+    work, norm = _norm_buffers(len(entries))
+    _check(lib().gs_gradient_norm(entries, ctypes.c_int64(len(entries)), _ptr(work.data_ptr()),
+                                  _ptr(norm.data_ptr()), _stream()))
+    return norm
+
+
+def gs_clip_gradients(grads, max_norm: float, out=None):
+    """Scales `grads` (into the tensors `out`, or in place) so that their joint norm is at most
+    max_norm; returns the norm before clipping, float32[1] on the device (nothing waits for it)."""
+    entries = _tensor_list(grads, "grads")
+    targets = None
+    if out is not None:
+        if len(out) != len(grads):
+            raise ValueError(f"{len(out)} outputs for {len(grads)} gradients")
+        targets = _tensor_list(out, "out")
+    work, norm = _norm_buffers(len(entries))
+    _check(lib().gs_clip_gradients(entries, targets, ctypes.c_int64(len(entries)), ctypes.c_float(max_norm),
+                                   _ptr(work.data_ptr()), _ptr(norm.data_ptr()), _stream()))
+    return norm

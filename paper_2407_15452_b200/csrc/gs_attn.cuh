@@ -1,0 +1,72 @@
+// Shared pieces of the attention kernels: the argument block that the launchers take and the
+// visibility rule.  Mathematics (per sequence b, query head h, key/value head g = h / group):
+//   s_ij = scale q_i.k_j      lse_i = log sum_j exp s_ij      o_i = sum_j exp(s_ij - lse_i) v_j
+// over the visible keys of row i, which are one interval [lo(i), hi(i)): with n_q, n_k the lengths
+// of the sequence and off = n_k - n_q,
+//   lo(i) = max(0, i + off - left), hi(i) = min(n_k, i + off + right + 1), nothing if i >= n_q;
+// a negative left or right lifts that bound.  Seen from key j the visible queries are again an
+// interval, [j - off - right, j - off + left].
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "gs_common.cuh"
+
+namespace gs {
+
+struct AttnTensor {
+    void *p;
+    int64_t sb, sl, sh;               // strides in elements: sequence, position, head
+};
+
+struct AttnArgs {
+    AttnTensor q, k, v, out, dout, dq, dk, dv;
+    float *lse, *delta;               // [batch][q_heads][q_len]
+    const int32_t *q_lens, *k_lens;   // may be null
+    int64_t batch;
+    int32_t q_len, k_len, q_heads, kv_heads, group, dim;
+    int32_t left, right;              // < 0: unbounded; otherwise at most q_len + k_len
+    float scale;
+    int32_t dtype;
+};
+
+struct AttnSeq {                      // one sequence's lengths
+    int nq, nk, off;
+};
+
+__device__ __forceinline__ AttnSeq attn_seq(const AttnArgs &a, int64_t b)
+{
+    AttnSeq s;
+    // a length outside [0, padded length] is clamped: the library never follows it out of range
+    s.nq = a.q_lens ? min(max(__ldg(a.q_lens + b), 0), a.q_len) : a.q_len;
+    s.nk = a.k_lens ? min(max(__ldg(a.k_lens + b), 0), a.k_len) : a.k_len;
+    s.off = s.nk - s.nq;
+    return s;
+}
+
+__device__ __forceinline__ int attn_lo(const AttnArgs &a, const AttnSeq &s, int i)
+{
+    return a.left < 0 ? 0 : max(0, i + s.off - a.left);
+}
+// 0 for a row past the sequence's end, so that [lo, hi) is empty there
+__device__ __forceinline__ int attn_hi(const AttnArgs &a, const AttnSeq &s, int i)
+{
+    if (i >= s.nq) return 0;
+    return a.right < 0 ? s.nk : min(s.nk, i + s.off + a.right + 1);
+}
+// queries that see a key of [j0, j1): the range [first, last)
+__device__ __forceinline__ int attn_q_first(const AttnArgs &a, const AttnSeq &s, int j0)
+{
+    return a.right < 0 ? 0 : max(0, j0 - s.off - a.right);
+}
+__device__ __forceinline__ int attn_q_last(const AttnArgs &a, const AttnSeq &s, int j1)
+{
+    return a.left < 0 ? s.nq : min(s.nq, j1 - s.off + a.left);
+}
+
+// gs_attn_simt.cu
+gs_status attn_simt_forward(const AttnArgs &a, cudaStream_t st);
+gs_status attn_simt_backward(const AttnArgs &a, cudaStream_t st);
+
+}  // namespace gs
