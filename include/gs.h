@@ -533,6 +533,14 @@ GS_API gs_status gs_sgns_epoch(const gs_graph *g, const uint64_t *d_alias,
  */
 GS_API gs_status gs_refused_ids(uint64_t *h_count, int32_t clear, void *stream);
 
+/*
+ * Sticky per-device count of thread blocks of the tensor-core attention kernels that gave up a wait inside
+ * the kernel (about two seconds without progress; the results of that call are then not valid).
+ * No input causes it; it is there so that a fault of the hardware or of the library ends as a number and not
+ * as a hang.  Reads the counter after the work queued on `stream`, clears it if clear != 0, and WAITS.
+ */
+GS_API gs_status gs_stalled_kernels(uint64_t *h_count, int32_t clear, void *stream);
+
 /* Frees the cached scratch memory of the current device (waits for the device). */
 GS_API gs_status gs_release_workspace(void);
 

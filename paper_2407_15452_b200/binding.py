@@ -36,7 +36,7 @@ EXPORTS = [
     "gs_subsample_walks", "gs_shuffled_starts", "gs_refused_ids",
     "gs_init_embeddings_bf16", "gs_sgns_step_bf16",
     "gs_attention_forward", "gs_attention_backward",
-    "gs_gradient_norm_work", "gs_gradient_norm", "gs_clip_gradients",
+    "gs_stalled_kernels", "gs_gradient_norm_work", "gs_gradient_norm", "gs_clip_gradients",
 ]
 
 
@@ -433,6 +433,13 @@ def gs_refused_ids(clear: bool = False) -> int:
     """Ids refused by the kernels of the current device so far (waits for the current stream)."""
     out = ctypes.c_uint64(0)
     _check(lib().gs_refused_ids(ctypes.byref(out), ctypes.c_int32(1 if clear else 0), _stream()))
+    return out.value
+
+
+def gs_stalled_kernels(clear: bool = False) -> int:
+    """Blocks of the tensor-core attention kernels that gave up a wait (waits for the current stream)."""
+    out = ctypes.c_uint64(0)
+    _check(lib().gs_stalled_kernels(ctypes.byref(out), ctypes.c_int32(1 if clear else 0), _stream()))
     return out.value
 
 

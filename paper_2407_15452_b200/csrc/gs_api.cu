@@ -165,6 +165,24 @@ unsigned long long *refused_counter()
     return (unsigned long long *)((char *)ws + 160);
 }
 
+unsigned long long *stall_counter()
+{
+    void *ws = nullptr;
+    if (workspace_get(WS_COUNTERS, 256, &ws) != GS_OK) return nullptr;
+    return (unsigned long long *)((char *)ws + 168);
+}
+
+static gs_status read_counter(unsigned long long *ctr, uint64_t *h_count, int32_t clear, cudaStream_t st)
+{
+    if (!ctr) return GS_ERR_OOM;
+    unsigned long long v = 0;
+    GS_CUDA_TRY(cudaMemcpyAsync(&v, ctr, sizeof(v), cudaMemcpyDeviceToHost, st));
+    if (clear) GS_CUDA_TRY(cudaMemsetAsync(ctr, 0, sizeof(v), st));
+    GS_CUDA_TRY(cudaStreamSynchronize(st));
+    *h_count = (uint64_t)v;
+    return GS_OK;
+}
+
 static bool dim_ok(int32_t dim) { return dim == 32 || dim == 64 || dim == 128 || dim == 256; }
 
 }  // namespace gs
@@ -178,15 +196,13 @@ const char *gs_last_error(void) { return g_err; }
 gs_status gs_refused_ids(uint64_t *h_count, int32_t clear, void *stream)
 {
     if (!h_count) return invalid("h_count is NULL");
-    unsigned long long *ctr = refused_counter();
-    if (!ctr) return GS_ERR_OOM;
-    cudaStream_t st = (cudaStream_t)stream;
-    unsigned long long v = 0;
-    GS_CUDA_TRY(cudaMemcpyAsync(&v, ctr, sizeof(v), cudaMemcpyDeviceToHost, st));
-    if (clear) GS_CUDA_TRY(cudaMemsetAsync(ctr, 0, sizeof(v), st));
-    GS_CUDA_TRY(cudaStreamSynchronize(st));
-    *h_count = (uint64_t)v;
-    return GS_OK;
+    return read_counter(refused_counter(), h_count, clear, (cudaStream_t)stream);
+}
+
+gs_status gs_stalled_kernels(uint64_t *h_count, int32_t clear, void *stream)
+{
+    if (!h_count) return invalid("h_count is NULL");
+    return read_counter(stall_counter(), h_count, clear, (cudaStream_t)stream);
 }
 
 gs_status gs_release_workspace(void)

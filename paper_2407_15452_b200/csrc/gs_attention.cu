@@ -97,6 +97,7 @@ gs_status gs_attention_forward(const gs_attention_config *cfg, const void *d_q, 
     if ((s = pointers_ok(need, a.k_len ? 4 : 2, a.dtype)) != GS_OK) return s;
     if (!d_lse) return bad("d_lse is NULL");
     if (!writable(a.out, a.batch, a.q_len, a.q_heads)) return bad("out has a zero stride");
+    if (a.q_len > 64 && a.k_len > 0 && attn_tc_forward_ok(a)) return attn_tc_forward(a, (cudaStream_t)stream);
     return attn_simt_forward(a, (cudaStream_t)stream);
 }
 
