@@ -601,8 +601,10 @@ GS_API gs_status gs_attention_forward(const gs_attention_config *cfg, const void
  * p_ij = exp(s_ij - lse_i) computed again and delta_i = dout_i . out_i:
  *   ds_ij = p_ij (dout_i . v_j - delta_i),  dq_i = scale sum_j ds_ij k_j,
  *   dk_j = scale sum_{h of the group, i} ds_ij q_i,  dv_j = sum_{h of the group, i} p_ij dout_i.
- * d_work: batch * q_heads * q_len floats of the caller's, written by the call.
+ * d_work: gs_attention_backward_work(cfg) floats of the caller's, written by the call (at least
+ * batch * q_heads * q_len; the function returns -1 for a configuration that the calls refuse).
  */
+GS_API int64_t gs_attention_backward_work(const gs_attention_config *cfg);
 GS_API gs_status gs_attention_backward(const gs_attention_config *cfg, const void *d_dout, const void *d_q,
                                 const void *d_k, const void *d_v, const void *d_out, const float *d_lse,
                                 float *d_work, void *d_dq, void *d_dk, void *d_dv, void *stream);

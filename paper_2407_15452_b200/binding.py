@@ -35,7 +35,7 @@ EXPORTS = [
     "gs_init_embeddings_f16", "gs_sgns_step_f16", "gs_sgns_step_adam", "gs_build_keep_thresholds",
     "gs_subsample_walks", "gs_shuffled_starts", "gs_refused_ids",
     "gs_init_embeddings_bf16", "gs_sgns_step_bf16",
-    "gs_attention_forward", "gs_attention_backward",
+    "gs_attention_forward", "gs_attention_backward", "gs_attention_backward_work",
     "gs_stalled_kernels", "gs_gradient_norm_work", "gs_gradient_norm", "gs_clip_gradients",
 ]
 
@@ -105,6 +105,7 @@ def lib():
             if name not in ("gs_last_error", "gs_graph_free"):
                 getattr(L, name).restype = ctypes.c_int32
         L.gs_gradient_norm_work.restype = ctypes.c_int64
+        L.gs_attention_backward_work.restype = ctypes.c_int64
         _lib = L
     return _lib
 
@@ -532,7 +533,8 @@ def gs_attention_backward(dout, q, k, v, out, lse, scale=None, window=(-1, -1), 
     for name, t, like in (("dout", dout, q), ("out", out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
         at[name] = _ptr(_heads(t, q, like.shape, name))
         getattr(cfg, f"{name}_stride")[:] = t.stride()[:3]
-    work = torch.empty(b * hq * n, dtype=torch.float32, device=q.device)
+    work = torch.empty(max(0, lib().gs_attention_backward_work(ctypes.byref(cfg))), dtype=torch.float32,
+                       device=q.device)
     _check(lib().gs_attention_backward(ctypes.byref(cfg), at["dout"], _ptr(pq), _ptr(pk), _ptr(pv), at["out"],
                                        _dev(lse, torch.float32, "lse"), _ptr(work.data_ptr()), at["dq"], at["dk"],
                                        at["dv"], _stream()))

@@ -128,7 +128,16 @@ gs_status gs_attention_backward(const gs_attention_config *cfg, const void *d_do
     if (!writable(a.dq, a.batch, a.q_len, a.q_heads) || !writable(a.dk, a.batch, a.k_len, a.kv_heads) ||
         !writable(a.dv, a.batch, a.k_len, a.kv_heads))
         return bad("a gradient has a zero stride");
+    if ((a.q_len > 64 || a.k_len > 64) && a.q_len > 0 && a.k_len > 0 && attn_tc_backward_ok(a))
+        return attn_tc_backward(a, (cudaStream_t)stream);
     return attn_simt_backward(a, (cudaStream_t)stream);
+}
+
+int64_t gs_attention_backward_work(const gs_attention_config *cfg)
+{
+    AttnArgs a;
+    if (fill(cfg, &a) != GS_OK) return -1;
+    return a.batch * a.q_heads * a.q_len + attn_tc_backward_work(a.batch, a.q_len, a.k_len, a.q_heads, a.kv_heads);
 }
 
 }  // extern "C"

@@ -22,7 +22,7 @@ struct AttnTensor {
 
 struct AttnArgs {
     AttnTensor q, k, v, out, dout, dq, dk, dv;
-    float *lse, *delta;               // [batch][q_heads][q_len]
+    float *lse, *delta;               // [batch][q_heads][q_len]; delta heads the caller's scratch
     const int32_t *q_lens, *k_lens;   // may be null
     int64_t batch;
     int32_t q_len, k_len, q_heads, kv_heads, group, dim;
@@ -72,5 +72,9 @@ gs_status attn_simt_backward(const AttnArgs &a, cudaStream_t st);
 // gs_attn_tc.cu
 bool attn_tc_forward_ok(const AttnArgs &a);
 gs_status attn_tc_forward(const AttnArgs &a, cudaStream_t st);
+// gs_attn_tc_bwd.cu
+bool attn_tc_backward_ok(const AttnArgs &a);
+int64_t attn_tc_backward_work(int64_t batch, int32_t q_len, int32_t k_len, int32_t q_heads, int32_t kv_heads);   // floats
+gs_status attn_tc_backward(const AttnArgs &a, cudaStream_t st);
 
 }  // namespace gs

@@ -15,8 +15,7 @@
 // The running maximum moves only when the new one is above it by more than 8 (a factor 256 in p):
 // most tiles then leave O and the sum alone, exact in any case because the quotient O / sum uses one base.
 // p is rounded to the tensors' type for the product with V; the sum takes it in fp32.
-#include "gs_attn.cuh"
-#include "gs_tc.cuh"
+#include "gs_attn_tc.cuh"
 
 namespace gs {
 
@@ -27,7 +26,6 @@ static constexpr int ROWS = 256, KEYS = 128;
 template <int DP>
 struct FwdSmem {
     static constexpr int TILE = 128 * DP * 2;                   // bytes of one 128-row tile
-    static constexpr int HALF = 128 * 128;                      // of one 64-value box
     static constexpr int SLOTS = DP == 128 ? 4 : 8;
     static constexpr int Q = 0, RING = 2 * TILE, BARS = RING + SLOTS * TILE;
     static constexpr int BYTES = BARS + 256 + 1024;             // 1024: alignment of the tiles
@@ -36,39 +34,6 @@ struct FwdSmem {
 struct TcMaps {
     CUtensorMap q, k, v;
 };
-
-// One 128-row tile of DP values into shared memory at `dst` (DP / 64 boxes)
-template <int DP>
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int pos, int head, int b)
-{
-#pragma unroll
-    for (int x = 0; x < DP / 64; ++x) tma_load(dst + x * 128 * 128, map, bar, x * 64, pos, head, b);
-}
-
-// 32 columns of one row, times mul (0: zeros whatever o holds)
-template <bool BF16>
-__device__ __forceinline__ void store32(uint16_t *row, int c, int dim, bool vec, const float (&o)[32], float mul)
-{
-    uint32_t u[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) u[i] = mul != 0.f ? pack2<BF16>(o[2 * i] * mul, o[2 * i + 1] * mul) : 0u;
-    if (vec) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + 8 * i < dim)
-                *reinterpret_cast<uint4 *>(row + c + 8 * i) = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (c + i < dim) row[c + i] = (uint16_t)(i & 1 ? u[i / 2] >> 16 : u[i / 2]);
-    }
-}
-
-// rows that 16-byte stores may write
-__device__ __forceinline__ bool rows16(const AttnTensor &t, int dim)
-{
-    return dim % 8 == 0 && (((uintptr_t)t.p | (uintptr_t)(2 * t.sb) | (uintptr_t)(2 * t.sl) | (uintptr_t)(2 * t.sh)) & 15) == 0;
-}
 
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(384, 1)
@@ -163,16 +128,8 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
                             bar_expect(patch ? fix : full, L::TILE);
                             load_tile<DP>(dst, kv ? &maps.v : &maps.k, patch ? fix : full, it * KEYS, g, (int)b);
                         }
-                        if (patch) {                              // only ever the last tile: `fix` is used once
-                            ok = __all_sync(0xffffffffu, bar_wait(fix, 0, &stalled));
-                            for (int e = (s.nk - it * KEYS) * 8 + lane; e < KEYS * 8; e += 32)
-#pragma unroll
-                                for (int x = 0; x < DP / 64; ++x)
-                                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst + x * L::HALF + e * 16), "r"(0) : "memory");
-                            fence_async_shared();
-                            __syncwarp();
-                            if (lane == 0) bar_arrive(full);
-                        }
+                            // only ever the last tile: `fix` is used once
+                        if (patch) ok = patch_tile<DP>(dst, s.nk - it * KEYS, fix, 0, full, &stalled);
                     }
                 }
             }
@@ -200,14 +157,14 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
                             fence_after();
 #pragma unroll
                             for (int k = 0; k < KEYS / 16; ++k)
-                                mma_ts(tmem + 256 + 128 * t, tmem + 128 * t + 8 * k, desc_rows(vt + 2048 * k, L::HALF), DESC_O,
+                                mma_ts(tmem + 256 + 128 * t, tmem + 128 * t + 8 * k, desc_rows(vt + 2048 * k, HALF_TILE), DESC_O,
                                        it - 1 > first[t] || k > 0);
                             if (it == last[t]) mma_commit(o_full + 8 * t);
                         }
                         if (it >= first[t] && it < last[t]) {
 #pragma unroll
                             for (int k = 0; k < DP / 16; ++k) {
-                                const uint32_t at = (k / 4) * L::HALF + (k % 4) * 32;
+                                const uint32_t at = (k / 4) * HALF_TILE + (k % 4) * 32;
                                 mma_ss(tmem + 128 * t, desc_values(base + L::Q + t * L::TILE + at), desc_values(kt + at), DESC_S, k > 0);
                             }
                             mma_commit(s_full + 8 * t);
@@ -227,7 +184,7 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
         const int r = r0 + 128 * t + (threadIdx.x & 127);
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const uint32_t ts = tmem + lanes + 128 * t, to = tmem + lanes + 256 + 128 * t;
-        const float mul = a.scale * 1.44269504088896341f;         // log2(e): exponents are taken in base 2
+        const float mul = a.scale * LOG2E;                      // exponents are taken in base 2
         const bool row = r < s.nq;
         const int lo = row ? attn_lo(a, s, r) : 0, hi = row ? attn_hi(a, s, r) : s.nk;
         // tiles that every row of this tile sees whole need no mask
@@ -301,7 +258,7 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
         if (ok && some) ok = __all_sync(0xffffffffu, bar_wait(o_full + 8 * t, 0, &stalled));
         fence_after();
         const float inv = row && some && sum != 0.f ? 1.f / sum : 0.f;
-        if (r < a.q_len) a.lse[bh * a.q_len + r] = inv != 0.f ? (top + log2f(sum)) * 0.693147180559945309f : -INFINITY;
+        if (r < a.q_len) a.lse[bh * a.q_len + r] = inv != 0.f ? (top + log2f(sum)) * LN2 : -INFINITY;
         uint16_t *out = reinterpret_cast<uint16_t *>(a.out.p) + b * a.out.sb + (int64_t)r * a.out.sl + h * a.out.sh;
         const bool vec = rows16(a.out, a.dim);
 #pragma unroll
@@ -319,14 +276,7 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
     fence_before();
     __syncthreads();
     fence_after();
-    if (stalled) {
-        // give loads and products in flight a bounded time to end before the block's memory goes
-        if (threadIdx.x == 0) {
-            for (int i = 0; i < 64; ++i) __nanosleep(100000);
-            if (stalls) atomicAdd(stalls, 1ull);
-        }
-        __syncthreads();
-    }
+    if (stalled) drain_stalled(stalls);
     if (warp == 8) tmem_free(tmem, 512);
 }
 
@@ -356,9 +306,8 @@ bool attn_tma_ok(const AttnTensor &t, int64_t batch, int64_t len, int64_t heads)
     return (uintptr_t)t.p % 16 == 0 && stride_ok(batch, t.sb) && stride_ok(len, t.sl) && stride_ok(heads, t.sh);
 }
 
-// boxes of `rows` positions x 64 values of a tensor for which attn_tma_ok holds
 gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_t batch, int64_t len, int64_t heads,
-                          int dim, int rows)
+                          int dim)
 {
     EncodeTiled fn = encoder();
     if (!fn) {
@@ -368,7 +317,7 @@ gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_
     const cuuint64_t extent[4] = {(cuuint64_t)dim, (cuuint64_t)len, (cuuint64_t)heads, (cuuint64_t)batch};
     const cuuint64_t stride[3] = {(cuuint64_t)(len > 1 ? 2 * t.sl : 256), (cuuint64_t)(heads > 1 ? 2 * t.sh : 256),
                                   (cuuint64_t)(batch > 1 ? 2 * t.sb : 256)};
-    const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64, 128, 1, 1}, step[4] = {1, 1, 1, 1};
     const CUresult r = fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, t.p, extent, stride,
                           box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -405,9 +354,9 @@ gs_status attn_tc_forward(const AttnArgs &a, cudaStream_t st)
     const bool bf16 = a.dtype == GS_TABLE_BF16;
     TcMaps m;
     gs_status s;
-    if ((s = attn_tensor_map(&m.q, a.q, bf16, a.batch, a.q_len, a.q_heads, a.dim, 128)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.k, a.k, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 128)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.v, a.v, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.q, a.q, bf16, a.batch, a.q_len, a.q_heads, a.dim)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.k, a.k, bf16, a.batch, a.k_len, a.kv_heads, a.dim)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.v, a.v, bf16, a.batch, a.k_len, a.kv_heads, a.dim)) != GS_OK) return s;
     if (a.dim <= 64) return bf16 ? forward_t<true, 64>(a, m, st) : forward_t<false, 64>(a, m, st);
     return bf16 ? forward_t<true, 128>(a, m, st) : forward_t<false, 128>(a, m, st);
 }

@@ -1,0 +1,80 @@
+// What the forward and backward tensor-core attention kernels share.
+#pragma once
+
+#include "gs_attn.cuh"
+#include "gs_tc.cuh"
+
+namespace gs {
+
+// host side: whether TMA can address a tensor, and its map with boxes of 128 positions x 64 values
+bool attn_tma_ok(const AttnTensor &t, int64_t batch, int64_t len, int64_t heads);
+gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_t batch, int64_t len, int64_t heads,
+                          int dim);
+
+static constexpr int HALF_TILE = 128 * 128;          // bytes of one box: 128 rows of 64 16-bit values
+static constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+
+// One 128-row tile of DP values into shared memory at `dst` (DP / 64 boxes)
+template <int DP>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int pos, int head, int b)
+{
+#pragma unroll
+    for (int x = 0; x < DP / 64; ++x) tc::tma_load(dst + x * HALF_TILE, map, bar, x * 64, pos, head, b);
+}
+
+// 32 columns of one row, times mul (0: zeros whatever o holds)
+template <bool BF16>
+__device__ __forceinline__ void store32(uint16_t *row, int c, int dim, bool vec, const float (&o)[32], float mul)
+{
+    uint32_t u[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) u[i] = mul != 0.f ? tc::pack2<BF16>(o[2 * i] * mul, o[2 * i + 1] * mul) : 0u;
+    if (vec) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + 8 * i < dim)
+                *reinterpret_cast<uint4 *>(row + c + 8 * i) = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (c + i < dim) row[c + i] = (uint16_t)(i & 1 ? u[i / 2] >> 16 : u[i / 2]);
+    }
+}
+
+// rows that 16-byte stores may write
+__device__ __forceinline__ bool rows16(const AttnTensor &t, int dim)
+{
+    return dim % 8 == 0 && (((uintptr_t)t.p | (uintptr_t)(2 * t.sb) | (uintptr_t)(2 * t.sl) | (uintptr_t)(2 * t.sh)) & 15) == 0;
+}
+
+// Rows [from, 128) of a tile that TMA has just written (bar `done`, first phase `parity`) become zeros,
+// then `full` is announced in TMA's stead.  Whole warp.  For operands whose rows are summed over: what lies
+// past a sequence's end must not meet a zero factor (0 * NaN).
+template <int DP>
+__device__ __forceinline__ bool patch_tile(uint32_t tile, int from, uint32_t done, uint32_t parity, uint32_t full,
+                                           volatile int *stalled)
+{
+    const bool ok = __all_sync(0xffffffffu, tc::bar_wait(done, parity, stalled));
+    const int lane = threadIdx.x & 31;
+    for (int e = from * 8 + lane; e < 128 * 8; e += 32)
+#pragma unroll
+        for (int x = 0; x < DP / 64; ++x)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + x * HALF_TILE + e * 16), "r"(0) : "memory");
+    tc::fence_async_shared();
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(full);
+    return ok;
+}
+
+// end of a block one of whose waits ran out: loads and products in flight get a bounded time to end
+// before the block's memory goes
+__device__ __forceinline__ void drain_stalled(unsigned long long *stalls)
+{
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 64; ++i) __nanosleep(100000);
+        if (stalls) atomicAdd(stalls, 1ull);
+    }
+    __syncthreads();
+}
+
+}  // namespace gs
