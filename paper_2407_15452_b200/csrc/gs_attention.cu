@@ -97,6 +97,7 @@ gs_status gs_attention_forward(const gs_attention_config *cfg, const void *d_q, 
     if ((s = pointers_ok(need, a.k_len ? 4 : 2, a.dtype)) != GS_OK) return s;
     if (!d_lse) return bad("d_lse is NULL");
     if (!writable(a.out, a.batch, a.q_len, a.q_heads)) return bad("out has a zero stride");
+    if (attn_walk_ok(a)) return attn_walk_forward(a, (cudaStream_t)stream);
     if (a.q_len > 64 && a.k_len > 0 && attn_tc_forward_ok(a)) return attn_tc_forward(a, (cudaStream_t)stream);
     return attn_simt_forward(a, (cudaStream_t)stream);
 }
@@ -128,6 +129,7 @@ gs_status gs_attention_backward(const gs_attention_config *cfg, const void *d_do
     if (!writable(a.dq, a.batch, a.q_len, a.q_heads) || !writable(a.dk, a.batch, a.k_len, a.kv_heads) ||
         !writable(a.dv, a.batch, a.k_len, a.kv_heads))
         return bad("a gradient has a zero stride");
+    if (attn_walk_ok(a)) return attn_walk_backward(a, (cudaStream_t)stream);
     if ((a.q_len > 64 || a.k_len > 64) && a.q_len > 0 && a.k_len > 0 && attn_tc_backward_ok(a))
         return attn_tc_backward(a, (cudaStream_t)stream);
     return attn_simt_backward(a, (cudaStream_t)stream);

@@ -69,6 +69,10 @@ __device__ __forceinline__ int attn_q_last(const AttnArgs &a, const AttnSeq &s, 
 gs_status attn_simt_forward(const AttnArgs &a, cudaStream_t st);
 gs_status attn_simt_backward(const AttnArgs &a, cudaStream_t st);
 
+// gs_attn_walk.cu
+bool attn_walk_ok(const AttnArgs &a);
+gs_status attn_walk_forward(const AttnArgs &a, cudaStream_t st);
+gs_status attn_walk_backward(const AttnArgs &a, cudaStream_t st);
 // gs_attn_tc.cu
 bool attn_tc_forward_ok(const AttnArgs &a);
 gs_status attn_tc_forward(const AttnArgs &a, cudaStream_t st);
