@@ -307,7 +307,7 @@ bool attn_tma_ok(const AttnTensor &t, int64_t batch, int64_t len, int64_t heads)
 }
 
 gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_t batch, int64_t len, int64_t heads,
-                          int dim)
+                          int dim, int values, int rows)
 {
     EncodeTiled fn = encoder();
     if (!fn) {
@@ -317,9 +317,10 @@ gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_
     const cuuint64_t extent[4] = {(cuuint64_t)dim, (cuuint64_t)len, (cuuint64_t)heads, (cuuint64_t)batch};
     const cuuint64_t stride[3] = {(cuuint64_t)(len > 1 ? 2 * t.sl : 256), (cuuint64_t)(heads > 1 ? 2 * t.sh : 256),
                                   (cuuint64_t)(batch > 1 ? 2 * t.sb : 256)};
-    const cuuint32_t box[4] = {64, 128, 1, 1}, step[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {(cuuint32_t)values, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
     const CUresult r = fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, t.p, extent, stride,
-                          box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          values == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : values == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         set_error("cuTensorMapEncodeTiled failed with %d", (int)r);
@@ -354,9 +355,9 @@ gs_status attn_tc_forward(const AttnArgs &a, cudaStream_t st)
     const bool bf16 = a.dtype == GS_TABLE_BF16;
     TcMaps m;
     gs_status s;
-    if ((s = attn_tensor_map(&m.q, a.q, bf16, a.batch, a.q_len, a.q_heads, a.dim)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.k, a.k, bf16, a.batch, a.k_len, a.kv_heads, a.dim)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.v, a.v, bf16, a.batch, a.k_len, a.kv_heads, a.dim)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.q, a.q, bf16, a.batch, a.q_len, a.q_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.k, a.k, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.v, a.v, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
     if (a.dim <= 64) return bf16 ? forward_t<true, 64>(a, m, st) : forward_t<false, 64>(a, m, st);
     return bf16 ? forward_t<true, 128>(a, m, st) : forward_t<false, 128>(a, m, st);
 }

@@ -669,10 +669,10 @@ gs_status attn_tc_backward(const AttnArgs &a, cudaStream_t st)
     const bool bf16 = a.dtype == GS_TABLE_BF16;
     BwdMaps m;
     gs_status s;
-    if ((s = attn_tensor_map(&m.q, a.q, bf16, a.batch, a.q_len, a.q_heads, a.dim)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.dout, a.dout, bf16, a.batch, a.q_len, a.q_heads, a.dim)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.k, a.k, bf16, a.batch, a.k_len, a.kv_heads, a.dim)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.v, a.v, bf16, a.batch, a.k_len, a.kv_heads, a.dim)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.q, a.q, bf16, a.batch, a.q_len, a.q_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.dout, a.dout, bf16, a.batch, a.q_len, a.q_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.k, a.k, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.v, a.v, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
     BwdNorms nm;
     nm.dout = a.delta + a.batch * a.q_heads * (int64_t)a.q_len;
     nm.v = nm.dout + a.batch * a.q_heads * tiles_of(a.q_len);

@@ -4,36 +4,46 @@
 // tens of thousands of walks: the bound is the traffic of q, k, v and the results.  So a unit - one head of one
 // sequence - is brought to shared memory once, whole, and everything happens there and in registers:
 // one warp per 16 rows, mma.sync m16n8k16 on 16 x 16 blocks, and only blocks that the window reaches.
-// A block takes several units, so that its rows stay contiguous in memory over the heads of a walk, and several
-// blocks share an SM, so that one's loads overlap another's arithmetic.
-//
+// The grid is as large as fits the device; a block goes through its share of the units, several at a time, and
+// TMA brings the next ones into a second set of tiles meanwhile.  Results leave through TMA too, from the
+// tiles whose rows they replace.  Tensors that TMA cannot address (odd strides or addresses) are copied by
+// the threads, and results stored by them.
 //  forward : scores of up to 64 keys at a time in registers, running maximum and sum over those
 //  backward: dq by query rows, then dk and dv by key rows, both from the same copy in shared memory.  delta =
 //            sum_j p_ij dp_ij comes from the probabilities themselves (a first walk over the row's blocks), so
 //            the forward output is neither read nor is its rounding part of the gradient.
-// Rows past a sequence's end are zeros in shared memory, never read from the tensors.
+// Rows past a sequence's end are zeros in shared memory, whatever the tensors hold there.
+// The window enters as the value that the scores' accumulators start from, 0 or -infinity: what a 16 x 16 block
+// shows depends on its distance from the diagonal only, and the few distances with a partly visible block
+// have their starting values in shared memory (a comparison and a select per score were a third of the
+// instructions, and instructions are what these kernels run out of first).
 // P and dS are rounded to the tensors' type for their products.  For binary16 they are scaled by powers
 // of two first, P by 2^14 (p <= 1), dS by the one that brings its bound |dS| <= max|dp| + |delta| below 2^15.
-#include "gs_attn.cuh"
-#include "gs_tc.cuh"
+#include "gs_attn_tc.cuh"
 
 namespace gs {
 
-using tc::exp2_fast;
-using tc::pack2;
-using tc::smem_u32;
+using namespace tc;
 
-static constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
-static constexpr int KEEP = 4;                    // blocks of 16 keys whose scores the forward pass holds
+static constexpr int KEEP = 3;                    // blocks of 16 keys whose scores the forward pass holds
 
-// byte offset of 16-byte chunk c of row r: rows of DP values, chunks permuted so that eight rows at one
-// column fall into different banks
+// A tile holds the padded rows of one head as TMA writes them: rows of DP values (of 64 values in two halves,
+// if DP is 128) whose 16-byte chunks are permuted within 8 rows, so that eight rows at one column fall
+// into different banks.
 template <int DP>
-__device__ __forceinline__ uint32_t at(int r, int c)
+struct Row {
+    static constexpr int HALVES = DP == 128 ? 2 : 1, BYTES = DP / HALVES * 2, CHUNKS = BYTES / 16;
+    static constexpr int FLIP = CHUNKS == 8 ? 0 : CHUNKS == 4 ? 1 : 2;         // row bits below the permutation
+    static constexpr uint32_t BLOCK = 16 * BYTES;                             // 16 rows of a half
+    // byte offset of chunk c of row r within a half
+    static __device__ __forceinline__ uint32_t at(int r, int c) { return r * BYTES + ((c ^ ((r >> FLIP) & (CHUNKS - 1))) << 4); }
+    static __host__ __device__ constexpr uint32_t tile(int rows16) { return HALVES * rows16 * BLOCK; }
+};
+// step k (16 values) of a row whose step 0 is at `block`; `half`: bytes of a half tile
+template <int DP>
+__device__ __forceinline__ uint32_t step_at(uint32_t block, int k, uint32_t half)
 {
-    constexpr int CH = DP / 8;                    // chunks per row
-    const int x = CH >= 8 ? (r & 7) : CH == 4 ? ((r >> 1) & 3) : ((r >> 2) & 1);
-    return (uint32_t)((r * CH + (c ^ x)) * 16);
+    return DP == 128 ? (block ^ (32 * (k & 3))) + (k >> 2) * half : block ^ (32 * k);
 }
 
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t addr)
@@ -57,40 +67,47 @@ __device__ __forceinline__ void mma(float *c, const uint32_t (&a)[4], uint32_t b
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// A fragments of rows [r0, r0 + 16)
-template <int DP>
-__device__ __forceinline__ void load_a(uint32_t (&f)[DP / 16][4], uint32_t tile, int r0)
+// A lane's offset in a block for ldmatrix.  The permutation of a row's chunks depends on the row within its 16
+// rows only, and chunk 2k + x is chunk x with bits of 2k flipped: a lane adds its offset to a block's
+// address once and takes step_at from there.
+template <int DP> __device__ __forceinline__ uint32_t lane_a() { const int l = threadIdx.x & 31; return Row<DP>::at(l & 15, l >> 4); }
+template <int DP> __device__ __forceinline__ uint32_t lane_b()
 {
-    const int lane = threadIdx.x & 31;
+    const int l = threadIdx.x & 31;
+    return Row<DP>::at((l & 7) + ((l >> 4) << 3), (l >> 3) & 1);
+}
+// lse, delta and bound of the padded query rows
+__host__ __device__ constexpr uint32_t stat_bytes(int qt) { return 3 * qt * 16 * 4; }
+
+// A fragments of 16 rows; `block` includes lane_a
+template <int DP>
+__device__ __forceinline__ void load_a(uint32_t (&f)[DP / 16][4], uint32_t block, uint32_t half)
+{
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k) ldm4(f[k], tile + at<DP>(r0 + (lane & 15), 2 * k + (lane >> 4)));
+    for (int k = 0; k < DP / 16; ++k) ldm4(f[k], step_at<DP>(block, k, half));
 }
 
-// s[16 x 16] = A B^T: rows j0..j0+15 of B are the columns.  s[0..3]: columns 0-7, s[4..7]: 8-15
+// s[16 x 16] += A B^T, the 16 rows of B are the columns; `block` includes lane_b.  s[0..3]: columns 0-7, s[4..7]: 8-15
 template <bool BF16, int DP>
-__device__ __forceinline__ void block_dot(float (&s)[8], const uint32_t (&a)[DP / 16][4], uint32_t b, int j0)
+__device__ __forceinline__ void block_dot(float (&s)[8], const uint32_t (&a)[DP / 16][4], uint32_t block, uint32_t half)
 {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s[i] = 0.f;
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k) {
         uint32_t f[4];
-        ldm4(f, b + at<DP>(j0 + (lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
+        ldm4(f, step_at<DP>(block, k, half));
         mma<BF16>(s, a[k], f[0], f[1]);
         mma<BF16>(s + 4, a[k], f[2], f[3]);
     }
 }
 
-// acc[16 x DP] += p[16 x 16] B, rows j0..j0+15 of B summed over
+// acc[16 x DP] += p[16 x 16] B, the 16 rows of B summed over; `block` includes lane_a
 template <bool BF16, int DP>
-__device__ __forceinline__ void block_mul(float (&acc)[DP / 8][4], const uint32_t (&p)[4], uint32_t b, int j0)
+__device__ __forceinline__ void block_mul(float (&acc)[DP / 8][4], const uint32_t (&p)[4], uint32_t block, uint32_t half)
 {
-    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int d = 0; d < DP / 16; ++d) {
         uint32_t f[4];
-        ldm4t(f, b + at<DP>(j0 + (lane & 15), 2 * d + (lane >> 4)));
+        ldm4t(f, step_at<DP>(block, d, half));
         mma<BF16>(acc[2 * d], p, f[0], f[1]);
         mma<BF16>(acc[2 * d + 1], p, f[2], f[3]);
     }
@@ -106,44 +123,135 @@ __device__ __forceinline__ void as_a(uint32_t (&p)[4], const float (&s)[8])
     p[3] = pack2<BF16>(s[6], s[7]);
 }
 
-// column of value i of a 16 x 16 block (rows: lane / 4 for i & 2 == 0, + 8 otherwise)
-__device__ __forceinline__ int col_of(int i) { return ((i >> 2) << 3) + 2 * (threadIdx.x & 3) + (i & 1); }
+// offset of value i's column from the thread's first one (rows: lane / 4 for i & 2 == 0, + 8 otherwise)
+__device__ __forceinline__ constexpr int step_of(int i) { return ((i >> 2) << 3) + (i & 1); }
 
-struct Lens {
+struct Unit {
     AttnSeq s;
     int64_t b;
     int h;
 };
 
-// rows [0, pad) of one head into shared memory: rows >= n and values >= dim are zeros
+__device__ __forceinline__ Unit unit_of(const AttnArgs &a, uint32_t u, uint32_t heads)
+{
+    Unit l;
+    const uint32_t b = u / heads;
+    l.b = b;
+    l.h = (int)(u - b * heads);
+    l.s = attn_seq(a, l.b);
+    return l;
+}
+
+// Blocks whose distance from the diagonal (in blocks, -7..7, column block minus row block) makes them partly
+// visible: their place among the starting values in shared memory; -1: wholly visible
+struct WalkMask {
+    signed char slot[16];
+    signed char dist[4];              // of each place
+    int n;
+    int left, right;                  // columns before and after the row's own that are visible, < 0: all
+};
+
+// bytes of the starting values: two planes of four floats per lane, for each place
+__host__ __device__ constexpr uint32_t mask_bytes(int n) { return n * 1024; }
+
+__device__ __forceinline__ void fill_masks(float *to, const WalkMask &m)
+{
+    for (int e = threadIdx.x; e < m.n * 256; e += blockDim.x) {
+        const int i = (e & 3) + ((e >> 7) & 1) * 4, lane = (e >> 2) & 31;
+        const int row = (lane >> 2) + (i & 2 ? 8 : 0), col = 2 * (lane & 3) + step_of(i);
+        const int at = 16 * m.dist[e >> 8] + col - row;
+        to[e] = (m.left < 0 || at >= -m.left) && (m.right < 0 || at <= m.right) ? 0.f : -INFINITY;
+    }
+}
+
+// starting values of the block `dist` blocks right of the diagonal.  shift != 0: rows and columns are shifted
+// against each other (queries and keys of different lengths), and the values are worked out here.
+__device__ __forceinline__ void start_scores(float (&s)[8], const WalkMask &m, uint32_t masks, int dist, int shift)
+{
+    const int lane = threadIdx.x & 31;
+    if (shift == 0) {
+        const int slot = m.slot[dist + 7];
+        if (slot >= 0) {
+            const uint32_t from = masks + slot * 1024 + lane * 16;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(s[0]), "=f"(s[1]), "=f"(s[2]), "=f"(s[3]) : "r"(from) : "memory");
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(s[4]), "=f"(s[5]), "=f"(s[6]), "=f"(s[7]) : "r"(from + 512) : "memory");
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = 0.f;
+        return;
+    }
+    const int at = 16 * dist + 2 * (lane & 3) - (lane >> 2) - shift;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int d = at + step_of(i) - (i & 2 ? 8 : 0);
+        s[i] = (m.left < 0 || d >= -m.left) && (m.right < 0 || d <= m.right) ? 0.f : -INFINITY;
+    }
+}
+
+// columns >= n of a block are not visible: keys past the sequence's end
+__device__ __forceinline__ void hide_from(float (&s)[8], int n)
+{
+    const int left = n - 2 * ((int)threadIdx.x & 3);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = step_of(i) < left ? s[i] : -INFINITY;
+}
+
+// what the launcher settles
+struct WalkPlan {
+    int units;                        // heads that a block works on at a time
+    int qt, kt;                       // 16-row tiles of the padded lengths
+    bool tma;                         // loads and stores through TMA
+    int stages;                       // sets of tiles: two if they fit (one without TMA)
+    bool vec;                         // without it: 16-byte loads and stores
+    WalkMask rows, cols;              // by query rows (columns: keys) and by key rows (columns: queries)
+};
+struct WalkMaps {                     // boxes of all rows for the inputs, of 16 rows for the results
+    CUtensorMap q, k, v, dout, out, dk, dv;
+};
+
+// one head's rows through TMA (one thread)
 template <int DP>
-__device__ __forceinline__ void load_head(uint32_t dst, const AttnTensor &t, int64_t b, int h, int n, int pad, int dim,
+__device__ __forceinline__ void tma_head(uint32_t dst, const CUtensorMap *map, uint32_t bar, int head, int64_t b, uint32_t half)
+{
+#pragma unroll
+    for (int x = 0; x < Row<DP>::HALVES; ++x) tma_load(dst + x * half, map, bar, x * 64, 0, head, (int)b);
+}
+
+// rows [0, pad) of one head by `threads` threads: rows >= n and values >= dim are zeros
+template <int DP>
+__device__ __forceinline__ void copy_head(uint32_t dst, const AttnTensor &t, int64_t b, int h, int n, int pad, int dim,
                                           bool vec, int tid, int threads)
 {
     constexpr int CH = DP / 8;
     const uint16_t *base = reinterpret_cast<const uint16_t *>(t.p) + b * t.sb + h * t.sh;
     for (int e = tid; e < pad * CH; e += threads) {
         const int r = e / CH, c = e % CH;
-        const uint32_t to = dst + at<DP>(r, c);
-        if (vec) {
-            const bool in = r < n && c * 8 < dim;
-            const uint16_t *from = in ? base + (int64_t)r * t.sl + c * 8 : base;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0) : "memory");
-        } else {
-            uint32_t u[4] = {};
-            if (r < n) {
-                const uint16_t *from = base + (int64_t)r * t.sl;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c * 8 + i < dim) u[i / 2] |= (uint32_t)from[c * 8 + i] << (16 * (i & 1));
+        const uint16_t *from = base + (int64_t)r * t.sl + c * 8;
+        uint32_t u[4] = {};
+        if (r < n && vec) {
+            if (c * 8 < dim) {
+                const uint4 w = __ldg(reinterpret_cast<const uint4 *>(from));
+                u[0] = w.x; u[1] = w.y; u[2] = w.z; u[3] = w.w;
             }
-            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
+        } else if (r < n) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c * 8 + i < dim) u[i / 2] |= (uint32_t)from[i] << (16 * (i & 1));
         }
+        const uint32_t to = dst + (c / Row<DP>::CHUNKS) * pad * Row<DP>::BYTES + Row<DP>::at(r, c % Row<DP>::CHUNKS);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
     }
 }
-__device__ __forceinline__ void loads_done()
+
+// rows [n, pad) become zeros: they take part in sums over rows, where a zero probability must not meet a NaN
+template <int DP>
+__device__ __forceinline__ void zero_rows(uint32_t tile, int n, int pad, int tid, int threads)
 {
-    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+    for (int e = n * Row<DP>::CHUNKS + tid; e < pad * Row<DP>::CHUNKS; e += threads)
+#pragma unroll
+        for (int x = 0; x < Row<DP>::HALVES; ++x)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + x * pad * Row<DP>::BYTES + e * 16), "r"(0) : "memory");
 }
 
 // the 16 x DP accumulator times its two row factors, in the tensors' type
@@ -157,38 +265,50 @@ __device__ __forceinline__ void pack_tile(uint32_t (&u)[DP / 8][2], const float 
     }
 }
 
-// this warp's 16 x DP result, as pack_tile left it, to rows [r0, r0 + 16) of a tensor: through the
-// 16 rows of `stage` in shared memory, which nobody else reads any more, for 16-byte stores.
-// Rows >= n become zeros, rows >= len are not written.
+// This warp's 16 x DP result, as pack_tile left it, to rows [r0, r0 + 16) of one head: first into the 16
+// rows at `stage` in shared memory, which nobody else reads any more, then in 16-byte pieces.
+// Rows >= n become zeros, rows >= len are not written.  TMA reads the stage until tma_stores_read.
 template <int DP>
-__device__ __forceinline__ void store_tile(const uint32_t (&u)[DP / 8][2], uint32_t stage, const AttnTensor &t,
-                                           int64_t b, int h, int r0, int n, int len, int dim, bool vec)
+__device__ __forceinline__ void store_tile(const uint32_t (&u)[DP / 8][2], uint32_t stage, uint32_t half, const WalkPlan &plan,
+                                           const CUtensorMap *map, const AttnTensor &t, int64_t b, int h, int r0, int n, int len, int dim)
 {
-    constexpr int CH = DP / 8;
+    constexpr int CH = Row<DP>::CHUNKS;
     const int lane = threadIdx.x & 31, row = lane >> 2;
     const bool in0 = r0 + row < n, in1 = r0 + row + 8 < n;
     __syncwarp();
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
+    for (int c = 0; c < DP / 8; ++c) {
         const uint32_t lo = in0 ? u[c][0] : 0u, hi = in1 ? u[c][1] : 0u;
-        asm volatile("st.shared.u32 [%0], %1;" ::"r"(stage + at<DP>(r0 + row, c) + 4 * (lane & 3)), "r"(lo) : "memory");
-        asm volatile("st.shared.u32 [%0], %1;" ::"r"(stage + at<DP>(r0 + row + 8, c) + 4 * (lane & 3)), "r"(hi) : "memory");
+        const uint32_t to = stage + (c / CH) * half + Row<DP>::at(row, c % CH) + 4 * (lane & 3);
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(lo) : "memory");
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 8 * Row<DP>::BYTES), "r"(hi) : "memory");      // row + 8: the same permutation
+    }
+    if (plan.tma) {
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) {
+#pragma unroll
+            for (int x = 0; x < Row<DP>::HALVES; ++x) tma_store(map, stage + x * half, x * 64, r0, h, (int)b);
+            tma_store_commit();
+        }
+        return;
     }
     __syncwarp();
     uint16_t *base = reinterpret_cast<uint16_t *>(t.p) + b * t.sb + h * t.sh;
-    for (int e = lane; e < 16 * CH; e += 32) {
-        const int r = r0 + e / CH, c = e % CH;
+    for (int e = lane; e < 2 * DP; e += 32) {
+        const int row = e / (DP / 8), c = e % (DP / 8), r = r0 + row;
         if (r >= len || c * 8 >= dim) continue;
-        uint4 u;
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(stage + at<DP>(r, c)) : "memory");
+        uint4 w;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                     : "r"(stage + (c / CH) * half + Row<DP>::at(row, c % CH)) : "memory");
         uint16_t *to = base + (int64_t)r * t.sl + c * 8;
-        if (vec) {
-            *reinterpret_cast<uint4 *>(to) = u;
+        if (plan.vec) {
+            *reinterpret_cast<uint4 *>(to) = w;
         } else {
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+            const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (c * 8 + i < dim) to[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+                if (c * 8 + i < dim) to[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
         }
     }
 }
@@ -204,74 +324,108 @@ __device__ __forceinline__ float quad_sum(float v)
     return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
 
-__device__ __forceinline__ Lens unit_of(const AttnArgs &a, int64_t u, int heads)
-{
-    Lens l;
-    l.b = u / heads;
-    l.h = (int)(u % heads);
-    l.s = attn_seq(a, l.b);
-    return l;
-}
+// Registers of a thread, and how many blocks of up to BLOCK_WARPS warps an SM is to hold with them.  Measured on
+// 16384 walks of 40 with 4 heads of 32 (forward) and 8192 of 80 (backward): 80 registers and 8 warps 188 us, 64
+// registers 208, 108 registers 264; backward 96 registers 448 us, 128 registers with p and dp of three blocks kept
+// for the second walk over them 465, 80 registers 523.
+template <int DP, bool BWD> constexpr int registers() { return DP <= 32 ? (BWD ? 96 : 80) : DP == 64 ? 128 : 255; }
+template <int DP, bool BWD> constexpr int blocks_per_sm() { return DP <= 32 ? (BWD ? 4 : 3) : DP == 64 ? 2 : 1; }
+static constexpr int BLOCK_WARPS = 8;             // a head of 128 rows
 
-// `units` heads per block; qt, kt: 16-row tiles of the padded lengths; one warp per (unit, query tile)
-// resident blocks of 256 threads that the register budget is set for
-template <int DP> constexpr int blocks_per_sm() { return DP <= 32 ? 3 : DP == 64 ? 2 : 1; }
-
+// one warp per (unit, query tile)
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(256, blocks_per_sm<DP>())
-attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, int units, int qt, int kt, bool vec)
+__global__ void __maxnreg__((registers<DP, false>()))
+attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ WalkPlan plan, const __grid_constant__ WalkMaps maps,
+                         unsigned long long *stalls)
 {
-    extern __shared__ uint4 smem[];
-    const uint32_t base = smem_u32(smem);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t total = a.batch * a.q_heads, u0 = (int64_t)blockIdx.x * units;
-    const uint32_t q_bytes = qt * 16 * DP * 2, k_bytes = kt * 16 * DP * 2, unit_bytes = q_bytes + 2 * k_bytes;
-    const int here = (int)min((int64_t)units, total - u0);
-    const int mine = warp / qt;                               // the unit that this warp's group of qt warps works on
-    if (mine < here) {
-        const Lens l = unit_of(a, u0 + mine, a.q_heads);
-        const uint32_t at0 = base + mine * unit_bytes;
-        const int tid = threadIdx.x - mine * qt * 32;
-        load_head<DP>(at0, a.q, l.b, l.h, l.s.nq, qt * 16, a.dim, vec, tid, qt * 32);
-        load_head<DP>(at0 + q_bytes, a.k, l.b, l.h / a.group, l.s.nk, kt * 16, a.dim, vec, tid, qt * 32);
-        load_head<DP>(at0 + q_bytes + k_bytes, a.v, l.b, l.h / a.group, l.s.nk, kt * 16, a.dim, vec, tid, qt * 32);
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ __align__(8) uint64_t full[2];
+    __shared__ volatile int stalled;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, qt = plan.qt, kt = plan.kt;
+    const uint32_t total = (uint32_t)a.batch * a.q_heads, step = gridDim.x * plan.units;
+    const uint32_t q_half = qt * Row<DP>::BLOCK, k_half = kt * Row<DP>::BLOCK;
+    const uint32_t q_bytes = Row<DP>::tile(qt), k_bytes = Row<DP>::tile(kt), unit_bytes = q_bytes + 2 * k_bytes;
+    const int mine = (int)((uint32_t)warp / (uint32_t)qt), tile = warp - mine * qt;   // qt warps work on one unit
+    const int tid = threadIdx.x - mine * qt * 32, threads = qt * 32;
+    const uint32_t bars = smem_u32(full);
+    const bool ragged = a.k_lens != nullptr && plan.tma;
+    auto tiles_at = [&](int st) { return smem_u32(smem) + (st * plan.units + mine) * unit_bytes; };
+    uint8_t *masks = smem + plan.stages * plan.units * unit_bytes;
+    const uint32_t mask_rows = smem_u32(masks);
+    fill_masks(reinterpret_cast<float *>(masks), plan.rows);
+    auto load = [&](uint32_t u, int st) {              // the unit's first thread
+        const uint32_t bar = bars + 8 * st, Q = tiles_at(st);
+        if (u >= total) {
+            bar_arrive(bar);
+            return;
+        }
+        const uint32_t b = u / (uint32_t)a.q_heads;
+        const int h = (int)(u - b * a.q_heads), g = h / a.group;
+        bar_expect(bar, unit_bytes);
+        tma_head<DP>(Q, &maps.q, bar, h, b, q_half);
+        tma_head<DP>(Q + q_bytes, &maps.k, bar, g, b, k_half);
+        tma_head<DP>(Q + q_bytes + k_bytes, &maps.v, bar, g, b, k_half);
+    };
+    if (threadIdx.x == 0) {
+        stalled = 0;
+        bar_init(bars, plan.units);
+        bar_init(bars + 8, plan.units);
+        fence_barrier_init();
     }
-    loads_done();
     __syncthreads();
-    if (mine >= here) return;
-    const Lens l = unit_of(a, u0 + mine, a.q_heads);
-    const uint32_t Q = base + mine * unit_bytes, K = Q + q_bytes, V = K + k_bytes;
-    const int r0 = (warp % qt) * 16, ra = r0 + (lane >> 2), rb = ra + 8;
-    const int lo_a = attn_lo(a, l.s, ra), hi_a = attn_hi(a, l.s, ra), lo_b = attn_lo(a, l.s, rb), hi_b = attn_hi(a, l.s, rb);
+    uint32_t u = blockIdx.x * plan.units + mine;
+    if (plan.tma && tid == 0) {
+        load(u, 0);
+        if (plan.stages == 2) load(u + step, 1);
+    }
+    const float mul = a.scale * LOG2E;
+    for (uint32_t u0 = blockIdx.x * plan.units, n = 0; u0 < total; u0 += step, u += step, ++n) {
+    const int st = n & (plan.stages - 1);
+    const bool active = u < total;
+    const Unit l = unit_of(a, active ? u : u0, a.q_heads);
+    const uint32_t Q = tiles_at(st), K = Q + q_bytes, V = K + k_bytes;
+    bool ok = true;
+    if (plan.tma) {
+        ok = bar_wait(bars + 8 * st, (n >> (plan.stages - 1)) & 1, &stalled);
+    } else if (active) {
+        const int g = l.h / a.group;
+        copy_head<DP>(Q, a.q, l.b, l.h, l.s.nq, qt * 16, a.dim, plan.vec, tid, threads);
+        copy_head<DP>(K, a.k, l.b, g, l.s.nk, kt * 16, a.dim, plan.vec, tid, threads);
+        copy_head<DP>(V, a.v, l.b, g, l.s.nk, kt * 16, a.dim, plan.vec, tid, threads);
+    }
+    if (ragged && ok && l.s.nk < a.k_len) zero_rows<DP>(V, l.s.nk, kt * 16, tid, threads);
+    if (!__syncthreads_and(ok)) break;
+    if (active) {
+    const int r0 = tile * 16, ra = r0 + (lane >> 2), rb = ra + 8;
     float acc[DP / 8][4] = {};
-    float top_a = -INFINITY, top_b = -INFINITY, sum_a = 0.f, sum_b = 0.f;
+    float top_a = -INFINITY, top_b = -INFINITY, sum_a = 0.f, sum_b = 0.f;     // top: largest score, not yet scaled
     const int r_end = min(r0 + 16, l.s.nq);
     const int j_begin = attn_lo(a, l.s, r0) / 16, j_end = r_end > r0 ? (attn_hi(a, l.s, r_end - 1) + 15) / 16 : 0;
-    const float mul = a.scale * LOG2E;
     if (j_begin < j_end) {
         uint32_t qf[DP / 16][4];
-        load_a<DP>(qf, Q, r0);
+        load_a<DP>(qf, Q + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half);
+        const uint32_t kb = K + lane_b<DP>(), vb = V + lane_a<DP>();
         for (int j = j_begin; j < j_end; j += KEEP) {
             float s[KEEP][8];
             float m_a = top_a, m_b = top_b;
 #pragma unroll
             for (int x = 0; x < KEEP; ++x) {
                 if (j + x >= j_end) break;
-                block_dot<BF16, DP>(s[x], qf, K, (j + x) * 16);
+                start_scores(s[x], plan.rows, mask_rows, j + x - tile, l.s.off);
+                block_dot<BF16, DP>(s[x], qf, kb + (j + x) * Row<DP>::BLOCK, k_half);
+                if ((j + x + 1) * 16 > l.s.nk) hide_from(s[x], l.s.nk - (j + x) * 16);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int c = (j + x) * 16 + col_of(i);
-                    const bool in = i & 2 ? (c >= lo_b && c < hi_b) : (c >= lo_a && c < hi_a);
-                    s[x][i] = in ? s[x][i] * mul : -INFINITY;
                     if (i & 2) m_b = fmaxf(m_b, s[x][i]);
                     else m_a = fmaxf(m_a, s[x][i]);
                 }
             }
             m_a = quad_max(m_a);
             m_b = quad_max(m_b);
-            const float base_a = m_a == -INFINITY ? 0.f : m_a, base_b = m_b == -INFINITY ? 0.f : m_b;
+            // nothing visible yet: every term is exp2(-inf) = 0
+            const float base_a = m_a == -INFINITY ? 0.f : m_a * mul, base_b = m_b == -INFINITY ? 0.f : m_b * mul;
             if (j > j_begin) {
-                const float keep_a = exp2_fast(top_a - base_a), keep_b = exp2_fast(top_b - base_b);
+                const float keep_a = exp2_fast(top_a * mul - base_a), keep_b = exp2_fast(top_b * mul - base_b);
                 sum_a *= keep_a;
                 sum_b *= keep_b;
 #pragma unroll
@@ -289,13 +443,13 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, int units, int qt, 
                 if (j + x >= j_end) break;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    s[x][i] = exp2_fast(s[x][i] - (i & 2 ? base_b : base_a));
+                    s[x][i] = exp2_fast(fmaf(s[x][i], mul, i & 2 ? -base_b : -base_a));
                     if (i & 2) sum_b += s[x][i];
                     else sum_a += s[x][i];
                 }
                 uint32_t p[4];
                 as_a<BF16>(p, s[x]);
-                block_mul<BF16, DP>(acc, p, V, (j + x) * 16);
+                block_mul<BF16, DP>(acc, p, vb + (j + x) * Row<DP>::BLOCK, k_half);
             }
         }
     }
@@ -303,12 +457,21 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, int units, int qt, 
     sum_b = quad_sum(sum_b);
     if ((lane & 3) == 0) {
         float *lse = a.lse + (l.b * a.q_heads + l.h) * a.q_len;
-        if (ra < a.q_len) lse[ra] = sum_a == 0.f ? -INFINITY : (top_a + log2f(sum_a)) * LN2;
-        if (rb < a.q_len) lse[rb] = sum_b == 0.f ? -INFINITY : (top_b + log2f(sum_b)) * LN2;
+        if (ra < a.q_len) lse[ra] = sum_a == 0.f || ra >= l.s.nq ? -INFINITY : (top_a * mul + log2_fast(sum_a)) * LN2;
+        if (rb < a.q_len) lse[rb] = sum_b == 0.f || rb >= l.s.nq ? -INFINITY : (top_b * mul + log2_fast(sum_b)) * LN2;
     }
     uint32_t out[DP / 8][2];
-    pack_tile<BF16, DP>(out, acc, sum_a == 0.f ? 0.f : 1.f / sum_a, sum_b == 0.f ? 0.f : 1.f / sum_b);
-    store_tile<DP>(out, Q, a.out, l.b, l.h, r0, l.s.nq, a.q_len, a.dim, vec);
+    pack_tile<BF16, DP>(out, acc, sum_a == 0.f ? 0.f : rcp_fast(sum_a), sum_b == 0.f ? 0.f : rcp_fast(sum_b));
+    store_tile<DP>(out, Q + tile * Row<DP>::BLOCK, q_half, plan, &maps.out, a.out, l.b, l.h, r0, l.s.nq, a.q_len, a.dim);
+    }
+    if (plan.tma) {
+        if (lane == 0) tma_stores_read();
+        if (ragged) fence_async_shared();               // zeroed rows, before TMA writes there again
+    }
+    __syncthreads();                                    // everybody is done with this set of tiles
+    if (plan.tma && tid == 0 && u0 + plan.stages * step < total) load(u + plan.stages * step, st);
+    }
+    if (stalled) drain_stalled(stalls);
 }
 
 // power of two that brings a bound below 2^15 (binary16 only)
@@ -320,113 +483,173 @@ __device__ __forceinline__ float lift(float bound)
     return __uint_as_float((uint32_t)(min(max(15 - e, -100), 100) + 127) << 23);
 }
 
-// `units` key/value heads per block, `tiles` = max(qt, kt) warps per unit
-// SHARED: several query heads per key/value head
+// `tiles` = max(qt, kt) warps per unit; a unit is a key/value head, gone through once per query head of its group.
+// SHARED: several query heads per key/value head.
 template <bool BF16, int DP, bool SHARED>
-__global__ void __launch_bounds__(256, blocks_per_sm<DP>())
-attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, int units, int qt, int kt, bool vec)
+__global__ void __maxnreg__((registers<DP, true>()))
+attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ WalkPlan plan, const __grid_constant__ WalkMaps maps,
+                          unsigned long long *stalls)
 {
-    extern __shared__ uint4 smem[];
-    const uint32_t base = smem_u32(smem);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tiles = max(qt, kt);
-    const int64_t total = a.batch * a.kv_heads, u0 = (int64_t)blockIdx.x * units;
-    const uint32_t q_bytes = qt * 16 * DP * 2, k_bytes = kt * 16 * DP * 2;
-    const uint32_t unit_bytes = 2 * q_bytes + 2 * k_bytes + 3 * qt * 16 * 4;
-    const int here = (int)min((int64_t)units, total - u0);
-    const int mine = warp / tiles, tile = warp % tiles, tid = threadIdx.x - mine * tiles * 32;
-    const bool active = mine < here;
-    const Lens l = unit_of(a, u0 + (active ? mine : 0), a.kv_heads);
-    const AttnSeq s = l.s;
-    const uint32_t Q = base + mine * unit_bytes, DO = Q + q_bytes, K = DO + q_bytes, V = K + k_bytes;
-    // per query row: lse in units of log2, delta, bound of |dS|
-    float *lse2 = reinterpret_cast<float *>(reinterpret_cast<char *>(smem) + mine * unit_bytes + 2 * q_bytes + 2 * k_bytes);
-    float *delta = lse2 + qt * 16, *bound = delta + qt * 16;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ __align__(8) uint64_t full[2];
+    __shared__ volatile int stalled;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, qt = plan.qt, kt = plan.kt, tiles = max(qt, kt);
+    const uint32_t total = (uint32_t)a.batch * a.kv_heads, step = gridDim.x * plan.units;
+    const uint32_t q_half = qt * Row<DP>::BLOCK, k_half = kt * Row<DP>::BLOCK;
+    const uint32_t q_bytes = Row<DP>::tile(qt), k_bytes = Row<DP>::tile(kt), unit_bytes = 2 * q_bytes + 2 * k_bytes;
+    const int mine = (int)((uint32_t)warp / (uint32_t)tiles), tile = warp - mine * tiles;
+    const int tid = threadIdx.x - mine * tiles * 32, threads = tiles * 32;
+    const uint32_t bars = smem_u32(full);
+    const bool ragged = (a.q_lens != nullptr || a.k_lens != nullptr) && plan.tma;
+    const int group = SHARED ? a.group : 1;
+    // per query row: -lse in units of log2, -delta, bound of |dS|
+    float *neg_lse = reinterpret_cast<float *>(smem + plan.stages * plan.units * unit_bytes + mine * stat_bytes(qt));
+    float *neg_delta = neg_lse + qt * 16, *bound = neg_delta + qt * 16;
+    uint8_t *masks = smem + plan.units * (plan.stages * unit_bytes + stat_bytes(qt));
+    const uint32_t mask_rows = smem_u32(masks), mask_cols = mask_rows + mask_bytes(plan.rows.n);
+    fill_masks(reinterpret_cast<float *>(masks), plan.rows);
+    fill_masks(reinterpret_cast<float *>(masks + mask_bytes(plan.rows.n)), plan.cols);
+    auto tiles_at = [&](int st) { return smem_u32(smem) + (st * plan.units + mine) * unit_bytes; };
+    auto load = [&](uint32_t u, int x, int st) {       // the unit's first thread; x: query head of the group
+        const uint32_t bar = bars + 8 * st, Q = tiles_at(st);
+        if (u >= total) {
+            bar_arrive(bar);
+            return;
+        }
+        const uint32_t b = u / (uint32_t)a.kv_heads;
+        const int g = (int)(u - b * a.kv_heads), h = g * group + x;
+        bar_expect(bar, unit_bytes);
+        tma_head<DP>(Q, &maps.q, bar, h, b, q_half);
+        tma_head<DP>(Q + q_bytes, &maps.dout, bar, h, b, q_half);
+        tma_head<DP>(Q + 2 * q_bytes, &maps.k, bar, g, b, k_half);
+        tma_head<DP>(Q + 2 * q_bytes + k_bytes, &maps.v, bar, g, b, k_half);
+    };
+    if (threadIdx.x == 0) {
+        stalled = 0;
+        bar_init(bars, plan.units);
+        bar_init(bars + 8, plan.units);
+        fence_barrier_init();
+    }
+    __syncthreads();
+    uint32_t u = blockIdx.x * plan.units + mine;
+    if (plan.tma && tid == 0) {
+        load(u, 0, 0);
+        if (plan.stages == 2) {
+            if (group > 1) load(u, 1, 1);
+            else load(u + step, 0, 1);
+        }
+    }
     const float mul = a.scale * LOG2E;
+    bool ok = true;
+    uint32_t n = 0;
+    for (uint32_t u0 = blockIdx.x * plan.units; u0 < total && ok; u0 += step, u += step) {
+    const bool active = u < total;
+    const Unit l = unit_of(a, active ? u : u0, a.kv_heads);
+    const AttnSeq s = l.s;
     float dk[DP / 8][4] = {}, dv[DP / 8][4] = {};
     float up_k = 1.f;
-
-    const int group = SHARED ? a.group : 1;
-    for (int x = 0; x < group; ++x) {
+    for (int x = 0; x < group; ++x, ++n) {
+        const int st = n & (plan.stages - 1);
         const int h = l.h * group + x;
-        if (x > 0) __syncthreads();
-        if (active) {
-            load_head<DP>(Q, a.q, l.b, h, s.nq, qt * 16, a.dim, vec, tid, tiles * 32);
-            load_head<DP>(DO, a.dout, l.b, h, s.nq, qt * 16, a.dim, vec, tid, tiles * 32);
-            if (x == 0) {
-                load_head<DP>(K, a.k, l.b, l.h, s.nk, kt * 16, a.dim, vec, tid, tiles * 32);
-                load_head<DP>(V, a.v, l.b, l.h, s.nk, kt * 16, a.dim, vec, tid, tiles * 32);
-            }
-            const float *lse = a.lse + (l.b * a.q_heads + h) * a.q_len;
-            for (int r = tid; r < qt * 16; r += tiles * 32) {
-                const float v = r < s.nq ? lse[r] * LOG2E : -INFINITY;
-                lse2[r] = v == -INFINITY ? INFINITY : v;      // p = 0 in rows that see nothing
-            }
+        const uint32_t Q = tiles_at(st), DO = Q + q_bytes, K = DO + q_bytes, V = K + k_bytes;
+        const float *lse = a.lse + (l.b * a.q_heads + h) * a.q_len;
+        for (int r = tid; r < qt * 16; r += threads) {
+            const float v = r < s.nq ? -lse[r] * LOG2E : -INFINITY;
+            neg_lse[r] = v == INFINITY ? -INFINITY : v;       // p = 0 in rows that see nothing
         }
-        loads_done();
-        __syncthreads();
+        if (plan.tma) {
+            ok = bar_wait(bars + 8 * st, (n >> (plan.stages - 1)) & 1, &stalled);
+        } else if (active) {
+            copy_head<DP>(Q, a.q, l.b, h, s.nq, qt * 16, a.dim, plan.vec, tid, threads);
+            copy_head<DP>(DO, a.dout, l.b, h, s.nq, qt * 16, a.dim, plan.vec, tid, threads);
+            copy_head<DP>(K, a.k, l.b, l.h, s.nk, kt * 16, a.dim, plan.vec, tid, threads);
+            copy_head<DP>(V, a.v, l.b, l.h, s.nk, kt * 16, a.dim, plan.vec, tid, threads);
+        }
+        if (ragged && ok && s.nq < a.q_len) {
+            zero_rows<DP>(Q, s.nq, qt * 16, tid, threads);
+            zero_rows<DP>(DO, s.nq, qt * 16, tid, threads);
+        }
+        if (ragged && ok && s.nk < a.k_len) {
+            zero_rows<DP>(K, s.nk, kt * 16, tid, threads);
+            zero_rows<DP>(V, s.nk, kt * 16, tid, threads);
+        }
+        ok = __syncthreads_and(ok);
+        if (!ok) break;
 
         // ---- dq of 16 query rows
         uint32_t dq[DP / 8][2] = {};
-        const int r0 = tile * 16, ra = r0 + (lane >> 2), rb = ra + 8;
+        const int r0 = tile * 16;
         if (active && tile < qt) {
-            const int lo_a = attn_lo(a, s, ra), hi_a = attn_hi(a, s, ra), lo_b = attn_lo(a, s, rb), hi_b = attn_hi(a, s, rb);
+            const int ra = r0 + (lane >> 2), rb = ra + 8;
             const int r_end = min(r0 + 16, s.nq);
             const int j_begin = attn_lo(a, s, r0) / 16, j_end = r_end > r0 ? (attn_hi(a, s, r_end - 1) + 15) / 16 : 0;
-            const float l_a = lse2[ra], l_b = lse2[rb];
+            const float l_a = neg_lse[ra], l_b = neg_lse[rb];
             uint32_t qf[DP / 16][4], df[DP / 16][4];
-            load_a<DP>(qf, Q, r0);
-            load_a<DP>(df, DO, r0);
+            load_a<DP>(qf, Q + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half);
+            load_a<DP>(df, DO + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half);
+            const uint32_t lb = lane_b<DP>(), kb = K + lane_a<DP>();
             float d_a = 0.f, d_b = 0.f, m_a = 0.f, m_b = 0.f;
+            // p and dp of one block
             auto scores = [&](int j, float (&p)[8], float (&dp)[8]) {
-                block_dot<BF16, DP>(p, qf, K, j * 16);
-                block_dot<BF16, DP>(dp, df, V, j * 16);
+                start_scores(p, plan.rows, mask_rows, j - tile, s.off);
+                block_dot<BF16, DP>(p, qf, K + lb + j * Row<DP>::BLOCK, k_half);
+                if ((j + 1) * 16 > s.nk) hide_from(p, s.nk - j * 16);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int c = j * 16 + col_of(i);
-                    const bool in = i & 2 ? (c >= lo_b && c < hi_b) : (c >= lo_a && c < hi_a);
-                    p[i] = in ? exp2_fast(fmaf(p[i], mul, -(i & 2 ? l_b : l_a))) : 0.f;
-                    dp[i] = in ? dp[i] : 0.f;
-                }
+                for (int i = 0; i < 8; ++i) dp[i] = 0.f;
+                block_dot<BF16, DP>(dp, df, V + lb + j * Row<DP>::BLOCK, k_half);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] = exp2_fast(fmaf(p[i], mul, i & 2 ? l_b : l_a));
             };
-            for (int j = j_begin; j < j_end; ++j) {
-                float p[8], dp[8];
-                scores(j, p, dp);
+            auto take = [&](const float (&p)[8], const float (&dp)[8]) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     if (i & 2) {
                         d_b = fmaf(p[i], dp[i], d_b);
-                        m_b = fmaxf(m_b, fabsf(dp[i]));
+                        if constexpr (!BF16) m_b = fmaxf(m_b, fabsf(dp[i]));
                     } else {
                         d_a = fmaf(p[i], dp[i], d_a);
-                        m_a = fmaxf(m_a, fabsf(dp[i]));
+                        if constexpr (!BF16) m_a = fmaxf(m_a, fabsf(dp[i]));
                     }
                 }
-            }
-            d_a = quad_sum(d_a);
-            d_b = quad_sum(d_b);
-            if constexpr (!BF16) {
-                m_a = quad_max(m_a) + fabsf(d_a);
-                m_b = quad_max(m_b) + fabsf(d_b);
-            }
-            if ((lane & 3) == 0) {
-                delta[ra] = d_a;
-                delta[rb] = d_b;
-                bound[ra] = m_a;
-                bound[rb] = m_b;
-            }
-            const float up_a = lift<BF16>(m_a), up_b = lift<BF16>(m_b);
-            float acc[DP / 8][4] = {};
-            for (int j = j_begin; j < j_end; ++j) {
-                float p[8], dp[8];
-                scores(j, p, dp);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    p[i] *= dp[i] - (i & 2 ? d_b : d_a);
-                    if constexpr (!BF16) p[i] *= i & 2 ? up_b : up_a;
+            };
+            float up_a = 1.f, up_b = 1.f;
+            auto rows_known = [&] {
+                d_a = quad_sum(d_a);
+                d_b = quad_sum(d_b);
+                if constexpr (!BF16) {
+                    m_a = quad_max(m_a) + fabsf(d_a);
+                    m_b = quad_max(m_b) + fabsf(d_b);
+                    up_a = lift<BF16>(m_a);
+                    up_b = lift<BF16>(m_b);
                 }
+                if ((lane & 3) == 0) {
+                    neg_delta[ra] = -d_a;
+                    neg_delta[rb] = -d_b;
+                    if constexpr (!BF16) {
+                        bound[ra] = m_a;
+                        bound[rb] = m_b;
+                    }
+                }
+            };
+            float acc[DP / 8][4] = {}, nd_a = 0.f, nd_b = 0.f;                // nd: -delta, scaled
+            auto add = [&](int j, float (&p)[8], const float (&dp)[8]) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] *= BF16 ? dp[i] - (i & 2 ? d_b : d_a) : fmaf(dp[i], i & 2 ? up_b : up_a, i & 2 ? nd_b : nd_a);
                 uint32_t w[4];
                 as_a<BF16>(w, p);
-                block_mul<BF16, DP>(acc, w, K, j * 16);
+                block_mul<BF16, DP>(acc, w, kb + j * Row<DP>::BLOCK, k_half);
+            };
+            float p[8], dp[8];
+            for (int j = j_begin; j < j_end; ++j) {
+                scores(j, p, dp);
+                take(p, dp);
+            }
+            rows_known();
+            nd_a = -d_a * up_a;
+            nd_b = -d_b * up_b;
+            for (int j = j_begin; j < j_end; ++j) {
+                scores(j, p, dp);
+                add(j, p, dp);
             }
             pack_tile<BF16, DP>(dq, acc, a.scale / up_a, a.scale / up_b);
         }
@@ -434,18 +657,16 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, int units, int qt,
 
         // ---- dk, dv of 16 key rows
         if (active && tile < kt) {
-            const int j0 = tile * 16, ja = j0 + (lane >> 2), jb = ja + 8;
-            const int lo_a = attn_q_first(a, s, ja), hi_a = ja < s.nk ? attn_q_last(a, s, ja + 1) : 0;
-            const int lo_b = attn_q_first(a, s, jb), hi_b = jb < s.nk ? attn_q_last(a, s, jb + 1) : 0;
+            const int j0 = tile * 16;
             const int j_end = min(j0 + 16, s.nk);
             const int q_begin = attn_q_first(a, s, j0) / 16, q_end = j_end > j0 ? (attn_q_last(a, s, j_end) + 15) / 16 : 0;
-            float up = 1.f;
+            float up_p = 1.f;                                 // of dp - delta, beside a p that is scaled itself
             if constexpr (!BF16) {                           // one scale per head: dk sums over its queries
                 float m = 0.f;
                 for (int r = lane; r < qt * 16; r += 32) m = fmaxf(m, bound[r]);
 #pragma unroll
                 for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                up = lift<BF16>(m);
+                const float up = lift<BF16>(m);
                 // a shared head's sums are carried from one query head's scale to the next one's
                 if (x > 0 && up != up_k) {
 #pragma unroll
@@ -454,52 +675,70 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, int units, int qt,
                         for (int i = 0; i < 4; ++i) dk[d][i] *= up / up_k;
                 }
                 up_k = up;
+                up_p = up / 16384.f;
             }
             if (q_begin < q_end) {
                 uint32_t kf[DP / 16][4], vf[DP / 16][4];
-                load_a<DP>(kf, K, j0);
-                load_a<DP>(vf, V, j0);
+                load_a<DP>(kf, K + tile * Row<DP>::BLOCK + lane_a<DP>(), k_half);
+                load_a<DP>(vf, V + tile * Row<DP>::BLOCK + lane_a<DP>(), k_half);
+                const uint32_t lb = lane_b<DP>(), la = lane_a<DP>();
                 for (int q = q_begin; q < q_end; ++q) {
+                    const uint32_t qb = Q + q * Row<DP>::BLOCK, ob = DO + q * Row<DP>::BLOCK;
                     float p[8], dp[8];
-                    block_dot<BF16, DP>(p, kf, Q, q * 16);
-                    block_dot<BF16, DP>(dp, vf, DO, q * 16);
-                    const int c0 = q * 16 + 2 * (lane & 3);
+                    // queries past the end: their lse makes p zero
+                    start_scores(p, plan.cols, mask_cols, q - tile, -s.off);
+                    block_dot<BF16, DP>(p, kf, qb + lb, q_half);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dp[i] = 0.f;
+                    block_dot<BF16, DP>(dp, vf, ob + lb, q_half);
+                    const int c = q * 16 + 2 * (lane & 3);
 #pragma unroll
                     for (int n = 0; n < 2; ++n) {
-                        const float2 ls = *reinterpret_cast<const float2 *>(lse2 + c0 + 8 * n);
-                        const float2 de = *reinterpret_cast<const float2 *>(delta + c0 + 8 * n);
+                        float2 nl = *reinterpret_cast<const float2 *>(neg_lse + c + 8 * n);
+                        float2 nd = *reinterpret_cast<const float2 *>(neg_delta + c + 8 * n);
+                        if constexpr (!BF16) {                // p by 2^14, ds by up
+                            nl.x += 14.f;
+                            nl.y += 14.f;
+                            nd.x *= up_p;
+                            nd.y *= up_p;
+                        }
 #pragma unroll
                         for (int i = 4 * n; i < 4 * n + 4; ++i) {
-                            const int c = c0 + 8 * n + (i & 1);
-                            const bool in = i & 2 ? (c >= lo_b && c < hi_b) : (c >= lo_a && c < hi_a);
-                            p[i] = in ? exp2_fast(fmaf(p[i], mul, -(i & 1 ? ls.y : ls.x))) : 0.f;
-                            dp[i] = in ? p[i] * (dp[i] - (i & 1 ? de.y : de.x)) : 0.f;
-                            if constexpr (!BF16) {
-                                dp[i] *= up;
-                                p[i] *= 16384.f;
-                            }
+                            p[i] = exp2_fast(fmaf(p[i], mul, i & 1 ? nl.y : nl.x));
+                            dp[i] = p[i] * (BF16 ? dp[i] + (i & 1 ? nd.y : nd.x) : fmaf(dp[i], up_p, i & 1 ? nd.y : nd.x));
                         }
                     }
                     uint32_t w[4];
                     as_a<BF16>(w, p);
-                    block_mul<BF16, DP>(dv, w, DO, q * 16);
+                    block_mul<BF16, DP>(dv, w, ob + la, q_half);
                     as_a<BF16>(w, dp);
-                    block_mul<BF16, DP>(dk, w, Q, q * 16);
+                    block_mul<BF16, DP>(dk, w, qb + la, q_half);
                 }
             }
         }
-        __syncthreads();                                     // nobody reads Q, dO (and K, V after the last head) any more
+        __syncthreads();                                      // nobody reads this set of tiles any more
         if (active && tile < qt)
-            store_tile<DP>(dq, Q, a.dq, l.b, h, r0, s.nq, a.q_len, a.dim, vec);
+            store_tile<DP>(dq, Q + tile * Row<DP>::BLOCK, q_half, plan, &maps.out, a.dq, l.b, h, r0, s.nq, a.q_len, a.dim);
+        if (active && tile < kt && x == group - 1) {
+            const float f = a.scale / up_k, g = BF16 ? 1.f : 1.f / 16384.f;
+            uint32_t w[DP / 8][2];
+            pack_tile<BF16, DP>(w, dk, f, f);
+            store_tile<DP>(w, K + tile * Row<DP>::BLOCK, k_half, plan, &maps.dk, a.dk, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
+            pack_tile<BF16, DP>(w, dv, g, g);
+            store_tile<DP>(w, V + tile * Row<DP>::BLOCK, k_half, plan, &maps.dv, a.dv, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
+        }
+        if (plan.tma) {
+            if (lane == 0) tma_stores_read();
+            if (ragged) fence_async_shared();                 // zeroed rows, before TMA writes there again
+        }
+        __syncthreads();
+        if (plan.tma && tid == 0) {                           // the step that uses these tiles next
+            const int ahead = (x + plan.stages) / group, x2 = (x + plan.stages) % group;
+            if (u0 + ahead * step < total) load(u + ahead * step, x2, st);
+        }
     }
-    if (active && tile < kt) {
-        const float f = a.scale / up_k, g = BF16 ? 1.f : 1.f / 16384.f;
-        uint32_t u[DP / 8][2];
-        pack_tile<BF16, DP>(u, dk, f, f);
-        store_tile<DP>(u, K, a.dk, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim, vec);
-        pack_tile<BF16, DP>(u, dv, g, g);
-        store_tile<DP>(u, V, a.dv, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim, vec);
     }
+    if (stalled) drain_stalled(stalls);
 }
 
 // 16-byte accesses need every row of every tensor aligned to eight values
@@ -511,26 +750,86 @@ static bool rows_of_eight(const AttnArgs &a, bool backward)
     return v && ok(a.out);
 }
 
+static bool all_tma(const AttnArgs &a, bool backward)
+{
+    auto on_q = [&](const AttnTensor &t) { return attn_tma_ok(t, a.batch, a.q_len, a.q_heads); };
+    auto on_k = [&](const AttnTensor &t) { return attn_tma_ok(t, a.batch, a.k_len, a.kv_heads); };
+    const bool v = a.dim % 8 == 0 && on_q(a.q) && on_k(a.k) && on_k(a.v);
+    if (backward) return v && on_q(a.dout) && on_q(a.dq) && on_k(a.dk) && on_k(a.dv);
+    return v && on_q(a.out);
+}
+
+static WalkMask mask_of(int left, int right)
+{
+    WalkMask m = {};
+    m.left = left;
+    m.right = right;
+    for (int d = -7; d <= 7; ++d) {
+        const int lo = 16 * d - 15, hi = 16 * d + 15;        // distances of the block's corners from the diagonal
+        const bool whole = (left < 0 || lo >= -left) && (right < 0 || hi <= right);
+        const bool some = (left < 0 || hi >= -left) && (right < 0 || lo <= right);
+        m.slot[d + 7] = -1;
+        if (some && !whole) {                                // at most two such blocks at each end of the window
+            m.slot[d + 7] = (signed char)m.n;
+            m.dist[m.n++] = (signed char)d;
+        }
+    }
+    return m;
+}
+
 template <bool BF16, int DP, bool BWD>
 static gs_status launch(const AttnArgs &a, cudaStream_t st)
 {
-    const int qt = (a.q_len + 15) / 16, kt = (a.k_len + 15) / 16, tiles = BWD ? (qt > kt ? qt : kt) : qt;
+    WalkPlan plan;
+    plan.rows = mask_of(a.left, a.right);
+    plan.cols = mask_of(a.right, a.left);
+    plan.qt = (a.q_len + 15) / 16;
+    plan.kt = (a.k_len + 15) / 16;
+    plan.tma = all_tma(a, BWD);
+    plan.vec = rows_of_eight(a, BWD);
+    const int tiles = BWD && plan.kt > plan.qt ? plan.kt : plan.qt;
     const int64_t total = a.batch * (BWD ? a.kv_heads : a.q_heads);
-    const int unit_bytes = (BWD ? 2 : 1) * qt * 16 * DP * 2 + 2 * kt * 16 * DP * 2 + (BWD ? 3 * qt * 16 * 4 : 0);
-    int units = 8 / tiles;                                    // eight warps a block, or one unit
-    while (units > 1 && units * unit_bytes > 48 * 1024) --units;
-    if (units < 1) units = 1;
-    const int64_t blocks = (total + units - 1) / units;
-    if (blocks == 0) return GS_OK;
-    if (blocks > 0x7FFFFFFF) {
-        set_error("attention of %lld blocks exceeds one launch", (long long)blocks);
+    if (total == 0) return GS_OK;
+    if (total > 0x3FFFFFFF) {
+        set_error("attention of %lld sequence heads exceeds one launch", (long long)total);
         return GS_ERR_UNSUPPORTED;
     }
+    WalkMaps m;
+    if (plan.tma) {
+        constexpr int BOX = DP < 64 ? DP : 64;
+        auto on_q = [&](CUtensorMap *t, const AttnTensor &x, int rows) {
+            return attn_tensor_map(t, x, BF16, a.batch, a.q_len, a.q_heads, a.dim, BOX, rows);
+        };
+        auto on_k = [&](CUtensorMap *t, const AttnTensor &x, int rows) {
+            return attn_tensor_map(t, x, BF16, a.batch, a.k_len, a.kv_heads, a.dim, BOX, rows);
+        };
+        gs_status s;
+        if ((s = on_q(&m.q, a.q, plan.qt * 16)) != GS_OK || (s = on_k(&m.k, a.k, plan.kt * 16)) != GS_OK ||
+            (s = on_k(&m.v, a.v, plan.kt * 16)) != GS_OK || (s = on_q(&m.out, BWD ? a.dq : a.out, 16)) != GS_OK)
+            return s;
+        if (BWD && ((s = on_q(&m.dout, a.dout, plan.qt * 16)) != GS_OK || (s = on_k(&m.dk, a.dk, 16)) != GS_OK ||
+                    (s = on_k(&m.dv, a.dv, 16)) != GS_OK))
+            return s;
+    }
+    const int unit = (BWD ? 2 : 1) * (int)Row<DP>::tile(plan.qt) + 2 * (int)Row<DP>::tile(plan.kt);
+    const int stats = BWD ? (int)stat_bytes(plan.qt) : 0;
+    const int masks = (int)(mask_bytes(plan.rows.n) + (BWD ? mask_bytes(plan.cols.n) : 0));
+    plan.stages = plan.tma && 2 * unit + stats + masks <= 226 * 1024 ? 2 : 1;
+    const int per_unit = plan.stages * unit + stats;
+    // as many units as the block's warps allow and as leave room for the resident blocks
+    const int room = (227 * 1024) / blocks_per_sm<DP, BWD>() - 2048;
+    plan.units = BLOCK_WARPS / tiles;
+    while (plan.units > 1 && plan.units * per_unit + masks > room) --plan.units;
+    if (plan.units < 1) plan.units = 1;
+    const int smem = plan.units * per_unit + masks;
     auto kernel = !BWD ? attn_walk_forward_kernel<BF16, DP>
                        : a.group > 1 ? attn_walk_backward_kernel<BF16, DP, true> : attn_walk_backward_kernel<BF16, DP, false>;
-    const int smem = units * unit_bytes;
     GS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    kernel<<<(unsigned)blocks, units * tiles * 32, smem, st>>>(a, units, qt, kt, rows_of_eight(a, BWD));
+    const int threads = plan.units * tiles * 32;
+    int resident = 0;
+    GS_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, smem));
+    const int64_t blocks = (total + plan.units - 1) / plan.units, most = (int64_t)sm_count() * (resident > 0 ? resident : 1);
+    kernel<<<(unsigned)(blocks < most ? blocks : most), threads, smem, st>>>(a, plan, m, stall_counter());
     GS_CUDA_TRY(cudaGetLastError());
     return GS_OK;
 }

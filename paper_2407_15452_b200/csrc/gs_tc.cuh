@@ -76,6 +76,16 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, u
                  ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(pos), "r"(head), "r"(b) : "memory");
 }
 
+// a box from shared memory; what lies outside the tensor is not written
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, int x, int pos, int head, int b)
+{
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(pos), "r"(head), "r"(b) : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// this thread's stores have read their shared memory
+__device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+
 // ---- tensor memory ----------------------------------------------------------------------
 __device__ __forceinline__ void tmem_alloc(uint32_t where, uint32_t columns)       // whole warp
 {
@@ -190,6 +200,18 @@ __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float log2_fast(float x)
+{
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_fast(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 template <bool BF16>
