@@ -9,6 +9,7 @@ not been built the first call raises.
 from __future__ import annotations
 
 import ctypes
+import struct
 from dataclasses import dataclass
 from pathlib import Path
 
@@ -104,8 +105,13 @@ def lib():
         for name in EXPORTS:
             if name not in ("gs_last_error", "gs_graph_free"):
                 getattr(L, name).restype = ctypes.c_int32
-        L.gs_gradient_norm_work.restype = ctypes.c_int64
-        L.gs_attention_backward_work.restype = ctypes.c_int64
+        p, i64 = ctypes.c_void_p, ctypes.c_int64
+        L.gs_attention_forward.argtypes = [p] * 7
+        L.gs_attention_backward.argtypes = [p] * 12
+        L.gs_attention_backward_work.argtypes, L.gs_attention_backward_work.restype = [p], i64
+        L.gs_gradient_norm_work.argtypes, L.gs_gradient_norm_work.restype = [i64], i64
+        L.gs_gradient_norm.argtypes = [p, i64, p, p, p]
+        L.gs_clip_gradients.argtypes = [p, p, i64, ctypes.c_float, p, p, p]
         _lib = L
     return _lib
 
@@ -453,68 +459,69 @@ def gs_tune_node2vec_group(lanes: int):
 
 
 # ---------------------------------------------------------------- sequence models over walks
+# These calls are a few microseconds of work for small batches, so their marshalling is lean: plain integers
+# against declared argument types, and the configuration packed in one step (the layout of AttentionConfig).
 _TABLE_DTYPE = {torch.float32: GS_TABLE_F32, torch.float16: GS_TABLE_F16, torch.bfloat16: GS_TABLE_BF16}
+_pack_config = struct.Struct("4iq4ifiQQ24q").pack
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_NO_STRIDE = (0, 0, 0)
 
 
-def _heads(t, like, shape, name):
-    """Checks one [batch, position, head, head_dim] tensor; returns its address."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == like.dtype and t.device == like.device):
-        raise TypeError(f"{name} must be a CUDA tensor of {like.dtype} on {like.device}")
+def _heads(t, dtype, device, shape, name):
+    """Checks one [batch, position, head, head_dim] tensor; returns its first three strides."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != device:
+        raise TypeError(f"{name} must be a tensor of {dtype} on cuda:{device}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.stride(3) != 1 and shape[3] > 1:
+    st = t.stride()
+    if st[3] != 1 and shape[3] > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
-    return t.data_ptr()
+    return st[:3]
 
 
-def _lens(t, batch, like, name):
+def _lens(t, batch, device, name):
     if t is None:
-        return None
-    if not (isinstance(t, torch.Tensor) and t.device == like.device and t.dtype == torch.int32
-            and t.is_contiguous() and t.shape == (batch,)):
-        raise TypeError(f"{name} must be a contiguous int32 tensor of {batch} lengths on {like.device}")
+        return 0
+    if not (isinstance(t, torch.Tensor) and t.get_device() == device and t.dtype is torch.int32
+            and t.shape == (batch,) and t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous int32 tensor of {batch} lengths on cuda:{device}")
     return t.data_ptr()
 
 
-def _attention_config(q, k, v, scale, window, q_lens, k_lens):
+def _attention_shape(q, k, scale, window, q_lens, k_lens):
+    """(device, leading fields of the configuration, shape of k and v)"""
     if not (isinstance(q, torch.Tensor) and q.is_cuda and q.dim() == 4 and q.dtype in _TABLE_DTYPE):
         raise TypeError("q must be a CUDA tensor [batch, position, head, head_dim] of float32, float16 or bfloat16")
     if not (isinstance(k, torch.Tensor) and k.dim() == 4):
         raise TypeError("k must be a tensor [batch, position, head, head_dim]")
-    if q.device.index != torch.cuda.current_device():
+    device = q.get_device()
+    if device != torch._C._cuda_getDevice():
         raise ValueError(f"q is on {q.device}, which is not the current device")
     b, n, hq, d = q.shape
-    m, hk = k.shape[1], k.shape[2]
+    _, m, hk, _ = k.shape
     if scale is None:
         scale = d ** -0.5 if d else 1.0
-    kv = (b, m, hk, d)
-    cfg = AttentionConfig(_TABLE_DTYPE[q.dtype], d, hq, hk, b, n, m, window[0], window[1], scale, 0,
-                          _lens(q_lens, b, q, "q_lens"), _lens(k_lens, b, q, "k_lens"))
-    cfg.q_stride[:] = q.stride()[:3]
-    cfg.k_stride[:] = k.stride()[:3]
-    cfg.v_stride[:] = v.stride()[:3]
-    return cfg, _heads(q, q, q.shape, "q"), _heads(k, q, kv, "k"), _heads(v, q, kv, "v")
-
-
-def _ptr(address) -> ctypes.c_void_p:
-    return ctypes.c_void_p(address)
+    return device, (_TABLE_DTYPE[q.dtype], d, hq, hk, b, n, m, window[0], window[1], scale, 0,
+                    _lens(q_lens, b, device, "q_lens"), _lens(k_lens, b, device, "k_lens")), (b, m, hk, d)
 
 
 def gs_attention_forward(q, k, v, scale=None, window=(-1, -1), q_lens=None, k_lens=None, out=None, lse=None):
     """Attention of q[batch, q_len, q_heads, head_dim] over k, v[batch, k_len, kv_heads, head_dim]
     (see gs.h for the visible keys).  Returns (out like q, lse float32[batch, q_heads, q_len])."""
-    cfg, pq, pk, pv = _attention_config(q, k, v, scale, window, q_lens, k_lens)
-    b, n, hq, _ = q.shape
+    device, lead, kv = _attention_shape(q, k, scale, window, q_lens, k_lens)
+    shape, dtype = q.shape, q.dtype
+    rows = (shape[0], shape[2], shape[1])
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(shape)
     if lse is None:
-        lse = torch.empty((b, hq, n), dtype=torch.float32, device=q.device)
-    elif lse.shape != (b, hq, n):
-        raise ValueError(f"lse has shape {tuple(lse.shape)}, expected {(b, hq, n)}")
-    po = _heads(out, q, q.shape, "out")
-    cfg.out_stride[:] = out.stride()[:3]
-    _check(lib().gs_attention_forward(ctypes.byref(cfg), _ptr(pq), _ptr(pk), _ptr(pv), _ptr(po),
-                                      _dev(lse, torch.float32, "lse"), _stream()))
+        lse = q.new_empty(rows, dtype=torch.float32)
+    elif lse.shape != rows or lse.dtype is not torch.float32 or lse.get_device() != device or not lse.is_contiguous():
+        raise ValueError(f"lse must be a contiguous float32 tensor of shape {rows} on cuda:{device}")
+    cfg = _pack_config(*lead, *_heads(q, dtype, device, shape, "q"), *_heads(k, dtype, device, kv, "k"),
+                       *_heads(v, dtype, device, kv, "v"), *_heads(out, dtype, device, shape, "out"),
+                       *_NO_STRIDE, *_NO_STRIDE, *_NO_STRIDE, *_NO_STRIDE)
+    _check(lib().gs_attention_forward(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                      _raw_stream(device)))
     return out, lse
 
 
@@ -522,62 +529,64 @@ def gs_attention_backward(dout, q, k, v, out, lse, scale=None, window=(-1, -1), 
                           dq=None, dk=None, dv=None):
     """Gradients of gs_attention_forward: returns (dq, dk, dv), shaped like q, k, v.  out and lse are
     the forward call's results, dout the gradient of out."""
-    cfg, pq, pk, pv = _attention_config(q, k, v, scale, window, q_lens, k_lens)
-    b, n, hq, _ = q.shape
-    if not (isinstance(lse, torch.Tensor) and lse.shape == (b, hq, n)):
-        raise ValueError(f"lse must be a tensor of shape {(b, hq, n)}")
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
-    dv = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dv is None else dv
-    at = {}
-    for name, t, like in (("dout", dout, q), ("out", out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
-        at[name] = _ptr(_heads(t, q, like.shape, name))
-        getattr(cfg, f"{name}_stride")[:] = t.stride()[:3]
-    work = torch.empty(max(0, lib().gs_attention_backward_work(ctypes.byref(cfg))), dtype=torch.float32,
-                       device=q.device)
-    _check(lib().gs_attention_backward(ctypes.byref(cfg), at["dout"], _ptr(pq), _ptr(pk), _ptr(pv), at["out"],
-                                       _dev(lse, torch.float32, "lse"), _ptr(work.data_ptr()), at["dq"], at["dk"],
-                                       at["dv"], _stream()))
+    device, lead, kv = _attention_shape(q, k, scale, window, q_lens, k_lens)
+    shape, dtype = q.shape, q.dtype
+    rows = (shape[0], shape[2], shape[1])
+    if not isinstance(lse, torch.Tensor) or lse.shape != rows or lse.dtype is not torch.float32 \
+            or lse.get_device() != device or not lse.is_contiguous():
+        raise ValueError(f"lse must be a contiguous float32 tensor of shape {rows} on cuda:{device}")
+    dq = q.new_empty(shape) if dq is None else dq
+    dk = q.new_empty(kv) if dk is None else dk
+    dv = q.new_empty(kv) if dv is None else dv
+    cfg = _pack_config(*lead, *_heads(q, dtype, device, shape, "q"), *_heads(k, dtype, device, kv, "k"),
+                       *_heads(v, dtype, device, kv, "v"), *_heads(out, dtype, device, shape, "out"),
+                       *_heads(dout, dtype, device, shape, "dout"), *_heads(dq, dtype, device, shape, "dq"),
+                       *_heads(dk, dtype, device, kv, "dk"), *_heads(dv, dtype, device, kv, "dv"))
+    L = lib()
+    work = lse.new_empty(max(0, L.gs_attention_backward_work(cfg)))
+    _check(L.gs_attention_backward(cfg, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                                   lse.data_ptr(), work.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                   _raw_stream(device)))
     return dq, dk, dv
 
 
-def _tensor_list(tensors, name):
-    device = torch.cuda.current_device()
-    entries = (TensorEntry * len(tensors))()
-    for e, t in zip(entries, tensors):
+def _tensor_list(tensors, device, name):
+    """The host array of gs_tensor entries, as bytes."""
+    words = []
+    for t in tensors:
         code = _TABLE_DTYPE.get(t.dtype)
-        if code is None or not t.is_cuda or t.device.index != device or not t.is_contiguous():
+        if code is None or t.get_device() != device or not t.is_contiguous():
             raise TypeError(f"{name} must be contiguous float32, float16 or bfloat16 tensors on the current CUDA device")
-        e.d_data, e.numel, e.dtype = t.data_ptr(), t.numel(), code
-    return entries
+        words += (t.data_ptr(), t.numel(), code)
+    return struct.pack(f"{len(words)}Q", *words)
 
 
-def _norm_buffers(n):
-    words = lib().gs_gradient_norm_work(ctypes.c_int64(n))
-    device = torch.cuda.current_device()
-    return (torch.empty(words, dtype=torch.float64, device=device),
-            torch.empty(1, dtype=torch.float32, device=device))
+def _norm_buffers(n, device):
+    words = lib().gs_gradient_norm_work(n)
+    on = torch.device("cuda", device)
+    return torch.empty(words, dtype=torch.float64, device=on), torch.empty(1, dtype=torch.float32, device=on)
 
 
 def gs_gradient_norm(grads):
     """Euclidean norm of all tensors of `grads` taken as one vector: float32[1] on the device."""
-    entries = _tensor_list(grads, "grads")
-    work, norm = _norm_buffers(len(entries))
-    _check(lib().gs_gradient_norm(entries, ctypes.c_int64(len(entries)), _ptr(work.data_ptr()),
-                                  _ptr(norm.data_ptr()), _stream()))
+    device = torch.cuda.current_device()
+    entries = _tensor_list(grads, device, "grads")
+    work, norm = _norm_buffers(len(grads), device)
+    _check(lib().gs_gradient_norm(entries, len(grads), work.data_ptr(), norm.data_ptr(), _raw_stream(device)))
     return norm
 
 
 def gs_clip_gradients(grads, max_norm: float, out=None):
     """Scales `grads` (into the tensors `out`, or in place) so that their joint norm is at most
     max_norm; returns the norm before clipping, float32[1] on the device (nothing waits for it)."""
-    entries = _tensor_list(grads, "grads")
+    device = torch.cuda.current_device()
+    entries = _tensor_list(grads, device, "grads")
     targets = None
     if out is not None:
         if len(out) != len(grads):
             raise ValueError(f"{len(out)} outputs for {len(grads)} gradients")
-        targets = _tensor_list(out, "out")
-    work, norm = _norm_buffers(len(entries))
-    _check(lib().gs_clip_gradients(entries, targets, ctypes.c_int64(len(entries)), ctypes.c_float(max_norm),
-                                   _ptr(work.data_ptr()), _ptr(norm.data_ptr()), _stream()))
+        targets = _tensor_list(out, device, "out")
+    work, norm = _norm_buffers(len(grads), device)
+    _check(lib().gs_clip_gradients(entries, targets, len(grads), max_norm, work.data_ptr(), norm.data_ptr(),
+                                   _raw_stream(device)))
     return norm

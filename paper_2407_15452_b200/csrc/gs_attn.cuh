@@ -11,6 +11,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "gs_common.cuh"
 
 namespace gs {
@@ -63,6 +65,23 @@ __device__ __forceinline__ int attn_q_first(const AttnArgs &a, const AttnSeq &s,
 __device__ __forceinline__ int attn_q_last(const AttnArgs &a, const AttnSeq &s, int j1)
 {
     return a.left < 0 ? s.nq : min(s.nq, j1 - s.off + a.left);
+}
+
+// Lets `kernel` use up to `bytes` of dynamic shared memory on the current device; `done` is the kernel's own record of
+// what each device allows already (the attribute costs about a microsecond to set).
+struct SharedRecord {
+    std::atomic<int> bytes[64];
+};
+template <typename K>
+static inline gs_status allow_shared(K kernel, int bytes, SharedRecord &done)
+{
+    int dev = 0;
+    GS_CUDA_TRY(cudaGetDevice(&dev));
+    const bool known = dev >= 0 && dev < 64;
+    if (known && done.bytes[dev].load(std::memory_order_relaxed) >= bytes) return GS_OK;
+    GS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    if (known) done.bytes[dev].store(bytes, std::memory_order_relaxed);
+    return GS_OK;
 }
 
 // gs_attn_simt.cu

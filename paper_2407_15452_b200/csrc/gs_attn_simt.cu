@@ -396,7 +396,7 @@ static bool rows_of_four(const AttnArgs &a, size_t es, bool backward)
 
 template <typename K>
 static gs_status launch(K kernel, const AttnArgs &a, int64_t heads, int32_t len, int bt, size_t smem, bool vec,
-                        cudaStream_t st)
+                        SharedRecord &record, cudaStream_t st)
 {
     const int tiles = (len + bt - 1) / bt;
     const int64_t blocks = heads * tiles;
@@ -405,7 +405,8 @@ static gs_status launch(K kernel, const AttnArgs &a, int64_t heads, int32_t len,
         set_error("attention of %lld row tiles exceeds one launch", (long long)blocks);
         return GS_ERR_UNSUPPORTED;
     }
-    GS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    gs_status s = allow_shared(kernel, (int)smem, record);
+    if (s != GS_OK) return s;
     kernel<<<(unsigned)blocks, bt * 4, smem, st>>>(a, tiles, vec);
     GS_CUDA_TRY(cudaGetLastError());
     return GS_OK;
@@ -415,8 +416,9 @@ template <typename T, int BT, int DP>
 static gs_status forward_t(const AttnArgs &a, cudaStream_t st)
 {
     const size_t smem = sizeof(float) * (2 * BT * (DP + 4) + BT * (BT + 4));
+    static SharedRecord record;
     return launch(attn_simt_forward_kernel<T, BT, DP>, a, a.batch * a.q_heads, a.q_len, BT, smem,
-                  rows_of_four(a, sizeof(T), false), st);
+                  rows_of_four(a, sizeof(T), false), record, st);
 }
 
 template <typename T, int BT, int DP>
@@ -424,9 +426,10 @@ static gs_status backward_t(const AttnArgs &a, cudaStream_t st)
 {
     const bool vec = rows_of_four(a, sizeof(T), true);
     const size_t rows = sizeof(float) * 4 * BT * (DP + 4), tile = sizeof(float) * BT * (BT + 4);
-    gs_status s = launch(attn_simt_dq_kernel<T, BT, DP>, a, a.batch * a.q_heads, a.q_len, BT, rows + tile, vec, st);
+    static SharedRecord record[2];
+    gs_status s = launch(attn_simt_dq_kernel<T, BT, DP>, a, a.batch * a.q_heads, a.q_len, BT, rows + tile, vec, record[0], st);
     if (s != GS_OK) return s;
-    return launch(attn_simt_dkdv_kernel<T, BT, DP>, a, a.batch * a.kv_heads, a.k_len, BT, rows + 2 * tile, vec, st);
+    return launch(attn_simt_dkdv_kernel<T, BT, DP>, a, a.batch * a.kv_heads, a.k_len, BT, rows + 2 * tile, vec, record[1], st);
 }
 
 template <typename T, bool BWD>

@@ -338,7 +338,9 @@ static gs_status forward_t(const AttnArgs &a, const TcMaps &maps, cudaStream_t s
         return GS_ERR_UNSUPPORTED;
     }
     auto kernel = attn_tc_forward_kernel<BF16, DP>;
-    GS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdSmem<DP>::BYTES));
+    static SharedRecord record;
+    gs_status s = allow_shared(kernel, FwdSmem<DP>::BYTES, record);
+    if (s != GS_OK) return s;
     kernel<<<(unsigned)blocks, 384, FwdSmem<DP>::BYTES, st>>>(a, maps, stall_counter());
     GS_CUDA_TRY(cudaGetLastError());
     return GS_OK;

@@ -655,8 +655,11 @@ static gs_status backward_t(const AttnArgs &a, const BwdMaps &maps, const BwdNor
         GS_CUDA_TRY(cudaGetLastError());
     }
     constexpr int smem = BwdSmem<DP>::BYTES;
-    GS_CUDA_TRY(cudaFuncSetAttribute(attn_tc_dq_kernel<BF16, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    GS_CUDA_TRY(cudaFuncSetAttribute(attn_tc_dkdv_kernel<BF16, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static SharedRecord record[2];
+    gs_status s;
+    if ((s = allow_shared(attn_tc_dq_kernel<BF16, DP>, smem, record[0])) != GS_OK ||
+        (s = allow_shared(attn_tc_dkdv_kernel<BF16, DP>, smem, record[1])) != GS_OK)
+        return s;
     attn_tc_dq_kernel<BF16, DP><<<(unsigned)q_blocks, 384, smem, st>>>(a, maps, norms, stalls);
     GS_CUDA_TRY(cudaGetLastError());
     attn_tc_dkdv_kernel<BF16, DP><<<(unsigned)k_blocks, 384, smem, st>>>(a, maps, norms, stalls);

@@ -803,7 +803,7 @@ static gs_status launch(const AttnArgs &a, cudaStream_t st)
         auto on_k = [&](CUtensorMap *t, const AttnTensor &x, int rows) {
             return attn_tensor_map(t, x, BF16, a.batch, a.k_len, a.kv_heads, a.dim, BOX, rows);
         };
-        gs_status s;
+        gs_status s = GS_OK;
         if ((s = on_q(&m.q, a.q, plan.qt * 16)) != GS_OK || (s = on_k(&m.k, a.k, plan.kt * 16)) != GS_OK ||
             (s = on_k(&m.v, a.v, plan.kt * 16)) != GS_OK || (s = on_q(&m.out, BWD ? a.dq : a.out, 16)) != GS_OK)
             return s;
@@ -824,10 +824,13 @@ static gs_status launch(const AttnArgs &a, cudaStream_t st)
     const int smem = plan.units * per_unit + masks;
     auto kernel = !BWD ? attn_walk_forward_kernel<BF16, DP>
                        : a.group > 1 ? attn_walk_backward_kernel<BF16, DP, true> : attn_walk_backward_kernel<BF16, DP, false>;
-    GS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static SharedRecord record[2];
+    gs_status s = allow_shared(kernel, smem, record[BWD && a.group > 1]);
+    if (s != GS_OK) return s;
     const int threads = plan.units * tiles * 32;
-    int resident = 0;
-    GS_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, smem));
+    // blocks that an SM holds, by shared memory (1 KB and the static variables on top) and by registers
+    const int by_shared = 228 * 1024 / (smem + 2048), by_registers = 65536 / (registers<DP, BWD>() * threads);
+    const int resident = by_shared < by_registers ? by_shared : by_registers;
     const int64_t blocks = (total + plan.units - 1) / plan.units, most = (int64_t)sm_count() * (resident > 0 ? resident : 1);
     kernel<<<(unsigned)(blocks < most ? blocks : most), threads, smem, st>>>(a, plan, m, stall_counter());
     GS_CUDA_TRY(cudaGetLastError());
