@@ -512,7 +512,7 @@ def gs_attention_forward(q, k, v, scale=None, window=(-1, -1), q_lens=None, k_le
     shape, dtype = q.shape, q.dtype
     rows = (shape[0], shape[2], shape[1])
     if out is None:
-        out = q.new_empty(shape)
+        out = torch.empty_like(q)
     if lse is None:
         lse = q.new_empty(rows, dtype=torch.float32)
     elif lse.shape != rows or lse.dtype is not torch.float32 or lse.get_device() != device or not lse.is_contiguous():
@@ -535,9 +535,9 @@ def gs_attention_backward(dout, q, k, v, out, lse, scale=None, window=(-1, -1), 
     if not isinstance(lse, torch.Tensor) or lse.shape != rows or lse.dtype is not torch.float32 \
             or lse.get_device() != device or not lse.is_contiguous():
         raise ValueError(f"lse must be a contiguous float32 tensor of shape {rows} on cuda:{device}")
-    dq = q.new_empty(shape) if dq is None else dq
-    dk = q.new_empty(kv) if dk is None else dk
-    dv = q.new_empty(kv) if dv is None else dv
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None else dk
+    dv = torch.empty_like(v) if dv is None else dv
     cfg = _pack_config(*lead, *_heads(q, dtype, device, shape, "q"), *_heads(k, dtype, device, kv, "k"),
                        *_heads(v, dtype, device, kv, "v"), *_heads(out, dtype, device, shape, "out"),
                        *_heads(dout, dtype, device, shape, "dout"), *_heads(dq, dtype, device, shape, "dq"),
