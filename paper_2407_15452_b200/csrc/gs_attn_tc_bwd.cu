@@ -36,11 +36,15 @@ struct BwdNorms {                                 // binary16: largest row norm 
 template <int DP>
 struct BwdSmem {
     static constexpr int TILE = T * DP * 2;
-    static constexpr int STAGES = DP == 128 ? 2 : 4;
-    static constexpr int A = 0, B = TILE, RING = 2 * TILE;      // two resident tiles, then stages of two tiles
-    static constexpr int STATS = RING + STAGES * 2 * TILE;      // dk/dv: lse and delta of a query tile, per stage
-    static constexpr int BARS = STATS + STAGES * 2 * T * 4;
-    static constexpr int BYTES = BARS + 256 + 1024;
+    // Two resident tiles, then two rings of tiles: X for the operand that a step needs first and last (K for dq, Q for
+    // dk/dv), Y for the other.  Three X tiles, because one is free only when its step's last product is done.
+    static constexpr int XS = DP == 128 ? 3 : 4, YS = DP == 128 ? 2 : 4, SS = 2;
+    static constexpr int A = 0, B = TILE, X = 2 * TILE, Y = X + XS * TILE;
+    static constexpr int STATS = Y + YS * TILE;                 // dk/dv: lse and delta of a query tile, SS of them
+    static constexpr int BARS = STATS + SS * 2 * T * 4;
+    static constexpr int WORDS = BARS + 8 * (10 + 2 * XS + 2 * YS + 2 * SS);    // stalled, address of the tensor memory
+    static constexpr int BYTES = WORDS + 16;
+    static_assert(BYTES <= 227 * 1024, "shared memory of one block");
 };
 
 // D[128 x 128] = A B^T over the head dimension, both tiles [rows][values]
@@ -126,20 +130,30 @@ __device__ __forceinline__ float2 unpack2(uint32_t u)
     else return __half22float2(*reinterpret_cast<__half2 *>(&u));
 }
 
-// dot product of two rows of 16-bit values in global memory
-template <bool BF16>
+// dot product of two rows of 16-bit values in global memory; 128 bytes of each are on their way at a time
+template <bool BF16, int DP>
 __device__ __forceinline__ float dot16(const uint16_t *x, const uint16_t *y, int dim, bool vec)
 {
     float d = 0.f;
     if (vec) {
-        for (int c = 0; c < dim; c += 8) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(x + c)), w = __ldg(reinterpret_cast<const uint4 *>(y + c));
-            const uint32_t p[4] = {u.x, u.y, u.z, u.w}, q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = unpack2<BF16>(p[i]), g = unpack2<BF16>(q[i]);
-                d = fmaf(f.x, g.x, d);
-                d = fmaf(f.y, g.y, d);
+        for (int c0 = 0; c0 < DP; c0 += 64) {
+            uint4 u[8], w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const bool in = c0 + 8 * k < dim;
+                u[k] = in ? __ldg(reinterpret_cast<const uint4 *>(x + c0 + 8 * k)) : make_uint4(0, 0, 0, 0);
+                w[k] = in ? __ldg(reinterpret_cast<const uint4 *>(y + c0 + 8 * k)) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t p[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, q[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = unpack2<BF16>(p[i]), g = unpack2<BF16>(q[i]);
+                    d = fmaf(f.x, g.x, d);
+                    d = fmaf(f.y, g.y, d);
+                }
             }
         }
     } else {
@@ -154,14 +168,14 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
                   unsigned long long *stalls)
 {
     using L = BwdSmem<DP>;
-    extern __shared__ uint8_t raw[];
-    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    __shared__ volatile int stalled;
-    __shared__ uint32_t tmem_base;
+    extern __shared__ __align__(1024) uint8_t smem[];           // no static shared memory: this starts at its beginning
+    const uint32_t base = smem_u32(smem);
+    volatile int &stalled = *reinterpret_cast<volatile int *>(smem + L::WORDS);
+    uint32_t &tmem_base = *reinterpret_cast<uint32_t *>(smem + L::WORDS + 4);
     const uint32_t bars = base + L::BARS;
     const uint32_t q_full = bars, fix = bars + 8, s_full = bars + 16, dp_full = bars + 32, dp_free = bars + 40,
-                   ds_full = bars + 48, done = bars + 56, k_full = bars + 64, v_full = k_full + 8 * L::STAGES,
-                   k_empty = v_full + 8 * L::STAGES, v_empty = k_empty + 8 * L::STAGES;
+                   ds_full = bars + 48, done = bars + 56, k_full = bars + 80, k_empty = k_full + 8 * L::XS,
+                   v_full = k_empty + 8 * L::XS, v_empty = v_full + 8 * L::YS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     const int64_t heads = a.batch * a.q_heads;
@@ -189,7 +203,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
         bar_init(dp_free, 256);
         bar_init(ds_full, 256);
         bar_init(done, 1);
-        for (int i = 0; i < 4 * L::STAGES; ++i) bar_init(k_full + 8 * i, 1);
+        for (int i = 0; i < 2 * (L::XS + L::YS); ++i) bar_init(k_full + 8 * i, 1);
         fence_barrier_init();
     }
     if (warp == 8) tmem_alloc(smem_u32(&tmem_base), 512);
@@ -213,59 +227,64 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
             }
             bool ok = true;
             for (int i = 0; i < n && ok; ++i) {
-                const int st = i % L::STAGES, round = i / L::STAGES, j0 = (first + i) * T;
-                const uint32_t kt = base + L::RING + st * 2 * L::TILE, vt = kt + L::TILE;
+                const int kst = i % L::XS, vst = i % L::YS, j0 = (first + i) * T;
+                const uint32_t kt = base + L::X + kst * L::TILE, vt = base + L::Y + vst * L::TILE;
                 const bool patch = s.nk < a.k_len && j0 + T > s.nk;        // K is summed over its rows in dS K
-                if (round > 0) ok = __all_sync(0xffffffffu, bar_wait(k_empty + 8 * st, (round - 1) & 1, &stalled));
+                if (i >= L::XS) ok = __all_sync(0xffffffffu, bar_wait(k_empty + 8 * kst, (i / L::XS - 1) & 1, &stalled));
                 if (!ok) break;
                 if (lane == 0) {
-                    const uint32_t bar = patch ? fix : k_full + 8 * st;
+                    const uint32_t bar = patch ? fix : k_full + 8 * kst;
                     bar_expect(bar, L::TILE);
                     load_tile<DP>(kt, &maps.k, bar, j0, g, (int)b);
                 }
-                if (round > 0) ok = __all_sync(0xffffffffu, bar_wait(v_empty + 8 * st, (round - 1) & 1, &stalled));
+                if (i >= L::YS) ok = __all_sync(0xffffffffu, bar_wait(v_empty + 8 * vst, (i / L::YS - 1) & 1, &stalled));
                 if (!ok) break;
                 if (lane == 0) {
-                    bar_expect(v_full + 8 * st, L::TILE);
-                    load_tile<DP>(vt, &maps.v, v_full + 8 * st, j0, g, (int)b);
+                    bar_expect(v_full + 8 * vst, L::TILE);
+                    load_tile<DP>(vt, &maps.v, v_full + 8 * vst, j0, g, (int)b);
                 }
-                if (patch) ok = patch_tile<DP>(kt, s.nk - j0, fix, 0, k_full + 8 * st, &stalled);
+                if (patch) ok = patch_tile<DP>(kt, s.nk - j0, fix, 0, k_full + 8 * kst, &stalled);
             }
         }
     } else if (warp == 8) {
         if (lane == 0 && n > 0) {
             constexpr uint32_t DESC_S = mma_desc(BF16, T, T, false), DESC_Q = mma_desc(BF16, T, DP, true);
-            auto kt = [&](int i) { return base + L::RING + (i % L::STAGES) * 2 * L::TILE; };
-            auto parity = [&](int i) { return (uint32_t)(i / L::STAGES) & 1u; };
-            bool ok = bar_wait(q_full, 0, &stalled) && bar_wait(k_full, 0, &stalled) && bar_wait(v_full, 0, &stalled);
+            auto kt = [&](int i) { return base + L::X + (i % L::XS) * L::TILE; };
+            auto vt = [&](int i) { return base + L::Y + (i % L::YS) * L::TILE; };
+            auto k_here = [&](int i) { return bar_wait(k_full + 8 * (i % L::XS), (i / L::XS) & 1, &stalled); };
+            auto v_here = [&](int i) { return bar_wait(v_full + 8 * (i % L::YS), (i / L::YS) & 1, &stalled); };
+            bool ok = bar_wait(q_full, 0, &stalled) && k_here(0);
             if (ok) {
                 fence_after();
                 mul_values<DP>(tmem, base + L::A, kt(0), DESC_S);
                 mma_commit(s_full);
-                mul_values<DP>(tmem + 256, base + L::B, kt(0) + L::TILE, DESC_S);
+                ok = v_here(0);
+            }
+            if (ok) {
+                fence_after();
+                mul_values<DP>(tmem + 256, base + L::B, vt(0), DESC_S);
                 mma_commit(dp_full);
                 mma_commit(v_empty);
             }
             for (int i = 0; i < n && ok; ++i) {
-                const int st = i % L::STAGES, nx = (i + 1) % L::STAGES;
                 if (i + 1 < n) {                      // the other S: its dS went into dQ(i - 1), issued before
-                    ok = bar_wait(k_full + 8 * nx, parity(i + 1), &stalled);
+                    ok = k_here(i + 1);
                     if (!ok) break;
                     fence_after();
                     mul_values<DP>(tmem + 128 * ((i + 1) & 1), base + L::A, kt(i + 1), DESC_S);
                     mma_commit(s_full + 8 * ((i + 1) & 1));
-                    ok = bar_wait(v_full + 8 * nx, parity(i + 1), &stalled) && bar_wait(dp_free, i & 1, &stalled);
+                    ok = v_here(i + 1) && bar_wait(dp_free, i & 1, &stalled);
                     if (!ok) break;
                     fence_after();
-                    mul_values<DP>(tmem + 256, base + L::B, kt(i + 1) + L::TILE, DESC_S);
+                    mul_values<DP>(tmem + 256, base + L::B, vt(i + 1), DESC_S);
                     mma_commit(dp_full);
-                    mma_commit(v_empty + 8 * nx);
+                    mma_commit(v_empty + 8 * ((i + 1) % L::YS));
                 }
                 ok = bar_wait(ds_full, i & 1, &stalled);
                 if (!ok) break;
                 fence_after();
                 mul_rows(tmem + 384, tmem + 128 * (i & 1), kt(i), DESC_Q, i > 0);
-                mma_commit(k_empty + 8 * st);
+                mma_commit(k_empty + 8 * (i % L::XS));
             }
             if (ok) mma_commit(done);
         }
@@ -281,7 +300,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
         float delta = 0.f, lse2 = 0.f;
         if (row) {
             const bool vec = rows16(a.out, a.dim) && rows16(a.dout, a.dim);
-            delta = dot16<BF16>(reinterpret_cast<const uint16_t *>(a.out.p) + b * a.out.sb + (int64_t)r * a.out.sl + h * a.out.sh,
+            delta = dot16<BF16, DP>(reinterpret_cast<const uint16_t *>(a.out.p) + b * a.out.sb + (int64_t)r * a.out.sl + h * a.out.sh,
                                 reinterpret_cast<const uint16_t *>(a.dout.p) + b * a.dout.sb + (int64_t)r * a.dout.sl + h * a.dout.sh,
                                 a.dim, vec);
             lse2 = a.lse[bh * a.q_len + r] * LOG2E;
@@ -359,17 +378,16 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     unsigned long long *stalls)
 {
     using L = BwdSmem<DP>;
-    extern __shared__ uint8_t raw[];
-    const uint32_t pad = ((smem_u32(raw) + 1023u) & ~1023u) - smem_u32(raw);
-    const uint32_t base = smem_u32(raw) + pad;
-    float *stats = reinterpret_cast<float *>(raw + pad + L::STATS);       // [stage][lse, delta][128]
-    __shared__ volatile int stalled;
-    __shared__ uint32_t tmem_base;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t base = smem_u32(smem);
+    float *stats = reinterpret_cast<float *>(smem + L::STATS);            // [slot][lse, delta][128]
+    volatile int &stalled = *reinterpret_cast<volatile int *>(smem + L::WORDS);
+    uint32_t &tmem_base = *reinterpret_cast<uint32_t *>(smem + L::WORDS + 4);
     const uint32_t bars = base + L::BARS;
     const uint32_t kv_full = bars, fix = bars + 8, s_full = bars + 24, dp_full = bars + 32, p_full = bars + 40,
-                   ds_full = bars + 48, done = bars + 56, q_full = bars + 64, do_full = q_full + 8 * L::STAGES,
-                   q_empty = do_full + 8 * L::STAGES, do_empty = q_empty + 8 * L::STAGES,
-                   st_full = do_empty + 8 * L::STAGES, st_empty = st_full + 8 * L::STAGES;
+                   ds_full = bars + 48, done = bars + 56, q_full = bars + 80, q_empty = q_full + 8 * L::XS,
+                   do_full = q_empty + 8 * L::XS, do_empty = do_full + 8 * L::YS,
+                   st_full = do_empty + 8 * L::YS, st_empty = st_full + 8 * L::SS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     const int64_t heads = a.batch * a.kv_heads;
@@ -397,8 +415,8 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         bar_init(p_full, 256);
         bar_init(ds_full, 256);
         bar_init(done, 1);
-        for (int i = 0; i < 4 * L::STAGES; ++i) bar_init(q_full + 8 * i, 1);
-        for (int i = 0; i < L::STAGES; ++i) {
+        for (int i = 0; i < 2 * (L::XS + L::YS); ++i) bar_init(q_full + 8 * i, 1);
+        for (int i = 0; i < L::SS; ++i) {
             bar_init(st_full + 8 * i, 32);
             bar_init(st_empty + 8 * i, 256);
         }
@@ -426,27 +444,27 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             bool ok = true;
             uint32_t patched = 0;
             for (int i = 0; i < n && ok; ++i) {
-                const int st = i % L::STAGES, round = i / L::STAGES;
+                const int qst = i % L::XS, ost = i % L::YS;
                 const int r0 = (first + i % per_head) * T, h = g * a.group + i / per_head;
-                const uint32_t qt = base + L::RING + st * 2 * L::TILE, dt = qt + L::TILE;
+                const uint32_t qt = base + L::X + qst * L::TILE, dt = base + L::Y + ost * L::TILE;
                 const bool patch = s.nq < a.q_len && r0 + T > s.nq;        // both are summed over their rows
-                if (round > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty + 8 * st, (round - 1) & 1, &stalled));
+                if (i >= L::XS) ok = __all_sync(0xffffffffu, bar_wait(q_empty + 8 * qst, (i / L::XS - 1) & 1, &stalled));
                 if (!ok) break;
                 if (lane == 0) {
-                    const uint32_t bar = patch ? fix : q_full + 8 * st;
+                    const uint32_t bar = patch ? fix : q_full + 8 * qst;
                     bar_expect(bar, L::TILE);
                     load_tile<DP>(qt, &maps.q, bar, r0, h, (int)b);
                 }
-                if (round > 0) ok = __all_sync(0xffffffffu, bar_wait(do_empty + 8 * st, (round - 1) & 1, &stalled));
+                if (i >= L::YS) ok = __all_sync(0xffffffffu, bar_wait(do_empty + 8 * ost, (i / L::YS - 1) & 1, &stalled));
                 if (!ok) break;
                 if (lane == 0) {
-                    const uint32_t bar = patch ? fix + 8 : do_full + 8 * st;
+                    const uint32_t bar = patch ? fix + 8 : do_full + 8 * ost;
                     bar_expect(bar, L::TILE);
                     load_tile<DP>(dt, &maps.dout, bar, r0, h, (int)b);
                 }
                 if (patch) {
-                    ok = patch_tile<DP>(qt, s.nq - r0, fix, patched, q_full + 8 * st, &stalled) &&
-                         patch_tile<DP>(dt, s.nq - r0, fix + 8, patched, do_full + 8 * st, &stalled);
+                    ok = patch_tile<DP>(qt, s.nq - r0, fix, patched, q_full + 8 * qst, &stalled) &&
+                         patch_tile<DP>(dt, s.nq - r0, fix + 8, patched, do_full + 8 * ost, &stalled);
                     patched ^= 1;
                 }
             }
@@ -454,29 +472,30 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     } else if (warp == 8) {
         if (lane == 0 && n > 0) {
             constexpr uint32_t DESC_S = mma_desc(BF16, T, T, false), DESC_G = mma_desc(BF16, T, DP, true);
-            auto qt = [&](int i) { return base + L::RING + (i % L::STAGES) * 2 * L::TILE; };
-            auto parity = [&](int i) { return (uint32_t)(i / L::STAGES) & 1u; };
-            bool ok = bar_wait(kv_full, 0, &stalled) && bar_wait(q_full, 0, &stalled);
+            auto qt = [&](int i) { return base + L::X + (i % L::XS) * L::TILE; };
+            auto dt = [&](int i) { return base + L::Y + (i % L::YS) * L::TILE; };
+            auto q_here = [&](int i) { return bar_wait(q_full + 8 * (i % L::XS), (i / L::XS) & 1, &stalled); };
+            auto do_here = [&](int i) { return bar_wait(do_full + 8 * (i % L::YS), (i / L::YS) & 1, &stalled); };
+            bool ok = bar_wait(kv_full, 0, &stalled) && q_here(0);
             if (ok) {
                 fence_after();
                 mul_values<DP>(tmem, base + L::A, qt(0), DESC_S);
                 mma_commit(s_full);
-                ok = bar_wait(do_full, 0, &stalled);
+                ok = do_here(0);
             }
             if (ok) {
                 fence_after();
-                mul_values<DP>(tmem + 128, base + L::B, qt(0) + L::TILE, DESC_S);
+                mul_values<DP>(tmem + 128, base + L::B, dt(0), DESC_S);
                 mma_commit(dp_full);
             }
             for (int i = 0; i < n && ok; ++i) {
-                const int st = i % L::STAGES, nx = (i + 1) % L::STAGES;
                 ok = bar_wait(p_full, i & 1, &stalled);
                 if (!ok) break;
                 fence_after();
-                mul_rows(tmem + 256, tmem, qt(i) + L::TILE, DESC_G, i > 0);
-                mma_commit(do_empty + 8 * st);
+                mul_rows(tmem + 256, tmem, dt(i), DESC_G, i > 0);
+                mma_commit(do_empty + 8 * (i % L::YS));
                 if (i + 1 < n) {
-                    ok = bar_wait(q_full + 8 * nx, parity(i + 1), &stalled);
+                    ok = q_here(i + 1);
                     if (!ok) break;
                     fence_after();
                     mul_values<DP>(tmem, base + L::A, qt(i + 1), DESC_S);
@@ -486,12 +505,12 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 if (!ok) break;
                 fence_after();
                 mul_rows(tmem + 384, tmem + 128, qt(i), DESC_G, i > 0);
-                mma_commit(q_empty + 8 * st);
+                mma_commit(q_empty + 8 * (i % L::XS));
                 if (i + 1 < n) {
-                    ok = bar_wait(do_full + 8 * nx, parity(i + 1), &stalled);
+                    ok = do_here(i + 1);
                     if (!ok) break;
                     fence_after();
-                    mul_values<DP>(tmem + 128, base + L::B, qt(i + 1) + L::TILE, DESC_S);
+                    mul_values<DP>(tmem + 128, base + L::B, dt(i + 1), DESC_S);
                     mma_commit(dp_full);
                 }
             }
@@ -502,7 +521,7 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         // lse (in units of log2; +inf where p is to be 0) and delta of each step's 128 queries
         bool ok = true;
         for (int i = 0; i < n && ok; ++i) {
-            const int st = i % L::STAGES, round = i / L::STAGES;
+            const int st = i % L::SS;
             const int r0 = (first + i % per_head) * T, h = g * a.group + i / per_head;
             const int64_t at = (b * a.q_heads + h) * a.q_len;
             float l[4], d[4];
@@ -513,7 +532,7 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 d[x] = r < s.nq ? a.delta[at + r] : 0.f;
                 if (l[x] == -INFINITY) l[x] = INFINITY;              // a row that sees nothing
             }
-            if (round > 0) ok = __all_sync(0xffffffffu, bar_wait(st_empty + 8 * st, (round - 1) & 1, &stalled));
+            if (i >= L::SS) ok = __all_sync(0xffffffffu, bar_wait(st_empty + 8 * st, (i / L::SS - 1) & 1, &stalled));
             if (!ok) break;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
@@ -536,9 +555,9 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         const uint32_t ts = tmem + lanes + 64 * half, td = ts + 128;
         bool ok = true;
         for (int i = 0; i < n; ++i) {
-            const int st = i % L::STAGES, r0 = (first + i % per_head) * T;
+            const int st = i % L::SS, r0 = (first + i % per_head) * T;
             const float *neg_lse = stats + st * 256 + 64 * half, *neg_delta = neg_lse + 128;
-            ok = __all_sync(0xffffffffu, bar_wait(st_full + 8 * st, (i / L::STAGES) & 1, &stalled) &&
+            ok = __all_sync(0xffffffffu, bar_wait(st_full + 8 * st, (i / L::SS) & 1, &stalled) &&
                                              bar_wait(s_full, i & 1, &stalled));
             if (!ok) break;
             fence_after();
