@@ -1,7 +1,8 @@
 // Forward attention of 16-bit tensors on the fifth-generation tensor cores.
 //
-// One block owns 256 query rows of a head as two tiles of 128 and walks the key tiles (128 keys)
-// that any of them sees.  Roles:
+// A work item is 256 query rows of a head, as two tiles of 128, and the key tiles (128 keys) that any of them
+// sees.  One block per SM goes through its items; loads and products of the next item run while the last
+// one's rows are divided and stored.  Roles:
 //   warps 0-3, 4-7  softmax of tile 0 and tile 1: thread = row.  Scores come from tensor memory,
 //                   probabilities go back there as 16-bit values over the scores they came from
 //   warp 8          one thread issues the tcgen05.mma: S_t = Q_t K^T (both from shared memory) and
@@ -28,7 +29,39 @@ struct FwdSmem {
     static constexpr int TILE = 128 * DP * 2;                   // bytes of one 128-row tile
     static constexpr int SLOTS = DP == 128 ? 4 : 8;
     static constexpr int Q = 0, RING = 2 * TILE, BARS = RING + SLOTS * TILE;
-    static constexpr int BYTES = BARS + 256 + 1024;             // 1024: alignment of the tiles
+    static constexpr int WORDS = BARS + 8 * (13 + 2 * SLOTS);   // stalled, address of the tensor memory
+    static constexpr int BYTES = WORDS + 16;
+};
+
+struct FwdItem {
+    AttnSeq s;
+    int b, h, g, r0;
+    int first[2], last[2];                                      // key tiles of the two row tiles
+    int it0, it1;                                               // of either
+    __device__ __forceinline__ FwdItem(const AttnArgs &a, uint32_t i)
+    {
+        const uint32_t heads = (uint32_t)a.batch * a.q_heads, tile = i / heads, bh = i - tile * heads;
+        b = (int)(bh / (uint32_t)a.q_heads);
+        h = (int)(bh - (uint32_t)b * a.q_heads);
+        g = h / a.group;
+        s = attn_seq(a, b);
+        r0 = ((a.q_len + ROWS - 1) / ROWS - 1 - (int)tile) * ROWS;      // the last rows of a causal bound are the longest
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int rt = r0 + 128 * t, re = min(rt + 128, s.nq);
+            first[t] = last[t] = 0;
+            if (rt < re) {
+                const int lo = attn_lo(a, s, rt), hi = attn_hi(a, s, re - 1);
+                if (lo < hi) {
+                    first[t] = lo / KEYS;
+                    last[t] = (hi + KEYS - 1) / KEYS;
+                }
+            }
+        }
+        const bool any0 = first[0] < last[0], any1 = first[1] < last[1];
+        it0 = any0 ? (any1 ? min(first[0], first[1]) : first[0]) : first[1];
+        it1 = any0 ? (any1 ? max(last[0], last[1]) : last[0]) : last[1];
+    }
 };
 
 struct TcMaps {
@@ -40,49 +73,27 @@ __global__ void __launch_bounds__(384, 1)
 attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps, unsigned long long *stalls)
 {
     using L = FwdSmem<DP>;
-    extern __shared__ uint8_t raw[];
-    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    __shared__ volatile int stalled;
-    __shared__ uint32_t tmem_base;
+    extern __shared__ __align__(1024) uint8_t smem[];           // no static shared memory: this starts at its beginning
+    const uint32_t base = smem_u32(smem);
+    volatile int &stalled = *reinterpret_cast<volatile int *>(smem + L::WORDS);
+    uint32_t &tmem_base = *reinterpret_cast<uint32_t *>(smem + L::WORDS + 4);
     const uint32_t bars = base + L::BARS;
-    const uint32_t q_full = bars, fix = bars + 8, s_full = bars + 16, p_full = bars + 32, o_full = bars + 48,
-                   kv_full = bars + 64, kv_empty = bars + 64 + 8 * L::SLOTS;
+    const uint32_t q_full = bars, q_empty = bars + 8, fix = bars + 16, s_full = bars + 24, p_full = bars + 40, o_full = bars + 56,
+                   o_empty = bars + 72, p_half = bars + 88, kv_full = bars + 104, kv_empty = kv_full + 8 * L::SLOTS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
-    const int64_t heads = a.batch * a.q_heads;
-    const int tiles = (a.q_len + ROWS - 1) / ROWS;
-    const int tile = tiles - 1 - (int)(blockIdx.x / heads);
-    const int64_t bh = blockIdx.x % heads, b = bh / a.q_heads;
-    const int h = (int)(bh % a.q_heads), g = h / a.group;
-    const AttnSeq s = attn_seq(a, b);
-    const int r0 = tile * ROWS;
-
-    // key tiles [first[t], last[t]) of the two row tiles
-    int first[2], last[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int rt = r0 + 128 * t, re = min(rt + 128, s.nq);
-        first[t] = last[t] = 0;
-        if (rt < re) {
-            const int lo = attn_lo(a, s, rt), hi = attn_hi(a, s, re - 1);
-            if (lo < hi) {
-                first[t] = lo / KEYS;
-                last[t] = (hi + KEYS - 1) / KEYS;
-            }
-        }
-    }
-    const bool any0 = first[0] < last[0], any1 = first[1] < last[1];
-    const int it0 = any0 ? (any1 ? min(first[0], first[1]) : first[0]) : first[1];
-    const int it1 = any0 ? (any1 ? max(last[0], last[1]) : last[0]) : last[1];
+    const uint32_t count = (uint32_t)a.batch * a.q_heads * ((a.q_len + ROWS - 1) / ROWS);
 
     if (threadIdx.x == 0) {
         stalled = 0;
         bar_init(q_full, 1);
+        bar_init(q_empty, 1);
         bar_init(fix, 1);
         for (int t = 0; t < 2; ++t) {
             bar_init(s_full + 8 * t, 1);
+            bar_init(p_half + 8 * t, 128);
             bar_init(p_full + 8 * t, 128);
             bar_init(o_full + 8 * t, 1);
+            bar_init(o_empty + 8 * t, 128);
         }
         for (int i = 0; i < L::SLOTS; ++i) {
             bar_init(kv_full + 8 * i, 1);
@@ -106,16 +117,21 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 9) {
-            // ---- loads: Q, then K and V of every key tile through the ring
-            if (it0 < it1) {
-                if (lane == 0) {
+            // ---- loads: Q of each item, K and V of its key tiles through the ring
+            int n = 0, items = 0;                                 // tiles loaded, items begun
+            uint32_t patched = 0;
+            bool ok = true;
+            for (Items i(count); i.more() && ok; i.next()) {
+                const FwdItem w(a, i.at);
+                if (w.it0 >= w.it1) continue;
+                if (items > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty, (items - 1) & 1, &stalled));
+                ++items;
+                if (ok && lane == 0) {
                     bar_expect(q_full, 2 * L::TILE);
-                    load_tile<DP>(base + L::Q, &maps.q, q_full, r0, h, (int)b);
-                    load_tile<DP>(base + L::Q + L::TILE, &maps.q, q_full, r0 + 128, h, (int)b);
+                    load_tile<DP>(base + L::Q, &maps.q, q_full, w.r0, w.h, w.b);
+                    load_tile<DP>(base + L::Q + L::TILE, &maps.q, q_full, w.r0 + 128, w.h, w.b);
                 }
-                int n = 0;
-                bool ok = true;
-                for (int it = it0; it < it1 && ok; ++it) {
+                for (int it = w.it0; it < w.it1 && ok; ++it) {
                     for (int kv = 0; kv < 2 && ok; ++kv, ++n) {
                         const int slot = n % L::SLOTS, round = n / L::SLOTS;
                         if (round > 0) ok = __all_sync(0xffffffffu, bar_wait(kv_empty + 8 * slot, (round - 1) & 1, &stalled));
@@ -123,56 +139,85 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
                         const uint32_t dst = base + L::RING + slot * L::TILE, full = kv_full + 8 * slot;
                         // values past the sequence's end (not past the tensor's, which TMA fills with zeros)
                         // must not meet a zero probability: 0 * NaN.  They are overwritten with zeros.
-                        const bool patch = kv == 1 && s.nk < a.k_len && (it + 1) * KEYS > s.nk;
+                        const bool patch = kv == 1 && w.s.nk < a.k_len && (it + 1) * KEYS > w.s.nk;
                         if (lane == 0) {
                             bar_expect(patch ? fix : full, L::TILE);
-                            load_tile<DP>(dst, kv ? &maps.v : &maps.k, patch ? fix : full, it * KEYS, g, (int)b);
+                            load_tile<DP>(dst, kv ? &maps.v : &maps.k, patch ? fix : full, it * KEYS, w.g, w.b);
                         }
-                            // only ever the last tile: `fix` is used once
-                        if (patch) ok = patch_tile<DP>(dst, s.nk - it * KEYS, fix, 0, full, &stalled);
+                        if (patch) {
+                            ok = patch_tile<DP>(dst, w.s.nk - it * KEYS, fix, patched, full, &stalled);
+                            patched ^= 1;
+                        }
                     }
                 }
             }
         } else if (warp == 8) {
             // ---- products
-            if (lane == 0 && it0 < it1) {
+            {
+                const bool one = elect_one();
                 constexpr uint32_t DESC_S = mma_desc(BF16, 128, KEYS, false), DESC_O = mma_desc(BF16, 128, DP, true);
-                bool ok = bar_wait(q_full, 0, &stalled);
-                int n = 0;                                        // ring position of K of step it; V of it - 1 is n - 1
-                uint32_t p_phase[2] = {0, 0};
-                for (int it = it0; it <= it1 && ok; ++it, n += 2) {
-                    const int ks = n % L::SLOTS, vs = (n + L::SLOTS - 1) % L::SLOTS;
-                    const bool have_k = it < it1, have_v = it > it0;
-                    if (have_v) ok = ok && bar_wait(kv_full + 8 * vs, ((n - 1) / L::SLOTS) & 1, &stalled);
-                    if (have_k) ok = ok && bar_wait(kv_full + 8 * ks, (n / L::SLOTS) & 1, &stalled);
-                    if (!ok) break;
-                    fence_after();
-                    const uint32_t kt = base + L::RING + ks * L::TILE, vt = base + L::RING + vs * L::TILE;
+                int n = 0, items = 0;                             // ring position of K of step it; V of it - 1 is n - 1
+                uint32_t p_phase[2] = {0, 0}, o_used[2] = {0, 0};
+                bool ok = true;
+                for (Items i(count); i.more() && ok; i.next()) {
+                    const FwdItem w(a, i.at);
+                    if (w.it0 >= w.it1) continue;
+                    ok = __all_sync(0xffffffffu, bar_wait(q_full, items & 1, &stalled));
+                    ++items;
+                    for (int it = w.it0; it <= w.it1 && ok; ++it) {
+                        const bool have_k = it < w.it1, have_v = it > w.it0;
+                        const int ks = n % L::SLOTS, vs = (n + L::SLOTS - 1) % L::SLOTS;
+                        if (have_v) ok = bar_wait(kv_full + 8 * vs, ((n - 1) / L::SLOTS) & 1, &stalled);
+                        if (have_k) ok = bar_wait(kv_full + 8 * ks, (n / L::SLOTS) & 1, &stalled) && ok;
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        fence_after();
+                        const uint32_t kt = base + L::RING + ks * L::TILE, vt = base + L::RING + vs * L::TILE;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        if (it - 1 >= first[t] && it - 1 < last[t]) {
-                            ok = ok && bar_wait(p_full + 8 * t, p_phase[t], &stalled);
-                            if (!ok) break;
-                            p_phase[t] ^= 1;
-                            fence_after();
+                        for (int t = 0; t < 2; ++t) {
+                            if (it - 1 >= w.first[t] && it - 1 < w.last[t]) {
+                                ok = bar_wait(p_half + 8 * t, p_phase[t], &stalled);
+                                if (ok && it - 1 == w.first[t] && o_used[t]++ > 0)      // the last item's rows have been read
+                                    ok = bar_wait(o_empty + 8 * t, o_used[t] & 1, &stalled);
+                                ok = __all_sync(0xffffffffu, ok);
+                                if (!ok) break;
+                                const uint64_t v0 = desc_rows(vt, HALF_TILE);
 #pragma unroll
-                            for (int k = 0; k < KEYS / 16; ++k)
-                                mma_ts(tmem + 256 + 128 * t, tmem + 128 * t + 8 * k, desc_rows(vt + 2048 * k, HALF_TILE), DESC_O,
-                                       it - 1 > first[t] || k > 0);
-                            if (it == last[t]) mma_commit(o_full + 8 * t);
-                        }
-                        if (it >= first[t] && it < last[t]) {
+                                for (int part = 0; part < 2; ++part) {
+                                    if (part == 1) ok = __all_sync(0xffffffffu, bar_wait(p_full + 8 * t, p_phase[t], &stalled));
+                                    if (!ok) break;
+                                    fence_after();
+                                    if (one) {
 #pragma unroll
-                            for (int k = 0; k < DP / 16; ++k) {
-                                const uint32_t at = (k / 4) * HALF_TILE + (k % 4) * 32;
-                                mma_ss(tmem + 128 * t, desc_values(base + L::Q + t * L::TILE + at), desc_values(kt + at), DESC_S, k > 0);
+                                        for (int k = part * KEYS / 32; k < (part + 1) * KEYS / 32; ++k)
+                                            mma_ts(tmem + 256 + 128 * t, tmem + 128 * t + 8 * k, v0 + desc_step(2048 * k), DESC_O,
+                                                   it - 1 > w.first[t] || k > 0);
+                                        if (part == 1 && it == w.last[t]) mma_commit(o_full + 8 * t);
+                                    }
+                                }
+                                if (!ok) break;
+                                p_phase[t] ^= 1;
                             }
-                            mma_commit(s_full + 8 * t);
+                            if (it >= w.first[t] && it < w.last[t]) {
+                                if (one) {
+const uint64_t q0 = desc_values(base + L::Q + t * L::TILE), k0 = desc_values(kt);
+#pragma unroll
+                                for (int k = 0; k < DP / 16; ++k) {
+                                    const uint64_t at = desc_step((k / 4) * HALF_TILE + (k % 4) * 32);
+                                    mma_ss(tmem + 128 * t, q0 + at, k0 + at, DESC_S, k > 0);
+                                }
+                                mma_commit(s_full + 8 * t);
+                                }
+                            }
                         }
+                        if (!ok) break;
+                        if (one) {
+                            if (have_v) mma_commit(kv_empty + 8 * vs);
+                            if (have_k) mma_commit(kv_empty + 8 * ks);
+                            if (it + 1 == w.it1) mma_commit(q_empty);
+                        }
+                        if (have_k) n += 2;
                     }
-                    if (!ok) break;
-                    if (have_v) mma_commit(kv_empty + 8 * vs);
-                    if (have_k) mma_commit(kv_empty + 8 * ks);
                 }
             }
             __syncwarp();
@@ -181,18 +226,22 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         // ---- softmax of one row
         const int t = warp >> 2;
-        const int r = r0 + 128 * t + (threadIdx.x & 127);
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const uint32_t ts = tmem + lanes + 128 * t, to = tmem + lanes + 256 + 128 * t;
-        const float mul = a.scale * LOG2E;                      // exponents are taken in base 2
+        const float mul = a.scale * LOG2E;                        // exponents are taken in base 2
+        const bool vec = rows16(a.out, a.dim);
+        bool ok = true;
+        uint32_t phase = 0, o_phase = 0;
+        for (Items i(count); i.more() && ok; i.next()) {
+        const FwdItem w(a, i.at);
+        const AttnSeq &s = w.s;
+        const int r = w.r0 + 128 * t + (threadIdx.x & 127);
         const bool row = r < s.nq;
         const int lo = row ? attn_lo(a, s, r) : 0, hi = row ? attn_hi(a, s, r) : s.nk;
         // tiles that every row of this tile sees whole need no mask
-        const int whole_lo = attn_lo(a, s, min(r0 + 128 * t + 127, max(s.nq - 1, 0))), whole_hi = attn_hi(a, s, r0 + 128 * t);
+        const int whole_lo = attn_lo(a, s, min(w.r0 + 128 * t + 127, max(s.nq - 1, 0))), whole_hi = attn_hi(a, s, w.r0 + 128 * t);
         float top = -INFINITY, sum = 0.f;                         // top: base of the exponents, in units of log2
-        bool ok = true;
-        uint32_t phase = 0;
-        const int it_first = t == 0 ? first[0] : first[1], it_last = t == 0 ? last[0] : last[1];
+        const int it_first = t == 0 ? w.first[0] : w.first[1], it_last = t == 0 ? w.last[0] : w.last[1];
         for (int it = it_first; it < it_last; ++it) {
             ok = __all_sync(0xffffffffu, bar_wait(s_full + 8 * t, phase, &stalled));
             if (!ok) break;
@@ -239,28 +288,32 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
             for (int c = 0; c < KEYS; c += 32) {
                 uint32_t p[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float2 e = fma2(make_float2(x[c + 2 * i], x[c + 2 * i + 1]), mul2v, sub2);
-                    e.x = exp2_fast(e.x);
-                    e.y = exp2_fast(e.y);
-                    acc[i & 1] = add2(acc[i & 1], e);
-                    p[i] = pack2<BF16>(e.x, e.y);
+                for (int k = 0; k < 16; ++k) {
+                    float2 e = fma2(make_float2(x[c + 2 * k], x[c + 2 * k + 1]), mul2v, sub2);
+                    e = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+                    acc[k & 1] = add2(acc[k & 1], e);
+                    p[k] = pack2<BF16>(e.x, e.y);
                 }
                 tmem_st16(ts + c / 2, p);
+                if (c == KEYS / 2 - 32 || c == KEYS - 32) {       // the product with V starts on the first half
+                    wait_st();
+                    fence_before();
+                    bar_arrive((c == KEYS - 32 ? p_full : p_half) + 8 * t);
+                }
             }
-            wait_st();
-            fence_before();
-            bar_arrive(p_full + 8 * t);
             const float2 part = add2(acc[0], acc[1]);
             sum += part.x + part.y;
         }
         const bool some = it_first < it_last;
-        if (ok && some) ok = __all_sync(0xffffffffu, bar_wait(o_full + 8 * t, 0, &stalled));
+        if (ok && some) {
+            ok = __all_sync(0xffffffffu, bar_wait(o_full + 8 * t, o_phase, &stalled));
+            o_phase ^= 1;
+        }
         fence_after();
         const float inv = row && some && sum != 0.f ? 1.f / sum : 0.f;
-        if (r < a.q_len) a.lse[bh * a.q_len + r] = inv != 0.f ? (top + log2f(sum)) * LN2 : -INFINITY;
-        uint16_t *out = reinterpret_cast<uint16_t *>(a.out.p) + b * a.out.sb + (int64_t)r * a.out.sl + h * a.out.sh;
-        const bool vec = rows16(a.out, a.dim);
+        if (r < a.q_len)
+            a.lse[((int64_t)w.b * a.q_heads + w.h) * a.q_len + r] = inv != 0.f ? (top + log2f(sum)) * LN2 : -INFINITY;
+        uint16_t *out = reinterpret_cast<uint16_t *>(a.out.p) + w.b * a.out.sb + (int64_t)r * a.out.sl + w.h * a.out.sh;
 #pragma unroll
         for (int c = 0; c < DP; c += 32) {
             float o[32];
@@ -268,8 +321,13 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
             if (some && ok) {
                 tmem_ld32(to + c, reinterpret_cast<uint32_t *>(o));
                 wait_ld();
+                if (c + 32 == DP) {
+                    fence_before();
+                    bar_arrive(o_empty + 8 * t);
+                }
             }
             if (r < a.q_len) store32<BF16>(out, c, a.dim, vec, o, inv);
+        }
         }
     }
 
@@ -332,16 +390,17 @@ gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_
 template <bool BF16, int DP>
 static gs_status forward_t(const AttnArgs &a, const TcMaps &maps, cudaStream_t st)
 {
-    const int64_t blocks = a.batch * a.q_heads * ((a.q_len + ROWS - 1) / ROWS);
-    if (blocks > 0x7FFFFFFF) {
-        set_error("attention of %lld row tiles exceeds one launch", (long long)blocks);
+    const int64_t items = a.batch * a.q_heads * ((a.q_len + ROWS - 1) / ROWS);
+    if (items > 0x7FFFFFFF) {
+        set_error("attention of %lld row tiles exceeds one launch", (long long)items);
         return GS_ERR_UNSUPPORTED;
     }
     auto kernel = attn_tc_forward_kernel<BF16, DP>;
     static SharedRecord record;
     gs_status s = allow_shared(kernel, FwdSmem<DP>::BYTES, record);
     if (s != GS_OK) return s;
-    kernel<<<(unsigned)blocks, 384, FwdSmem<DP>::BYTES, st>>>(a, maps, stall_counter());
+    const int64_t sms = sm_count();
+    kernel<<<(unsigned)(items < sms ? items : sms), 384, FwdSmem<DP>::BYTES, st>>>(a, maps, stall_counter());
     GS_CUDA_TRY(cudaGetLastError());
     return GS_OK;
 }

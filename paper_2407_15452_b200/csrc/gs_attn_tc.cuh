@@ -15,6 +15,19 @@ gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_
 static constexpr int HALF_TILE = 128 * 128;          // bytes of one box: 128 rows of 64 16-bit values
 static constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
+// The work items of one persistent block.  Items are sorted from the longest to the shortest; rounds over the
+// blocks alternate their direction, which evens out what a block gets.
+struct Items {
+    uint32_t n, at, step;
+    __device__ __forceinline__ explicit Items(uint32_t count) : n(count), at(blockIdx.x), step(2 * (gridDim.x - blockIdx.x) - 1) {}
+    __device__ __forceinline__ bool more() const { return at < n; }
+    __device__ __forceinline__ void next()
+    {
+        at += step;
+        step = 2 * gridDim.x - step;
+    }
+};
+
 // One 128-row tile of DP values into shared memory at `dst` (DP / 64 boxes)
 template <int DP>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, uint32_t bar, int pos, int head, int b)

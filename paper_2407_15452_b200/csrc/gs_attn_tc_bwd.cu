@@ -51,19 +51,21 @@ struct BwdSmem {
 template <int DP>
 __device__ __forceinline__ void mul_values(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc)
 {
+    const uint64_t a0 = desc_values(a), b0 = desc_values(b);
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k) {
-        const uint32_t at = (k / 4) * HALF_TILE + (k % 4) * 32;
-        mma_ss(d, desc_values(a + at), desc_values(b + at), idesc, k > 0);
+        const uint64_t at = desc_step((k / 4) * HALF_TILE + (k % 4) * 32);
+        mma_ss(d, a0 + at, b0 + at, idesc, k > 0);
     }
 }
 
 // D[128 x DP] += A B, A 128 x 128 in tensor memory (two halves of 32 columns, 64 apart), B [rows][values]
 __device__ __forceinline__ void mul_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add)
 {
+    const uint64_t b0 = desc_rows(b, HALF_TILE);
 #pragma unroll
     for (int k = 0; k < T / 16; ++k)
-        mma_ts(d, a + (k / 4) * 64 + (k % 4) * 8, desc_rows(b + 2048 * k, HALF_TILE), idesc, add || k > 0);
+        mma_ts(d, a + (k / 4) * 64 + (k % 4) * 8, b0 + desc_step(2048 * k), idesc, add || k > 0);
 }
 
 __device__ __forceinline__ float warp_max(float v)
@@ -247,46 +249,57 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
             }
         }
     } else if (warp == 8) {
-        if (lane == 0 && n > 0) {
+        if (n > 0) {
+            const bool one = elect_one();
             constexpr uint32_t DESC_S = mma_desc(BF16, T, T, false), DESC_Q = mma_desc(BF16, T, DP, true);
             auto kt = [&](int i) { return base + L::X + (i % L::XS) * L::TILE; };
             auto vt = [&](int i) { return base + L::Y + (i % L::YS) * L::TILE; };
             auto k_here = [&](int i) { return bar_wait(k_full + 8 * (i % L::XS), (i / L::XS) & 1, &stalled); };
             auto v_here = [&](int i) { return bar_wait(v_full + 8 * (i % L::YS), (i / L::YS) & 1, &stalled); };
-            bool ok = bar_wait(q_full, 0, &stalled) && k_here(0);
+            bool ok = __all_sync(0xffffffffu, bar_wait(q_full, 0, &stalled) && k_here(0));
             if (ok) {
                 fence_after();
-                mul_values<DP>(tmem, base + L::A, kt(0), DESC_S);
-                mma_commit(s_full);
-                ok = v_here(0);
+                if (one) {
+                    mul_values<DP>(tmem, base + L::A, kt(0), DESC_S);
+                    mma_commit(s_full);
+                }
+                ok = __all_sync(0xffffffffu, v_here(0));
             }
             if (ok) {
                 fence_after();
-                mul_values<DP>(tmem + 256, base + L::B, vt(0), DESC_S);
-                mma_commit(dp_full);
-                mma_commit(v_empty);
+                if (one) {
+                    mul_values<DP>(tmem + 256, base + L::B, vt(0), DESC_S);
+                    mma_commit(dp_full);
+                    mma_commit(v_empty);
+                }
             }
             for (int i = 0; i < n && ok; ++i) {
                 if (i + 1 < n) {                      // the other S: its dS went into dQ(i - 1), issued before
-                    ok = k_here(i + 1);
+                    ok = __all_sync(0xffffffffu, k_here(i + 1));
                     if (!ok) break;
                     fence_after();
-                    mul_values<DP>(tmem + 128 * ((i + 1) & 1), base + L::A, kt(i + 1), DESC_S);
-                    mma_commit(s_full + 8 * ((i + 1) & 1));
-                    ok = v_here(i + 1) && bar_wait(dp_free, i & 1, &stalled);
+                    if (one) {
+                        mul_values<DP>(tmem + 128 * ((i + 1) & 1), base + L::A, kt(i + 1), DESC_S);
+                        mma_commit(s_full + 8 * ((i + 1) & 1));
+                    }
+                    ok = __all_sync(0xffffffffu, v_here(i + 1) && bar_wait(dp_free, i & 1, &stalled));
                     if (!ok) break;
                     fence_after();
-                    mul_values<DP>(tmem + 256, base + L::B, vt(i + 1), DESC_S);
-                    mma_commit(dp_full);
-                    mma_commit(v_empty + 8 * ((i + 1) % L::YS));
+                    if (one) {
+                        mul_values<DP>(tmem + 256, base + L::B, vt(i + 1), DESC_S);
+                        mma_commit(dp_full);
+                        mma_commit(v_empty + 8 * ((i + 1) % L::YS));
+                    }
                 }
-                ok = bar_wait(ds_full, i & 1, &stalled);
+                ok = __all_sync(0xffffffffu, bar_wait(ds_full, i & 1, &stalled));
                 if (!ok) break;
                 fence_after();
-                mul_rows(tmem + 384, tmem + 128 * (i & 1), kt(i), DESC_Q, i > 0);
-                mma_commit(k_empty + 8 * (i % L::XS));
+                if (one) {
+                    mul_rows(tmem + 384, tmem + 128 * (i & 1), kt(i), DESC_Q, i > 0);
+                    mma_commit(k_empty + 8 * (i % L::XS));
+                }
             }
-            if (ok) mma_commit(done);
+            if (ok && one) mma_commit(done);
         }
         __syncwarp();
     } else if (warp < 8) {
@@ -470,51 +483,64 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             }
         }
     } else if (warp == 8) {
-        if (lane == 0 && n > 0) {
+        if (n > 0) {
+            const bool one = elect_one();
             constexpr uint32_t DESC_S = mma_desc(BF16, T, T, false), DESC_G = mma_desc(BF16, T, DP, true);
             auto qt = [&](int i) { return base + L::X + (i % L::XS) * L::TILE; };
             auto dt = [&](int i) { return base + L::Y + (i % L::YS) * L::TILE; };
             auto q_here = [&](int i) { return bar_wait(q_full + 8 * (i % L::XS), (i / L::XS) & 1, &stalled); };
             auto do_here = [&](int i) { return bar_wait(do_full + 8 * (i % L::YS), (i / L::YS) & 1, &stalled); };
-            bool ok = bar_wait(kv_full, 0, &stalled) && q_here(0);
+            bool ok = __all_sync(0xffffffffu, bar_wait(kv_full, 0, &stalled) && q_here(0));
             if (ok) {
                 fence_after();
-                mul_values<DP>(tmem, base + L::A, qt(0), DESC_S);
-                mma_commit(s_full);
-                ok = do_here(0);
-            }
-            if (ok) {
-                fence_after();
-                mul_values<DP>(tmem + 128, base + L::B, dt(0), DESC_S);
-                mma_commit(dp_full);
-            }
-            for (int i = 0; i < n && ok; ++i) {
-                ok = bar_wait(p_full, i & 1, &stalled);
-                if (!ok) break;
-                fence_after();
-                mul_rows(tmem + 256, tmem, dt(i), DESC_G, i > 0);
-                mma_commit(do_empty + 8 * (i % L::YS));
-                if (i + 1 < n) {
-                    ok = q_here(i + 1);
-                    if (!ok) break;
-                    fence_after();
-                    mul_values<DP>(tmem, base + L::A, qt(i + 1), DESC_S);
+                if (one) {
+                    mul_values<DP>(tmem, base + L::A, qt(0), DESC_S);
                     mma_commit(s_full);
                 }
-                ok = bar_wait(ds_full, i & 1, &stalled);
-                if (!ok) break;
+                ok = __all_sync(0xffffffffu, do_here(0));
+            }
+            if (ok) {
                 fence_after();
-                mul_rows(tmem + 384, tmem + 128, qt(i), DESC_G, i > 0);
-                mma_commit(q_empty + 8 * (i % L::XS));
-                if (i + 1 < n) {
-                    ok = do_here(i + 1);
-                    if (!ok) break;
-                    fence_after();
-                    mul_values<DP>(tmem + 128, base + L::B, dt(i + 1), DESC_S);
+                if (one) {
+                    mul_values<DP>(tmem + 128, base + L::B, dt(0), DESC_S);
                     mma_commit(dp_full);
                 }
             }
-            if (ok) mma_commit(done);
+            for (int i = 0; i < n && ok; ++i) {
+                ok = __all_sync(0xffffffffu, bar_wait(p_full, i & 1, &stalled));
+                if (!ok) break;
+                fence_after();
+                if (one) {
+                    mul_rows(tmem + 256, tmem, dt(i), DESC_G, i > 0);
+                    mma_commit(do_empty + 8 * (i % L::YS));
+                }
+                if (i + 1 < n) {
+                    ok = __all_sync(0xffffffffu, q_here(i + 1));
+                    if (!ok) break;
+                    fence_after();
+                    if (one) {
+                        mul_values<DP>(tmem, base + L::A, qt(i + 1), DESC_S);
+                        mma_commit(s_full);
+                    }
+                }
+                ok = __all_sync(0xffffffffu, bar_wait(ds_full, i & 1, &stalled));
+                if (!ok) break;
+                fence_after();
+                if (one) {
+                    mul_rows(tmem + 384, tmem + 128, qt(i), DESC_G, i > 0);
+                    mma_commit(q_empty + 8 * (i % L::XS));
+                }
+                if (i + 1 < n) {
+                    ok = __all_sync(0xffffffffu, do_here(i + 1));
+                    if (!ok) break;
+                    fence_after();
+                    if (one) {
+                        mul_values<DP>(tmem + 128, base + L::B, dt(i + 1), DESC_S);
+                        mma_commit(dp_full);
+                    }
+                }
+            }
+            if (ok && one) mma_commit(done);
         }
         __syncwarp();
     } else if (warp == 10) {
