@@ -2,21 +2,22 @@
 // compute the scores again, so that every gradient has one owner and no value is summed with atomics
 // (seven products of 128 x 128 tiles where a single kernel with atomics on dq needs five).
 //
-//  dq     : one block per 128 query rows.  S = Q K^T, dP = dO V^T, dS = P (dP - delta), dQ += dS K.
+//  dq     : an item is 128 query rows.  S = Q K^T, dP = dO V^T, dS = P (dP - delta), dQ += dS K.
 //           Thread = query row; S of the next keys is computed while this one's dS is formed, dP's columns are
-//           free for the next product as soon as they are in registers.  Leaves delta = dO.O for the other kernel.
-//  dk, dv : one block per 128 keys, looping over the query heads of their group and their query tiles.
+//           free for the next product as soon as they are in registers.
+//  dk, dv : an item is 128 keys, with the query heads of their group and their query tiles.
 //           Everything transposed: S^T = K Q^T, dP^T = V dO^T, so that P^T and dS^T come out with one key per
 //           lane and feed dV += P^T dO, dK += dS^T Q from tensor memory without passing through shared memory.
 //           Tensor memory is full (S^T, dP^T, dV, dK: 128 columns each); the order dV(i), S^T(i+1) while dS(i)
 //           is formed, then dK(i), dP^T(i+1) while P(i+1) is formed, keeps both sides busy.
-// In both, eight warps do the elementwise part, four per 64 columns of a tile; a warp overwrites only
-// columns that it has read itself.  Warp 8 issues the products, warp 9 the loads, warp 10 brings the
-// row statistics of dk/dv's query tiles.
+// One block per SM goes through its items, the longest first; loads and products of the next item run while
+// the last one's results are stored.  Eight warps do the elementwise part, four per 64 columns of a tile; a
+// warp overwrites only columns that it has read itself.  Warp 8 issues the products, warp 9 the loads, warp 10
+// brings the row statistics.  A first kernel works out delta = dO.O.
 //
 // P and dS are rounded to the tensors' type for their products.  binary16 has no range for that as it
 // stands: P is scaled by 2^15 (P <= 1), dS by the power of two that brings its bound
-// |dS| <= 2 max|do| max|v| (row norms) near 2^15; the bound needs a pass over dO and V, for binary16 only.
+// |dS| <= 2 max|do| max|v| (row norms) near 2^15; the first kernel finds the norms too then.
 #include "gs_attn_tc.cuh"
 
 namespace gs {
@@ -40,9 +41,10 @@ struct BwdSmem {
     // dk/dv), Y for the other.  Three X tiles, because one is free only when its step's last product is done.
     static constexpr int XS = DP == 128 ? 3 : 4, YS = DP == 128 ? 2 : 4, SS = 2;
     static constexpr int A = 0, B = TILE, X = 2 * TILE, Y = X + XS * TILE;
-    static constexpr int STATS = Y + YS * TILE;                 // dk/dv: lse and delta of a query tile, SS of them
-    static constexpr int BARS = STATS + SS * 2 * T * 4;
-    static constexpr int WORDS = BARS + 8 * (10 + 2 * XS + 2 * YS + 2 * SS);    // stalled, address of the tensor memory
+    static constexpr int STATS = Y + YS * TILE;                 // SS of: -lse (log2) and -delta of a query tile, scale of dS
+    static constexpr int STAT = 2 * T + 4;                      // floats of one
+    static constexpr int BARS = STATS + SS * STAT * 4;
+    static constexpr int WORDS = BARS + 8 * (12 + 2 * XS + 2 * YS + 2 * SS);    // stalled, address of the tensor memory
     static constexpr int BYTES = WORDS + 16;
     static_assert(BYTES <= 227 * 1024, "shared memory of one block");
 };
@@ -91,40 +93,6 @@ __device__ __forceinline__ float ds_scale(const AttnArgs &a, const BwdNorms &nm,
     return ldexpf(1.f, min(max(15 - e, -100), 100));
 }
 
-// largest row norm of each 128-row tile of dO and V.  Block: one tile; a warp takes every fourth row.
-__global__ void __launch_bounds__(128) attn_tc_norms_kernel(const __grid_constant__ AttnArgs a, BwdNorms nm)
-{
-    const int qt = (a.q_len + T - 1) / T, kt = (a.k_len + T - 1) / T;
-    int64_t i = blockIdx.x;
-    const int64_t nq = a.batch * a.q_heads * qt;
-    const bool on_q = i < nq;
-    if (!on_q) i -= nq;
-    const int tiles = on_q ? qt : kt, nh = on_q ? a.q_heads : a.kv_heads;
-    const int tile = (int)(i % tiles);
-    const int64_t bh = i / tiles, b = bh / nh;
-    const int h = (int)(bh % nh);
-    const AttnTensor &t = on_q ? a.dout : a.v;
-    const AttnSeq s = attn_seq(a, b);
-    const int end = min((tile + 1) * T, on_q ? s.nq : s.nk), lane = threadIdx.x & 31;
-    const __half *base = reinterpret_cast<const __half *>(t.p) + b * t.sb + h * t.sh;
-    float top = 0.f;
-    for (int r = tile * T + (threadIdx.x >> 5); r < end; r += 4) {
-        float x = 0.f;
-        for (int c = lane; c < a.dim; c += 32) {
-            const float v = __half2float(base[(int64_t)r * t.sl + c]);
-            x = fmaf(v, v, x);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-        top = fmaxf(top, x);
-    }
-    __shared__ float sh[4];
-    if (lane == 0) sh[threadIdx.x >> 5] = top;
-    __syncthreads();
-    if (threadIdx.x == 0)
-        (on_q ? nm.dout : nm.v)[i] = sqrtf(fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3])));
-}
-
 template <bool BF16>
 __device__ __forceinline__ float2 unpack2(uint32_t u)
 {
@@ -132,37 +100,109 @@ __device__ __forceinline__ float2 unpack2(uint32_t u)
     else return __half22float2(*reinterpret_cast<__half2 *>(&u));
 }
 
-// dot product of two rows of 16-bit values in global memory; 128 bytes of each are on their way at a time
-template <bool BF16, int DP>
-__device__ __forceinline__ float dot16(const uint16_t *x, const uint16_t *y, int dim, bool vec)
+// dot product of the first min(8, n) values at two addresses, 16-byte aligned
+template <bool BF16>
+__device__ __forceinline__ float dot8(const uint16_t *x, const uint16_t *y, int n)
 {
     float d = 0.f;
-    if (vec) {
+    if (n >= 8) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(x)), w = __ldg(reinterpret_cast<const uint4 *>(y));
+        const uint32_t p[4] = {u.x, u.y, u.z, u.w}, q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int c0 = 0; c0 < DP; c0 += 64) {
-            uint4 u[8], w[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const bool in = c0 + 8 * k < dim;
-                u[k] = in ? __ldg(reinterpret_cast<const uint4 *>(x + c0 + 8 * k)) : make_uint4(0, 0, 0, 0);
-                w[k] = in ? __ldg(reinterpret_cast<const uint4 *>(y + c0 + 8 * k)) : make_uint4(0, 0, 0, 0);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const uint32_t p[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, q[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 f = unpack2<BF16>(p[i]), g = unpack2<BF16>(q[i]);
-                    d = fmaf(f.x, g.x, d);
-                    d = fmaf(f.y, g.y, d);
-                }
-            }
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2<BF16>(p[i]), g = unpack2<BF16>(q[i]);
+            d = fmaf(f.x, g.x, d);
+            d = fmaf(f.y, g.y, d);
         }
     } else {
-        for (int c = 0; c < dim; ++c) d = fmaf(unpack2<BF16>(x[c]).x, unpack2<BF16>(y[c]).x, d);
+        for (int i = 0; i < n; ++i) d = fmaf(unpack2<BF16>(x[i]).x, unpack2<BF16>(y[i]).x, d);
     }
     return d;
 }
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// Before the products: delta = dO.O of every query row and, for binary16, the largest row norm of each 128-row tile
+// of dO and V.  One block per tile, DP / 8 lanes per row, all of a thread's loads on their way at once.
+template <bool BF16, int DP>
+__global__ void __launch_bounds__(256) attn_tc_prepare_kernel(const __grid_constant__ AttnArgs a, BwdNorms nm)
+{
+    constexpr int LANES = DP / 8, STEP = 256 / LANES, ROUNDS = T / STEP;
+    const int qt = (a.q_len + T - 1) / T, kt = (a.k_len + T - 1) / T;
+    int64_t i = blockIdx.x;
+    const int64_t nq = a.batch * a.q_heads * qt;
+    const bool on_q = i < nq;
+    if (!on_q) i -= nq;                                         // only binary16 has these blocks
+    const int tiles = on_q ? qt : kt, nh = on_q ? a.q_heads : a.kv_heads;
+    const int tile = (int)(i % tiles);
+    const int64_t bh = i / tiles, b = bh / nh;
+    const int h = (int)(bh % nh);
+    const AttnSeq s = attn_seq(a, b);
+    const int end = on_q ? s.nq : s.nk, col = ((int)threadIdx.x % LANES) * 8, n = a.dim - col;
+    const AttnTensor &t = on_q ? a.dout : a.v;                  // both can be read by TMA: rows are aligned to 16 bytes
+    const uint16_t *x = reinterpret_cast<const uint16_t *>(t.p) + b * t.sb + h * t.sh + col;
+    const uint16_t *o = reinterpret_cast<const uint16_t *>(a.out.p) + b * a.out.sb + h * a.out.sh + col;
+    const bool vec = rows16(a.out, a.dim);
+    float top = 0.f, delta[ROUNDS], norm[ROUNDS];
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+        const int r = tile * T + (int)threadIdx.x / LANES + k * STEP;
+        delta[k] = norm[k] = 0.f;
+        if (r < end) {
+            const uint16_t *y = x + (int64_t)r * t.sl, *z = o + (int64_t)r * a.out.sl;
+            if (!BF16) norm[k] = dot8<BF16>(y, y, n);
+            if (on_q && vec) delta[k] = dot8<BF16>(y, z, n);
+            else if (on_q)
+                for (int e = 0; e < min(8, n); ++e) delta[k] = fmaf(unpack2<BF16>(y[e]).x, unpack2<BF16>(z[e]).x, delta[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+        const int r = tile * T + (int)threadIdx.x / LANES + k * STEP;
+        if (!BF16) top = fmaxf(top, lanes_sum<LANES>(norm[k]));
+        const float d = lanes_sum<LANES>(delta[k]);
+        if (on_q && threadIdx.x % LANES == 0 && r < a.q_len) a.delta[bh * a.q_len + r] = d;
+    }
+    if constexpr (!BF16) {
+        __shared__ float sh[8];
+        top = warp_max(top);
+        if (threadIdx.x % 32 == 0) sh[threadIdx.x >> 5] = top;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int w = 0; w < 8; ++w) top = fmaxf(top, sh[w]);
+            (on_q ? nm.dout : nm.v)[i] = sqrtf(top);
+        }
+    }
+}
+
+struct DqItem {
+    AttnSeq s;
+    int b, h, g, r0;
+    int first, n;                                               // key tiles
+    __device__ __forceinline__ DqItem(const AttnArgs &a, uint32_t i)
+    {
+        const uint32_t heads = (uint32_t)a.batch * a.q_heads, tile = i / heads, bh = i - tile * heads;
+        b = (int)(bh / (uint32_t)a.q_heads);
+        h = (int)(bh - (uint32_t)b * a.q_heads);
+        g = h / a.group;
+        s = attn_seq(a, b);
+        r0 = ((a.q_len + T - 1) / T - 1 - (int)tile) * T;       // the last rows of a causal bound are the longest
+        first = n = 0;
+        if (r0 < s.nq) {
+            const int lo = attn_lo(a, s, r0), hi = attn_hi(a, s, min(r0 + T, s.nq) - 1);
+            if (lo < hi) {
+                first = lo / T;
+                n = (hi + T - 1) / T - first;
+            }
+        }
+    }
+};
 
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(384, 1)
@@ -172,32 +212,21 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
     using L = BwdSmem<DP>;
     extern __shared__ __align__(1024) uint8_t smem[];           // no static shared memory: this starts at its beginning
     const uint32_t base = smem_u32(smem);
+    float *stats = reinterpret_cast<float *>(smem + L::STATS);
     volatile int &stalled = *reinterpret_cast<volatile int *>(smem + L::WORDS);
     uint32_t &tmem_base = *reinterpret_cast<uint32_t *>(smem + L::WORDS + 4);
     const uint32_t bars = base + L::BARS;
-    const uint32_t q_full = bars, fix = bars + 8, s_full = bars + 16, dp_full = bars + 32, dp_free = bars + 40,
-                   ds_full = bars + 48, done = bars + 56, k_full = bars + 80, k_empty = k_full + 8 * L::XS,
-                   v_full = k_empty + 8 * L::XS, v_empty = v_full + 8 * L::YS;
+    const uint32_t q_full = bars, q_empty = bars + 8, fix = bars + 16, s_full = bars + 24, dp_full = bars + 40, dp_free = bars + 48,
+                   ds_full = bars + 56, done = bars + 64, dq_empty = bars + 72, k_full = bars + 96, k_empty = k_full + 8 * L::XS,
+                   v_full = k_empty + 8 * L::XS, v_empty = v_full + 8 * L::YS, st_full = v_empty + 8 * L::YS,
+                   st_empty = st_full + 8 * L::SS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
-    const int64_t heads = a.batch * a.q_heads;
-    const int tiles = (a.q_len + T - 1) / T;
-    const int r0 = (tiles - 1 - (int)(blockIdx.x / heads)) * T;     // the longest rows of a causal bound go first
-    const int64_t bh = blockIdx.x % heads, b = bh / a.q_heads;
-    const int h = (int)(bh % a.q_heads), g = h / a.group;
-    const AttnSeq s = attn_seq(a, b);
-    int first = 0, n = 0;
-    if (r0 < s.nq) {
-        const int lo = attn_lo(a, s, r0), hi = attn_hi(a, s, min(r0 + T, s.nq) - 1);
-        if (lo < hi) {
-            first = lo / T;
-            n = (hi + T - 1) / T - first;
-        }
-    }
+    const uint32_t count = (uint32_t)a.batch * a.q_heads * ((a.q_len + T - 1) / T);
 
     if (threadIdx.x == 0) {
         stalled = 0;
         bar_init(q_full, 1);
+        bar_init(q_empty, 1);
         bar_init(fix, 1);
         bar_init(s_full, 1);
         bar_init(s_full + 8, 1);
@@ -205,7 +234,12 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
         bar_init(dp_free, 256);
         bar_init(ds_full, 256);
         bar_init(done, 1);
+        bar_init(dq_empty, 256);
         for (int i = 0; i < 2 * (L::XS + L::YS); ++i) bar_init(k_full + 8 * i, 1);
+        for (int i = 0; i < L::SS; ++i) {
+            bar_init(st_full + 8 * i, 32);
+            bar_init(st_empty + 8 * i, 256);
+        }
         fence_barrier_init();
     }
     if (warp == 8) tmem_alloc(smem_u32(&tmem_base), 512);
@@ -220,161 +254,197 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
     fence_after();
     const uint32_t tmem = tmem_base;                  // S of even and odd steps, dP, dQ
 
+    // c counts a block's steps (key tiles) over all its items, t the items that have any
+    bool ok = true;
+    int c = 0, t = 0;
     if (warp == 9) {
-        if (n > 0) {
-            if (lane == 0) {
+        uint32_t patched = 0;
+        for (Items it(count); it.more() && ok; it.next()) {
+            const DqItem w(a, it.at);
+            if (w.n == 0) continue;
+            if (t > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty, (t - 1) & 1, &stalled));
+            ++t;
+            if (ok && lane == 0) {
                 bar_expect(q_full, 2 * L::TILE);
-                load_tile<DP>(base + L::A, &maps.q, q_full, r0, h, (int)b);
-                load_tile<DP>(base + L::B, &maps.dout, q_full, r0, h, (int)b);
+                load_tile<DP>(base + L::A, &maps.q, q_full, w.r0, w.h, w.b);
+                load_tile<DP>(base + L::B, &maps.dout, q_full, w.r0, w.h, w.b);
             }
-            bool ok = true;
-            for (int i = 0; i < n && ok; ++i) {
-                const int kst = i % L::XS, vst = i % L::YS, j0 = (first + i) * T;
+            for (int i = 0; i < w.n && ok; ++i, ++c) {
+                const int kst = c % L::XS, vst = c % L::YS, j0 = (w.first + i) * T;
                 const uint32_t kt = base + L::X + kst * L::TILE, vt = base + L::Y + vst * L::TILE;
-                const bool patch = s.nk < a.k_len && j0 + T > s.nk;        // K is summed over its rows in dS K
-                if (i >= L::XS) ok = __all_sync(0xffffffffu, bar_wait(k_empty + 8 * kst, (i / L::XS - 1) & 1, &stalled));
+                const bool patch = w.s.nk < a.k_len && j0 + T > w.s.nk;        // K is summed over its rows in dS K
+                if (c >= L::XS) ok = __all_sync(0xffffffffu, bar_wait(k_empty + 8 * kst, (c / L::XS - 1) & 1, &stalled));
                 if (!ok) break;
                 if (lane == 0) {
                     const uint32_t bar = patch ? fix : k_full + 8 * kst;
                     bar_expect(bar, L::TILE);
-                    load_tile<DP>(kt, &maps.k, bar, j0, g, (int)b);
+                    load_tile<DP>(kt, &maps.k, bar, j0, w.g, w.b);
                 }
-                if (i >= L::YS) ok = __all_sync(0xffffffffu, bar_wait(v_empty + 8 * vst, (i / L::YS - 1) & 1, &stalled));
+                if (c >= L::YS) ok = __all_sync(0xffffffffu, bar_wait(v_empty + 8 * vst, (c / L::YS - 1) & 1, &stalled));
                 if (!ok) break;
                 if (lane == 0) {
                     bar_expect(v_full + 8 * vst, L::TILE);
-                    load_tile<DP>(vt, &maps.v, v_full + 8 * vst, j0, g, (int)b);
+                    load_tile<DP>(vt, &maps.v, v_full + 8 * vst, j0, w.g, w.b);
                 }
-                if (patch) ok = patch_tile<DP>(kt, s.nk - j0, fix, 0, k_full + 8 * kst, &stalled);
+                if (patch) {
+                    ok = patch_tile<DP>(kt, w.s.nk - j0, fix, patched, k_full + 8 * kst, &stalled);
+                    patched ^= 1;
+                }
             }
         }
     } else if (warp == 8) {
-        if (n > 0) {
-            const bool one = elect_one();
-            constexpr uint32_t DESC_S = mma_desc(BF16, T, T, false), DESC_Q = mma_desc(BF16, T, DP, true);
-            auto kt = [&](int i) { return base + L::X + (i % L::XS) * L::TILE; };
-            auto vt = [&](int i) { return base + L::Y + (i % L::YS) * L::TILE; };
-            auto k_here = [&](int i) { return bar_wait(k_full + 8 * (i % L::XS), (i / L::XS) & 1, &stalled); };
-            auto v_here = [&](int i) { return bar_wait(v_full + 8 * (i % L::YS), (i / L::YS) & 1, &stalled); };
-            bool ok = __all_sync(0xffffffffu, bar_wait(q_full, 0, &stalled) && k_here(0));
-            if (ok) {
-                fence_after();
-                if (one) {
-                    mul_values<DP>(tmem, base + L::A, kt(0), DESC_S);
-                    mma_commit(s_full);
-                }
-                ok = __all_sync(0xffffffffu, v_here(0));
+        const bool one = elect_one();
+        constexpr uint32_t DESC_S = mma_desc(BF16, T, T, false), DESC_Q = mma_desc(BF16, T, DP, true);
+        auto kt = [&](int x) { return base + L::X + (x % L::XS) * L::TILE; };
+        // S and dP of step x
+        auto scores = [&](int x) {
+            ok = __all_sync(0xffffffffu, bar_wait(k_full + 8 * (x % L::XS), (x / L::XS) & 1, &stalled));
+            if (!ok) return;
+            fence_after();
+            if (one) {                                // this S: its last dS went into dQ(x - 2), issued before
+                mul_values<DP>(tmem + 128 * (x & 1), base + L::A, kt(x), DESC_S);
+                mma_commit(s_full + 8 * (x & 1));
             }
-            if (ok) {
-                fence_after();
-                if (one) {
-                    mul_values<DP>(tmem + 256, base + L::B, vt(0), DESC_S);
-                    mma_commit(dp_full);
-                    mma_commit(v_empty);
-                }
+            ok = bar_wait(v_full + 8 * (x % L::YS), (x / L::YS) & 1, &stalled);
+            if (x > 0) ok = bar_wait(dp_free, (x - 1) & 1, &stalled) && ok;
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return;
+            fence_after();
+            if (one) {
+                mul_values<DP>(tmem + 256, base + L::B, base + L::Y + (x % L::YS) * L::TILE, DESC_S);
+                mma_commit(dp_full);
+                mma_commit(v_empty + 8 * (x % L::YS));
             }
-            for (int i = 0; i < n && ok; ++i) {
-                if (i + 1 < n) {                      // the other S: its dS went into dQ(i - 1), issued before
-                    ok = __all_sync(0xffffffffu, k_here(i + 1));
-                    if (!ok) break;
-                    fence_after();
-                    if (one) {
-                        mul_values<DP>(tmem + 128 * ((i + 1) & 1), base + L::A, kt(i + 1), DESC_S);
-                        mma_commit(s_full + 8 * ((i + 1) & 1));
-                    }
-                    ok = __all_sync(0xffffffffu, v_here(i + 1) && bar_wait(dp_free, i & 1, &stalled));
-                    if (!ok) break;
-                    fence_after();
-                    if (one) {
-                        mul_values<DP>(tmem + 256, base + L::B, vt(i + 1), DESC_S);
-                        mma_commit(dp_full);
-                        mma_commit(v_empty + 8 * ((i + 1) % L::YS));
-                    }
-                }
-                ok = __all_sync(0xffffffffu, bar_wait(ds_full, i & 1, &stalled));
+        };
+        for (Items it(count); it.more() && ok; it.next()) {
+            const DqItem w(a, it.at);
+            if (w.n == 0) continue;
+            ok = __all_sync(0xffffffffu, bar_wait(q_full, t & 1, &stalled));
+            if (ok) scores(c);
+            for (int i = 0; i < w.n && ok; ++i, ++c) {
+                if (i + 1 < w.n) scores(c + 1);
+                if (i == max(w.n - 2, 0) && ok && one) mma_commit(q_empty);       // Q and dO have met all their keys
+                if (ok) ok = bar_wait(ds_full, c & 1, &stalled);
+                if (i == 0 && t > 0) ok = bar_wait(dq_empty, (t - 1) & 1, &stalled) && ok;      // the last item's dQ has been read
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 fence_after();
                 if (one) {
-                    mul_rows(tmem + 384, tmem + 128 * (i & 1), kt(i), DESC_Q, i > 0);
-                    mma_commit(k_empty + 8 * (i % L::XS));
+                    mul_rows(tmem + 384, tmem + 128 * (c & 1), kt(c), DESC_Q, i > 0);
+                    mma_commit(k_empty + 8 * (c % L::XS));
+                    if (i + 1 == w.n) mma_commit(done);
                 }
             }
-            if (ok && one) mma_commit(done);
+            ++t;
         }
         __syncwarp();
+    } else if (warp == 10) {
+        // -lse in units of log2, -delta and the scale of dS of each item's rows
+        for (Items it(count); it.more() && ok; it.next()) {
+            const DqItem w(a, it.at);
+            if (w.n == 0) continue;
+            const int st = t % L::SS;
+            const int64_t at = ((int64_t)w.b * a.q_heads + w.h) * a.q_len;
+            float l[4], d[4], up = 1.f;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int r = w.r0 + lane + 32 * x;
+                l[x] = r < w.s.nq ? -a.lse[at + r] * LOG2E : 0.f;
+                d[x] = r < w.s.nq ? -a.delta[at + r] : 0.f;
+            }
+            if constexpr (!BF16) up = ds_scale(a, norms, w.b, w.h, w.h + 1, w.g);
+            if (t >= L::SS) ok = __all_sync(0xffffffffu, bar_wait(st_empty + 8 * st, (t / L::SS - 1) & 1, &stalled));
+            ++t;
+            if (!ok) break;
+            float *to = stats + st * L::STAT;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                to[lane + 32 * x] = l[x];
+                to[T + lane + 32 * x] = d[x];
+            }
+            if (lane == 0) to[2 * T] = up;
+            bar_arrive(st_full + 8 * st);
+        }
     } else if (warp < 8) {
         const int half = warp >> 2;                   // columns [64 half, 64 half + 64)
-        const int r = r0 + (threadIdx.x & 127);
+        const int lane_row = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
-        const bool row = r < s.nq;
-        const int lo = row ? attn_lo(a, s, r) : 0, hi = row ? attn_hi(a, s, r) : 0;
-        const int whole_lo = attn_lo(a, s, min(r0 + T, s.nq) - 1), whole_hi = attn_hi(a, s, r0);
-        const bool whole = r0 + T <= s.nq;
-        float delta = 0.f, lse2 = 0.f;
-        if (row) {
-            const bool vec = rows16(a.out, a.dim) && rows16(a.dout, a.dim);
-            delta = dot16<BF16, DP>(reinterpret_cast<const uint16_t *>(a.out.p) + b * a.out.sb + (int64_t)r * a.out.sl + h * a.out.sh,
-                                reinterpret_cast<const uint16_t *>(a.dout.p) + b * a.dout.sb + (int64_t)r * a.dout.sl + h * a.dout.sh,
-                                a.dim, vec);
-            lse2 = a.lse[bh * a.q_len + r] * LOG2E;
-        }
-        if (half == 0 && r < a.q_len) a.delta[bh * a.q_len + r] = delta;
         const float mul = a.scale * LOG2E;
-        float up = 1.f;
-        if constexpr (!BF16) up = ds_scale(a, norms, b, h, h + 1, g);
-        bool ok = true;
-        for (int i = 0; i < n; ++i) {
-            ok = __all_sync(0xffffffffu, bar_wait(s_full + 8 * (i & 1), (i >> 1) & 1, &stalled) &&
-                                             bar_wait(dp_full, i & 1, &stalled));
-            if (!ok) break;
-            fence_after();
-            float x[64], dp[64];
-            const uint32_t ts = tmem + lanes + 128 * (i & 1) + 64 * half, td = tmem + lanes + 256 + 64 * half;
-            tmem_ld32(td, reinterpret_cast<uint32_t *>(dp));
-            tmem_ld32(td + 32, reinterpret_cast<uint32_t *>(dp) + 32);
-            tmem_ld32(ts, reinterpret_cast<uint32_t *>(x));
-            tmem_ld32(ts + 32, reinterpret_cast<uint32_t *>(x) + 32);
-            wait_ld();
-            fence_before();
-            bar_arrive(dp_free);
-            const int j0 = (first + i) * T;
-#pragma unroll
-            for (int c = 0; c < 64; c += 2) {
-                const float2 e = fma2(make_float2(x[c], x[c + 1]), make_float2(mul, mul), make_float2(-lse2, -lse2));
-                float2 p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
-                if constexpr (!BF16) p = mul2(p, make_float2(up, up));
-                const float2 d = mul2(p, add2(make_float2(dp[c], dp[c + 1]), make_float2(-delta, -delta)));
-                x[c] = d.x;
-                x[c + 1] = d.y;
-            }
-            if (!whole || j0 < whole_lo || j0 + T > whole_hi) {
-                const int c0 = lo - j0 - 64 * half, c1 = hi - j0 - 64 * half;
-#pragma unroll
-                for (int c = 0; c < 64; ++c) x[c] = c >= c0 && c < c1 ? x[c] : 0.f;
-            }
-            uint32_t u[32];
-#pragma unroll
-            for (int c = 0; c < 32; ++c) u[c] = pack2<BF16>(x[2 * c], x[2 * c + 1]);
-            tmem_st32(ts, u);
-            wait_st();
-            fence_before();
-            bar_arrive(ds_full);
-        }
-        if (ok && n > 0) ok = __all_sync(0xffffffffu, bar_wait(done, 0, &stalled));
-        fence_after();
-        const float factor = row && n > 0 ? a.scale / up : 0.f;
-        uint16_t *out = reinterpret_cast<uint16_t *>(a.dq.p) + b * a.dq.sb + (int64_t)r * a.dq.sl + h * a.dq.sh;
         const bool vec = rows16(a.dq, a.dim);
-#pragma unroll
-        for (int c = 0; c < DP / 2; c += 32) {        // each half of the warps stores half of the columns
-            const int col = half * (DP / 2) + c;
-            float o[32];
-            __syncwarp();
-            if (n > 0 && ok) {
-                tmem_ld32(tmem + lanes + 384 + col, reinterpret_cast<uint32_t *>(o));
-                wait_ld();
+        for (Items it(count); it.more() && ok; it.next()) {
+            const DqItem w(a, it.at);
+            const AttnSeq &s = w.s;
+            const int r = w.r0 + lane_row;
+            const bool row = r < s.nq;
+            const int lo = row ? attn_lo(a, s, r) : 0, hi = row ? attn_hi(a, s, r) : 0;
+            // key tiles inside [whole_lo, whole_hi) are seen whole by every row
+            const bool whole = w.r0 + T <= s.nq;
+            const int whole_lo = whole ? attn_lo(a, s, w.r0 + T - 1) : s.nk, whole_hi = attn_hi(a, s, w.r0);
+            float neg_lse = 0.f, neg_delta = 0.f, up = 1.f;
+            if (w.n > 0) {
+                const int st = t % L::SS;
+                ok = __all_sync(0xffffffffu, bar_wait(st_full + 8 * st, (t / L::SS) & 1, &stalled));
+                neg_lse = stats[st * L::STAT + lane_row];
+                neg_delta = stats[st * L::STAT + T + lane_row];
+                if constexpr (!BF16) up = stats[st * L::STAT + 2 * T];
+                bar_arrive(st_empty + 8 * st);
             }
-            if (r < a.q_len) store32<BF16>(out, col, a.dim, vec, o, factor);
+            for (int i = 0; i < w.n && ok; ++i, ++c) {
+                ok = __all_sync(0xffffffffu, bar_wait(s_full + 8 * (c & 1), (c >> 1) & 1, &stalled) &&
+                                                 bar_wait(dp_full, c & 1, &stalled));
+                if (!ok) break;
+                fence_after();
+                float x[64], dp[64];
+                const uint32_t ts = tmem + lanes + 128 * (c & 1) + 64 * half, td = tmem + lanes + 256 + 64 * half;
+                tmem_ld32(td, reinterpret_cast<uint32_t *>(dp));
+                tmem_ld32(td + 32, reinterpret_cast<uint32_t *>(dp) + 32);
+                tmem_ld32(ts, reinterpret_cast<uint32_t *>(x));
+                tmem_ld32(ts + 32, reinterpret_cast<uint32_t *>(x) + 32);
+                wait_ld();
+                fence_before();
+                bar_arrive(dp_free);
+                const int j0 = (w.first + i) * T;
+#pragma unroll
+                for (int k = 0; k < 64; k += 2) {
+                    const float2 e = fma2(make_float2(x[k], x[k + 1]), make_float2(mul, mul), make_float2(neg_lse, neg_lse));
+                    float2 p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+                    if constexpr (!BF16) p = mul2(p, make_float2(up, up));
+                    const float2 d = mul2(p, add2(make_float2(dp[k], dp[k + 1]), make_float2(neg_delta, neg_delta)));
+                    x[k] = d.x;
+                    x[k + 1] = d.y;
+                }
+                if (j0 < whole_lo || j0 + T > whole_hi) {
+                    const int c0 = lo - j0 - 64 * half, c1 = hi - j0 - 64 * half;
+#pragma unroll
+                    for (int k = 0; k < 64; ++k) x[k] = k >= c0 && k < c1 ? x[k] : 0.f;
+                }
+                uint32_t u[32];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) u[k] = pack2<BF16>(x[2 * k], x[2 * k + 1]);
+                tmem_st32(ts, u);
+                wait_st();
+                fence_before();
+                bar_arrive(ds_full);
+            }
+            if (ok && w.n > 0) ok = __all_sync(0xffffffffu, bar_wait(done, t & 1, &stalled));
+            fence_after();
+            const float factor = row && w.n > 0 ? a.scale / up : 0.f;
+            uint16_t *out = reinterpret_cast<uint16_t *>(a.dq.p) + w.b * a.dq.sb + (int64_t)r * a.dq.sl + w.h * a.dq.sh;
+#pragma unroll
+            for (int k = 0; k < DP / 2; k += 32) {    // each half of the warps stores half of the columns
+                float o[32];
+                __syncwarp();
+                if (w.n > 0 && ok) {
+                    tmem_ld32(tmem + lanes + 384 + half * (DP / 2) + k, reinterpret_cast<uint32_t *>(o));
+                    wait_ld();
+                    if (k + 32 == DP / 2) {
+                        fence_before();
+                        bar_arrive(dq_empty);
+                    }
+                }
+                if (r < a.q_len) store32<BF16>(out, half * (DP / 2) + k, a.dim, vec, o, factor);
+            }
+            if (w.n > 0) ++t;
         }
     }
 
@@ -385,6 +455,32 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
     if (warp == 8) tmem_free(tmem, 512);
 }
 
+struct KvItem {
+    AttnSeq s;
+    int b, g, j0;
+    int first, per_head, n;                                     // query tiles; steps: query heads of the group x their tiles
+    __device__ __forceinline__ KvItem(const AttnArgs &a, uint32_t i)
+    {
+        const uint32_t heads = (uint32_t)a.batch * a.kv_heads, tile = i / heads, bg = i - tile * heads;
+        b = (int)(bg / (uint32_t)a.kv_heads);
+        g = (int)(bg - (uint32_t)b * a.kv_heads);
+        s = attn_seq(a, b);
+        j0 = (int)tile * T;                                     // the first keys of a causal bound have most queries
+        first = per_head = 0;
+        if (j0 < s.nk) {
+            const int lo = attn_q_first(a, s, j0), hi = attn_q_last(a, s, min(j0 + T, s.nk));
+            if (lo < hi) {
+                first = lo / T;
+                per_head = (hi + T - 1) / T - first;
+            }
+        }
+        n = per_head * a.group;
+    }
+    // step i: query head and first row
+    __device__ __forceinline__ int head(const AttnArgs &a, int i) const { return g * a.group + i / per_head; }
+    __device__ __forceinline__ int row(int i) const { return (first + i % per_head) * T; }
+};
+
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(384, 1)
 attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ BwdMaps maps, const BwdNorms norms,
@@ -393,34 +489,21 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     using L = BwdSmem<DP>;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
-    float *stats = reinterpret_cast<float *>(smem + L::STATS);            // [slot][lse, delta][128]
+    float *stats = reinterpret_cast<float *>(smem + L::STATS);
     volatile int &stalled = *reinterpret_cast<volatile int *>(smem + L::WORDS);
     uint32_t &tmem_base = *reinterpret_cast<uint32_t *>(smem + L::WORDS + 4);
     const uint32_t bars = base + L::BARS;
-    const uint32_t kv_full = bars, fix = bars + 8, s_full = bars + 24, dp_full = bars + 32, p_full = bars + 40,
-                   ds_full = bars + 48, done = bars + 56, q_full = bars + 80, q_empty = q_full + 8 * L::XS,
+    const uint32_t kv_full = bars, kv_empty = bars + 8, fix = bars + 16, s_full = bars + 32, dp_full = bars + 40, p_full = bars + 48,
+                   ds_full = bars + 56, done = bars + 64, acc_empty = bars + 72, q_full = bars + 96, q_empty = q_full + 8 * L::XS,
                    do_full = q_empty + 8 * L::XS, do_empty = do_full + 8 * L::YS,
                    st_full = do_empty + 8 * L::YS, st_empty = st_full + 8 * L::SS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
-    const int64_t heads = a.batch * a.kv_heads;
-    const int j0 = (int)(blockIdx.x / heads) * T;                   // the first keys of a causal bound have most queries
-    const int64_t bg = blockIdx.x % heads, b = bg / a.kv_heads;
-    const int g = (int)(bg % a.kv_heads);
-    const AttnSeq s = attn_seq(a, b);
-    int first = 0, per_head = 0;
-    if (j0 < s.nk) {
-        const int lo = attn_q_first(a, s, j0), hi = attn_q_last(a, s, min(j0 + T, s.nk));
-        if (lo < hi) {
-            first = lo / T;
-            per_head = (hi + T - 1) / T - first;
-        }
-    }
-    const int n = per_head * a.group;                               // steps: query heads of the group x their tiles
+    const uint32_t count = (uint32_t)a.batch * a.kv_heads * ((a.k_len + T - 1) / T);
 
     if (threadIdx.x == 0) {
         stalled = 0;
         bar_init(kv_full, 1);
+        bar_init(kv_empty, 1);
         bar_init(fix, 1);
         bar_init(fix + 8, 1);
         bar_init(s_full, 1);
@@ -428,6 +511,7 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         bar_init(p_full, 256);
         bar_init(ds_full, 256);
         bar_init(done, 1);
+        bar_init(acc_empty, 256);
         for (int i = 0; i < 2 * (L::XS + L::YS); ++i) bar_init(q_full + 8 * i, 1);
         for (int i = 0; i < L::SS; ++i) {
             bar_init(st_full + 8 * i, 32);
@@ -447,221 +531,237 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     fence_after();
     const uint32_t tmem = tmem_base;                                // S^T, dP^T, dV, dK
 
+    // c counts a block's steps over all its items, t the items that have any
+    bool ok = true;
+    int c = 0, t = 0;
     if (warp == 9) {
-        if (n > 0) {
-            if (lane == 0) {
+        uint32_t patched = 0;
+        for (Items it(count); it.more() && ok; it.next()) {
+            const KvItem w(a, it.at);
+            if (w.n == 0) continue;
+            if (t > 0) ok = __all_sync(0xffffffffu, bar_wait(kv_empty, (t - 1) & 1, &stalled));
+            ++t;
+            if (ok && lane == 0) {
                 bar_expect(kv_full, 2 * L::TILE);
-                load_tile<DP>(base + L::A, &maps.k, kv_full, j0, g, (int)b);
-                load_tile<DP>(base + L::B, &maps.v, kv_full, j0, g, (int)b);
+                load_tile<DP>(base + L::A, &maps.k, kv_full, w.j0, w.g, w.b);
+                load_tile<DP>(base + L::B, &maps.v, kv_full, w.j0, w.g, w.b);
             }
-            bool ok = true;
-            uint32_t patched = 0;
-            for (int i = 0; i < n && ok; ++i) {
-                const int qst = i % L::XS, ost = i % L::YS;
-                const int r0 = (first + i % per_head) * T, h = g * a.group + i / per_head;
+            for (int i = 0; i < w.n && ok; ++i, ++c) {
+                const int qst = c % L::XS, ost = c % L::YS, r0 = w.row(i), h = w.head(a, i);
                 const uint32_t qt = base + L::X + qst * L::TILE, dt = base + L::Y + ost * L::TILE;
-                const bool patch = s.nq < a.q_len && r0 + T > s.nq;        // both are summed over their rows
-                if (i >= L::XS) ok = __all_sync(0xffffffffu, bar_wait(q_empty + 8 * qst, (i / L::XS - 1) & 1, &stalled));
+                const bool patch = w.s.nq < a.q_len && r0 + T > w.s.nq;    // both are summed over their rows
+                if (c >= L::XS) ok = __all_sync(0xffffffffu, bar_wait(q_empty + 8 * qst, (c / L::XS - 1) & 1, &stalled));
                 if (!ok) break;
                 if (lane == 0) {
                     const uint32_t bar = patch ? fix : q_full + 8 * qst;
                     bar_expect(bar, L::TILE);
-                    load_tile<DP>(qt, &maps.q, bar, r0, h, (int)b);
+                    load_tile<DP>(qt, &maps.q, bar, r0, h, w.b);
                 }
-                if (i >= L::YS) ok = __all_sync(0xffffffffu, bar_wait(do_empty + 8 * ost, (i / L::YS - 1) & 1, &stalled));
+                if (c >= L::YS) ok = __all_sync(0xffffffffu, bar_wait(do_empty + 8 * ost, (c / L::YS - 1) & 1, &stalled));
                 if (!ok) break;
                 if (lane == 0) {
                     const uint32_t bar = patch ? fix + 8 : do_full + 8 * ost;
                     bar_expect(bar, L::TILE);
-                    load_tile<DP>(dt, &maps.dout, bar, r0, h, (int)b);
+                    load_tile<DP>(dt, &maps.dout, bar, r0, h, w.b);
                 }
                 if (patch) {
-                    ok = patch_tile<DP>(qt, s.nq - r0, fix, patched, q_full + 8 * qst, &stalled) &&
-                         patch_tile<DP>(dt, s.nq - r0, fix + 8, patched, do_full + 8 * ost, &stalled);
+                    ok = patch_tile<DP>(qt, w.s.nq - r0, fix, patched, q_full + 8 * qst, &stalled) &&
+                         patch_tile<DP>(dt, w.s.nq - r0, fix + 8, patched, do_full + 8 * ost, &stalled);
                     patched ^= 1;
                 }
             }
         }
     } else if (warp == 8) {
-        if (n > 0) {
-            const bool one = elect_one();
-            constexpr uint32_t DESC_S = mma_desc(BF16, T, T, false), DESC_G = mma_desc(BF16, T, DP, true);
-            auto qt = [&](int i) { return base + L::X + (i % L::XS) * L::TILE; };
-            auto dt = [&](int i) { return base + L::Y + (i % L::YS) * L::TILE; };
-            auto q_here = [&](int i) { return bar_wait(q_full + 8 * (i % L::XS), (i / L::XS) & 1, &stalled); };
-            auto do_here = [&](int i) { return bar_wait(do_full + 8 * (i % L::YS), (i / L::YS) & 1, &stalled); };
-            bool ok = __all_sync(0xffffffffu, bar_wait(kv_full, 0, &stalled) && q_here(0));
-            if (ok) {
-                fence_after();
-                if (one) {
-                    mul_values<DP>(tmem, base + L::A, qt(0), DESC_S);
-                    mma_commit(s_full);
-                }
-                ok = __all_sync(0xffffffffu, do_here(0));
+        const bool one = elect_one();
+        constexpr uint32_t DESC_S = mma_desc(BF16, T, T, false), DESC_G = mma_desc(BF16, T, DP, true);
+        auto qt = [&](int x) { return base + L::X + (x % L::XS) * L::TILE; };
+        auto dt = [&](int x) { return base + L::Y + (x % L::YS) * L::TILE; };
+        auto scores = [&](int x) {                                  // S^T of step x
+            ok = __all_sync(0xffffffffu, bar_wait(q_full + 8 * (x % L::XS), (x / L::XS) & 1, &stalled));
+            if (!ok) return;
+            fence_after();
+            if (one) {
+                mul_values<DP>(tmem, base + L::A, qt(x), DESC_S);
+                mma_commit(s_full);
             }
-            if (ok) {
-                fence_after();
-                if (one) {
-                    mul_values<DP>(tmem + 128, base + L::B, dt(0), DESC_S);
-                    mma_commit(dp_full);
-                }
+        };
+        auto dscores = [&](int x) {                                 // dP^T of step x
+            ok = __all_sync(0xffffffffu, bar_wait(do_full + 8 * (x % L::YS), (x / L::YS) & 1, &stalled));
+            if (!ok) return;
+            fence_after();
+            if (one) {
+                mul_values<DP>(tmem + 128, base + L::B, dt(x), DESC_S);
+                mma_commit(dp_full);
             }
-            for (int i = 0; i < n && ok; ++i) {
-                ok = __all_sync(0xffffffffu, bar_wait(p_full, i & 1, &stalled));
+        };
+        for (Items it(count); it.more() && ok; it.next()) {
+            const KvItem w(a, it.at);
+            if (w.n == 0) continue;
+            ok = __all_sync(0xffffffffu, bar_wait(kv_full, t & 1, &stalled));
+            if (ok) scores(c);
+            if (ok) dscores(c);
+            if (w.n == 1 && ok && one) mma_commit(kv_empty);
+            for (int i = 0; i < w.n && ok; ++i, ++c) {
+                ok = bar_wait(p_full, c & 1, &stalled);
+                if (i == 0 && t > 0) ok = bar_wait(acc_empty, (t - 1) & 1, &stalled) && ok;     // the last item's dV, dK have been read
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 fence_after();
                 if (one) {
-                    mul_rows(tmem + 256, tmem, dt(i), DESC_G, i > 0);
-                    mma_commit(do_empty + 8 * (i % L::YS));
+                    mul_rows(tmem + 256, tmem, dt(c), DESC_G, i > 0);
+                    mma_commit(do_empty + 8 * (c % L::YS));
                 }
-                if (i + 1 < n) {
-                    ok = __all_sync(0xffffffffu, q_here(i + 1));
-                    if (!ok) break;
-                    fence_after();
-                    if (one) {
-                        mul_values<DP>(tmem, base + L::A, qt(i + 1), DESC_S);
-                        mma_commit(s_full);
-                    }
-                }
-                ok = __all_sync(0xffffffffu, bar_wait(ds_full, i & 1, &stalled));
+                if (i + 1 < w.n) scores(c + 1);
+                if (ok) ok = __all_sync(0xffffffffu, bar_wait(ds_full, c & 1, &stalled));
                 if (!ok) break;
                 fence_after();
                 if (one) {
-                    mul_rows(tmem + 384, tmem + 128, qt(i), DESC_G, i > 0);
-                    mma_commit(q_empty + 8 * (i % L::XS));
+                    mul_rows(tmem + 384, tmem + 128, qt(c), DESC_G, i > 0);
+                    mma_commit(q_empty + 8 * (c % L::XS));
+                    if (i + 1 == w.n) mma_commit(done);
                 }
-                if (i + 1 < n) {
-                    ok = __all_sync(0xffffffffu, do_here(i + 1));
-                    if (!ok) break;
-                    fence_after();
-                    if (one) {
-                        mul_values<DP>(tmem + 128, base + L::B, dt(i + 1), DESC_S);
-                        mma_commit(dp_full);
-                    }
-                }
+                if (i + 1 < w.n) dscores(c + 1);
+                if (i + 2 == w.n && ok && one) mma_commit(kv_empty);       // K and V have met all their queries
             }
-            if (ok && one) mma_commit(done);
+            ++t;
         }
         __syncwarp();
     } else if (warp == 10) {
-        // lse (in units of log2; +inf where p is to be 0) and delta of each step's 128 queries
-        bool ok = true;
-        for (int i = 0; i < n && ok; ++i) {
-            const int st = i % L::SS;
-            const int r0 = (first + i % per_head) * T, h = g * a.group + i / per_head;
-            const int64_t at = (b * a.q_heads + h) * a.q_len;
-            float l[4], d[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int r = r0 + lane + 32 * x;
-                l[x] = r < s.nq ? a.lse[at + r] * LOG2E : INFINITY;
-                d[x] = r < s.nq ? a.delta[at + r] : 0.f;
-                if (l[x] == -INFINITY) l[x] = INFINITY;              // a row that sees nothing
+        // -lse (in units of log2; -inf where p is to be 0) and -delta of each step's 128 queries
+        for (Items it(count); it.more() && ok; it.next()) {
+            const KvItem w(a, it.at);
+            float up = 1.f;
+            if constexpr (!BF16) {
+                if (w.n > 0) up = ds_scale(a, norms, w.b, w.g * a.group, (w.g + 1) * a.group, w.g);
             }
-            if (i >= L::SS) ok = __all_sync(0xffffffffu, bar_wait(st_empty + 8 * st, (i / L::SS - 1) & 1, &stalled));
-            if (!ok) break;
+            for (int i = 0; i < w.n && ok; ++i, ++c) {
+                const int st = c % L::SS, r0 = w.row(i);
+                const int64_t at = ((int64_t)w.b * a.q_heads + w.head(a, i)) * a.q_len;
+                float l[4], d[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                stats[st * 256 + lane + 32 * x] = -l[x];
-                stats[st * 256 + 128 + lane + 32 * x] = -d[x];
+                for (int x = 0; x < 4; ++x) {
+                    const int r = r0 + lane + 32 * x;
+                    l[x] = r < w.s.nq ? -a.lse[at + r] * LOG2E : -INFINITY;
+                    d[x] = r < w.s.nq ? -a.delta[at + r] : 0.f;
+                    if (l[x] == INFINITY) l[x] = -INFINITY;          // a row that sees nothing
+                }
+                if (c >= L::SS) ok = __all_sync(0xffffffffu, bar_wait(st_empty + 8 * st, (c / L::SS - 1) & 1, &stalled));
+                if (!ok) break;
+                float *to = stats + st * L::STAT;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    to[lane + 32 * x] = l[x];
+                    to[T + lane + 32 * x] = d[x];
+                }
+                if (lane == 0) to[2 * T] = up;
+                bar_arrive(st_full + 8 * st);
             }
-            bar_arrive(st_full + 8 * st);
         }
     } else if (warp < 8) {
         const int half = warp >> 2;                                 // queries [64 half, 64 half + 64) of a tile
-        const int j = j0 + (threadIdx.x & 127);
+        const int lane_row = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
-        const bool row = j < s.nk;
-        const int lo = row ? attn_q_first(a, s, j) : 0, hi = row ? attn_q_last(a, s, j + 1) : 0;
-        // query tiles inside [whole_lo, whole_hi) are seen whole by every key of this block
-        const int whole_lo = attn_q_first(a, s, min(j0 + T, s.nk) - 1), whole_hi = attn_q_last(a, s, j0 + 1);
         const float mul = a.scale * LOG2E;
-        float up = 1.f;
-        if constexpr (!BF16) up = ds_scale(a, norms, b, g * a.group, (g + 1) * a.group, g);
         const uint32_t ts = tmem + lanes + 64 * half, td = ts + 128;
-        bool ok = true;
-        for (int i = 0; i < n; ++i) {
-            const int st = i % L::SS, r0 = (first + i % per_head) * T;
-            const float *neg_lse = stats + st * 256 + 64 * half, *neg_delta = neg_lse + 128;
-            ok = __all_sync(0xffffffffu, bar_wait(st_full + 8 * st, (i / L::SS) & 1, &stalled) &&
-                                             bar_wait(s_full, i & 1, &stalled));
-            if (!ok) break;
-            fence_after();
-            float x[64];
-            tmem_ld32(ts, reinterpret_cast<uint32_t *>(x));
-            tmem_ld32(ts + 32, reinterpret_cast<uint32_t *>(x) + 32);
-            wait_ld();
+        const AttnTensor &to = half == 0 ? a.dv : a.dk;             // the first four warps store dV, the others dK
+        const bool vec = rows16(to, a.dim);
+        for (Items it(count); it.more() && ok; it.next()) {
+            const KvItem w(a, it.at);
+            const AttnSeq &s = w.s;
+            const int j = w.j0 + lane_row;
+            const bool row = j < s.nk;
+            const int lo = row ? attn_q_first(a, s, j) : 0, hi = row ? attn_q_last(a, s, j + 1) : 0;
+            // query tiles inside [whole_lo, whole_hi) are seen whole by every key of this block
+            const int whole_lo = attn_q_first(a, s, min(w.j0 + T, s.nk) - 1), whole_hi = attn_q_last(a, s, w.j0 + 1);
+            float up = 1.f;
+            int tile = 0;                                           // of the head: i % per_head
+            for (int i = 0; i < w.n && ok; ++i, ++c) {
+                const int st = c % L::SS, r0 = (w.first + tile) * T;
+                if (++tile == w.per_head) tile = 0;
+                const float *neg_lse = stats + st * L::STAT + 64 * half, *neg_delta = neg_lse + T;
+                ok = __all_sync(0xffffffffu, bar_wait(st_full + 8 * st, (c / L::SS) & 1, &stalled) &&
+                                                 bar_wait(s_full, c & 1, &stalled));
+                if (!ok) break;
+                fence_after();
+                float x[64];
+                tmem_ld32(ts, reinterpret_cast<uint32_t *>(x));
+                tmem_ld32(ts + 32, reinterpret_cast<uint32_t *>(x) + 32);
+                wait_ld();
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const float4 l = *reinterpret_cast<const float4 *>(neg_lse + c);
-                const float2 e = fma2(make_float2(x[c], x[c + 1]), make_float2(mul, mul), make_float2(l.x, l.y));
-                const float2 f = fma2(make_float2(x[c + 2], x[c + 3]), make_float2(mul, mul), make_float2(l.z, l.w));
-                x[c] = exp2_fast(e.x);
-                x[c + 1] = exp2_fast(e.y);
-                x[c + 2] = exp2_fast(f.x);
-                x[c + 3] = exp2_fast(f.y);
-            }
-            if (r0 < whole_lo || r0 + T > whole_hi) {
-                const int c0 = lo - r0 - 64 * half, c1 = hi - r0 - 64 * half;
+                for (int k = 0; k < 64; k += 4) {
+                    const float4 l = *reinterpret_cast<const float4 *>(neg_lse + k);
+                    const float2 e = fma2(make_float2(x[k], x[k + 1]), make_float2(mul, mul), make_float2(l.x, l.y));
+                    const float2 f = fma2(make_float2(x[k + 2], x[k + 3]), make_float2(mul, mul), make_float2(l.z, l.w));
+                    x[k] = exp2_fast(e.x);
+                    x[k + 1] = exp2_fast(e.y);
+                    x[k + 2] = exp2_fast(f.x);
+                    x[k + 3] = exp2_fast(f.y);
+                }
+                if (r0 < whole_lo || r0 + T > whole_hi) {
+                    const int c0 = lo - r0 - 64 * half, c1 = hi - r0 - 64 * half;
 #pragma unroll
-                for (int c = 0; c < 64; ++c) x[c] = c >= c0 && c < c1 ? x[c] : 0.f;
-            }
-            {
+                    for (int k = 0; k < 64; ++k) x[k] = k >= c0 && k < c1 ? x[k] : 0.f;
+                }
+                {
+                    uint32_t u[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        u[k] = BF16 ? pack2<BF16>(x[2 * k], x[2 * k + 1]) : pack2<BF16>(x[2 * k] * 32768.f, x[2 * k + 1] * 32768.f);
+                    tmem_st32(ts, u);
+                }
+                wait_st();
+                fence_before();
+                bar_arrive(p_full);
+                if constexpr (!BF16) up = stats[st * L::STAT + 2 * T];
+                ok = __all_sync(0xffffffffu, bar_wait(dp_full, c & 1, &stalled));
+                if (!ok) break;
+                fence_after();
                 uint32_t u[32];
 #pragma unroll
-                for (int c = 0; c < 32; ++c)
-                    u[c] = BF16 ? pack2<BF16>(x[2 * c], x[2 * c + 1]) : pack2<BF16>(x[2 * c] * 32768.f, x[2 * c + 1] * 32768.f);
-                tmem_st32(ts, u);
-            }
-            wait_st();
-            fence_before();
-            bar_arrive(p_full);
-            ok = __all_sync(0xffffffffu, bar_wait(dp_full, i & 1, &stalled));
-            if (!ok) break;
-            fence_after();
-            uint32_t u[32];
+                for (int k0 = 0; k0 < 64; k0 += 32) {
+                    float dp[32];
+                    tmem_ld32(td + k0, reinterpret_cast<uint32_t *>(dp));
+                    wait_ld();
 #pragma unroll
-            for (int c0 = 0; c0 < 64; c0 += 32) {
-                float dp[32];
-                tmem_ld32(td + c0, reinterpret_cast<uint32_t *>(dp));
-                wait_ld();
-#pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    const float4 dl = *reinterpret_cast<const float4 *>(neg_delta + c0 + c);
-                    float2 p = make_float2(x[c0 + c], x[c0 + c + 1]), q = make_float2(x[c0 + c + 2], x[c0 + c + 3]);
-                    if constexpr (!BF16) {
-                        p = mul2(p, make_float2(up, up));
-                        q = mul2(q, make_float2(up, up));
+                    for (int k = 0; k < 32; k += 4) {
+                        const float4 dl = *reinterpret_cast<const float4 *>(neg_delta + k0 + k);
+                        float2 p = make_float2(x[k0 + k], x[k0 + k + 1]), q = make_float2(x[k0 + k + 2], x[k0 + k + 3]);
+                        if constexpr (!BF16) {
+                            p = mul2(p, make_float2(up, up));
+                            q = mul2(q, make_float2(up, up));
+                        }
+                        p = mul2(p, add2(make_float2(dp[k], dp[k + 1]), make_float2(dl.x, dl.y)));
+                        q = mul2(q, add2(make_float2(dp[k + 2], dp[k + 3]), make_float2(dl.z, dl.w)));
+                        u[(k0 + k) / 2] = pack2<BF16>(p.x, p.y);
+                        u[(k0 + k) / 2 + 1] = pack2<BF16>(q.x, q.y);
                     }
-                    p = mul2(p, add2(make_float2(dp[c], dp[c + 1]), make_float2(dl.x, dl.y)));
-                    q = mul2(q, add2(make_float2(dp[c + 2], dp[c + 3]), make_float2(dl.z, dl.w)));
-                    u[(c0 + c) / 2] = pack2<BF16>(p.x, p.y);
-                    u[(c0 + c) / 2 + 1] = pack2<BF16>(q.x, q.y);
                 }
+                tmem_st32(td, u);
+                wait_st();
+                fence_before();
+                bar_arrive(ds_full);
+                bar_arrive(st_empty + 8 * st);
             }
-            tmem_st32(td, u);
-            wait_st();
-            fence_before();
-            bar_arrive(ds_full);
-            bar_arrive(st_empty + 8 * st);
-        }
-        if (ok && n > 0) ok = __all_sync(0xffffffffu, bar_wait(done, 0, &stalled));
-        fence_after();
-        // the first four warps store dV, the others dK
-        const AttnTensor &to = half == 0 ? a.dv : a.dk;
-        float factor = half == 0 ? (BF16 ? 1.f : 1.f / 32768.f) : a.scale / up;
-        if (!row || n == 0) factor = 0.f;
-        uint16_t *out = reinterpret_cast<uint16_t *>(to.p) + b * to.sb + (int64_t)j * to.sl + g * to.sh;
-        const bool vec = rows16(to, a.dim);
+            if (ok && w.n > 0) ok = __all_sync(0xffffffffu, bar_wait(done, t & 1, &stalled));
+            fence_after();
+            float factor = half == 0 ? (BF16 ? 1.f : 1.f / 32768.f) : a.scale / up;
+            if (!row || w.n == 0) factor = 0.f;
+            uint16_t *out = reinterpret_cast<uint16_t *>(to.p) + w.b * to.sb + (int64_t)j * to.sl + w.g * to.sh;
 #pragma unroll
-        for (int c = 0; c < DP; c += 32) {
-            float o[32];
-            __syncwarp();
-            if (n > 0 && ok) {
-                tmem_ld32(tmem + lanes + 256 + 128 * half + c, reinterpret_cast<uint32_t *>(o));
-                wait_ld();
+            for (int k = 0; k < DP; k += 32) {
+                float o[32];
+                __syncwarp();
+                if (w.n > 0 && ok) {
+                    tmem_ld32(tmem + lanes + 256 + 128 * half + k, reinterpret_cast<uint32_t *>(o));
+                    wait_ld();
+                    if (k + 32 == DP) {
+                        fence_before();
+                        bar_arrive(acc_empty);
+                    }
+                }
+                if (j < a.k_len) store32<BF16>(out, k, a.dim, vec, o, factor);
             }
-            if (j < a.k_len) store32<BF16>(out, c, a.dim, vec, o, factor);
+            if (w.n > 0) ++t;
         }
     }
 
@@ -695,19 +795,18 @@ static gs_status backward_t(const AttnArgs &a, const BwdMaps &maps, const BwdNor
         return GS_ERR_UNSUPPORTED;
     }
     unsigned long long *stalls = stall_counter();
-    if (!BF16) {
-        attn_tc_norms_kernel<<<(unsigned)(q_blocks + k_blocks), 128, 0, st>>>(a, norms);
-        GS_CUDA_TRY(cudaGetLastError());
-    }
+    const int64_t sms = sm_count();
+    attn_tc_prepare_kernel<BF16, DP><<<(unsigned)(q_blocks + (BF16 ? 0 : k_blocks)), 256, 0, st>>>(a, norms);
+    GS_CUDA_TRY(cudaGetLastError());
     constexpr int smem = BwdSmem<DP>::BYTES;
     static SharedRecord record[2];
     gs_status s;
     if ((s = allow_shared(attn_tc_dq_kernel<BF16, DP>, smem, record[0])) != GS_OK ||
         (s = allow_shared(attn_tc_dkdv_kernel<BF16, DP>, smem, record[1])) != GS_OK)
         return s;
-    attn_tc_dq_kernel<BF16, DP><<<(unsigned)q_blocks, 384, smem, st>>>(a, maps, norms, stalls);
+    attn_tc_dq_kernel<BF16, DP><<<(unsigned)(q_blocks < sms ? q_blocks : sms), 384, smem, st>>>(a, maps, norms, stalls);
     GS_CUDA_TRY(cudaGetLastError());
-    attn_tc_dkdv_kernel<BF16, DP><<<(unsigned)k_blocks, 384, smem, st>>>(a, maps, norms, stalls);
+    attn_tc_dkdv_kernel<BF16, DP><<<(unsigned)(k_blocks < sms ? k_blocks : sms), 384, smem, st>>>(a, maps, norms, stalls);
     GS_CUDA_TRY(cudaGetLastError());
     return GS_OK;
 }
