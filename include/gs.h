@@ -612,7 +612,7 @@ GS_API gs_status gs_attention_backward(const gs_attention_config *cfg, const voi
 /*
  * Norm of the gradients of many tensors taken as one vector, and clipping by it (the bound on an
  * update's length before it reaches a table).  *d_norm = sqrt(sum of all squares); squares are
- * taken in fp32 (an element beyond 1.8e19 in magnitude makes the norm infinite), summed in fp32 over 32
+ * taken in fp32 (an element beyond 1.8e19 in magnitude makes the norm infinite), summed in fp32 over 16
  * elements of a tensor and in fp64 from there, in an order that the sizes alone fix.
  * gs_clip_gradients writes out = g * factor, rounded once to the output's type, with factor =
  * max_norm / norm if the norm is finite and greater than max_norm, else 1 (a norm that is not finite leaves

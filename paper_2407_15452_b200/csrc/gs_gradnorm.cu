@@ -4,10 +4,11 @@
 //   factor = max_norm / norm if norm > max_norm and norm is finite, else 1.
 //
 // The tensors travel in the kernel's parameters (no device-side list to upload or to keep).  All of
-// them are cut into chunks of 8192 elements; the blocks of a fixed grid take chunks round robin, so
+// them are cut into chunks of 4096 elements; the blocks of a grid take chunks round robin, so
 // one large matrix and hundreds of small vectors load the SMs alike, and the order of every sum is
-// fixed by the sizes alone: results are bitwise repeatable.  Squares are summed in fp32 over the 32
-// elements that a thread takes of a chunk and in fp64 from there on.
+// fixed by the sizes alone: results are bitwise repeatable.  Squares are summed in fp32 over the 16
+// elements that a thread takes of a chunk and in fp64 from there on.  Bound: memory traffic.  The second pass runs
+// backwards and finds the last of the first's reads in L2.
 #include <math.h>
 
 #include <cuda_bf16.h>
@@ -17,7 +18,11 @@
 
 namespace gs {
 
-static constexpr int NT = 256, UNROLL = 4, CHUNK = NT * 8 * UNROLL;
+static constexpr int NT = 256, UNROLL = 4, CHUNK = NT * 4 * UNROLL;
+// Resident blocks of an SM, and how many times as many the grids have: a pass in one round of blocks, each with its
+// fixed share, waits for the slowest.  Measured over two fp32 tensors of 128M elements: one round 163 + 381 us, 4
+// and 16 rounds 158 + 319 us (a copy of the same bytes: 317 us); the sums take fewer because each leaves a partial sum.
+static constexpr int RESIDENT = 8, ROUNDS_SUM = 4, ROUNDS_SCALE = 16;
 
 struct GradTensor {
     const void *in;
@@ -34,32 +39,26 @@ struct GradList {
     int32_t count;
 };
 
-__device__ __forceinline__ void unpack8(const float *p, float (&f)[8])
+// Four elements a thread and access: 16 bytes of fp32 or 8 of a 16-bit type, so that a warp's access is one
+// contiguous piece in either, also where gradients and outputs differ in type (eight elements a thread leave
+// every second 16 bytes of an fp32 access to the next one: 394 instead of 331 us for a pass over 256M fp32 elements)
+__device__ __forceinline__ void unpack4(const float *p, float (&f)[4])
 {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    const float4 a = *reinterpret_cast<const float4 *>(p);
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
-template <typename T2>
-__device__ __forceinline__ float2 two_floats(uint32_t u);
-template <> __device__ __forceinline__ float2 two_floats<__half2>(uint32_t u)
+__device__ __forceinline__ void unpack4(const __half *p, float (&f)[4])
 {
-    return __half22float2(*reinterpret_cast<__half2 *>(&u));
-}
-template <> __device__ __forceinline__ float2 two_floats<__nv_bfloat162>(uint32_t u)
-{
-    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
-}
-template <typename T2>
-__device__ __forceinline__ void unpack8_16(const void *p, float (&f)[8])
-{
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const float2 a = two_floats<T2>(u.x), b = two_floats<T2>(u.y), c = two_floats<T2>(u.z), d = two_floats<T2>(u.w);
+    uint2 u = *reinterpret_cast<const uint2 *>(p);
+    const float2 a = __half22float2(*reinterpret_cast<__half2 *>(&u.x)), b = __half22float2(*reinterpret_cast<__half2 *>(&u.y));
     f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
-    f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
 }
-__device__ __forceinline__ void unpack8(const __half *p, float (&f)[8]) { unpack8_16<__half2>(p, f); }
-__device__ __forceinline__ void unpack8(const __nv_bfloat16 *p, float (&f)[8]) { unpack8_16<__nv_bfloat162>(p, f); }
+__device__ __forceinline__ void unpack4(const __nv_bfloat16 *p, float (&f)[4])
+{
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    f[0] = __uint_as_float(u.x << 16); f[1] = __uint_as_float(u.x & 0xFFFF0000u);
+    f[2] = __uint_as_float(u.y << 16); f[3] = __uint_as_float(u.y & 0xFFFF0000u);
+}
 
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
@@ -69,24 +68,19 @@ __device__ __forceinline__ void put(float *p, float x) { *p = x; }
 __device__ __forceinline__ void put(__half *p, float x) { *p = __float2half_rn(x); }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
 
-__device__ __forceinline__ void pack8(float *p, const float (&f)[8])
+__device__ __forceinline__ void pack4(float *p, const float (&f)[4])
 {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+    *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
 }
-__device__ __forceinline__ void pack8(__half *p, const float (&f)[8])
+__device__ __forceinline__ void pack4(__half *p, const float (&f)[4])
 {
-    __half2 h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
-    *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<uint4 *>(h);
+    __half2 h[2] = {__floats2half2_rn(f[0], f[1]), __floats2half2_rn(f[2], f[3])};
+    *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<uint2 *>(h);
 }
-__device__ __forceinline__ void pack8(__nv_bfloat16 *p, const float (&f)[8])
+__device__ __forceinline__ void pack4(__nv_bfloat16 *p, const float (&f)[4])
 {
-    __nv_bfloat162 h[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-    *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<uint4 *>(h);
+    __nv_bfloat162 h[2] = {__floats2bfloat162_rn(f[0], f[1]), __floats2bfloat162_rn(f[2], f[3])};
+    *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<uint2 *>(h);
 }
 
 // tensor of a chunk: the last one whose first chunk is <= c
@@ -122,23 +116,23 @@ __device__ __forceinline__ double squares(const T *p, int64_t n, int head, int64
     const T *q = p + head + c * CHUNK;
     const int64_t rest = n - head - c * CHUNK;
     if (rest >= CHUNK) {
-        float f[UNROLL][8];
+        float f[UNROLL][4];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) unpack8(q + (u * NT + threadIdx.x) * 8, f[u]);
+        for (int u = 0; u < UNROLL; ++u) unpack4(q + (u * NT + threadIdx.x) * 4, f[u]);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s = fmaf(f[u][i], f[u][i], s);
+            for (int i = 0; i < 4; ++i) s = fmaf(f[u][i], f[u][i], s);
     } else if (rest > 0) {
-        const int m = (int)rest, groups = m >> 3;
+        const int m = (int)rest, groups = m >> 2;
         for (int e = threadIdx.x; e < groups; e += NT) {
-            float f[8];
-            unpack8(q + e * 8, f);
+            float f[4];
+            unpack4(q + e * 4, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s = fmaf(f[i], f[i], s);
+            for (int i = 0; i < 4; ++i) s = fmaf(f[i], f[i], s);
         }
-        if ((int)threadIdx.x < (m & 7)) {
-            const float x = as_float(q[groups * 8 + threadIdx.x]);
+        if ((int)threadIdx.x < (m & 3)) {
+            const float x = as_float(q[groups * 4 + threadIdx.x]);
             s = fmaf(x, x, s);
         }
     }
@@ -159,9 +153,10 @@ __device__ __forceinline__ double block_sum(double v, double *sh)
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(NT) grad_squares_kernel(const __grid_constant__ GradList<CAP> l, double *partial)
+__global__ void __launch_bounds__(NT, RESIDENT) grad_squares_kernel(const __grid_constant__ GradList<CAP> l, double *partial)
 {
     __shared__ double sh[NT / 32];
+    cudaTriggerProgrammaticLaunchCompletion();           // the next kernel may take up its place and wait
     double s = 0.0;
     const int chunks = l.first[l.count];
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
@@ -187,6 +182,7 @@ __device__ __forceinline__ float norm_of(const double *partial, int n, double *s
 __global__ void __launch_bounds__(NT) grad_norm_kernel(const double *partial, int n, float *norm)
 {
     __shared__ double sh[NT / 32];
+    cudaGridDependencySynchronize();
     const float v = norm_of(partial, n, sh);
     if (threadIdx.x == 0) *norm = v;
 }
@@ -206,26 +202,26 @@ __device__ __forceinline__ void scale_chunk(const I *p, O *o, int64_t n, int hea
     O *w = o + head + c * CHUNK;
     const int64_t rest = n - head - c * CHUNK;
     if (rest >= CHUNK) {
-        float f[UNROLL][8];
+        float f[UNROLL][4];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) unpack8(q + (u * NT + threadIdx.x) * 8, f[u]);
+        for (int u = 0; u < UNROLL; ++u) unpack4(q + (u * NT + threadIdx.x) * 4, f[u]);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[u][i] *= factor;
-            pack8(w + (u * NT + threadIdx.x) * 8, f[u]);
+            for (int i = 0; i < 4; ++i) f[u][i] *= factor;
+            pack4(w + (u * NT + threadIdx.x) * 4, f[u]);
         }
     } else if (rest > 0) {
-        const int m = (int)rest, groups = m >> 3;
+        const int m = (int)rest, groups = m >> 2;
         for (int e = threadIdx.x; e < groups; e += NT) {
-            float f[8];
-            unpack8(q + e * 8, f);
+            float f[4];
+            unpack4(q + e * 4, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] *= factor;
-            pack8(w + e * 8, f);
+            for (int i = 0; i < 4; ++i) f[i] *= factor;
+            pack4(w + e * 4, f);
         }
-        if ((int)threadIdx.x < (m & 7))
-            put(w + groups * 8 + threadIdx.x, as_float(q[groups * 8 + threadIdx.x]) * factor);
+        if ((int)threadIdx.x < (m & 3))
+            put(w + groups * 4 + threadIdx.x, as_float(q[groups * 4 + threadIdx.x]) * factor);
     }
 }
 
@@ -238,10 +234,11 @@ __device__ __forceinline__ void scale_to(const I *p, void *o, int out_type, int6
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(NT) grad_scale_kernel(const __grid_constant__ GradList<CAP> l, const double *partial,
+__global__ void __launch_bounds__(NT, RESIDENT) grad_scale_kernel(const __grid_constant__ GradList<CAP> l, const double *partial,
                                                         int n_partial, float max_norm, bool in_place, float *norm_out)
 {
     __shared__ double sh[NT / 32];
+    cudaGridDependencySynchronize();
     const float norm = norm_of(partial, n_partial, sh);
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
     const bool over = norm > max_norm && isfinite(norm);
@@ -300,7 +297,27 @@ static int fill(GradList<CAP> *l, const gs_tensor *in, const gs_tensor *out, int
     return (int)chunks;
 }
 
-static int grid_cap() { return sm_count() * 8; }
+static int grid_for(int chunks, int rounds)
+{
+    const int cap = sm_count() * RESIDENT * rounds;
+    return chunks < 1 ? 1 : chunks < cap ? chunks : cap;
+}
+
+// launches behind a kernel of this file whose results it reads after cudaGridDependencySynchronize
+template <typename... P, typename... A>
+static cudaError_t launch_after(void (*kernel)(P...), int grid, cudaStream_t st, A... args)
+{
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(NT);
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
 
 static int64_t launches_of(int64_t n) { return n <= SMALL ? 1 : (n + LARGE - 1) / LARGE; }
 
@@ -309,28 +326,25 @@ static gs_status run(const gs_tensor *in, const gs_tensor *out, int64_t n, bool 
                      float *norm, cudaStream_t st)
 {
     GradList<CAP> l;
-    const int cap = grid_cap();
     int64_t at = 0;
     int partials = 0;
     do {
         const int chunks = fill(&l, in, out, n, &at);
-        const int grid = chunks < cap ? (chunks > 0 ? chunks : 1) : cap;
+        const int grid = grid_for(chunks, ROUNDS_SUM);
         grad_squares_kernel<CAP><<<grid, NT, 0, st>>>(l, work + partials);
         GS_CUDA_TRY(cudaGetLastError());
         partials += grid;
     } while (at < n);
     if (!scale) {
-        grad_norm_kernel<<<1, NT, 0, st>>>(work, partials, norm);
-        GS_CUDA_TRY(cudaGetLastError());
+        GS_CUDA_TRY(launch_after(grad_norm_kernel, 1, st, work, partials, norm));
         return GS_OK;
     }
     const bool in_place = in == out;
     at = 0;
     do {
         const int chunks = fill(&l, in, out, n, &at);
-        const int grid = chunks < cap ? (chunks > 0 ? chunks : 1) : cap;
-        grad_scale_kernel<CAP><<<grid, NT, 0, st>>>(l, work, partials, max_norm, in_place, norm);
-        GS_CUDA_TRY(cudaGetLastError());
+        const int grid = grid_for(chunks, ROUNDS_SCALE);
+        GS_CUDA_TRY(launch_after(grad_scale_kernel<CAP>, grid, st, l, work, partials, max_norm, in_place, norm));
     } while (at < n);
     return GS_OK;
 }
@@ -383,7 +397,7 @@ extern "C" {
 int64_t gs_gradient_norm_work(int64_t n_tensors)
 {
     if (n_tensors < 0) return 0;
-    return launches_of(n_tensors) * grid_cap();
+    return launches_of(n_tensors) * (int64_t)(sm_count() * RESIDENT * ROUNDS_SUM);
 }
 
 gs_status gs_gradient_norm(const gs_tensor *h_grads, int64_t n_tensors, double *d_work, float *d_norm, void *stream)
