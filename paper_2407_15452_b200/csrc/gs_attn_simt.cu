@@ -596,12 +596,12 @@ static gs_status backward_t(const AttnArgs &a, cudaStream_t st)
     const bool vec = rows_of_four(a, sizeof(T), true);
     const int smem = sizeof(BwdTiles<BT, DP>);
     gs_status s;
-    if (BT < 64 || (a.q_len <= BT && a.k_len <= BT)) {      // by_shape gives the smaller tiles to nothing longer
+    if (BT == 16 || (a.q_len <= BT && a.k_len <= BT)) {     // by_shape gives 16-row tiles to nothing longer
         auto kernel = attn_simt_backward_one_kernel<T, BT, DP>;
         const int64_t blocks = a.batch * a.kv_heads;
         if ((s = blocks_ok(blocks)) != GS_OK || (s = allow_shared(kernel, smem, record[0])) != GS_OK) return s;
         kernel<<<(unsigned)blocks, BT * 4, smem, st>>>(a, vec);
-    } else if constexpr (BT == 64) {
+    } else if constexpr (BT >= 32) {
         auto kernel = attn_simt_backward_kernel<T, BT, DP>;
         const int q_tiles = (a.q_len + BT - 1) / BT, k_tiles = (a.k_len + BT - 1) / BT;
         const int64_t k_blocks = a.batch * a.kv_heads * k_tiles, blocks = k_blocks + a.batch * a.q_heads * q_tiles;
@@ -623,7 +623,13 @@ static gs_status by_shape(const AttnArgs &a, cudaStream_t st)
         if (a.dim <= 64) GS_SIMT_CASE(16, 64);
         GS_SIMT_CASE(16, 128);
     }
-    if (n <= 32) {
+    // Tiles of 64 rows do more with what they read, tiles of 32 waste less of a causal bound and make four times the
+    // blocks for a device that 64-row tiles fill less than one and a half times (two blocks of an SM, one with 128
+    // columns).  Backward, 64 | 32 rows: 8 x 4 heads of 333 x 64 104 | 83 us, 16 x 8 heads 327 | 313, 4 x 8 heads of
+    // 1024 507 | 579, 8 heads of 1500 x 128 1041 | 1166.  Up to 64 rows one block has all of a head.
+    const int64_t blocks64 = (n + 63) / 64 * a.batch * (BWD ? a.q_heads + a.kv_heads : a.q_heads);
+    const int64_t slots = (a.dim <= 64 ? 2 : 1) * (int64_t)sm_count();
+    if (n <= 32 || (n > 64 && 2 * blocks64 < 3 * slots)) {
         if (a.dim <= 32) GS_SIMT_CASE(32, 32);
         if (a.dim <= 64) GS_SIMT_CASE(32, 64);
         GS_SIMT_CASE(32, 128);
