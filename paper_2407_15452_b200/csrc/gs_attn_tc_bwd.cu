@@ -25,6 +25,7 @@ namespace gs {
 using namespace tc;
 
 static constexpr int T = 128;                     // rows of every tile
+static constexpr int THREADS = 384;
 
 struct BwdMaps {
     CUtensorMap q, k, v, dout;
@@ -133,6 +134,7 @@ template <bool BF16, int DP>
 __global__ void __launch_bounds__(256) attn_tc_prepare_kernel(const __grid_constant__ AttnArgs a, BwdNorms nm)
 {
     constexpr int LANES = DP / 8, STEP = 256 / LANES, ROUNDS = T / STEP;
+    cudaTriggerProgrammaticLaunchCompletion();                  // the dq kernel may set itself up meanwhile
     const int qt = (a.q_len + T - 1) / T, kt = (a.k_len + T - 1) / T;
     int64_t i = blockIdx.x;
     const int64_t nq = a.batch * a.q_heads * qt;
@@ -205,7 +207,7 @@ struct DqItem {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(384, 1)
+__global__ void __launch_bounds__(THREADS, 1)
 attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ BwdMaps maps, const BwdNorms norms,
                   unsigned long long *stalls)
 {
@@ -340,6 +342,8 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
         __syncwarp();
     } else if (warp == 10) {
         // -lse in units of log2, -delta and the scale of dS of each item's rows
+        cudaGridDependencySynchronize();              // delta and the norms; nobody else here reads what the first kernel writes
+        cudaTriggerProgrammaticLaunchCompletion();
         for (Items it(count); it.more() && ok; it.next()) {
             const DqItem w(a, it.at);
             if (w.n == 0) continue;
@@ -482,7 +486,7 @@ struct KvItem {
 };
 
 template <bool BF16, int DP>
-__global__ void __launch_bounds__(384, 1)
+__global__ void __launch_bounds__(THREADS, 1)
 attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ BwdMaps maps, const BwdNorms norms,
                     unsigned long long *stalls)
 {
@@ -770,6 +774,9 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     fence_after();
     if (stalled) drain_stalled(stalls);
     if (warp == 8) tmem_free(tmem, 512);
+    // This kernel starts once every block of the dq kernel has seen the first kernel's end, and fills the SMs that they
+    // leave; it is not to end before them.
+    if (threadIdx.x == 0) cudaGridDependencySynchronize();
 }
 
 static int64_t tiles_of(int64_t n) { return (n + T - 1) / T; }
@@ -804,10 +811,8 @@ static gs_status backward_t(const AttnArgs &a, const BwdMaps &maps, const BwdNor
     if ((s = allow_shared(attn_tc_dq_kernel<BF16, DP>, smem, record[0])) != GS_OK ||
         (s = allow_shared(attn_tc_dkdv_kernel<BF16, DP>, smem, record[1])) != GS_OK)
         return s;
-    attn_tc_dq_kernel<BF16, DP><<<(unsigned)(q_blocks < sms ? q_blocks : sms), 384, smem, st>>>(a, maps, norms, stalls);
-    GS_CUDA_TRY(cudaGetLastError());
-    attn_tc_dkdv_kernel<BF16, DP><<<(unsigned)(k_blocks < sms ? k_blocks : sms), 384, smem, st>>>(a, maps, norms, stalls);
-    GS_CUDA_TRY(cudaGetLastError());
+    GS_CUDA_TRY(launch_after(attn_tc_dq_kernel<BF16, DP>, (int)(q_blocks < sms ? q_blocks : sms), THREADS, smem, st, a, maps, norms, stalls));
+    GS_CUDA_TRY(launch_after(attn_tc_dkdv_kernel<BF16, DP>, (int)(k_blocks < sms ? k_blocks : sms), THREADS, smem, st, a, maps, norms, stalls));
     return GS_OK;
 }
 

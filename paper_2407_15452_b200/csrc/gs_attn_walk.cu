@@ -100,6 +100,34 @@ __device__ __forceinline__ void block_dot(float (&s)[8], const uint32_t (&a)[DP 
     }
 }
 
+// The 16 rows that a warp multiplies with block after block: in registers where they are few, from shared
+// memory each time where they would crowd out the accumulators (head_dim above 32)
+template <int DP>
+struct Rows {
+    static constexpr bool HELD = DP <= 32;
+    uint32_t f[HELD ? DP / 16 : 1][4], block, half;
+    __device__ __forceinline__ Rows(uint32_t b, uint32_t h) : block(b), half(h)
+    {
+        if constexpr (HELD) load_a<DP>(f, block, half);
+    }
+};
+template <bool BF16, int DP>
+__device__ __forceinline__ void block_dot(float (&s)[8], const Rows<DP> &a, uint32_t block, uint32_t half)
+{
+    if constexpr (Rows<DP>::HELD) {
+        block_dot<BF16, DP>(s, a.f, block, half);
+    } else {
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) {
+            uint32_t x[4], f[4];
+            ldm4(x, step_at<DP>(a.block, k, a.half));
+            ldm4(f, step_at<DP>(block, k, half));
+            mma<BF16>(s, x, f[0], f[1]);
+            mma<BF16>(s + 4, x, f[2], f[3]);
+        }
+    }
+}
+
 // acc[16 x DP] += p[16 x 16] B, the 16 rows of B summed over; `block` includes lane_a
 template <bool BF16, int DP>
 __device__ __forceinline__ void block_mul(float (&acc)[DP / 8][4], const uint32_t (&p)[4], uint32_t block, uint32_t half)
@@ -584,9 +612,7 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
             const int r_end = min(r0 + 16, s.nq);
             const int j_begin = attn_lo(a, s, r0) / 16, j_end = r_end > r0 ? (attn_hi(a, s, r_end - 1) + 15) / 16 : 0;
             const float l_a = neg_lse[ra], l_b = neg_lse[rb];
-            uint32_t qf[DP / 16][4], df[DP / 16][4];
-            load_a<DP>(qf, Q + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half);
-            load_a<DP>(df, DO + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half);
+            const Rows<DP> qf(Q + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half), df(DO + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half);
             const uint32_t lb = lane_b<DP>(), kb = K + lane_a<DP>();
             float d_a = 0.f, d_b = 0.f, m_a = 0.f, m_b = 0.f;
             // p and dp of one block
@@ -678,9 +704,7 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
                 up_p = up / 16384.f;
             }
             if (q_begin < q_end) {
-                uint32_t kf[DP / 16][4], vf[DP / 16][4];
-                load_a<DP>(kf, K + tile * Row<DP>::BLOCK + lane_a<DP>(), k_half);
-                load_a<DP>(vf, V + tile * Row<DP>::BLOCK + lane_a<DP>(), k_half);
+                const Rows<DP> kf(K + tile * Row<DP>::BLOCK + lane_a<DP>(), k_half), vf(V + tile * Row<DP>::BLOCK + lane_a<DP>(), k_half);
                 const uint32_t lb = lane_b<DP>(), la = lane_a<DP>();
                 for (int q = q_begin; q < q_end; ++q) {
                     const uint32_t qb = Q + q * Row<DP>::BLOCK, ob = DO + q * Row<DP>::BLOCK;
@@ -814,10 +838,11 @@ static gs_status launch(const AttnArgs &a, cudaStream_t st)
     const int unit = (BWD ? 2 : 1) * (int)Row<DP>::tile(plan.qt) + 2 * (int)Row<DP>::tile(plan.kt);
     const int stats = BWD ? (int)stat_bytes(plan.qt) : 0;
     const int masks = (int)(mask_bytes(plan.rows.n) + (BWD ? mask_bytes(plan.cols.n) : 0));
-    plan.stages = plan.tma && 2 * unit + stats + masks <= 226 * 1024 ? 2 : 1;
-    const int per_unit = plan.stages * unit + stats;
-    // as many units as the block's warps allow and as leave room for the resident blocks
+    // two sets of tiles if one unit leaves room for the resident blocks, and as many units as the block's warps
+    // and that room allow
     const int room = (227 * 1024) / blocks_per_sm<DP, BWD>() - 2048;
+    plan.stages = plan.tma && 2 * unit + stats + masks <= room ? 2 : 1;
+    const int per_unit = plan.stages * unit + stats;
     plan.units = BLOCK_WARPS / tiles;
     while (plan.units > 1 && plan.units * per_unit + masks > room) --plan.units;
     if (plan.units < 1) plan.units = 1;

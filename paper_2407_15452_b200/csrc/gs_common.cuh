@@ -20,6 +20,25 @@ gs_status cuda_fail(cudaError_t e, const char *what);
         if (_e != cudaSuccess) return ::gs::cuda_fail(_e, #expr);      \
     } while (0)
 
+// ---- launches ----------------------------------------------------------------
+// Launch that may start before the kernel ahead of it in the stream has ended (once all its blocks have called
+// cudaTriggerProgrammaticLaunchCompletion or ended); it reads that kernel's results only after cudaGridDependencySynchronize.
+template <typename... P, typename... A>
+static inline cudaError_t launch_after(void (*kernel)(P...), int grid, int threads, size_t shared, cudaStream_t st, A... args)
+{
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 // ---- per-device scratch (grow-only, cached) --------------------------------
 // Returns a 256-byte aligned scratch block of at least `bytes` for slot `slot`
 // (independent blocks so that kernels on different streams do not share one).

@@ -303,22 +303,6 @@ static int grid_for(int chunks, int rounds)
     return chunks < 1 ? 1 : chunks < cap ? chunks : cap;
 }
 
-// launches behind a kernel of this file whose results it reads after cudaGridDependencySynchronize
-template <typename... P, typename... A>
-static cudaError_t launch_after(void (*kernel)(P...), int grid, cudaStream_t st, A... args)
-{
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(NT);
-    cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
-}
-
 static int64_t launches_of(int64_t n) { return n <= SMALL ? 1 : (n + LARGE - 1) / LARGE; }
 
 template <int CAP>
@@ -336,7 +320,7 @@ static gs_status run(const gs_tensor *in, const gs_tensor *out, int64_t n, bool 
         partials += grid;
     } while (at < n);
     if (!scale) {
-        GS_CUDA_TRY(launch_after(grad_norm_kernel, 1, st, work, partials, norm));
+        GS_CUDA_TRY(launch_after(grad_norm_kernel, 1, NT, 0, st, work, partials, norm));
         return GS_OK;
     }
     const bool in_place = in == out;
@@ -344,7 +328,7 @@ static gs_status run(const gs_tensor *in, const gs_tensor *out, int64_t n, bool 
     do {
         const int chunks = fill(&l, in, out, n, &at);
         const int grid = grid_for(chunks, ROUNDS_SCALE);
-        GS_CUDA_TRY(launch_after(grad_scale_kernel<CAP>, grid, st, l, work, partials, max_norm, in_place, norm));
+        GS_CUDA_TRY(launch_after(grad_scale_kernel<CAP>, grid, NT, 0, st, l, work, partials, max_norm, in_place, norm));
     } while (at < n);
     return GS_OK;
 }
