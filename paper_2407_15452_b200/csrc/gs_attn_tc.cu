@@ -7,7 +7,7 @@
 //                   probabilities go back there as 16-bit values over the scores they came from
 //   warp 8          one thread issues the tcgen05.mma: S_t = Q_t K^T (both from shared memory) and
 //                   O_t += P_t V (P from tensor memory)
-//   warp 9          TMA loads of Q and of the ring of K and V tiles
+//   warp 9          TMA loads of Q and of the ring of K and V tiles; asks for the next item
 // While one tile's warps exponentiate, the tensor core works on the other tile.  Tensor memory: S_0,
 // S_1, O_0, O_1 of 128 columns.  The order of one thread's tcgen05.mma is kept, so S_t of the next
 // keys, issued behind P_t V, may overwrite P_t without another barrier; and the barrier that
@@ -29,7 +29,8 @@ struct FwdSmem {
     static constexpr int TILE = 128 * DP * 2;                   // bytes of one 128-row tile
     static constexpr int SLOTS = DP == 128 ? 4 : 8;
     static constexpr int Q = 0, RING = 2 * TILE, BARS = RING + SLOTS * TILE;
-    static constexpr int WORDS = BARS + 8 * (13 + 2 * SLOTS);   // stalled, address of the tensor memory
+    static constexpr int QUEUE = (BARS + 8 * (13 + 2 * SLOTS) + 15) / 16 * 16;      // answers and barriers of the items
+    static constexpr int WORDS = QUEUE + 64;                    // stalled, address of the tensor memory
     static constexpr int BYTES = WORDS + 16;
 };
 
@@ -41,8 +42,8 @@ struct FwdItem {
     __device__ __forceinline__ FwdItem(const AttnArgs &a, uint32_t i)
     {
         const uint32_t heads = (uint32_t)a.batch * a.q_heads, tile = i / heads, bh = i - tile * heads;
-        b = (int)(bh / (uint32_t)a.q_heads);
-        h = (int)(bh - (uint32_t)b * a.q_heads);
+        h = (int)(bh / (uint32_t)a.batch);                    // neighbours in the list are other sequences: lengths mix
+        b = (int)(bh - (uint32_t)h * (uint32_t)a.batch);
         g = h / a.group;
         s = attn_seq(a, b);
         r0 = ((a.q_len + ROWS - 1) / ROWS - 1 - (int)tile) * ROWS;      // the last rows of a causal bound are the longest
@@ -70,7 +71,8 @@ struct TcMaps {
 
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(384, 1)
-attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps, unsigned long long *stalls)
+attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcMaps maps, uint32_t count,
+                       unsigned long long *stalls)
 {
     using L = FwdSmem<DP>;
     extern __shared__ __align__(1024) uint8_t smem[];           // no static shared memory: this starts at its beginning
@@ -81,10 +83,11 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
     const uint32_t q_full = bars, q_empty = bars + 8, fix = bars + 16, s_full = bars + 24, p_full = bars + 40, o_full = bars + 56,
                    o_empty = bars + 72, p_half = bars + 88, kv_full = bars + 104, kv_empty = kv_full + 8 * L::SLOTS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t count = (uint32_t)a.batch * a.q_heads * ((a.q_len + ROWS - 1) / ROWS);
+    const ItemQueue queue{count, base + L::QUEUE, base + L::QUEUE + 32, base + L::QUEUE + 48, &stalled};
 
     if (threadIdx.x == 0) {
         stalled = 0;
+        queue.init(9);                                          // warps 0-8
         bar_init(q_full, 1);
         bar_init(q_empty, 1);
         bar_init(fix, 1);
@@ -121,7 +124,7 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
             int n = 0, items = 0;                                 // tiles loaded, items begun
             uint32_t patched = 0;
             bool ok = true;
-            for (Items i(count); i.more() && ok; i.next()) {
+            for (Items<true> i(queue); i.more() && ok; i.next()) {
                 const FwdItem w(a, i.at);
                 if (w.it0 >= w.it1) continue;
                 if (items > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty, (items - 1) & 1, &stalled));
@@ -159,7 +162,7 @@ attn_tc_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant
                 int n = 0, items = 0;                             // ring position of K of step it; V of it - 1 is n - 1
                 uint32_t p_phase[2] = {0, 0}, o_used[2] = {0, 0};
                 bool ok = true;
-                for (Items i(count); i.more() && ok; i.next()) {
+                for (Items<false> i(queue); i.more() && ok; i.next()) {
                     const FwdItem w(a, i.at);
                     if (w.it0 >= w.it1) continue;
                     ok = __all_sync(0xffffffffu, bar_wait(q_full, items & 1, &stalled));
@@ -232,7 +235,7 @@ const uint64_t q0 = desc_values(base + L::Q + t * L::TILE), k0 = desc_values(kt)
         const bool vec = rows16(a.out, a.dim);
         bool ok = true;
         uint32_t phase = 0, o_phase = 0;
-        for (Items i(count); i.more() && ok; i.next()) {
+        for (Items<false> i(queue); i.more() && ok; i.next()) {
         const FwdItem w(a, i.at);
         const AttnSeq &s = w.s;
         const int r = w.r0 + 128 * t + (threadIdx.x & 127);
@@ -400,7 +403,8 @@ static gs_status forward_t(const AttnArgs &a, const TcMaps &maps, cudaStream_t s
     gs_status s = allow_shared(kernel, FwdSmem<DP>::BYTES, record);
     if (s != GS_OK) return s;
     const int64_t sms = sm_count();
-    kernel<<<(unsigned)(items < sms ? items : sms), 384, FwdSmem<DP>::BYTES, st>>>(a, maps, stall_counter());
+    const bool asked = items_asked(a, items);
+    kernel<<<(unsigned)(asked || items < sms ? items : sms), 384, FwdSmem<DP>::BYTES, st>>>(a, maps, asked ? 0u : (uint32_t)items, stall_counter());
     GS_CUDA_TRY(cudaGetLastError());
     return GS_OK;
 }

@@ -10,10 +10,10 @@
 //           lane and feed dV += P^T dO, dK += dS^T Q from tensor memory without passing through shared memory.
 //           Tensor memory is full (S^T, dP^T, dV, dK: 128 columns each); the order dV(i), S^T(i+1) while dS(i)
 //           is formed, then dK(i), dP^T(i+1) while P(i+1) is formed, keeps both sides busy.
-// One block per SM goes through its items, the longest first; loads and products of the next item run while
+// One block per SM goes through items; loads and products of the next item run while
 // the last one's results are stored.  Eight warps do the elementwise part, four per 64 columns of a tile; a
-// warp overwrites only columns that it has read itself.  Warp 8 issues the products, warp 9 the loads, warp 10
-// brings the row statistics.  A first kernel works out delta = dO.O.
+// warp overwrites only columns that it has read itself.  Warp 8 issues the products, warp 9 loads and
+// asks for the next item, warp 10 brings the row statistics.  A first kernel works out delta = dO.O.
 //
 // P and dS are rounded to the tensors' type for their products.  binary16 has no range for that as it
 // stands: P is scaled by 2^15 (P <= 1), dS by the power of two that brings its bound
@@ -45,7 +45,8 @@ struct BwdSmem {
     static constexpr int STATS = Y + YS * TILE;                 // SS of: -lse (log2) and -delta of a query tile, scale of dS
     static constexpr int STAT = 2 * T + 4;                      // floats of one
     static constexpr int BARS = STATS + SS * STAT * 4;
-    static constexpr int WORDS = BARS + 8 * (12 + 2 * XS + 2 * YS + 2 * SS);    // stalled, address of the tensor memory
+    static constexpr int QUEUE = (BARS + 8 * (12 + 2 * XS + 2 * YS + 2 * SS) + 15) / 16 * 16;      // answers and barriers of the items
+    static constexpr int WORDS = QUEUE + 64;                    // stalled, address of the tensor memory
     static constexpr int BYTES = WORDS + 16;
     static_assert(BYTES <= 227 * 1024, "shared memory of one block");
 };
@@ -190,8 +191,8 @@ struct DqItem {
     __device__ __forceinline__ DqItem(const AttnArgs &a, uint32_t i)
     {
         const uint32_t heads = (uint32_t)a.batch * a.q_heads, tile = i / heads, bh = i - tile * heads;
-        b = (int)(bh / (uint32_t)a.q_heads);
-        h = (int)(bh - (uint32_t)b * a.q_heads);
+        h = (int)(bh / (uint32_t)a.batch);                    // neighbours in the list are other sequences: lengths mix
+        b = (int)(bh - (uint32_t)h * (uint32_t)a.batch);
         g = h / a.group;
         s = attn_seq(a, b);
         r0 = ((a.q_len + T - 1) / T - 1 - (int)tile) * T;       // the last rows of a causal bound are the longest
@@ -209,7 +210,7 @@ struct DqItem {
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ BwdMaps maps, const BwdNorms norms,
-                  unsigned long long *stalls)
+                  uint32_t count, unsigned long long *stalls)
 {
     using L = BwdSmem<DP>;
     extern __shared__ __align__(1024) uint8_t smem[];           // no static shared memory: this starts at its beginning
@@ -223,10 +224,11 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
                    v_full = k_empty + 8 * L::XS, v_empty = v_full + 8 * L::YS, st_full = v_empty + 8 * L::YS,
                    st_empty = st_full + 8 * L::SS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t count = (uint32_t)a.batch * a.q_heads * ((a.q_len + T - 1) / T);
+    const ItemQueue queue{count, base + L::QUEUE, base + L::QUEUE + 32, base + L::QUEUE + 48, &stalled};
 
     if (threadIdx.x == 0) {
         stalled = 0;
+        queue.init(10);                               // warps 0-8 and 10
         bar_init(q_full, 1);
         bar_init(q_empty, 1);
         bar_init(fix, 1);
@@ -261,7 +263,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
     int c = 0, t = 0;
     if (warp == 9) {
         uint32_t patched = 0;
-        for (Items it(count); it.more() && ok; it.next()) {
+        for (Items<true> it(queue); it.more() && ok; it.next()) {
             const DqItem w(a, it.at);
             if (w.n == 0) continue;
             if (t > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty, (t - 1) & 1, &stalled));
@@ -318,7 +320,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
                 mma_commit(v_empty + 8 * (x % L::YS));
             }
         };
-        for (Items it(count); it.more() && ok; it.next()) {
+        for (Items<false> it(queue); it.more() && ok; it.next()) {
             const DqItem w(a, it.at);
             if (w.n == 0) continue;
             ok = __all_sync(0xffffffffu, bar_wait(q_full, t & 1, &stalled));
@@ -344,7 +346,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
         // -lse in units of log2, -delta and the scale of dS of each item's rows
         cudaGridDependencySynchronize();              // delta and the norms; nobody else here reads what the first kernel writes
         cudaTriggerProgrammaticLaunchCompletion();
-        for (Items it(count); it.more() && ok; it.next()) {
+        for (Items<false> it(queue); it.more() && ok; it.next()) {
             const DqItem w(a, it.at);
             if (w.n == 0) continue;
             const int st = t % L::SS;
@@ -375,7 +377,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const float mul = a.scale * LOG2E;
         const bool vec = rows16(a.dq, a.dim);
-        for (Items it(count); it.more() && ok; it.next()) {
+        for (Items<false> it(queue); it.more() && ok; it.next()) {
             const DqItem w(a, it.at);
             const AttnSeq &s = w.s;
             const int r = w.r0 + lane_row;
@@ -466,8 +468,8 @@ struct KvItem {
     __device__ __forceinline__ KvItem(const AttnArgs &a, uint32_t i)
     {
         const uint32_t heads = (uint32_t)a.batch * a.kv_heads, tile = i / heads, bg = i - tile * heads;
-        b = (int)(bg / (uint32_t)a.kv_heads);
-        g = (int)(bg - (uint32_t)b * a.kv_heads);
+        g = (int)(bg / (uint32_t)a.batch);                    // neighbours in the list are other sequences: lengths mix
+        b = (int)(bg - (uint32_t)g * (uint32_t)a.batch);
         s = attn_seq(a, b);
         j0 = (int)tile * T;                                     // the first keys of a causal bound have most queries
         first = per_head = 0;
@@ -488,7 +490,7 @@ struct KvItem {
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ BwdMaps maps, const BwdNorms norms,
-                    unsigned long long *stalls)
+                    uint32_t count, unsigned long long *stalls)
 {
     using L = BwdSmem<DP>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -502,10 +504,11 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                    do_full = q_empty + 8 * L::XS, do_empty = do_full + 8 * L::YS,
                    st_full = do_empty + 8 * L::YS, st_empty = st_full + 8 * L::SS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t count = (uint32_t)a.batch * a.kv_heads * ((a.k_len + T - 1) / T);
+    const ItemQueue queue{count, base + L::QUEUE, base + L::QUEUE + 32, base + L::QUEUE + 48, &stalled};
 
     if (threadIdx.x == 0) {
         stalled = 0;
+        queue.init(10);
         bar_init(kv_full, 1);
         bar_init(kv_empty, 1);
         bar_init(fix, 1);
@@ -540,7 +543,7 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     int c = 0, t = 0;
     if (warp == 9) {
         uint32_t patched = 0;
-        for (Items it(count); it.more() && ok; it.next()) {
+        for (Items<true> it(queue); it.more() && ok; it.next()) {
             const KvItem w(a, it.at);
             if (w.n == 0) continue;
             if (t > 0) ok = __all_sync(0xffffffffu, bar_wait(kv_empty, (t - 1) & 1, &stalled));
@@ -598,7 +601,7 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 mma_commit(dp_full);
             }
         };
-        for (Items it(count); it.more() && ok; it.next()) {
+        for (Items<false> it(queue); it.more() && ok; it.next()) {
             const KvItem w(a, it.at);
             if (w.n == 0) continue;
             ok = __all_sync(0xffffffffu, bar_wait(kv_full, t & 1, &stalled));
@@ -632,7 +635,7 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         __syncwarp();
     } else if (warp == 10) {
         // -lse (in units of log2; -inf where p is to be 0) and -delta of each step's 128 queries
-        for (Items it(count); it.more() && ok; it.next()) {
+        for (Items<false> it(queue); it.more() && ok; it.next()) {
             const KvItem w(a, it.at);
             float up = 1.f;
             if constexpr (!BF16) {
@@ -669,7 +672,7 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         const uint32_t ts = tmem + lanes + 64 * half, td = ts + 128;
         const AttnTensor &to = half == 0 ? a.dv : a.dk;             // the first four warps store dV, the others dK
         const bool vec = rows16(to, a.dim);
-        for (Items it(count); it.more() && ok; it.next()) {
+        for (Items<false> it(queue); it.more() && ok; it.next()) {
             const KvItem w(a, it.at);
             const AttnSeq &s = w.s;
             const int j = w.j0 + lane_row;
@@ -811,8 +814,13 @@ static gs_status backward_t(const AttnArgs &a, const BwdMaps &maps, const BwdNor
     if ((s = allow_shared(attn_tc_dq_kernel<BF16, DP>, smem, record[0])) != GS_OK ||
         (s = allow_shared(attn_tc_dkdv_kernel<BF16, DP>, smem, record[1])) != GS_OK)
         return s;
-    GS_CUDA_TRY(launch_after(attn_tc_dq_kernel<BF16, DP>, (int)(q_blocks < sms ? q_blocks : sms), THREADS, smem, st, a, maps, norms, stalls));
-    GS_CUDA_TRY(launch_after(attn_tc_dkdv_kernel<BF16, DP>, (int)(k_blocks < sms ? k_blocks : sms), THREADS, smem, st, a, maps, norms, stalls));
+    auto launch = [&](auto kernel, int64_t items) {
+        const bool asked = items_asked(a, items);
+        return launch_after(kernel, (int)(asked || items < sms ? items : sms), THREADS, smem, st, a, maps, norms,
+                            asked ? 0u : (uint32_t)items, stalls);
+    };
+    GS_CUDA_TRY(launch(attn_tc_dq_kernel<BF16, DP>, q_blocks));
+    GS_CUDA_TRY(launch(attn_tc_dkdv_kernel<BF16, DP>, k_blocks));
     return GS_OK;
 }
 

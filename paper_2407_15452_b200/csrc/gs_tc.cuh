@@ -86,6 +86,27 @@ __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk
 // this thread's stores have read their shared memory
 __device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 
+// ---- work of blocks that have not started -----------------------------------------------------
+// asks for the cancellation of one block's launch; the 16-byte answer arrives at `answer` and counts 16 bytes on `bar`
+__device__ __forceinline__ void cancel_block(uint32_t answer, uint32_t bar)
+{
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                 ::"r"(answer), "r"(bar) : "memory");
+}
+// index of the block that an answer gives, UINT32_MAX if none is left
+__device__ __forceinline__ uint32_t canceled_block(uint32_t answer)
+{
+    uint32_t x;
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b128 h;\n\t.reg .b32 c;\n\t"
+                 "ld.shared.b128 h, [%1];\n\t"
+                 "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+                 "mov.b32 %0, 0xffffffff;\n\t"
+                 "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 c, h;\n\t"
+                 "@p mov.b32 %0, c;\n\t}"
+                 : "=r"(x) : "r"(answer) : "memory");
+    return x;
+}
+
 // ---- tensor memory ----------------------------------------------------------------------
 __device__ __forceinline__ void tmem_alloc(uint32_t where, uint32_t columns)       // whole warp
 {

@@ -95,6 +95,68 @@ def test_ragged_batches_never_read_the_padding(n, d, lens, window, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("b,n,hq,hk,window,ragged", [
+    (90, 300, 4, 2, CAUSAL, False),        # every block goes through several work items, in fixed rounds
+    (90, 300, 4, 2, CAUSAL, True),         # handed out as SMs come free; some sequences empty
+    (40, 700, 3, 3, (150, 0), True),
+    (200, 130, 2, 1, ALL, True),
+], ids=["fixed", "asked", "asked_window", "asked_short"])
+def test_more_work_items_than_sms(b, n, hq, hk, window, ragged, d, dt):
+    q, k, v, dout = tensors(b, n, n, hq, hk, d, dt, seed=b)
+    m = None
+    if ragged:
+        gen = torch.Generator().manual_seed(b)
+        values = torch.randint(0, n + 1, (b,), generator=gen)
+        values[::7] = 0
+        m = values.to(torch.int32).to(DEV)
+        for s in range(b):
+            v[s, int(values[s]):] = math.nan
+            q[s, int(values[s]):] = math.nan
+    out, lse, grads = run_both(q, k, v, dout, window, m, m)
+    again = B.gs_attention_backward(dout, q, k, v, *B.gs_attention_forward(q, k, v, window=window, q_lens=m, k_lens=m),
+                                    window=window, q_lens=m, k_lens=m)
+    assert all(torch.equal(x, y) for x, y in zip(grads, again))            # whoever did which item
+    assert B.gs_stalled_kernels() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n", [40, 200])
+def test_many_short_sequences(n, dt):
+    # more heads than one round of resident blocks takes, with and without dead ends
+    b = 3000 if n == 40 else 400
+    q, k, v, dout = tensors(b, n, n, 2, 2, 32, dt, seed=n)
+    values = torch.randint(0, n + 1, (b,), generator=torch.Generator().manual_seed(n))
+    values[: b // 2] = n
+    m = values.to(torch.int32).to(DEV)
+    for lens in (None, m):
+        out, lse, grads = run_both(q, k, v, dout, (10, 10), lens, lens)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,row", [(60, 64), (100, 104), (4, 8), (20, 24)])
+@pytest.mark.parametrize("n", [24, 200])
+def test_head_dims_within_wider_rows(n, d, row, dt):
+    # rows that TMA can address, of head_dims that are no multiple of its 16 bytes; NaN between the rows
+    make = lambda t: torch.full((*t.shape[:3], row), math.nan, dtype=dt, device=DEV)      # noqa: E731
+    parts = []
+    for t in tensors(2, n, n, 2, 2, d, dt, seed=d):
+        x = make(t)
+        x[..., :d] = t
+        parts.append(x[..., :d])
+    q, k, v, dout = parts
+    run_both(q, k, v, dout, CAUSAL)
+    out, lse = B.gs_attention_forward(q, k, v, window=CAUSAL)
+    room = torch.full((4, 2, n, 2, row), 7.0, dtype=dt, device=DEV)
+    B.gs_attention_forward(q, k, v, window=CAUSAL, out=room[0, ..., :d])
+    B.gs_attention_backward(dout, q, k, v, out, lse, window=CAUSAL, dq=room[1, ..., :d], dk=room[2, ..., :d], dv=room[3, ..., :d])
+    assert torch.equal(room[0, ..., :d], out) and (room[..., d:] == 7).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dt", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
 def test_query_and_key_lengths_differ_per_sequence(dt):
     q, k, v, dout = tensors(5, 70, 140, 2, 2, 64, dt, seed=3)
