@@ -9,6 +9,7 @@ not been built the first call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 from dataclasses import dataclass
 from pathlib import Path
@@ -525,6 +526,12 @@ def gs_attention_forward(q, k, v, scale=None, window=(-1, -1), q_lens=None, k_le
     return out, lse
 
 
+@functools.lru_cache(maxsize=256)
+def _backward_work(lead):
+    """Floats of scratch for a configuration (its first fields; pointers and strides do not matter)."""
+    return max(0, lib().gs_attention_backward_work(_pack_config(*lead, 0, 0, *(_NO_STRIDE * 8))))
+
+
 def gs_attention_backward(dout, q, k, v, out, lse, scale=None, window=(-1, -1), q_lens=None, k_lens=None,
                           dq=None, dk=None, dv=None):
     """Gradients of gs_attention_forward: returns (dq, dk, dv), shaped like q, k, v.  out and lse are
@@ -542,11 +549,10 @@ def gs_attention_backward(dout, q, k, v, out, lse, scale=None, window=(-1, -1), 
                        *_heads(v, dtype, device, kv, "v"), *_heads(out, dtype, device, shape, "out"),
                        *_heads(dout, dtype, device, shape, "dout"), *_heads(dq, dtype, device, shape, "dq"),
                        *_heads(dk, dtype, device, kv, "dk"), *_heads(dv, dtype, device, kv, "dv"))
-    L = lib()
-    work = lse.new_empty(max(0, L.gs_attention_backward_work(cfg)))
-    _check(L.gs_attention_backward(cfg, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-                                   lse.data_ptr(), work.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                   _raw_stream(device)))
+    work = lse.new_empty(_backward_work(lead[:11]))
+    _check(lib().gs_attention_backward(cfg, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                                       lse.data_ptr(), work.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                       _raw_stream(device)))
     return dq, dk, dv
 
 
@@ -561,15 +567,19 @@ def _tensor_list(tensors, device, name):
     return struct.pack(f"{len(words)}Q", *words)
 
 
+@functools.lru_cache(maxsize=64)
+def _norm_work(n, device):
+    return lib().gs_gradient_norm_work(n), torch.device("cuda", device)
+
+
 def _norm_buffers(n, device):
-    words = lib().gs_gradient_norm_work(n)
-    on = torch.device("cuda", device)
+    words, on = _norm_work(n, device)
     return torch.empty(words, dtype=torch.float64, device=on), torch.empty(1, dtype=torch.float32, device=on)
 
 
 def gs_gradient_norm(grads):
     """Euclidean norm of all tensors of `grads` taken as one vector: float32[1] on the device."""
-    device = torch.cuda.current_device()
+    device = torch._C._cuda_getDevice()
     entries = _tensor_list(grads, device, "grads")
     work, norm = _norm_buffers(len(grads), device)
     _check(lib().gs_gradient_norm(entries, len(grads), work.data_ptr(), norm.data_ptr(), _raw_stream(device)))
@@ -579,7 +589,7 @@ def gs_gradient_norm(grads):
 def gs_clip_gradients(grads, max_norm: float, out=None):
     """Scales `grads` (into the tensors `out`, or in place) so that their joint norm is at most
     max_norm; returns the norm before clipping, float32[1] on the device (nothing waits for it)."""
-    device = torch.cuda.current_device()
+    device = torch._C._cuda_getDevice()
     entries = _tensor_list(grads, device, "grads")
     targets = None
     if out is not None:
