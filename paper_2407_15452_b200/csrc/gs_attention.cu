@@ -75,6 +75,20 @@ static gs_status pointers_ok(const AttnTensor *t, int n, int32_t dtype)
     return GS_OK;
 }
 
+// Whether fp32 tensors that attn_walk_ok accepts go there (products as three of tf32 each, whole heads in
+// shared memory) or to the CUDA cores.  Measured, whole heads | CUDA cores, us:
+//  forward : 8192 heads of 30 x 32 36 | 90, 4096 of 60 x 64 121 | 169, 2048 of 30 x 128 61 | 62, 1024 of 90 x 128 168 | 288
+//  backward: 2048 heads of 100 x 64 807 | 1058, 1024 of 90 x 128 746 | 1086, 32 of 100 x 64 49 | 27; up to 64 positions, where
+//            a block of the CUDA cores has all of a head, 4096 of 60 x 64 675 | 422, 16384 of 16 x 32 110 | 82, but
+//            16384 of 40 x 32 with a window of 10 on each side 427 | 731
+static bool f32_whole(const AttnArgs &a, bool backward)
+{
+    const int n = a.q_len > a.k_len ? a.q_len : a.k_len;
+    if (!backward) return a.dim <= 64 || n > 64;
+    if (n > 64) return a.batch * a.kv_heads >= sm_count();
+    return n > 32 && a.dim <= 32 && a.left >= 0 && a.right >= 0 && a.left + a.right <= 32;
+}
+
 }  // namespace gs
 
 using namespace gs;
@@ -101,7 +115,8 @@ gs_status gs_attention_forward(const gs_attention_config *cfg, const void *d_q, 
     // and 128 positions the wide heads go to the tiles as well: 4096 heads of 100 x 128 take 127 us there and
     // 146 us whole, 8192 heads of 100 x 64 196 and 141 us.
     const bool tiles = a.k_len > 0 && attn_tc_forward_ok(a);
-    if (attn_walk_ok(a) && !(tiles && a.q_len > 64 && a.dim > 64)) return attn_walk_forward(a, (cudaStream_t)stream);
+    const bool whole = a.dtype == GS_TABLE_F32 ? f32_whole(a, false) : !(tiles && a.q_len > 64 && a.dim > 64);
+    if (whole && attn_walk_ok(a, false)) return attn_walk_forward(a, (cudaStream_t)stream);
     if (tiles) return attn_tc_forward(a, (cudaStream_t)stream);
     return attn_simt_forward(a, (cudaStream_t)stream);
 }
@@ -138,7 +153,8 @@ gs_status gs_attention_backward(const gs_attention_config *cfg, const void *d_do
     const bool tiles = a.q_len > 0 && a.k_len > 0 && attn_tc_backward_ok(a);
     const bool narrow = a.left >= 0 && a.right >= 0 && a.left + a.right < 64;
     const bool wide = (a.q_len > 64 || a.k_len > 64) && (a.dim > 64 || (a.dim > 32 && !narrow));
-    if (attn_walk_ok(a) && !(tiles && wide)) return attn_walk_backward(a, (cudaStream_t)stream);
+    const bool whole = a.dtype == GS_TABLE_F32 ? f32_whole(a, true) : !(tiles && wide);
+    if (whole && attn_walk_ok(a, true)) return attn_walk_backward(a, (cudaStream_t)stream);
     if (tiles) return attn_tc_backward(a, (cudaStream_t)stream);
     return attn_simt_backward(a, (cudaStream_t)stream);
 }

@@ -89,7 +89,7 @@ gs_status attn_simt_forward(const AttnArgs &a, cudaStream_t st);
 gs_status attn_simt_backward(const AttnArgs &a, cudaStream_t st);
 
 // gs_attn_walk.cu
-bool attn_walk_ok(const AttnArgs &a);
+bool attn_walk_ok(const AttnArgs &a, bool backward);
 gs_status attn_walk_forward(const AttnArgs &a, cudaStream_t st);
 gs_status attn_walk_backward(const AttnArgs &a, cudaStream_t st);
 // gs_attn_tc.cu

@@ -1,4 +1,5 @@
-// Attention on the CUDA cores, everything in fp32 (products included).
+// Attention on the CUDA cores, everything in fp32 (products included): fp32 tensors that are not short walks, and
+// long 16-bit tensors that TMA cannot address.
 //
 // A block of 4 * BT threads works on BT x BT tiles of scores; thread (ty, tx) holds 4 rows x BT/16
 // columns of a tile and 4 rows x DP/16 columns of an accumulator, DP = head_dim padded to 32, 64 or
@@ -618,10 +619,14 @@ static gs_status by_shape(const AttnArgs &a, cudaStream_t st)
     // one 16 x 16 or 32 x 32 tile holds all scores of a short sequence's head
     const int n = a.q_len > a.k_len ? a.q_len : a.k_len;
 #define GS_SIMT_CASE(BT, DP) return BWD ? backward_t<T, BT, DP>(a, st) : forward_t<T, BT, DP>(a, st)
-    if (n <= 16) {
-        if (a.dim <= 32) GS_SIMT_CASE(16, 32);
-        if (a.dim <= 64) GS_SIMT_CASE(16, 64);
-        GS_SIMT_CASE(16, 128);
+    if constexpr (sizeof(T) == 4) {                        // 16-bit tensors come here beyond 128 positions only
+        if (n <= 16) {
+            if constexpr (BWD) {                           // forward, narrower heads are done whole elsewhere
+                if (a.dim <= 32) GS_SIMT_CASE(16, 32);
+                if (a.dim <= 64) GS_SIMT_CASE(16, 64);
+            }
+            GS_SIMT_CASE(16, 128);
+        }
     }
     // Tiles of 64 rows do more with what they read, tiles of 32 waste less of a causal bound and make four times the
     // blocks for a device that 64-row tiles fill less than one and a half times (two blocks of an SM, one with 128

@@ -359,15 +359,16 @@ static EncodeTiled encoder()
     return fn;
 }
 
-bool attn_tma_ok(const AttnTensor &t, int64_t batch, int64_t len, int64_t heads)
+bool attn_tma_ok(const AttnTensor &t, int32_t dtype, int64_t batch, int64_t len, int64_t heads)
 {
-    auto stride_ok = [](int64_t extent, int64_t s) {
-        return extent <= 1 || (s > 0 && s % 8 == 0 && s < ((int64_t)1 << 38));
+    const int n = dtype == GS_TABLE_F32 ? 4 : 8;                // strides of whole 16 bytes, below 2^40
+    auto stride_ok = [&](int64_t extent, int64_t s) {
+        return extent <= 1 || (s > 0 && s % n == 0 && s < ((int64_t)1 << 37));
     };
     return (uintptr_t)t.p % 16 == 0 && stride_ok(batch, t.sb) && stride_ok(len, t.sl) && stride_ok(heads, t.sh);
 }
 
-gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_t batch, int64_t len, int64_t heads,
+gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, int32_t dtype, int64_t batch, int64_t len, int64_t heads,
                           int dim, int values, int rows)
 {
     EncodeTiled fn = encoder();
@@ -376,13 +377,24 @@ gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_
         return GS_ERR_CUDA;
     }
     const cuuint64_t extent[4] = {(cuuint64_t)dim, (cuuint64_t)len, (cuuint64_t)heads, (cuuint64_t)batch};
-    const cuuint64_t stride[3] = {(cuuint64_t)(len > 1 ? 2 * t.sl : 256), (cuuint64_t)(heads > 1 ? 2 * t.sh : 256),
-                                  (cuuint64_t)(batch > 1 ? 2 * t.sb : 256)};
+    const int es = dtype == GS_TABLE_F32 ? 4 : 2;
+    const cuuint64_t stride[3] = {(cuuint64_t)(len > 1 ? es * t.sl : 512), (cuuint64_t)(heads > 1 ? es * t.sh : 512),
+                                  (cuuint64_t)(batch > 1 ? es * t.sb : 512)};
     const cuuint32_t box[4] = {(cuuint32_t)values, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
-    const CUresult r = fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, t.p, extent, stride,
-                          box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          values == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : values == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
-                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    auto encode = [&] {
+        return fn(m, dtype == GS_TABLE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                  : dtype == GS_TABLE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, t.p, extent, stride,
+                              box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              values * es == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : values * es == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    if (r == CUDA_ERROR_INVALID_CONTEXT) {          // a thread that has not used the device yet, such as autograd's
+        int dev = 0;
+        GS_CUDA_TRY(cudaGetDevice(&dev));
+        GS_CUDA_TRY(cudaSetDevice(dev));
+        r = encode();
+    }
     if (r != CUDA_SUCCESS) {
         set_error("cuTensorMapEncodeTiled failed with %d", (int)r);
         return GS_ERR_CUDA;
@@ -411,8 +423,8 @@ static gs_status forward_t(const AttnArgs &a, const TcMaps &maps, cudaStream_t s
 
 bool attn_tc_forward_ok(const AttnArgs &a)
 {
-    return a.dtype != GS_TABLE_F32 && a.batch < ((int64_t)1 << 31) && attn_tma_ok(a.q, a.batch, a.q_len, a.q_heads) &&
-           attn_tma_ok(a.k, a.batch, a.k_len, a.kv_heads) && attn_tma_ok(a.v, a.batch, a.k_len, a.kv_heads);
+    return a.dtype != GS_TABLE_F32 && a.batch < ((int64_t)1 << 31) && attn_tma_ok(a.q, a.dtype, a.batch, a.q_len, a.q_heads) &&
+           attn_tma_ok(a.k, a.dtype, a.batch, a.k_len, a.kv_heads) && attn_tma_ok(a.v, a.dtype, a.batch, a.k_len, a.kv_heads);
 }
 
 gs_status attn_tc_forward(const AttnArgs &a, cudaStream_t st)
@@ -420,9 +432,9 @@ gs_status attn_tc_forward(const AttnArgs &a, cudaStream_t st)
     const bool bf16 = a.dtype == GS_TABLE_BF16;
     TcMaps m;
     gs_status s;
-    if ((s = attn_tensor_map(&m.q, a.q, bf16, a.batch, a.q_len, a.q_heads, a.dim, 64, 128)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.k, a.k, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.v, a.v, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.q, a.q, a.dtype, a.batch, a.q_len, a.q_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.k, a.k, a.dtype, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.v, a.v, a.dtype, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
     if (a.dim <= 64) return bf16 ? forward_t<true, 64>(a, m, st) : forward_t<false, 64>(a, m, st);
     return bf16 ? forward_t<true, 128>(a, m, st) : forward_t<false, 128>(a, m, st);
 }

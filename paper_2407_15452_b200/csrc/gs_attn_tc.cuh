@@ -6,10 +6,10 @@
 
 namespace gs {
 
-// host side: whether TMA can address a tensor, and its map with boxes of `rows` positions x `values` (16, 32 or
-// 64) values, swizzled over their width
-bool attn_tma_ok(const AttnTensor &t, int64_t batch, int64_t len, int64_t heads);
-gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, bool bf16, int64_t batch, int64_t len, int64_t heads,
+// host side: whether TMA can address a tensor, and its map with boxes of `rows` positions x `values` values (32, 64 or
+// 128 bytes), swizzled over their width
+bool attn_tma_ok(const AttnTensor &t, int32_t dtype, int64_t batch, int64_t len, int64_t heads);
+gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, int32_t dtype, int64_t batch, int64_t len, int64_t heads,
                           int dim, int values, int rows);
 
 static constexpr int HALF_TILE = 128 * 128;          // bytes of one box: 128 rows of 64 16-bit values

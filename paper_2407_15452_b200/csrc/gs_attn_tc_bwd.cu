@@ -791,9 +791,9 @@ int64_t attn_tc_backward_work(int64_t batch, int32_t q_len, int32_t k_len, int32
 
 bool attn_tc_backward_ok(const AttnArgs &a)
 {
-    return a.dtype != GS_TABLE_F32 && a.batch < ((int64_t)1 << 31) && attn_tma_ok(a.q, a.batch, a.q_len, a.q_heads) &&
-           attn_tma_ok(a.dout, a.batch, a.q_len, a.q_heads) && attn_tma_ok(a.k, a.batch, a.k_len, a.kv_heads) &&
-           attn_tma_ok(a.v, a.batch, a.k_len, a.kv_heads);
+    return a.dtype != GS_TABLE_F32 && a.batch < ((int64_t)1 << 31) && attn_tma_ok(a.q, a.dtype, a.batch, a.q_len, a.q_heads) &&
+           attn_tma_ok(a.dout, a.dtype, a.batch, a.q_len, a.q_heads) && attn_tma_ok(a.k, a.dtype, a.batch, a.k_len, a.kv_heads) &&
+           attn_tma_ok(a.v, a.dtype, a.batch, a.k_len, a.kv_heads);
 }
 
 template <bool BF16, int DP>
@@ -829,10 +829,10 @@ gs_status attn_tc_backward(const AttnArgs &a, cudaStream_t st)
     const bool bf16 = a.dtype == GS_TABLE_BF16;
     BwdMaps m;
     gs_status s;
-    if ((s = attn_tensor_map(&m.q, a.q, bf16, a.batch, a.q_len, a.q_heads, a.dim, 64, 128)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.dout, a.dout, bf16, a.batch, a.q_len, a.q_heads, a.dim, 64, 128)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.k, a.k, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
-    if ((s = attn_tensor_map(&m.v, a.v, bf16, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.q, a.q, a.dtype, a.batch, a.q_len, a.q_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.dout, a.dout, a.dtype, a.batch, a.q_len, a.q_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.k, a.k, a.dtype, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
+    if ((s = attn_tensor_map(&m.v, a.v, a.dtype, a.batch, a.k_len, a.kv_heads, a.dim, 64, 128)) != GS_OK) return s;
     BwdNorms nm;
     nm.dout = a.delta + a.batch * a.q_heads * (int64_t)a.q_len;
     nm.v = nm.dout + a.batch * a.q_heads * tiles_of(a.q_len);

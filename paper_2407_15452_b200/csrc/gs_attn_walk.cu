@@ -1,14 +1,15 @@
-// Attention of short 16-bit sequences (up to 128 positions): walks.
+// Attention of short sequences (up to 128 positions): walks.
 //
 // A walk's scores are a few 16 x 16 blocks, far less than a 128 x 128 tensor-core tile, and there are
 // tens of thousands of walks: the bound is the traffic of q, k, v and the results.  So a unit - one head of one
 // sequence - is brought to shared memory once, whole, and everything happens there and in registers:
-// one warp per 16 rows, mma.sync m16n8k16 on 16 x 16 blocks, and only blocks that the window reaches.
+// one warp per 16 rows, mma.sync on 16 x 16 blocks (fp32 as three tf32 products), and only blocks that the window
+// reaches.
 // The grid is as large as fits the device; a block goes through its share of the units, several at a time, and
 // TMA brings the next ones into a second set of tiles meanwhile.  Results leave through TMA too, from the
 // tiles whose rows they replace.  Tensors that TMA cannot address (odd strides or addresses) are copied by
 // the threads, and results stored by them.
-//  forward : scores of up to 64 keys at a time in registers, running maximum and sum over those
+//  forward : scores of up to 48 keys at a time in registers, running maximum and sum over those
 //  backward: dq by query rows, then dk and dv by key rows, both from the same copy in shared memory.  delta =
 //            sum_j p_ij dp_ij comes from the probabilities themselves (a first walk over the row's blocks), so
 //            the forward output is neither read nor is its rounding part of the gradient.
@@ -17,7 +18,7 @@
 // shows depends on its distance from the diagonal only, and the few distances with a partly visible block
 // have their starting values in shared memory (a comparison and a select per score were a third of the
 // instructions, and instructions are what these kernels run out of first).
-// P and dS are rounded to the tensors' type for their products.  For binary16 they are scaled by powers
+// P and dS are rounded to 16-bit tensors' type for their products.  For binary16 they are scaled by powers
 // of two first, P by 2^14 (p <= 1), dS by the one that brings its bound |dS| <= max|dp| + |delta| below 2^15.
 #include "gs_attn_tc.cuh"
 
@@ -27,24 +28,24 @@ using namespace tc;
 
 static constexpr int KEEP = 3;                    // blocks of 16 keys whose scores the forward pass holds
 
-// A tile holds the padded rows of one head as TMA writes them: rows of DP values (of 64 values in two halves,
-// if DP is 128) whose 16-byte chunks are permuted within 8 rows, so that eight rows at one column fall
-// into different banks.
-template <int DP>
+enum Kind { F16, BF16, F32 };
+
+// A tile holds the padded rows of one head as TMA writes them: rows of DP values, in pieces of at most 128 bytes a
+// row (one after the other), whose 16-byte chunks are permuted within 8 rows, so that eight rows at one
+// column fall into different banks.
+template <int K, int DP>
 struct Row {
-    static constexpr int HALVES = DP == 128 ? 2 : 1, BYTES = DP / HALVES * 2, CHUNKS = BYTES / 16;
+    static constexpr int SIZE = K == F32 ? 4 : 2, PIECES = DP * SIZE > 128 ? DP * SIZE / 128 : 1;
+    static constexpr int VALUES = DP / PIECES, BYTES = VALUES * SIZE, CHUNKS = BYTES / 16;
     static constexpr int FLIP = CHUNKS == 8 ? 0 : CHUNKS == 4 ? 1 : 2;         // row bits below the permutation
-    static constexpr uint32_t BLOCK = 16 * BYTES;                             // 16 rows of a half
-    // byte offset of chunk c of row r within a half
+    static constexpr uint32_t BLOCK = 16 * BYTES;                             // 16 rows of a piece
+    static constexpr int WORDS = K == F32 ? 4 : 2;                            // of a thread's four values in the tensors' type
+    // byte offset of chunk c of row r within a piece
     static __device__ __forceinline__ uint32_t at(int r, int c) { return r * BYTES + ((c ^ ((r >> FLIP) & (CHUNKS - 1))) << 4); }
-    static __host__ __device__ constexpr uint32_t tile(int rows16) { return HALVES * rows16 * BLOCK; }
+    static __host__ __device__ constexpr uint32_t tile(int rows16) { return PIECES * rows16 * BLOCK; }
 };
-// step k (16 values) of a row whose step 0 is at `block`; `half`: bytes of a half tile
-template <int DP>
-__device__ __forceinline__ uint32_t step_at(uint32_t block, int k, uint32_t half)
-{
-    return DP == 128 ? (block ^ (32 * (k & 3))) + (k >> 2) * half : block ^ (32 * k);
-}
+// lse, delta and bound of the padded query rows
+__host__ __device__ constexpr uint32_t stat_bytes(int qt) { return 3 * qt * 16 * 4; }
 
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t addr)
 {
@@ -56,99 +57,162 @@ __device__ __forceinline__ void ldm4t(uint32_t (&r)[4], uint32_t addr)
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-template <bool BF16>
+__device__ __forceinline__ float lds(uint32_t addr)
+{
+    float x;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(addr) : "memory");
+    return x;
+}
+template <int K>
 __device__ __forceinline__ void mma(float *c, const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    if constexpr (BF16)
+    if constexpr (K == BF16)
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
+    else if constexpr (K == F16)
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// A lane's offset in a block for ldmatrix.  The permutation of a row's chunks depends on the row within its 16
-// rows only, and chunk 2k + x is chunk x with bits of 2k flipped: a lane adds its offset to a block's
-// address once and takes step_at from there.
-template <int DP> __device__ __forceinline__ uint32_t lane_a() { const int l = threadIdx.x & 31; return Row<DP>::at(l & 15, l >> 4); }
-template <int DP> __device__ __forceinline__ uint32_t lane_b()
+// fp32 on the tensor cores: x = hi + lo, hi rounded to the 11 significant bits that tf32 keeps and lo what is left
+// (exact; its own last bits beyond 11 are dropped), and x y = hi hi + hi lo + lo hi with a relative error below 2^-21,
+// eight units of fp32, where the sum over the head dimension itself may be off by as many as it has terms.
+__device__ __forceinline__ void split(float x, uint32_t &hi, uint32_t &lo)
+{
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
+    lo = __float_as_uint(x - __uint_as_float(hi));
+}
+__device__ __forceinline__ void mma3(float *c, const uint32_t (&ah)[4], const uint32_t (&al)[4], float y0, float y1)
+{
+    uint32_t h0, l0, h1, l1;
+    split(y0, h0, l0);
+    split(y1, h1, l1);
+    mma<F32>(c, al, h0, h1);
+    mma<F32>(c, ah, l0, l1);
+    mma<F32>(c, ah, h0, h1);
+}
+
+// A lane's offset in a block of 16 rows.  The permutation of a row's chunks depends on the row within its 16 rows
+// only, and a later step of the columns is the first one with bits of its chunk flipped: a lane adds its offset to a
+// block's address once and flips from there.
+//  rows: as the A operand; dot: as the B operand of a product over columns; mul: of one over rows
+// 16-bit values come by ldmatrix, fp32 values one by one: lane (g, t) = (lane / 4, lane % 4) holds rows g and
+// g + 8, columns t and t + 4 of a step of eight, or for mul rows 2t and 2t + 1 - the order in which a thread holds
+// its scores, so that they serve as A operand as they are - of column g.
+template <int K, int DP> __device__ __forceinline__ uint32_t lane_dot()
 {
     const int l = threadIdx.x & 31;
-    return Row<DP>::at((l & 7) + ((l >> 4) << 3), (l >> 3) & 1);
+    if constexpr (K == F32) return Row<K, DP>::at(l >> 2, 0) + 4 * (l & 3);
+    else return Row<K, DP>::at((l & 7) + ((l >> 4) << 3), (l >> 3) & 1);
 }
-// lse, delta and bound of the padded query rows
-__host__ __device__ constexpr uint32_t stat_bytes(int qt) { return 3 * qt * 16 * 4; }
-
-// A fragments of 16 rows; `block` includes lane_a
-template <int DP>
-__device__ __forceinline__ void load_a(uint32_t (&f)[DP / 16][4], uint32_t block, uint32_t half)
+template <int K, int DP> __device__ __forceinline__ uint32_t lane_mul()
 {
-#pragma unroll
-    for (int k = 0; k < DP / 16; ++k) ldm4(f[k], step_at<DP>(block, k, half));
+    const int l = threadIdx.x & 31;
+    if constexpr (K == F32) return Row<K, DP>::at(2 * (l & 3), l >> 4) + 4 * ((l >> 2) & 3);
+    else return Row<K, DP>::at(l & 15, l >> 4);
 }
-
-// s[16 x 16] += A B^T, the 16 rows of B are the columns; `block` includes lane_b.  s[0..3]: columns 0-7, s[4..7]: 8-15
-template <bool BF16, int DP>
-__device__ __forceinline__ void block_dot(float (&s)[8], const uint32_t (&a)[DP / 16][4], uint32_t block, uint32_t half)
+template <int K, int DP> __device__ __forceinline__ uint32_t lane_rows()
 {
-#pragma unroll
-    for (int k = 0; k < DP / 16; ++k) {
-        uint32_t f[4];
-        ldm4(f, step_at<DP>(block, k, half));
-        mma<BF16>(s, a[k], f[0], f[1]);
-        mma<BF16>(s + 4, a[k], f[2], f[3]);
-    }
+    if constexpr (K == F32) return lane_dot<K, DP>();
+    else return lane_mul<K, DP>();
+}
+// step k of the columns (32 bytes) of a row whose step 0 is at `block`; `piece`: bytes of a piece of a tile
+template <int K, int DP>
+__device__ __forceinline__ uint32_t step_at(uint32_t block, int k, uint32_t piece)
+{
+    constexpr int STEPS = Row<K, DP>::BYTES / 32;
+    return (block ^ (32 * (k % STEPS))) + (Row<K, DP>::PIECES > 1 ? (k / STEPS) * piece : 0);
 }
 
-// The 16 rows that a warp multiplies with block after block: in registers where they are few, from shared
-// memory each time where they would crowd out the accumulators (head_dim above 32)
-template <int DP>
+// The 16 rows that a warp multiplies with block after block: in registers (HELD), or from shared
+// memory each time where they would crowd out the accumulators
+template <int K, int DP, bool HELD = DP <= 32>
 struct Rows {
-    static constexpr bool HELD = DP <= 32;
-    uint32_t f[HELD ? DP / 16 : 1][4], block, half;
-    __device__ __forceinline__ Rows(uint32_t b, uint32_t h) : block(b), half(h)
+    static constexpr int STEPS = DP * Row<K, DP>::SIZE / 32;                  // of 16 values, or of 8 fp32 values
+    uint32_t f[HELD ? STEPS : 1][4], g[HELD && K == F32 ? STEPS : 1][4], block, piece;      // fp32: hi and lo
+    __device__ __forceinline__ Rows(uint32_t b, uint32_t p) : block(b), piece(p)
     {
-        if constexpr (HELD) load_a<DP>(f, block, half);
+        if constexpr (HELD) {
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) load(f[k], g[K == F32 ? k : 0], k);
+        }
+    }
+    __device__ __forceinline__ void load(uint32_t (&hi)[4], uint32_t (&lo)[4], int k) const
+    {
+        const uint32_t at = step_at<K, DP>(block, k, piece);
+        if constexpr (K == F32) {
+            split(lds(at), hi[0], lo[0]);
+            split(lds(at + 8 * Row<K, DP>::BYTES), hi[1], lo[1]);
+            split(lds(at ^ 16), hi[2], lo[2]);
+            split(lds((at ^ 16) + 8 * Row<K, DP>::BYTES), hi[3], lo[3]);
+        } else {
+            ldm4(hi, at);
+        }
     }
 };
-template <bool BF16, int DP>
-__device__ __forceinline__ void block_dot(float (&s)[8], const Rows<DP> &a, uint32_t block, uint32_t half)
+
+// s[16 x 16] += A B^T, the 16 rows of B are the columns; `block` includes lane_dot.  s[0..3]: columns 0-7, s[4..7]: 8-15
+template <int K, int DP, bool HELD>
+__device__ __forceinline__ void block_dot(float (&s)[8], const Rows<K, DP, HELD> &a, uint32_t block, uint32_t piece)
 {
-    if constexpr (Rows<DP>::HELD) {
-        block_dot<BF16, DP>(s, a.f, block, half);
-    } else {
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k) {
-            uint32_t x[4], f[4];
-            ldm4(x, step_at<DP>(a.block, k, a.half));
-            ldm4(f, step_at<DP>(block, k, half));
-            mma<BF16>(s, x, f[0], f[1]);
-            mma<BF16>(s + 4, x, f[2], f[3]);
+    for (int k = 0; k < Rows<K, DP, HELD>::STEPS; ++k) {
+        uint32_t hi[4], lo[4];
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                hi[i] = a.f[k][i];
+                if constexpr (K == F32) lo[i] = a.g[k][i];
+            }
+        } else {
+            a.load(hi, lo, k);
+        }
+        const uint32_t at = step_at<K, DP>(block, k, piece);
+        if constexpr (K == F32) {
+            mma3(s, hi, lo, lds(at), lds(at ^ 16));
+            mma3(s + 4, hi, lo, lds(at + 8 * Row<K, DP>::BYTES), lds((at ^ 16) + 8 * Row<K, DP>::BYTES));
+        } else {
+            uint32_t f[4];
+            ldm4(f, at);
+            mma<K>(s, hi, f[0], f[1]);
+            mma<K>(s + 4, hi, f[2], f[3]);
         }
     }
 }
 
-// acc[16 x DP] += p[16 x 16] B, the 16 rows of B summed over; `block` includes lane_a
-template <bool BF16, int DP>
-__device__ __forceinline__ void block_mul(float (&acc)[DP / 8][4], const uint32_t (&p)[4], uint32_t block, uint32_t half)
+// acc[16 x DP] += p[16 x 16] B, the 16 rows of B summed over; `block` includes lane_mul.  The thread's values of p,
+// eight columns of which are s[0..3] and s[4..7], are the A operand as they stand, rounded for 16-bit types.
+template <int K, int DP>
+__device__ __forceinline__ void block_mul(float (&acc)[DP / 8][4], const float (&s)[8], uint32_t block, uint32_t piece)
 {
+    if constexpr (K == F32) {
 #pragma unroll
-    for (int d = 0; d < DP / 16; ++d) {
-        uint32_t f[4];
-        ldm4t(f, step_at<DP>(block, d, half));
-        mma<BF16>(acc[2 * d], p, f[0], f[1]);
-        mma<BF16>(acc[2 * d + 1], p, f[2], f[3]);
+        for (int j = 0; j < 2; ++j) {
+            uint32_t hi[4], lo[4];
+            split(s[4 * j], hi[0], lo[0]);
+            split(s[4 * j + 2], hi[1], lo[1]);
+            split(s[4 * j + 1], hi[2], lo[2]);
+            split(s[4 * j + 3], hi[3], lo[3]);
+#pragma unroll
+            for (int d = 0; d < DP / 8; ++d) {
+                const uint32_t at = step_at<K, DP>(block + j * 8 * Row<K, DP>::BYTES, d, piece);
+                mma3(acc[d], hi, lo, lds(at), lds(at ^ (Row<K, DP>::BYTES | 16)));
+            }
+        }
+    } else {
+        const uint32_t p[4] = {pack2<K == BF16>(s[0], s[1]), pack2<K == BF16>(s[2], s[3]), pack2<K == BF16>(s[4], s[5]),
+                               pack2<K == BF16>(s[6], s[7])};
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) {
+            uint32_t f[4];
+            ldm4t(f, step_at<K, DP>(block, d, piece));
+            mma<K>(acc[2 * d], p, f[0], f[1]);
+            mma<K>(acc[2 * d + 1], p, f[2], f[3]);
+        }
     }
-}
-
-// the C layout of two 8-column blocks is the A layout of one 16-column block
-template <bool BF16>
-__device__ __forceinline__ void as_a(uint32_t (&p)[4], const float (&s)[8])
-{
-    p[0] = pack2<BF16>(s[0], s[1]);
-    p[1] = pack2<BF16>(s[2], s[3]);
-    p[2] = pack2<BF16>(s[4], s[5]);
-    p[3] = pack2<BF16>(s[6], s[7]);
 }
 
 // offset of value i's column from the thread's first one (rows: lane / 4 for i & 2 == 0, + 8 otherwise)
@@ -239,105 +303,140 @@ struct WalkMaps {                     // boxes of all rows for the inputs, of 16
 };
 
 // one head's rows through TMA (one thread)
-template <int DP>
-__device__ __forceinline__ void tma_head(uint32_t dst, const CUtensorMap *map, uint32_t bar, int head, int64_t b, uint32_t half)
+template <int K, int DP>
+__device__ __forceinline__ void tma_head(uint32_t dst, const CUtensorMap *map, uint32_t bar, int head, int64_t b, uint32_t piece)
 {
 #pragma unroll
-    for (int x = 0; x < Row<DP>::HALVES; ++x) tma_load(dst + x * half, map, bar, x * 64, 0, head, (int)b);
+    for (int x = 0; x < Row<K, DP>::PIECES; ++x) tma_load(dst + x * piece, map, bar, x * Row<K, DP>::VALUES, 0, head, (int)b);
+}
+
+// 16 bytes of a row from value c on in global memory, zeros from value dim on; and back
+template <int K>
+__device__ __forceinline__ uint4 read_chunk(const void *row, int c, int dim, bool vec)
+{
+    uint32_t u[4] = {};
+    if (vec) {
+        if (c < dim) return __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(row) + c * (K == F32 ? 4 : 2)));
+    } else if constexpr (K == F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < dim) u[i] = reinterpret_cast<const uint32_t *>(row)[c + i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < dim) u[i / 2] |= (uint32_t) reinterpret_cast<const uint16_t *>(row)[c + i] << (16 * (i & 1));
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+template <int K>
+__device__ __forceinline__ void write_chunk(void *row, int c, int dim, bool vec, uint4 w)
+{
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+    if (vec) {
+        if (c < dim) *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(row) + c * (K == F32 ? 4 : 2)) = w;
+    } else if constexpr (K == F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < dim) reinterpret_cast<uint32_t *>(row)[c + i] = v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < dim) reinterpret_cast<uint16_t *>(row)[c + i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+    }
+}
+template <int K>
+__device__ __forceinline__ char *row_at(const AttnTensor &t, int64_t b, int h, int r)
+{
+    return reinterpret_cast<char *>(t.p) + (b * t.sb + h * t.sh + (int64_t)r * t.sl) * (K == F32 ? 4 : 2);
 }
 
 // rows [0, pad) of one head by `threads` threads: rows >= n and values >= dim are zeros
-template <int DP>
+template <int K, int DP>
 __device__ __forceinline__ void copy_head(uint32_t dst, const AttnTensor &t, int64_t b, int h, int n, int pad, int dim,
                                           bool vec, int tid, int threads)
 {
-    constexpr int CH = DP / 8;
-    const uint16_t *base = reinterpret_cast<const uint16_t *>(t.p) + b * t.sb + h * t.sh;
+    constexpr int CH = Row<K, DP>::CHUNKS * Row<K, DP>::PIECES, PER = 16 / Row<K, DP>::SIZE;
     for (int e = tid; e < pad * CH; e += threads) {
         const int r = e / CH, c = e % CH;
-        const uint16_t *from = base + (int64_t)r * t.sl + c * 8;
-        uint32_t u[4] = {};
-        if (r < n && vec) {
-            if (c * 8 < dim) {
-                const uint4 w = __ldg(reinterpret_cast<const uint4 *>(from));
-                u[0] = w.x; u[1] = w.y; u[2] = w.z; u[3] = w.w;
-            }
-        } else if (r < n) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c * 8 + i < dim) u[i / 2] |= (uint32_t)from[i] << (16 * (i & 1));
-        }
-        const uint32_t to = dst + (c / Row<DP>::CHUNKS) * pad * Row<DP>::BYTES + Row<DP>::at(r, c % Row<DP>::CHUNKS);
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
+        const uint4 u = r < n ? read_chunk<K>(row_at<K>(t, b, h, r), c * PER, dim, vec) : make_uint4(0, 0, 0, 0);
+        const uint32_t to = dst + (c / Row<K, DP>::CHUNKS) * pad * Row<K, DP>::BYTES + Row<K, DP>::at(r, c % Row<K, DP>::CHUNKS);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
     }
 }
 
 // rows [n, pad) become zeros: they take part in sums over rows, where a zero probability must not meet a NaN
-template <int DP>
+template <int K, int DP>
 __device__ __forceinline__ void zero_rows(uint32_t tile, int n, int pad, int tid, int threads)
 {
-    for (int e = n * Row<DP>::CHUNKS + tid; e < pad * Row<DP>::CHUNKS; e += threads)
+    for (int e = n * Row<K, DP>::CHUNKS + tid; e < pad * Row<K, DP>::CHUNKS; e += threads)
 #pragma unroll
-        for (int x = 0; x < Row<DP>::HALVES; ++x)
-            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + x * pad * Row<DP>::BYTES + e * 16), "r"(0) : "memory");
+        for (int x = 0; x < Row<K, DP>::PIECES; ++x)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + x * pad * Row<K, DP>::BYTES + e * 16), "r"(0) : "memory");
 }
 
 // the 16 x DP accumulator times its two row factors, in the tensors' type
-template <bool BF16, int DP>
-__device__ __forceinline__ void pack_tile(uint32_t (&u)[DP / 8][2], const float (&acc)[DP / 8][4], float f0, float f1)
+template <int K, int DP>
+__device__ __forceinline__ void pack_tile(uint32_t (&u)[DP / 8][Row<K, DP>::WORDS], const float (&acc)[DP / 8][4], float f0, float f1)
 {
 #pragma unroll
     for (int c = 0; c < DP / 8; ++c) {
-        u[c][0] = pack2<BF16>(acc[c][0] * f0, acc[c][1] * f0);
-        u[c][1] = pack2<BF16>(acc[c][2] * f1, acc[c][3] * f1);
+        if constexpr (K == F32) {
+            u[c][0] = __float_as_uint(acc[c][0] * f0);
+            u[c][1] = __float_as_uint(acc[c][1] * f0);
+            u[c][2] = __float_as_uint(acc[c][2] * f1);
+            u[c][3] = __float_as_uint(acc[c][3] * f1);
+        } else {
+            u[c][0] = pack2<K == BF16>(acc[c][0] * f0, acc[c][1] * f0);
+            u[c][1] = pack2<K == BF16>(acc[c][2] * f1, acc[c][3] * f1);
+        }
     }
 }
 
 // This warp's 16 x DP result, as pack_tile left it, to rows [r0, r0 + 16) of one head: first into the 16
 // rows at `stage` in shared memory, which nobody else reads any more, then in 16-byte pieces.
 // Rows >= n become zeros, rows >= len are not written.  TMA reads the stage until tma_stores_read.
-template <int DP>
-__device__ __forceinline__ void store_tile(const uint32_t (&u)[DP / 8][2], uint32_t stage, uint32_t half, const WalkPlan &plan,
-                                           const CUtensorMap *map, const AttnTensor &t, int64_t b, int h, int r0, int n, int len, int dim)
+template <int K, int DP>
+__device__ __forceinline__ void store_tile(const uint32_t (&u)[DP / 8][Row<K, DP>::WORDS], uint32_t stage, uint32_t piece,
+                                           const WalkPlan &plan, const CUtensorMap *map, const AttnTensor &t, int64_t b, int h,
+                                           int r0, int n, int len, int dim)
 {
-    constexpr int CH = Row<DP>::CHUNKS;
-    const int lane = threadIdx.x & 31, row = lane >> 2;
+    constexpr int CH = Row<K, DP>::CHUNKS, PER = 16 / Row<K, DP>::SIZE;
+    const int lane = threadIdx.x & 31, row = lane >> 2, t4 = lane & 3;
     const bool in0 = r0 + row < n, in1 = r0 + row + 8 < n;
     __syncwarp();
 #pragma unroll
-    for (int c = 0; c < DP / 8; ++c) {
-        const uint32_t lo = in0 ? u[c][0] : 0u, hi = in1 ? u[c][1] : 0u;
-        const uint32_t to = stage + (c / CH) * half + Row<DP>::at(row, c % CH) + 4 * (lane & 3);
-        asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(lo) : "memory");
-        asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 8 * Row<DP>::BYTES), "r"(hi) : "memory");      // row + 8: the same permutation
+    for (int c = 0; c < DP / 8; ++c) {                       // the thread's columns 8c + 2 t4 and the next
+        if constexpr (K == F32) {
+            const int chunk = 2 * c;
+            const uint32_t to = stage + (chunk / CH) * piece + Row<K, DP>::at(row, chunk % CH + (t4 >> 1)) + 8 * (t4 & 1);
+            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(in0 ? u[c][0] : 0u), "r"(in0 ? u[c][1] : 0u) : "memory");
+            asm volatile("st.shared.v2.u32 [%0], {%1, %2};"
+                         ::"r"(to + 8 * Row<K, DP>::BYTES), "r"(in1 ? u[c][2] : 0u), "r"(in1 ? u[c][3] : 0u) : "memory");
+        } else {
+            const uint32_t to = stage + (c / CH) * piece + Row<K, DP>::at(row, c % CH) + 4 * t4;
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(in0 ? u[c][0] : 0u) : "memory");
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 8 * Row<K, DP>::BYTES), "r"(in1 ? u[c][1] : 0u) : "memory");   // row + 8: the same permutation
+        }
     }
     if (plan.tma) {
         fence_async_shared();
         __syncwarp();
         if (lane == 0) {
 #pragma unroll
-            for (int x = 0; x < Row<DP>::HALVES; ++x) tma_store(map, stage + x * half, x * 64, r0, h, (int)b);
+            for (int x = 0; x < Row<K, DP>::PIECES; ++x) tma_store(map, stage + x * piece, x * Row<K, DP>::VALUES, r0, h, (int)b);
             tma_store_commit();
         }
         return;
     }
     __syncwarp();
-    uint16_t *base = reinterpret_cast<uint16_t *>(t.p) + b * t.sb + h * t.sh;
-    for (int e = lane; e < 2 * DP; e += 32) {
-        const int row = e / (DP / 8), c = e % (DP / 8), r = r0 + row;
-        if (r >= len || c * 8 >= dim) continue;
+    constexpr int ALL = CH * Row<K, DP>::PIECES;
+    for (int e = lane; e < 16 * ALL; e += 32) {
+        const int rr = e / ALL, c = e % ALL, r = r0 + rr;
+        if (r >= len) continue;
         uint4 w;
         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
-                     : "r"(stage + (c / CH) * half + Row<DP>::at(row, c % CH)) : "memory");
-        uint16_t *to = base + (int64_t)r * t.sl + c * 8;
-        if (plan.vec) {
-            *reinterpret_cast<uint4 *>(to) = w;
-        } else {
-            const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c * 8 + i < dim) to[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
-        }
+                     : "r"(stage + (c / CH) * piece + Row<K, DP>::at(rr, c % CH)) : "memory");
+        write_chunk<K>(row_at<K>(t, b, h, r), c * PER, dim, plan.vec, w);
     }
 }
 
@@ -356,13 +455,21 @@ __device__ __forceinline__ float quad_sum(float v)
 // 16384 walks of 40 with 4 heads of 32 (forward) and 8192 of 80 (backward): 80 registers and 8 warps 188 us, 64
 // registers 208, 108 registers 264; backward 96 registers 448 us, 128 registers with p and dp of three blocks kept
 // for the second walk over them 465, 80 registers 523.
-template <int DP, bool BWD> constexpr int registers() { return DP <= 32 ? (BWD ? 96 : 80) : DP == 64 ? 128 : 255; }
-template <int DP, bool BWD> constexpr int blocks_per_sm() { return DP <= 32 ? (BWD ? 4 : 3) : DP == 64 ? 2 : 1; }
+template <int K, int DP, bool BWD> constexpr int registers()
+{
+    if (K == F32) return DP <= 32 && !BWD ? 128 : DP <= 64 ? 168 : 255;
+    return DP <= 32 ? (BWD ? 96 : 80) : DP == 64 ? 128 : 255;
+}
+template <int K, int DP, bool BWD> constexpr int blocks_per_sm()
+{
+    if (K == F32) return DP <= 32 && !BWD ? 2 : 1;
+    return DP <= 32 ? (BWD ? 4 : 3) : DP == 64 ? 2 : 1;
+}
 static constexpr int BLOCK_WARPS = 8;             // a head of 128 rows
 
 // one warp per (unit, query tile)
-template <bool BF16, int DP>
-__global__ void __maxnreg__((registers<DP, false>()))
+template <int K, int DP>
+__global__ void __maxnreg__((registers<K, DP, false>()))
 attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ WalkPlan plan, const __grid_constant__ WalkMaps maps,
                          unsigned long long *stalls)
 {
@@ -371,8 +478,8 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     __shared__ volatile int stalled;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, qt = plan.qt, kt = plan.kt;
     const uint32_t total = (uint32_t)a.batch * a.q_heads, step = gridDim.x * plan.units;
-    const uint32_t q_half = qt * Row<DP>::BLOCK, k_half = kt * Row<DP>::BLOCK;
-    const uint32_t q_bytes = Row<DP>::tile(qt), k_bytes = Row<DP>::tile(kt), unit_bytes = q_bytes + 2 * k_bytes;
+    const uint32_t q_half = qt * Row<K, DP>::BLOCK, k_half = kt * Row<K, DP>::BLOCK;
+    const uint32_t q_bytes = Row<K, DP>::tile(qt), k_bytes = Row<K, DP>::tile(kt), unit_bytes = q_bytes + 2 * k_bytes;
     const int mine = (int)((uint32_t)warp / (uint32_t)qt), tile = warp - mine * qt;   // qt warps work on one unit
     const int tid = threadIdx.x - mine * qt * 32, threads = qt * 32;
     const uint32_t bars = smem_u32(full);
@@ -390,9 +497,9 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
         const uint32_t b = u / (uint32_t)a.q_heads;
         const int h = (int)(u - b * a.q_heads), g = h / a.group;
         bar_expect(bar, unit_bytes);
-        tma_head<DP>(Q, &maps.q, bar, h, b, q_half);
-        tma_head<DP>(Q + q_bytes, &maps.k, bar, g, b, k_half);
-        tma_head<DP>(Q + q_bytes + k_bytes, &maps.v, bar, g, b, k_half);
+        tma_head<K, DP>(Q, &maps.q, bar, h, b, q_half);
+        tma_head<K, DP>(Q + q_bytes, &maps.k, bar, g, b, k_half);
+        tma_head<K, DP>(Q + q_bytes + k_bytes, &maps.v, bar, g, b, k_half);
     };
     if (threadIdx.x == 0) {
         stalled = 0;
@@ -411,17 +518,17 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     const int st = n & (plan.stages - 1);
     const bool active = u < total;
     const Unit l = unit_of(a, active ? u : u0, a.q_heads);
-    const uint32_t Q = tiles_at(st), K = Q + q_bytes, V = K + k_bytes;
+    const uint32_t Q = tiles_at(st), Kt = Q + q_bytes, V = Kt + k_bytes;
     bool ok = true;
     if (plan.tma) {
         ok = bar_wait(bars + 8 * st, (n >> (plan.stages - 1)) & 1, &stalled);
     } else if (active) {
         const int g = l.h / a.group;
-        copy_head<DP>(Q, a.q, l.b, l.h, l.s.nq, qt * 16, a.dim, plan.vec, tid, threads);
-        copy_head<DP>(K, a.k, l.b, g, l.s.nk, kt * 16, a.dim, plan.vec, tid, threads);
-        copy_head<DP>(V, a.v, l.b, g, l.s.nk, kt * 16, a.dim, plan.vec, tid, threads);
+        copy_head<K, DP>(Q, a.q, l.b, l.h, l.s.nq, qt * 16, a.dim, plan.vec, tid, threads);
+        copy_head<K, DP>(Kt, a.k, l.b, g, l.s.nk, kt * 16, a.dim, plan.vec, tid, threads);
+        copy_head<K, DP>(V, a.v, l.b, g, l.s.nk, kt * 16, a.dim, plan.vec, tid, threads);
     }
-    if (ragged && ok && l.s.nk < a.k_len) zero_rows<DP>(V, l.s.nk, kt * 16, tid, threads);
+    if (ragged && ok && l.s.nk < a.k_len) zero_rows<K, DP>(V, l.s.nk, kt * 16, tid, threads);
     if (!__syncthreads_and(ok)) break;
     if (active) {
     const int r0 = tile * 16, ra = r0 + (lane >> 2), rb = ra + 8;
@@ -430,9 +537,8 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     const int r_end = min(r0 + 16, l.s.nq);
     const int j_begin = attn_lo(a, l.s, r0) / 16, j_end = r_end > r0 ? (attn_hi(a, l.s, r_end - 1) + 15) / 16 : 0;
     if (j_begin < j_end) {
-        uint32_t qf[DP / 16][4];
-        load_a<DP>(qf, Q + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half);
-        const uint32_t kb = K + lane_b<DP>(), vb = V + lane_a<DP>();
+        const Rows<K, DP, (K != F32 || DP <= 32)> qf(Q + tile * Row<K, DP>::BLOCK + lane_rows<K, DP>(), q_half);
+        const uint32_t kb = Kt + lane_dot<K, DP>(), vb = V + lane_mul<K, DP>();
         for (int j = j_begin; j < j_end; j += KEEP) {
             float s[KEEP][8];
             float m_a = top_a, m_b = top_b;
@@ -440,7 +546,7 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
             for (int x = 0; x < KEEP; ++x) {
                 if (j + x >= j_end) break;
                 start_scores(s[x], plan.rows, mask_rows, j + x - tile, l.s.off);
-                block_dot<BF16, DP>(s[x], qf, kb + (j + x) * Row<DP>::BLOCK, k_half);
+                block_dot<K, DP>(s[x], qf, kb + (j + x) * Row<K, DP>::BLOCK, k_half);
                 if ((j + x + 1) * 16 > l.s.nk) hide_from(s[x], l.s.nk - (j + x) * 16);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -475,9 +581,7 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
                     if (i & 2) sum_b += s[x][i];
                     else sum_a += s[x][i];
                 }
-                uint32_t p[4];
-                as_a<BF16>(p, s[x]);
-                block_mul<BF16, DP>(acc, p, vb + (j + x) * Row<DP>::BLOCK, k_half);
+                block_mul<K, DP>(acc, s[x], vb + (j + x) * Row<K, DP>::BLOCK, k_half);
             }
         }
     }
@@ -488,9 +592,9 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
         if (ra < a.q_len) lse[ra] = sum_a == 0.f || ra >= l.s.nq ? -INFINITY : (top_a * mul + log2_fast(sum_a)) * LN2;
         if (rb < a.q_len) lse[rb] = sum_b == 0.f || rb >= l.s.nq ? -INFINITY : (top_b * mul + log2_fast(sum_b)) * LN2;
     }
-    uint32_t out[DP / 8][2];
-    pack_tile<BF16, DP>(out, acc, sum_a == 0.f ? 0.f : rcp_fast(sum_a), sum_b == 0.f ? 0.f : rcp_fast(sum_b));
-    store_tile<DP>(out, Q + tile * Row<DP>::BLOCK, q_half, plan, &maps.out, a.out, l.b, l.h, r0, l.s.nq, a.q_len, a.dim);
+    uint32_t out[DP / 8][Row<K, DP>::WORDS];
+    pack_tile<K, DP>(out, acc, sum_a == 0.f ? 0.f : rcp_fast(sum_a), sum_b == 0.f ? 0.f : rcp_fast(sum_b));
+    store_tile<K, DP>(out, Q + tile * Row<K, DP>::BLOCK, q_half, plan, &maps.out, a.out, l.b, l.h, r0, l.s.nq, a.q_len, a.dim);
     }
     if (plan.tma) {
         if (lane == 0) tma_stores_read();
@@ -503,18 +607,18 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
 }
 
 // power of two that brings a bound below 2^15 (binary16 only)
-template <bool BF16>
+template <int K>
 __device__ __forceinline__ float lift(float bound)
 {
-    if (BF16 || !(bound > 0.f) || !isfinite(bound)) return 1.f;
+    if (K != F16 || !(bound > 0.f) || !isfinite(bound)) return 1.f;
     const int e = (int)((__float_as_uint(bound) >> 23) & 255) - 126;       // bound < 2^e
     return __uint_as_float((uint32_t)(min(max(15 - e, -100), 100) + 127) << 23);
 }
 
 // `tiles` = max(qt, kt) warps per unit; a unit is a key/value head, gone through once per query head of its group.
 // SHARED: several query heads per key/value head.
-template <bool BF16, int DP, bool SHARED>
-__global__ void __maxnreg__((registers<DP, true>()))
+template <int K, int DP, bool SHARED>
+__global__ void __maxnreg__((registers<K, DP, true>()))
 attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ WalkPlan plan, const __grid_constant__ WalkMaps maps,
                           unsigned long long *stalls)
 {
@@ -523,8 +627,8 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
     __shared__ volatile int stalled;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, qt = plan.qt, kt = plan.kt, tiles = max(qt, kt);
     const uint32_t total = (uint32_t)a.batch * a.kv_heads, step = gridDim.x * plan.units;
-    const uint32_t q_half = qt * Row<DP>::BLOCK, k_half = kt * Row<DP>::BLOCK;
-    const uint32_t q_bytes = Row<DP>::tile(qt), k_bytes = Row<DP>::tile(kt), unit_bytes = 2 * q_bytes + 2 * k_bytes;
+    const uint32_t q_half = qt * Row<K, DP>::BLOCK, k_half = kt * Row<K, DP>::BLOCK;
+    const uint32_t q_bytes = Row<K, DP>::tile(qt), k_bytes = Row<K, DP>::tile(kt), unit_bytes = 2 * q_bytes + 2 * k_bytes;
     const int mine = (int)((uint32_t)warp / (uint32_t)tiles), tile = warp - mine * tiles;
     const int tid = threadIdx.x - mine * tiles * 32, threads = tiles * 32;
     const uint32_t bars = smem_u32(full);
@@ -547,10 +651,10 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
         const uint32_t b = u / (uint32_t)a.kv_heads;
         const int g = (int)(u - b * a.kv_heads), h = g * group + x;
         bar_expect(bar, unit_bytes);
-        tma_head<DP>(Q, &maps.q, bar, h, b, q_half);
-        tma_head<DP>(Q + q_bytes, &maps.dout, bar, h, b, q_half);
-        tma_head<DP>(Q + 2 * q_bytes, &maps.k, bar, g, b, k_half);
-        tma_head<DP>(Q + 2 * q_bytes + k_bytes, &maps.v, bar, g, b, k_half);
+        tma_head<K, DP>(Q, &maps.q, bar, h, b, q_half);
+        tma_head<K, DP>(Q + q_bytes, &maps.dout, bar, h, b, q_half);
+        tma_head<K, DP>(Q + 2 * q_bytes, &maps.k, bar, g, b, k_half);
+        tma_head<K, DP>(Q + 2 * q_bytes + k_bytes, &maps.v, bar, g, b, k_half);
     };
     if (threadIdx.x == 0) {
         stalled = 0;
@@ -579,7 +683,7 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
     for (int x = 0; x < group; ++x, ++n) {
         const int st = n & (plan.stages - 1);
         const int h = l.h * group + x;
-        const uint32_t Q = tiles_at(st), DO = Q + q_bytes, K = DO + q_bytes, V = K + k_bytes;
+        const uint32_t Q = tiles_at(st), DO = Q + q_bytes, Kt = DO + q_bytes, V = Kt + k_bytes;
         const float *lse = a.lse + (l.b * a.q_heads + h) * a.q_len;
         for (int r = tid; r < qt * 16; r += threads) {
             const float v = r < s.nq ? -lse[r] * LOG2E : -INFINITY;
@@ -588,41 +692,41 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
         if (plan.tma) {
             ok = bar_wait(bars + 8 * st, (n >> (plan.stages - 1)) & 1, &stalled);
         } else if (active) {
-            copy_head<DP>(Q, a.q, l.b, h, s.nq, qt * 16, a.dim, plan.vec, tid, threads);
-            copy_head<DP>(DO, a.dout, l.b, h, s.nq, qt * 16, a.dim, plan.vec, tid, threads);
-            copy_head<DP>(K, a.k, l.b, l.h, s.nk, kt * 16, a.dim, plan.vec, tid, threads);
-            copy_head<DP>(V, a.v, l.b, l.h, s.nk, kt * 16, a.dim, plan.vec, tid, threads);
+            copy_head<K, DP>(Q, a.q, l.b, h, s.nq, qt * 16, a.dim, plan.vec, tid, threads);
+            copy_head<K, DP>(DO, a.dout, l.b, h, s.nq, qt * 16, a.dim, plan.vec, tid, threads);
+            copy_head<K, DP>(Kt, a.k, l.b, l.h, s.nk, kt * 16, a.dim, plan.vec, tid, threads);
+            copy_head<K, DP>(V, a.v, l.b, l.h, s.nk, kt * 16, a.dim, plan.vec, tid, threads);
         }
         if (ragged && ok && s.nq < a.q_len) {
-            zero_rows<DP>(Q, s.nq, qt * 16, tid, threads);
-            zero_rows<DP>(DO, s.nq, qt * 16, tid, threads);
+            zero_rows<K, DP>(Q, s.nq, qt * 16, tid, threads);
+            zero_rows<K, DP>(DO, s.nq, qt * 16, tid, threads);
         }
         if (ragged && ok && s.nk < a.k_len) {
-            zero_rows<DP>(K, s.nk, kt * 16, tid, threads);
-            zero_rows<DP>(V, s.nk, kt * 16, tid, threads);
+            zero_rows<K, DP>(Kt, s.nk, kt * 16, tid, threads);
+            zero_rows<K, DP>(V, s.nk, kt * 16, tid, threads);
         }
         ok = __syncthreads_and(ok);
         if (!ok) break;
 
         // ---- dq of 16 query rows
-        uint32_t dq[DP / 8][2] = {};
+        uint32_t dq[DP / 8][Row<K, DP>::WORDS] = {};
         const int r0 = tile * 16;
         if (active && tile < qt) {
             const int ra = r0 + (lane >> 2), rb = ra + 8;
             const int r_end = min(r0 + 16, s.nq);
             const int j_begin = attn_lo(a, s, r0) / 16, j_end = r_end > r0 ? (attn_hi(a, s, r_end - 1) + 15) / 16 : 0;
             const float l_a = neg_lse[ra], l_b = neg_lse[rb];
-            const Rows<DP> qf(Q + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half), df(DO + tile * Row<DP>::BLOCK + lane_a<DP>(), q_half);
-            const uint32_t lb = lane_b<DP>(), kb = K + lane_a<DP>();
+            const Rows<K, DP> qf(Q + tile * Row<K, DP>::BLOCK + lane_rows<K, DP>(), q_half), df(DO + tile * Row<K, DP>::BLOCK + lane_rows<K, DP>(), q_half);
+            const uint32_t lb = lane_dot<K, DP>(), kb = Kt + lane_mul<K, DP>();
             float d_a = 0.f, d_b = 0.f, m_a = 0.f, m_b = 0.f;
             // p and dp of one block
             auto scores = [&](int j, float (&p)[8], float (&dp)[8]) {
                 start_scores(p, plan.rows, mask_rows, j - tile, s.off);
-                block_dot<BF16, DP>(p, qf, K + lb + j * Row<DP>::BLOCK, k_half);
+                block_dot<K, DP>(p, qf, Kt + lb + j * Row<K, DP>::BLOCK, k_half);
                 if ((j + 1) * 16 > s.nk) hide_from(p, s.nk - j * 16);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) dp[i] = 0.f;
-                block_dot<BF16, DP>(dp, df, V + lb + j * Row<DP>::BLOCK, k_half);
+                block_dot<K, DP>(dp, df, V + lb + j * Row<K, DP>::BLOCK, k_half);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) p[i] = exp2_fast(fmaf(p[i], mul, i & 2 ? l_b : l_a));
             };
@@ -631,10 +735,10 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
                 for (int i = 0; i < 8; ++i) {
                     if (i & 2) {
                         d_b = fmaf(p[i], dp[i], d_b);
-                        if constexpr (!BF16) m_b = fmaxf(m_b, fabsf(dp[i]));
+                        if constexpr (K == F16) m_b = fmaxf(m_b, fabsf(dp[i]));
                     } else {
                         d_a = fmaf(p[i], dp[i], d_a);
-                        if constexpr (!BF16) m_a = fmaxf(m_a, fabsf(dp[i]));
+                        if constexpr (K == F16) m_a = fmaxf(m_a, fabsf(dp[i]));
                     }
                 }
             };
@@ -642,16 +746,16 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
             auto rows_known = [&] {
                 d_a = quad_sum(d_a);
                 d_b = quad_sum(d_b);
-                if constexpr (!BF16) {
+                if constexpr (K == F16) {
                     m_a = quad_max(m_a) + fabsf(d_a);
                     m_b = quad_max(m_b) + fabsf(d_b);
-                    up_a = lift<BF16>(m_a);
-                    up_b = lift<BF16>(m_b);
+                    up_a = lift<K>(m_a);
+                    up_b = lift<K>(m_b);
                 }
                 if ((lane & 3) == 0) {
                     neg_delta[ra] = -d_a;
                     neg_delta[rb] = -d_b;
-                    if constexpr (!BF16) {
+                    if constexpr (K == F16) {
                         bound[ra] = m_a;
                         bound[rb] = m_b;
                     }
@@ -660,10 +764,8 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
             float acc[DP / 8][4] = {}, nd_a = 0.f, nd_b = 0.f;                // nd: -delta, scaled
             auto add = [&](int j, float (&p)[8], const float (&dp)[8]) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] *= BF16 ? dp[i] - (i & 2 ? d_b : d_a) : fmaf(dp[i], i & 2 ? up_b : up_a, i & 2 ? nd_b : nd_a);
-                uint32_t w[4];
-                as_a<BF16>(w, p);
-                block_mul<BF16, DP>(acc, w, kb + j * Row<DP>::BLOCK, k_half);
+                for (int i = 0; i < 8; ++i) p[i] *= K != F16 ? dp[i] - (i & 2 ? d_b : d_a) : fmaf(dp[i], i & 2 ? up_b : up_a, i & 2 ? nd_b : nd_a);
+                block_mul<K, DP>(acc, p, kb + j * Row<K, DP>::BLOCK, k_half);
             };
             float p[8], dp[8];
             for (int j = j_begin; j < j_end; ++j) {
@@ -677,7 +779,7 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
                 scores(j, p, dp);
                 add(j, p, dp);
             }
-            pack_tile<BF16, DP>(dq, acc, a.scale / up_a, a.scale / up_b);
+            pack_tile<K, DP>(dq, acc, a.scale / up_a, a.scale / up_b);
         }
         __syncthreads();
 
@@ -687,12 +789,12 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
             const int j_end = min(j0 + 16, s.nk);
             const int q_begin = attn_q_first(a, s, j0) / 16, q_end = j_end > j0 ? (attn_q_last(a, s, j_end) + 15) / 16 : 0;
             float up_p = 1.f;                                 // of dp - delta, beside a p that is scaled itself
-            if constexpr (!BF16) {                           // one scale per head: dk sums over its queries
+            if constexpr (K == F16) {                           // one scale per head: dk sums over its queries
                 float m = 0.f;
                 for (int r = lane; r < qt * 16; r += 32) m = fmaxf(m, bound[r]);
 #pragma unroll
                 for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                const float up = lift<BF16>(m);
+                const float up = lift<K>(m);
                 // a shared head's sums are carried from one query head's scale to the next one's
                 if (x > 0 && up != up_k) {
 #pragma unroll
@@ -704,23 +806,23 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
                 up_p = up / 16384.f;
             }
             if (q_begin < q_end) {
-                const Rows<DP> kf(K + tile * Row<DP>::BLOCK + lane_a<DP>(), k_half), vf(V + tile * Row<DP>::BLOCK + lane_a<DP>(), k_half);
-                const uint32_t lb = lane_b<DP>(), la = lane_a<DP>();
+                const Rows<K, DP> kf(Kt + tile * Row<K, DP>::BLOCK + lane_rows<K, DP>(), k_half), vf(V + tile * Row<K, DP>::BLOCK + lane_rows<K, DP>(), k_half);
+                const uint32_t lb = lane_dot<K, DP>(), la = lane_mul<K, DP>();
                 for (int q = q_begin; q < q_end; ++q) {
-                    const uint32_t qb = Q + q * Row<DP>::BLOCK, ob = DO + q * Row<DP>::BLOCK;
+                    const uint32_t qb = Q + q * Row<K, DP>::BLOCK, ob = DO + q * Row<K, DP>::BLOCK;
                     float p[8], dp[8];
                     // queries past the end: their lse makes p zero
                     start_scores(p, plan.cols, mask_cols, q - tile, -s.off);
-                    block_dot<BF16, DP>(p, kf, qb + lb, q_half);
+                    block_dot<K, DP>(p, kf, qb + lb, q_half);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) dp[i] = 0.f;
-                    block_dot<BF16, DP>(dp, vf, ob + lb, q_half);
+                    block_dot<K, DP>(dp, vf, ob + lb, q_half);
                     const int c = q * 16 + 2 * (lane & 3);
 #pragma unroll
                     for (int n = 0; n < 2; ++n) {
                         float2 nl = *reinterpret_cast<const float2 *>(neg_lse + c + 8 * n);
                         float2 nd = *reinterpret_cast<const float2 *>(neg_delta + c + 8 * n);
-                        if constexpr (!BF16) {                // p by 2^14, ds by up
+                        if constexpr (K == F16) {                // p by 2^14, ds by up
                             nl.x += 14.f;
                             nl.y += 14.f;
                             nd.x *= up_p;
@@ -729,27 +831,24 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
 #pragma unroll
                         for (int i = 4 * n; i < 4 * n + 4; ++i) {
                             p[i] = exp2_fast(fmaf(p[i], mul, i & 1 ? nl.y : nl.x));
-                            dp[i] = p[i] * (BF16 ? dp[i] + (i & 1 ? nd.y : nd.x) : fmaf(dp[i], up_p, i & 1 ? nd.y : nd.x));
+                            dp[i] = p[i] * (K != F16 ? dp[i] + (i & 1 ? nd.y : nd.x) : fmaf(dp[i], up_p, i & 1 ? nd.y : nd.x));
                         }
                     }
-                    uint32_t w[4];
-                    as_a<BF16>(w, p);
-                    block_mul<BF16, DP>(dv, w, ob + la, q_half);
-                    as_a<BF16>(w, dp);
-                    block_mul<BF16, DP>(dk, w, qb + la, q_half);
+                    block_mul<K, DP>(dv, p, ob + la, q_half);
+                    block_mul<K, DP>(dk, dp, qb + la, q_half);
                 }
             }
         }
         __syncthreads();                                      // nobody reads this set of tiles any more
         if (active && tile < qt)
-            store_tile<DP>(dq, Q + tile * Row<DP>::BLOCK, q_half, plan, &maps.out, a.dq, l.b, h, r0, s.nq, a.q_len, a.dim);
+            store_tile<K, DP>(dq, Q + tile * Row<K, DP>::BLOCK, q_half, plan, &maps.out, a.dq, l.b, h, r0, s.nq, a.q_len, a.dim);
         if (active && tile < kt && x == group - 1) {
-            const float f = a.scale / up_k, g = BF16 ? 1.f : 1.f / 16384.f;
-            uint32_t w[DP / 8][2];
-            pack_tile<BF16, DP>(w, dk, f, f);
-            store_tile<DP>(w, K + tile * Row<DP>::BLOCK, k_half, plan, &maps.dk, a.dk, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
-            pack_tile<BF16, DP>(w, dv, g, g);
-            store_tile<DP>(w, V + tile * Row<DP>::BLOCK, k_half, plan, &maps.dv, a.dv, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
+            const float f = a.scale / up_k, g = K != F16 ? 1.f : 1.f / 16384.f;
+            uint32_t w[DP / 8][Row<K, DP>::WORDS];
+            pack_tile<K, DP>(w, dk, f, f);
+            store_tile<K, DP>(w, Kt + tile * Row<K, DP>::BLOCK, k_half, plan, &maps.dk, a.dk, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
+            pack_tile<K, DP>(w, dv, g, g);
+            store_tile<K, DP>(w, V + tile * Row<K, DP>::BLOCK, k_half, plan, &maps.dv, a.dv, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
         }
         if (plan.tma) {
             if (lane == 0) tma_stores_read();
@@ -765,20 +864,21 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
     if (stalled) drain_stalled(stalls);
 }
 
-// 16-byte accesses need every row of every tensor aligned to eight values
-static bool rows_of_eight(const AttnArgs &a, bool backward)
+// 16-byte accesses need every row of every tensor aligned to them
+static bool rows_of_16_bytes(const AttnArgs &a, bool backward)
 {
-    auto ok = [](const AttnTensor &t) { return (uintptr_t)t.p % 16 == 0 && (t.sb | t.sl | t.sh) % 8 == 0; };
-    bool v = a.dim % 8 == 0 && ok(a.q) && ok(a.k) && ok(a.v);
+    const int n = a.dtype == GS_TABLE_F32 ? 4 : 8;
+    auto ok = [&](const AttnTensor &t) { return (uintptr_t)t.p % 16 == 0 && (t.sb | t.sl | t.sh) % n == 0; };
+    bool v = a.dim % n == 0 && ok(a.q) && ok(a.k) && ok(a.v);
     if (backward) return v && ok(a.dout) && ok(a.dq) && ok(a.dk) && ok(a.dv);
     return v && ok(a.out);
 }
 
 static bool all_tma(const AttnArgs &a, bool backward)
 {
-    auto on_q = [&](const AttnTensor &t) { return attn_tma_ok(t, a.batch, a.q_len, a.q_heads); };
-    auto on_k = [&](const AttnTensor &t) { return attn_tma_ok(t, a.batch, a.k_len, a.kv_heads); };
-    const bool v = a.dim % 8 == 0 && on_q(a.q) && on_k(a.k) && on_k(a.v);
+    auto on_q = [&](const AttnTensor &t) { return attn_tma_ok(t, a.dtype, a.batch, a.q_len, a.q_heads); };
+    auto on_k = [&](const AttnTensor &t) { return attn_tma_ok(t, a.dtype, a.batch, a.k_len, a.kv_heads); };
+    const bool v = a.dim % (a.dtype == GS_TABLE_F32 ? 4 : 8) == 0 && on_q(a.q) && on_k(a.k) && on_k(a.v);
     if (backward) return v && on_q(a.dout) && on_q(a.dq) && on_k(a.dk) && on_k(a.dv);
     return v && on_q(a.out);
 }
@@ -801,7 +901,7 @@ static WalkMask mask_of(int left, int right)
     return m;
 }
 
-template <bool BF16, int DP, bool BWD>
+template <int K, int DP, bool BWD>
 static gs_status launch(const AttnArgs &a, cudaStream_t st)
 {
     WalkPlan plan;
@@ -810,7 +910,7 @@ static gs_status launch(const AttnArgs &a, cudaStream_t st)
     plan.qt = (a.q_len + 15) / 16;
     plan.kt = (a.k_len + 15) / 16;
     plan.tma = all_tma(a, BWD);
-    plan.vec = rows_of_eight(a, BWD);
+    plan.vec = rows_of_16_bytes(a, BWD);
     const int tiles = BWD && plan.kt > plan.qt ? plan.kt : plan.qt;
     const int64_t total = a.batch * (BWD ? a.kv_heads : a.q_heads);
     if (total == 0) return GS_OK;
@@ -820,12 +920,12 @@ static gs_status launch(const AttnArgs &a, cudaStream_t st)
     }
     WalkMaps m;
     if (plan.tma) {
-        constexpr int BOX = DP < 64 ? DP : 64;
+        constexpr int BOX = Row<K, DP>::VALUES;
         auto on_q = [&](CUtensorMap *t, const AttnTensor &x, int rows) {
-            return attn_tensor_map(t, x, BF16, a.batch, a.q_len, a.q_heads, a.dim, BOX, rows);
+            return attn_tensor_map(t, x, a.dtype, a.batch, a.q_len, a.q_heads, a.dim, BOX, rows);
         };
         auto on_k = [&](CUtensorMap *t, const AttnTensor &x, int rows) {
-            return attn_tensor_map(t, x, BF16, a.batch, a.k_len, a.kv_heads, a.dim, BOX, rows);
+            return attn_tensor_map(t, x, a.dtype, a.batch, a.k_len, a.kv_heads, a.dim, BOX, rows);
         };
         gs_status s = GS_OK;
         if ((s = on_q(&m.q, a.q, plan.qt * 16)) != GS_OK || (s = on_k(&m.k, a.k, plan.kt * 16)) != GS_OK ||
@@ -835,26 +935,26 @@ static gs_status launch(const AttnArgs &a, cudaStream_t st)
                     (s = on_k(&m.dv, a.dv, 16)) != GS_OK))
             return s;
     }
-    const int unit = (BWD ? 2 : 1) * (int)Row<DP>::tile(plan.qt) + 2 * (int)Row<DP>::tile(plan.kt);
+    const int unit = (BWD ? 2 : 1) * (int)Row<K, DP>::tile(plan.qt) + 2 * (int)Row<K, DP>::tile(plan.kt);
     const int stats = BWD ? (int)stat_bytes(plan.qt) : 0;
     const int masks = (int)(mask_bytes(plan.rows.n) + (BWD ? mask_bytes(plan.cols.n) : 0));
     // two sets of tiles if one unit leaves room for the resident blocks, and as many units as the block's warps
     // and that room allow
-    const int room = (227 * 1024) / blocks_per_sm<DP, BWD>() - 2048;
+    const int room = (227 * 1024) / blocks_per_sm<K, DP, BWD>() - 2048;
     plan.stages = plan.tma && 2 * unit + stats + masks <= room ? 2 : 1;
     const int per_unit = plan.stages * unit + stats;
     plan.units = BLOCK_WARPS / tiles;
     while (plan.units > 1 && plan.units * per_unit + masks > room) --plan.units;
     if (plan.units < 1) plan.units = 1;
     const int smem = plan.units * per_unit + masks;
-    auto kernel = !BWD ? attn_walk_forward_kernel<BF16, DP>
-                       : a.group > 1 ? attn_walk_backward_kernel<BF16, DP, true> : attn_walk_backward_kernel<BF16, DP, false>;
+    auto kernel = !BWD ? attn_walk_forward_kernel<K, DP>
+                       : a.group > 1 ? attn_walk_backward_kernel<K, DP, true> : attn_walk_backward_kernel<K, DP, false>;
     static SharedRecord record[2];
     gs_status s = allow_shared(kernel, smem, record[BWD && a.group > 1]);
     if (s != GS_OK) return s;
     const int threads = plan.units * tiles * 32;
     // blocks that an SM holds, by shared memory (1 KB and the static variables on top) and by registers
-    const int by_shared = 228 * 1024 / (smem + 2048), by_registers = 65536 / (registers<DP, BWD>() * threads);
+    const int by_shared = 228 * 1024 / (smem + 2048), by_registers = 65536 / (registers<K, DP, BWD>() * threads);
     const int resident = by_shared < by_registers ? by_shared : by_registers;
     const int64_t blocks = (total + plan.units - 1) / plan.units, most = (int64_t)sm_count() * (resident > 0 ? resident : 1);
     kernel<<<(unsigned)(blocks < most ? blocks : most), threads, smem, st>>>(a, plan, m, stall_counter());
@@ -862,26 +962,35 @@ static gs_status launch(const AttnArgs &a, cudaStream_t st)
     return GS_OK;
 }
 
-template <bool BF16, bool BWD>
+template <int K, bool BWD>
 static gs_status by_dim(const AttnArgs &a, cudaStream_t st)
 {
-    if (a.dim <= 16) return launch<BF16, 16, BWD>(a, st);
-    if (a.dim <= 32) return launch<BF16, 32, BWD>(a, st);
-    if (a.dim <= 64) return launch<BF16, 64, BWD>(a, st);
-    return launch<BF16, 128, BWD>(a, st);
+    if (K != F32 && a.dim <= 16) return launch<K, K == F32 ? 32 : 16, BWD>(a, st);
+    if (a.dim <= 32) return launch<K, 32, BWD>(a, st);
+    if (a.dim <= 64) return launch<K, 64, BWD>(a, st);
+    return launch<K, 128, BWD>(a, st);
 }
 
-bool attn_walk_ok(const AttnArgs &a)
+// bytes of one head's tiles, which have to fit one block (fp32 with 128 columns does up to 96 positions backward)
+static int64_t head_bytes(const AttnArgs &a, bool backward)
 {
-    return a.dtype != GS_TABLE_F32 && a.q_len > 0 && a.k_len > 0 && a.q_len <= 128 && a.k_len <= 128;
+    const int64_t row = (a.dtype == GS_TABLE_F32 ? 4 : 2) * (a.dim <= 32 ? 32 : a.dim <= 64 ? 64 : 128);
+    return row * ((backward ? 2 : 1) * ((a.q_len + 15) / 16 * 16) + 2 * ((a.k_len + 15) / 16 * 16));
+}
+
+bool attn_walk_ok(const AttnArgs &a, bool backward)
+{
+    return a.q_len > 0 && a.k_len > 0 && a.q_len <= 128 && a.k_len <= 128 && head_bytes(a, backward) <= 208 * 1024;
 }
 gs_status attn_walk_forward(const AttnArgs &a, cudaStream_t st)
 {
-    return a.dtype == GS_TABLE_BF16 ? by_dim<true, false>(a, st) : by_dim<false, false>(a, st);
+    if (a.dtype == GS_TABLE_F32) return by_dim<F32, false>(a, st);
+    return a.dtype == GS_TABLE_BF16 ? by_dim<BF16, false>(a, st) : by_dim<F16, false>(a, st);
 }
 gs_status attn_walk_backward(const AttnArgs &a, cudaStream_t st)
 {
-    return a.dtype == GS_TABLE_BF16 ? by_dim<true, true>(a, st) : by_dim<false, true>(a, st);
+    if (a.dtype == GS_TABLE_F32) return by_dim<F32, true>(a, st);
+    return a.dtype == GS_TABLE_BF16 ? by_dim<BF16, true>(a, st) : by_dim<F16, true>(a, st);
 }
 
 }  // namespace gs
