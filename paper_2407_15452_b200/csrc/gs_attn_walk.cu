@@ -519,17 +519,19 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     const bool active = u < total;
     const Unit l = unit_of(a, active ? u : u0, a.q_heads);
     const uint32_t Q = tiles_at(st), Kt = Q + q_bytes, V = Kt + k_bytes;
-    bool ok = true;
+    // Once a wait has run out all others return at once: the loop then goes on to its end without data, so that
+    // nobody is left alone at a barrier.
     if (plan.tma) {
-        ok = bar_wait(bars + 8 * st, (n >> (plan.stages - 1)) & 1, &stalled);
+        bar_wait(bars + 8 * st, (n >> (plan.stages - 1)) & 1, &stalled);
+        __syncwarp();
     } else if (active) {
         const int g = l.h / a.group;
         copy_head<K, DP>(Q, a.q, l.b, l.h, l.s.nq, qt * 16, a.dim, plan.vec, tid, threads);
         copy_head<K, DP>(Kt, a.k, l.b, g, l.s.nk, kt * 16, a.dim, plan.vec, tid, threads);
         copy_head<K, DP>(V, a.v, l.b, g, l.s.nk, kt * 16, a.dim, plan.vec, tid, threads);
     }
-    if (ragged && ok && l.s.nk < a.k_len) zero_rows<K, DP>(V, l.s.nk, kt * 16, tid, threads);
-    if (!__syncthreads_and(ok)) break;
+    if (ragged && l.s.nk < a.k_len) zero_rows<K, DP>(V, l.s.nk, kt * 16, tid, threads);
+    if (ragged || !plan.tma) __syncthreads();           // rows that other threads have written
     if (active) {
     const int r0 = tile * 16, ra = r0 + (lane >> 2), rb = ra + 8;
     float acc[DP / 8][4] = {};
@@ -672,9 +674,8 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
         }
     }
     const float mul = a.scale * LOG2E;
-    bool ok = true;
     uint32_t n = 0;
-    for (uint32_t u0 = blockIdx.x * plan.units; u0 < total && ok; u0 += step, u += step) {
+    for (uint32_t u0 = blockIdx.x * plan.units; u0 < total; u0 += step, u += step) {
     const bool active = u < total;
     const Unit l = unit_of(a, active ? u : u0, a.kv_heads);
     const AttnSeq s = l.s;
@@ -689,33 +690,35 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
             const float v = r < s.nq ? -lse[r] * LOG2E : -INFINITY;
             neg_lse[r] = v == INFINITY ? -INFINITY : v;       // p = 0 in rows that see nothing
         }
-        if (plan.tma) {
-            ok = bar_wait(bars + 8 * st, (n >> (plan.stages - 1)) & 1, &stalled);
+        // the dq rows of this thread
+        const int r0 = tile * 16, ra = r0 + (lane >> 2), rb = ra + 8;
+        float l_a = ra < s.nq ? -lse[ra] * LOG2E : -INFINITY, l_b = rb < s.nq ? -lse[rb] * LOG2E : -INFINITY;
+        l_a = l_a == INFINITY ? -INFINITY : l_a;
+        l_b = l_b == INFINITY ? -INFINITY : l_b;
+        if (plan.tma) {                                       // as in the forward kernel, a wait that runs out ends no loop
+            bar_wait(bars + 8 * st, (n >> (plan.stages - 1)) & 1, &stalled);
+            __syncwarp();
         } else if (active) {
             copy_head<K, DP>(Q, a.q, l.b, h, s.nq, qt * 16, a.dim, plan.vec, tid, threads);
             copy_head<K, DP>(DO, a.dout, l.b, h, s.nq, qt * 16, a.dim, plan.vec, tid, threads);
             copy_head<K, DP>(Kt, a.k, l.b, l.h, s.nk, kt * 16, a.dim, plan.vec, tid, threads);
             copy_head<K, DP>(V, a.v, l.b, l.h, s.nk, kt * 16, a.dim, plan.vec, tid, threads);
         }
-        if (ragged && ok && s.nq < a.q_len) {
+        if (ragged && s.nq < a.q_len) {
             zero_rows<K, DP>(Q, s.nq, qt * 16, tid, threads);
             zero_rows<K, DP>(DO, s.nq, qt * 16, tid, threads);
         }
-        if (ragged && ok && s.nk < a.k_len) {
+        if (ragged && s.nk < a.k_len) {
             zero_rows<K, DP>(Kt, s.nk, kt * 16, tid, threads);
             zero_rows<K, DP>(V, s.nk, kt * 16, tid, threads);
         }
-        ok = __syncthreads_and(ok);
-        if (!ok) break;
+        if (ragged || !plan.tma) __syncthreads();             // rows that other threads have written
 
         // ---- dq of 16 query rows
         uint32_t dq[DP / 8][Row<K, DP>::WORDS] = {};
-        const int r0 = tile * 16;
         if (active && tile < qt) {
-            const int ra = r0 + (lane >> 2), rb = ra + 8;
             const int r_end = min(r0 + 16, s.nq);
             const int j_begin = attn_lo(a, s, r0) / 16, j_end = r_end > r0 ? (attn_hi(a, s, r_end - 1) + 15) / 16 : 0;
-            const float l_a = neg_lse[ra], l_b = neg_lse[rb];
             const Rows<K, DP> qf(Q + tile * Row<K, DP>::BLOCK + lane_rows<K, DP>(), q_half), df(DO + tile * Row<K, DP>::BLOCK + lane_rows<K, DP>(), q_half);
             const uint32_t lb = lane_dot<K, DP>(), kb = Kt + lane_mul<K, DP>();
             float d_a = 0.f, d_b = 0.f, m_a = 0.f, m_b = 0.f;
