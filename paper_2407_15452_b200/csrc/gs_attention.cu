@@ -89,6 +89,23 @@ static bool f32_whole(const AttnArgs &a, bool backward)
     return n > 32 && a.dim <= 32 && a.left >= 0 && a.right >= 0 && a.left + a.right <= 32;
 }
 
+// Whether the fp32 tensors that are left go to 64-row tiles on the tensor cores or to the CUDA cores.  Measured,
+// tensor | CUDA cores, us (causal unless said):
+//  forward : 8 x 4 heads of 333 x 64 33 | 33, 16 x 8 heads of 333 x 64 69 | 98, 16 heads of 2048 x 64 230 | 294, 16 of
+//            2048 x 128 413 | 532, 16 of 4096 x 64, all visible, 1381 | 2111, 64 x 4 heads of 200 x 32, window 10, 24 | 57
+//  backward: 16 x 8 heads of 333 x 64 229 | 326, 16 heads of 2048 x 64 799 | 964, 16 of 4096 x 64 5048 | 7263, 200 x 32
+//            82 | 170; but 8 x 4 heads of 333 x 64 114 | 83, where the blocks do not fill the device one and a half
+//            times and the CUDA cores' 32-row tiles are twice as many, and 16 heads of 2048 x 128 4031 | 2415 (the
+//            accumulators of 128 columns do not fit a thread's registers).
+static bool f32_tiles(const AttnArgs &a, bool backward)
+{
+    if (a.dtype != GS_TABLE_F32 || a.q_len <= 0 || a.k_len <= 0) return false;
+    const int n = a.q_len > a.k_len ? a.q_len : a.k_len;
+    if (n <= 64 || !backward) return n > 64;
+    const int64_t blocks = (n + 63) / 64 * a.batch * (a.q_heads + a.kv_heads);
+    return a.dim <= 64 && blocks >= 3 * (int64_t)sm_count();
+}
+
 }  // namespace gs
 
 using namespace gs;
@@ -118,6 +135,7 @@ gs_status gs_attention_forward(const gs_attention_config *cfg, const void *d_q, 
     const bool whole = a.dtype == GS_TABLE_F32 ? f32_whole(a, false) : !(tiles && a.q_len > 64 && a.dim > 64);
     if (whole && attn_walk_ok(a, false)) return attn_walk_forward(a, (cudaStream_t)stream);
     if (tiles) return attn_tc_forward(a, (cudaStream_t)stream);
+    if (f32_tiles(a, false)) return attn_f32_forward(a, (cudaStream_t)stream);
     return attn_simt_forward(a, (cudaStream_t)stream);
 }
 
@@ -156,6 +174,7 @@ gs_status gs_attention_backward(const gs_attention_config *cfg, const void *d_do
     const bool whole = a.dtype == GS_TABLE_F32 ? f32_whole(a, true) : !(tiles && wide);
     if (whole && attn_walk_ok(a, true)) return attn_walk_backward(a, (cudaStream_t)stream);
     if (tiles) return attn_tc_backward(a, (cudaStream_t)stream);
+    if (f32_tiles(a, true)) return attn_f32_backward(a, (cudaStream_t)stream);
     return attn_simt_backward(a, (cudaStream_t)stream);
 }
 

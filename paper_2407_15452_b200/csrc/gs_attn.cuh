@@ -88,6 +88,9 @@ static inline gs_status allow_shared(K kernel, int bytes, SharedRecord &done)
 gs_status attn_simt_forward(const AttnArgs &a, cudaStream_t st);
 gs_status attn_simt_backward(const AttnArgs &a, cudaStream_t st);
 
+// gs_attn_f32.cu
+gs_status attn_f32_forward(const AttnArgs &a, cudaStream_t st);
+gs_status attn_f32_backward(const AttnArgs &a, cudaStream_t st);
 // gs_attn_walk.cu
 bool attn_walk_ok(const AttnArgs &a, bool backward);
 gs_status attn_walk_forward(const AttnArgs &a, cudaStream_t st);

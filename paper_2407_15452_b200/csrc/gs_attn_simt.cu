@@ -1,5 +1,5 @@
-// Attention on the CUDA cores, everything in fp32 (products included): fp32 tensors that are not short walks, and
-// long 16-bit tensors that TMA cannot address.
+// Attention on the CUDA cores, everything in fp32 (products included): fp32 tensors that the tensor cores do not take
+// (short ones, and backward few or wide heads), and long 16-bit tensors that TMA cannot address.
 //
 // A block of 4 * BT threads works on BT x BT tiles of scores; thread (ty, tx) holds 4 rows x BT/16
 // columns of a tile and 4 rows x DP/16 columns of an accumulator, DP = head_dim padded to 32, 64 or

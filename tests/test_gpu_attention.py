@@ -414,3 +414,41 @@ def test_refusals_of_the_library_without_a_gpu():
         args = list(bwd)
         args[missing] = None
         assert lib.gs_attention_backward(ctypes.byref(cfg()), *args, None) == -1
+
+
+# fp32 in tiles on the tensor cores: enough heads to fill the device, head_dims of both widths, a last tile of one
+# row, shared heads, empty sequences with NaN in the padding, windows that leave warps and tiles out
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [7, 32, 40, 64])
+@pytest.mark.parametrize("n,hq,hk,window,ragged", [
+    (193, 4, 4, ALL, False),
+    (193, 6, 2, CAUSAL, True),
+    (257, 4, 1, (40, 3), True),
+    (150, 4, 4, (0, 0), False),
+], ids=["all", "causal_ragged", "window_ragged", "diagonal"])
+def test_many_heads_of_fp32_tiles(n, hq, hk, window, ragged, d):
+    b = 32
+    q, k, v, dout = tensors(b, n, n, hq, hk, d, F32, seed=n + d)
+    m = None
+    if ragged:
+        values = torch.randint(0, n + 1, (b,), generator=torch.Generator().manual_seed(d))
+        values[:4] = torch.tensor([0, 1, n, 65])
+        m = values.to(torch.int32).to(DEV)
+        for s, length in enumerate(values.tolist()):
+            for t in (q, k, v, dout):
+                t[s, length:] = math.nan
+    run_both(q, k, v, dout, window, m, m)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["fused", "heads_first", "odd_offset", "odd_rows", "broadcast", "reversed_batch"])
+def test_layouts_of_fp32_tiles(kind):
+    q, k, v, dout = _layouts(40, 150, 2, 64, F32, kind)
+    run_both(q, k, v, dout, CAUSAL)
+
+
+@pytest.mark.gpu
+def test_fp32_tiles_of_unequal_lengths():
+    q, k, v, dout = tensors(40, 70, 140, 2, 2, 64, F32, seed=3)
+    run_both(q, k, v, dout, CAUSAL)
+    run_both(q, k, v, dout, CAUSAL, lengths([0, 70, 70, 30, 1000] * 8), lengths([140, 0, 20, -5, 140] * 8))
