@@ -12,6 +12,7 @@
 #include <cuda_fp16.h>
 
 #include <atomic>
+#include <mutex>
 
 #include "gs_common.cuh"
 
@@ -68,9 +69,11 @@ __device__ __forceinline__ int attn_q_last(const AttnArgs &a, const AttnSeq &s, 
 }
 
 // Lets `kernel` use up to `bytes` of dynamic shared memory on the current device; `done` is the kernel's own record of
-// what each device allows already (the attribute costs about a microsecond to set).
+// what each device allows already (the attribute costs about a microsecond to set).  Setting and recording are one step
+// under a lock: of two threads that ask for different sizes, the smaller one must not undo the larger.
 struct SharedRecord {
     std::atomic<int> bytes[64];
+    std::mutex lock;
 };
 template <typename K>
 static inline gs_status allow_shared(K kernel, int bytes, SharedRecord &done)
@@ -78,9 +81,11 @@ static inline gs_status allow_shared(K kernel, int bytes, SharedRecord &done)
     int dev = 0;
     GS_CUDA_TRY(cudaGetDevice(&dev));
     const bool known = dev >= 0 && dev < 64;
+    if (known && done.bytes[dev].load(std::memory_order_acquire) >= bytes) return GS_OK;
+    std::lock_guard<std::mutex> hold(done.lock);
     if (known && done.bytes[dev].load(std::memory_order_relaxed) >= bytes) return GS_OK;
     GS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-    if (known) done.bytes[dev].store(bytes, std::memory_order_relaxed);
+    if (known) done.bytes[dev].store(bytes, std::memory_order_release);
     return GS_OK;
 }
 
