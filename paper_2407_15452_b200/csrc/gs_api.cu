@@ -6,6 +6,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <atomic>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -167,20 +168,30 @@ unsigned long long *refused_counter()
 
 unsigned long long *stall_counter()
 {
-    void *ws = nullptr;
-    if (workspace_get(WS_COUNTERS, 256, &ws) != GS_OK) return nullptr;
-    return (unsigned long long *)((char *)ws + 168);
-}
-
-static gs_status read_counter(unsigned long long *ctr, uint64_t *h_count, int32_t clear, cudaStream_t st)
-{
-    if (!ctr) return GS_ERR_OOM;
-    unsigned long long v = 0;
-    GS_CUDA_TRY(cudaMemcpyAsync(&v, ctr, sizeof(v), cudaMemcpyDeviceToHost, st));
-    if (clear) GS_CUDA_TRY(cudaMemsetAsync(ctr, 0, sizeof(v), st));
-    GS_CUDA_TRY(cudaStreamSynchronize(st));
-    *h_count = (uint64_t)v;
-    return GS_OK;
+    static std::atomic<unsigned long long *> words{nullptr};      // eight per device, a cache line
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+    unsigned long long *w = words.load(std::memory_order_acquire);
+    if (!w) {
+        std::lock_guard<std::mutex> lk(g_mu);
+        w = words.load(std::memory_order_relaxed);
+        if (!w) {
+            // the first call may be one that a stream capture records, where allocating is refused unless asked for
+            cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+            void *p = nullptr;
+            cudaThreadExchangeStreamCaptureMode(&mode);
+            const cudaError_t e = cudaHostAlloc(&p, 64 * 64, cudaHostAllocPortable | cudaHostAllocMapped);
+            cudaThreadExchangeStreamCaptureMode(&mode);
+            if (e != cudaSuccess) {
+                cudaGetLastError();
+                return nullptr;
+            }
+            memset(p, 0, 64 * 64);
+            w = (unsigned long long *)p;
+            words.store(w, std::memory_order_release);
+        }
+    }
+    return w + 8 * dev;
 }
 
 static bool dim_ok(int32_t dim) { return dim == 32 || dim == 64 || dim == 128 || dim == 256; }
@@ -196,13 +207,26 @@ const char *gs_last_error(void) { return g_err; }
 gs_status gs_refused_ids(uint64_t *h_count, int32_t clear, void *stream)
 {
     if (!h_count) return invalid("h_count is NULL");
-    return read_counter(refused_counter(), h_count, clear, (cudaStream_t)stream);
+    unsigned long long *ctr = refused_counter();
+    if (!ctr) return GS_ERR_OOM;
+    cudaStream_t st = (cudaStream_t)stream;
+    unsigned long long v = 0;
+    GS_CUDA_TRY(cudaMemcpyAsync(&v, ctr, sizeof(v), cudaMemcpyDeviceToHost, st));
+    if (clear) GS_CUDA_TRY(cudaMemsetAsync(ctr, 0, sizeof(v), st));
+    GS_CUDA_TRY(cudaStreamSynchronize(st));
+    *h_count = (uint64_t)v;
+    return GS_OK;
 }
 
 gs_status gs_stalled_kernels(uint64_t *h_count, int32_t clear, void *stream)
 {
     if (!h_count) return invalid("h_count is NULL");
-    return read_counter(stall_counter(), h_count, clear, (cudaStream_t)stream);
+    volatile unsigned long long *ctr = stall_counter();
+    if (!ctr) { set_error("no page-locked host memory for the count"); return GS_ERR_OOM; }
+    GS_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
+    *h_count = (uint64_t)*ctr;
+    if (clear) *ctr = 0;
+    return GS_OK;
 }
 
 gs_status gs_release_workspace(void)

@@ -140,7 +140,7 @@ __device__ __forceinline__ void drain_stalled(unsigned long long *stalls)
 {
     if (threadIdx.x == 0) {
         for (int i = 0; i < 64; ++i) __nanosleep(100000);
-        if (stalls) atomicAdd(stalls, 1ull);
+        if (stalls) atomicAdd_system(stalls, 1ull);
     }
     __syncthreads();
 }

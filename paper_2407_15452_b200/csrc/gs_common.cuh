@@ -51,7 +51,9 @@ int sm_count();
 // walk entries, alias cells outside [0, n_nodes)); nullptr if it cannot be had.  Lives in the
 // WS_COUNTERS block (bytes 0..127: epoch counters, 128: walk ticket, 160: this counter).
 unsigned long long *refused_counter();
-// The same for kernels whose bounded wait ran out (byte 168 of the block).
+// Where kernels of the current device count blocks whose bounded wait ran out: a word of page-locked host memory, which
+// a call can have during a stream capture.  Never freed: captured graphs keep the address.  nullptr
+// if it cannot be had.
 unsigned long long *stall_counter();
 
 // ---- graph handle --------------------------------------------------------------

@@ -3,7 +3,7 @@
 //
 // Waits are bounded.  A kernel whose wait runs out (which no input should cause) sets a flag in
 // shared memory that ends every other wait of its block, drains what it has in flight, frees its
-// tensor memory and adds one to a device counter that gs_stalled_kernels reads.
+// tensor memory and adds one to the count that gs_stalled_kernels reads.
 #pragma once
 
 #include <cuda.h>
