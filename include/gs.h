@@ -536,10 +536,15 @@ GS_API gs_status gs_refused_ids(uint64_t *h_count, int32_t clear, void *stream);
 /*
  * Sticky per-device count of thread blocks of the tensor-core attention kernels that gave up a wait inside
  * the kernel (about two seconds without progress; the results of that call are then not valid).
- * No input causes it; it is there so that a fault of the hardware or of the library ends as a number and not
- * as a hang.  Reads the counter after the work queued on `stream`, clears it if clear != 0, and WAITS.
+ * No input causes it; it is there so that a fault of the hardware or of the library ends as an error and not
+ * as a hang.  While the count is not zero, gs_attention_forward and gs_attention_backward on that device
+ * return GS_ERR_CUDA: the call after the one that failed reports it, as the runtime does with errors of kernels.
+ * Reads the count of the current device after the work queued on `stream`, clears it if clear != 0, and WAITS.
+ * gs_stall_drill queues one block whose wait nothing ends (it gives up after about a millisecond), so that an application
+ * can see what it does with the error; the count goes up by one, no data is touched.  Errors: GS_ERR_OOM, GS_ERR_CUDA.
  */
 GS_API gs_status gs_stalled_kernels(uint64_t *h_count, int32_t clear, void *stream);
+GS_API gs_status gs_stall_drill(void *stream);
 
 /* Frees the cached scratch memory of the current device (waits for the device). */
 GS_API gs_status gs_release_workspace(void);

@@ -38,7 +38,7 @@ EXPORTS = [
     "gs_subsample_walks", "gs_shuffled_starts", "gs_refused_ids",
     "gs_init_embeddings_bf16", "gs_sgns_step_bf16",
     "gs_attention_forward", "gs_attention_backward", "gs_attention_backward_work",
-    "gs_stalled_kernels", "gs_gradient_norm_work", "gs_gradient_norm", "gs_clip_gradients",
+    "gs_stalled_kernels", "gs_stall_drill", "gs_gradient_norm_work", "gs_gradient_norm", "gs_clip_gradients",
 ]
 
 
@@ -445,10 +445,16 @@ def gs_refused_ids(clear: bool = False) -> int:
 
 
 def gs_stalled_kernels(clear: bool = False) -> int:
-    """Blocks of the tensor-core attention kernels that gave up a wait (waits for the current stream)."""
+    """Blocks of the tensor-core attention kernels that gave up a wait (waits for the current stream).  While it is not
+    zero, attention calls raise."""
     out = ctypes.c_uint64(0)
     _check(lib().gs_stalled_kernels(ctypes.byref(out), ctypes.c_int32(1 if clear else 0), _stream()))
     return out.value
+
+
+def gs_stall_drill():
+    """Queues a block whose wait runs out after about a millisecond, to see what a caller does with the error."""
+    _check(lib().gs_stall_drill(_stream()))
 
 
 def gs_release_workspace():

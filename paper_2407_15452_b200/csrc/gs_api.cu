@@ -194,6 +194,15 @@ unsigned long long *stall_counter()
     return w + 8 * dev;
 }
 
+gs_status stalled_before()
+{
+    const volatile unsigned long long *w = stall_counter();
+    if (!w || *w == 0) return GS_OK;
+    set_error("%llu blocks of earlier calls gave up a wait and left results that are not valid; "
+              "gs_stalled_kernels reads and clears the count", (unsigned long long)*w);
+    return GS_ERR_CUDA;
+}
+
 static bool dim_ok(int32_t dim) { return dim == 32 || dim == 64 || dim == 128 || dim == 256; }
 
 }  // namespace gs

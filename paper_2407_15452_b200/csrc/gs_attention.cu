@@ -128,6 +128,7 @@ gs_status gs_attention_forward(const gs_attention_config *cfg, const void *d_q, 
     if ((s = pointers_ok(need, a.k_len ? 4 : 2, a.dtype)) != GS_OK) return s;
     if (!d_lse) return bad("d_lse is NULL");
     if (!writable(a.out, a.batch, a.q_len, a.q_heads)) return bad("out has a zero stride");
+    if ((s = stalled_before()) != GS_OK) return s;
     // 16-bit tensors: up to 128 positions by whole heads, longer ones on 128 x 128 tiles, which need TMA.  Between 65
     // and 128 positions the wide heads go to the tiles as well: 4096 heads of 100 x 128 take 127 us there and
     // 146 us whole, 8192 heads of 100 x 64 196 and 141 us.
@@ -166,6 +167,7 @@ gs_status gs_attention_backward(const gs_attention_config *cfg, const void *d_do
     if (!writable(a.dq, a.batch, a.q_len, a.q_heads) || !writable(a.dk, a.batch, a.k_len, a.kv_heads) ||
         !writable(a.dv, a.batch, a.k_len, a.kv_heads))
         return bad("a gradient has a zero stride");
+    if ((s = stalled_before()) != GS_OK) return s;
     // As above; backward, 4096 heads of 100 x 128 321 us on tiles and 523 us whole, 8192 heads of 100 x 64 424 and
     // 490 us, but 272 us with a window of 10 on each side, which the whole heads make use of.
     const bool tiles = a.q_len > 0 && a.k_len > 0 && attn_tc_backward_ok(a);
@@ -177,6 +179,8 @@ gs_status gs_attention_backward(const gs_attention_config *cfg, const void *d_do
     if (f32_tiles(a, true)) return attn_f32_backward(a, (cudaStream_t)stream);
     return attn_simt_backward(a, (cudaStream_t)stream);
 }
+
+gs_status gs_stall_drill(void *stream) { return attn_stall_drill((cudaStream_t)stream); }
 
 int64_t gs_attention_backward_work(const gs_attention_config *cfg)
 {

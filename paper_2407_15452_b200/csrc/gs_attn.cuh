@@ -103,6 +103,7 @@ gs_status attn_walk_backward(const AttnArgs &a, cudaStream_t st);
 // gs_attn_tc.cu
 bool attn_tc_forward_ok(const AttnArgs &a);
 gs_status attn_tc_forward(const AttnArgs &a, cudaStream_t st);
+gs_status attn_stall_drill(cudaStream_t st);
 // gs_attn_tc_bwd.cu
 bool attn_tc_backward_ok(const AttnArgs &a);
 int64_t attn_tc_backward_work(int64_t batch, int32_t q_len, int32_t k_len, int32_t q_heads, int32_t kv_heads);   // floats

@@ -439,4 +439,33 @@ gs_status attn_tc_forward(const AttnArgs &a, cudaStream_t st)
     return bf16 ? forward_t<true, 128>(a, m, st) : forward_t<false, 128>(a, m, st);
 }
 
+// One block whose wait nothing ends; it gives up after about a millisecond and is counted like any other
+__global__ void attn_stall_drill_kernel(unsigned long long *stalls)
+{
+    __shared__ __align__(8) uint64_t never;
+    __shared__ volatile int stalled;
+    const uint32_t bar = smem_u32(&never);
+    if (threadIdx.x == 0) {
+        stalled = 0;
+        bar_init(bar, 1);
+        fence_barrier_init();
+    }
+    __syncthreads();
+    bar_wait(bar, 0, &stalled, 2000000);
+    __syncthreads();
+    if (stalled) drain_stalled(stalls);
+}
+
+gs_status attn_stall_drill(cudaStream_t st)
+{
+    unsigned long long *stalls = stall_counter();
+    if (!stalls) {
+        set_error("no page-locked host memory for the count");
+        return GS_ERR_OOM;
+    }
+    attn_stall_drill_kernel<<<1, 32, 0, st>>>(stalls);
+    GS_CUDA_TRY(cudaGetLastError());
+    return GS_OK;
+}
+
 }  // namespace gs

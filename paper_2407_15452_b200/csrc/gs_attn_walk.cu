@@ -519,8 +519,8 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     const bool active = u < total;
     const Unit l = unit_of(a, active ? u : u0, a.q_heads);
     const uint32_t Q = tiles_at(st), Kt = Q + q_bytes, V = Kt + k_bytes;
-    // Once a wait has run out all others return at once: the loop then goes on to its end without data, so that
-    // nobody is left alone at a barrier.
+    // Once a wait has run out all others return at once: the loop then goes on to its end without data and without
+    // new loads, so that nobody is left alone at a barrier and no barrier is armed a second time.
     if (plan.tma) {
         bar_wait(bars + 8 * st, (n >> (plan.stages - 1)) & 1, &stalled);
         __syncwarp();
@@ -603,7 +603,7 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
         if (ragged) fence_async_shared();               // zeroed rows, before TMA writes there again
     }
     __syncthreads();                                    // everybody is done with this set of tiles
-    if (plan.tma && tid == 0 && u0 + plan.stages * step < total) load(u + plan.stages * step, st);
+    if (plan.tma && tid == 0 && !stalled && u0 + plan.stages * step < total) load(u + plan.stages * step, st);
     }
     if (stalled) drain_stalled(stalls);
 }
@@ -858,7 +858,7 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
             if (ragged) fence_async_shared();                 // zeroed rows, before TMA writes there again
         }
         __syncthreads();
-        if (plan.tma && tid == 0) {                           // the step that uses these tiles next
+        if (plan.tma && tid == 0 && !stalled) {               // the step that uses these tiles next
             const int ahead = (x + plan.stages) / group, x2 = (x + plan.stages) % group;
             if (u0 + ahead * step < total) load(u + ahead * step, x2, st);
         }

@@ -51,10 +51,12 @@ int sm_count();
 // walk entries, alias cells outside [0, n_nodes)); nullptr if it cannot be had.  Lives in the
 // WS_COUNTERS block (bytes 0..127: epoch counters, 128: walk ticket, 160: this counter).
 unsigned long long *refused_counter();
-// Where kernels of the current device count blocks whose bounded wait ran out: a word of page-locked host memory, which
-// a call can have during a stream capture.  Never freed: captured graphs keep the address.  nullptr
+// Where kernels of the current device count blocks whose bounded wait ran out: a word of page-locked host memory, so
+// that the next call sees it without waiting for the device.  Never freed: captured graphs keep the address.  nullptr
 // if it cannot be had.
 unsigned long long *stall_counter();
+// GS_ERR_CUDA if that count is not zero: results of an earlier call are not valid
+gs_status stalled_before();
 
 // ---- graph handle --------------------------------------------------------------
 }  // namespace gs

@@ -3,7 +3,7 @@
 //
 // Waits are bounded.  A kernel whose wait runs out (which no input should cause) sets a flag in
 // shared memory that ends every other wait of its block, drains what it has in flight, frees its
-// tensor memory and adds one to the count that gs_stalled_kernels reads.
+// tensor memory and adds one to the count that the next call finds and gs_stalled_kernels reads.
 #pragma once
 
 #include <cuda.h>
@@ -43,7 +43,7 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 static constexpr long long WAIT_CYCLES = 4000000000ll;      // about two seconds
 
 // true once the barrier's phase has completed; false if the wait ran out here or elsewhere in the block
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *stalled)
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *stalled, long long limit = WAIT_CYCLES)
 {
     if (bar_try(bar, parity)) return true;
     const long long t0 = clock64();
@@ -52,7 +52,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
         for (int i = 0; i < 32; ++i)
             if (bar_try(bar, parity)) return true;
         if (*stalled) return false;
-        if (clock64() - t0 > WAIT_CYCLES) {
+        if (clock64() - t0 > limit) {
             *stalled = 1;
             return false;
         }

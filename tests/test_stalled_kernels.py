@@ -1,12 +1,40 @@
-"""Where the count of waits that ran out inside attention kernels lives."""
+"""What happens when a wait inside an attention kernel runs out, and where the count of such waits lives."""
 import os
 import subprocess
 import sys
 from pathlib import Path
 
 import pytest
+import torch
+
+from paper_2407_15452_b200 import binding as B
+from paper_2407_15452_b200.attention import attention
+
 pytestmark = pytest.mark.gpu
 ROOT = Path(__file__).resolve().parent.parent
+
+
+def test_a_wait_that_runs_out_is_reported_by_the_next_call():
+    q, k, v = (torch.randn((2, 30, 2, 32), device="cuda", dtype=torch.bfloat16, requires_grad=True) for _ in range(3))
+    out = attention(q, k, v)
+    want = out.detach().clone()
+    assert B.gs_stalled_kernels() == 0
+    B.gs_stall_drill()                                      # nothing ever arrives at this block's barrier
+    torch.cuda.synchronize()
+    try:
+        with pytest.raises(B.GsError, match="gave up a wait") as e:
+            attention(q, k, v)
+        assert e.value.status == -4
+        with pytest.raises(B.GsError, match="gave up a wait"):
+            out.sum().backward()
+        assert B.gs_stalled_kernels() == 1                  # reading it does not clear it
+        B.gs_release_workspace()
+        assert B.gs_stalled_kernels() == 1
+    finally:
+        assert B.gs_stalled_kernels(clear=True) == 1
+    assert B.gs_stalled_kernels() == 0
+    assert torch.equal(attention(q, k, v), want)            # the device is none the worse for it
+    attention(q, k, v).sum().backward()
 
 
 CAPTURED_FIRST = """
