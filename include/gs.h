@@ -623,7 +623,7 @@ GS_API gs_status gs_attention_backward(const gs_attention_config *cfg, const voi
  * max_norm / norm if the norm is finite and greater than max_norm, else 1 (a norm that is not finite leaves
  * the gradients as they are for the caller to drop the step).  h_out NULL: in place.  An output may be
  * its own gradient's buffer only if both have one type, and must not overlap another tensor.
- *   h_grads, h_out : HOST arrays, read during the call; empty tensors (numel 0) are allowed
+ *   h_grads, h_out : HOST arrays, read during the call; empty tensors (numel 0) are allowed; 2^42 elements in all
  *   d_work         : gs_gradient_norm_work(n_tensors) doubles of the caller's, written by the call
  * Errors: GS_ERR_INVALID_ARG (bad type, size, pointer or max_norm), GS_ERR_CUDA.
  */

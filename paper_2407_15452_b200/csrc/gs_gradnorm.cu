@@ -279,7 +279,6 @@ static int fill(GradList<CAP> *l, const gs_tensor *in, const gs_tensor *out, int
     while (*at < n && l->count < CAP) {
         const gs_tensor &t = in[*at];
         const int64_t c = (t.numel + CHUNK - 1) / CHUNK;
-        if (chunks + c > 0x7FFFFFF0) break;
         if (c > 0) {
             const int i = l->count++;
             l->t[i].in = t.d_data;
@@ -333,15 +332,24 @@ static gs_status run(const gs_tensor *in, const gs_tensor *out, int64_t n, bool 
     return GS_OK;
 }
 
+// Chunks of all tensors (2^42 elements): every index of a chunk, one grid past the last included, is an int
+static constexpr int64_t MOST_CHUNKS = 1 << 30;
+
 static gs_status check(const gs_tensor *t, int64_t n, const char *what)
 {
+    int64_t chunks = 0;
     for (int64_t i = 0; i < n; ++i) {
         const bool type_ok = t[i].dtype == GS_TABLE_F32 || t[i].dtype == GS_TABLE_F16 || t[i].dtype == GS_TABLE_BF16;
-        if (!type_ok || t[i].numel < 0 || t[i].numel > ((int64_t)1 << 43) || (t[i].numel > 0 && !t[i].d_data) ||
+        if (!type_ok || t[i].numel < 0 || t[i].numel > MOST_CHUNKS * CHUNK || (t[i].numel > 0 && !t[i].d_data) ||
             (uintptr_t)t[i].d_data % size_of(t[i].dtype) != 0) {
             set_error("invalid argument: %s %lld has a bad type, size, pointer or alignment", what, (long long)i);
             return GS_ERR_INVALID_ARG;
         }
+        chunks += (t[i].numel + CHUNK - 1) / CHUNK;
+    }
+    if (chunks > MOST_CHUNKS) {
+        set_error("invalid argument: the tensors have more than 2^42 elements");
+        return GS_ERR_INVALID_ARG;
     }
     return GS_OK;
 }
