@@ -6,9 +6,10 @@
 // The tensors travel in the kernel's parameters (no device-side list to upload or to keep).  All of
 // them are cut into chunks of 4096 elements; the blocks of a grid take chunks round robin, so
 // one large matrix and hundreds of small vectors load the SMs alike, and the order of every sum is
-// fixed by the sizes alone: results are bitwise repeatable.  Squares are summed in fp32 over the 16
-// elements that a thread takes of a chunk and in fp64 from there on.  Bound: memory traffic.  The second pass runs
-// backwards and finds the last of the first's reads in L2.
+// fixed by the gradients' sizes, types and alignment (and the number of SMs), whatever they are scaled into: results are
+// bitwise repeatable, and the norm alone is the clipping call's norm.  Squares are summed in fp32 over the 16 elements that
+// a thread takes of a chunk (18 in a tensor's ragged first or last one) and in fp64 from there on.  Bound: memory
+// traffic.  The second pass runs backwards and finds the last of the first's reads in L2.
 #include <math.h>
 
 #include <cuda_bf16.h>
@@ -35,7 +36,7 @@ struct GradList {
     GradTensor t[CAP];
     int32_t first[CAP + 1];          // first chunk of each tensor; first[count] = number of chunks
     uint8_t in_type[CAP], out_type[CAP];
-    uint8_t head[CAP];               // elements before both sides are 16-byte aligned; 255: never both
+    uint8_t head[CAP];               // elements before what a pass accesses is 16-byte aligned; 255: never all of it
     int32_t count;
 };
 
@@ -100,15 +101,6 @@ template <typename T>
 __device__ __forceinline__ double squares(const T *p, int64_t n, int head, int64_t c)
 {
     float s = 0.f;
-    if (head == 255) {                                   // rows that no shift aligns: element by element
-        const int64_t at = c * CHUNK;
-        const int m = (int)min((int64_t)CHUNK, n - at);
-        for (int e = threadIdx.x; e < m; e += NT) {
-            const float x = as_float(p[at + e]);
-            s = fmaf(x, x, s);
-        }
-        return (double)s;
-    }
     if (c == 0 && (int)threadIdx.x < head && (int64_t)threadIdx.x < n) {
         const float x = as_float(p[threadIdx.x]);
         s = fmaf(x, x, s);
@@ -190,7 +182,7 @@ __global__ void __launch_bounds__(NT) grad_norm_kernel(const double *partial, in
 template <typename I, typename O>
 __device__ __forceinline__ void scale_chunk(const I *p, O *o, int64_t n, int head, int64_t c, float factor)
 {
-    if (head == 255) {
+    if (head == 255) {                                   // two sides that no shift aligns: element by element
         const int64_t at = c * CHUNK;
         const int m = (int)min((int64_t)CHUNK, n - at);
         for (int e = threadIdx.x; e < m; e += NT) put(o + at + e, as_float(p[at + e]) * factor);
@@ -268,9 +260,10 @@ static int aligned_head(const gs_tensor &in, const gs_tensor &out)
     return 255;
 }
 
-static constexpr int SMALL = 64, LARGE = 800;       // tensors per launch: 2 KB and 28 KB of parameters
+static constexpr int SMALL = 64, LARGE = 800;       // tensors per launch: 2.0 KB and 24.8 KB of parameters
 
-// fills `l` from tensors [*at, n); advances *at.  Returns the number of chunks.
+// fills `l` from tensors [*at, n) for a pass from `in` to `out`, or over `in` alone if they are the same; advances *at.
+// Returns the number of chunks.
 template <int CAP>
 static int fill(GradList<CAP> *l, const gs_tensor *in, const gs_tensor *out, int64_t n, int64_t *at)
 {
@@ -312,7 +305,7 @@ static gs_status run(const gs_tensor *in, const gs_tensor *out, int64_t n, bool 
     int64_t at = 0;
     int partials = 0;
     do {
-        const int chunks = fill(&l, in, out, n, &at);
+        const int chunks = fill(&l, in, in, n, &at);
         const int grid = grid_for(chunks, ROUNDS_SUM);
         grad_squares_kernel<CAP><<<grid, NT, 0, st>>>(l, work + partials);
         GS_CUDA_TRY(cudaGetLastError());
