@@ -362,11 +362,16 @@ static gs_status entry(const gs_tensor *in, const gs_tensor *out, int64_t n, boo
     if (s != GS_OK) return s;
     if (out) {
         if ((s = check(out, n, "output")) != GS_OK) return s;
-        for (int64_t i = 0; i < n; ++i)
+        for (int64_t i = 0; i < n; ++i) {
             if (out[i].numel != in[i].numel) {
                 set_error("invalid argument: output %lld has another size than its gradient", (long long)i);
                 return GS_ERR_INVALID_ARG;
             }
+            if (out[i].d_data == in[i].d_data && out[i].dtype != in[i].dtype && in[i].numel > 0) {
+                set_error("invalid argument: output %lld is its gradient's buffer in another type", (long long)i);
+                return GS_ERR_INVALID_ARG;
+            }
+        }
     }
     if (!out) out = in;
     if (n <= SMALL) return run<SMALL>(in, out, n, scale, max_norm, work, norm, (cudaStream_t)stream);

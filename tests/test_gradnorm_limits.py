@@ -26,3 +26,11 @@ def test_more_elements_than_chunk_indexes_reach(lib, sizes):
     assert lib.gs_gradient_norm(t, len(sizes), P, P, None) == -1
     assert lib.gs_clip_gradients(t, None, len(sizes), 1.0, P, P, None) == -1
     assert lib.gs_clip_gradients(t, t, len(sizes), 1.0, P, P, None) == -1
+
+
+def test_a_gradient_scaled_in_place_into_another_type(lib):
+    # a chunk's results would land on elements that another block has yet to read
+    t = entries(8, 8)
+    for wrong in (entries(8, 8, dtype=B.GS_TABLE_F32), entries(8, 8, dtype=B.GS_TABLE_F16)):
+        assert lib.gs_clip_gradients(t, wrong, 2, 1.0, P, P, None) == -1
+        assert b"another type" in lib.gs_last_error()
