@@ -46,6 +46,12 @@ static gs_status fill(const gs_attention_config *c, AttnArgs *a)
         set_error("lengths up to 2^29, 2^20 heads and 2^31 sequences are supported");
         return GS_ERR_UNSUPPORTED;
     }
+    // rows of all heads, which launches and scratch are counted in, fit 64 bits with room to spare
+    const int64_t longest = c->q_len > c->k_len ? c->q_len : c->k_len;
+    if (longest > 0 && c->batch * c->q_heads > ((int64_t)1 << 56) / longest) {
+        set_error("attention of more than 2^56 rows is not supported");
+        return GS_ERR_UNSUPPORTED;
+    }
     memset(a, 0, sizeof(*a));
     a->batch = c->batch;
     a->q_len = c->q_len;
