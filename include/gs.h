@@ -535,12 +535,13 @@ GS_API gs_status gs_refused_ids(uint64_t *h_count, int32_t clear, void *stream);
 
 /*
  * Sticky per-device count of thread blocks of the tensor-core attention kernels that gave up a wait inside
- * the kernel (about two seconds without progress; the results of that call are then not valid).
- * No input causes it; it is there so that a fault of the hardware or of the library ends as an error and not
+ * the kernel (about twenty seconds without progress; the results of that call are then not valid).
+ * No finite input causes it (a row of gradients that has to be computed a second time, below, over some 10^6 positions
+ * and query heads takes that long); it is there so that a fault of the hardware or of the library ends as an error and not
  * as a hang.  While the count is not zero, gs_attention_forward and gs_attention_backward on that device
  * return GS_ERR_CUDA: the call after the one that failed reports it, as the runtime does with errors of kernels.
  * Reads the count of the current device after the work queued on `stream`, clears it if clear != 0, and WAITS.
- * gs_stall_drill queues one block whose wait nothing ends (it gives up after about a millisecond), so that an application
+ * gs_stall_drill queues one block whose wait nothing ends (it gives up within about two seconds), so that an application
  * can see what it does with the error; the count goes up by one, no data is touched.  Errors: GS_ERR_OOM, GS_ERR_CUDA.
  */
 GS_API gs_status gs_stalled_kernels(uint64_t *h_count, int32_t clear, void *stream);
@@ -571,9 +572,11 @@ GS_API gs_status gs_tune_node2vec_group(int32_t lanes);
  *   -window_left <= j - (i + n_k - n_q) <= window_right,
  * a negative bound meaning none: (-1, -1) everything, (-1, 0) causal with the last query at the last
  * key, (w, w) the window of the skip-gram pairs.  A row that sees nothing has out = 0,
- * lse = -infinity and gives no gradient.  Positions at or beyond n_q and n_k are never read (they may
- * hold anything, NaN included); their outputs and gradients are written as zeros.  Lengths
- * outside [0, q_len] and [0, k_len] are clamped to it.
+ * lse = -infinity and gives no gradient, and so does one whose every score is -infinity.  Positions at or beyond
+ * n_q and n_k are never used (they may hold anything, NaN included); their outputs and gradients are written as zeros.
+ * Lengths outside [0, q_len] and [0, k_len] are clamped to it.  Every sum is over visible positions only: an infinity or
+ * a NaN reaches the results of the rows that see it, as the formulas have it, and no others.  Rows that meet one take
+ * longer (they are computed a second time, one by one).
  *
  * Tensors are [batch][position][head][head_dim] with any strides (in elements) over the first three
  * and contiguous head_dim values; dtype GS_TABLE_F32, GS_TABLE_F16 or GS_TABLE_BF16 for all of them.

@@ -453,7 +453,7 @@ def gs_stalled_kernels(clear: bool = False) -> int:
 
 
 def gs_stall_drill():
-    """Queues a block whose wait runs out after about a millisecond, to see what a caller does with the error."""
+    """Queues a block whose wait runs out within about two seconds, to see what a caller does with the error."""
     _check(lib().gs_stall_drill(_stream()))
 
 

@@ -68,6 +68,15 @@ __device__ __forceinline__ int attn_q_last(const AttnArgs &a, const AttnSeq &s, 
     return a.left < 0 ? s.nq : min(s.nq, j1 - s.off + a.left);
 }
 
+template <typename T> __device__ __forceinline__ float to_f(T x);
+template <> __device__ __forceinline__ float to_f<float>(float x) { return x; }
+template <> __device__ __forceinline__ float to_f<__half>(__half x) { return __half2float(x); }
+template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T from_f(float x);
+template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
+template <> __device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
 // Lets `kernel` use up to `bytes` of dynamic shared memory on the current device; `done` is the kernel's own record of
 // what each device allows already (the attribute costs about a microsecond to set).  Setting and recording are one step
 // under a lock: of two threads that ask for different sizes, the smaller one must not undo the larger.

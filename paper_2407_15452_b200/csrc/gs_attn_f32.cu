@@ -14,7 +14,7 @@
 // tensor instructions.  16 heads of 4096 x 64, all visible: forward 1381 us (50 TFLOP/s), backward 5048 us.
 // The tensor cores round towards zero as they add, so sums over positions start from zero in every tile and the tiles'
 // sums are added by the CUDA cores, rounded to nearest.
-#include "gs_attn.cuh"
+#include "gs_attn_again.cuh"
 #include "gs_tc.cuh"
 
 namespace gs {
@@ -185,6 +185,16 @@ __device__ __forceinline__ void store_row(float *row, const float (&acc)[DP / 8]
     }
 }
 
+// whether this thread's part of a result holds a NaN: a sum of it does
+template <int N>
+__device__ __forceinline__ bool has_nan(const float (&acc)[N][4])
+{
+    float t = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) t += (acc[n][0] + acc[n][1]) + (acc[n][2] + acc[n][3]);
+    return t != t;
+}
+
 __device__ __forceinline__ float quad_max(float v)
 {
     v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
@@ -296,6 +306,7 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 3 : 2) attn_f32_forward_ke
         store_row<DP>(row_of(a.out, b, i, h), acc, r, total == 0.f ? 0.f : 1.f / total, a.dim, vec);
         if (t == 0) a.lse[bh * a.q_len + i] = total == 0.f ? -INFINITY : fmaf(top[r], LN2, logf(total));
     }
+    if (__any_sync(0xffffffffu, has_nan(acc))) again::outputs<float>(a, b, h, w0, w0 + 16);
 }
 
 // delta_i = dO_i . out_i; 16 lanes a row, heads of a position one after the other
@@ -397,6 +408,7 @@ __device__ __forceinline__ void dq_block(const AttnArgs &a, float *smem, int til
         const int i = w0 + g8 + 8 * r;
         if (i < a.q_len) store_row<DP>(row_of(a.dq, b, i, h), acc, r, a.scale, a.dim, vec);
     }
+    if (__any_sync(0xffffffffu, has_nan(acc))) again::query_gradients<float>(a, b, h, w0, w0 + 16, 0, a.dim);
 }
 
 template <int DP>
@@ -490,6 +502,7 @@ __device__ __forceinline__ void dkdv_block(const AttnArgs &a, float *smem, int t
         store_row<DP>(row_of(a.dk, b, j, g), dk, r, a.scale, a.dim, vec);
         store_row<DP>(row_of(a.dv, b, j, g), dv, r, 1.f, a.dim, vec);
     }
+    if (__any_sync(0xffffffffu, has_nan(dk) || has_nan(dv))) again::key_gradients<float>(a, b, g, w0, w0 + 16, true, true);
 }
 
 // blocks [0, k_blocks) make dk and dv, the others dq.  Each kind starts with its longest: under a causal bound

@@ -13,22 +13,13 @@
 //            Longer ones: blocks of BT query rows make dq, blocks of BT key rows dk and dv, in one launch; each
 //            computes p = exp(s - lse) and the delta it needs.  A key block loops over the query heads of
 //            its group and their query tiles, so shared heads are summed in a fixed order without atomics.
-#include "gs_attn.cuh"
+#include "gs_attn_again.cuh"
 #include "gs_tc.cuh"
 
 namespace gs {
 
 using tc::fma2;
 using tc::mul2;
-
-template <typename T> __device__ __forceinline__ float to_f(T x);
-template <> __device__ __forceinline__ float to_f<float>(float x) { return x; }
-template <> __device__ __forceinline__ float to_f<__half>(__half x) { return __half2float(x); }
-template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <typename T> __device__ __forceinline__ T from_f(float x);
-template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
-template <> __device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 template <typename T>
 __device__ __forceinline__ T *row_of(const AttnTensor &t, int64_t b, int64_t pos, int64_t head)
@@ -207,6 +198,17 @@ __device__ __forceinline__ void store_row(T *row, const float2 (&acc)[DP / 32], 
     }
 }
 
+// first of the eight rows of a tile that this thread's warp has
+__device__ __forceinline__ int warp_rows() { return (int)(threadIdx.x >> 5) * 8; }
+
+template <int N>
+__device__ __forceinline__ bool has_nan(const float2 (&acc)[N])
+{
+    float t = 0.f;
+#pragma unroll
+    for (int c = 0; c < N; ++c) t += acc[c].x + acc[c].y;
+    return t != t;
+}
 __device__ __forceinline__ float half_warp_max(float v)
 {
 #pragma unroll
@@ -221,7 +223,7 @@ __device__ __forceinline__ float half_warp_sum(float v)
 }
 
 template <typename T, int BT, int DP>
-__global__ void __launch_bounds__(BT * 4, BT == 64 && DP <= 64 ? 2 : 1) attn_simt_forward_kernel(const AttnArgs a, int tiles, bool vec)
+__global__ void __launch_bounds__(BT * 4, BT == 64 && DP <= 64 ? 2 : 1) attn_simt_forward_kernel(const __grid_constant__ AttnArgs a, int tiles, bool vec)
 {
     extern __shared__ float4 smem4[];
     float(*Q)[DP + 4] = reinterpret_cast<float(*)[DP + 4]>(smem4);
@@ -292,13 +294,33 @@ __global__ void __launch_bounds__(BT * 4, BT == 64 && DP <= 64 ? 2 : 1) attn_sim
         mul_rows<BT, DP>(acc, P, KV, ty, tx);
         __syncthreads();
     }
+    bool nan = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = r0 + 4 * ty + i;
+        nan = nan || has_nan(acc[i]);
         if (r >= a.q_len) continue;
         store_row<T, DP>(row_of<T>(a.out, b, r, h), acc[i], sum[i] > 0.f || sum[i] != sum[i] ? 1.f / sum[i] : 0.f, tx, a.dim, vec);
         if (tx == 0) a.lse[bh * a.q_len + r] = sum[i] == 0.f ? -INFINITY : top[i] + logf(sum[i]);
     }
+    if (__any_sync(0xffffffffu, nan)) again::outputs<T>(a, b, h, r0 + warp_rows(), r0 + warp_rows() + 8);
+}
+
+// dk and dv of the keys j0 + 4 ty..
+template <typename T, int BT, int DP>
+__device__ __forceinline__ void store_keys(const AttnArgs &a, int64_t b, int g, int j0, const float2 (&dk)[4][DP / 32],
+                                           const float2 (&dv)[4][DP / 32], int tx, int ty, bool vec)
+{
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = j0 + 4 * ty + i;
+        nan = nan || has_nan(dk[i]) || has_nan(dv[i]);
+        if (j >= a.k_len) continue;
+        store_row<T, DP>(row_of<T>(a.dk, b, j, g), dk[i], a.scale, tx, a.dim, vec);
+        store_row<T, DP>(row_of<T>(a.dv, b, j, g), dv[i], 1.f, tx, a.dim, vec);
+    }
+    if (__any_sync(0xffffffffu, nan)) again::key_gradients<T>(a, b, g, j0 + warp_rows(), j0 + warp_rows() + 8, true, true);
 }
 
 template <int BT, int DP>
@@ -326,7 +348,7 @@ __device__ __forceinline__ void p_and_ds(float (&p)[4][BT / 16], float (&dp)[4][
 
 // sequences of up to BT queries and keys; one block per key/value head
 template <typename T, int BT, int DP>
-__global__ void __launch_bounds__(BT * 4) attn_simt_backward_one_kernel(const AttnArgs a, bool vec)
+__global__ void __launch_bounds__(BT * 4) attn_simt_backward_one_kernel(const __grid_constant__ AttnArgs a, bool vec)
 {
     extern __shared__ float4 smem4[];
     BwdTiles<BT, DP> &t = *reinterpret_cast<BwdTiles<BT, DP> *>(smem4);
@@ -345,6 +367,7 @@ __global__ void __launch_bounds__(BT * 4) attn_simt_backward_one_kernel(const At
         lo[i] = attn_lo(a, s, 4 * ty + i);
         hi[i] = attn_hi(a, s, 4 * ty + i);
     }
+    bool nan = false;
     for (int h = g * a.group; h < (g + 1) * a.group; ++h) {
         const float *lse_at = a.lse + (b * a.q_heads + h) * a.q_len;
         float lse[4], delta[4] = {};
@@ -379,15 +402,14 @@ __global__ void __launch_bounds__(BT * 4) attn_simt_backward_one_kernel(const At
         mul_cols<BT, DP>(dk, t.s, t.c, ty, tx);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
+        {
+            nan = nan || has_nan(dq[i]);
             if (4 * ty + i < a.q_len) store_row<T, DP>(row_of<T>(a.dq, b, 4 * ty + i, h), dq[i], a.scale, tx, a.dim, vec);
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int j = 4 * ty + i;
-        if (j >= a.k_len) continue;
-        store_row<T, DP>(row_of<T>(a.dk, b, j, g), dk[i], a.scale, tx, a.dim, vec);
-        store_row<T, DP>(row_of<T>(a.dv, b, j, g), dv[i], 1.f, tx, a.dim, vec);
-    }
+    store_keys<T, BT, DP>(a, b, g, 0, dk, dv, tx, ty, vec);
+    if (__any_sync(0xffffffffu, nan))
+        for (int h = g * a.group; h < (g + 1) * a.group; ++h) again::query_gradients<T>(a, b, h, warp_rows(), warp_rows() + 8, 0, a.dim);
 }
 
 // this thread's part (every 16th group of four columns) of the dot products of rows 4 ty.. of dO, in shared
@@ -469,11 +491,14 @@ __device__ __forceinline__ void dq_block(const AttnArgs &a, BwdTiles<BT, DP> &t,
             __syncthreads();
         }
     }
+    bool nan = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = r0 + 4 * ty + i;
+        nan = nan || has_nan(acc[i]);
         if (r < a.q_len) store_row<T, DP>(row_of<T>(a.dq, b, r, h), acc[i], a.scale, tx, a.dim, vec);
     }
+    if (__any_sync(0xffffffffu, nan)) again::query_gradients<T>(a, b, h, r0 + warp_rows(), r0 + warp_rows() + 8, 0, a.dim);
 }
 
 template <typename T, int BT, int DP>
@@ -533,19 +558,13 @@ __device__ __forceinline__ void dkdv_block(const AttnArgs &a, BwdTiles<BT, DP> &
             __syncthreads();
         }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int j = j0 + 4 * ty + i;
-        if (j >= a.k_len) continue;
-        store_row<T, DP>(row_of<T>(a.dk, b, j, g), dk[i], a.scale, tx, a.dim, vec);
-        store_row<T, DP>(row_of<T>(a.dv, b, j, g), dv[i], 1.f, tx, a.dim, vec);
-    }
+    store_keys<T, BT, DP>(a, b, g, j0, dk, dv, tx, ty, vec);
 }
 
 // blocks [0, k_blocks) make dk and dv, the others dq.  Each kind starts with its longest: under a causal bound
 // the first keys have most queries and the last queries most keys.
 template <typename T, int BT, int DP>
-__global__ void __launch_bounds__(BT * 4, DP <= 64 ? 2 : 1) attn_simt_backward_kernel(const AttnArgs a, int64_t k_blocks, int q_tiles, bool vec)
+__global__ void __launch_bounds__(BT * 4, DP <= 64 ? 2 : 1) attn_simt_backward_kernel(const __grid_constant__ AttnArgs a, int64_t k_blocks, int q_tiles, bool vec)
 {
     extern __shared__ float4 smem4[];
     BwdTiles<BT, DP> &t = *reinterpret_cast<BwdTiles<BT, DP> *>(smem4);

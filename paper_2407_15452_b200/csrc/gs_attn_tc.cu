@@ -16,6 +16,7 @@
 // The running maximum moves only when the new one is above it by more than 8 (a factor 256 in p):
 // most tiles then leave O and the sum alone, exact in any case because the quotient O / sum uses one base.
 // p is rounded to the tensors' type for the product with V; the sum takes it in fp32.
+#include "gs_attn_again.cuh"
 #include "gs_attn_tc.cuh"
 
 namespace gs {
@@ -317,6 +318,7 @@ const uint64_t q0 = desc_values(base + L::Q + t * L::TILE), k0 = desc_values(kt)
         if (r < a.q_len)
             a.lse[((int64_t)w.b * a.q_heads + w.h) * a.q_len + r] = inv != 0.f ? (top + log2f(sum)) * LN2 : -INFINITY;
         uint16_t *out = reinterpret_cast<uint16_t *>(a.out.p) + w.b * a.out.sb + (int64_t)r * a.out.sl + w.h * a.out.sh;
+        NanSums total;                     // whether one of the row's values is NaN
 #pragma unroll
         for (int c = 0; c < DP; c += 32) {
             float o[32];
@@ -328,8 +330,13 @@ const uint64_t q0 = desc_values(base + L::Q + t * L::TILE), k0 = desc_values(kt)
                     fence_before();
                     bar_arrive(o_empty + 8 * t);
                 }
+                total.add(o);
             }
             if (r < a.q_len) store32<BF16>(out, c, a.dim, vec, o, inv);
+        }
+        if (__any_sync(0xffffffffu, row && total.found())) {
+            const int r32 = w.r0 + 128 * t + 32 * (warp & 3);
+            again::outputs<typename Tensor16<BF16>::T>(a, w.b, w.h, r32, r32 + 32);
         }
         }
     }
@@ -439,7 +446,7 @@ gs_status attn_tc_forward(const AttnArgs &a, cudaStream_t st)
     return bf16 ? forward_t<true, 128>(a, m, st) : forward_t<false, 128>(a, m, st);
 }
 
-// One block whose wait nothing ends; it gives up after about a millisecond and is counted like any other
+// One block whose wait nothing ends; it gives up within about two seconds and is counted like any other
 __global__ void attn_stall_drill_kernel(unsigned long long *stalls)
 {
     __shared__ __align__(8) uint64_t never;
@@ -451,7 +458,7 @@ __global__ void attn_stall_drill_kernel(unsigned long long *stalls)
         fence_barrier_init();
     }
     __syncthreads();
-    bar_wait(bar, 0, &stalled, 2000000);
+    bar_wait(bar, 0, &stalled, 0);
     __syncthreads();
     if (stalled) drain_stalled(stalls);
 }

@@ -18,6 +18,7 @@
 // P and dS are rounded to the tensors' type for their products.  binary16 has no range for that as it
 // stands: P is scaled by 2^15 (P <= 1), dS by the power of two that brings its bound
 // |dS| <= 2 max|do| max|v| (row norms) near 2^15; the first kernel finds the norms too then.
+#include "gs_attn_again.cuh"
 #include "gs_attn_tc.cuh"
 
 namespace gs {
@@ -167,7 +168,10 @@ __global__ void __launch_bounds__(256) attn_tc_prepare_kernel(const __grid_const
 #pragma unroll
     for (int k = 0; k < ROUNDS; ++k) {
         const int r = tile * T + (int)threadIdx.x / LANES + k * STEP;
-        if (!BF16) top = fmaxf(top, lanes_sum<LANES>(norm[k]));
+        if (!BF16) {                              // a row that is not finite must not cost the others their scale
+            const float n2 = lanes_sum<LANES>(norm[k]);
+            top = fmaxf(top, n2 < INFINITY ? n2 : 0.f);
+        }
         const float d = lanes_sum<LANES>(delta[k]);
         if (on_q && threadIdx.x % LANES == 0 && r < a.q_len) a.delta[bh * a.q_len + r] = d;
     }
@@ -436,6 +440,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
             fence_after();
             const float factor = row && w.n > 0 ? a.scale / up : 0.f;
             uint16_t *out = reinterpret_cast<uint16_t *>(a.dq.p) + w.b * a.dq.sb + (int64_t)r * a.dq.sl + w.h * a.dq.sh;
+            NanSums total;     // whether one of the row's values is NaN
 #pragma unroll
             for (int k = 0; k < DP / 2; k += 32) {    // each half of the warps stores half of the columns
                 float o[32];
@@ -447,8 +452,13 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Bw
                         fence_before();
                         bar_arrive(dq_empty);
                     }
+                    total.add(o);
                 }
                 if (r < a.q_len) store32<BF16>(out, half * (DP / 2) + k, a.dim, vec, o, factor);
+            }
+            if (__any_sync(0xffffffffu, row && total.found())) {
+                const int r32 = w.r0 + 32 * (warp & 3);
+                again::query_gradients<typename Tensor16<BF16>::T>(a, w.b, w.h, r32, r32 + 32, half * (DP / 2), (half + 1) * (DP / 2));
             }
             if (w.n > 0) ++t;
         }
@@ -754,6 +764,7 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             float factor = half == 0 ? (BF16 ? 1.f : 1.f / 32768.f) : a.scale / up;
             if (!row || w.n == 0) factor = 0.f;
             uint16_t *out = reinterpret_cast<uint16_t *>(to.p) + w.b * to.sb + (int64_t)j * to.sl + w.g * to.sh;
+            NanSums total;                   // whether one of the row's values is NaN
 #pragma unroll
             for (int k = 0; k < DP; k += 32) {
                 float o[32];
@@ -765,8 +776,13 @@ attn_tc_dkdv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                         fence_before();
                         bar_arrive(acc_empty);
                     }
+                    total.add(o);
                 }
                 if (j < a.k_len) store32<BF16>(out, k, a.dim, vec, o, factor);
+            }
+            if (__any_sync(0xffffffffu, row && total.found())) {
+                const int j32 = w.j0 + 32 * (warp & 3);
+                again::key_gradients<typename Tensor16<BF16>::T>(a, w.b, w.g, j32, j32 + 32, half == 1, half == 0);
             }
             if (w.n > 0) ++t;
         }

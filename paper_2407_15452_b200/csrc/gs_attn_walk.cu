@@ -20,6 +20,9 @@
 // instructions, and instructions are what these kernels run out of first).
 // P and dS are rounded to 16-bit tensors' type for their products.  For binary16 they are scaled by powers
 // of two first, P by 2^14 (p <= 1), dS by the one that brings its bound |dS| <= max|dp| + |delta| below 2^15.
+#include <type_traits>
+
+#include "gs_attn_again.cuh"
 #include "gs_attn_tc.cuh"
 
 namespace gs {
@@ -29,6 +32,9 @@ using namespace tc;
 static constexpr int KEEP = 3;                    // blocks of 16 keys whose scores the forward pass holds
 
 enum Kind { F16, BF16, F32 };
+template <int K> struct TypeOf { using T = float; };
+template <> struct TypeOf<F16> { using T = __half; };
+template <> struct TypeOf<BF16> { using T = __nv_bfloat16; };
 
 // A tile holds the padded rows of one head as TMA writes them: rows of DP values, in pieces of at most 128 bytes a
 // row (one after the other), whose 16-byte chunks are permuted within 8 rows, so that eight rows at one
@@ -392,32 +398,57 @@ __device__ __forceinline__ void pack_tile(uint32_t (&u)[DP / 8][Row<K, DP>::WORD
     }
 }
 
+// A sum whose only use is that it is NaN if one of the words' values is.  One of 16-bit values may also become NaN by
+// running over; then rows are looked at for nothing.
+template <int K>
+struct NanSum {
+    using Pair = typename std::conditional<K == F32, float, typename std::conditional<K == BF16, __nv_bfloat162, __half2>::type>::type;
+    uint32_t t = 0;
+    __device__ __forceinline__ uint32_t add(uint32_t w)        // passes the word on
+    {
+        Pair &s = reinterpret_cast<Pair &>(t);
+        if constexpr (K == F32) s += __uint_as_float(w);
+        else s = __hadd2(s, reinterpret_cast<const Pair &>(w));
+        return w;
+    }
+    __device__ __forceinline__ bool found()
+    {
+        Pair &s = reinterpret_cast<Pair &>(t);
+        if constexpr (K == F32) return s != s;
+        else return __hisnan(__hadd(s.x, s.y));
+    }
+};
+
 // This warp's 16 x DP result, as pack_tile left it, to rows [r0, r0 + 16) of one head: first into the 16
 // rows at `stage` in shared memory, which nobody else reads any more, then in 16-byte pieces.
-// Rows >= n become zeros, rows >= len are not written.  TMA reads the stage until tma_stores_read.
+// Rows >= n become zeros, rows >= len are not written.  TMA reads the stage until tma_stores_read.  Returns whether this
+// thread's part of rows < n holds a NaN (or may).
 template <int K, int DP>
-__device__ __forceinline__ void store_tile(const uint32_t (&u)[DP / 8][Row<K, DP>::WORDS], uint32_t stage, uint32_t piece,
+__device__ __forceinline__ bool store_tile(const uint32_t (&u)[DP / 8][Row<K, DP>::WORDS], uint32_t stage, uint32_t piece,
                                            const WalkPlan &plan, const CUtensorMap *map, const AttnTensor &t, int64_t b, int h,
                                            int r0, int n, int len, int dim)
 {
     constexpr int CH = Row<K, DP>::CHUNKS, PER = 16 / Row<K, DP>::SIZE;
     const int lane = threadIdx.x & 31, row = lane >> 2, t4 = lane & 3;
     const bool in0 = r0 + row < n, in1 = r0 + row + 8 < n;
+    NanSum<K> top, bottom;                                     // rows 0-7 and 8-15
     __syncwarp();
 #pragma unroll
     for (int c = 0; c < DP / 8; ++c) {                       // the thread's columns 8c + 2 t4 and the next
         if constexpr (K == F32) {
             const int chunk = 2 * c;
             const uint32_t to = stage + (chunk / CH) * piece + Row<K, DP>::at(row, chunk % CH + (t4 >> 1)) + 8 * (t4 & 1);
-            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(in0 ? u[c][0] : 0u), "r"(in0 ? u[c][1] : 0u) : "memory");
+            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(top.add(in0 ? u[c][0] : 0u)), "r"(top.add(in0 ? u[c][1] : 0u)) : "memory");
             asm volatile("st.shared.v2.u32 [%0], {%1, %2};"
-                         ::"r"(to + 8 * Row<K, DP>::BYTES), "r"(in1 ? u[c][2] : 0u), "r"(in1 ? u[c][3] : 0u) : "memory");
+                         ::"r"(to + 8 * Row<K, DP>::BYTES), "r"(bottom.add(in1 ? u[c][2] : 0u)), "r"(bottom.add(in1 ? u[c][3] : 0u)) : "memory");
         } else {
             const uint32_t to = stage + (c / CH) * piece + Row<K, DP>::at(row, c % CH) + 4 * t4;
-            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(in0 ? u[c][0] : 0u) : "memory");
-            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 8 * Row<K, DP>::BYTES), "r"(in1 ? u[c][1] : 0u) : "memory");   // row + 8: the same permutation
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(top.add(in0 ? u[c][0] : 0u)) : "memory");
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 8 * Row<K, DP>::BYTES), "r"(bottom.add(in1 ? u[c][1] : 0u)) : "memory");   // row + 8: the same permutation
         }
     }
+    top.add(bottom.t);
+    const bool nan = top.found();
     if (plan.tma) {
         fence_async_shared();
         __syncwarp();
@@ -426,7 +457,7 @@ __device__ __forceinline__ void store_tile(const uint32_t (&u)[DP / 8][Row<K, DP
             for (int x = 0; x < Row<K, DP>::PIECES; ++x) tma_store(map, stage + x * piece, x * Row<K, DP>::VALUES, r0, h, (int)b);
             tma_store_commit();
         }
-        return;
+        return nan;
     }
     __syncwarp();
     constexpr int ALL = CH * Row<K, DP>::PIECES;
@@ -438,6 +469,7 @@ __device__ __forceinline__ void store_tile(const uint32_t (&u)[DP / 8][Row<K, DP
                      : "r"(stage + (c / CH) * piece + Row<K, DP>::at(rr, c % CH)) : "memory");
         write_chunk<K>(row_at<K>(t, b, h, r), c * PER, dim, plan.vec, w);
     }
+    return nan;
 }
 
 __device__ __forceinline__ float quad_max(float v)
@@ -476,6 +508,7 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ __align__(8) uint64_t full[2];
     __shared__ volatile int stalled;
+    __shared__ volatile int nan;                          // one of the block's results holds one
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, qt = plan.qt, kt = plan.kt;
     const uint32_t total = (uint32_t)a.batch * a.q_heads, step = gridDim.x * plan.units;
     const uint32_t q_half = qt * Row<K, DP>::BLOCK, k_half = kt * Row<K, DP>::BLOCK;
@@ -502,7 +535,7 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
         tma_head<K, DP>(Q + q_bytes + k_bytes, &maps.v, bar, g, b, k_half);
     };
     if (threadIdx.x == 0) {
-        stalled = 0;
+        stalled = nan = 0;
         bar_init(bars, plan.units);
         bar_init(bars + 8, plan.units);
         fence_barrier_init();
@@ -596,7 +629,8 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     }
     uint32_t out[DP / 8][Row<K, DP>::WORDS];
     pack_tile<K, DP>(out, acc, sum_a == 0.f ? 0.f : rcp_fast(sum_a), sum_b == 0.f ? 0.f : rcp_fast(sum_b));
-    store_tile<K, DP>(out, Q + tile * Row<K, DP>::BLOCK, q_half, plan, &maps.out, a.out, l.b, l.h, r0, l.s.nq, a.q_len, a.dim);
+    if (store_tile<K, DP>(out, Q + tile * Row<K, DP>::BLOCK, q_half, plan, &maps.out, a.out, l.b, l.h, r0, l.s.nq, a.q_len, a.dim))
+        nan = 1;
     }
     if (plan.tma) {
         if (lane == 0) tma_stores_read();
@@ -606,6 +640,11 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     if (plan.tma && tid == 0 && !stalled && u0 + plan.stages * step < total) load(u + plan.stages * step, st);
     }
     if (stalled) drain_stalled(stalls);
+    if (nan) {
+        if (plan.tma && lane == 0) tma_stores_done();
+        for (uint32_t v = blockIdx.x * plan.units + mine; v < total; v += step)
+            again::outputs<typename TypeOf<K>::T>(a, v / (uint32_t)a.q_heads, (int)(v % (uint32_t)a.q_heads), tile * 16, tile * 16 + 16);
+    }
 }
 
 // power of two that brings a bound below 2^15 (binary16 only)
@@ -627,6 +666,7 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ __align__(8) uint64_t full[2];
     __shared__ volatile int stalled;
+    __shared__ volatile int nan;                          // one of the block's results holds one
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, qt = plan.qt, kt = plan.kt, tiles = max(qt, kt);
     const uint32_t total = (uint32_t)a.batch * a.kv_heads, step = gridDim.x * plan.units;
     const uint32_t q_half = qt * Row<K, DP>::BLOCK, k_half = kt * Row<K, DP>::BLOCK;
@@ -659,7 +699,7 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
         tma_head<K, DP>(Q + 2 * q_bytes + k_bytes, &maps.v, bar, g, b, k_half);
     };
     if (threadIdx.x == 0) {
-        stalled = 0;
+        stalled = nan = 0;
         bar_init(bars, plan.units);
         bar_init(bars + 8, plan.units);
         fence_barrier_init();
@@ -758,9 +798,9 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
                 if ((lane & 3) == 0) {
                     neg_delta[ra] = -d_a;
                     neg_delta[rb] = -d_b;
-                    if constexpr (K == F16) {
-                        bound[ra] = m_a;
-                        bound[rb] = m_b;
+                    if constexpr (K == F16) {                   // an infinity must not cost the head's other rows their scale
+                        bound[ra] = m_a < INFINITY ? m_a : 0.f;
+                        bound[rb] = m_b < INFINITY ? m_b : 0.f;
                     }
                 }
             };
@@ -843,15 +883,17 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
             }
         }
         __syncthreads();                                      // nobody reads this set of tiles any more
-        if (active && tile < qt)
-            store_tile<K, DP>(dq, Q + tile * Row<K, DP>::BLOCK, q_half, plan, &maps.out, a.dq, l.b, h, r0, s.nq, a.q_len, a.dim);
+        if (active && tile < qt &&
+            store_tile<K, DP>(dq, Q + tile * Row<K, DP>::BLOCK, q_half, plan, &maps.out, a.dq, l.b, h, r0, s.nq, a.q_len, a.dim))
+            nan = 1;
         if (active && tile < kt && x == group - 1) {
             const float f = a.scale / up_k, g = K != F16 ? 1.f : 1.f / 16384.f;
             uint32_t w[DP / 8][Row<K, DP>::WORDS];
             pack_tile<K, DP>(w, dk, f, f);
-            store_tile<K, DP>(w, Kt + tile * Row<K, DP>::BLOCK, k_half, plan, &maps.dk, a.dk, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
+            bool found = store_tile<K, DP>(w, Kt + tile * Row<K, DP>::BLOCK, k_half, plan, &maps.dk, a.dk, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
             pack_tile<K, DP>(w, dv, g, g);
-            store_tile<K, DP>(w, V + tile * Row<K, DP>::BLOCK, k_half, plan, &maps.dv, a.dv, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
+            found |= store_tile<K, DP>(w, V + tile * Row<K, DP>::BLOCK, k_half, plan, &maps.dv, a.dv, l.b, l.h, tile * 16, s.nk, a.k_len, a.dim);
+            if (found) nan = 1;
         }
         if (plan.tma) {
             if (lane == 0) tma_stores_read();
@@ -865,6 +907,16 @@ attn_walk_backward_kernel(const __grid_constant__ AttnArgs a, const __grid_const
     }
     }
     if (stalled) drain_stalled(stalls);
+    if (nan) {
+        using T = typename TypeOf<K>::T;
+        if (plan.tma && lane == 0) tma_stores_done();
+        for (uint32_t v = blockIdx.x * plan.units + mine; v < total; v += step) {
+            const int64_t b = v / (uint32_t)a.kv_heads;
+            const int g = (int)(v % (uint32_t)a.kv_heads);
+            for (int x = 0; x < group; ++x) again::query_gradients<T>(a, b, g * group + x, tile * 16, tile * 16 + 16, 0, a.dim);
+            again::key_gradients<T>(a, b, g, tile * 16, tile * 16 + 16, true, true);
+        }
+    }
 }
 
 // 16-byte accesses need every row of every tensor aligned to them

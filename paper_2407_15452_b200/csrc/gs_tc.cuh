@@ -1,7 +1,7 @@
 // The Blackwell instructions that the tensor-core attention kernels use, one thin wrapper each:
 // mbarriers with bounded waits, TMA tile loads, tensor memory and tcgen05.mma.
 //
-// Waits are bounded.  A kernel whose wait runs out (which no input should cause) sets a flag in
+// Waits are bounded.  A kernel whose wait runs out (which no finite input should cause) sets a flag in
 // shared memory that ends every other wait of its block, drains what it has in flight, frees its
 // tensor memory and adds one to the count that the next call finds and gs_stalled_kernels reads.
 #pragma once
@@ -40,23 +40,28 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
     return done != 0;
 }
 
-static constexpr long long WAIT_CYCLES = 4000000000ll;      // about two seconds
+// In units of 2^32 cycles, about two seconds each: the upper half of the clock is all that a wait looks at, since the code
+// of the waits is a good part of these kernels' and shows where items are short.  About twenty seconds: a warp that does
+// rows again (gs_attn_again.cuh) keeps the others of its block waiting, and 32 keys of 8 query heads of 240000 positions
+// take that long, one after the other.
+static constexpr uint32_t WAIT_LIMIT = 9;
+__device__ __forceinline__ uint32_t clock_upper()
+{
+    uint32_t t;
+    asm volatile("mov.u32 %0, %%clock_hi;" : "=r"(t));
+    return t;
+}
 
 // true once the barrier's phase has completed; false if the wait ran out here or elsewhere in the block
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *stalled, long long limit = WAIT_CYCLES)
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *stalled, uint32_t limit = WAIT_LIMIT)
 {
     if (bar_try(bar, parity)) return true;
-    const long long t0 = clock64();
-    for (;;) {
-#pragma unroll 1
-        for (int i = 0; i < 32; ++i)
-            if (bar_try(bar, parity)) return true;
+    const uint32_t t0 = clock_upper();
+    while (!bar_try(bar, parity)) {
+        if (clock_upper() - t0 > limit) *stalled = 1;
         if (*stalled) return false;
-        if (clock64() - t0 > limit) {
-            *stalled = 1;
-            return false;
-        }
     }
+    return true;
 }
 
 __device__ __forceinline__ void fence_barrier_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
@@ -85,6 +90,8 @@ __device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, 
 __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // this thread's stores have read their shared memory
 __device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+// ... and have been written
+__device__ __forceinline__ void tma_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // ---- work of blocks that have not started -----------------------------------------------------
 // asks for the cancellation of one block's launch; the 16-byte answer arrives at `answer` and counts 16 bytes on `bar`
