@@ -191,22 +191,31 @@ __device__ __forceinline__ void block_dot(float (&s)[8], const Rows<K, DP, HELD>
 
 // acc[16 x DP] += p[16 x 16] B, the 16 rows of B summed over; `block` includes lane_mul.  The thread's values of p,
 // eight columns of which are s[0..3] and s[4..7], are the A operand as they stand, rounded for 16-bit types.
+// The tensor cores round towards zero as they add.  fp32 sums over positions therefore start from zero in every block
+// and the blocks' sums are added to nearest: 200 heads of 128 x 64, root mean square error of the output 6.5e-7 of its own,
+// one running sum 1.3e-6, everything in fp32 3.9e-7; 256 x 4 heads of 100 x 64 80 us instead of 78, backward 350 instead of 328.
 template <int K, int DP>
 __device__ __forceinline__ void block_mul(float (&acc)[DP / 8][4], const float (&s)[8], uint32_t block, uint32_t piece)
 {
     if constexpr (K == F32) {
+        uint32_t hi[2][4], lo[2][4];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            uint32_t hi[4], lo[4];
-            split(s[4 * j], hi[0], lo[0]);
-            split(s[4 * j + 2], hi[1], lo[1]);
-            split(s[4 * j + 1], hi[2], lo[2]);
-            split(s[4 * j + 3], hi[3], lo[3]);
+            split(s[4 * j], hi[j][0], lo[j][0]);
+            split(s[4 * j + 2], hi[j][1], lo[j][1]);
+            split(s[4 * j + 1], hi[j][2], lo[j][2]);
+            split(s[4 * j + 3], hi[j][3], lo[j][3]);
+        }
 #pragma unroll
-            for (int d = 0; d < DP / 8; ++d) {
+        for (int d = 0; d < DP / 8; ++d) {
+            float c[4] = {};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
                 const uint32_t at = step_at<K, DP>(block + j * 8 * Row<K, DP>::BYTES, d, piece);
-                mma3(acc[d], hi, lo, lds(at), lds(at ^ (Row<K, DP>::BYTES | 16)));
+                mma3(c, hi[j], lo[j], lds(at), lds(at ^ (Row<K, DP>::BYTES | 16)));
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[d][i] += c[i];
         }
     } else {
         const uint32_t p[4] = {pack2<K == BF16>(s[0], s[1]), pack2<K == BF16>(s[2], s[3]), pack2<K == BF16>(s[4], s[5]),
