@@ -153,14 +153,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t *r)
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
                  ::GS_I8(r, 0), GS_I8(r, 8), GS_I8(r, 16), GS_I8(r, 24), "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t *r)
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : GS_R8(r, 0) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t *r)
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::GS_I8(r, 0), "r"(addr) : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *r)
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
@@ -244,38 +236,11 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
         : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
     return d;
 }
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-// 2^x of two values on the multiply-add pipes, for x <= 100: x = n + f with n the nearest integer, 2^f by the
-// polynomial of degree 5 with the smallest largest relative error on [-1/2, 1/2] (7.5e-8; coefficients from
-// a Remez exchange), n added to the exponent bits.  Below -126 the result is about 2^-126 and not 0; NaN stays NaN.
-// The exponential unit gives 16 results a cycle and SM, half of what a tile's products leave time for.
-__device__ __forceinline__ float2 exp2_poly(float2 x)
-{
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
-    const float2 big = make_float2(12582912.f, 12582912.f);             // 1.5 * 2^23: its last bit is worth 1
-    const float2 t = add2(x, big);
-    const float2 n = add2(t, make_float2(-12582912.f, -12582912.f));
-    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
-    float2 p = make_float2(0x1.5c08e6p-10f, 0x1.5c08e6p-10f);
-    p = fma2(p, f, make_float2(0x1.3d0c52p-7f, 0x1.3d0c52p-7f));
-    p = fma2(p, f, make_float2(0x1.c6b6e4p-5f, 0x1.c6b6e4p-5f));
-    p = fma2(p, f, make_float2(0x1.ebf918p-3f, 0x1.ebf918p-3f));
-    p = fma2(p, f, make_float2(0x1.62e428p-1f, 0x1.62e428p-1f));
-    p = fma2(p, f, make_float2(1.f, 1.f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 __device__ __forceinline__ float log2_fast(float x)
 {
