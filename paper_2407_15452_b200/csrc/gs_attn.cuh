@@ -18,6 +18,8 @@
 
 namespace gs {
 
+static constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+
 struct AttnTensor {
     void *p;
     int64_t sb, sl, sh;               // strides in elements: sequence, position, head
@@ -96,6 +98,23 @@ static inline gs_status allow_shared(K kernel, int bytes, SharedRecord &done)
     GS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
     if (known) done.bytes[dev].store(bytes, std::memory_order_release);
     return GS_OK;
+}
+
+// Accesses of four elements (of `es` bytes) need every row of every tensor aligned to them
+static inline bool rows_of_four(const AttnArgs &a, size_t es, bool backward)
+{
+    auto ok = [&](const AttnTensor &t) {
+        return ((uintptr_t)t.p % (4 * es)) == 0 && (t.sb | t.sl | t.sh) % 4 == 0;
+    };
+    bool v = a.dim % 4 == 0 && ok(a.q) && ok(a.k) && ok(a.v) && ok(a.out);
+    if (backward) v = v && ok(a.dout) && ok(a.dq) && ok(a.dk) && ok(a.dv);
+    return v;
+}
+static inline gs_status blocks_ok(int64_t blocks)
+{
+    if (blocks <= 0x7FFFFFFF) return GS_OK;
+    set_error("attention of %lld row tiles exceeds one launch", (long long)blocks);
+    return GS_ERR_UNSUPPORTED;
 }
 
 // gs_attn_simt.cu

@@ -1,4 +1,5 @@
-// Attention of fp32 tensors beyond 128 positions, on the tensor cores: every product as three of tf32
+// Attention of fp32 tensors on the tensor cores, forward beyond 128 positions and backward, with up to 64 columns, from 65
+// positions where blocks of 64 rows fill the device one and a half times: every product as three of tf32
 // (mma.sync m16n8k8; a tcgen05 product would need both parts of every operand in shared memory, P and dS included).
 //
 // A block of four warps owns 64 rows - queries for the output and dq, keys for dk and dv - and the rows of the other
@@ -24,7 +25,6 @@ using namespace tc;
 namespace {
 
 constexpr int OWN = 64, THREADS = 128;
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // Rows are DP + 8 floats apart: four rows whose numbers differ modulo 4 then lie in different groups of 8 banks.  The
 // lanes (g, t) = (lane / 4, lane % 4) read pairs of floats, 16 lanes at a time, without a conflict:
@@ -36,13 +36,6 @@ template <int DP> constexpr int STRIDE = DP + 8;
 __device__ __forceinline__ int other(int t) { return 4 + ((t + 2) & 3); }
 __device__ __forceinline__ int row_of_8(int g) { return g & 1 ? other(g >> 1) : g >> 1; }
 
-// x = hi + lo: hi rounded to the 11 bits that tf32 keeps, lo the rest (its own last bit beyond 11 is dropped).  Of
-// x y = hi hi + hi lo + lo hi + lo lo the last is left out: a relative error below 2^-21.
-__device__ __forceinline__ void split(float x, uint32_t &hi, uint32_t &lo)
-{
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
-    lo = __float_as_uint(x - __uint_as_float(hi));
-}
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -193,17 +186,6 @@ __device__ __forceinline__ bool has_nan(const float (&acc)[N][4])
 #pragma unroll
     for (int n = 0; n < N; ++n) t += (acc[n][0] + acc[n][1]) + (acc[n][2] + acc[n][3]);
     return t != t;
-}
-
-__device__ __forceinline__ float quad_max(float v)
-{
-    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
-    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
-}
-__device__ __forceinline__ float quad_sum(float v)
-{
-    v += __shfl_xor_sync(0xffffffffu, v, 1);
-    return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
 
 // What 16 rows see of a tile [x0, x0 + len): row r sees [lo(r), hi(r)), both rising with r
@@ -521,22 +503,6 @@ __global__ void __launch_bounds__(THREADS, 3) attn_f32_backward_kernel(const __g
     }
 }
 
-// 16-byte accesses need every row of every tensor aligned to four elements
-bool rows_of_four(const AttnArgs &a, bool backward)
-{
-    auto ok = [](const AttnTensor &t) { return (uintptr_t)t.p % 16 == 0 && (t.sb | t.sl | t.sh) % 4 == 0; };
-    bool v = a.dim % 4 == 0 && ok(a.q) && ok(a.k) && ok(a.v) && ok(a.out);
-    if (backward) v = v && ok(a.dout) && ok(a.dq) && ok(a.dk) && ok(a.dv);
-    return v;
-}
-
-gs_status blocks_ok(int64_t blocks)
-{
-    if (blocks <= 0x7FFFFFFF) return GS_OK;
-    set_error("attention of %lld row tiles exceeds one launch", (long long)blocks);
-    return GS_ERR_UNSUPPORTED;
-}
-
 template <int DP>
 gs_status forward_t(const AttnArgs &a, cudaStream_t st)
 {
@@ -545,7 +511,7 @@ gs_status forward_t(const AttnArgs &a, cudaStream_t st)
     const int64_t blocks = a.batch * a.q_heads * tiles;
     gs_status s;
     if ((s = blocks_ok(blocks)) != GS_OK || (s = allow_shared(attn_f32_forward_kernel<DP>, fwd_shared<DP>(), record)) != GS_OK) return s;
-    attn_f32_forward_kernel<DP><<<(unsigned)blocks, THREADS, fwd_shared<DP>(), st>>>(a, tiles, rows_of_four(a, false));
+    attn_f32_forward_kernel<DP><<<(unsigned)blocks, THREADS, fwd_shared<DP>(), st>>>(a, tiles, rows_of_four(a, 4, false));
     GS_CUDA_TRY(cudaGetLastError());
     return GS_OK;
 }
@@ -554,7 +520,7 @@ template <int DP>
 gs_status backward_t(const AttnArgs &a, cudaStream_t st)
 {
     static SharedRecord record;
-    const bool vec = rows_of_four(a, true);
+    const bool vec = rows_of_four(a, 4, true);
     const int q_tiles = (a.q_len + OWN - 1) / OWN, k_tiles = (a.k_len + OWN - 1) / OWN;
     const int64_t k_blocks = a.batch * a.kv_heads * k_tiles, blocks = k_blocks + a.batch * a.q_heads * q_tiles;
     const int64_t delta_blocks = (a.batch * a.q_heads * a.q_len + 15) / 16;

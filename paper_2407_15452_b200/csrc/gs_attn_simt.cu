@@ -577,24 +577,6 @@ __global__ void __launch_bounds__(BT * 4, DP <= 64 ? 2 : 1) attn_simt_backward_k
     }
 }
 
-// 4-element vector accesses need every row of every tensor aligned to four elements
-static bool rows_of_four(const AttnArgs &a, size_t es, bool backward)
-{
-    auto ok = [&](const AttnTensor &t) {
-        return ((uintptr_t)t.p % (4 * es)) == 0 && (t.sb | t.sl | t.sh) % 4 == 0;
-    };
-    bool v = a.dim % 4 == 0 && ok(a.q) && ok(a.k) && ok(a.v) && ok(a.out);
-    if (backward) v = v && ok(a.dout) && ok(a.dq) && ok(a.dk) && ok(a.dv);
-    return v;
-}
-
-static gs_status blocks_ok(int64_t blocks)
-{
-    if (blocks <= 0x7FFFFFFF) return GS_OK;
-    set_error("attention of %lld row tiles exceeds one launch", (long long)blocks);
-    return GS_ERR_UNSUPPORTED;
-}
-
 template <typename T, int BT, int DP>
 static gs_status forward_t(const AttnArgs &a, cudaStream_t st)
 {

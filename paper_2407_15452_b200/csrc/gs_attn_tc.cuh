@@ -13,7 +13,6 @@ gs_status attn_tensor_map(CUtensorMap *m, const AttnTensor &t, int32_t dtype, in
                           int dim, int values, int rows);
 
 static constexpr int HALF_TILE = 128 * 128;          // bytes of one box: 128 rows of 64 16-bit values
-static constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
 // Work items, sorted from the longest to the shortest as far as their indexes tell.  Two ways to hand them out:
 //  fixed : as many blocks as SMs; block b takes every gridDim.x-th item, in rounds of alternating direction, which evens

@@ -83,14 +83,6 @@ __device__ __forceinline__ void mma(float *c, const uint32_t (&a)[4], uint32_t b
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// fp32 on the tensor cores: x = hi + lo, hi rounded to the 11 significant bits that tf32 keeps and lo what is left
-// (exact; its own last bits beyond 11 are dropped), and x y = hi hi + hi lo + lo hi with a relative error below 2^-21,
-// eight units of fp32, where the sum over the head dimension itself may be off by as many as it has terms.
-__device__ __forceinline__ void split(float x, uint32_t &hi, uint32_t &lo)
-{
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
-    lo = __float_as_uint(x - __uint_as_float(hi));
-}
 __device__ __forceinline__ void mma3(float *c, const uint32_t (&ah)[4], const uint32_t (&al)[4], float y0, float y1)
 {
     uint32_t h0, l0, h1, l1;
@@ -479,17 +471,6 @@ __device__ __forceinline__ bool store_tile(const uint32_t (&u)[DP / 8][Row<K, DP
         write_chunk<K>(row_at<K>(t, b, h, r), c * PER, dim, plan.vec, w);
     }
     return nan;
-}
-
-__device__ __forceinline__ float quad_max(float v)
-{
-    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
-    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
-}
-__device__ __forceinline__ float quad_sum(float v)
-{
-    v += __shfl_xor_sync(0xffffffffu, v, 1);
-    return v + __shfl_xor_sync(0xffffffffu, v, 2);
 }
 
 // Registers of a thread, and how many blocks of up to BLOCK_WARPS warps an SM is to hold with them.  Measured on
