@@ -583,8 +583,10 @@ GS_API gs_status gs_tune_node2vec_group(int32_t lanes);
  * d_lse is float [batch][q_heads][q_len], contiguous.  Inputs may have zero strides (broadcast
  * values); outputs may not, and no output may overlap an input.  Sums, maxima and gradients are kept
  * in fp32; 16-bit tensors multiply on the tensor cores with the probabilities and score gradients rounded
- * to the tensors' type; products of fp32 tensors are exact to 2^-21 or better.  Results do not depend on scheduling: no value is summed with atomics.
- * Supported: head_dim 1..128, lengths below 2^29.  No library scratch: calls on several streams may overlap.
+ * to the tensors' type; products of fp32 tensors are exact to 2^-21 or better (three tf32 products on the tensor cores
+ * or one multiply-add, by shape; there is no switch to multiply-adds alone).  Results do not depend on scheduling: no
+ * value is summed with atomics.
+ * Supported: head_dim 1..128, lengths up to 2^29, 2^56 rows (sequences x heads x positions) in all.  No library scratch: calls on several streams may overlap.
  * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED, GS_ERR_CUDA.
  */
 typedef struct gs_attention_config {

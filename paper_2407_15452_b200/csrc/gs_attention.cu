@@ -82,11 +82,15 @@ static gs_status pointers_ok(const AttnTensor *t, int n, int32_t dtype)
 }
 
 // Whether fp32 tensors that attn_walk_ok accepts go there (products as three of tf32 each, whole heads in
-// shared memory) or to the CUDA cores.  Measured, whole heads | CUDA cores, us:
-//  forward : 8192 heads of 30 x 32 36 | 90, 4096 of 60 x 64 121 | 169, 2048 of 30 x 128 61 | 62, 1024 of 90 x 128 168 | 288
-//  backward: 2048 heads of 100 x 64 807 | 1058, 1024 of 90 x 128 746 | 1086, 32 of 100 x 64 49 | 27; up to 64 positions, where
-//            a block of the CUDA cores has all of a head, 4096 of 60 x 64 675 | 422, 16384 of 16 x 32 110 | 82, but
-//            16384 of 40 x 32 with a window of 10 on each side 427 | 731
+// shared memory) or to the CUDA cores.  Measured, whole heads | CUDA cores, us (all visible unless said):
+//  forward : 8192 heads of 30 x 32 41 | 88, 4096 of 60 x 64 126 | 159, with a window of 5 on each side 93 | 160, 2048 of
+//            30 x 128 57 | 63, 1024 of 90 x 128 159 | 284
+//  backward, beyond 64 positions: 2048 heads of 100 x 64 822 | 1057, 1024 of 90 x 128 769 | 1082, 150 of 100 x 64, window 10,
+//            57 | 85, 140 of 100 x 64 61 | 75, 32 of 100 x 64 60 | 27
+//  backward, up to 64 positions, where a block of the CUDA cores has all of a head: 4096 heads of 60 x 64 711 | 316, window 5
+//            547 | 310, 4096 of 40 x 64, window 10, 349 | 303, 16384 of 16 x 32 110 | 86, 4096 of 60 x 32 252 | 201, window
+//            20 253 | 200, window 10 204 | 197; but 16384 of 40 x 32, window 10, 433 | 741.  A causal bound alone, 4096 of
+//            48 x 32 110 | 193, is on the wrong side of the rule.
 static bool f32_whole(const AttnArgs &a, bool backward)
 {
     const int n = a.q_len > a.k_len ? a.q_len : a.k_len;
@@ -97,12 +101,14 @@ static bool f32_whole(const AttnArgs &a, bool backward)
 
 // Whether the fp32 tensors that are left go to 64-row tiles on the tensor cores or to the CUDA cores.  Measured,
 // tensor | CUDA cores, us (causal unless said):
-//  forward : 8 x 4 heads of 333 x 64 33 | 33, 16 x 8 heads of 333 x 64 69 | 98, 16 heads of 2048 x 64 230 | 294, 16 of
+//  forward : 8 x 4 heads of 333 x 64 34 | 33, 12 x 4 36 | 40, 16 x 8 67 | 94, 16 heads of 2048 x 64 230 | 294, 16 of
 //            2048 x 128 413 | 532, 16 of 4096 x 64, all visible, 1381 | 2111, 64 x 4 heads of 200 x 32, window 10, 24 | 57
-//  backward: 16 x 8 heads of 333 x 64 229 | 326, 16 heads of 2048 x 64 799 | 964, 16 of 4096 x 64 5048 | 7263, 200 x 32
-//            82 | 170; but 8 x 4 heads of 333 x 64 114 | 83, where the blocks do not fill the device one and a half
-//            times and the CUDA cores' 32-row tiles are twice as many, and 16 heads of 2048 x 128 4031 | 2415 (the
-//            accumulators of 128 columns do not fit a thread's registers).
+//  backward, by the number of 64-row blocks (n): 4 x 4 heads of 700 x 64 (352) 225 | 149, 8 x 4 of 333 x 64 (384) 115 | 81,
+//            10 x 4 (480) 117 | 112, 12 x 4 (576) 112 | 126, 8 x 4 of 700 x 64 (704) 261 | 252, 16 x 4 of 333 x 64 (768)
+//            142 | 168, 20 x 4 (960) 156 | 210, 16 x 8 (1536) 244 | 327, 40 x 4 of 150 x 64 (960) 84 | 123, 4 x 4 of 1024 x 32, all
+//            visible, (512) 194 | 295, 16 heads of 4096 x 64 5048 | 7263: where the blocks do not fill the device one and a
+//            half times (444), the CUDA cores' 32-row tiles, twice as many, are ahead.  16 heads of 2048 x 128 4031 |
+//            2415: the accumulators of 128 columns do not fit a thread's registers.
 static bool f32_tiles(const AttnArgs &a, bool backward)
 {
     if (a.dtype != GS_TABLE_F32 || a.q_len <= 0 || a.k_len <= 0) return false;
@@ -135,9 +141,11 @@ gs_status gs_attention_forward(const gs_attention_config *cfg, const void *d_q, 
     if (!d_lse) return bad("d_lse is NULL");
     if (!writable(a.out, a.batch, a.q_len, a.q_heads)) return bad("out has a zero stride");
     if ((s = stalled_before()) != GS_OK) return s;
-    // 16-bit tensors: up to 128 positions by whole heads, longer ones on 128 x 128 tiles, which need TMA.  Between 65
-    // and 128 positions the wide heads go to the tiles as well: 4096 heads of 100 x 128 take 127 us there and
-    // 146 us whole, 8192 heads of 100 x 64 196 and 141 us.
+    // 16-bit tensors: up to 128 positions by whole heads, longer ones on 128 x 128 tiles, which need TMA (without it
+    // the CUDA cores take 61 us instead of 13 for 4 x 4 heads of 500 x 64, causal, and 117 instead of 17 backward).  Between 65
+    // and 128 positions the wide heads go to the tiles as well.  Tiles | whole, us: 4096 heads of 100 x 128 136 | 141, 300 of
+    // them 16 | 18, 4096 of 70 x 128 131 | 112; 8192 of 100 x 64 226 | 136, 4096 of 60 x 128 130 | 57.  With a window of 10 on
+    // each side, which only whole heads make use of, 4096 of 100 x 128 take 140 | 84: the rule does not look at windows.
     const bool tiles = a.k_len > 0 && attn_tc_forward_ok(a);
     const bool whole = a.dtype == GS_TABLE_F32 ? f32_whole(a, false) : !(tiles && a.q_len > 64 && a.dim > 64);
     if (whole && attn_walk_ok(a, false)) return attn_walk_forward(a, (cudaStream_t)stream);
@@ -174,8 +182,9 @@ gs_status gs_attention_backward(const gs_attention_config *cfg, const void *d_do
         !writable(a.dv, a.batch, a.k_len, a.kv_heads))
         return bad("a gradient has a zero stride");
     if ((s = stalled_before()) != GS_OK) return s;
-    // As above; backward, 4096 heads of 100 x 128 321 us on tiles and 523 us whole, 8192 heads of 100 x 64 424 and
-    // 490 us, but 272 us with a window of 10 on each side, which the whole heads make use of.
+    // As above.  Backward, tiles | whole, us: 4096 heads of 100 x 128 345 | 525, with a window of 10 on each side 346 | 308 (the
+    // rule takes tiles for both), 8192 heads of 100 x 64 469 | 490, window 10 468 | 273, causal 4096 of 128 x 64 259 | 232, 4096
+    // of 100 x 32 216 | 201, 300 heads of 100 x 64 27 | 31.
     const bool tiles = a.q_len > 0 && a.k_len > 0 && attn_tc_backward_ok(a);
     const bool narrow = a.left >= 0 && a.right >= 0 && a.left + a.right < 64;
     const bool wide = (a.q_len > 64 || a.k_len > 64) && (a.dim > 64 || (a.dim > 32 && !narrow));

@@ -12,7 +12,7 @@
 //  forward : scores of up to 48 keys at a time in registers, running maximum and sum over those
 //  backward: dq by query rows, then dk and dv by key rows, both from the same copy in shared memory.  delta =
 //            sum_j p_ij dp_ij comes from the probabilities themselves (a first walk over the row's blocks), so
-//            the forward output is neither read nor is its rounding part of the gradient.
+//            the forward output is neither read nor is its rounding part of the gradient (but in rows done again).
 // Rows past a sequence's end are zeros in shared memory, whatever the tensors hold there.
 // The window enters as the value that the scores' accumulators start from, 0 or -infinity: what a 16 x 16 block
 // shows depends on its distance from the diagonal only, and the few distances with a partly visible block
