@@ -622,7 +622,8 @@ GS_API gs_status gs_attention_backward(const gs_attention_config *cfg, const voi
 /*
  * Norm of the gradients of many tensors taken as one vector, and clipping by it (the bound on an
  * update's length before it reaches a table).  *d_norm = sqrt(sum of all squares); squares are
- * taken in fp32 (an element beyond 1.8e19 in magnitude makes the norm infinite), summed in fp32 over up to
+ * taken in fp32 (an element beyond 1.8e19 in magnitude makes the norm infinite, one
+ * below 1e-19 counts with fewer bits and one below 2.6e-23 not at all), summed in fp32 over up to
  * 18 elements of a tensor and in fp64 from there, in an order that the gradients' sizes, types and alignment and the
  * device fix: the norm is the same bits from either call, and from every call on the same buffers.
  * gs_clip_gradients writes out = g * factor, rounded once to the output's type, with factor =

@@ -11,8 +11,10 @@
 //  backward: delta by a small kernel ahead; then, in one launch, blocks of keys make dk and dv and blocks of queries dq,
 //            both from p = exp(s - lse).  A block of keys goes through the query heads of its group one after the
 //            other, so shared heads are summed in a fixed order without atomics.
-// The bound is the issue rate: a product of 16 x 8 x 8 needs about as many instructions to fetch and split its operands as
-// tensor instructions.  16 heads of 4096 x 64, all visible: forward 1381 us (50 TFLOP/s), backward 5048 us.
+// A product of 16 x 8 x 8 needs about as many instructions to fetch and split its operands as tensor instructions, and an
+// SM holds 12 warps: neither the tensor pipe (53 % busy forward, 50 % backward; 64 heads of 1024 x 64) nor the issue
+// slots (52 and 48 %) are full, each product waits for its operands' conversion.  16 heads of 4096 x 64, all visible:
+// forward 1381 us (50 TFLOP/s), backward 5048 us.
 // The tensor cores round towards zero as they add, so sums over positions start from zero in every tile and the tiles'
 // sums are added by the CUDA cores, rounded to nearest.
 #include "gs_attn_again.cuh"
