@@ -607,7 +607,8 @@ GS_API gs_status gs_attention_forward(const gs_attention_config *cfg, const void
                                const void *d_v, void *d_out, float *d_lse, void *stream);
 
 /*
- * d_out and d_lse are the forward call's results, d_dout the gradient of d_out.  With
+ * d_out and d_lse are the forward call's results, d_dout the gradient of d_out.  d_lse is fp32: p is off by |lse| 2^-24 of
+ * itself beside everything else, so scores beyond some 10^5 cost gradients (not outputs) their precision.  With
  * p_ij = exp(s_ij - lse_i) computed again and delta_i = dout_i . out_i:
  *   ds_ij = p_ij (dout_i . v_j - delta_i),  dq_i = scale sum_j ds_ij k_j,
  *   dk_j = scale sum_{h of the group, i} ds_ij q_i,  dv_j = sum_{h of the group, i} p_ij dout_i.

@@ -4,8 +4,8 @@
 // infinity or a NaN is NaN.  fp32 products as three of tf32 turn an infinite factor into a NaN as well (its low part is
 // inf - inf).  Either way the row's result holds a NaN, so a warp that meets one among its results has those rows, once
 // they are stored, done again here, in fp32 and term by term: infinities give what the formulas in gs_attn.cuh give for
-// them, hidden positions give nothing, and a NaN that the row does see stays a NaN.  Finite inputs never come here; a
-// tile kernel pays one addition per result to know.
+// them, hidden positions give nothing, and a NaN that the row does see stays a NaN.  A tile kernel pays one addition per
+// result to know.  Of finite inputs only rows with scores beyond 10^7 come here (row_factor).
 //
 // Scores are made by one lane per position, sums over positions by lanes that own the columns lane, lane + 32, ..; the
 // loop ends at the first NaN that reaches every column.
@@ -84,6 +84,22 @@ __device__ __forceinline__ void fill(float (&acc)[4], float v)
 {
 #pragma unroll
     for (int x = 0; x < 4; ++x) acc[x] = v;
+}
+
+// What the accumulators of a row are multiplied by at the end, `top` being the base of its exponents in powers of two and
+// `inverse` that of its sum.  Exponents are formed as s * mul - top in one operation, of which top has been rounded; that is
+// one factor for the whole row as long as it is a few powers of two, but beyond 2^31 the largest probability itself becomes
+// zero or infinite (in binary16 beyond 2^28).  From 2^24 on, where it may be half a power, the row is marked
+// to be done again, where the exponents are differences of scores.
+__device__ __forceinline__ float row_factor(float top, float inverse)
+{
+    if (fabsf(top) < 16777216.f) return inverse;
+    return top == -INFINITY && !is_nan(inverse) ? 0.f : NAN;       // 0: nothing visible, or nothing above -infinity
+}
+// the row's lse, from the same and the sum's logarithm in powers of two
+__device__ __forceinline__ float row_lse(float top, float factor, float log2_sum)
+{
+    return factor == 0.f ? -INFINITY : is_nan(factor) ? NAN : (top + log2_sum) * LN2;
 }
 
 // output and lse of query row i < n_q

@@ -282,15 +282,17 @@ __global__ void __launch_bounds__(THREADS, DP <= 64 ? 3 : 2) attn_f32_forward_ke
         }
         mul<N, DP>(acc, p, V);
     }
+    bool nan = has_nan(acc);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int i = w0 + g8 + 8 * r;
-        const float total = quad_sum(sum[r]);
+        const float total = quad_sum(sum[r]), by = again::row_factor(top[r], 1.f / total);
+        nan = nan || again::is_nan(by);
         if (i >= a.q_len) continue;
-        store_row<DP>(row_of(a.out, b, i, h), acc, r, total == 0.f ? 0.f : 1.f / total, a.dim, vec);
-        if (t == 0) a.lse[bh * a.q_len + i] = total == 0.f ? -INFINITY : fmaf(top[r], LN2, logf(total));
+        store_row<DP>(row_of(a.out, b, i, h), acc, r, by, a.dim, vec);
+        if (t == 0) a.lse[bh * a.q_len + i] = again::row_lse(top[r], by, log2f(total));
     }
-    if (__any_sync(0xffffffffu, has_nan(acc))) again::outputs<float>(a, b, h, w0, w0 + 16);
+    if (__any_sync(0xffffffffu, nan)) again::outputs<float>(a, b, h, w0, w0 + 16);
 }
 
 // delta_i = dO_i . out_i; 16 lanes a row, heads of a position one after the other

@@ -314,9 +314,8 @@ const uint64_t q0 = desc_values(base + L::Q + t * L::TILE), k0 = desc_values(kt)
             o_phase ^= 1;
         }
         fence_after();
-        const float inv = row && some && sum != 0.f ? 1.f / sum : 0.f;
-        if (r < a.q_len)
-            a.lse[((int64_t)w.b * a.q_heads + w.h) * a.q_len + r] = inv != 0.f ? (top + log2f(sum)) * LN2 : -INFINITY;
+        const float inv = row && some ? again::row_factor(top, 1.f / sum) : 0.f;
+        if (r < a.q_len) a.lse[((int64_t)w.b * a.q_heads + w.h) * a.q_len + r] = again::row_lse(top, inv, log2f(sum));
         uint16_t *out = reinterpret_cast<uint16_t *>(a.out.p) + w.b * a.out.sb + (int64_t)r * a.out.sl + w.h * a.out.sh;
         NanSums total;                     // whether one of the row's values is NaN
 #pragma unroll
@@ -334,7 +333,7 @@ const uint64_t q0 = desc_values(base + L::Q + t * L::TILE), k0 = desc_values(kt)
             }
             if (r < a.q_len) store32<BF16>(out, c, a.dim, vec, o, inv);
         }
-        if (__any_sync(0xffffffffu, row && total.found())) {
+        if (__any_sync(0xffffffffu, row && (total.found() || again::is_nan(inv)))) {
             const int r32 = w.r0 + 128 * t + 32 * (warp & 3);
             again::outputs<typename Tensor16<BF16>::T>(a, w.b, w.h, r32, r32 + 32);
         }

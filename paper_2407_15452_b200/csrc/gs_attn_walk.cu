@@ -612,13 +612,16 @@ attn_walk_forward_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     }
     sum_a = quad_sum(sum_a);
     sum_b = quad_sum(sum_b);
+    top_a *= mul;
+    top_b *= mul;
+    const float by_a = again::row_factor(top_a, rcp_fast(sum_a)), by_b = again::row_factor(top_b, rcp_fast(sum_b));
     if ((lane & 3) == 0) {
         float *lse = a.lse + (l.b * a.q_heads + l.h) * a.q_len;
-        if (ra < a.q_len) lse[ra] = sum_a == 0.f || ra >= l.s.nq ? -INFINITY : (top_a * mul + log2_fast(sum_a)) * LN2;
-        if (rb < a.q_len) lse[rb] = sum_b == 0.f || rb >= l.s.nq ? -INFINITY : (top_b * mul + log2_fast(sum_b)) * LN2;
+        if (ra < a.q_len) lse[ra] = ra >= l.s.nq ? -INFINITY : again::row_lse(top_a, by_a, log2_fast(sum_a));
+        if (rb < a.q_len) lse[rb] = rb >= l.s.nq ? -INFINITY : again::row_lse(top_b, by_b, log2_fast(sum_b));
     }
     uint32_t out[DP / 8][Row<K, DP>::WORDS];
-    pack_tile<K, DP>(out, acc, sum_a == 0.f ? 0.f : rcp_fast(sum_a), sum_b == 0.f ? 0.f : rcp_fast(sum_b));
+    pack_tile<K, DP>(out, acc, by_a, by_b);
     if (store_tile<K, DP>(out, Q + tile * Row<K, DP>::BLOCK, q_half, plan, &maps.out, a.out, l.b, l.h, r0, l.s.nq, a.q_len, a.dim))
         nan = 1;
     }
