@@ -394,7 +394,7 @@ __device__ __forceinline__ void dq_block(const AttnArgs &a, float *smem, int til
         const int i = w0 + g8 + 8 * r;
         if (i < a.q_len) store_row<DP>(row_of(a.dq, b, i, h), acc, r, a.scale, a.dim, vec);
     }
-    if (__any_sync(0xffffffffu, has_nan(acc))) again::query_gradients<float>(a, b, h, w0, w0 + 16, 0, a.dim);
+    if (__any_sync(0xffffffffu, has_nan(acc))) again::query_gradients_here<float>(a, b, h, w0, w0 + 16, 0, a.dim);
 }
 
 template <int DP>
@@ -488,7 +488,7 @@ __device__ __forceinline__ void dkdv_block(const AttnArgs &a, float *smem, int t
         store_row<DP>(row_of(a.dk, b, j, g), dk, r, a.scale, a.dim, vec);
         store_row<DP>(row_of(a.dv, b, j, g), dv, r, 1.f, a.dim, vec);
     }
-    if (__any_sync(0xffffffffu, has_nan(dk) || has_nan(dv))) again::key_gradients<float>(a, b, g, w0, w0 + 16, true, true);
+    if (__any_sync(0xffffffffu, has_nan(dk) || has_nan(dv))) again::key_gradients_here<float>(a, b, g, w0, w0 + 16, true, true);
 }
 
 // blocks [0, k_blocks) make dk and dv, the others dq.  Each kind starts with its longest: under a causal bound
