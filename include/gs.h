@@ -648,6 +648,95 @@ GS_API gs_status gs_gradient_norm(const gs_tensor *h_grads, int64_t n_tensors, d
 GS_API gs_status gs_clip_gradients(const gs_tensor *h_grads, const gs_tensor *h_out, int64_t n_tensors,
                             float max_norm, double *d_work, float *d_norm, void *stream);
 
+/* ---------------------------------------------------------------- layers around attention */
+/*
+ * Layer norm over the columns of every position of [batch][length][columns] tensors, and its gradient:
+ *   mean = sum_c x_c / columns, rstd = 1 / sqrt(sum_c (x_c - mean)^2 / columns + eps),
+ *   xh_c = (x_c - mean) rstd, y_c = xh_c weight_c + bias_c,
+ *   g_c = dy_c weight_c, dx_c = rstd (g_c - sum_k g_k / columns - xh_c sum_k g_k xh_k / columns),
+ *   dweight_c = sum over positions of dy_c xh_c, dbias_c = sum over positions of dy_c.
+ * d_lens[b] positions of sequence b are valid (length if NULL; clamped to [0, length]); the others are never read
+ * (they may hold anything, NaN included), their y, stats and dx are written as zeros and they add nothing to the sums.
+ * x, y, dy, dx have type dtype, any strides (in elements) over batch and position and contiguous columns; d_weight,
+ * d_bias and their gradients have type weight_dtype (GS_TABLE_F32 or dtype) and may be NULL (weight 1, bias 0; a
+ * gradient that is NULL is not computed).  d_stats is float [batch][length][2]: mean and rstd, contiguous (NULL in
+ * the forward call if no gradient will be asked for).  Inputs may have zero strides, outputs may not; no
+ * output may overlap an input or another output.  Sums are fp32 in an order that the shapes, the types, the alignment and the device
+ * fix: results are bitwise repeatable.
+ * With d_packed and d_scales the forward call also keeps x as gs_checkpoint_pack does (rows = batch * length), zeros
+ * and a scale of zero at positions that are not valid; the backward call then takes them in place of x (d_x NULL): the gradients of
+ * the formulas above with mean and rstd of the original and x as the checkpoint has it.
+ * d_work: gs_layer_norm_backward_work(cfg) floats of the caller's, written by the call (-1 for a configuration that
+ * the calls refuse).  Supported: 1 to 16384 columns, 2^40 rows.  Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED, GS_ERR_CUDA.
+ */
+typedef struct gs_layer_norm_config {
+    int32_t dtype;
+    int32_t weight_dtype;
+    int64_t batch, length;
+    int32_t columns;
+    float   eps;                          /* >= 0 */
+    const int32_t *d_lens;                /* [batch] or NULL */
+    int64_t x_stride[2], y_stride[2];     /* batch, position */
+    int64_t dy_stride[2], dx_stride[2];   /* backward only   */
+} gs_layer_norm_config;
+
+GS_API gs_status gs_layer_norm_forward(const gs_layer_norm_config *cfg, const void *d_x, const void *d_weight,
+                                const void *d_bias, void *d_y, float *d_stats, int8_t *d_packed, float *d_scales,
+                                void *stream);
+GS_API int64_t gs_layer_norm_backward_work(const gs_layer_norm_config *cfg);
+GS_API gs_status gs_layer_norm_backward(const gs_layer_norm_config *cfg, const void *d_dy, const void *d_x,
+                                 const int8_t *d_packed, const float *d_scales, const void *d_weight,
+                                 const float *d_stats, float *d_work, void *d_dx, void *d_dweight, void *d_dbias,
+                                 void *stream);
+
+/*
+ * Gated linear recurrence along the positions of [batch][length][channels] tensors, channel by channel, and its gradient:
+ *   a_t = 1 / (1 + exp(-gate_t)), h_t = a_t h_(t-1) + (1 - a_t) x_t, out_t = h_t, final = h after the last valid position,
+ *   g_t = dout_t + a_(t+1) g_(t+1) (dfinal in place of the second term at the last valid position),
+ *   dx_t = (1 - a_t) g_t, dgate_t = a_t (1 - a_t) (h_(t-1) - x_t) g_t, dh0 = a_0 g_0.
+ * h_(-1) is d_h0 (float [batch][channels], NULL: zeros).  d_lens as for gs_layer_norm_forward: positions that are not valid
+ * are never read, give zeros and leave the state as it is (a sequence of length 0 has final = h0, dh0 = dfinal).
+ * d_final (float [batch][channels]) may be NULL, and may be d_h0 itself: sequences are continued one position or many at a time
+ * by handing the final state to the next call.
+ * d_states (NULL if no gradient will be asked for): gs_recurrence_states(cfg) floats, [batch][(length - 1) / 128][channels], the state
+ * after every 128 positions but the last, from which the backward call computes the states in between again.
+ * d_dout, d_dfinal NULL: zeros; d_dh0 NULL: not wanted.
+ * Tensors have type dtype, any strides (in elements) over batch and position, contiguous channels; zero strides of inputs, overlaps
+ * and repeatability as above (but for d_final = d_h0).  Products and sums are fp32.  What follows an infinity in x or a state is infinite or NaN.
+ * Supported: length up to 2^30, 2^40 values of a batch entry's position (batch x channels).  Errors: as above.
+ */
+typedef struct gs_recurrence_config {
+    int32_t dtype;
+    int32_t length;
+    int64_t batch, channels;
+    const int32_t *d_lens;                                        /* [batch] or NULL */
+    int64_t gate_stride[2], x_stride[2], out_stride[2];           /* batch, position */
+    int64_t dout_stride[2], dgate_stride[2], dx_stride[2];        /* backward only   */
+} gs_recurrence_config;
+
+GS_API int64_t gs_recurrence_states(const gs_recurrence_config *cfg);
+GS_API gs_status gs_recurrence_forward(const gs_recurrence_config *cfg, const void *d_gate, const void *d_x,
+                                const float *d_h0, void *d_out, float *d_final, float *d_states, void *stream);
+GS_API gs_status gs_recurrence_backward(const gs_recurrence_config *cfg, const void *d_dout, const float *d_dfinal,
+                                 const void *d_gate, const void *d_x, const float *d_h0, const float *d_states,
+                                 void *d_dgate, void *d_dx, float *d_dh0, void *stream);
+
+/*
+ * Activations kept in 8 bits between the forward and the backward pass: rows of `columns` values (row_stride elements
+ * apart), every 128 columns of a row with a scale of their own,
+ *   scale = max |x| / 127 rounded towards zero to fp32, packed = the whole number nearest to x / scale (ties to even, decided
+ *   exactly; at most 127 in magnitude), value = packed * scale in fp32, rounded once to the type that gs_checkpoint_unpack writes.
+ * A value is off by at most half a scale (1 / 254 of its block's largest magnitude; more only where the scale is subnormal), and
+ * a block whose largest magnitude is below 127 * 2^-149 gives zeros.  A block that holds an infinity or a NaN has scale NaN and comes
+ * back as NaN altogether: a bad activation is not hidden.
+ * d_packed is int8 [rows][columns] and d_scales float [rows][(columns + 127) / 128], contiguous.
+ * Supported: 2^40 rows, 2^31 - 1 columns, 2^46 values.  Errors: as above.
+ */
+GS_API gs_status gs_checkpoint_pack(int32_t dtype, const void *d_x, int64_t rows, int64_t columns, int64_t row_stride,
+                             int8_t *d_packed, float *d_scales, void *stream);
+GS_API gs_status gs_checkpoint_unpack(int32_t dtype, const int8_t *d_packed, const float *d_scales, int64_t rows,
+                               int64_t columns, int64_t row_stride, void *d_x, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -39,6 +39,9 @@ EXPORTS = [
     "gs_init_embeddings_bf16", "gs_sgns_step_bf16",
     "gs_attention_forward", "gs_attention_backward", "gs_attention_backward_work",
     "gs_stalled_kernels", "gs_stall_drill", "gs_gradient_norm_work", "gs_gradient_norm", "gs_clip_gradients",
+    "gs_layer_norm_forward", "gs_layer_norm_backward", "gs_layer_norm_backward_work",
+    "gs_recurrence_states", "gs_recurrence_forward", "gs_recurrence_backward",
+    "gs_checkpoint_pack", "gs_checkpoint_unpack",
 ]
 
 
@@ -72,6 +75,20 @@ class AttentionConfig(ctypes.Structure):
         ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
         ("d_q_lens", ctypes.c_void_p), ("d_k_lens", ctypes.c_void_p),
     ] + [(f"{t}_stride", ctypes.c_int64 * 3) for t in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+
+
+class LayerNormConfig(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32), ("batch", ctypes.c_int64),
+        ("length", ctypes.c_int64), ("columns", ctypes.c_int32), ("eps", ctypes.c_float), ("d_lens", ctypes.c_void_p),
+    ] + [(f"{t}_stride", ctypes.c_int64 * 2) for t in ("x", "y", "dy", "dx")]
+
+
+class RecurrenceConfig(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("length", ctypes.c_int32), ("batch", ctypes.c_int64), ("channels", ctypes.c_int64),
+        ("d_lens", ctypes.c_void_p),
+    ] + [(f"{t}_stride", ctypes.c_int64 * 2) for t in ("gate", "x", "out", "dout", "dgate", "dx")]
 
 
 class TensorEntry(ctypes.Structure):
@@ -113,6 +130,15 @@ def lib():
         L.gs_gradient_norm_work.argtypes, L.gs_gradient_norm_work.restype = [i64], i64
         L.gs_gradient_norm.argtypes = [p, i64, p, p, p]
         L.gs_clip_gradients.argtypes = [p, p, i64, ctypes.c_float, p, p, p]
+        i32 = ctypes.c_int32
+        L.gs_layer_norm_forward.argtypes = [p] * 9
+        L.gs_layer_norm_backward_work.argtypes, L.gs_layer_norm_backward_work.restype = [p], i64
+        L.gs_layer_norm_backward.argtypes = [p] * 12
+        L.gs_recurrence_states.argtypes, L.gs_recurrence_states.restype = [p], i64
+        L.gs_recurrence_forward.argtypes = [p] * 8
+        L.gs_recurrence_backward.argtypes = [p] * 11
+        L.gs_checkpoint_pack.argtypes = [i32, p, i64, i64, i64, p, p, p]
+        L.gs_checkpoint_unpack.argtypes = [i32, p, p, i64, i64, i64, p, p]
         _lib = L
     return _lib
 
@@ -606,3 +632,211 @@ def gs_clip_gradients(grads, max_norm: float, out=None):
     _check(lib().gs_clip_gradients(entries, targets, len(grads), max_norm, work.data_ptr(), norm.data_ptr(),
                                    _raw_stream(device)))
     return norm
+
+
+# ---------------------------------------------------------------- layers around attention
+_pack_norm = struct.Struct("2i2qifQ8q").pack
+_pack_recurrence = struct.Struct("2i2qQ12q").pack
+_NO_STRIDE2 = (0, 0)
+
+
+def _positions(t, dtype, device, shape, name):
+    """Checks one [batch, position, column] tensor; returns its first two strides."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != device:
+        raise TypeError(f"{name} must be a tensor of {dtype} on cuda:{device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    st = t.stride()
+    if st[2] != 1 and shape[2] > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return st[:2]
+
+
+def _leading(t, name, dtypes):
+    """Device and dtype code of the tensor that a call's other tensors are measured by."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in dtypes):
+        raise TypeError(f"{name} must be a CUDA tensor [batch, position, column] of {', '.join(str(d)[6:] for d in dtypes)}")
+    device = t.get_device()
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+    return device
+
+
+def _vector(t, dtype, device, columns, name):
+    if t is None:
+        return 0
+    if not (isinstance(t, torch.Tensor) and t.get_device() == device and t.dtype is dtype and t.shape == (columns,)
+            and t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous tensor of {columns} values of {dtype} on cuda:{device}")
+    return t.data_ptr()
+
+
+def _vector_dtype(weight, bias, dtype):
+    """Type of weight and bias: float32 or the tensors' own, one for both."""
+    given = weight if weight is not None else bias
+    if given is None:
+        return torch.float32
+    if not isinstance(given, torch.Tensor) or (given.dtype is not torch.float32 and given.dtype is not dtype):
+        raise TypeError(f"weight and bias must be tensors of float32 or {dtype}")
+    return given.dtype
+
+
+def _exactly(t, dtype, device, shape, name):
+    """Checks a contiguous tensor of the library's own layout; returns its address."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape
+            and t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous tensor of {dtype} and shape {tuple(shape)} on cuda:{device}")
+    return t.data_ptr()
+
+
+def gs_layer_norm_forward(x, weight=None, bias=None, eps=1e-5, lens=None, checkpoint=False, y=None):
+    """Layer norm of x[batch, length, columns] over its columns (see gs.h).  Returns (y like x, stats float32[batch, length, 2]),
+    with checkpoint=True (y, stats, packed, scales): x in 8 bits, to be given to gs_layer_norm_backward in its place."""
+    device = _leading(x, "x", _TABLE_DTYPE)
+    shape, dtype = x.shape, x.dtype
+    b, n, c = shape
+    wt = _vector_dtype(weight, bias, dtype)
+    y = torch.empty_like(x) if y is None else y
+    stats = x.new_empty((b, n, 2), dtype=torch.float32)
+    packed = scales = None
+    if checkpoint:
+        packed = x.new_empty(shape, dtype=torch.int8)
+        scales = x.new_empty((b, n, (c + 127) // 128), dtype=torch.float32)
+    cfg = _pack_norm(_TABLE_DTYPE[dtype], _TABLE_DTYPE[wt], b, n, c, eps, _lens(lens, b, device, "lens"),
+                     *_positions(x, dtype, device, shape, "x"), *_positions(y, dtype, device, shape, "y"), *_NO_STRIDE2, *_NO_STRIDE2)
+    _check(lib().gs_layer_norm_forward(cfg, x.data_ptr(), _vector(weight, wt, device, c, "weight"),
+                                       _vector(bias, wt, device, c, "bias"), y.data_ptr(), stats.data_ptr(),
+                                       packed.data_ptr() if checkpoint else 0, scales.data_ptr() if checkpoint else 0,
+                                       _raw_stream(device)))
+    return (y, stats, packed, scales) if checkpoint else (y, stats)
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_backward_work(dtype, columns, device):
+    return max(0, lib().gs_layer_norm_backward_work(_pack_norm(dtype, dtype, 0, 0, columns, 0.0, 0, *(_NO_STRIDE2 * 4))))
+
+
+def gs_layer_norm_backward(dy, x, weight, bias, stats, lens=None, scales=None, dx=None):
+    """Gradients of gs_layer_norm_forward: returns (dx like dy, dweight, dbias), None for a weight or bias that is None.
+    x: the forward call's, or its `packed` together with its `scales`."""
+    device = _leading(dy, "dy", _TABLE_DTYPE)
+    shape, dtype = dy.shape, dy.dtype
+    b, n, c = shape
+    wt = _vector_dtype(weight, bias, dtype)
+    dx = torch.empty_like(dy) if dx is None else dx
+    if scales is None:
+        at_x, strides, packed, at_scales = None, _positions(x, dtype, device, shape, "x"), 0, 0
+        at_x = x.data_ptr()
+    else:
+        packed, strides, at_x = _exactly(x, torch.int8, device, shape, "x"), _NO_STRIDE2, 0
+        at_scales = _exactly(scales, torch.float32, device, (b, n, (c + 127) // 128), "scales")
+    at_stats = _exactly(stats, torch.float32, device, (b, n, 2), "stats")
+    cfg = _pack_norm(_TABLE_DTYPE[dtype], _TABLE_DTYPE[wt], b, n, c, 0.0, _lens(lens, b, device, "lens"), *strides, *_NO_STRIDE2,
+                     *_positions(dy, dtype, device, shape, "dy"), *_positions(dx, dtype, device, shape, "dx"))
+    at_weight = _vector(weight, wt, device, c, "weight")
+    _vector(bias, wt, device, c, "bias")
+    dweight = None if weight is None else torch.empty_like(weight)
+    dbias = None if bias is None else torch.empty_like(bias)
+    work = stats.new_empty(_norm_backward_work(_TABLE_DTYPE[dtype], c, device))
+    _check(lib().gs_layer_norm_backward(cfg, dy.data_ptr(), at_x, packed, at_scales, at_weight, at_stats, work.data_ptr(),
+                                        dx.data_ptr(), 0 if dweight is None else dweight.data_ptr(),
+                                        0 if dbias is None else dbias.data_ptr(), _raw_stream(device)))
+    return dx, dweight, dbias
+
+
+GS_RECURRENCE_SPAN = 128              # positions between two of the states that the forward call keeps
+
+
+def _state(t, device, shape, name):
+    return 0 if t is None else _exactly(t, torch.float32, device, shape, name)
+
+
+def gs_recurrence_forward(gate, x, h0=None, lens=None, keep=True, out=None, final=None):
+    """Gated linear recurrence along the positions of x[batch, length, channels] (see gs.h) from the state h0 float32[batch, channels]
+    (zeros if None).  Returns (out like x, final float32[batch, channels], states): states is what gs_recurrence_backward needs,
+    None with keep=False.  final may be h0: sequences are continued by handing it to the next call."""
+    device = _leading(x, "x", _TABLE_DTYPE)
+    shape, dtype = x.shape, x.dtype
+    b, n, c = shape
+    out = torch.empty_like(x) if out is None else out
+    final = x.new_empty((b, c), dtype=torch.float32) if final is None else final
+    states = x.new_empty((b, max(0, n - 1) // GS_RECURRENCE_SPAN, c), dtype=torch.float32) if keep else None
+    cfg = _pack_recurrence(_TABLE_DTYPE[dtype], n, b, c, _lens(lens, b, device, "lens"),
+                           *_positions(gate, dtype, device, shape, "gate"), *_positions(x, dtype, device, shape, "x"),
+                           *_positions(out, dtype, device, shape, "out"), *(_NO_STRIDE2 * 3))
+    _check(lib().gs_recurrence_forward(cfg, gate.data_ptr(), x.data_ptr(), _state(h0, device, (b, c), "h0"), out.data_ptr(),
+                                       _state(final, device, (b, c), "final"), states.data_ptr() if keep else 0,
+                                       _raw_stream(device)))
+    return out, final, states
+
+
+def gs_recurrence_backward(dout, gate, x, h0=None, states=None, dfinal=None, lens=None, dgate=None, dx=None):
+    """Gradients of gs_recurrence_forward: returns (dgate, dx, dh0 float32[batch, channels]).  dout and dfinal are the gradients of
+    out and final (None: zeros), states the forward call's."""
+    device = _leading(x, "x", _TABLE_DTYPE)
+    shape, dtype = x.shape, x.dtype
+    b, n, c = shape
+    dgate = torch.empty_like(gate) if dgate is None else dgate
+    dx = torch.empty_like(x) if dx is None else dx
+    dh0 = x.new_empty((b, c), dtype=torch.float32)
+    kept = max(0, n - 1) // GS_RECURRENCE_SPAN
+    cfg = _pack_recurrence(_TABLE_DTYPE[dtype], n, b, c, _lens(lens, b, device, "lens"),
+                           *_positions(gate, dtype, device, shape, "gate"), *_positions(x, dtype, device, shape, "x"), *_NO_STRIDE2,
+                           *(_NO_STRIDE2 if dout is None else _positions(dout, dtype, device, shape, "dout")),
+                           *_positions(dgate, dtype, device, shape, "dgate"), *_positions(dx, dtype, device, shape, "dx"))
+    at_states = _exactly(states, torch.float32, device, (b, kept, c), "states") if kept else 0
+    _check(lib().gs_recurrence_backward(cfg, 0 if dout is None else dout.data_ptr(), _state(dfinal, device, (b, c), "dfinal"),
+                                        gate.data_ptr(), x.data_ptr(), _state(h0, device, (b, c), "h0"), at_states,
+                                        dgate.data_ptr(), dx.data_ptr(), dh0.data_ptr(), _raw_stream(device)))
+    return dgate, dx, dh0
+
+
+def _rows(t, name):
+    """(rows, columns, row stride) of a tensor whose leading dimensions are one run of rows."""
+    if t.dim() == 0:
+        raise ValueError(f"{name} must have at least one dimension")
+    columns = t.shape[-1]
+    rows = t.numel() // columns if columns else 0
+    if t.is_contiguous():
+        return rows, columns, columns
+    if t.dim() == 2 and (t.stride(1) == 1 or columns == 1):
+        return rows, columns, t.stride(0)
+    raise ValueError(f"{name} must be contiguous, or have two dimensions and contiguous rows")
+
+
+def gs_checkpoint_pack(x):
+    """x[..., columns] in 8 bits (see gs.h): returns (packed int8 like x, scales float32[..., ceil(columns / 128)])."""
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype in _TABLE_DTYPE):
+        raise TypeError("x must be a CUDA tensor of float32, float16 or bfloat16")
+    device = x.get_device()
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"x is on {x.device}, which is not the current device")
+    rows, columns, stride = _rows(x, "x")
+    packed = x.new_empty(x.shape, dtype=torch.int8)
+    scales = x.new_empty((*x.shape[:-1], (columns + 127) // 128), dtype=torch.float32)
+    _check(lib().gs_checkpoint_pack(_TABLE_DTYPE[x.dtype], x.data_ptr(), rows, columns, stride, packed.data_ptr(),
+                                    scales.data_ptr(), _raw_stream(device)))
+    return packed, scales
+
+
+def gs_checkpoint_unpack(packed, scales, dtype=torch.float32, out=None):
+    """The values of gs_checkpoint_pack's result as a tensor of `dtype` (or in `out`)."""
+    if not (isinstance(packed, torch.Tensor) and packed.is_cuda and packed.dtype is torch.int8 and packed.is_contiguous()
+            and packed.dim() > 0):
+        raise TypeError("packed must be a contiguous int8 CUDA tensor")
+    device = packed.get_device()
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"packed is on {packed.device}, which is not the current device")
+    at_scales = _exactly(scales, torch.float32, device, (*packed.shape[:-1], (packed.shape[-1] + 127) // 128), "scales")
+    if out is None:
+        if dtype not in _TABLE_DTYPE:
+            raise TypeError("dtype must be float32, float16 or bfloat16")
+        out = packed.new_empty(packed.shape, dtype=dtype)
+    elif not isinstance(out, torch.Tensor) or out.dtype not in _TABLE_DTYPE or out.get_device() != device:
+        raise TypeError(f"out must be a tensor of float32, float16 or bfloat16 on cuda:{device}")
+    elif out.shape != packed.shape:
+        raise ValueError(f"out has shape {tuple(out.shape)}, expected {tuple(packed.shape)}")
+    rows, columns, stride = _rows(out, "out")
+    _check(lib().gs_checkpoint_unpack(_TABLE_DTYPE[out.dtype], packed.data_ptr(), at_scales, rows, columns, stride, out.data_ptr(),
+                                      _raw_stream(device)))
+    return out

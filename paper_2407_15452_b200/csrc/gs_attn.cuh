@@ -11,9 +11,6 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include <atomic>
-#include <mutex>
-
 #include "gs_common.cuh"
 
 namespace gs {
@@ -78,27 +75,6 @@ template <typename T> __device__ __forceinline__ T from_f(float x);
 template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
 template <> __device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-
-// Lets `kernel` use up to `bytes` of dynamic shared memory on the current device; `done` is the kernel's own record of
-// what each device allows already (the attribute costs about a microsecond to set).  Setting and recording are one step
-// under a lock: of two threads that ask for different sizes, the smaller one must not undo the larger.
-struct SharedRecord {
-    std::atomic<int> bytes[64];
-    std::mutex lock;
-};
-template <typename K>
-static inline gs_status allow_shared(K kernel, int bytes, SharedRecord &done)
-{
-    int dev = 0;
-    GS_CUDA_TRY(cudaGetDevice(&dev));
-    const bool known = dev >= 0 && dev < 64;
-    if (known && done.bytes[dev].load(std::memory_order_acquire) >= bytes) return GS_OK;
-    std::lock_guard<std::mutex> hold(done.lock);
-    if (known && done.bytes[dev].load(std::memory_order_relaxed) >= bytes) return GS_OK;
-    GS_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-    if (known) done.bytes[dev].store(bytes, std::memory_order_release);
-    return GS_OK;
-}
 
 // Accesses of four elements (of `es` bytes) need every row of every tensor aligned to them
 static inline bool rows_of_four(const AttnArgs &a, size_t es, bool backward)

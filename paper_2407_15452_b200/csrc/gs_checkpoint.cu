@@ -1,0 +1,207 @@
+// Activations in 8 bits: packing and unpacking.
+//
+// A block of 128 columns is held by 16 or 32 lanes, 16 bytes of values each (or, where rows are not aligned to that, by a warp,
+// one value at a time), so that its largest magnitude is a few shuffles and every value is read once.  Bound: memory traffic.
+#include "gs_norm.cuh"
+
+namespace gs {
+
+static constexpr int PACK_THREADS = 256, PACK_BLOCKS = 8;             // blocks of an SM
+
+struct PackArgs {
+    NormRows x;
+    int8_t *packed;
+    float *scales;
+    const int32_t *lens;
+    Divider by_blocks, by_length;
+    int64_t rows, length, columns, blocks_of_row, blocks;              // blocks: of 128 columns, in all
+};
+
+// Lanes that hold a block of columns, and values of a lane's access
+template <typename T, bool ALIGNED> struct Holders {
+    static constexpr int VEC = ALIGNED ? Wide<T>::N : 1, LANES = ALIGNED ? KEPT_BLOCK / VEC : 32, PIECES = KEPT_BLOCK / VEC / LANES;
+    static constexpr int AT_ONCE = ALIGNED ? 4 : 1;                    // blocks that a group of lanes has under way
+};
+
+struct BlockAt {
+    int64_t row, first, b, t;                                          // first column
+    bool there;
+};
+__device__ __forceinline__ BlockAt block_at(const PackArgs &a, int64_t i)
+{
+    BlockAt p;
+    p.there = i < a.blocks;
+    p.row = p.there ? a.by_blocks.of(i) : 0;
+    p.first = p.there ? (i - p.row * a.blocks_of_row) * KEPT_BLOCK : 0;
+    p.b = a.by_length.of(p.row);
+    p.t = p.row - p.b * a.length;
+    return p;
+}
+
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const __grid_constant__ PackArgs a)
+{
+    typedef Holders<T, ALIGNED> H;
+    typedef Piece<T, H::VEC> P;
+    const int member = threadIdx.x % H::LANES;
+    const int64_t groups = (int64_t)gridDim.x * (PACK_THREADS / H::LANES);
+    // the same number of rounds for all lanes of a warp: they reduce together
+    for (int64_t i0 = (int64_t)blockIdx.x * (PACK_THREADS / H::LANES); i0 < a.blocks; i0 += groups * H::AT_ONCE) {
+        BlockAt at[H::AT_ONCE];
+        typename P::raw r[H::AT_ONCE][H::PIECES];
+#pragma unroll
+        for (int u = 0; u < H::AT_ONCE; ++u) {
+            at[u] = block_at(a, i0 + u * groups + threadIdx.x / H::LANES);
+            const bool live = at[u].there && (!a.lens || at[u].t < __ldg(a.lens + at[u].b));
+            const T *row = static_cast<const T *>(a.x.p) + at[u].b * a.x.sb + at[u].t * a.x.st;
+#pragma unroll
+            for (int k = 0; k < H::PIECES; ++k) {
+                const int64_t c = at[u].first + (k * H::LANES + member) * H::VEC;
+                r[u][k] = live && c < a.columns ? *reinterpret_cast<const typename P::raw *>(row + c) : P::none();
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < H::AT_ONCE; ++u) {
+            float f[H::PIECES][H::VEC];
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < H::PIECES; ++k) {
+                P::get(r[u][k], f[k]);
+#pragma unroll
+                for (int e = 0; e < H::VEC; ++e) top = max(top, magnitude(f[k][e]));
+            }
+            const KeptScale scale(largest<H::LANES>(top));
+            if (!at[u].there) continue;
+#pragma unroll
+            for (int k = 0; k < H::PIECES; ++k) {
+                const int64_t c = at[u].first + (k * H::LANES + member) * H::VEC;
+                int q[H::VEC];
+#pragma unroll
+                for (int e = 0; e < H::VEC; ++e) q[e] = scale.of(f[k][e]);
+                if (c < a.columns)
+                    *reinterpret_cast<typename Kept<H::VEC>::raw *>(a.packed + at[u].row * a.columns + c) = Kept<H::VEC>::put(q);
+            }
+            if (member == 0) a.scales[at[u].row * a.blocks_of_row + at[u].first / KEPT_BLOCK] = scale.s;
+        }
+    }
+}
+
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(PACK_THREADS) unpack_kernel(const __grid_constant__ PackArgs a)
+{
+    typedef Holders<T, ALIGNED> H;
+    typedef Piece<T, H::VEC> P;
+    const int member = threadIdx.x % H::LANES;
+    const int64_t groups = (int64_t)gridDim.x * (PACK_THREADS / H::LANES);
+    for (int64_t i0 = (int64_t)blockIdx.x * (PACK_THREADS / H::LANES); i0 < a.blocks; i0 += groups * H::AT_ONCE) {
+        BlockAt at[H::AT_ONCE];
+        typename Kept<H::VEC>::raw r[H::AT_ONCE][H::PIECES];
+        float s[H::AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < H::AT_ONCE; ++u) {
+            at[u] = block_at(a, i0 + u * groups + threadIdx.x / H::LANES);
+            s[u] = at[u].there ? a.scales[at[u].row * a.blocks_of_row + at[u].first / KEPT_BLOCK] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < H::PIECES; ++k) {
+                const int64_t c = at[u].first + (k * H::LANES + member) * H::VEC;
+                r[u][k] = at[u].there && c < a.columns
+                              ? *reinterpret_cast<const typename Kept<H::VEC>::raw *>(a.packed + at[u].row * a.columns + c)
+                              : Kept<H::VEC>::none();
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < H::AT_ONCE; ++u) {
+            if (!at[u].there) continue;
+            T *row = static_cast<T *>(a.x.p) + at[u].b * a.x.sb + at[u].t * a.x.st;
+#pragma unroll
+            for (int k = 0; k < H::PIECES; ++k) {
+                const int64_t c = at[u].first + (k * H::LANES + member) * H::VEC;
+                int q[H::VEC];
+                float f[H::VEC];
+                Kept<H::VEC>::get(r[u][k], q);
+#pragma unroll
+                for (int e = 0; e < H::VEC; ++e) f[e] = kept_value(q[e], s[u]);
+                if (c < a.columns) *reinterpret_cast<typename P::raw *>(row + c) = P::put(f);
+            }
+        }
+    }
+}
+
+template <typename T, bool ALIGNED>
+static gs_status launch(const PackArgs &a, bool pack, cudaStream_t st)
+{
+    typedef Holders<T, ALIGNED> H;
+    const int64_t each = (int64_t)(PACK_THREADS / H::LANES) * H::AT_ONCE, blocks = (a.blocks + each - 1) / each;
+    const int64_t most = (int64_t)sm_count() * PACK_BLOCKS * 4;
+    const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+    if (pack) pack_kernel<T, ALIGNED><<<grid, PACK_THREADS, 0, st>>>(a);
+    else unpack_kernel<T, ALIGNED><<<grid, PACK_THREADS, 0, st>>>(a);
+    GS_CUDA_TRY(cudaGetLastError());
+    return GS_OK;
+}
+
+static gs_status run(int32_t dtype, const NormRows &x, const int32_t *lens, int64_t batch, int64_t length, int64_t columns, int8_t *packed,
+                     float *scales, bool pack, cudaStream_t st)
+{
+    PackArgs a = {};
+    a.x = x;
+    a.packed = packed;
+    a.scales = scales;
+    a.lens = lens;
+    a.rows = batch * length;
+    a.length = length;
+    a.columns = columns;
+    a.blocks_of_row = (columns + KEPT_BLOCK - 1) / KEPT_BLOCK;
+    a.blocks = a.rows * a.blocks_of_row;
+    a.by_blocks = Divider(a.blocks_of_row);
+    a.by_length = Divider(length);
+    const int64_t es = (int64_t)size_of(dtype);
+    const bool aligned = columns * es % 16 == 0 && (uintptr_t)x.p % 16 == 0 && (x.sb * es | x.st * es) % 16 == 0 && (uintptr_t)packed % 8 == 0;
+    return with_type(dtype, [&](auto t) {
+        typedef decltype(t) T;
+        return aligned ? launch<T, true>(a, pack, st) : launch<T, false>(a, pack, st);
+    });
+}
+
+gs_status checkpoint_pack(int32_t dtype, const NormRows &x, const int32_t *lens, int64_t batch, int64_t length, int64_t columns,
+                          int8_t *packed, float *scales, cudaStream_t st)
+{
+    return run(dtype, x, lens, batch, length, columns, packed, scales, true, st);
+}
+
+static gs_status entry(int32_t dtype, const void *x, int64_t rows, int64_t columns, int64_t row_stride, const int8_t *packed,
+                       const float *scales, bool pack, void *stream)
+{
+    if (!known_type(dtype)) return bad("dtype must be GS_TABLE_F32, GS_TABLE_F16 or GS_TABLE_BF16");
+    if (rows < 0 || columns < 0) return bad("negative number of rows or columns");
+    if (rows > ((int64_t)1 << 40) || columns > 0x7FFFFFFF || (columns > 0 && rows > ((int64_t)1 << 46) / columns)) {
+        set_error("checkpoints of up to 2^40 rows, 2^31 - 1 columns and 2^46 values are supported");
+        return GS_ERR_UNSUPPORTED;
+    }
+    if (rows == 0 || columns == 0) return GS_OK;
+    if (!x || !packed || !scales) return bad("null pointer");
+    if ((uintptr_t)x % size_of(dtype) || (uintptr_t)scales % 4) return bad("tensor not aligned to its element size");
+    if (!pack && rows > 1 && row_stride == 0) return bad("an output has a zero stride");
+    const NormRows r = {const_cast<void *>(x), 0, row_stride};
+    return run(dtype, r, nullptr, 1, rows, columns, const_cast<int8_t *>(packed), const_cast<float *>(scales), pack, (cudaStream_t)stream);
+}
+
+}  // namespace gs
+
+using namespace gs;
+
+extern "C" {
+
+gs_status gs_checkpoint_pack(int32_t dtype, const void *d_x, int64_t rows, int64_t columns, int64_t row_stride, int8_t *d_packed,
+                             float *d_scales, void *stream)
+{
+    return entry(dtype, d_x, rows, columns, row_stride, d_packed, d_scales, true, stream);
+}
+
+gs_status gs_checkpoint_unpack(int32_t dtype, const int8_t *d_packed, const float *d_scales, int64_t rows, int64_t columns,
+                               int64_t row_stride, void *d_x, void *stream)
+{
+    return entry(dtype, d_x, rows, columns, row_stride, d_packed, d_scales, false, stream);
+}
+
+}  // extern "C"

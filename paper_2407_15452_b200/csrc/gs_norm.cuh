@@ -1,0 +1,156 @@
+// Layer norm: what the forward and the backward kernels share.
+//
+// A row is held by a team, the lanes of a part of a warp or all threads of a block, in registers from its only read to its only
+// write: thread i of the team has NV pieces of VEC neighbouring columns, piece v at column (v * team + i) * VEC.  A thread's
+// columns are the same in every row, so weights, and in the backward pass the sums for their gradients, stay in registers while the team goes
+// through its rows; the next row's values are on their way while the present one is summed.
+#pragma once
+
+#include "gs_layers.cuh"
+
+namespace gs {
+
+static constexpr int NORM_THREADS = 256;              // of blocks that hold several teams
+static constexpr int NORM_MOST_COLUMNS = 16384;
+static constexpr int NORM_PARTIALS = 8;               // blocks of a backward launch per SM, at most
+
+struct NormRows {
+    void *p;
+    int64_t sb, st;                                   // strides in elements: sequence, position
+};
+
+struct NormArgs {
+    NormRows x, y, dy, dx;
+    const void *weight, *bias;
+    float *stats, *scales, *partial;
+    int8_t *packed;
+    const int32_t *lens;
+    Divider by_length;
+    int64_t rows, length;
+    int32_t columns, kept_blocks;                     // kept_blocks = ceil(columns / KEPT_BLOCK)
+    int32_t weight_f32;
+    float eps;
+};
+
+// A row's place: `there`: it exists; `live`: its position is valid
+struct RowAt {
+    int64_t row, b, t;
+    bool there, live;
+};
+__device__ __forceinline__ RowAt row_at(const NormArgs &a, int64_t row)
+{
+    RowAt r;
+    r.row = row;
+    r.there = row < a.rows;
+    r.b = r.there ? a.by_length.of(row) : 0;
+    r.t = r.there ? row - r.b * a.length : 0;
+    r.live = r.there && (!a.lens || r.t < __ldg(a.lens + r.b));
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ T *row_of(const NormRows &t, const RowAt &r)
+{
+    return static_cast<T *>(t.p) + r.b * t.sb + r.t * t.st;
+}
+
+// The shape of a team.  LANES 8, 16, 32: part of a warp; 0: the block, of up to 512 threads.  FAR: the rows' weights (and sums)
+// do not fit the threads' registers: weights are read again for every row, sums live in shared memory.
+template <int VEC_, int NV_, int LANES_, bool FAR_ = false>
+struct Team {
+    static constexpr int VEC = VEC_, NV = NV_, LANES = LANES_;
+    static constexpr bool FAR = FAR_, BLOCK = LANES_ == 0;
+    static constexpr int GROUP = BLOCK ? 32 : LANES;                  // lanes that reduce by shuffles
+    static constexpr int KEPT_LANES = GROUP < KEPT_BLOCK / VEC ? GROUP : KEPT_BLOCK / VEC;   // that hold a scale's columns
+    static constexpr int THREADS = BLOCK ? 512 : NORM_THREADS;        // at most
+    static __device__ __forceinline__ int size() { return BLOCK ? blockDim.x : LANES; }
+    static __device__ __forceinline__ int member() { return BLOCK ? threadIdx.x : threadIdx.x % LANES; }
+    static __device__ __forceinline__ int teams() { return BLOCK ? 1 : NORM_THREADS / LANES; }
+    static __device__ __forceinline__ int index() { return BLOCK ? 0 : threadIdx.x / LANES; }
+    static __device__ __forceinline__ int column(int v) { return (v * size() + member()) * VEC; }
+};
+
+// Sums over a team, two at a time.  The warps of a block leave theirs in one of two places in turn, so that one barrier a sum is enough:
+// a place is written again two sums later, when every thread has met the barrier in between.
+struct PairSums {
+    float2 (*place)[16];
+    int turn;
+};
+template <typename S>
+__device__ __forceinline__ float2 team_sum(float2 v, PairSums &sums)
+{
+#pragma unroll
+    for (int o = S::GROUP / 2; o; o >>= 1) {
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    }
+    if (!S::BLOCK) return v;
+    float2 *place = sums.place[sums.turn];
+    sums.turn ^= 1;
+    if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
+    __syncthreads();
+    float2 all = place[0];
+    for (int w = 1; w < (int)blockDim.x >> 5; ++w) {
+        all.x += place[w].x;
+        all.y += place[w].y;
+    }
+    return all;
+}
+
+// the columns [c, c + VEC) of a row; all of them lie in the row or none (VEC > 1 only where columns % VEC == 0)
+template <typename T, int VEC>
+__device__ __forceinline__ typename Piece<T, VEC>::raw load_piece(const T *row, int c, int columns, bool live)
+{
+    if (live && c < columns) return *reinterpret_cast<const typename Piece<T, VEC>::raw *>(row + c);
+    return Piece<T, VEC>::none();
+}
+
+template <typename T> __device__ __forceinline__ float vector_at(const void *p, int32_t f32, int c)
+{
+    return f32 ? static_cast<const float *>(p)[c] : to_float(static_cast<const T *>(p)[c]);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void vector_piece(const void *p, int32_t f32, int c, int columns, float without, float (&f)[VEC])
+{
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[e] = p && c < columns ? vector_at<T>(p, f32, c + e) : without;
+}
+
+// Calls launch(Team, threads, shared) with the team for rows of `columns` values.  Teams within a warp hold up to 16 columns a thread and up
+// to 512 in all (joins by shuffles alone); a block's 16 columns a thread up to 8192, 32 beyond.
+template <typename T, typename F>
+static gs_status with_team(int columns, bool aligned, F &&launch)
+{
+    constexpr int W = Wide<T>::N;
+    auto block = [&](int per_thread) { return (columns + 32 * per_thread - 1) / (32 * per_thread) * 32; };
+    if (aligned) {
+        if (columns <= 8 * W) return launch(Team<W, 1, 8>(), NORM_THREADS);
+        if (columns <= 16 * W) return launch(Team<W, 1, 16>(), NORM_THREADS);
+        if (columns <= 32 * W) return launch(Team<W, 1, 32>(), NORM_THREADS);
+        if (columns <= 64 * W) return launch(Team<W, 2, 32>(), NORM_THREADS);
+        if (W == 4 && columns <= 512) return launch(Team<W, W == 4 ? 4 : 2, 32>(), NORM_THREADS);
+        if (columns <= 8192) return launch(Team<W, 16 / W, 0>(), block(16));
+        return launch(Team<W, 32 / W, 0, true>(), block(32));
+    }
+    if (columns <= 32) return launch(Team<1, 1, 32>(), NORM_THREADS);
+    if (columns <= 128) return launch(Team<1, 4, 32>(), NORM_THREADS);
+    if (columns <= 512) return launch(Team<1, 16, 32>(), NORM_THREADS);
+    if (columns <= 8192) return launch(Team<1, 16, 0>(), block(16));
+    return launch(Team<1, 32, 0, true>(), block(32));
+}
+
+template <typename F>
+static gs_status with_type(int32_t dtype, F &&f)
+{
+    if (dtype == GS_TABLE_F32) return f(float());
+    if (dtype == GS_TABLE_F16) return f(__half());
+    return f(__nv_bfloat16());
+}
+
+// gs_norm_forward.cu, gs_norm_backward.cu
+gs_status norm_forward(const NormArgs &a, int32_t dtype, bool aligned, cudaStream_t st);
+gs_status norm_backward(const NormArgs &a, int32_t dtype, bool aligned, void *dweight, void *dbias, cudaStream_t st);
+// gs_checkpoint.cu
+gs_status checkpoint_pack(int32_t dtype, const NormRows &x, const int32_t *lens, int64_t batch, int64_t length, int64_t columns,
+                          int8_t *packed, float *scales, cudaStream_t st);
+
+}  // namespace gs

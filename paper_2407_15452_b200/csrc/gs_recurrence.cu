@@ -1,0 +1,524 @@
+// Gated linear recurrence along the positions of a sequence, and its gradient.
+//
+//   a_t = sigmoid(z_t), h_t = a_t h_(t-1) + (1 - a_t) x_t;   g_t = dout_t + r_(t+1), r_t = a_t g_t,
+//   dx_t = (1 - a_t) g_t, dz_t = a_t (1 - a_t) (h_(t-1) - x_t) g_t.
+//
+// Over a stretch of positions the state is an affine function of the state before it, h_end = P h_start + B with
+// P the product of the a_t, and r_start = P r_end + R with the same P, so stretches can be computed side by side and joined.
+// A warp has a stretch of up to 16 positions of 32 (or 64) channels, a block 8 stretches one after another, SPAN positions,
+// and sequences longer than that are a cluster's: its blocks take neighbouring spans, exchange the (P, B) of theirs through
+// distributed shared memory and go on to the next window of spans with the state that all of them know.  Every input is read once and every
+// output written once; the joins are made in a fixed order.  The backward pass reads the state before each span, which the
+// forward pass left, computes h again (one stream fewer than reading it, and in fp32) and joins only r.
+#include <math.h>
+
+#include "gs_layers.cuh"
+
+namespace gs {
+
+static constexpr int STEPS = 16, WARPS = 8, SPAN = STEPS * WARPS, MOST_BLOCKS = 8;
+
+struct ScanTensor {
+    void *p;
+    int64_t sb, st;                       // strides in elements: sequence, position
+};
+
+struct ScanArgs {
+    ScanTensor gate, x, out, dout, dgate, dx;
+    const float *h0, *dfinal;
+    float *final_state, *dh0, *states;
+    const int32_t *lens;
+    int64_t batch, channels, chains;      // chains = batch * slabs
+    int32_t length, slabs, spans;         // slabs of 32 * V channels; spans = ceil(length / SPAN)
+    int32_t stretches;                    // warps that share a span
+    int32_t blocks;                       // blocks of a cluster
+};
+
+// V neighbouring channels of a lane as they travel: a register each
+template <typename T, int V> struct Lane;
+template <> struct Lane<float, 1> {
+    typedef float raw;
+    static __device__ __forceinline__ void get(raw r, float (&f)[1]) { f[0] = r; }
+    static __device__ __forceinline__ raw put(const float (&f)[1]) { return f[0]; }
+};
+template <typename T> struct Lane<T, 1> {
+    typedef T raw;
+    static __device__ __forceinline__ void get(raw r, float (&f)[1]) { f[0] = to_float(r); }
+    static __device__ __forceinline__ raw put(const float (&f)[1]) { return from_float<T>(f[0]); }
+};
+template <typename T> struct Lane<T, 2> {
+    typedef uint32_t raw;
+    static __device__ __forceinline__ void get(raw r, float (&f)[2]) { unpack2<T>(r, f[0], f[1]); }
+    static __device__ __forceinline__ raw put(const float (&f)[2]) { return pack2<T>(f[0], f[1]); }
+};
+template <typename R> __device__ __forceinline__ R zero_raw() { return R(0.0f); }
+template <> __device__ __forceinline__ uint32_t zero_raw<uint32_t>() { return 0u; }
+
+// The gate as the smaller of a and 1 - a, with the sign set where that is 1 - a: both are then at hand with their full
+// relative precision (1 - a from a rounded a near 1 has none), and so are products and interpolations with them.
+__device__ __forceinline__ float gate_of(float z)
+{
+    const float e = expf(-fabsf(z));
+    const float m = __fdividef(e, 1.0f + e);
+    return z >= 0.0f ? -m : m;
+}
+// a * p
+__device__ __forceinline__ float keep(float gate, float p)
+{
+    const float m = fabsf(gate);
+    return signbit(gate) ? fmaf(-m, p, p) : m * p;
+}
+// a * h + (1 - a) * x, from the end that the gate is nearer to
+__device__ __forceinline__ float advance(float gate, float h, float x)
+{
+    const bool near_h = signbit(gate);
+    const float from = near_h ? h : x, to = near_h ? x : h;
+    return fmaf(fabsf(gate), to - from, from);
+}
+
+struct Place {                            // what a warp works on
+    int64_t b, c;                         // sequence; first channel of the lane
+    bool on;                              // the lane has a channel, and the warp a chain
+    int len;                              // valid positions
+};
+
+template <int V>
+__device__ __forceinline__ Place place_of(const ScanArgs &a, int64_t chain, int lane)
+{
+    Place p;
+    p.on = chain < a.chains;
+    p.b = p.on ? chain / a.slabs : 0;
+    p.c = (chain - p.b * a.slabs) * (32 * V) + lane * V;
+    p.on = p.on && p.c < a.channels;
+    p.len = a.lens ? min(max(__ldg(a.lens + p.b), 0), a.length) : a.length;
+    return p;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ typename Lane<T, V>::raw *at(const ScanTensor &t, const Place &p, int pos)
+{
+    return reinterpret_cast<typename Lane<T, V>::raw *>(static_cast<T *>(t.p) + p.b * t.sb + pos * t.st + p.c);
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// stores a pair into the shared memory of another block of the cluster, at the place that `local` has in this one
+__device__ __forceinline__ void store_remote(const float2 *local, uint32_t rank, float2 v)
+{
+    uint32_t there;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
+}
+
+// Joins of a window.  `own`: (P, B) of this warp's stretch.  Returns the carry into the stretch, and moves `carry` over the whole
+// window.  BACK: the chain runs from the last stretch to the first.
+template <int V, bool CLUSTER, bool BACK>
+struct Joins {
+    float2 (*part)[WARPS][32 * V];                   // [2 by parity][stretch][channel]: of this block
+    float2 (*span)[MOST_BLOCKS][32 * V];             // [2 by parity][rank][channel]: of the cluster's blocks
+    int stretches, blocks, rank, warp, lane, first;  // first: index of the block's warp that has this chain's first stretch
+    int parity;
+
+    __device__ __forceinline__ void publish(const float (&p)[V], const float (&b)[V])
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) part[parity][first + warp][v * 32 + lane] = make_float2(p[v], b[v]);
+    }
+    __device__ __forceinline__ void join(float (&carry)[V], float (&into)[V])
+    {
+        __syncthreads();
+        float2 all[V];
+        if (CLUSTER) {
+            // the block's own span, which every warp joins for itself and one of them hands to each block
+#pragma unroll
+            for (int v = 0; v < V; ++v) all[v] = make_float2(1.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) {
+                const int w = BACK ? WARPS - 1 - i : i;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float2 s = part[parity][w][v * 32 + lane];
+                    all[v].y = fmaf(s.x, all[v].y, s.y);
+                    all[v].x *= s.x;
+                }
+            }
+            if (warp < blocks)
+#pragma unroll
+                for (int v = 0; v < V; ++v) store_remote(&span[parity][rank][v * 32 + lane], warp, all[v]);
+            cluster_arrive();
+            cluster_wait();
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) into[v] = carry[v];
+        if (CLUSTER) {
+            for (int i = 0; i < blocks; ++i) {
+                const int k = BACK ? blocks - 1 - i : i;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float2 s = span[parity][k][v * 32 + lane];
+                    if (k == rank) into[v] = carry[v];
+                    carry[v] = fmaf(s.x, carry[v], s.y);
+                }
+            }
+        }
+        const int before = BACK ? stretches - 1 - warp : warp;
+        for (int i = 0; i < before; ++i) {
+            const int w = first + (BACK ? stretches - 1 - i : i);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float2 s = part[parity][w][v * 32 + lane];
+                into[v] = fmaf(s.x, into[v], s.y);
+            }
+        }
+        parity ^= 1;
+    }
+};
+
+template <typename T, int V, bool CLUSTER>
+__global__ void __launch_bounds__(32 * WARPS) scan_forward_kernel(const __grid_constant__ ScanArgs a)
+{
+    typedef typename Lane<T, V>::raw raw;
+    __shared__ float2 part[CLUSTER ? 2 : 1][WARPS][32 * V];
+    __shared__ float2 span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32 * V];
+    const int lane = threadIdx.x & 31, index = threadIdx.x >> 5;
+    const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
+    const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
+    const int64_t chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * groups + group;
+    const Place p = place_of<V>(a, chain, lane);
+    __syncwarp();
+    if (CLUSTER) cluster_arrive();                      // completed by the wait before the first remote store
+
+    float carry[V], into[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry[v] = a.h0 && p.on ? a.h0[p.b * a.channels + p.c + v] : 0.0f;
+    Joins<V, CLUSTER, false> joins = {reinterpret_cast<float2(*)[WARPS][32 * V]>(part),
+                                      reinterpret_cast<float2(*)[MOST_BLOCKS][32 * V]>(span),
+                                      a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
+    if (CLUSTER) cluster_wait();
+
+    for (int k0 = 0; k0 < a.spans; k0 += a.blocks) {
+        const int k = k0 + rank;
+        const int t0 = k * SPAN + warp * STEPS;
+        const int rows = p.on ? min(max(a.length - t0, 0), STEPS) : 0, valid = min(rows, max(p.len - t0, 0));
+        raw z[STEPS], x[STEPS];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (s < valid) {
+                z[s] = *at<T, V>(a.gate, p, t0 + s);
+                x[s] = *at<T, V>(a.x, p, t0 + s);
+            }
+        float h[STEPS][V], pr[STEPS][V], hn[V], pn[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) hn[v] = 0.0f, pn[v] = 1.0f;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            if (s < valid) {
+                float zf[V], xf[V];
+                Lane<T, V>::get(z[s], zf);
+                Lane<T, V>::get(x[s], xf);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float gate = gate_of(zf[v]);
+                    hn[v] = advance(gate, hn[v], xf[v]);
+                    pn[v] = keep(gate, pn[v]);
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[s][v] = hn[v], pr[s][v] = pn[v];
+        }
+        if (CLUSTER || a.stretches > 1) {
+            joins.publish(pn, hn);
+            joins.join(carry, into);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) into[v] = carry[v];
+        }
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (s < rows) {
+                float o[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) o[v] = s < valid ? fmaf(pr[s][v], into[v], h[s][v]) : 0.0f;
+                *at<T, V>(a.out, p, t0 + s) = Lane<T, V>::put(o);
+            }
+        if (p.on && warp == a.stretches - 1 && k < a.spans) {
+            float *to = k < a.spans - 1 ? (a.states ? a.states + (p.b * (a.spans - 1) + k) * a.channels : nullptr)
+                                        : (a.final_state ? a.final_state + p.b * a.channels : nullptr);
+            if (to)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    to[p.c + v] = fmaf(pn[v], into[v], hn[v]);
+        }
+    }
+}
+
+template <typename T, int V, bool CLUSTER>
+__global__ void __launch_bounds__(32 * WARPS) scan_backward_kernel(const __grid_constant__ ScanArgs a)
+{
+    typedef typename Lane<T, V>::raw raw;
+    __shared__ float2 part[CLUSTER ? 2 : 1][WARPS][32 * V];
+    __shared__ float2 span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32 * V];
+    __shared__ float ahead[CLUSTER ? 2 : 1][WARPS][32 * V];          // B of the stretches, for h
+    const int lane = threadIdx.x & 31, index = threadIdx.x >> 5;
+    const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
+    const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
+    const int64_t chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * groups + group;
+    const Place p = place_of<V>(a, chain, lane);
+    __syncwarp();
+    if (CLUSTER) cluster_arrive();
+
+    float carry[V], into[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        carry[v] = a.dfinal && p.on ? a.dfinal[p.b * a.channels + p.c + v] : 0.0f;
+    Joins<V, CLUSTER, true> joins = {reinterpret_cast<float2(*)[WARPS][32 * V]>(part),
+                                     reinterpret_cast<float2(*)[MOST_BLOCKS][32 * V]>(span),
+                                     a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
+    if (CLUSTER) cluster_wait();
+
+    for (int k0 = (a.spans - 1) / a.blocks * a.blocks; k0 >= 0; k0 -= a.blocks) {
+        const int k = k0 + rank;
+        const int t0 = k * SPAN + warp * STEPS;
+        const int rows = p.on ? min(max(a.length - t0, 0), STEPS) : 0, valid = min(rows, max(p.len - t0, 0));
+        raw z[STEPS], x[STEPS], g[STEPS];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (s < valid) {
+                z[s] = *at<T, V>(a.gate, p, t0 + s);
+                x[s] = *at<T, V>(a.x, p, t0 + s);
+                g[s] = a.dout.p ? *at<T, V>(a.dout, p, t0 + s) : zero_raw<raw>();
+            }
+        // the state before the block's span
+        float h[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            h[v] = 0.0f;
+            if (p.on && k < a.spans) {
+                if (k > 0) h[v] = a.states[(p.b * (a.spans - 1) + k - 1) * a.channels + p.c + v];
+                else if (a.h0) h[v] = a.h0[p.b * a.channels + p.c + v];
+            }
+        }
+        float gate[STEPS][V], hn[V], pn[V], rn[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) hn[v] = 0.0f, pn[v] = 1.0f, rn[v] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (s < valid) {
+                float zf[V], xf[V], gf[V];
+                Lane<T, V>::get(z[s], zf);
+                Lane<T, V>::get(x[s], xf);
+                Lane<T, V>::get(g[s], gf);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    gate[s][v] = gate_of(zf[v]);
+                    hn[v] = advance(gate[s][v], hn[v], xf[v]);
+                    pn[v] = keep(gate[s][v], pn[v]);
+                    rn[v] = fmaf(pn[v], gf[v], rn[v]);
+                }
+            }
+        if (CLUSTER || a.stretches > 1) {
+            const int parity = joins.parity;
+            joins.publish(pn, rn);
+#pragma unroll
+            for (int v = 0; v < V; ++v) ahead[parity][index][v * 32 + lane] = hn[v];
+            joins.join(carry, into);
+            for (int i = 0; i < warp; ++i)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const int w = group * a.stretches + i;
+                    h[v] = fmaf(part[parity][w][v * 32 + lane].x, h[v], ahead[parity][w][v * 32 + lane]);
+                }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) into[v] = carry[v];
+        }
+        float d[STEPS][V];                                           // h_(t-1) - x_t
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (s < valid) {
+                float xf[V];
+                Lane<T, V>::get(x[s], xf);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    d[s][v] = h[v] - xf[v];
+                    h[v] = advance(gate[s][v], h[v], xf[v]);
+                }
+            }
+#pragma unroll
+        for (int s = STEPS - 1; s >= 0; --s)
+            if (s < rows) {
+                float dx[V], dz[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) dx[v] = dz[v] = 0.0f;
+                if (s < valid) {
+                    float gf[V];
+                    Lane<T, V>::get(g[s], gf);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const float full = gf[v] + into[v], m = fabsf(gate[s][v]);
+                        const float near = m * full, far = fmaf(-m, full, full);
+                        const bool open = signbit(gate[s][v]);
+                        dx[v] = open ? near : far;
+                        into[v] = open ? far : near;
+                        dz[v] = d[s][v] * (m * far);
+                    }
+                }
+                *at<T, V>(a.dx, p, t0 + s) = Lane<T, V>::put(dx);
+                *at<T, V>(a.dgate, p, t0 + s) = Lane<T, V>::put(dz);
+            }
+        if (a.dh0 && p.on && k == 0 && warp == 0)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                a.dh0[p.b * a.channels + p.c + v] = into[v];
+    }
+}
+
+template <typename T, int V>
+static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
+{
+    ScanArgs a = args;
+    a.slabs = (int32_t)((a.channels + 32 * V - 1) / (32 * V));
+    a.chains = a.batch * a.slabs;
+    a.spans = (a.length + SPAN - 1) / SPAN;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr = {};
+    int64_t grid;
+    if (a.spans > 1) {
+        // as few windows as a cluster of MOST_BLOCKS allows, and no more blocks than these need
+        const int windows = (a.spans + MOST_BLOCKS - 1) / MOST_BLOCKS;
+        a.blocks = (a.spans + windows - 1) / windows;
+        a.stretches = WARPS;
+        grid = a.chains * a.blocks;
+        cfg.blockDim = dim3(32 * WARPS);
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)a.blocks;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+    } else {
+        // several chains a block where one needs few warps
+        a.blocks = 1;
+        a.stretches = a.length > STEPS ? (a.length + STEPS - 1) / STEPS : 1;
+        const int groups = WARPS / a.stretches > 0 ? WARPS / a.stretches : 1;
+        grid = (a.chains + groups - 1) / groups;
+        cfg.blockDim = dim3(32 * groups * a.stretches);
+    }
+    if (grid > 0x7FFFFFFF) {
+        set_error("a recurrence of %lld blocks exceeds one launch", (long long)grid);
+        return GS_ERR_UNSUPPORTED;
+    }
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.stream = st;
+    if (backward)
+        GS_CUDA_TRY(cudaLaunchKernelEx(&cfg, a.spans > 1 ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>, a));
+    else
+        GS_CUDA_TRY(cudaLaunchKernelEx(&cfg, a.spans > 1 ? scan_forward_kernel<T, V, true> : scan_forward_kernel<T, V, false>, a));
+    return GS_OK;
+}
+
+static gs_status check(const gs_recurrence_config *c, ScanArgs *a)
+{
+    if (!c) return bad("config is NULL");
+    if (!known_type(c->dtype)) return bad("dtype must be GS_TABLE_F32, GS_TABLE_F16 or GS_TABLE_BF16");
+    if (c->batch < 0 || c->length < 0 || c->channels <= 0) return bad("negative batch or length, or no channels");
+    if (c->length > (1 << 30) || c->channels > ((int64_t)1 << 31) || (c->batch > 0 && c->channels > ((int64_t)1 << 40) / c->batch)) {
+        set_error("recurrences of up to 2^30 positions, 2^31 channels and 2^40 states are supported");
+        return GS_ERR_UNSUPPORTED;
+    }
+    *a = ScanArgs{};
+    a->batch = c->batch;
+    a->channels = c->channels;
+    a->length = c->length;
+    a->lens = c->d_lens;
+    return GS_OK;
+}
+
+static ScanTensor tensor(const void *p, const int64_t (&stride)[2])
+{
+    return {const_cast<void *>(p), stride[0], stride[1]};
+}
+
+// an empty sequence ends with the state that it starts with
+static gs_status copy_states(const float *from, float *to, int64_t n, cudaStream_t st)
+{
+    if (!to || to == from) return GS_OK;
+    if (from) GS_CUDA_TRY(cudaMemcpyAsync(to, from, n * sizeof(float), cudaMemcpyDeviceToDevice, st));
+    else GS_CUDA_TRY(cudaMemsetAsync(to, 0, n * sizeof(float), st));
+    return GS_OK;
+}
+
+static gs_status run(ScanArgs &a, int32_t dtype, const ScanTensor *const *t, int n, int outputs, bool backward, cudaStream_t st)
+{
+    const uintptr_t es = size_of(dtype);
+    bool pairs = dtype != GS_TABLE_F32 && a.channels % 2 == 0;
+    for (int i = 0; i < n; ++i) {
+        if (!t[i]->p) return bad("null pointer");
+        if ((uintptr_t)t[i]->p % es) return bad("tensor not aligned to its element size");
+        if (i < outputs && ((a.batch > 1 && t[i]->sb == 0) || (a.length > 1 && t[i]->st == 0)))
+            return bad("an output has a zero stride");
+        pairs = pairs && (uintptr_t)t[i]->p % 4 == 0 && (t[i]->sb | t[i]->st) % 2 == 0;
+    }
+    if (dtype == GS_TABLE_F32) return launch<float, 1>(a, backward, st);
+    if (dtype == GS_TABLE_F16) return pairs ? launch<__half, 2>(a, backward, st) : launch<__half, 1>(a, backward, st);
+    return pairs ? launch<__nv_bfloat16, 2>(a, backward, st) : launch<__nv_bfloat16, 1>(a, backward, st);
+}
+
+}  // namespace gs
+
+using namespace gs;
+
+extern "C" {
+
+int64_t gs_recurrence_states(const gs_recurrence_config *cfg)
+{
+    ScanArgs a;
+    if (check(cfg, &a) != GS_OK) return -1;
+    return a.length > 0 ? a.batch * a.channels * ((a.length - 1) / SPAN) : 0;
+}
+
+gs_status gs_recurrence_forward(const gs_recurrence_config *cfg, const void *d_gate, const void *d_x, const float *d_h0,
+                                void *d_out, float *d_final, float *d_states, void *stream)
+{
+    ScanArgs a;
+    gs_status s = check(cfg, &a);
+    if (s != GS_OK || a.batch == 0) return s;
+    a.h0 = d_h0;
+    a.final_state = d_final;
+    a.states = d_states;
+    if (a.length == 0) return copy_states(d_h0, d_final, a.batch * a.channels, (cudaStream_t)stream);
+    a.gate = tensor(d_gate, cfg->gate_stride);
+    a.x = tensor(d_x, cfg->x_stride);
+    a.out = tensor(d_out, cfg->out_stride);
+    const ScanTensor *all[3] = {&a.out, &a.gate, &a.x};
+    return run(a, cfg->dtype, all, 3, 1, false, (cudaStream_t)stream);
+}
+
+gs_status gs_recurrence_backward(const gs_recurrence_config *cfg, const void *d_dout, const float *d_dfinal,
+                                 const void *d_gate, const void *d_x, const float *d_h0, const float *d_states,
+                                 void *d_dgate, void *d_dx, float *d_dh0, void *stream)
+{
+    ScanArgs a;
+    gs_status s = check(cfg, &a);
+    if (s != GS_OK || a.batch == 0) return s;
+    a.h0 = d_h0;
+    a.dfinal = d_dfinal;
+    a.dh0 = d_dh0;
+    a.states = const_cast<float *>(d_states);
+    if (a.length == 0) return copy_states(d_dfinal, d_dh0, a.batch * a.channels, (cudaStream_t)stream);
+    if (a.length > SPAN && !d_states) return bad("d_states is NULL");
+    a.gate = tensor(d_gate, cfg->gate_stride);
+    a.x = tensor(d_x, cfg->x_stride);
+    a.dgate = tensor(d_dgate, cfg->dgate_stride);
+    a.dx = tensor(d_dx, cfg->dx_stride);
+    a.dout = tensor(d_dout, cfg->dout_stride);
+    const ScanTensor *all[5] = {&a.dgate, &a.dx, &a.gate, &a.x, &a.dout};
+    return run(a, cfg->dtype, all, d_dout ? 5 : 4, 2, true, (cudaStream_t)stream);
+}
+
+}  // extern "C"
