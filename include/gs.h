@@ -703,7 +703,7 @@ GS_API gs_status gs_layer_norm_backward(const gs_layer_norm_config *cfg, const v
  * d_dout, d_dfinal NULL: zeros; d_dh0 NULL: not wanted.
  * Tensors have type dtype, any strides (in elements) over batch and position, contiguous channels; zero strides of inputs, overlaps
  * and repeatability as above (but for d_final = d_h0).  Products and sums are fp32.  What follows an infinity in x or a state is infinite or NaN.
- * Supported: length up to 2^30, 2^40 values of a batch entry's position (batch x channels).  Errors: as above.
+ * Supported: lengths and channels up to 2^30, 2^40 states (batch x channels).  Errors: as above.
  */
 typedef struct gs_recurrence_config {
     int32_t dtype;

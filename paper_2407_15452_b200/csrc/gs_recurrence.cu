@@ -30,7 +30,7 @@ struct ScanArgs {
     const int32_t *lens;
     int64_t batch, channels, chains;      // chains = batch * slabs
     int32_t length, slabs, spans;         // slabs of 32 * V channels; spans = ceil(length / SPAN)
-    int32_t stretches;                    // warps that share a span
+    int32_t stretches, steps;             // warps that share a span, positions of each
     int32_t blocks;                       // blocks of a cluster
 };
 
@@ -54,31 +54,32 @@ template <typename T> struct Lane<T, 2> {
 template <typename R> __device__ __forceinline__ R zero_raw() { return R(0.0f); }
 template <> __device__ __forceinline__ uint32_t zero_raw<uint32_t>() { return 0u; }
 
-// The gate as the smaller of a and 1 - a, with the sign set where that is 1 - a: both are then at hand with their full
-// relative precision (1 - a from a rounded a near 1 has none), and so are products and interpolations with them.
-__device__ __forceinline__ float gate_of(float z)
+// 1 - a = 1 / (1 + exp(z)), to a few units of its own last place however small it is: from a rounded a it would have no
+// digits left where a channel remembers for long.  exp(z) in fp32 has its argument's product with log2(e) rounded, |z| 2^-24
+// of the result, which tensors of 16 bits do not see; fp32 tensors take the library's.
+template <typename T> __device__ __forceinline__ float exp_of(float z) { return __expf(z); }
+template <> __device__ __forceinline__ float exp_of<float>(float z) { return expf(z); }
+template <typename T> __device__ __forceinline__ float shut_of(float z) { return __fdividef(1.0f, 1.0f + exp_of<T>(z)); }
+
+// a h + (1 - a) x from u = 1 - a: h - u h is rounded once, so a state that is kept for long loses nothing to a rounded a, and
+// one that is given up (u = 1) leaves nothing behind
+__device__ __forceinline__ float advance(float u, float h, float x) { return fmaf(u, x, fmaf(-u, h, h)); }
+
+// What the backward pass keeps of a gate: the smaller of a and 1 - a, with the sign bit set where that is a.  Both factors of a (1 - a) are then
+// at hand with all their digits, also where one of them is nearly 1.
+template <typename T>
+__device__ __forceinline__ float gate_of(float z, float &u)
 {
-    const float e = expf(-fabsf(z));
-    const float m = __fdividef(e, 1.0f + e);
-    return z >= 0.0f ? -m : m;
-}
-// a * p
-__device__ __forceinline__ float keep(float gate, float p)
-{
-    const float m = fabsf(gate);
-    return signbit(gate) ? fmaf(-m, p, p) : m * p;
-}
-// a * h + (1 - a) * x, from the end that the gate is nearer to
-__device__ __forceinline__ float advance(float gate, float h, float x)
-{
-    const bool near_h = signbit(gate);
-    const float from = near_h ? h : x, to = near_h ? x : h;
-    return fmaf(fabsf(gate), to - from, from);
+    const float e = exp_of<T>(-fabsf(z)), larger = __fdividef(1.0f, 1.0f + e), m = e * larger;
+    const bool shut = signbit(z);
+    u = shut ? larger : m;
+    return shut ? -m : m;
 }
 
 struct Place {                            // what a warp works on
-    int64_t b, c;                         // sequence; first channel of the lane
-    bool on;                              // the lane has a channel, and the warp a chain
+    int64_t b;                            // sequence
+    uint32_t c;                           // the lane's first channel
+    bool on, writes;                      // the warp has a chain; the lane has a channel (one that has none reads another's)
     int len;                              // valid positions
 };
 
@@ -88,17 +89,28 @@ __device__ __forceinline__ Place place_of(const ScanArgs &a, int64_t chain, int 
     Place p;
     p.on = chain < a.chains;
     p.b = p.on ? chain / a.slabs : 0;
-    p.c = (chain - p.b * a.slabs) * (32 * V) + lane * V;
-    p.on = p.on && p.c < a.channels;
+    p.c = p.on ? (uint32_t)(chain - p.b * a.slabs) * (32 * V) + lane * V : 0;
+    p.writes = p.on && p.c < a.channels;
+    if (!p.writes) p.c = 0;
     p.len = a.lens ? min(max(__ldg(a.lens + p.b), 0), a.length) : a.length;
     return p;
 }
 
+// A lane's channels of one tensor at position `pos + s`.  The warp's part of the address is the same in all its lanes, so the
+// accesses of a stretch need one register of each.
 template <typename T, int V>
-__device__ __forceinline__ typename Lane<T, V>::raw *at(const ScanTensor &t, const Place &p, int pos)
-{
-    return reinterpret_cast<typename Lane<T, V>::raw *>(static_cast<T *>(t.p) + p.b * t.sb + pos * t.st + p.c);
-}
+struct Walker {
+    typedef typename Lane<T, V>::raw raw;
+    char *p;                              // of the warp
+    int64_t step;
+    uint32_t lane;
+    __device__ __forceinline__ Walker(const ScanTensor &t, const Place &at, int pos)
+        : p(static_cast<char *>(t.p) + (at.b * t.sb + pos * t.st) * (int64_t)sizeof(T)), step(t.st * (int64_t)sizeof(T)),
+          lane((uint32_t)at.c * (uint32_t)sizeof(T))
+    {
+    }
+    __device__ __forceinline__ raw &operator[](int s) const { return *reinterpret_cast<raw *>(p + s * step + lane); }
+};
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -116,77 +128,79 @@ __device__ __forceinline__ void store_remote(const float2 *local, uint32_t rank,
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
 }
 
-// Joins of a window.  `own`: (P, B) of this warp's stretch.  Returns the carry into the stretch, and moves `carry` over the whole
-// window.  BACK: the chain runs from the last stretch to the first.
+// Joins of a window's stretches, (P, B) each: publish, then join.  BACK: the chain runs from the last stretch to the first.  Places are
+// used in turn: one is written again two windows later, when every thread has met the barriers in between.
 template <int V, bool CLUSTER, bool BACK>
 struct Joins {
-    float2 (*part)[WARPS][32 * V];                   // [2 by parity][stretch][channel]: of this block
-    float2 (*span)[MOST_BLOCKS][32 * V];             // [2 by parity][rank][channel]: of the cluster's blocks
+    float2 (*part)[WARPS][32 * V];                   // [2 by turn][stretch][channel]: of this block
+    float2 (*span)[MOST_BLOCKS][32 * V];             // [2 by turn][rank][channel]: of the cluster's blocks
     int stretches, blocks, rank, warp, lane, first;  // first: index of the block's warp that has this chain's first stretch
-    int parity;
+    int turn;
 
     __device__ __forceinline__ void publish(const float (&p)[V], const float (&b)[V])
     {
 #pragma unroll
-        for (int v = 0; v < V; ++v) part[parity][first + warp][v * 32 + lane] = make_float2(p[v], b[v]);
+        for (int v = 0; v < V; ++v) part[turn][first + warp][v * 32 + lane] = make_float2(p[v], b[v]);
     }
+    // `into`: the carry into this warp's stretch; `carry`: over the whole window
     __device__ __forceinline__ void join(float (&carry)[V], float (&into)[V])
     {
         __syncthreads();
-        float2 all[V];
-        if (CLUSTER) {
-            // the block's own span, which every warp joins for itself and one of them hands to each block
-#pragma unroll
-            for (int v = 0; v < V; ++v) all[v] = make_float2(1.0f, 0.0f);
-#pragma unroll
-            for (int i = 0; i < WARPS; ++i) {
-                const int w = BACK ? WARPS - 1 - i : i;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float2 s = part[parity][w][v * 32 + lane];
-                    all[v].y = fmaf(s.x, all[v].y, s.y);
-                    all[v].x *= s.x;
-                }
-            }
-            if (warp < blocks)
-#pragma unroll
-                for (int v = 0; v < V; ++v) store_remote(&span[parity][rank][v * 32 + lane], warp, all[v]);
-            cluster_arrive();
-            cluster_wait();
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) into[v] = carry[v];
-        if (CLUSTER) {
-            for (int i = 0; i < blocks; ++i) {
-                const int k = BACK ? blocks - 1 - i : i;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float2 s = span[parity][k][v * 32 + lane];
-                    if (k == rank) into[v] = carry[v];
-                    carry[v] = fmaf(s.x, carry[v], s.y);
-                }
-            }
-        }
         const int before = BACK ? stretches - 1 - warp : warp;
-        for (int i = 0; i < before; ++i) {
-            const int w = first + (BACK ? stretches - 1 - i : i);
+        if (!CLUSTER) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) into[v] = carry[v];
+            for (int i = 0; i < before; ++i) {
+                const int w = first + (BACK ? stretches - 1 - i : i);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float2 s = part[0][w][v * 32 + lane];
+                    into[v] = fmaf(s.x, into[v], s.y);
+                }
+            }
+            return;
+        }
+        // the block's span, which every warp joins for itself (and what comes before its stretch on the way); each of
+        // them hands it to one block
+        float2 all[V], own[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) own[v] = all[v] = make_float2(1.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) {
+            const int w = BACK ? WARPS - 1 - i : i;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float2 s = part[parity][w][v * 32 + lane];
-                into[v] = fmaf(s.x, into[v], s.y);
+                const float2 s = part[turn][w][v * 32 + lane];
+                if (i == before) own[v] = all[v];
+                all[v].y = fmaf(s.x, all[v].y, s.y);
+                all[v].x *= s.x;
             }
         }
-        parity ^= 1;
+        if (warp < blocks)
+#pragma unroll
+            for (int v = 0; v < V; ++v) store_remote(&span[turn][rank][v * 32 + lane], warp, all[v]);
+        cluster_arrive();
+        cluster_wait();
+        for (int i = 0; CLUSTER && i < blocks; ++i) {
+            const int k = BACK ? blocks - 1 - i : i;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float2 s = span[turn][k][v * 32 + lane];
+                if (k == rank) into[v] = fmaf(own[v].x, carry[v], own[v].y);
+                carry[v] = fmaf(s.x, carry[v], s.y);
+            }
+        }
+        turn ^= 1;
     }
 };
 
 template <typename T, int V, bool CLUSTER>
-__global__ void __launch_bounds__(32 * WARPS) scan_forward_kernel(const __grid_constant__ ScanArgs a)
+__global__ void __launch_bounds__(32 * WARPS, 3) scan_forward_kernel(const __grid_constant__ ScanArgs a)
 {
     typedef typename Lane<T, V>::raw raw;
     __shared__ float2 part[CLUSTER ? 2 : 1][WARPS][32 * V];
     __shared__ float2 span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32 * V];
-    const int lane = threadIdx.x & 31, index = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
     const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
     const int64_t chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * groups + group;
@@ -204,36 +218,34 @@ __global__ void __launch_bounds__(32 * WARPS) scan_forward_kernel(const __grid_c
 
     for (int k0 = 0; k0 < a.spans; k0 += a.blocks) {
         const int k = k0 + rank;
-        const int t0 = k * SPAN + warp * STEPS;
-        const int rows = p.on ? min(max(a.length - t0, 0), STEPS) : 0, valid = min(rows, max(p.len - t0, 0));
+        const int t0 = k * SPAN + warp * a.steps, steps = CLUSTER ? STEPS : a.steps;
+        const int rows = p.on ? min(max(a.length - t0, 0), steps) : 0, valid = min(rows, max(p.len - t0, 0));
         raw z[STEPS], x[STEPS];
+        Walker<T, V> at_z(a.gate, p, t0), at_x(a.x, p, t0), at_out(a.out, p, t0);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
             if (s < valid) {
-                z[s] = *at<T, V>(a.gate, p, t0 + s);
-                x[s] = *at<T, V>(a.x, p, t0 + s);
+                z[s] = at_z[s];
+                x[s] = at_x[s];
             }
-        float h[STEPS][V], pr[STEPS][V], hn[V], pn[V];
+        float u[STEPS][V], h[V], pn[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) hn[v] = 0.0f, pn[v] = 1.0f;
+        for (int v = 0; v < V; ++v) h[v] = 0.0f, pn[v] = 1.0f;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
+        for (int s = 0; s < STEPS; ++s)
             if (s < valid) {
                 float zf[V], xf[V];
                 Lane<T, V>::get(z[s], zf);
                 Lane<T, V>::get(x[s], xf);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const float gate = gate_of(zf[v]);
-                    hn[v] = advance(gate, hn[v], xf[v]);
-                    pn[v] = keep(gate, pn[v]);
+                    u[s][v] = shut_of<T>(zf[v]);
+                    h[v] = advance(u[s][v], h[v], xf[v]);
+                    pn[v] = fmaf(-u[s][v], pn[v], pn[v]);
                 }
             }
-#pragma unroll
-            for (int v = 0; v < V; ++v) h[s][v] = hn[v], pr[s][v] = pn[v];
-        }
         if (CLUSTER || a.stretches > 1) {
-            joins.publish(pn, hn);
+            joins.publish(pn, h);
             joins.join(carry, into);
         } else {
 #pragma unroll
@@ -244,28 +256,32 @@ __global__ void __launch_bounds__(32 * WARPS) scan_forward_kernel(const __grid_c
             if (s < rows) {
                 float o[V];
 #pragma unroll
-                for (int v = 0; v < V; ++v) o[v] = s < valid ? fmaf(pr[s][v], into[v], h[s][v]) : 0.0f;
-                *at<T, V>(a.out, p, t0 + s) = Lane<T, V>::put(o);
+                for (int v = 0; v < V; ++v) o[v] = 0.0f;
+                if (s < valid) {
+                    Lane<T, V>::get(x[s], o);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) o[v] = into[v] = advance(u[s][v], into[v], o[v]);
+                }
+                if (p.writes) at_out[s] = Lane<T, V>::put(o);
             }
-        if (p.on && warp == a.stretches - 1 && k < a.spans) {
+        if (p.writes && warp == a.stretches - 1 && k < a.spans) {
             float *to = k < a.spans - 1 ? (a.states ? a.states + (p.b * (a.spans - 1) + k) * a.channels : nullptr)
                                         : (a.final_state ? a.final_state + p.b * a.channels : nullptr);
             if (to)
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    to[p.c + v] = fmaf(pn[v], into[v], hn[v]);
+                for (int v = 0; v < V; ++v) to[p.c + v] = into[v];
         }
     }
 }
 
 template <typename T, int V, bool CLUSTER>
-__global__ void __launch_bounds__(32 * WARPS) scan_backward_kernel(const __grid_constant__ ScanArgs a)
+__global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __grid_constant__ ScanArgs a)
 {
     typedef typename Lane<T, V>::raw raw;
     __shared__ float2 part[CLUSTER ? 2 : 1][WARPS][32 * V];
     __shared__ float2 span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32 * V];
     __shared__ float ahead[CLUSTER ? 2 : 1][WARPS][32 * V];          // B of the stretches, for h
-    const int lane = threadIdx.x & 31, index = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
     const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
     const int64_t chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * groups + group;
@@ -275,8 +291,7 @@ __global__ void __launch_bounds__(32 * WARPS) scan_backward_kernel(const __grid_
 
     float carry[V], into[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        carry[v] = a.dfinal && p.on ? a.dfinal[p.b * a.channels + p.c + v] : 0.0f;
+    for (int v = 0; v < V; ++v) carry[v] = a.dfinal && p.on ? a.dfinal[p.b * a.channels + p.c + v] : 0.0f;
     Joins<V, CLUSTER, true> joins = {reinterpret_cast<float2(*)[WARPS][32 * V]>(part),
                                      reinterpret_cast<float2(*)[MOST_BLOCKS][32 * V]>(span),
                                      a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
@@ -284,15 +299,16 @@ __global__ void __launch_bounds__(32 * WARPS) scan_backward_kernel(const __grid_
 
     for (int k0 = (a.spans - 1) / a.blocks * a.blocks; k0 >= 0; k0 -= a.blocks) {
         const int k = k0 + rank;
-        const int t0 = k * SPAN + warp * STEPS;
-        const int rows = p.on ? min(max(a.length - t0, 0), STEPS) : 0, valid = min(rows, max(p.len - t0, 0));
+        const int t0 = k * SPAN + warp * a.steps, steps = CLUSTER ? STEPS : a.steps;
+        const int rows = p.on ? min(max(a.length - t0, 0), steps) : 0, valid = min(rows, max(p.len - t0, 0));
         raw z[STEPS], x[STEPS], g[STEPS];
+        Walker<T, V> at_z(a.gate, p, t0), at_x(a.x, p, t0), at_g(a.dout, p, t0);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
             if (s < valid) {
-                z[s] = *at<T, V>(a.gate, p, t0 + s);
-                x[s] = *at<T, V>(a.x, p, t0 + s);
-                g[s] = a.dout.p ? *at<T, V>(a.dout, p, t0 + s) : zero_raw<raw>();
+                z[s] = at_z[s];
+                x[s] = at_x[s];
+                g[s] = a.dout.p ? at_g[s] : zero_raw<raw>();
             }
         // the state before the block's span
         float h[V];
@@ -316,29 +332,30 @@ __global__ void __launch_bounds__(32 * WARPS) scan_backward_kernel(const __grid_
                 Lane<T, V>::get(g[s], gf);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    gate[s][v] = gate_of(zf[v]);
-                    hn[v] = advance(gate[s][v], hn[v], xf[v]);
-                    pn[v] = keep(gate[s][v], pn[v]);
+                    float u;
+                    gate[s][v] = gate_of<T>(zf[v], u);
+                    hn[v] = advance(u, hn[v], xf[v]);
+                    pn[v] = fmaf(-u, pn[v], pn[v]);
                     rn[v] = fmaf(pn[v], gf[v], rn[v]);
                 }
             }
         if (CLUSTER || a.stretches > 1) {
-            const int parity = joins.parity;
+            const int turn = joins.turn;
             joins.publish(pn, rn);
 #pragma unroll
-            for (int v = 0; v < V; ++v) ahead[parity][index][v * 32 + lane] = hn[v];
+            for (int v = 0; v < V; ++v) ahead[turn][index][v * 32 + lane] = hn[v];
             joins.join(carry, into);
             for (int i = 0; i < warp; ++i)
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const int w = group * a.stretches + i;
-                    h[v] = fmaf(part[parity][w][v * 32 + lane].x, h[v], ahead[parity][w][v * 32 + lane]);
+                    h[v] = fmaf(part[turn][w][v * 32 + lane].x, h[v], ahead[turn][w][v * 32 + lane]);
                 }
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) into[v] = carry[v];
         }
-        float d[STEPS][V];                                           // h_(t-1) - x_t
+        float u[STEPS][V], d[STEPS][V];                              // 1 - a; a (1 - a) (h_(t-1) - x_t)
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
             if (s < valid) {
@@ -346,10 +363,13 @@ __global__ void __launch_bounds__(32 * WARPS) scan_backward_kernel(const __grid_
                 Lane<T, V>::get(x[s], xf);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    d[s][v] = h[v] - xf[v];
-                    h[v] = advance(gate[s][v], h[v], xf[v]);
+                    const float m = fabsf(gate[s][v]);
+                    u[s][v] = signbit(gate[s][v]) ? 1.0f - m : m;
+                    d[s][v] = fmaf(-m, m, m) * (h[v] - xf[v]);
+                    h[v] = advance(u[s][v], h[v], xf[v]);
                 }
             }
+        Walker<T, V> at_dx(a.dx, p, t0), at_dz(a.dgate, p, t0);
 #pragma unroll
         for (int s = STEPS - 1; s >= 0; --s)
             if (s < rows) {
@@ -361,21 +381,20 @@ __global__ void __launch_bounds__(32 * WARPS) scan_backward_kernel(const __grid_
                     Lane<T, V>::get(g[s], gf);
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        const float full = gf[v] + into[v], m = fabsf(gate[s][v]);
-                        const float near = m * full, far = fmaf(-m, full, full);
-                        const bool open = signbit(gate[s][v]);
-                        dx[v] = open ? near : far;
-                        into[v] = open ? far : near;
-                        dz[v] = d[s][v] * (m * far);
+                        const float full = gf[v] + into[v];
+                        dx[v] = u[s][v] * full;
+                        into[v] = full - dx[v];
+                        dz[v] = d[s][v] * full;
                     }
                 }
-                *at<T, V>(a.dx, p, t0 + s) = Lane<T, V>::put(dx);
-                *at<T, V>(a.dgate, p, t0 + s) = Lane<T, V>::put(dz);
+                if (p.writes) {
+                    at_dx[s] = Lane<T, V>::put(dx);
+                    at_dz[s] = Lane<T, V>::put(dz);
+                }
             }
-        if (a.dh0 && p.on && k == 0 && warp == 0)
+        if (a.dh0 && p.writes && k == 0 && warp == 0)
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                a.dh0[p.b * a.channels + p.c + v] = into[v];
+            for (int v = 0; v < V; ++v) a.dh0[p.b * a.channels + p.c + v] = into[v];
     }
 }
 
@@ -394,6 +413,7 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
         const int windows = (a.spans + MOST_BLOCKS - 1) / MOST_BLOCKS;
         a.blocks = (a.spans + windows - 1) / windows;
         a.stretches = WARPS;
+        a.steps = STEPS;
         grid = a.chains * a.blocks;
         cfg.blockDim = dim3(32 * WARPS);
         attr.id = cudaLaunchAttributeClusterDimension;
@@ -405,6 +425,7 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
         // several chains a block where one needs few warps
         a.blocks = 1;
         a.stretches = a.length > STEPS ? (a.length + STEPS - 1) / STEPS : 1;
+        a.steps = (a.length + a.stretches - 1) / a.stretches;
         const int groups = WARPS / a.stretches > 0 ? WARPS / a.stretches : 1;
         grid = (a.chains + groups - 1) / groups;
         cfg.blockDim = dim3(32 * groups * a.stretches);
@@ -427,8 +448,8 @@ static gs_status check(const gs_recurrence_config *c, ScanArgs *a)
     if (!c) return bad("config is NULL");
     if (!known_type(c->dtype)) return bad("dtype must be GS_TABLE_F32, GS_TABLE_F16 or GS_TABLE_BF16");
     if (c->batch < 0 || c->length < 0 || c->channels <= 0) return bad("negative batch or length, or no channels");
-    if (c->length > (1 << 30) || c->channels > ((int64_t)1 << 31) || (c->batch > 0 && c->channels > ((int64_t)1 << 40) / c->batch)) {
-        set_error("recurrences of up to 2^30 positions, 2^31 channels and 2^40 states are supported");
+    if (c->length > (1 << 30) || c->channels > ((int64_t)1 << 30) || (c->batch > 0 && c->channels > ((int64_t)1 << 40) / c->batch)) {
+        set_error("recurrences of up to 2^30 positions, 2^30 channels and 2^40 states are supported");
         return GS_ERR_UNSUPPORTED;
     }
     *a = ScanArgs{};
@@ -464,6 +485,7 @@ static gs_status run(ScanArgs &a, int32_t dtype, const ScanTensor *const *t, int
             return bad("an output has a zero stride");
         pairs = pairs && (uintptr_t)t[i]->p % 4 == 0 && (t[i]->sb | t[i]->st) % 2 == 0;
     }
+    pairs = pairs && a.channels > 32;                   // one channel a lane where two would leave half the lanes idle
     if (dtype == GS_TABLE_F32) return launch<float, 1>(a, backward, st);
     if (dtype == GS_TABLE_F16) return pairs ? launch<__half, 2>(a, backward, st) : launch<__half, 1>(a, backward, st);
     return pairs ? launch<__nv_bfloat16, 2>(a, backward, st) : launch<__nv_bfloat16, 1>(a, backward, st);

@@ -72,7 +72,7 @@ def test_layer_norm_pointers(lib):
 @pytest.mark.parametrize("kw,want,word", [
     (dict(dtype=7), INVALID, "dtype"), (dict(batch=-1), INVALID, "batch"), (dict(length=-1), INVALID, "length"),
     (dict(channels=0), INVALID, "channels"), (dict(length=(1 << 30) + 1), UNSUPPORTED, "positions"),
-    (dict(channels=(1 << 31) + 1), UNSUPPORTED, "channels"), (dict(batch=1 << 40, channels=2), UNSUPPORTED, "states"),
+    (dict(channels=(1 << 30) + 1), UNSUPPORTED, "channels"), (dict(batch=1 << 40, channels=2), UNSUPPORTED, "states"),
     (dict(batch=1 << 62, channels=1 << 31), UNSUPPORTED, "states"), (dict(batch=1 << 32, channels=64), UNSUPPORTED, "one launch"),
 ])
 def test_recurrence_configurations(lib, kw, want, word):
