@@ -17,6 +17,8 @@
 namespace gs {
 
 static constexpr int STEPS = 16, WARPS = 8, SPAN = STEPS * WARPS, MOST_BLOCKS = 8;
+// Blocks of an SM: what their registers and the shared memory that the next inputs wait in allow
+static constexpr int FORWARD_BLOCKS = 3, BACKWARD_BLOCKS = 2;
 
 struct ScanTensor {
     void *p;
@@ -28,6 +30,7 @@ struct ScanArgs {
     const float *h0, *dfinal;
     float *final_state, *dh0, *states;
     const int32_t *lens;
+    Divider by_slabs;
     int64_t batch, channels, chains;      // chains = batch * slabs
     int32_t length, slabs, spans;         // slabs of 32 * V channels; spans = ceil(length / SPAN)
     int32_t stretches, steps;             // warps that share a span, positions of each
@@ -76,27 +79,31 @@ __device__ __forceinline__ float gate_of(float z, float &u)
     return shut ? -m : m;
 }
 
-struct Place {                            // what a warp works on
+struct Place {                            // what a warp works on: positions [t0, t0 + rows) of a chain, `valid` of them valid
     int64_t b;                            // sequence
     uint32_t c;                           // the lane's first channel
     bool on, writes;                      // the warp has a chain; the lane has a channel (one that has none reads another's)
-    int len;                              // valid positions
+    int k, t0, rows, valid;               // k: the span
 };
 
 template <int V>
-__device__ __forceinline__ Place place_of(const ScanArgs &a, int64_t chain, int lane)
+__device__ __forceinline__ Place place_of(const ScanArgs &a, int64_t chain, int lane, int k, int warp)
 {
     Place p;
     p.on = chain < a.chains;
-    p.b = p.on ? chain / a.slabs : 0;
+    p.b = p.on ? a.by_slabs.of(chain) : 0;
     p.c = p.on ? (uint32_t)(chain - p.b * a.slabs) * (32 * V) + lane * V : 0;
     p.writes = p.on && p.c < a.channels;
     if (!p.writes) p.c = 0;
-    p.len = a.lens ? min(max(__ldg(a.lens + p.b), 0), a.length) : a.length;
+    p.k = k;
+    p.t0 = k * SPAN + warp * a.steps;
+    p.rows = p.on ? min(max(a.length - p.t0, 0), a.steps) : 0;
+    const int len = a.lens && p.on ? min(max(__ldg(a.lens + p.b), 0), a.length) : a.length;
+    p.valid = min(p.rows, max(len - p.t0, 0));
     return p;
 }
 
-// A lane's channels of one tensor at position `pos + s`.  The warp's part of the address is the same in all its lanes, so the
+// A lane's channels of one tensor at position t0 + s.  The warp's part of the address is the same in all its lanes, so the
 // accesses of a stretch need one register of each.
 template <typename T, int V>
 struct Walker {
@@ -104,13 +111,44 @@ struct Walker {
     char *p;                              // of the warp
     int64_t step;
     uint32_t lane;
-    __device__ __forceinline__ Walker(const ScanTensor &t, const Place &at, int pos)
-        : p(static_cast<char *>(t.p) + (at.b * t.sb + pos * t.st) * (int64_t)sizeof(T)), step(t.st * (int64_t)sizeof(T)),
-          lane((uint32_t)at.c * (uint32_t)sizeof(T))
+    __device__ __forceinline__ Walker(const ScanTensor &t, const Place &at)
+        : p(static_cast<char *>(t.p) + (at.b * t.sb + at.t0 * t.st) * (int64_t)sizeof(T)), step(t.st * (int64_t)sizeof(T)),
+          lane(at.c * (uint32_t)sizeof(T))
     {
     }
     __device__ __forceinline__ raw &operator[](int s) const { return *reinterpret_cast<raw *>(p + s * step + lane); }
 };
+
+// Inputs wait in shared memory, each in a place that only the lane that asked for it reads again: no registers are held while they are on
+// their way, and no barrier is needed when they have come.
+template <typename R>
+struct Stage {
+    R (*place)[32];                       // [step][lane]
+    int lane;
+    template <typename W>
+    __device__ __forceinline__ void fetch(const W &from, int valid)
+    {
+        if constexpr (sizeof(R) == 4) {
+            const uint32_t to = (uint32_t)__cvta_generic_to_shared(&place[0][lane]);
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+                if (s < valid)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + s * 128), "l"(&from[s]) : "memory");
+        } else {                          // two bytes are less than such a copy moves
+            R r[STEPS];
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+                if (s < valid) r[s] = from[s];
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+                if (s < valid) place[s][lane] = r[s];
+        }
+    }
+    __device__ __forceinline__ R operator[](int s) const { return place[s][lane]; }
+};
+__device__ __forceinline__ void fetches_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// all but the latest group of this thread's fetches have come
+__device__ __forceinline__ void fetches_wait() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -128,25 +166,33 @@ __device__ __forceinline__ void store_remote(const float2 *local, uint32_t rank,
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
 }
 
-// Joins of a window's stretches, (P, B) each: publish, then join.  BACK: the chain runs from the last stretch to the first.  Places are
-// used in turn: one is written again two windows later, when every thread has met the barriers in between.
+// Joins of stretches, (P, B) each.  BACK: the chain runs from the last stretch to the first.  A block's pairs are published, read by
+// all its warps after a barrier, and may be overwritten after the next one (of the block or the cluster) that `join` ends with.
 template <int V, bool CLUSTER, bool BACK>
 struct Joins {
-    float2 (*part)[WARPS][32 * V];                   // [2 by turn][stretch][channel]: of this block
-    float2 (*span)[MOST_BLOCKS][32 * V];             // [2 by turn][rank][channel]: of the cluster's blocks
+    float2 (*part)[32 * V];                          // [stretch][channel]: of this block
+    float2 (*span)[MOST_BLOCKS][32 * V];             // [2 in turn][rank][channel]: of the cluster's blocks
+    float (*ahead)[32 * V];                          // [stretch][channel]: B of the stretches in the other direction
     int stretches, blocks, rank, warp, lane, first;  // first: index of the block's warp that has this chain's first stretch
     int turn;
 
-    __device__ __forceinline__ void publish(const float (&p)[V], const float (&b)[V])
+    // p, b: of this warp's stretch; carry: into the window, moved over it; into: into this stretch.  With `ahead`: h, the state
+    // before the block's span, and hb, its B over this stretch; h becomes the state before the stretch.
+    __device__ __forceinline__ void join(const float (&p)[V], const float (&b)[V], float (&carry)[V], float (&into)[V],
+                                         const float (&hb)[V], float (&h)[V])
     {
 #pragma unroll
-        for (int v = 0; v < V; ++v) part[turn][first + warp][v * 32 + lane] = make_float2(p[v], b[v]);
-    }
-    // `into`: the carry into this warp's stretch; `carry`: over the whole window
-    __device__ __forceinline__ void join(float (&carry)[V], float (&into)[V])
-    {
+        for (int v = 0; v < V; ++v) {
+            part[first + warp][v * 32 + lane] = make_float2(p[v], b[v]);
+            if (BACK) ahead[first + warp][v * 32 + lane] = hb[v];
+        }
         __syncthreads();
         const int before = BACK ? stretches - 1 - warp : warp;
+        if (BACK)
+            for (int i = 0; i < warp; ++i)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    h[v] = fmaf(part[first + i][v * 32 + lane].x, h[v], ahead[first + i][v * 32 + lane]);
         if (!CLUSTER) {
 #pragma unroll
             for (int v = 0; v < V; ++v) into[v] = carry[v];
@@ -154,10 +200,11 @@ struct Joins {
                 const int w = first + (BACK ? stretches - 1 - i : i);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const float2 s = part[0][w][v * 32 + lane];
+                    const float2 s = part[w][v * 32 + lane];
                     into[v] = fmaf(s.x, into[v], s.y);
                 }
             }
+            __syncthreads();
             return;
         }
         // the block's span, which every warp joins for itself (and what comes before its stretch on the way); each of
@@ -170,7 +217,7 @@ struct Joins {
             const int w = BACK ? WARPS - 1 - i : i;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float2 s = part[turn][w][v * 32 + lane];
+                const float2 s = part[w][v * 32 + lane];
                 if (i == before) own[v] = all[v];
                 all[v].y = fmaf(s.x, all[v].y, s.y);
                 all[v].x *= s.x;
@@ -190,50 +237,92 @@ struct Joins {
                 carry[v] = fmaf(s.x, carry[v], s.y);
             }
         }
-        turn ^= 1;
+        turn ^= 1;                        // written again two windows later, behind a barrier that follows every read
     }
 };
 
+// A warp's items: a cluster has one chain and goes through its windows; a block of short chains goes from one group of chains to
+// another, as long as there are some.
+template <bool CLUSTER, bool BACK>
+struct Items {
+    int64_t chain, stride;                           // of the present item
+    int window, windows;
+    __device__ __forceinline__ bool next(const ScanArgs &a)
+    {
+        if (!CLUSTER) {
+            chain += stride;
+            return chain - chain_offset < a.chains;
+        }
+        window += BACK ? -1 : 1;
+        return BACK ? window >= 0 : window < windows;
+    }
+    int64_t chain_offset;                            // of the warp's group in its block: all warps of a block take the same number of items
+};
+template <bool CLUSTER, bool BACK>
+__device__ __forceinline__ Items<CLUSTER, BACK> first_item(const ScanArgs &a, int group, int groups)
+{
+    Items<CLUSTER, BACK> it;
+    it.windows = (a.spans + a.blocks - 1) / a.blocks;
+    it.window = CLUSTER && BACK ? it.windows - 1 : 0;
+    it.chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * groups + group;
+    it.chain_offset = group;
+    it.stride = (int64_t)gridDim.x * groups;
+    return it;
+}
+
 template <typename T, int V, bool CLUSTER>
-__global__ void __launch_bounds__(32 * WARPS, 3) scan_forward_kernel(const __grid_constant__ ScanArgs a)
+__global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan_forward_kernel(const __grid_constant__ ScanArgs a)
 {
     typedef typename Lane<T, V>::raw raw;
-    __shared__ float2 part[CLUSTER ? 2 : 1][WARPS][32 * V];
+    __shared__ float2 part[WARPS][32 * V];
     __shared__ float2 span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32 * V];
+    extern __shared__ uint32_t room[];                               // [2 in turn][gate, x][warp][step][lane]
     const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
     const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
-    const int64_t chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * groups + group;
-    const Place p = place_of<V>(a, chain, lane);
-    __syncwarp();
+    raw (*stages)[32] = reinterpret_cast<raw(*)[32]>(room) + index * STEPS;
+    constexpr int ROWS = WARPS * STEPS;
     if (CLUSTER) cluster_arrive();                      // completed by the wait before the first remote store
 
-    float carry[V], into[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = a.h0 && p.on ? a.h0[p.b * a.channels + p.c + v] : 0.0f;
-    Joins<V, CLUSTER, false> joins = {reinterpret_cast<float2(*)[WARPS][32 * V]>(part),
-                                      reinterpret_cast<float2(*)[MOST_BLOCKS][32 * V]>(span),
-                                      a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
-    if (CLUSTER) cluster_wait();
+    auto item = first_item<CLUSTER, false>(a, group, groups);
+    Place next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
+    auto fetch = [&](const Place &p, int turn) {
+        Stage<raw>{stages + (2 * turn) * ROWS, lane}.fetch(Walker<T, V>(a.gate, p), p.valid);
+        Stage<raw>{stages + (2 * turn + 1) * ROWS, lane}.fetch(Walker<T, V>(a.x, p), p.valid);
+    };
+    fetch(next, 0);
+    fetches_end();
 
-    for (int k0 = 0; k0 < a.spans; k0 += a.blocks) {
-        const int k = k0 + rank;
-        const int t0 = k * SPAN + warp * a.steps, steps = CLUSTER ? STEPS : a.steps;
-        const int rows = p.on ? min(max(a.length - t0, 0), steps) : 0, valid = min(rows, max(p.len - t0, 0));
-        raw z[STEPS], x[STEPS];
-        Walker<T, V> at_z(a.gate, p, t0), at_x(a.x, p, t0), at_out(a.out, p, t0);
+    Joins<V, CLUSTER, false> joins = {part, reinterpret_cast<float2(*)[MOST_BLOCKS][32 * V]>(span), nullptr,
+                                      a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
+    float carry[V], into[V];
+    if (CLUSTER) {
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-            if (s < valid) {
-                z[s] = at_z[s];
-                x[s] = at_x[s];
-            }
+        for (int v = 0; v < V; ++v) carry[v] = a.h0 ? a.h0[next.b * a.channels + next.c + v] : 0.0f;
+        cluster_wait();
+    }
+    bool more;
+    int turn = 0;
+    do {
+        const Place p = next;
+        more = item.next(a);
+        if (more) {
+            next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
+            fetch(next, turn ^ 1);
+        }
+        fetches_end();
+        if (!CLUSTER)
+#pragma unroll
+            for (int v = 0; v < V; ++v) carry[v] = a.h0 ? a.h0[p.b * a.channels + p.c + v] : 0.0f;
+        fetches_wait();
+        const Stage<raw> z = {stages + (2 * turn) * ROWS, lane}, x = {stages + (2 * turn + 1) * ROWS, lane};
+        turn ^= 1;
         float u[STEPS][V], h[V], pn[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = 0.0f, pn[v] = 1.0f;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
-            if (s < valid) {
+            if (s < p.valid) {
                 float zf[V], xf[V];
                 Lane<T, V>::get(z[s], zf);
                 Lane<T, V>::get(x[s], xf);
@@ -245,140 +334,140 @@ __global__ void __launch_bounds__(32 * WARPS, 3) scan_forward_kernel(const __gri
                 }
             }
         if (CLUSTER || a.stretches > 1) {
-            joins.publish(pn, h);
-            joins.join(carry, into);
+            joins.join(pn, h, carry, into, h, h);
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) into[v] = carry[v];
         }
+        const Walker<T, V> out(a.out, p);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
-            if (s < rows) {
+            if (s < p.rows) {
                 float o[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) o[v] = 0.0f;
-                if (s < valid) {
+                if (s < p.valid) {
                     Lane<T, V>::get(x[s], o);
 #pragma unroll
                     for (int v = 0; v < V; ++v) o[v] = into[v] = advance(u[s][v], into[v], o[v]);
                 }
-                if (p.writes) at_out[s] = Lane<T, V>::put(o);
+                if (p.writes) out[s] = Lane<T, V>::put(o);
             }
-        if (p.writes && warp == a.stretches - 1 && k < a.spans) {
-            float *to = k < a.spans - 1 ? (a.states ? a.states + (p.b * (a.spans - 1) + k) * a.channels : nullptr)
-                                        : (a.final_state ? a.final_state + p.b * a.channels : nullptr);
+        if (p.writes && warp == a.stretches - 1 && p.k < a.spans) {
+            float *to = p.k < a.spans - 1 ? (a.states ? a.states + (p.b * (a.spans - 1) + p.k) * a.channels : nullptr)
+                                          : (a.final_state ? a.final_state + p.b * a.channels : nullptr);
             if (to)
 #pragma unroll
                 for (int v = 0; v < V; ++v) to[p.c + v] = into[v];
         }
-    }
+    } while (more);
 }
 
 template <typename T, int V, bool CLUSTER>
-__global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __grid_constant__ ScanArgs a)
+__global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_kernel(const __grid_constant__ ScanArgs a)
 {
     typedef typename Lane<T, V>::raw raw;
-    __shared__ float2 part[CLUSTER ? 2 : 1][WARPS][32 * V];
+    __shared__ float2 part[WARPS][32 * V];
+    __shared__ float ahead[WARPS][32 * V];
     __shared__ float2 span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32 * V];
-    __shared__ float ahead[CLUSTER ? 2 : 1][WARPS][32 * V];          // B of the stretches, for h
+    extern __shared__ uint32_t room[];                               // [2 in turn][gate, x, dout][warp][step][lane]
     const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
     const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
-    const int64_t chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * groups + group;
-    const Place p = place_of<V>(a, chain, lane);
-    __syncwarp();
+    raw (*stages)[32] = reinterpret_cast<raw(*)[32]>(room) + index * STEPS;
+    constexpr int ROWS = WARPS * STEPS;
     if (CLUSTER) cluster_arrive();
 
-    float carry[V], into[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = a.dfinal && p.on ? a.dfinal[p.b * a.channels + p.c + v] : 0.0f;
-    Joins<V, CLUSTER, true> joins = {reinterpret_cast<float2(*)[WARPS][32 * V]>(part),
-                                     reinterpret_cast<float2(*)[MOST_BLOCKS][32 * V]>(span),
-                                     a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
-    if (CLUSTER) cluster_wait();
+    auto item = first_item<CLUSTER, true>(a, group, groups);
+    Place next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
+    auto fetch = [&](const Place &p, int turn) {
+        Stage<raw>{stages + (3 * turn) * ROWS, lane}.fetch(Walker<T, V>(a.gate, p), p.valid);
+        Stage<raw>{stages + (3 * turn + 1) * ROWS, lane}.fetch(Walker<T, V>(a.x, p), p.valid);
+        if (a.dout.p) Stage<raw>{stages + (3 * turn + 2) * ROWS, lane}.fetch(Walker<T, V>(a.dout, p), p.valid);
+    };
+    fetch(next, 0);
+    fetches_end();
 
-    for (int k0 = (a.spans - 1) / a.blocks * a.blocks; k0 >= 0; k0 -= a.blocks) {
-        const int k = k0 + rank;
-        const int t0 = k * SPAN + warp * a.steps, steps = CLUSTER ? STEPS : a.steps;
-        const int rows = p.on ? min(max(a.length - t0, 0), steps) : 0, valid = min(rows, max(p.len - t0, 0));
-        raw z[STEPS], x[STEPS], g[STEPS];
-        Walker<T, V> at_z(a.gate, p, t0), at_x(a.x, p, t0), at_g(a.dout, p, t0);
+    Joins<V, CLUSTER, true> joins = {part, reinterpret_cast<float2(*)[MOST_BLOCKS][32 * V]>(span), ahead,
+                                     a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
+    float carry[V], into[V];
+    if (CLUSTER) {
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-            if (s < valid) {
-                z[s] = at_z[s];
-                x[s] = at_x[s];
-                g[s] = a.dout.p ? at_g[s] : zero_raw<raw>();
-            }
-        // the state before the block's span
-        float h[V];
+        for (int v = 0; v < V; ++v) carry[v] = a.dfinal ? a.dfinal[next.b * a.channels + next.c + v] : 0.0f;
+        cluster_wait();
+    }
+    bool more;
+    int turn = 0;
+    do {
+        const Place p = next;
+        more = item.next(a);
+        if (more) {
+            next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
+            fetch(next, turn ^ 1);
+        }
+        fetches_end();
+        float h[V];                                                  // the state before the block's span
 #pragma unroll
         for (int v = 0; v < V; ++v) {
+            const int64_t at = p.b * a.channels + p.c + v;
+            if (!CLUSTER) carry[v] = a.dfinal ? a.dfinal[at] : 0.0f;
             h[v] = 0.0f;
-            if (p.on && k < a.spans) {
-                if (k > 0) h[v] = a.states[(p.b * (a.spans - 1) + k - 1) * a.channels + p.c + v];
-                else if (a.h0) h[v] = a.h0[p.b * a.channels + p.c + v];
-            }
+            if (CLUSTER && p.k > 0 && p.k < a.spans) h[v] = a.states[(p.b * (a.spans - 1) + p.k - 1) * a.channels + p.c + v];
+            else if (p.k == 0 && a.h0) h[v] = a.h0[at];
         }
-        float gate[STEPS][V], hn[V], pn[V], rn[V];
+        fetches_wait();
+        const Stage<raw> z = {stages + (3 * turn) * ROWS, lane}, x = {stages + (3 * turn + 1) * ROWS, lane},
+                         g = {stages + (3 * turn + 2) * ROWS, lane};
+        turn ^= 1;
+        float u[STEPS][V], hn[V], pn[V], rn[V];                      // u: first as gate_of has it, then 1 - a
 #pragma unroll
         for (int v = 0; v < V; ++v) hn[v] = 0.0f, pn[v] = 1.0f, rn[v] = 0.0f;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
-            if (s < valid) {
+            if (s < p.valid) {
                 float zf[V], xf[V], gf[V];
                 Lane<T, V>::get(z[s], zf);
                 Lane<T, V>::get(x[s], xf);
-                Lane<T, V>::get(g[s], gf);
+                Lane<T, V>::get(a.dout.p ? g[s] : zero_raw<raw>(), gf);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    float u;
-                    gate[s][v] = gate_of<T>(zf[v], u);
-                    hn[v] = advance(u, hn[v], xf[v]);
-                    pn[v] = fmaf(-u, pn[v], pn[v]);
+                    float shut;
+                    u[s][v] = gate_of<T>(zf[v], shut);
+                    hn[v] = advance(shut, hn[v], xf[v]);
+                    pn[v] = fmaf(-shut, pn[v], pn[v]);
                     rn[v] = fmaf(pn[v], gf[v], rn[v]);
                 }
             }
         if (CLUSTER || a.stretches > 1) {
-            const int turn = joins.turn;
-            joins.publish(pn, rn);
-#pragma unroll
-            for (int v = 0; v < V; ++v) ahead[turn][index][v * 32 + lane] = hn[v];
-            joins.join(carry, into);
-            for (int i = 0; i < warp; ++i)
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const int w = group * a.stretches + i;
-                    h[v] = fmaf(part[turn][w][v * 32 + lane].x, h[v], ahead[turn][w][v * 32 + lane]);
-                }
+            joins.join(pn, rn, carry, into, hn, h);
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) into[v] = carry[v];
         }
-        float u[STEPS][V], d[STEPS][V];                              // 1 - a; a (1 - a) (h_(t-1) - x_t)
+        float d[STEPS][V];                                           // a (1 - a) (h_(t-1) - x_t)
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
-            if (s < valid) {
+            if (s < p.valid) {
                 float xf[V];
                 Lane<T, V>::get(x[s], xf);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const float m = fabsf(gate[s][v]);
-                    u[s][v] = signbit(gate[s][v]) ? 1.0f - m : m;
+                    const float m = fabsf(u[s][v]);
+                    u[s][v] = signbit(u[s][v]) ? 1.0f - m : m;
                     d[s][v] = fmaf(-m, m, m) * (h[v] - xf[v]);
                     h[v] = advance(u[s][v], h[v], xf[v]);
                 }
             }
-        Walker<T, V> at_dx(a.dx, p, t0), at_dz(a.dgate, p, t0);
+        const Walker<T, V> at_dx(a.dx, p), at_dz(a.dgate, p);
 #pragma unroll
         for (int s = STEPS - 1; s >= 0; --s)
-            if (s < rows) {
+            if (s < p.rows) {
                 float dx[V], dz[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) dx[v] = dz[v] = 0.0f;
-                if (s < valid) {
+                if (s < p.valid) {
                     float gf[V];
-                    Lane<T, V>::get(g[s], gf);
+                    Lane<T, V>::get(a.dout.p ? g[s] : zero_raw<raw>(), gf);
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
                         const float full = gf[v] + into[v];
@@ -392,10 +481,10 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
                     at_dz[s] = Lane<T, V>::put(dz);
                 }
             }
-        if (a.dh0 && p.writes && k == 0 && warp == 0)
+        if (a.dh0 && p.writes && p.k == 0 && warp == 0)
 #pragma unroll
             for (int v = 0; v < V; ++v) a.dh0[p.b * a.channels + p.c + v] = into[v];
-    }
+    } while (more);
 }
 
 template <typename T, int V>
@@ -403,12 +492,19 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
 {
     ScanArgs a = args;
     a.slabs = (int32_t)((a.channels + 32 * V - 1) / (32 * V));
+    a.by_slabs = Divider(a.slabs);
     a.chains = a.batch * a.slabs;
     a.spans = (a.length + SPAN - 1) / SPAN;
+    const bool cluster = a.spans > 1;
+    static SharedRecord records[4];
+    auto kernel = backward ? cluster ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>
+                           : cluster ? scan_forward_kernel<T, V, true> : scan_forward_kernel<T, V, false>;
+    SharedRecord &record = records[2 * backward + cluster];
+    const size_t shared = (size_t)2 * (backward ? 3 : 2) * SPAN * 32 * sizeof(typename Lane<T, V>::raw);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr = {};
     int64_t grid;
-    if (a.spans > 1) {
+    if (cluster) {
         // as few windows as a cluster of MOST_BLOCKS allows, and no more blocks than these need
         const int windows = (a.spans + MOST_BLOCKS - 1) / MOST_BLOCKS;
         a.blocks = (a.spans + windows - 1) / windows;
@@ -427,19 +523,30 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
         a.stretches = a.length > STEPS ? (a.length + STEPS - 1) / STEPS : 1;
         a.steps = (a.length + a.stretches - 1) / a.stretches;
         const int groups = WARPS / a.stretches > 0 ? WARPS / a.stretches : 1;
-        grid = (a.chains + groups - 1) / groups;
         cfg.blockDim = dim3(32 * groups * a.stretches);
+        const int64_t most = (int64_t)sm_count() * (backward ? BACKWARD_BLOCKS : FORWARD_BLOCKS);
+        grid = (a.chains + groups - 1) / groups;
+        if (grid > most) grid = most;
     }
     if (grid > 0x7FFFFFFF) {
         set_error("a recurrence of %lld blocks exceeds one launch", (long long)grid);
         return GS_ERR_UNSUPPORTED;
     }
+    gs_status s = allow_shared(kernel, (int)shared, record);
+    if (s != GS_OK) return s;
     cfg.gridDim = dim3((unsigned)grid);
+    cfg.dynamicSmemBytes = shared;
     cfg.stream = st;
-    if (backward)
-        GS_CUDA_TRY(cudaLaunchKernelEx(&cfg, a.spans > 1 ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>, a));
-    else
-        GS_CUDA_TRY(cudaLaunchKernelEx(&cfg, a.spans > 1 ? scan_forward_kernel<T, V, true> : scan_forward_kernel<T, V, false>, a));
+    GS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
+    return GS_OK;
+}
+
+// an empty sequence ends with the state that it starts with
+static gs_status copy_states(const float *from, float *to, int64_t n, cudaStream_t st)
+{
+    if (!to || to == from) return GS_OK;
+    if (from) GS_CUDA_TRY(cudaMemcpyAsync(to, from, n * sizeof(float), cudaMemcpyDeviceToDevice, st));
+    else GS_CUDA_TRY(cudaMemsetAsync(to, 0, n * sizeof(float), st));
     return GS_OK;
 }
 
@@ -463,15 +570,6 @@ static gs_status check(const gs_recurrence_config *c, ScanArgs *a)
 static ScanTensor tensor(const void *p, const int64_t (&stride)[2])
 {
     return {const_cast<void *>(p), stride[0], stride[1]};
-}
-
-// an empty sequence ends with the state that it starts with
-static gs_status copy_states(const float *from, float *to, int64_t n, cudaStream_t st)
-{
-    if (!to || to == from) return GS_OK;
-    if (from) GS_CUDA_TRY(cudaMemcpyAsync(to, from, n * sizeof(float), cudaMemcpyDeviceToDevice, st));
-    else GS_CUDA_TRY(cudaMemsetAsync(to, 0, n * sizeof(float), st));
-    return GS_OK;
 }
 
 static gs_status run(ScanArgs &a, int32_t dtype, const ScanTensor *const *t, int n, int outputs, bool backward, cudaStream_t st)
