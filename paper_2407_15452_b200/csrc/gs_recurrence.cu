@@ -12,6 +12,8 @@
 // forward pass left, computes h again (one stream fewer than reading it, and in fp32) and joins only r.
 #include <math.h>
 
+#include <type_traits>
+
 #include "gs_layers.cuh"
 
 namespace gs {
@@ -54,15 +56,40 @@ template <typename T> struct Lane<T, 2> {
     static __device__ __forceinline__ void get(raw r, float (&f)[2]) { unpack2<T>(r, f[0], f[1]); }
     static __device__ __forceinline__ raw put(const float (&f)[2]) { return pack2<T>(f[0], f[1]); }
 };
-template <typename R> __device__ __forceinline__ R zero_raw() { return R(0.0f); }
-template <> __device__ __forceinline__ uint32_t zero_raw<uint32_t>() { return 0u; }
+// the same value in all of a lane's channels
+template <typename T, int V> __device__ __forceinline__ typename Lane<T, V>::raw all_of(float x)
+{
+    float f[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) f[v] = x;
+    return Lane<T, V>::put(f);
+}
 
+// Powers of two and reciprocals as the special-function units have them, 2^-22 and 2^-23 of the result; below 2^-126 they are zero.
+__device__ __forceinline__ float power_of_two(float y)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float y)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+    return r;
+}
+// exp(z) = 2^y, y = z log2(e).  Rounding y costs |z| 2^-24 of the result, which tensors of 16 bits do not see; fp32 tensors get the first
+// term of what it left out back.
+template <typename T> __device__ __forceinline__ float exp_of(float z) { return power_of_two(1.44269504f * z); }
+template <> __device__ __forceinline__ float exp_of<float>(float z)
+{
+    asm("min.NaN.f32 %0, %0, 0f42C80000;\n\tmax.NaN.f32 %0, %0, 0fC2C80000;" : "+f"(z));    // to [-100, 100]: infinities have no remainder
+    const float y = 1.44269504f * z, rest = fmaf(1.44269504f, z, -y) + 1.92596299e-8f * z;
+    return power_of_two(y) * fmaf(0.693147181f, rest, 1.0f);
+}
 // 1 - a = 1 / (1 + exp(z)), to a few units of its own last place however small it is: from a rounded a it would have no
-// digits left where a channel remembers for long.  exp(z) in fp32 has its argument's product with log2(e) rounded, |z| 2^-24
-// of the result, which tensors of 16 bits do not see; fp32 tensors take the library's.
-template <typename T> __device__ __forceinline__ float exp_of(float z) { return __expf(z); }
-template <> __device__ __forceinline__ float exp_of<float>(float z) { return expf(z); }
-template <typename T> __device__ __forceinline__ float shut_of(float z) { return __fdividef(1.0f, 1.0f + exp_of<T>(z)); }
+// digits left where a channel remembers for long.
+template <typename T> __device__ __forceinline__ float shut_of(float z) { return reciprocal(1.0f + exp_of<T>(z)); }
 
 // a h + (1 - a) x from u = 1 - a: h - u h is rounded once, so a state that is kept for long loses nothing to a rounded a, and
 // one that is given up (u = 1) leaves nothing behind
@@ -73,7 +100,7 @@ __device__ __forceinline__ float advance(float u, float h, float x) { return fma
 template <typename T>
 __device__ __forceinline__ float gate_of(float z, float &u)
 {
-    const float e = exp_of<T>(-fabsf(z)), larger = __fdividef(1.0f, 1.0f + e), m = e * larger;
+    const float e = exp_of<T>(-fabsf(z)), larger = reciprocal(1.0f + e), m = e * larger;
     const bool shut = signbit(z);
     u = shut ? larger : m;
     return shut ? -m : m;
@@ -120,29 +147,37 @@ struct Walker {
 };
 
 // Inputs wait in shared memory, each in a place that only the lane that asked for it reads again: no registers are held while they are on
-// their way, and no barrier is needed when they have come.
+// their way, and no barrier is needed when they have come.  In the places of positions that are not valid stands `without`, a gate that is open
+// (a = 1) or a zero, so that what is computed from them changes nothing and needs no test.
 template <typename R>
 struct Stage {
     R (*place)[32];                       // [step][lane]
     int lane;
     template <typename W>
-    __device__ __forceinline__ void fetch(const W &from, int valid)
+    __device__ __forceinline__ void fetch(const W &from, int valid, R without)
     {
         if constexpr (sizeof(R) == 4) {
             const uint32_t to = (uint32_t)__cvta_generic_to_shared(&place[0][lane]);
+            if (valid == STEPS) {
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s)
-                if (s < valid)
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + s * 128), "l"(&from[s]) : "memory");
+                for (int s = 0; s < STEPS; ++s) copy(to + s * 128, &from[s]);
+            } else {
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+                    if (s < valid) copy(to + s * 128, &from[s]);
+                    else place[s][lane] = without;
+            }
         } else {                          // two bytes are less than such a copy moves
             R r[STEPS];
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s)
-                if (s < valid) r[s] = from[s];
+            for (int s = 0; s < STEPS; ++s) r[s] = s < valid ? from[s] : without;
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s)
-                if (s < valid) place[s][lane] = r[s];
+            for (int s = 0; s < STEPS; ++s) place[s][lane] = r[s];
         }
+    }
+    static __device__ __forceinline__ void copy(uint32_t to, const R *from)
+    {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
     }
     __device__ __forceinline__ R operator[](int s) const { return place[s][lane]; }
 };
@@ -287,8 +322,8 @@ __global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan
     auto item = first_item<CLUSTER, false>(a, group, groups);
     Place next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
     auto fetch = [&](const Place &p, int turn) {
-        Stage<raw>{stages + (2 * turn) * ROWS, lane}.fetch(Walker<T, V>(a.gate, p), p.valid);
-        Stage<raw>{stages + (2 * turn + 1) * ROWS, lane}.fetch(Walker<T, V>(a.x, p), p.valid);
+        Stage<raw>{stages + (2 * turn) * ROWS, lane}.fetch(Walker<T, V>(a.gate, p), p.valid, all_of<T, V>(INFINITY));
+        Stage<raw>{stages + (2 * turn + 1) * ROWS, lane}.fetch(Walker<T, V>(a.x, p), p.valid, all_of<T, V>(0.0f));
     };
     fetch(next, 0);
     fetches_end();
@@ -321,18 +356,17 @@ __global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = 0.0f, pn[v] = 1.0f;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-            if (s < p.valid) {
-                float zf[V], xf[V];
-                Lane<T, V>::get(z[s], zf);
-                Lane<T, V>::get(x[s], xf);
+        for (int s = 0; s < STEPS; ++s) {
+            float zf[V], xf[V];
+            Lane<T, V>::get(z[s], zf);
+            Lane<T, V>::get(x[s], xf);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    u[s][v] = shut_of<T>(zf[v]);
-                    h[v] = advance(u[s][v], h[v], xf[v]);
-                    pn[v] = fmaf(-u[s][v], pn[v], pn[v]);
-                }
+            for (int v = 0; v < V; ++v) {
+                u[s][v] = shut_of<T>(zf[v]);
+                h[v] = advance(u[s][v], h[v], xf[v]);
+                pn[v] = fmaf(-u[s][v], pn[v], pn[v]);
             }
+        }
         if (CLUSTER || a.stretches > 1) {
             joins.join(pn, h, carry, into, h, h);
         } else {
@@ -340,19 +374,24 @@ __global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan
             for (int v = 0; v < V; ++v) into[v] = carry[v];
         }
         const Walker<T, V> out(a.out, p);
+        auto write = [&](auto full_stretch) {
+            constexpr bool whole = decltype(full_stretch)::value;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-            if (s < p.rows) {
+            for (int s = 0; s < STEPS; ++s) {
                 float o[V];
+                Lane<T, V>::get(x[s], o);
 #pragma unroll
-                for (int v = 0; v < V; ++v) o[v] = 0.0f;
-                if (s < p.valid) {
-                    Lane<T, V>::get(x[s], o);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) o[v] = into[v] = advance(u[s][v], into[v], o[v]);
+                for (int v = 0; v < V; ++v) {
+                    o[v] = into[v] = advance(u[s][v], into[v], o[v]);
+                    if (!whole && s >= p.valid) o[v] = 0.0f;
                 }
-                if (p.writes) out[s] = Lane<T, V>::put(o);
+                if (whole || s < p.rows) out[s] = Lane<T, V>::put(o);
             }
+        };
+        if (p.writes) {
+            if (p.valid == STEPS) write(std::true_type());
+            else write(std::false_type());
+        }
         if (p.writes && warp == a.stretches - 1 && p.k < a.spans) {
             float *to = p.k < a.spans - 1 ? (a.states ? a.states + (p.b * (a.spans - 1) + p.k) * a.channels : nullptr)
                                           : (a.final_state ? a.final_state + p.b * a.channels : nullptr);
@@ -381,9 +420,9 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
     auto item = first_item<CLUSTER, true>(a, group, groups);
     Place next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
     auto fetch = [&](const Place &p, int turn) {
-        Stage<raw>{stages + (3 * turn) * ROWS, lane}.fetch(Walker<T, V>(a.gate, p), p.valid);
-        Stage<raw>{stages + (3 * turn + 1) * ROWS, lane}.fetch(Walker<T, V>(a.x, p), p.valid);
-        if (a.dout.p) Stage<raw>{stages + (3 * turn + 2) * ROWS, lane}.fetch(Walker<T, V>(a.dout, p), p.valid);
+        Stage<raw>{stages + (3 * turn) * ROWS, lane}.fetch(Walker<T, V>(a.gate, p), p.valid, all_of<T, V>(INFINITY));
+        Stage<raw>{stages + (3 * turn + 1) * ROWS, lane}.fetch(Walker<T, V>(a.x, p), p.valid, all_of<T, V>(0.0f));
+        Stage<raw>{stages + (3 * turn + 2) * ROWS, lane}.fetch(Walker<T, V>(a.dout, p), a.dout.p ? p.valid : 0, all_of<T, V>(0.0f));
     };
     fetch(next, 0);
     fetches_end();
@@ -423,21 +462,20 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
 #pragma unroll
         for (int v = 0; v < V; ++v) hn[v] = 0.0f, pn[v] = 1.0f, rn[v] = 0.0f;
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-            if (s < p.valid) {
-                float zf[V], xf[V], gf[V];
-                Lane<T, V>::get(z[s], zf);
-                Lane<T, V>::get(x[s], xf);
-                Lane<T, V>::get(a.dout.p ? g[s] : zero_raw<raw>(), gf);
+        for (int s = 0; s < STEPS; ++s) {
+            float zf[V], xf[V], gf[V];
+            Lane<T, V>::get(z[s], zf);
+            Lane<T, V>::get(x[s], xf);
+            Lane<T, V>::get(g[s], gf);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    float shut;
-                    u[s][v] = gate_of<T>(zf[v], shut);
-                    hn[v] = advance(shut, hn[v], xf[v]);
-                    pn[v] = fmaf(-shut, pn[v], pn[v]);
-                    rn[v] = fmaf(pn[v], gf[v], rn[v]);
-                }
+            for (int v = 0; v < V; ++v) {
+                float shut;
+                u[s][v] = gate_of<T>(zf[v], shut);
+                hn[v] = advance(shut, hn[v], xf[v]);
+                pn[v] = fmaf(-shut, pn[v], pn[v]);
+                rn[v] = fmaf(pn[v], gf[v], rn[v]);
             }
+        }
         if (CLUSTER || a.stretches > 1) {
             joins.join(pn, rn, carry, into, hn, h);
         } else {
@@ -446,41 +484,42 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
         }
         float d[STEPS][V];                                           // a (1 - a) (h_(t-1) - x_t)
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-            if (s < p.valid) {
-                float xf[V];
-                Lane<T, V>::get(x[s], xf);
+        for (int s = 0; s < STEPS; ++s) {
+            float xf[V];
+            Lane<T, V>::get(x[s], xf);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float m = fabsf(u[s][v]);
+                u[s][v] = signbit(u[s][v]) ? 1.0f - m : m;
+                d[s][v] = fmaf(-m, m, m) * (h[v] - xf[v]);
+                h[v] = advance(u[s][v], h[v], xf[v]);
+            }
+        }
+        const Walker<T, V> at_dx(a.dx, p), at_dz(a.dgate, p);
+        auto write = [&](auto full_stretch) {
+            constexpr bool whole = decltype(full_stretch)::value;
+#pragma unroll
+            for (int s = STEPS - 1; s >= 0; --s) {
+                float gf[V], dx[V], dz[V];
+                Lane<T, V>::get(g[s], gf);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const float m = fabsf(u[s][v]);
-                    u[s][v] = signbit(u[s][v]) ? 1.0f - m : m;
-                    d[s][v] = fmaf(-m, m, m) * (h[v] - xf[v]);
-                    h[v] = advance(u[s][v], h[v], xf[v]);
+                    const float full = gf[v] + into[v];
+                    dx[v] = u[s][v] * full;
+                    into[v] = full - dx[v];
+                    dz[v] = d[s][v] * full;
+                    if (!whole && s >= p.valid) dx[v] = dz[v] = 0.0f;
                 }
-            }
-        const Walker<T, V> at_dx(a.dx, p), at_dz(a.dgate, p);
-#pragma unroll
-        for (int s = STEPS - 1; s >= 0; --s)
-            if (s < p.rows) {
-                float dx[V], dz[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) dx[v] = dz[v] = 0.0f;
-                if (s < p.valid) {
-                    float gf[V];
-                    Lane<T, V>::get(a.dout.p ? g[s] : zero_raw<raw>(), gf);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        const float full = gf[v] + into[v];
-                        dx[v] = u[s][v] * full;
-                        into[v] = full - dx[v];
-                        dz[v] = d[s][v] * full;
-                    }
-                }
-                if (p.writes) {
+                if (whole || s < p.rows) {
                     at_dx[s] = Lane<T, V>::put(dx);
                     at_dz[s] = Lane<T, V>::put(dz);
                 }
             }
+        };
+        if (p.writes) {
+            if (p.valid == STEPS) write(std::true_type());
+            else write(std::false_type());
+        }
         if (a.dh0 && p.writes && p.k == 0 && warp == 0)
 #pragma unroll
             for (int v = 0; v < V; ++v) a.dh0[p.b * a.channels + p.c + v] = into[v];

@@ -13,11 +13,12 @@ Backward, from given statistics, X = mean |g xh|, G = mean |g|:
   dweight, dbias: rows of a team (148 blocks at least, or one row each) <= rows / 148 + 1, then 32 teams, 148 eighths of the
   blocks and 8 of those: (rows / 148 + 190 + 4) e of the sum of magnitudes, + u of the result.
 
-Recurrence.  m = min(a, 1 - a) is off by 10 e of itself (exp 2 ulp, quotient 2 ulp, sum); a step of the state by 3 e of the states'
-magnitudes H (recursion over magnitudes; the products of stretches and their joins among them) and 10 e m (H + |x|):
-  E_t = a_t E_(t-1) + 3 e (H_t + H_(t-1)) + 12 e m (H_(t-1) + |x|)
+Recurrence.  m = min(a, 1 - a) is off by 10 e of itself (exp 2 ulp, quotient 2 ulp, sum), for 16-bit tensors by 2 |z| e more (the product
+z log2(e) is rounded); a step of the state by 3 e of the states' magnitudes H (recursion over magnitudes; the products of stretches and
+their joins among them) and that of m (H + |x|):
+  E_t = a_t E_(t-1) + 3 e (H_t + H_(t-1)) + (12 + 2 |z|) e m (H_(t-1) + |x|)
 and likewise for r = a g with the magnitudes of its own recursion.  dx = (1 - a) g: (1 - a) E_g + 12 e |dx|;
-dgate = a (1 - a) d g: a (1 - a) (|g| (E_h + 3 e |d|) + |d| E_g) + 25 e |dgate|; + u of each result.
+dgate = a (1 - a) d g: a (1 - a) (|g| (E_h + 3 e |d|) + |d| E_g) + (25 + 4 |z|) e |dgate|; + u of each result.
 """
 import torch
 
@@ -86,7 +87,8 @@ def recurrence(gate, x, h0=None, lens=None, dout=None, dfinal=None):
     on = valid_rows(lens, b, n, x.device)
     z = gate.double().masked_fill(~on, 0.0)
     a, u = torch.sigmoid(z), torch.sigmoid(-z)
-    m = torch.minimum(a, u)
+    far = z.abs().clamp(max=200.0) * (0.0 if x.dtype in (torch.float32, torch.float64) else 2.0)
+    m = torch.minimum(a, u) * (12 + far)
     v = x.double().masked_fill(~on, 0.0)
     h = torch.zeros((b, c), **f64) if h0 is None else h0.double()
     big, err = h.abs(), torch.zeros((b, c), **f64)
@@ -95,7 +97,7 @@ def recurrence(gate, x, h0=None, lens=None, dout=None, dfinal=None):
     for t in range(n):
         before[:, t], err_before[:, t] = h, err
         now, size = a[:, t] * h + u[:, t] * v[:, t], a[:, t] * big + u[:, t] * v[:, t].abs()
-        e = a[:, t] * err + 3 * E32 * (size + big) + 12 * E32 * m[:, t] * (big + v[:, t].abs())
+        e = a[:, t] * err + 3 * E32 * (size + big) + E32 * m[:, t] * (big + v[:, t].abs())
         h, big, err = torch.where(on[:, t], now, h), torch.where(on[:, t], size, big), torch.where(on[:, t], e, err)
         hs[:, t], es[:, t] = h, err
     hide = lambda t: t.masked_fill(~on, 0.0)                                        # noqa: E731
@@ -114,10 +116,10 @@ def recurrence(gate, x, h0=None, lens=None, dout=None, dfinal=None):
         d = before[:, t] - v[:, t]
         dx, dz = u[:, t] * g, a[:, t] * u[:, t] * d * g
         r["dx"][:, t], r["dgate"][:, t] = dx, dz
-        r["dx_bound"][:, t] = u[:, t] * eg + 12 * E32 * dx.abs() + rounded(dx, x.dtype)
+        r["dx_bound"][:, t] = u[:, t] * eg + (12 + far[:, t]) * E32 * dx.abs() + rounded(dx, x.dtype)
         r["dgate_bound"][:, t] = (a[:, t] * u[:, t] * (g.abs() * (err_before[:, t] + 3 * E32 * (before[:, t].abs() + v[:, t].abs()))
-                                                       + d.abs() * eg) + 25 * E32 * dz.abs() + rounded(dz, x.dtype))
-        e = a[:, t] * eg + 3 * E32 * (a[:, t] * size + size) + 12 * E32 * m[:, t] * size
+                                                       + d.abs() * eg) + (25 + 2 * far[:, t]) * E32 * dz.abs() + rounded(dz, x.dtype))
+        e = a[:, t] * eg + 3 * E32 * (a[:, t] * size + size) + E32 * m[:, t] * size
         back = torch.where(on[:, t], a[:, t] * g, back)
         big, err = torch.where(on[:, t], a[:, t] * size, big), torch.where(on[:, t], e, err)
     r["dh0"], r["dh0_bound"] = back, err + E32 * back.abs() + 1e-38
