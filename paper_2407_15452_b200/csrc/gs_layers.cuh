@@ -84,6 +84,15 @@ template <> struct Wide<float> { static constexpr int N = 4; };
 template <> struct Wide<__half> { static constexpr int N = 8; };
 template <> struct Wide<__nv_bfloat16> { static constexpr int N = 8; };
 
+// calls f(T()) with the type of a dtype
+template <typename F>
+static gs_status with_type(int32_t dtype, F &&f)
+{
+    if (dtype == GS_TABLE_F32) return f(float());
+    if (dtype == GS_TABLE_F16) return f(__half());
+    return f(__nv_bfloat16());
+}
+
 // ---- rows -------------------------------------------------------------------------------
 // n / d for n < 2^31 as a multiplication: m = floor(2^(31+s) / d) + 1 with 2^s >= d, so that n m / 2^(31+s) exceeds
 // n / d by less than n / 2^(31+s) <= 1 / d and has the same whole part.

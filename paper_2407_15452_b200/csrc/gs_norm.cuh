@@ -138,14 +138,6 @@ static gs_status with_team(int columns, bool aligned, F &&launch)
     return launch(Team<1, 32, 0, true>(), block(32));
 }
 
-template <typename F>
-static gs_status with_type(int32_t dtype, F &&f)
-{
-    if (dtype == GS_TABLE_F32) return f(float());
-    if (dtype == GS_TABLE_F16) return f(__half());
-    return f(__nv_bfloat16());
-}
-
 // gs_norm_forward.cu, gs_norm_backward.cu
 gs_status norm_forward(const NormArgs &a, int32_t dtype, bool aligned, cudaStream_t st);
 gs_status norm_backward(const NormArgs &a, int32_t dtype, bool aligned, void *dweight, void *dbias, cudaStream_t st);

@@ -56,15 +56,6 @@ template <typename T> struct Lane<T, 2> {
     static __device__ __forceinline__ void get(raw r, float (&f)[2]) { unpack2<T>(r, f[0], f[1]); }
     static __device__ __forceinline__ raw put(const float (&f)[2]) { return pack2<T>(f[0], f[1]); }
 };
-// the same value in all of a lane's channels
-template <typename T, int V> __device__ __forceinline__ typename Lane<T, V>::raw all_of(float x)
-{
-    float f[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) f[v] = x;
-    return Lane<T, V>::put(f);
-}
-
 // Powers of two and reciprocals as the special-function units have them, 2^-22 and 2^-23 of the result; below 2^-126 they are zero.
 __device__ __forceinline__ float power_of_two(float y)
 {
@@ -107,83 +98,98 @@ __device__ __forceinline__ float gate_of(float z, float &u)
 }
 
 struct Place {                            // what a warp works on: positions [t0, t0 + rows) of a chain, `valid` of them valid
-    int64_t b;                            // sequence
-    uint32_t c;                           // the lane's first channel
-    bool on, writes;                      // the warp has a chain; the lane has a channel (one that has none reads another's)
+    int64_t b, c;                         // sequence; the warp's first channel
     int k, t0, rows, valid;               // k: the span
+    bool on;                              // the lane has a channel, and the warp a chain
 };
 
 template <int V>
 __device__ __forceinline__ Place place_of(const ScanArgs &a, int64_t chain, int lane, int k, int warp)
 {
     Place p;
-    p.on = chain < a.chains;
-    p.b = p.on ? a.by_slabs.of(chain) : 0;
-    p.c = p.on ? (uint32_t)(chain - p.b * a.slabs) * (32 * V) + lane * V : 0;
-    p.writes = p.on && p.c < a.channels;
-    if (!p.writes) p.c = 0;
+    const bool there = chain < a.chains;
+    p.b = there ? a.by_slabs.of(chain) : 0;
+    p.c = there ? (chain - p.b * a.slabs) * (32 * V) : 0;
+    p.on = there && p.c + lane * V < a.channels;
     p.k = k;
     p.t0 = k * SPAN + warp * a.steps;
-    p.rows = p.on ? min(max(a.length - p.t0, 0), a.steps) : 0;
-    const int len = a.lens && p.on ? min(max(__ldg(a.lens + p.b), 0), a.length) : a.length;
+    p.rows = there ? min(max(a.length - p.t0, 0), a.steps) : 0;
+    const int len = a.lens && there ? min(max(__ldg(a.lens + p.b), 0), a.length) : a.length;
     p.valid = min(p.rows, max(len - p.t0, 0));
     return p;
 }
 
-// A lane's channels of one tensor at position t0 + s.  The warp's part of the address is the same in all its lanes, so the
-// accesses of a stretch need one register of each.
-template <typename T, int V>
-struct Walker {
-    typedef typename Lane<T, V>::raw raw;
-    char *p;                              // of the warp
-    int64_t step;
-    uint32_t lane;
-    __device__ __forceinline__ Walker(const ScanTensor &t, const Place &at)
-        : p(static_cast<char *>(t.p) + (at.b * t.sb + at.t0 * t.st) * (int64_t)sizeof(T)), step(t.st * (int64_t)sizeof(T)),
-          lane(at.c * (uint32_t)sizeof(T))
-    {
-    }
-    __device__ __forceinline__ raw &operator[](int s) const { return *reinterpret_cast<raw *>(p + s * step + lane); }
-};
-
-// Inputs wait in shared memory, each in a place that only the lane that asked for it reads again: no registers are held while they are on
-// their way, and no barrier is needed when they have come.  In the places of positions that are not valid stands `without`, a gate that is open
-// (a = 1) or a zero, so that what is computed from them changes nothing and needs no test.
-template <typename R>
+// A warp's stretch of one tensor in shared memory, [step][lane].  Lanes bring (and take away) CHUNK bytes each, 16 where the tensors' rows are
+// aligned to that, so that a stretch is four copies of a warp; each lane computes with its own channels of every position.  No registers
+// are held while inputs are on their way.  In the places of positions that are not valid stands `without`, a gate that is open (a = 1) or a zero, so that
+// what is computed from them changes nothing and needs no test.
+template <typename T, int V, int CHUNK>
 struct Stage {
-    R (*place)[32];                       // [step][lane]
+    typedef typename Lane<T, V>::raw raw;
+    static constexpr int ROW = 32 * (int)sizeof(raw), ACROSS = ROW / CHUNK, AT_ONCE = 32 / ACROSS, ROUNDS = STEPS / AT_ONCE;
+    static constexpr int BYTES = STEPS * ROW;
+    char *room;
     int lane;
-    template <typename W>
-    __device__ __forceinline__ void fetch(const W &from, int valid, R without)
+
+    __device__ __forceinline__ raw &operator[](int s) const { return *reinterpret_cast<raw *>(room + s * ROW + lane * sizeof(raw)); }
+    __device__ __forceinline__ char *global(const ScanTensor &t, const Place &p) const
     {
-        if constexpr (sizeof(R) == 4) {
-            const uint32_t to = (uint32_t)__cvta_generic_to_shared(&place[0][lane]);
-            if (valid == STEPS) {
+        return static_cast<char *>(t.p) + (p.b * t.sb + (p.t0 + lane / ACROSS) * t.st + p.c) * (int64_t)sizeof(T) + lane % ACROSS * CHUNK;
+    }
+    __device__ __forceinline__ bool inside(const ScanArgs &a, const Place &p) const
+    {
+        return p.c + lane % ACROSS * (CHUNK / (int)sizeof(T)) < a.channels;
+    }
+    __device__ __forceinline__ void fetch(const ScanArgs &a, const ScanTensor &t, const Place &p, int valid, uint32_t without) const
+    {
+        const char *from = global(t, p);
+        const int64_t step = AT_ONCE * t.st * (int64_t)sizeof(T);
+        const bool in = inside(a, p);
+        char *to = room + lane * CHUNK;
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s) copy(to + s * 128, &from[s]);
-            } else {
-#pragma unroll
-                for (int s = 0; s < STEPS; ++s)
-                    if (s < valid) copy(to + s * 128, &from[s]);
-                    else place[s][lane] = without;
-            }
-        } else {                          // two bytes are less than such a copy moves
-            R r[STEPS];
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) r[s] = s < valid ? from[s] : without;
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) place[s][lane] = r[s];
+        for (int i = 0; i < ROUNDS; ++i, from += step, to += 32 * CHUNK) {
+            if (i * AT_ONCE + lane / ACROSS < valid) {
+                if (!in) continue;
+                if constexpr (CHUNK == 2) *reinterpret_cast<uint16_t *>(to) = *reinterpret_cast<const uint16_t *>(from);
+                else if constexpr (CHUNK == 4)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+                else
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+            } else if constexpr (CHUNK == 2) *reinterpret_cast<uint16_t *>(to) = (uint16_t)without;
+            else if constexpr (CHUNK == 4) *reinterpret_cast<uint32_t *>(to) = without;
+            else *reinterpret_cast<uint4 *>(to) = make_uint4(without, without, without, without);
         }
     }
-    static __device__ __forceinline__ void copy(uint32_t to, const R *from)
+    // positions that are not valid are written as zeros
+    __device__ __forceinline__ void write(const ScanArgs &a, const ScanTensor &t, const Place &p) const
     {
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+        char *to = global(t, p);
+        const int64_t step = AT_ONCE * t.st * (int64_t)sizeof(T);
+        const bool in = inside(a, p);
+        const char *from = room + lane * CHUNK;
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i, to += step, from += 32 * CHUNK) {
+            const int s = i * AT_ONCE + lane / ACROSS;
+            if (!in || s >= p.rows) continue;
+            if constexpr (CHUNK == 2) *reinterpret_cast<uint16_t *>(to) = s < p.valid ? *reinterpret_cast<const uint16_t *>(from) : (uint16_t)0;
+            else if constexpr (CHUNK == 4) *reinterpret_cast<uint32_t *>(to) = s < p.valid ? *reinterpret_cast<const uint32_t *>(from) : 0u;
+            else *reinterpret_cast<uint4 *>(to) = s < p.valid ? *reinterpret_cast<const uint4 *>(from) : make_uint4(0u, 0u, 0u, 0u);
+        }
     }
-    __device__ __forceinline__ R operator[](int s) const { return place[s][lane]; }
 };
+// a value as the words that its tensor holds
+template <typename T> __device__ __forceinline__ uint32_t words_of(float x)
+{
+    if constexpr (sizeof(T) == 4) return __float_as_uint(x);
+    else return pack2<T>(x, x);
+}
 __device__ __forceinline__ void fetches_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// all but the latest group of this thread's fetches have come
-__device__ __forceinline__ void fetches_wait() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+// all but the latest group of the warp's fetches have come
+__device__ __forceinline__ void fetches_wait()
+{
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncwarp();
+}
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -193,86 +199,104 @@ __device__ __forceinline__ uint32_t cluster_rank()
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-// stores a pair into the shared memory of another block of the cluster, at the place that `local` has in this one
-__device__ __forceinline__ void store_remote(const float2 *local, uint32_t rank, float2 v)
-{
-    uint32_t there;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(v.x), "f"(v.y) : "memory");
-}
-
-// Joins of stretches, (P, B) each.  BACK: the chain runs from the last stretch to the first.  A block's pairs are published, read by
-// all its warps after a barrier, and may be overwritten after the next one (of the block or the cluster) that `join` ends with.
-template <int V, bool CLUSTER, bool BACK>
-struct Joins {
-    float2 (*part)[32 * V];                          // [stretch][channel]: of this block
-    float2 (*span)[MOST_BLOCKS][32 * V];             // [2 in turn][rank][channel]: of the cluster's blocks
-    float (*ahead)[32 * V];                          // [stretch][channel]: B of the stretches in the other direction
-    int stretches, blocks, rank, warp, lane, first;  // first: index of the block's warp that has this chain's first stretch
-    int turn;
-
-    // p, b: of this warp's stretch; carry: into the window, moved over it; into: into this stretch.  With `ahead`: h, the state
-    // before the block's span, and hb, its B over this stretch; h becomes the state before the stretch.
-    __device__ __forceinline__ void join(const float (&p)[V], const float (&b)[V], float (&carry)[V], float (&into)[V],
-                                         const float (&hb)[V], float (&h)[V])
+// A lane's share of the affine function of a stretch, x -> p x + b
+template <int V> struct alignas(8 * V) Affine {
+    float p[V], b[V];
+    __device__ __forceinline__ void after(const Affine &first)          // this one behind `first`
     {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            part[first + warp][v * 32 + lane] = make_float2(p[v], b[v]);
-            if (BACK) ahead[first + warp][v * 32 + lane] = hb[v];
+            b[v] = fmaf(p[v], first.b[v], b[v]);
+            p[v] *= first.p[v];
         }
-        __syncthreads();
-        const int before = BACK ? stretches - 1 - warp : warp;
-        if (BACK)
-            for (int i = 0; i < warp; ++i)
+    }
+    __device__ __forceinline__ void apply(float (&x)[V]) const
+    {
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    h[v] = fmaf(part[first + i][v * 32 + lane].x, h[v], ahead[first + i][v * 32 + lane]);
-        if (!CLUSTER) {
+        for (int v = 0; v < V; ++v) x[v] = fmaf(p[v], x[v], b[v]);
+    }
+};
+// stores into the shared memory of another block of the cluster, at the place that `local` has in this one
+template <int V>
+__device__ __forceinline__ void store_remote(const Affine<V> *local, uint32_t rank, const Affine<V> &f)
+{
+    uint32_t there;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
+    if constexpr (V == 2)
+        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(f.p[0]), "f"(f.p[1]), "f"(f.b[0]), "f"(f.b[1]) : "memory");
+    else
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(f.p[0]), "f"(f.b[0]) : "memory");
+}
+
+// The functions of a window's stretches, and of a cluster's spans, where the warps that need them find them.  BACK: the chain runs
+// from the last stretch to the first, and beside it h from the first to the last (with the same p, and `ahead` for its b).
+// Places are used in turn (those of a block's stretches only if the block is no cluster's: there a barrier of the cluster lies between
+// the last read and the next write).
+template <int V, bool CLUSTER, bool BACK>
+struct Board {
+    static constexpr int TURNS = CLUSTER ? 1 : 2;
+    Affine<V> stretch[TURNS][WARPS][32];
+    float ahead[BACK ? TURNS : 1][BACK ? WARPS : 1][32][V];
+    Affine<V> span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32];
+};
+template <int V, bool CLUSTER, bool BACK>
+struct Joins {
+    Board<V, CLUSTER, BACK> &board;
+    int stretches, blocks, rank, warp, lane, first;  // first: index of the block's warp that has this chain's first stretch
+    int turn;
+    Affine<V> before;                                // of what lies between the block's edge and this warp's stretch
+
+    // Gives away the function of this warp's stretch and hb, the b of h over it; h moves from the state before the block's first stretch to
+    // that before this one.
+    __device__ __forceinline__ void give(const Affine<V> &own, const float (&hb)[V], float (&h)[V])
+    {
+        const int place = CLUSTER ? 0 : turn;
+        board.stretch[place][first + warp][lane] = own;
+        if (BACK)
+#pragma unroll
+            for (int v = 0; v < V; ++v) board.ahead[BACK ? place : 0][BACK ? first + warp : 0][lane][v] = hb[v];
+        __syncthreads();
+        if (BACK)
+            for (int i = 0; i < warp; ++i) {
+                Affine<V> f = board.stretch[place][first + i][lane];
+#pragma unroll
+                for (int v = 0; v < V; ++v) f.b[v] = board.ahead[BACK ? place : 0][BACK ? first + i : 0][lane][v];
+                f.apply(h);
+            }
+#pragma unroll
+        for (int v = 0; v < V; ++v) before.p[v] = 1.0f, before.b[v] = 0.0f;
+        const int count = BACK ? stretches - 1 - warp : warp;
+        for (int i = 0; i < count; ++i) {
+            Affine<V> f = board.stretch[place][first + (BACK ? stretches - 1 - i : i)][lane];
+            f.after(before);
+            before = f;
+        }
+        if (!CLUSTER) return;
+        if (count == WARPS - 1) {                    // this stretch ends the block's span
+            Affine<V> all = own;
+            all.after(before);
+            for (int r = 0; r < blocks; ++r) store_remote(&board.span[turn][rank][lane], r, all);
+        }
+        cluster_arrive();
+    }
+    // carry: the state (or r) at the window's edge, moved over the window; into: at this stretch's
+    __device__ __forceinline__ void take(float (&carry)[V], float (&into)[V])
+    {
+        if (CLUSTER) {
+            cluster_wait();
+            for (int i = 0; i < blocks; ++i) {
+                const int k = BACK ? blocks - 1 - i : i;
+                if (k == rank)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) into[v] = carry[v];
+                board.span[CLUSTER ? turn : 0][CLUSTER ? k : 0][lane].apply(carry);
+            }
+        } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) into[v] = carry[v];
-            for (int i = 0; i < before; ++i) {
-                const int w = first + (BACK ? stretches - 1 - i : i);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float2 s = part[w][v * 32 + lane];
-                    into[v] = fmaf(s.x, into[v], s.y);
-                }
-            }
-            __syncthreads();
-            return;
         }
-        // the block's span, which every warp joins for itself (and what comes before its stretch on the way); each of
-        // them hands it to one block
-        float2 all[V], own[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) own[v] = all[v] = make_float2(1.0f, 0.0f);
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) {
-            const int w = BACK ? WARPS - 1 - i : i;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float2 s = part[w][v * 32 + lane];
-                if (i == before) own[v] = all[v];
-                all[v].y = fmaf(s.x, all[v].y, s.y);
-                all[v].x *= s.x;
-            }
-        }
-        if (warp < blocks)
-#pragma unroll
-            for (int v = 0; v < V; ++v) store_remote(&span[turn][rank][v * 32 + lane], warp, all[v]);
-        cluster_arrive();
-        cluster_wait();
-        for (int i = 0; CLUSTER && i < blocks; ++i) {
-            const int k = BACK ? blocks - 1 - i : i;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float2 s = span[turn][k][v * 32 + lane];
-                if (k == rank) into[v] = fmaf(own[v].x, carry[v], own[v].y);
-                carry[v] = fmaf(s.x, carry[v], s.y);
-            }
-        }
-        turn ^= 1;                        // written again two windows later, behind a barrier that follows every read
+        before.apply(into);
+        turn ^= 1;
     }
 };
 
@@ -305,35 +329,45 @@ __device__ __forceinline__ Items<CLUSTER, BACK> first_item(const ScanArgs &a, in
     return it;
 }
 
-template <typename T, int V, bool CLUSTER>
+template <int V>
+__device__ __forceinline__ void load_state(const float *from, int64_t row, int64_t channels, const Place &p, int lane, float (&h)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = from && p.on ? from[row * channels + p.c + lane * V + v] : 0.0f;
+}
+template <int V>
+__device__ __forceinline__ void store_state(float *to, int64_t row, int64_t channels, const Place &p, int lane, const float (&h)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (to && p.on) to[row * channels + p.c + lane * V + v] = h[v];
+}
+
+template <typename T, int V, int CHUNK, bool CLUSTER>
 __global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan_forward_kernel(const __grid_constant__ ScanArgs a)
 {
-    typedef typename Lane<T, V>::raw raw;
-    __shared__ float2 part[WARPS][32 * V];
-    __shared__ float2 span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32 * V];
-    extern __shared__ uint32_t room[];                               // [2 in turn][gate, x][warp][step][lane]
+    typedef Stage<T, V, CHUNK> S;
+    __shared__ Board<V, CLUSTER, false> board;
+    extern __shared__ uint4 room[];                                  // [2 in turn][warp][gate, x]
     const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
     const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
-    raw (*stages)[32] = reinterpret_cast<raw(*)[32]>(room) + index * STEPS;
-    constexpr int ROWS = WARPS * STEPS;
     if (CLUSTER) cluster_arrive();                      // completed by the wait before the first remote store
 
     auto item = first_item<CLUSTER, false>(a, group, groups);
     Place next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
+    auto stage = [&](int turn, int which) { return S{reinterpret_cast<char *>(room) + ((turn * WARPS + index) * 2 + which) * S::BYTES, lane}; };
     auto fetch = [&](const Place &p, int turn) {
-        Stage<raw>{stages + (2 * turn) * ROWS, lane}.fetch(Walker<T, V>(a.gate, p), p.valid, all_of<T, V>(INFINITY));
-        Stage<raw>{stages + (2 * turn + 1) * ROWS, lane}.fetch(Walker<T, V>(a.x, p), p.valid, all_of<T, V>(0.0f));
+        stage(turn, 0).fetch(a, a.gate, p, p.valid, words_of<T>(INFINITY));
+        stage(turn, 1).fetch(a, a.x, p, p.valid, 0u);
+        fetches_end();
     };
     fetch(next, 0);
-    fetches_end();
 
-    Joins<V, CLUSTER, false> joins = {part, reinterpret_cast<float2(*)[MOST_BLOCKS][32 * V]>(span), nullptr,
-                                      a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
+    Joins<V, CLUSTER, false> joins = {board, a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
     float carry[V], into[V];
     if (CLUSTER) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) carry[v] = a.h0 ? a.h0[next.b * a.channels + next.c + v] : 0.0f;
+        load_state<V>(a.h0, next.b, a.channels, next, lane, carry);
         cluster_wait();
     }
     bool more;
@@ -344,17 +378,17 @@ __global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan
         if (more) {
             next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
             fetch(next, turn ^ 1);
+        } else {
+            fetches_end();
         }
-        fetches_end();
-        if (!CLUSTER)
-#pragma unroll
-            for (int v = 0; v < V; ++v) carry[v] = a.h0 ? a.h0[p.b * a.channels + p.c + v] : 0.0f;
+        if (!CLUSTER) load_state<V>(a.h0, p.b, a.channels, p, lane, carry);
         fetches_wait();
-        const Stage<raw> z = {stages + (2 * turn) * ROWS, lane}, x = {stages + (2 * turn + 1) * ROWS, lane};
+        const S z = stage(turn, 0), x = stage(turn, 1);
         turn ^= 1;
-        float u[STEPS][V], h[V], pn[V];
+        float u[STEPS][V], h[V];
+        Affine<V> own;
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = 0.0f, pn[v] = 1.0f;
+        for (int v = 0; v < V; ++v) h[v] = 0.0f, own.p[v] = 1.0f;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             float zf[V], xf[V];
@@ -364,75 +398,62 @@ __global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan
             for (int v = 0; v < V; ++v) {
                 u[s][v] = shut_of<T>(zf[v]);
                 h[v] = advance(u[s][v], h[v], xf[v]);
-                pn[v] = fmaf(-u[s][v], pn[v], pn[v]);
+                own.p[v] = fmaf(-u[s][v], own.p[v], own.p[v]);
             }
         }
         if (CLUSTER || a.stretches > 1) {
-            joins.join(pn, h, carry, into, h, h);
+#pragma unroll
+            for (int v = 0; v < V; ++v) own.b[v] = h[v];
+            joins.give(own, h, h);
+            joins.take(carry, into);
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) into[v] = carry[v];
         }
-        const Walker<T, V> out(a.out, p);
-        auto write = [&](auto full_stretch) {
-            constexpr bool whole = decltype(full_stretch)::value;
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                float o[V];
-                Lane<T, V>::get(x[s], o);
+        for (int s = 0; s < STEPS; ++s) {
+            float o[V];
+            Lane<T, V>::get(x[s], o);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    o[v] = into[v] = advance(u[s][v], into[v], o[v]);
-                    if (!whole && s >= p.valid) o[v] = 0.0f;
-                }
-                if (whole || s < p.rows) out[s] = Lane<T, V>::put(o);
-            }
-        };
-        if (p.writes) {
-            if (p.valid == STEPS) write(std::true_type());
-            else write(std::false_type());
+            for (int v = 0; v < V; ++v) o[v] = into[v] = advance(u[s][v], into[v], o[v]);
+            x[s] = Lane<T, V>::put(o);
         }
-        if (p.writes && warp == a.stretches - 1 && p.k < a.spans) {
-            float *to = p.k < a.spans - 1 ? (a.states ? a.states + (p.b * (a.spans - 1) + p.k) * a.channels : nullptr)
-                                          : (a.final_state ? a.final_state + p.b * a.channels : nullptr);
-            if (to)
-#pragma unroll
-                for (int v = 0; v < V; ++v) to[p.c + v] = into[v];
+        __syncwarp();
+        x.write(a, a.out, p);
+        if (warp == a.stretches - 1) {
+            if (p.k < a.spans - 1) store_state<V>(a.states, p.b * (a.spans - 1) + p.k, a.channels, p, lane, into);
+            else if (p.k == a.spans - 1) store_state<V>(a.final_state, p.b, a.channels, p, lane, into);
         }
+        __syncwarp();                                                // before the stage is filled again
     } while (more);
 }
 
-template <typename T, int V, bool CLUSTER>
+template <typename T, int V, int CHUNK, bool CLUSTER>
 __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_kernel(const __grid_constant__ ScanArgs a)
 {
-    typedef typename Lane<T, V>::raw raw;
-    __shared__ float2 part[WARPS][32 * V];
-    __shared__ float ahead[WARPS][32 * V];
-    __shared__ float2 span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32 * V];
-    extern __shared__ uint32_t room[];                               // [2 in turn][gate, x, dout][warp][step][lane]
+    typedef Stage<T, V, CHUNK> S;
+    __shared__ Board<V, CLUSTER, true> board;
+    extern __shared__ uint4 room[];                                  // [2 in turn][warp][gate, x, dout]
     const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
     const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
-    raw (*stages)[32] = reinterpret_cast<raw(*)[32]>(room) + index * STEPS;
-    constexpr int ROWS = WARPS * STEPS;
     if (CLUSTER) cluster_arrive();
 
     auto item = first_item<CLUSTER, true>(a, group, groups);
     Place next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
+    auto stage = [&](int turn, int which) { return S{reinterpret_cast<char *>(room) + ((turn * WARPS + index) * 3 + which) * S::BYTES, lane}; };
     auto fetch = [&](const Place &p, int turn) {
-        Stage<raw>{stages + (3 * turn) * ROWS, lane}.fetch(Walker<T, V>(a.gate, p), p.valid, all_of<T, V>(INFINITY));
-        Stage<raw>{stages + (3 * turn + 1) * ROWS, lane}.fetch(Walker<T, V>(a.x, p), p.valid, all_of<T, V>(0.0f));
-        Stage<raw>{stages + (3 * turn + 2) * ROWS, lane}.fetch(Walker<T, V>(a.dout, p), a.dout.p ? p.valid : 0, all_of<T, V>(0.0f));
+        stage(turn, 0).fetch(a, a.gate, p, p.valid, words_of<T>(INFINITY));
+        stage(turn, 1).fetch(a, a.x, p, p.valid, 0u);
+        stage(turn, 2).fetch(a, a.dout, p, a.dout.p ? p.valid : 0, 0u);
+        fetches_end();
     };
     fetch(next, 0);
-    fetches_end();
 
-    Joins<V, CLUSTER, true> joins = {part, reinterpret_cast<float2(*)[MOST_BLOCKS][32 * V]>(span), ahead,
-                                     a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
+    Joins<V, CLUSTER, true> joins = {board, a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
     float carry[V], into[V];
     if (CLUSTER) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) carry[v] = a.dfinal ? a.dfinal[next.b * a.channels + next.c + v] : 0.0f;
+        load_state<V>(a.dfinal, next.b, a.channels, next, lane, carry);
         cluster_wait();
     }
     bool more;
@@ -443,24 +464,20 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
         if (more) {
             next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
             fetch(next, turn ^ 1);
+        } else {
+            fetches_end();
         }
-        fetches_end();
         float h[V];                                                  // the state before the block's span
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int64_t at = p.b * a.channels + p.c + v;
-            if (!CLUSTER) carry[v] = a.dfinal ? a.dfinal[at] : 0.0f;
-            h[v] = 0.0f;
-            if (CLUSTER && p.k > 0 && p.k < a.spans) h[v] = a.states[(p.b * (a.spans - 1) + p.k - 1) * a.channels + p.c + v];
-            else if (p.k == 0 && a.h0) h[v] = a.h0[at];
-        }
+        if (p.k == 0) load_state<V>(a.h0, p.b, a.channels, p, lane, h);
+        else load_state<V>(p.k < a.spans ? a.states : nullptr, p.b * (a.spans - 1) + p.k - 1, a.channels, p, lane, h);
+        if (!CLUSTER) load_state<V>(a.dfinal, p.b, a.channels, p, lane, carry);
         fetches_wait();
-        const Stage<raw> z = {stages + (3 * turn) * ROWS, lane}, x = {stages + (3 * turn + 1) * ROWS, lane},
-                         g = {stages + (3 * turn + 2) * ROWS, lane};
+        const S z = stage(turn, 0), x = stage(turn, 1), g = stage(turn, 2);
         turn ^= 1;
-        float u[STEPS][V], hn[V], pn[V], rn[V];                      // u: first as gate_of has it, then 1 - a
+        float u[STEPS][V], hn[V];                                    // u: first as gate_of has it, then 1 - a
+        Affine<V> own;
 #pragma unroll
-        for (int v = 0; v < V; ++v) hn[v] = 0.0f, pn[v] = 1.0f, rn[v] = 0.0f;
+        for (int v = 0; v < V; ++v) hn[v] = 0.0f, own.p[v] = 1.0f, own.b[v] = 0.0f;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             float zf[V], xf[V], gf[V];
@@ -472,16 +489,12 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
                 float shut;
                 u[s][v] = gate_of<T>(zf[v], shut);
                 hn[v] = advance(shut, hn[v], xf[v]);
-                pn[v] = fmaf(-shut, pn[v], pn[v]);
-                rn[v] = fmaf(pn[v], gf[v], rn[v]);
+                own.p[v] = fmaf(-shut, own.p[v], own.p[v]);
+                own.b[v] = fmaf(own.p[v], gf[v], own.b[v]);
             }
         }
-        if (CLUSTER || a.stretches > 1) {
-            joins.join(pn, rn, carry, into, hn, h);
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) into[v] = carry[v];
-        }
+        const bool joined = CLUSTER || a.stretches > 1;
+        if (joined) joins.give(own, hn, h);
         float d[STEPS][V];                                           // a (1 - a) (h_(t-1) - x_t)
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
@@ -495,38 +508,35 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
                 h[v] = advance(u[s][v], h[v], xf[v]);
             }
         }
-        const Walker<T, V> at_dx(a.dx, p), at_dz(a.dgate, p);
-        auto write = [&](auto full_stretch) {
-            constexpr bool whole = decltype(full_stretch)::value;
+        if (joined) {
+            joins.take(carry, into);
+        } else {
 #pragma unroll
-            for (int s = STEPS - 1; s >= 0; --s) {
-                float gf[V], dx[V], dz[V];
-                Lane<T, V>::get(g[s], gf);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float full = gf[v] + into[v];
-                    dx[v] = u[s][v] * full;
-                    into[v] = full - dx[v];
-                    dz[v] = d[s][v] * full;
-                    if (!whole && s >= p.valid) dx[v] = dz[v] = 0.0f;
-                }
-                if (whole || s < p.rows) {
-                    at_dx[s] = Lane<T, V>::put(dx);
-                    at_dz[s] = Lane<T, V>::put(dz);
-                }
-            }
-        };
-        if (p.writes) {
-            if (p.valid == STEPS) write(std::true_type());
-            else write(std::false_type());
+            for (int v = 0; v < V; ++v) into[v] = carry[v];
         }
-        if (a.dh0 && p.writes && p.k == 0 && warp == 0)
 #pragma unroll
-            for (int v = 0; v < V; ++v) a.dh0[p.b * a.channels + p.c + v] = into[v];
+        for (int s = STEPS - 1; s >= 0; --s) {
+            float gf[V], dx[V], dz[V];
+            Lane<T, V>::get(g[s], gf);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float full = gf[v] + into[v];
+                dx[v] = u[s][v] * full;
+                into[v] = full - dx[v];
+                dz[v] = d[s][v] * full;
+            }
+            x[s] = Lane<T, V>::put(dx);
+            z[s] = Lane<T, V>::put(dz);
+        }
+        __syncwarp();
+        x.write(a, a.dx, p);
+        z.write(a, a.dgate, p);
+        if (p.k == 0 && warp == 0) store_state<V>(a.dh0, p.b, a.channels, p, lane, into);
+        __syncwarp();                                                // before the stage is filled again
     } while (more);
 }
 
-template <typename T, int V>
+template <typename T, int V, int CHUNK>
 static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
 {
     ScanArgs a = args;
@@ -536,10 +546,10 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
     a.spans = (a.length + SPAN - 1) / SPAN;
     const bool cluster = a.spans > 1;
     static SharedRecord records[4];
-    auto kernel = backward ? cluster ? scan_backward_kernel<T, V, true> : scan_backward_kernel<T, V, false>
-                           : cluster ? scan_forward_kernel<T, V, true> : scan_forward_kernel<T, V, false>;
+    auto kernel = backward ? cluster ? scan_backward_kernel<T, V, CHUNK, true> : scan_backward_kernel<T, V, CHUNK, false>
+                           : cluster ? scan_forward_kernel<T, V, CHUNK, true> : scan_forward_kernel<T, V, CHUNK, false>;
     SharedRecord &record = records[2 * backward + cluster];
-    const size_t shared = (size_t)2 * (backward ? 3 : 2) * SPAN * 32 * sizeof(typename Lane<T, V>::raw);
+    const size_t shared = (size_t)2 * (backward ? 3 : 2) * WARPS * Stage<T, V, CHUNK>::BYTES;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr = {};
     int64_t grid;
@@ -613,19 +623,25 @@ static ScanTensor tensor(const void *p, const int64_t (&stride)[2])
 
 static gs_status run(ScanArgs &a, int32_t dtype, const ScanTensor *const *t, int n, int outputs, bool backward, cudaStream_t st)
 {
-    const uintptr_t es = size_of(dtype);
-    bool pairs = dtype != GS_TABLE_F32 && a.channels % 2 == 0;
+    const int64_t es = (int64_t)size_of(dtype);
+    bool pairs = es == 2 && a.channels % 2 == 0, wide = a.channels * es % 16 == 0;
     for (int i = 0; i < n; ++i) {
         if (!t[i]->p) return bad("null pointer");
         if ((uintptr_t)t[i]->p % es) return bad("tensor not aligned to its element size");
         if (i < outputs && ((a.batch > 1 && t[i]->sb == 0) || (a.length > 1 && t[i]->st == 0)))
             return bad("an output has a zero stride");
         pairs = pairs && (uintptr_t)t[i]->p % 4 == 0 && (t[i]->sb | t[i]->st) % 2 == 0;
+        wide = wide && (uintptr_t)t[i]->p % 16 == 0 && (t[i]->sb * es | t[i]->st * es) % 16 == 0;
     }
     pairs = pairs && a.channels > 32;                   // one channel a lane where two would leave half the lanes idle
-    if (dtype == GS_TABLE_F32) return launch<float, 1>(a, backward, st);
-    if (dtype == GS_TABLE_F16) return pairs ? launch<__half, 2>(a, backward, st) : launch<__half, 1>(a, backward, st);
-    return pairs ? launch<__nv_bfloat16, 2>(a, backward, st) : launch<__nv_bfloat16, 1>(a, backward, st);
+    return with_type(dtype, [&](auto type) {
+        typedef decltype(type) T;
+        if constexpr (sizeof(T) == 4) return wide ? launch<T, 1, 16>(a, backward, st) : launch<T, 1, 4>(a, backward, st);
+        else {
+            if (pairs) return wide ? launch<T, 2, 16>(a, backward, st) : launch<T, 2, 4>(a, backward, st);
+            return wide ? launch<T, 1, 16>(a, backward, st) : launch<T, 1, 2>(a, backward, st);
+        }
+    });
 }
 
 }  // namespace gs
