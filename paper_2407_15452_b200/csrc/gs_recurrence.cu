@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "gs_layers.cuh"
+#include "gs_tc.cuh"
 
 namespace gs {
 
@@ -39,63 +40,78 @@ struct ScanArgs {
     int32_t blocks;                       // blocks of a cluster
 };
 
-// V neighbouring channels of a lane as they travel: a register each
+// V neighbouring channels of a lane: Lane<T, V>::raw as they travel, Vec<V>::type in fp32, two of them in one instruction each
+template <int V> struct Vec;
+template <> struct Vec<1> { typedef float type; };
+template <> struct Vec<2> { typedef float2 type; };
+__device__ __forceinline__ float fma_of(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float2 fma_of(float2 a, float2 b, float2 c) { return tc::fma2(a, b, c); }
+__device__ __forceinline__ float mul_of(float a, float b) { return a * b; }
+__device__ __forceinline__ float2 mul_of(float2 a, float2 b) { return tc::mul2(a, b); }
+__device__ __forceinline__ float add_of(float a, float b) { return a + b; }
+__device__ __forceinline__ float2 add_of(float2 a, float2 b) { return tc::add2(a, b); }
+template <int V> __device__ __forceinline__ typename Vec<V>::type all_of(float x)
+{
+    if constexpr (V == 1) return x;
+    else return make_float2(x, x);
+}
 template <typename T, int V> struct Lane;
-template <> struct Lane<float, 1> {
-    typedef float raw;
-    static __device__ __forceinline__ void get(raw r, float (&f)[1]) { f[0] = r; }
-    static __device__ __forceinline__ raw put(const float (&f)[1]) { return f[0]; }
-};
 template <typename T> struct Lane<T, 1> {
     typedef T raw;
-    static __device__ __forceinline__ void get(raw r, float (&f)[1]) { f[0] = to_float(r); }
-    static __device__ __forceinline__ raw put(const float (&f)[1]) { return from_float<T>(f[0]); }
+    static __device__ __forceinline__ float get(raw r) { return to_float(r); }
+    static __device__ __forceinline__ float get_negative(raw r) { return -to_float(r); }
+    static __device__ __forceinline__ raw put(float f) { return from_float<T>(f); }
+    static __device__ __forceinline__ raw put_negative(float f) { return from_float<T>(-f); }
 };
 template <typename T> struct Lane<T, 2> {
     typedef uint32_t raw;
-    static __device__ __forceinline__ void get(raw r, float (&f)[2]) { unpack2<T>(r, f[0], f[1]); }
-    static __device__ __forceinline__ raw put(const float (&f)[2]) { return pack2<T>(f[0], f[1]); }
+    static constexpr uint32_t SIGNS = 0x80008000u;
+    static __device__ __forceinline__ float2 get(raw r)
+    {
+        float2 f;
+        unpack2<T>(r, f.x, f.y);
+        return f;
+    }
+    static __device__ __forceinline__ float2 get_negative(raw r) { return get(r ^ SIGNS); }
+    static __device__ __forceinline__ raw put(float2 f) { return pack2<T>(f.x, f.y); }
+    static __device__ __forceinline__ raw put_negative(float2 f) { return put(f) ^ SIGNS; }
 };
-// Powers of two and reciprocals as the special-function units have them, 2^-22 and 2^-23 of the result; below 2^-126 they are zero.
-__device__ __forceinline__ float power_of_two(float y)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
-    return r;
-}
-__device__ __forceinline__ float reciprocal(float y)
-{
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
-    return r;
-}
+
 // exp(z) = 2^y, y = z log2(e).  Rounding y costs |z| 2^-24 of the result, which tensors of 16 bits do not see; fp32 tensors get the first
-// term of what it left out back.
-template <typename T> __device__ __forceinline__ float exp_of(float z) { return power_of_two(1.44269504f * z); }
-template <> __device__ __forceinline__ float exp_of<float>(float z)
+// term of what it left out back.  Beyond 2^127 an infinity or, where products follow that have no use for one, about 2^127.
+static constexpr float LOG2_E = 1.44269504f, LOG2_E_REST = 1.92596299e-8f, LN_2 = 0.693147181f;
+template <typename T, bool FINITE> __device__ __forceinline__ float exp_of_one(float z, float y)
 {
-    asm("min.NaN.f32 %0, %0, 0f42C80000;\n\tmax.NaN.f32 %0, %0, 0fC2C80000;" : "+f"(z));    // to [-100, 100]: infinities have no remainder
-    const float y = 1.44269504f * z, rest = fmaf(1.44269504f, z, -y) + 1.92596299e-8f * z;
-    return power_of_two(y) * fmaf(0.693147181f, rest, 1.0f);
+    // NaN stays what it is
+    if (FINITE && sizeof(T) == 2) asm("min.NaN.f32 %0, %0, 0f42FF0000;" : "+f"(y));                          // 127.5
+    if constexpr (sizeof(T) == 4) {
+        asm("min.NaN.f32 %0, %0, 0f42B0BD4A;\n\tmax.NaN.f32 %0, %0, 0fC2C80000;" : "+f"(z));                   // 88.36971 (127.5 ln 2), -100
+        y = LOG2_E * z;
+        const float rest = fmaf(LOG2_E, z, -y) + LOG2_E_REST * z;
+        return tc::exp2_fast(y) * fmaf(LN_2, rest, 1.0f);
+    }
+    return tc::exp2_fast(y);
 }
-// 1 - a = 1 / (1 + exp(z)), to a few units of its own last place however small it is: from a rounded a it would have no
-// digits left where a channel remembers for long.
-template <typename T> __device__ __forceinline__ float shut_of(float z) { return reciprocal(1.0f + exp_of<T>(z)); }
-
-// a h + (1 - a) x from u = 1 - a: h - u h is rounded once, so a state that is kept for long loses nothing to a rounded a, and
-// one that is given up (u = 1) leaves nothing behind
-__device__ __forceinline__ float advance(float u, float h, float x) { return fmaf(u, x, fmaf(-u, h, h)); }
-
-// What the backward pass keeps of a gate: the smaller of a and 1 - a, with the sign bit set where that is a.  Both factors of a (1 - a) are then
-// at hand with all their digits, also where one of them is nearly 1.
-template <typename T>
-__device__ __forceinline__ float gate_of(float z, float &u)
+template <typename T, bool FINITE> __device__ __forceinline__ float exp_of(float z) { return exp_of_one<T, FINITE>(z, LOG2_E * z); }
+template <typename T, bool FINITE> __device__ __forceinline__ float2 exp_of(float2 z)
 {
-    const float e = exp_of<T>(-fabsf(z)), larger = reciprocal(1.0f + e), m = e * larger;
-    const bool shut = signbit(z);
-    u = shut ? larger : m;
-    return shut ? -m : m;
+    const float2 y = mul_of(z, make_float2(LOG2_E, LOG2_E));
+    return make_float2(exp_of_one<T, FINITE>(z.x, y.x), exp_of_one<T, FINITE>(z.y, y.y));
 }
+__device__ __forceinline__ float reciprocal(float x) { return tc::rcp_fast(x); }
+__device__ __forceinline__ float2 reciprocal(float2 x) { return make_float2(tc::rcp_fast(x.x), tc::rcp_fast(x.y)); }
+
+// -(1 - a) = 1 / (-1 - e), e = exp(z), to a few units of its own last place however small it is: from a rounded a it would have no digits
+// left where a channel remembers for long.  Negative, because that is what multiply-adds take.
+template <typename F>
+__device__ __forceinline__ F minus_shut(F e)
+{
+    const F one = all_of<sizeof(F) / 4>(-1.0f);
+    return reciprocal(fma_of(e, one, one));
+}
+// a h + (1 - a) x from n = -(1 - a) and -x: h + n h is rounded once, so a state that is kept for long loses nothing to a rounded a, and
+// one that is given up (n = -1) leaves nothing behind
+template <typename F> __device__ __forceinline__ F advance(F n, F h, F minus_x) { return fma_of(n, minus_x, fma_of(n, h, h)); }
 
 struct Place {                            // what a warp works on: positions [t0, t0 + rows) of a chain, `valid` of them valid
     int64_t b, c;                         // sequence; the warp's first channel
@@ -201,20 +217,14 @@ __device__ __forceinline__ uint32_t cluster_rank()
 }
 // A lane's share of the affine function of a stretch, x -> p x + b
 template <int V> struct alignas(8 * V) Affine {
-    float p[V], b[V];
+    typedef typename Vec<V>::type F;
+    F p, b;
     __device__ __forceinline__ void after(const Affine &first)          // this one behind `first`
     {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            b[v] = fmaf(p[v], first.b[v], b[v]);
-            p[v] *= first.p[v];
-        }
+        b = fma_of(p, first.b, b);
+        p = mul_of(p, first.p);
     }
-    __device__ __forceinline__ void apply(float (&x)[V]) const
-    {
-#pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = fmaf(p[v], x[v], b[v]);
-    }
+    __device__ __forceinline__ F of(F x) const { return fma_of(p, x, b); }
 };
 // stores into the shared memory of another block of the cluster, at the place that `local` has in this one
 template <int V>
@@ -223,9 +233,9 @@ __device__ __forceinline__ void store_remote(const Affine<V> *local, uint32_t ra
     uint32_t there;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
     if constexpr (V == 2)
-        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(f.p[0]), "f"(f.p[1]), "f"(f.b[0]), "f"(f.b[1]) : "memory");
+        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(f.p.x), "f"(f.p.y), "f"(f.b.x), "f"(f.b.y) : "memory");
     else
-        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(f.p[0]), "f"(f.b[0]) : "memory");
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(f.p), "f"(f.b) : "memory");
 }
 
 // The functions of a window's stretches, and of a cluster's spans, where the warps that need them find them.  BACK: the chain runs
@@ -236,11 +246,12 @@ template <int V, bool CLUSTER, bool BACK>
 struct Board {
     static constexpr int TURNS = CLUSTER ? 1 : 2;
     Affine<V> stretch[TURNS][WARPS][32];
-    float ahead[BACK ? TURNS : 1][BACK ? WARPS : 1][32][V];
+    typename Vec<V>::type ahead[BACK ? TURNS : 1][BACK ? WARPS : 1][32];
     Affine<V> span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32];
 };
 template <int V, bool CLUSTER, bool BACK>
 struct Joins {
+    typedef typename Vec<V>::type F;
     Board<V, CLUSTER, BACK> &board;
     int stretches, blocks, rank, warp, lane, first;  // first: index of the block's warp that has this chain's first stretch
     int turn;
@@ -248,23 +259,17 @@ struct Joins {
 
     // Gives away the function of this warp's stretch and hb, the b of h over it; h moves from the state before the block's first stretch to
     // that before this one.
-    __device__ __forceinline__ void give(const Affine<V> &own, const float (&hb)[V], float (&h)[V])
+    __device__ __forceinline__ void give(const Affine<V> &own, F hb, F &h)
     {
         const int place = CLUSTER ? 0 : turn;
         board.stretch[place][first + warp][lane] = own;
-        if (BACK)
-#pragma unroll
-            for (int v = 0; v < V; ++v) board.ahead[BACK ? place : 0][BACK ? first + warp : 0][lane][v] = hb[v];
+        if (BACK) board.ahead[BACK ? place : 0][BACK ? first + warp : 0][lane] = hb;
         __syncthreads();
         if (BACK)
-            for (int i = 0; i < warp; ++i) {
-                Affine<V> f = board.stretch[place][first + i][lane];
-#pragma unroll
-                for (int v = 0; v < V; ++v) f.b[v] = board.ahead[BACK ? place : 0][BACK ? first + i : 0][lane][v];
-                f.apply(h);
-            }
-#pragma unroll
-        for (int v = 0; v < V; ++v) before.p[v] = 1.0f, before.b[v] = 0.0f;
+            for (int i = 0; i < warp; ++i)
+                h = fma_of(board.stretch[place][first + i][lane].p, h, board.ahead[BACK ? place : 0][BACK ? first + i : 0][lane]);
+        before.p = all_of<V>(1.0f);
+        before.b = all_of<V>(0.0f);
         const int count = BACK ? stretches - 1 - warp : warp;
         for (int i = 0; i < count; ++i) {
             Affine<V> f = board.stretch[place][first + (BACK ? stretches - 1 - i : i)][lane];
@@ -279,24 +284,20 @@ struct Joins {
         }
         cluster_arrive();
     }
-    // carry: the state (or r) at the window's edge, moved over the window; into: at this stretch's
-    __device__ __forceinline__ void take(float (&carry)[V], float (&into)[V])
+    // carry: the state (or r) at the window's edge, moved over the window; returns that at this stretch's
+    __device__ __forceinline__ F take(F &carry)
     {
+        F into = carry;
         if (CLUSTER) {
             cluster_wait();
             for (int i = 0; i < blocks; ++i) {
                 const int k = BACK ? blocks - 1 - i : i;
-                if (k == rank)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) into[v] = carry[v];
-                board.span[CLUSTER ? turn : 0][CLUSTER ? k : 0][lane].apply(carry);
+                if (k == rank) into = carry;
+                carry = board.span[CLUSTER ? turn : 0][CLUSTER ? k : 0][lane].of(carry);
             }
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) into[v] = carry[v];
         }
-        before.apply(into);
         turn ^= 1;
+        return before.of(into);
     }
 };
 
@@ -330,23 +331,31 @@ __device__ __forceinline__ Items<CLUSTER, BACK> first_item(const ScanArgs &a, in
 }
 
 template <int V>
-__device__ __forceinline__ void load_state(const float *from, int64_t row, int64_t channels, const Place &p, int lane, float (&h)[V])
+__device__ __forceinline__ typename Vec<V>::type load_state(const float *from, int64_t row, int64_t channels, const Place &p, int lane)
 {
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = from && p.on ? from[row * channels + p.c + lane * V + v] : 0.0f;
+    if (!from || !p.on) return all_of<V>(0.0f);
+    from += row * channels + p.c + lane * V;
+    if constexpr (V == 1) return from[0];
+    else return make_float2(from[0], from[1]);
 }
 template <int V>
-__device__ __forceinline__ void store_state(float *to, int64_t row, int64_t channels, const Place &p, int lane, const float (&h)[V])
+__device__ __forceinline__ void store_state(float *to, int64_t row, int64_t channels, const Place &p, int lane, typename Vec<V>::type h)
 {
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (to && p.on) to[row * channels + p.c + lane * V + v] = h[v];
+    if (!to || !p.on) return;
+    to += row * channels + p.c + lane * V;
+    if constexpr (V == 1) to[0] = h;
+    else {
+        to[0] = h.x;
+        to[1] = h.y;
+    }
 }
 
 template <typename T, int V, int CHUNK, bool CLUSTER>
 __global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan_forward_kernel(const __grid_constant__ ScanArgs a)
 {
     typedef Stage<T, V, CHUNK> S;
+    typedef Lane<T, V> L;
+    typedef typename Vec<V>::type F;
     __shared__ Board<V, CLUSTER, false> board;
     extern __shared__ uint4 room[];                                  // [2 in turn][warp][gate, x]
     const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
@@ -365,11 +374,8 @@ __global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan
     fetch(next, 0);
 
     Joins<V, CLUSTER, false> joins = {board, a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
-    float carry[V], into[V];
-    if (CLUSTER) {
-        load_state<V>(a.h0, next.b, a.channels, next, lane, carry);
-        cluster_wait();
-    }
+    F carry = load_state<V>(a.h0, next.b, a.channels, next, lane);
+    if (CLUSTER) cluster_wait();
     bool more;
     int turn = 0;
     do {
@@ -381,42 +387,27 @@ __global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan
         } else {
             fetches_end();
         }
-        if (!CLUSTER) load_state<V>(a.h0, p.b, a.channels, p, lane, carry);
+        if (!CLUSTER) carry = load_state<V>(a.h0, p.b, a.channels, p, lane);
         fetches_wait();
         const S z = stage(turn, 0), x = stage(turn, 1);
         turn ^= 1;
-        float u[STEPS][V], h[V];
-        Affine<V> own;
-#pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = 0.0f, own.p[v] = 1.0f;
+        F n[STEPS];
+        Affine<V> own = {all_of<V>(1.0f), all_of<V>(0.0f)};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            float zf[V], xf[V];
-            Lane<T, V>::get(z[s], zf);
-            Lane<T, V>::get(x[s], xf);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                u[s][v] = shut_of<T>(zf[v]);
-                h[v] = advance(u[s][v], h[v], xf[v]);
-                own.p[v] = fmaf(-u[s][v], own.p[v], own.p[v]);
-            }
+            n[s] = minus_shut(exp_of<T, false>(L::get(z[s])));
+            own.b = advance(n[s], own.b, L::get_negative(x[s]));
+            own.p = fma_of(n[s], own.p, own.p);
         }
+        F into = carry;
         if (CLUSTER || a.stretches > 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) own.b[v] = h[v];
-            joins.give(own, h, h);
-            joins.take(carry, into);
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) into[v] = carry[v];
+            joins.give(own, own.b, own.b);
+            into = joins.take(carry);
         }
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            float o[V];
-            Lane<T, V>::get(x[s], o);
-#pragma unroll
-            for (int v = 0; v < V; ++v) o[v] = into[v] = advance(u[s][v], into[v], o[v]);
-            x[s] = Lane<T, V>::put(o);
+            into = advance(n[s], into, L::get_negative(x[s]));
+            x[s] = L::put(into);
         }
         __syncwarp();
         x.write(a, a.out, p);
@@ -432,6 +423,8 @@ template <typename T, int V, int CHUNK, bool CLUSTER>
 __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_kernel(const __grid_constant__ ScanArgs a)
 {
     typedef Stage<T, V, CHUNK> S;
+    typedef Lane<T, V> L;
+    typedef typename Vec<V>::type F;
     __shared__ Board<V, CLUSTER, true> board;
     extern __shared__ uint4 room[];                                  // [2 in turn][warp][gate, x, dout]
     const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
@@ -451,11 +444,8 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
     fetch(next, 0);
 
     Joins<V, CLUSTER, true> joins = {board, a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
-    float carry[V], into[V];
-    if (CLUSTER) {
-        load_state<V>(a.dfinal, next.b, a.channels, next, lane, carry);
-        cluster_wait();
-    }
+    F carry = load_state<V>(a.dfinal, next.b, a.channels, next, lane);
+    if (CLUSTER) cluster_wait();
     bool more;
     int turn = 0;
     do {
@@ -467,66 +457,39 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
         } else {
             fetches_end();
         }
-        float h[V];                                                  // the state before the block's span
-        if (p.k == 0) load_state<V>(a.h0, p.b, a.channels, p, lane, h);
-        else load_state<V>(p.k < a.spans ? a.states : nullptr, p.b * (a.spans - 1) + p.k - 1, a.channels, p, lane, h);
-        if (!CLUSTER) load_state<V>(a.dfinal, p.b, a.channels, p, lane, carry);
+        F h;                                                         // the state before the block's span
+        if (p.k == 0) h = load_state<V>(a.h0, p.b, a.channels, p, lane);
+        else h = load_state<V>(p.k < a.spans ? a.states : nullptr, p.b * (a.spans - 1) + p.k - 1, a.channels, p, lane);
+        if (!CLUSTER) carry = load_state<V>(a.dfinal, p.b, a.channels, p, lane);
         fetches_wait();
         const S z = stage(turn, 0), x = stage(turn, 1), g = stage(turn, 2);
         turn ^= 1;
-        float u[STEPS][V], hn[V];                                    // u: first as gate_of has it, then 1 - a
-        Affine<V> own;
-#pragma unroll
-        for (int v = 0; v < V; ++v) hn[v] = 0.0f, own.p[v] = 1.0f, own.b[v] = 0.0f;
+        F n[STEPS], d[STEPS], hb = all_of<V>(0.0f);                  // d: a (1 - a), then that times h_(t-1) - x_t
+        Affine<V> own = {all_of<V>(1.0f), all_of<V>(0.0f)};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            float zf[V], xf[V], gf[V];
-            Lane<T, V>::get(z[s], zf);
-            Lane<T, V>::get(x[s], xf);
-            Lane<T, V>::get(g[s], gf);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float shut;
-                u[s][v] = gate_of<T>(zf[v], shut);
-                hn[v] = advance(shut, hn[v], xf[v]);
-                own.p[v] = fmaf(-shut, own.p[v], own.p[v]);
-                own.b[v] = fmaf(own.p[v], gf[v], own.b[v]);
-            }
+            const F e = exp_of<T, true>(L::get(z[s]));
+            n[s] = minus_shut(e);
+            d[s] = mul_of(mul_of(e, n[s]), n[s]);                    // -a times -(1 - a)
+            hb = advance(n[s], hb, L::get_negative(x[s]));
+            own.p = fma_of(n[s], own.p, own.p);
+            own.b = fma_of(own.p, L::get(g[s]), own.b);
         }
         const bool joined = CLUSTER || a.stretches > 1;
-        if (joined) joins.give(own, hn, h);
-        float d[STEPS][V];                                           // a (1 - a) (h_(t-1) - x_t)
+        if (joined) joins.give(own, hb, h);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            float xf[V];
-            Lane<T, V>::get(x[s], xf);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float m = fabsf(u[s][v]);
-                u[s][v] = signbit(u[s][v]) ? 1.0f - m : m;
-                d[s][v] = fmaf(-m, m, m) * (h[v] - xf[v]);
-                h[v] = advance(u[s][v], h[v], xf[v]);
-            }
+            const F minus_x = L::get_negative(x[s]);
+            d[s] = mul_of(d[s], add_of(h, minus_x));
+            h = advance(n[s], h, minus_x);
         }
-        if (joined) {
-            joins.take(carry, into);
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) into[v] = carry[v];
-        }
+        F into = joined ? joins.take(carry) : carry;
 #pragma unroll
         for (int s = STEPS - 1; s >= 0; --s) {
-            float gf[V], dx[V], dz[V];
-            Lane<T, V>::get(g[s], gf);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float full = gf[v] + into[v];
-                dx[v] = u[s][v] * full;
-                into[v] = full - dx[v];
-                dz[v] = d[s][v] * full;
-            }
-            x[s] = Lane<T, V>::put(dx);
-            z[s] = Lane<T, V>::put(dz);
+            const F full = add_of(L::get(g[s]), into);
+            x[s] = L::put_negative(mul_of(n[s], full));
+            into = fma_of(n[s], full, full);
+            z[s] = L::put(mul_of(d[s], full));
         }
         __syncwarp();
         x.write(a, a.dx, p);
