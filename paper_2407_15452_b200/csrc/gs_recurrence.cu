@@ -38,6 +38,7 @@ struct ScanArgs {
     int32_t length, slabs, spans;         // slabs of 32 * V channels; spans = ceil(length / SPAN)
     int32_t stretches, steps;             // warps that share a span, positions of each
     int32_t blocks;                       // blocks of a cluster
+    unsigned long long *stalls;           // where blocks whose waits ran out are counted
 };
 
 // V neighbouring channels of a lane: Lane<T, V>::raw as they travel, Vec<V>::type in fp32, two of them in one instruction each
@@ -59,22 +60,19 @@ template <typename T, int V> struct Lane;
 template <typename T> struct Lane<T, 1> {
     typedef T raw;
     static __device__ __forceinline__ float get(raw r) { return to_float(r); }
-    static __device__ __forceinline__ float get_negative(raw r) { return -to_float(r); }
     static __device__ __forceinline__ raw put(float f) { return from_float<T>(f); }
     static __device__ __forceinline__ raw put_negative(float f) { return from_float<T>(-f); }
 };
 template <typename T> struct Lane<T, 2> {
     typedef uint32_t raw;
-    static constexpr uint32_t SIGNS = 0x80008000u;
     static __device__ __forceinline__ float2 get(raw r)
     {
         float2 f;
         unpack2<T>(r, f.x, f.y);
         return f;
     }
-    static __device__ __forceinline__ float2 get_negative(raw r) { return get(r ^ SIGNS); }
     static __device__ __forceinline__ raw put(float2 f) { return pack2<T>(f.x, f.y); }
-    static __device__ __forceinline__ raw put_negative(float2 f) { return put(f) ^ SIGNS; }
+    static __device__ __forceinline__ raw put_negative(float2 f) { return pack2<T>(-f.x, -f.y); }
 };
 
 // exp(z) = 2^y, y = z log2(e).  Rounding y costs |z| 2^-24 of the result, which tensors of 16 bits do not see; fp32 tensors get the first
@@ -109,29 +107,33 @@ __device__ __forceinline__ F minus_shut(F e)
     const F one = all_of<sizeof(F) / 4>(-1.0f);
     return reciprocal(fma_of(e, one, one));
 }
-// a h + (1 - a) x from n = -(1 - a) and -x: h + n h is rounded once, so a state that is kept for long loses nothing to a rounded a, and
-// one that is given up (n = -1) leaves nothing behind
-template <typename F> __device__ __forceinline__ F advance(F n, F h, F minus_x) { return fma_of(n, minus_x, fma_of(n, h, h)); }
+// States travel negated, -h: -(a h + (1 - a) x) = (-h) + n (-h) + n x with n = -(1 - a).  (-h) + n (-h) is rounded once, so a state that is
+// kept for long loses nothing to a rounded a, and one that is given up (n = -1) leaves nothing behind.
+template <typename F> __device__ __forceinline__ F advance(F n, F minus_h, F x) { return fma_of(n, x, fma_of(n, minus_h, minus_h)); }
 
 struct Place {                            // what a warp works on: positions [t0, t0 + rows) of a chain, `valid` of them valid
     int64_t b, c;                         // sequence; the warp's first channel
+    int len;                              // valid positions of the sequence
     int k, t0, rows, valid;               // k: the span
-    bool on;                              // the lane has a channel, and the warp a chain
-};
+    bool there, on;                       // the warp has a chain; and the lane a channel
 
+    __device__ __forceinline__ void stretch(const ScanArgs &a, int span, int warp, int steps)
+    {
+        k = span;
+        t0 = k * SPAN + warp * steps;
+        rows = there ? min(max(a.length - t0, 0), steps) : 0;
+        valid = min(rows, max(len - t0, 0));
+    }
+};
 template <int V>
-__device__ __forceinline__ Place place_of(const ScanArgs &a, int64_t chain, int lane, int k, int warp)
+__device__ __forceinline__ Place place_of(const ScanArgs &a, int64_t chain, int lane)
 {
     Place p;
-    const bool there = chain < a.chains;
-    p.b = there ? a.by_slabs.of(chain) : 0;
-    p.c = there ? (chain - p.b * a.slabs) * (32 * V) : 0;
-    p.on = there && p.c + lane * V < a.channels;
-    p.k = k;
-    p.t0 = k * SPAN + warp * a.steps;
-    p.rows = there ? min(max(a.length - p.t0, 0), a.steps) : 0;
-    const int len = a.lens && there ? min(max(__ldg(a.lens + p.b), 0), a.length) : a.length;
-    p.valid = min(p.rows, max(len - p.t0, 0));
+    p.there = chain < a.chains;
+    p.b = p.there ? a.by_slabs.of(chain) : 0;
+    p.c = p.there ? (chain - p.b * a.slabs) * (32 * V) : 0;
+    p.on = p.there && p.c + lane * V < a.channels;
+    p.len = a.lens && p.there ? min(max(__ldg(a.lens + p.b), 0), a.length) : a.length;
     return p;
 }
 
@@ -148,49 +150,63 @@ struct Stage {
     int lane;
 
     __device__ __forceinline__ raw &operator[](int s) const { return *reinterpret_cast<raw *>(room + s * ROW + lane * sizeof(raw)); }
-    __device__ __forceinline__ char *global(const ScanTensor &t, const Place &p) const
+    // where the lane's first chunk of a stretch lies in a tensor; the others follow AT_ONCE positions apart
+    static __device__ __forceinline__ char *chunk(const ScanTensor &t, const Place &p, int lane)
     {
         return static_cast<char *>(t.p) + (p.b * t.sb + (p.t0 + lane / ACROSS) * t.st + p.c) * (int64_t)sizeof(T) + lane % ACROSS * CHUNK;
     }
-    __device__ __forceinline__ bool inside(const ScanArgs &a, const Place &p) const
+    static __device__ __forceinline__ bool inside(const ScanArgs &a, const Place &p, int lane)
     {
         return p.c + lane % ACROSS * (CHUNK / (int)sizeof(T)) < a.channels;
     }
-    __device__ __forceinline__ void fetch(const ScanArgs &a, const ScanTensor &t, const Place &p, int valid, uint32_t without) const
+    static __device__ __forceinline__ int64_t round(const ScanTensor &t) { return AT_ONCE * t.st * (int64_t)sizeof(T); }
+
+    __device__ __forceinline__ void fetch(const char *from, int64_t step, bool in, int valid, uint32_t without) const
     {
-        const char *from = global(t, p);
-        const int64_t step = AT_ONCE * t.st * (int64_t)sizeof(T);
-        const bool in = inside(a, p);
         char *to = room + lane * CHUNK;
+        const int row = lane / ACROSS;
+        if constexpr (CHUNK == 2) {
 #pragma unroll
-        for (int i = 0; i < ROUNDS; ++i, from += step, to += 32 * CHUNK) {
-            if (i * AT_ONCE + lane / ACROSS < valid) {
-                if (!in) continue;
-                if constexpr (CHUNK == 2) *reinterpret_cast<uint16_t *>(to) = *reinterpret_cast<const uint16_t *>(from);
-                else if constexpr (CHUNK == 4)
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+            for (int i = 0; i < ROUNDS; ++i, from += step, to += 32 * CHUNK)
+                *reinterpret_cast<uint16_t *>(to) = in && i < valid ? *reinterpret_cast<const uint16_t *>(from) : (uint16_t)without;
+        } else {
+            const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+#pragma unroll
+            for (int i = 0; i < ROUNDS; ++i, from += step) {
+                const int on = in && i * AT_ONCE + row < valid;
+                if constexpr (CHUNK == 4)
+                    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], 4;\n\t}"
+                                 ::"r"(at + i * 32 * CHUNK), "l"(from), "r"(on) : "memory");
                 else
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
-            } else if constexpr (CHUNK == 2) *reinterpret_cast<uint16_t *>(to) = (uint16_t)without;
-            else if constexpr (CHUNK == 4) *reinterpret_cast<uint32_t *>(to) = without;
-            else *reinterpret_cast<uint4 *>(to) = make_uint4(without, without, without, without);
+                    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}"
+                                 ::"r"(at + i * 32 * CHUNK), "l"(from), "r"(on) : "memory");
+            }
+            if (valid < STEPS)
+#pragma unroll
+                for (int i = 0; i < ROUNDS; ++i, to += 32 * CHUNK)
+                    if (i * AT_ONCE + row >= valid) {
+                        if constexpr (CHUNK == 4) *reinterpret_cast<uint32_t *>(to) = without;
+                        else *reinterpret_cast<uint4 *>(to) = make_uint4(without, without, without, without);
+                    }
         }
     }
     // positions that are not valid are written as zeros
-    __device__ __forceinline__ void write(const ScanArgs &a, const ScanTensor &t, const Place &p) const
+    __device__ __forceinline__ void write(char *to, int64_t step, bool in, const Place &p) const
     {
-        char *to = global(t, p);
-        const int64_t step = AT_ONCE * t.st * (int64_t)sizeof(T);
-        const bool in = inside(a, p);
+        typedef typename std::conditional<CHUNK == 2, uint16_t, typename std::conditional<CHUNK == 4, uint32_t, uint4>::type>::type word;
         const char *from = room + lane * CHUNK;
+        const int row = lane / ACROSS;
+        word w[ROUNDS];
 #pragma unroll
-        for (int i = 0; i < ROUNDS; ++i, to += step, from += 32 * CHUNK) {
-            const int s = i * AT_ONCE + lane / ACROSS;
-            if (!in || s >= p.rows) continue;
-            if constexpr (CHUNK == 2) *reinterpret_cast<uint16_t *>(to) = s < p.valid ? *reinterpret_cast<const uint16_t *>(from) : (uint16_t)0;
-            else if constexpr (CHUNK == 4) *reinterpret_cast<uint32_t *>(to) = s < p.valid ? *reinterpret_cast<const uint32_t *>(from) : 0u;
-            else *reinterpret_cast<uint4 *>(to) = s < p.valid ? *reinterpret_cast<const uint4 *>(from) : make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < ROUNDS; ++i) w[i] = *reinterpret_cast<const word *>(from + i * 32 * CHUNK);
+        if (p.valid < STEPS) {
+#pragma unroll
+            for (int i = 0; i < ROUNDS; ++i)
+                if (i * AT_ONCE + row >= p.valid) w[i] = word{};
         }
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i, to += step)
+            if (in && i * AT_ONCE + row < p.rows) *reinterpret_cast<word *>(to) = w[i];
     }
 };
 // a value as the words that its tensor holds
@@ -200,10 +216,11 @@ template <typename T> __device__ __forceinline__ uint32_t words_of(float x)
     else return pack2<T>(x, x);
 }
 __device__ __forceinline__ void fetches_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// all but the latest group of the warp's fetches have come
+// all but the latest LATER groups of the warp's fetches have come
+template <int LATER>
 __device__ __forceinline__ void fetches_wait()
 {
-    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(LATER) : "memory");
     __syncwarp();
 }
 
@@ -219,204 +236,288 @@ __device__ __forceinline__ uint32_t cluster_rank()
 template <int V> struct alignas(8 * V) Affine {
     typedef typename Vec<V>::type F;
     F p, b;
-    __device__ __forceinline__ void after(const Affine &first)          // this one behind `first`
+    __device__ __forceinline__ void before(const Affine &next)          // this one, then `next`
     {
-        b = fma_of(p, first.b, b);
-        p = mul_of(p, first.p);
+        b = fma_of(next.p, b, next.b);
+        p = mul_of(next.p, p);
     }
     __device__ __forceinline__ F of(F x) const { return fma_of(p, x, b); }
 };
-// stores into the shared memory of another block of the cluster, at the place that `local` has in this one
-template <int V>
-__device__ __forceinline__ void store_remote(const Affine<V> *local, uint32_t rank, const Affine<V> &f)
+__device__ __forceinline__ uint32_t in_block(uint32_t address, uint32_t rank)
 {
     uint32_t there;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(address), "r"(rank));
+    return there;
+}
+// stores into the shared memory of another block of the cluster, at the place that `to` is in this one, and counts the bytes on that block's
+// barrier `bar`
+template <int V>
+__device__ __forceinline__ void store_remote(uint32_t to, uint32_t bar, uint32_t rank, const Affine<V> &f)
+{
     if constexpr (V == 2)
-        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(f.p.x), "f"(f.p.y), "f"(f.b.x), "f"(f.b.y) : "memory");
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                     ::"r"(in_block(to, rank)), "f"(f.p.x), "f"(f.p.y), "f"(f.b.x), "f"(f.b.y), "r"(in_block(bar, rank)) : "memory");
     else
-        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(f.p), "f"(f.b) : "memory");
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                     ::"r"(in_block(to, rank)), "f"(f.p), "f"(f.b), "r"(in_block(bar, rank)) : "memory");
 }
 
 // The functions of a window's stretches, and of a cluster's spans, where the warps that need them find them.  BACK: the chain runs
 // from the last stretch to the first, and beside it h from the first to the last (with the same p, and `ahead` for its b).
-// Places are used in turn (those of a block's stretches only if the block is no cluster's: there a barrier of the cluster lies between
-// the last read and the next write).
+//
+// A cluster's blocks send each other their spans' functions, which a barrier of the receiver counts in (`come`), without waiting for one another: the
+// places of a window are written again two windows later, and who sends then has the functions of the window between from all blocks, which
+// these sent when all of their warps had read the window before.  Places of the stretches are written again when the block's warps have counted their
+// reads on `read` (clusters), or in turn (blocks, whose warps meet at a barrier in every window).
 template <int V, bool CLUSTER, bool BACK>
 struct Board {
     static constexpr int TURNS = CLUSTER ? 1 : 2;
     Affine<V> stretch[TURNS][WARPS][32];
     typename Vec<V>::type ahead[BACK ? TURNS : 1][BACK ? WARPS : 1][32];
     Affine<V> span[CLUSTER ? 2 : 1][CLUSTER ? MOST_BLOCKS : 1][32];
+    unsigned long long come[2], read;
+    int stalled;
 };
 template <int V, bool CLUSTER, bool BACK>
 struct Joins {
     typedef typename Vec<V>::type F;
     Board<V, CLUSTER, BACK> &board;
     int stretches, blocks, rank, warp, lane, first;  // first: index of the block's warp that has this chain's first stretch
-    int turn;
-    Affine<V> before;                                // of what lies between the block's edge and this warp's stretch
+    int window;                                      // counted from the first that is worked on
+    Affine<V> ahead;                                 // of what lies between the block's edge and this warp's stretch
+
+    static __device__ __forceinline__ uint32_t address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+    // before any other use, by all threads of the cluster
+    __device__ __forceinline__ void open()
+    {
+        if (!CLUSTER) return;
+        if (threadIdx.x == 0) {
+            board.stalled = 0;
+            tc::bar_init(address(&board.come[0]), 1);
+            tc::bar_init(address(&board.come[1]), 1);
+            tc::bar_init(address(&board.read), WARPS);
+            tc::fence_barrier_init();
+        }
+        __syncwarp();
+        cluster_arrive();
+    }
+    // no block leaves while another may still send to it, whatever became of the waits
+    __device__ __forceinline__ void close(unsigned long long *stalls)
+    {
+        if (!CLUSTER) return;
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+        if (threadIdx.x == 0 && stalls && *(volatile int *)&board.stalled) atomicAdd_system(stalls, 1ull);
+    }
 
     // Gives away the function of this warp's stretch and hb, the b of h over it; h moves from the state before the block's first stretch to
     // that before this one.
     __device__ __forceinline__ void give(const Affine<V> &own, F hb, F &h)
     {
-        const int place = CLUSTER ? 0 : turn;
+        const int place = CLUSTER ? 0 : window & 1;
+        if (CLUSTER && window > 0) tc::bar_wait(address(&board.read), (window - 1) & 1, &board.stalled);
         board.stretch[place][first + warp][lane] = own;
         if (BACK) board.ahead[BACK ? place : 0][BACK ? first + warp : 0][lane] = hb;
         __syncthreads();
         if (BACK)
-            for (int i = 0; i < warp; ++i)
-                h = fma_of(board.stretch[place][first + i][lane].p, h, board.ahead[BACK ? place : 0][BACK ? first + i : 0][lane]);
-        before.p = all_of<V>(1.0f);
-        before.b = all_of<V>(0.0f);
-        const int count = BACK ? stretches - 1 - warp : warp;
-        for (int i = 0; i < count; ++i) {
-            Affine<V> f = board.stretch[place][first + (BACK ? stretches - 1 - i : i)][lane];
-            f.after(before);
-            before = f;
-        }
+#pragma unroll
+            for (int i = 0; i < WARPS - 1; ++i)
+                if (i < warp)
+                    h = fma_of(board.stretch[place][first + i][lane].p, h, board.ahead[BACK ? place : 0][BACK ? first + i : 0][lane]);
+        ahead.p = all_of<V>(1.0f);
+        ahead.b = all_of<V>(0.0f);
+        const int count = BACK ? stretches - 1 - warp : warp, edge = BACK ? first + stretches - 1 : first;
+#pragma unroll
+        for (int i = 0; i < WARPS - 1; ++i)
+            if (i < count) ahead.before(board.stretch[place][BACK ? edge - i : edge + i][lane]);
         if (!CLUSTER) return;
+        __syncwarp();
+        if (lane == 0) tc::bar_arrive(address(&board.read));
+        const uint32_t bar = address(&board.come[window & 1]);
         if (count == WARPS - 1) {                    // this stretch ends the block's span
-            Affine<V> all = own;
-            all.after(before);
-            for (int r = 0; r < blocks; ++r) store_remote(&board.span[turn][rank][lane], r, all);
+            if (lane == 0) tc::bar_expect(bar, blocks * (int)sizeof(board.span[0][0]));
+            Affine<V> all = ahead;
+            all.before(own);
+            for (int r = 0; r < blocks; ++r) store_remote(address(&board.span[window & 1][rank][lane]), bar, r, all);
         }
-        cluster_arrive();
     }
     // carry: the state (or r) at the window's edge, moved over the window; returns that at this stretch's
     __device__ __forceinline__ F take(F &carry)
     {
         F into = carry;
         if (CLUSTER) {
-            cluster_wait();
-            for (int i = 0; i < blocks; ++i) {
-                const int k = BACK ? blocks - 1 - i : i;
-                if (k == rank) into = carry;
-                carry = board.span[CLUSTER ? turn : 0][CLUSTER ? k : 0][lane].of(carry);
+            const int place = window & 1;
+            tc::bar_wait(address(&board.come[place]), (window >> 1) & 1, &board.stalled);
+#pragma unroll
+            for (int i = 0; i < MOST_BLOCKS; ++i) {
+                const int k = BACK ? MOST_BLOCKS - 1 - i : i;
+                if (k < blocks) {
+                    const Affine<V> f = board.span[CLUSTER ? place : 0][CLUSTER ? k : 0][lane];
+                    if (BACK ? k > rank : k < rank) into = f.of(into);
+                    carry = f.of(carry);
+                }
             }
         }
-        turn ^= 1;
-        return before.of(into);
+        ++window;
+        return ahead.of(into);
     }
 };
 
-// A warp's items: a cluster has one chain and goes through its windows; a block of short chains goes from one group of chains to
-// another, as long as there are some.
-template <bool CLUSTER, bool BACK>
-struct Items {
-    int64_t chain, stride;                           // of the present item
-    int window, windows;
-    __device__ __forceinline__ bool next(const ScanArgs &a)
-    {
-        if (!CLUSTER) {
-            chain += stride;
-            return chain - chain_offset < a.chains;
-        }
-        window += BACK ? -1 : 1;
-        return BACK ? window >= 0 : window < windows;
-    }
-    int64_t chain_offset;                            // of the warp's group in its block: all warps of a block take the same number of items
-};
-template <bool CLUSTER, bool BACK>
-__device__ __forceinline__ Items<CLUSTER, BACK> first_item(const ScanArgs &a, int group, int groups)
-{
-    Items<CLUSTER, BACK> it;
-    it.windows = (a.spans + a.blocks - 1) / a.blocks;
-    it.window = CLUSTER && BACK ? it.windows - 1 : 0;
-    it.chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * groups + group;
-    it.chain_offset = group;
-    it.stride = (int64_t)gridDim.x * groups;
-    return it;
-}
-
+// a lane's states, times `sign`
 template <int V>
-__device__ __forceinline__ typename Vec<V>::type load_state(const float *from, int64_t row, int64_t channels, const Place &p, int lane)
+__device__ __forceinline__ typename Vec<V>::type load_state(const float *from, int64_t row, int64_t channels, const Place &p, int lane,
+                                                            float sign = -1.0f)
 {
     if (!from || !p.on) return all_of<V>(0.0f);
     from += row * channels + p.c + lane * V;
-    if constexpr (V == 1) return from[0];
-    else return make_float2(from[0], from[1]);
+    if constexpr (V == 1) return sign * from[0];
+    else return make_float2(sign * from[0], sign * from[1]);
 }
 template <int V>
-__device__ __forceinline__ void store_state(float *to, int64_t row, int64_t channels, const Place &p, int lane, typename Vec<V>::type h)
+__device__ __forceinline__ void store_state(float *to, int64_t row, int64_t channels, const Place &p, int lane, typename Vec<V>::type h,
+                                            float sign = -1.0f)
 {
     if (!to || !p.on) return;
     to += row * channels + p.c + lane * V;
-    if constexpr (V == 1) to[0] = h;
+    if constexpr (V == 1) to[0] = sign * h;
     else {
-        to[0] = h.x;
-        to[1] = h.y;
+        to[0] = sign * h.x;
+        to[1] = sign * h.y;
     }
 }
 
+// What both directions need to know about their warp
+template <bool CLUSTER>
+struct Seat {
+    int lane, index, group, warp, rank, groups;
+    __device__ __forceinline__ explicit Seat(const ScanArgs &a)
+    {
+        lane = threadIdx.x & 31;
+        index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
+        group = CLUSTER ? 0 : index / a.stretches;
+        warp = CLUSTER ? index : index - group * a.stretches;
+        rank = CLUSTER ? (int)cluster_rank() : 0;
+        groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
+    }
+};
+
+// A warp's items one after another: a cluster's windows of its chain (BACK: the last first), or the groups of chains that a block of short chains has.
+// All warps of a block have the same number of them.
+template <typename T, int V, int CHUNK, bool CLUSTER, bool BACK>
+struct Items {
+    typedef Stage<T, V, CHUNK> S;
+    const ScanArgs &a;
+    const Seat<CLUSTER> &seat;
+    Place place;
+    bool in;                                         // the lane's chunks lie in the tensors
+    int64_t chain;
+    int window, windows;
+
+    __device__ __forceinline__ Items(const ScanArgs &args, const Seat<CLUSTER> &s) : a(args), seat(s)
+    {
+        windows = CLUSTER ? (a.spans + a.blocks - 1) / a.blocks : 1;
+        window = CLUSTER && BACK ? windows - 1 : 0;
+        chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * seat.groups + seat.group;
+        settle();
+    }
+    __device__ __forceinline__ void settle()
+    {
+        place = place_of<V>(a, chain, seat.lane);
+        in = S::inside(a, place, seat.lane);
+        place.stretch(a, CLUSTER ? window * a.blocks + seat.rank : 0, seat.warp, CLUSTER ? STEPS : a.steps);
+    }
+    __device__ __forceinline__ bool next()
+    {
+        if (CLUSTER) {
+            window += BACK ? -1 : 1;
+            if (BACK ? window < 0 : window >= windows) return false;
+            place.stretch(a, window * a.blocks + seat.rank, seat.warp, STEPS);
+        } else {
+            chain += (int64_t)gridDim.x * seat.groups;
+            if (chain - seat.group >= a.chains) return false;
+            settle();
+        }
+        return true;
+    }
+    // of a line that was at the item before
+    __device__ __forceinline__ void follow(char *&line, const ScanTensor &t) const
+    {
+        if (CLUSTER) line += (BACK ? -1 : 1) * (int64_t)a.blocks * SPAN * t.st * (int64_t)sizeof(T);
+        else line = S::chunk(t, place, seat.lane);
+    }
+};
+
 template <typename T, int V, int CHUNK, bool CLUSTER>
-__global__ void __launch_bounds__(32 * WARPS, CLUSTER ? 2 : FORWARD_BLOCKS) scan_forward_kernel(const __grid_constant__ ScanArgs a)
+__global__ void __launch_bounds__(32 * WARPS, FORWARD_BLOCKS) scan_forward_kernel(const __grid_constant__ ScanArgs a)
 {
     typedef Stage<T, V, CHUNK> S;
     typedef Lane<T, V> L;
     typedef typename Vec<V>::type F;
     __shared__ Board<V, CLUSTER, false> board;
-    extern __shared__ uint4 room[];                                  // [2 in turn][warp][gate, x]
-    const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
-    const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
-    const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
-    if (CLUSTER) cluster_arrive();                      // completed by the wait before the first remote store
+    extern __shared__ uint4 room[];                                  // [warp][gate, x, the next x]
+    const Seat<CLUSTER> seat(a);
+    Joins<V, CLUSTER, false> joins = {board, a.stretches, a.blocks, seat.rank, seat.warp, seat.lane, seat.group * a.stretches, 0};
+    joins.open();
 
-    auto item = first_item<CLUSTER, false>(a, group, groups);
-    Place next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
-    auto stage = [&](int turn, int which) { return S{reinterpret_cast<char *>(room) + ((turn * WARPS + index) * 2 + which) * S::BYTES, lane}; };
-    auto fetch = [&](const Place &p, int turn) {
-        stage(turn, 0).fetch(a, a.gate, p, p.valid, words_of<T>(INFINITY));
-        stage(turn, 1).fetch(a, a.x, p, p.valid, 0u);
-        fetches_end();
-    };
-    fetch(next, 0);
+    Items<T, V, CHUNK, CLUSTER, false> item(a, seat);
+    char *const stages = reinterpret_cast<char *>(room) + seat.index * 3 * S::BYTES;
+    const S z = {stages, seat.lane};
+    S x = {stages + S::BYTES, seat.lane}, spare = {stages + 2 * S::BYTES, seat.lane};
+    char *line_z = S::chunk(a.gate, item.place, seat.lane), *line_x = S::chunk(a.x, item.place, seat.lane),
+         *line_out = S::chunk(a.out, item.place, seat.lane);
+    z.fetch(line_z, S::round(a.gate), item.in, item.place.valid, words_of<T>(INFINITY));
+    x.fetch(line_x, S::round(a.x), item.in, item.place.valid, 0u);
+    fetches_end();
 
-    Joins<V, CLUSTER, false> joins = {board, a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
-    F carry = load_state<V>(a.h0, next.b, a.channels, next, lane);
+    F carry = load_state<V>(a.h0, item.place.b, a.channels, item.place, seat.lane);       // negated, as all states are
     if (CLUSTER) cluster_wait();
     bool more;
-    int turn = 0;
     do {
-        const Place p = next;
-        more = item.next(a);
-        if (more) {
-            next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
-            fetch(next, turn ^ 1);
-        } else {
-            fetches_end();
-        }
-        if (!CLUSTER) carry = load_state<V>(a.h0, p.b, a.channels, p, lane);
-        fetches_wait();
-        const S z = stage(turn, 0), x = stage(turn, 1);
-        turn ^= 1;
+        const Place p = item.place;
+        const bool in = item.in;
+        fetches_wait<0>();
         F n[STEPS];
         Affine<V> own = {all_of<V>(1.0f), all_of<V>(0.0f)};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             n[s] = minus_shut(exp_of<T, false>(L::get(z[s])));
-            own.b = advance(n[s], own.b, L::get_negative(x[s]));
+            own.b = advance(n[s], own.b, L::get(x[s]));
             own.p = fma_of(n[s], own.p, own.p);
         }
+        // the gates' stage is free again, and the results will take the place of x
         F into = carry;
+        more = item.next();
+        __syncwarp();
+        if (more) {
+            item.follow(line_z, a.gate);
+            item.follow(line_x, a.x);
+            z.fetch(line_z, S::round(a.gate), item.in, item.place.valid, words_of<T>(INFINITY));
+            spare.fetch(line_x, S::round(a.x), item.in, item.place.valid, 0u);
+            if (!CLUSTER) carry = load_state<V>(a.h0, item.place.b, a.channels, item.place, seat.lane);
+        }
+        fetches_end();
         if (CLUSTER || a.stretches > 1) {
             joins.give(own, own.b, own.b);
-            into = joins.take(carry);
+            into = CLUSTER ? joins.take(carry) : joins.take(into);
         }
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            into = advance(n[s], into, L::get_negative(x[s]));
-            x[s] = L::put(into);
+            into = advance(n[s], into, L::get(x[s]));
+            x[s] = L::put_negative(into);
         }
         __syncwarp();
-        x.write(a, a.out, p);
-        if (warp == a.stretches - 1) {
-            if (p.k < a.spans - 1) store_state<V>(a.states, p.b * (a.spans - 1) + p.k, a.channels, p, lane, into);
-            else if (p.k == a.spans - 1) store_state<V>(a.final_state, p.b, a.channels, p, lane, into);
+        x.write(line_out, S::round(a.out), in, p);
+        if (seat.warp == a.stretches - 1) {
+            if (p.k < a.spans - 1) store_state<V>(a.states, p.b * (a.spans - 1) + p.k, a.channels, p, seat.lane, into);
+            else if (p.k == a.spans - 1) store_state<V>(a.final_state, p.b, a.channels, p, seat.lane, into);
         }
-        __syncwarp();                                                // before the stage is filled again
+        item.follow(line_out, a.out);
+        const S was = x;
+        x = spare;
+        spare = was;
     } while (more);
+    joins.close(a.stalls);
 }
 
 template <typename T, int V, int CHUNK, bool CLUSTER>
@@ -426,52 +527,59 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
     typedef Lane<T, V> L;
     typedef typename Vec<V>::type F;
     __shared__ Board<V, CLUSTER, true> board;
-    extern __shared__ uint4 room[];                                  // [2 in turn][warp][gate, x, dout]
-    const int lane = threadIdx.x & 31, index = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
-    const int group = CLUSTER ? 0 : index / a.stretches, warp = CLUSTER ? index : index - group * a.stretches;
-    const int rank = CLUSTER ? (int)cluster_rank() : 0, groups = CLUSTER ? 1 : (blockDim.x >> 5) / a.stretches;
-    if (CLUSTER) cluster_arrive();
+    extern __shared__ uint4 room[];                                  // [warp][2 in turn][gate, x, dout]
+    const Seat<CLUSTER> seat(a);
+    Joins<V, CLUSTER, true> joins = {board, a.stretches, a.blocks, seat.rank, seat.warp, seat.lane, seat.group * a.stretches, 0};
+    joins.open();
 
-    auto item = first_item<CLUSTER, true>(a, group, groups);
-    Place next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
-    auto stage = [&](int turn, int which) { return S{reinterpret_cast<char *>(room) + ((turn * WARPS + index) * 3 + which) * S::BYTES, lane}; };
-    auto fetch = [&](const Place &p, int turn) {
-        stage(turn, 0).fetch(a, a.gate, p, p.valid, words_of<T>(INFINITY));
-        stage(turn, 1).fetch(a, a.x, p, p.valid, 0u);
-        stage(turn, 2).fetch(a, a.dout, p, a.dout.p ? p.valid : 0, 0u);
-        fetches_end();
+    Items<T, V, CHUNK, CLUSTER, true> item(a, seat);
+    char *const stages = reinterpret_cast<char *>(room) + seat.index * 6 * S::BYTES;
+    char *line_z = S::chunk(a.gate, item.place, seat.lane), *line_x = S::chunk(a.x, item.place, seat.lane),
+         *line_g = S::chunk(a.dout, item.place, seat.lane), *line_dx = S::chunk(a.dx, item.place, seat.lane),
+         *line_dz = S::chunk(a.dgate, item.place, seat.lane);
+    auto fetch = [&](int turn) {
+        char *const to = stages + turn * 3 * S::BYTES;
+        S{to, seat.lane}.fetch(line_z, S::round(a.gate), item.in, item.place.valid, words_of<T>(INFINITY));
+        S{to + S::BYTES, seat.lane}.fetch(line_x, S::round(a.x), item.in, item.place.valid, 0u);
+        S{to + 2 * S::BYTES, seat.lane}.fetch(line_g, S::round(a.dout), item.in, a.dout.p ? item.place.valid : 0, 0u);
     };
-    fetch(next, 0);
+    fetch(0);
+    fetches_end();
 
-    Joins<V, CLUSTER, true> joins = {board, a.stretches, a.blocks, rank, warp, lane, group * a.stretches, 0};
-    F carry = load_state<V>(a.dfinal, next.b, a.channels, next, lane);
-    if (CLUSTER) cluster_wait();
+    F carry = all_of<V>(0.0f);
+    if (CLUSTER) {
+        carry = load_state<V>(a.dfinal, item.place.b, a.channels, item.place, seat.lane, 1.0f);
+        cluster_wait();
+    }
     bool more;
     int turn = 0;
     do {
-        const Place p = next;
-        more = item.next(a);
+        const Place p = item.place;
+        const bool in = item.in;
+        more = item.next();
         if (more) {
-            next = place_of<V>(a, item.chain, lane, item.window * a.blocks + rank, warp);
-            fetch(next, turn ^ 1);
-        } else {
-            fetches_end();
+            item.follow(line_z, a.gate);
+            item.follow(line_x, a.x);
+            item.follow(line_g, a.dout);
+            fetch(turn ^ 1);
         }
-        F h;                                                         // the state before the block's span
-        if (p.k == 0) h = load_state<V>(a.h0, p.b, a.channels, p, lane);
-        else h = load_state<V>(p.k < a.spans ? a.states : nullptr, p.b * (a.spans - 1) + p.k - 1, a.channels, p, lane);
-        if (!CLUSTER) carry = load_state<V>(a.dfinal, p.b, a.channels, p, lane);
-        fetches_wait();
-        const S z = stage(turn, 0), x = stage(turn, 1), g = stage(turn, 2);
+        fetches_end();
+        F h;                                                         // the state before the block's span, negated
+        if (p.k == 0) h = load_state<V>(a.h0, p.b, a.channels, p, seat.lane);
+        else h = load_state<V>(p.k < a.spans ? a.states : nullptr, p.b * (a.spans - 1) + p.k - 1, a.channels, p, seat.lane);
+        if (!CLUSTER) carry = load_state<V>(a.dfinal, p.b, a.channels, p, seat.lane, 1.0f);
+        fetches_wait<1>();
+        char *const at = stages + turn * 3 * S::BYTES;
+        const S z = {at, seat.lane}, x = {at + S::BYTES, seat.lane}, g = {at + 2 * S::BYTES, seat.lane};
         turn ^= 1;
-        F n[STEPS], d[STEPS], hb = all_of<V>(0.0f);                  // d: a (1 - a), then that times h_(t-1) - x_t
+        F n[STEPS], d[STEPS], hb = all_of<V>(0.0f);                  // d: -a (1 - a), then that times x_t - h_(t-1)
         Affine<V> own = {all_of<V>(1.0f), all_of<V>(0.0f)};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             const F e = exp_of<T, true>(L::get(z[s]));
             n[s] = minus_shut(e);
             d[s] = mul_of(mul_of(e, n[s]), n[s]);                    // -a times -(1 - a)
-            hb = advance(n[s], hb, L::get_negative(x[s]));
+            hb = advance(n[s], hb, L::get(x[s]));
             own.p = fma_of(n[s], own.p, own.p);
             own.b = fma_of(own.p, L::get(g[s]), own.b);
         }
@@ -479,9 +587,9 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
         if (joined) joins.give(own, hb, h);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            const F minus_x = L::get_negative(x[s]);
-            d[s] = mul_of(d[s], add_of(h, minus_x));
-            h = advance(n[s], h, minus_x);
+            const F xf = L::get(x[s]);
+            d[s] = mul_of(d[s], add_of(h, xf));                      // a (1 - a) (x_t - h_(t-1))
+            h = advance(n[s], h, xf);
         }
         F into = joined ? joins.take(carry) : carry;
 #pragma unroll
@@ -489,14 +597,17 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
             const F full = add_of(L::get(g[s]), into);
             x[s] = L::put_negative(mul_of(n[s], full));
             into = fma_of(n[s], full, full);
-            z[s] = L::put(mul_of(d[s], full));
+            z[s] = L::put_negative(mul_of(d[s], full));
         }
         __syncwarp();
-        x.write(a, a.dx, p);
-        z.write(a, a.dgate, p);
-        if (p.k == 0 && warp == 0) store_state<V>(a.dh0, p.b, a.channels, p, lane, into);
+        x.write(line_dx, S::round(a.dx), in, p);
+        z.write(line_dz, S::round(a.dgate), in, p);
+        item.follow(line_dx, a.dx);
+        item.follow(line_dz, a.dgate);
+        if (p.k == 0 && seat.warp == 0) store_state<V>(a.dh0, p.b, a.channels, p, seat.lane, into, 1.0f);
         __syncwarp();                                                // before the stage is filled again
     } while (more);
+    joins.close(a.stalls);
 }
 
 template <typename T, int V, int CHUNK>
@@ -512,7 +623,7 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
     auto kernel = backward ? cluster ? scan_backward_kernel<T, V, CHUNK, true> : scan_backward_kernel<T, V, CHUNK, false>
                            : cluster ? scan_forward_kernel<T, V, CHUNK, true> : scan_forward_kernel<T, V, CHUNK, false>;
     SharedRecord &record = records[2 * backward + cluster];
-    const size_t shared = (size_t)2 * (backward ? 3 : 2) * WARPS * Stage<T, V, CHUNK>::BYTES;
+    const size_t shared = (size_t)(backward ? 6 : 3) * WARPS * Stage<T, V, CHUNK>::BYTES;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr = {};
     int64_t grid;
@@ -539,6 +650,11 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
         const int64_t most = (int64_t)sm_count() * (backward ? BACKWARD_BLOCKS : FORWARD_BLOCKS);
         grid = (a.chains + groups - 1) / groups;
         if (grid > most) grid = most;
+    }
+    if (cluster) {
+        a.stalls = stall_counter();
+        gs_status s = stalled_before();
+        if (s != GS_OK) return s;
     }
     if (grid > 0x7FFFFFFF) {
         set_error("a recurrence of %lld blocks exceeds one launch", (long long)grid);
