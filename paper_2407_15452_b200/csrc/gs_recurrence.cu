@@ -36,7 +36,7 @@ struct ScanArgs {
     Divider by_slabs;
     int64_t batch, channels, chains;      // chains = batch * slabs
     int32_t length, slabs, spans;         // slabs of 32 * V channels; spans = ceil(length / SPAN)
-    int32_t stretches, steps;             // warps that share a span, positions of each
+    int32_t stretches;                    // warps that share a span
     int32_t blocks;                       // blocks of a cluster
     unsigned long long *stalls;           // where blocks whose waits ran out are counted
 };
@@ -60,6 +60,11 @@ template <typename T, int V> struct Lane;
 template <typename T> struct Lane<T, 1> {
     typedef T raw;
     static __device__ __forceinline__ float get(raw r) { return to_float(r); }
+    static __device__ __forceinline__ raw at_most_88(raw r)
+    {
+        if constexpr (sizeof(T) == 4) return r;       // exp_of does it
+        else return __hmin_nan(r, from_float<T>(88.0f));
+    }
     static __device__ __forceinline__ raw put(float f) { return from_float<T>(f); }
     static __device__ __forceinline__ raw put_negative(float f) { return from_float<T>(-f); }
 };
@@ -71,30 +76,36 @@ template <typename T> struct Lane<T, 2> {
         unpack2<T>(r, f.x, f.y);
         return f;
     }
+    static __device__ __forceinline__ raw at_most_88(raw r)
+    {
+        typedef typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type two;
+        const uint32_t most = pack2<T>(88.0f, 88.0f);
+        const two m = __hmin2_nan(*reinterpret_cast<const two *>(&r), *reinterpret_cast<const two *>(&most));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
     static __device__ __forceinline__ raw put(float2 f) { return pack2<T>(f.x, f.y); }
-    static __device__ __forceinline__ raw put_negative(float2 f) { return pack2<T>(-f.x, -f.y); }
+    static __device__ __forceinline__ raw put_negative(float2 f) { return put(f) ^ 0x80008000u; }
 };
 
 // exp(z) = 2^y, y = z log2(e).  Rounding y costs |z| 2^-24 of the result, which tensors of 16 bits do not see; fp32 tensors get the first
-// term of what it left out back.  Beyond 2^127 an infinity or, where products follow that have no use for one, about 2^127.
+// term of what it left out back.  Where products follow that have no use for an infinity, z is held to 88 (Lane::at_most_88,
+// in the words that it travels in); 1 / (1 + exp(88)) is zero already, as all that is below 2^-126.  NaN stays NaN.
 static constexpr float LOG2_E = 1.44269504f, LOG2_E_REST = 1.92596299e-8f, LN_2 = 0.693147181f;
-template <typename T, bool FINITE> __device__ __forceinline__ float exp_of_one(float z, float y)
+template <typename T> __device__ __forceinline__ float exp_of_one(float z, float y)
 {
-    // NaN stays what it is
-    if (FINITE && sizeof(T) == 2) asm("min.NaN.f32 %0, %0, 0f42FF0000;" : "+f"(y));                          // 127.5
     if constexpr (sizeof(T) == 4) {
-        asm("min.NaN.f32 %0, %0, 0f42B0BD4A;\n\tmax.NaN.f32 %0, %0, 0fC2C80000;" : "+f"(z));                   // 88.36971 (127.5 ln 2), -100
+        asm("min.NaN.f32 %0, %0, 0f42B00000;\n\tmax.NaN.f32 %0, %0, 0fC2C80000;" : "+f"(z));                   // to [-100, 88]
         y = LOG2_E * z;
         const float rest = fmaf(LOG2_E, z, -y) + LOG2_E_REST * z;
         return tc::exp2_fast(y) * fmaf(LN_2, rest, 1.0f);
     }
     return tc::exp2_fast(y);
 }
-template <typename T, bool FINITE> __device__ __forceinline__ float exp_of(float z) { return exp_of_one<T, FINITE>(z, LOG2_E * z); }
-template <typename T, bool FINITE> __device__ __forceinline__ float2 exp_of(float2 z)
+template <typename T> __device__ __forceinline__ float exp_of(float z) { return exp_of_one<T>(z, LOG2_E * z); }
+template <typename T> __device__ __forceinline__ float2 exp_of(float2 z)
 {
     const float2 y = mul_of(z, make_float2(LOG2_E, LOG2_E));
-    return make_float2(exp_of_one<T, FINITE>(z.x, y.x), exp_of_one<T, FINITE>(z.y, y.y));
+    return make_float2(exp_of_one<T>(z.x, y.x), exp_of_one<T>(z.y, y.y));
 }
 __device__ __forceinline__ float reciprocal(float x) { return tc::rcp_fast(x); }
 __device__ __forceinline__ float2 reciprocal(float2 x) { return make_float2(tc::rcp_fast(x.x), tc::rcp_fast(x.y)); }
@@ -117,11 +128,11 @@ struct Place {                            // what a warp works on: positions [t0
     int k, t0, rows, valid;               // k: the span
     bool there, on;                       // the warp has a chain; and the lane a channel
 
-    __device__ __forceinline__ void stretch(const ScanArgs &a, int span, int warp, int steps)
+    __device__ __forceinline__ void stretch(const ScanArgs &a, int span, int warp)
     {
         k = span;
-        t0 = k * SPAN + warp * steps;
-        rows = there ? min(max(a.length - t0, 0), steps) : 0;
+        t0 = k * SPAN + warp * STEPS;
+        rows = there ? min(max(a.length - t0, 0), STEPS) : 0;
         valid = min(rows, max(len - t0, 0));
     }
 };
@@ -364,26 +375,23 @@ struct Joins {
     }
 };
 
-// a lane's states, times `sign`
 template <int V>
-__device__ __forceinline__ typename Vec<V>::type load_state(const float *from, int64_t row, int64_t channels, const Place &p, int lane,
-                                                            float sign = -1.0f)
+__device__ __forceinline__ typename Vec<V>::type load_state(const float *from, int64_t row, int64_t channels, const Place &p, int lane)
 {
     if (!from || !p.on) return all_of<V>(0.0f);
     from += row * channels + p.c + lane * V;
-    if constexpr (V == 1) return sign * from[0];
-    else return make_float2(sign * from[0], sign * from[1]);
+    if constexpr (V == 1) return from[0];
+    else return make_float2(from[0], from[1]);
 }
 template <int V>
-__device__ __forceinline__ void store_state(float *to, int64_t row, int64_t channels, const Place &p, int lane, typename Vec<V>::type h,
-                                            float sign = -1.0f)
+__device__ __forceinline__ void store_state(float *to, int64_t row, int64_t channels, const Place &p, int lane, typename Vec<V>::type h)
 {
     if (!to || !p.on) return;
     to += row * channels + p.c + lane * V;
-    if constexpr (V == 1) to[0] = sign * h;
+    if constexpr (V == 1) to[0] = h;
     else {
-        to[0] = sign * h.x;
-        to[1] = sign * h.y;
+        to[0] = h.x;
+        to[1] = h.y;
     }
 }
 
@@ -425,14 +433,14 @@ struct Items {
     {
         place = place_of<V>(a, chain, seat.lane);
         in = S::inside(a, place, seat.lane);
-        place.stretch(a, CLUSTER ? window * a.blocks + seat.rank : 0, seat.warp, CLUSTER ? STEPS : a.steps);
+        place.stretch(a, CLUSTER ? window * a.blocks + seat.rank : 0, seat.warp);
     }
     __device__ __forceinline__ bool next()
     {
         if (CLUSTER) {
             window += BACK ? -1 : 1;
             if (BACK ? window < 0 : window >= windows) return false;
-            place.stretch(a, window * a.blocks + seat.rank, seat.warp, STEPS);
+            place.stretch(a, window * a.blocks + seat.rank, seat.warp);
         } else {
             chain += (int64_t)gridDim.x * seat.groups;
             if (chain - seat.group >= a.chains) return false;
@@ -470,23 +478,24 @@ __global__ void __launch_bounds__(32 * WARPS, FORWARD_BLOCKS) scan_forward_kerne
     x.fetch(line_x, S::round(a.x), item.in, item.place.valid, 0u);
     fetches_end();
 
-    F carry = load_state<V>(a.h0, item.place.b, a.channels, item.place, seat.lane);       // negated, as all states are
+    const F minus = all_of<V>(-1.0f);
+    F next_h = load_state<V>(a.h0, item.place.b, a.channels, item.place, seat.lane), carry = mul_of(next_h, minus);
     if (CLUSTER) cluster_wait();
     bool more;
     do {
         const Place p = item.place;
         const bool in = item.in;
+        if (!CLUSTER) carry = mul_of(next_h, minus);                 // negated, as all states are
         fetches_wait<0>();
         F n[STEPS];
         Affine<V> own = {all_of<V>(1.0f), all_of<V>(0.0f)};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            n[s] = minus_shut(exp_of<T, false>(L::get(z[s])));
+            n[s] = minus_shut(exp_of<T>(L::get(z[s])));
             own.b = advance(n[s], own.b, L::get(x[s]));
             own.p = fma_of(n[s], own.p, own.p);
         }
         // the gates' stage is free again, and the results will take the place of x
-        F into = carry;
         more = item.next();
         __syncwarp();
         if (more) {
@@ -494,12 +503,13 @@ __global__ void __launch_bounds__(32 * WARPS, FORWARD_BLOCKS) scan_forward_kerne
             item.follow(line_x, a.x);
             z.fetch(line_z, S::round(a.gate), item.in, item.place.valid, words_of<T>(INFINITY));
             spare.fetch(line_x, S::round(a.x), item.in, item.place.valid, 0u);
-            if (!CLUSTER) carry = load_state<V>(a.h0, item.place.b, a.channels, item.place, seat.lane);
+            if (!CLUSTER) next_h = load_state<V>(a.h0, item.place.b, a.channels, item.place, seat.lane);
         }
         fetches_end();
+        F into = carry;
         if (CLUSTER || a.stretches > 1) {
             joins.give(own, own.b, own.b);
-            into = CLUSTER ? joins.take(carry) : joins.take(into);
+            into = joins.take(carry);
         }
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
@@ -509,8 +519,8 @@ __global__ void __launch_bounds__(32 * WARPS, FORWARD_BLOCKS) scan_forward_kerne
         __syncwarp();
         x.write(line_out, S::round(a.out), in, p);
         if (seat.warp == a.stretches - 1) {
-            if (p.k < a.spans - 1) store_state<V>(a.states, p.b * (a.spans - 1) + p.k, a.channels, p, seat.lane, into);
-            else if (p.k == a.spans - 1) store_state<V>(a.final_state, p.b, a.channels, p, seat.lane, into);
+            if (p.k < a.spans - 1) store_state<V>(a.states, p.b * (a.spans - 1) + p.k, a.channels, p, seat.lane, mul_of(into, minus));
+            else if (p.k == a.spans - 1) store_state<V>(a.final_state, p.b, a.channels, p, seat.lane, mul_of(into, minus));
         }
         item.follow(line_out, a.out);
         const S was = x;
@@ -546,28 +556,30 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
     fetch(0);
     fetches_end();
 
-    F carry = all_of<V>(0.0f);
-    if (CLUSTER) {
-        carry = load_state<V>(a.dfinal, item.place.b, a.channels, item.place, seat.lane, 1.0f);
-        cluster_wait();
-    }
+    // the state before the item's span, and r behind its end: asked for with the inputs
+    auto state_before = [&](const Place &p) {
+        if (p.k == 0) return load_state<V>(a.h0, p.b, a.channels, p, seat.lane);
+        return load_state<V>(p.k < a.spans ? a.states : nullptr, p.b * (a.spans - 1) + p.k - 1, a.channels, p, seat.lane);
+    };
+    F next_h = state_before(item.place), carry = load_state<V>(a.dfinal, item.place.b, a.channels, item.place, seat.lane), next_carry = carry;
+    if (CLUSTER) cluster_wait();
     bool more;
     int turn = 0;
     do {
         const Place p = item.place;
         const bool in = item.in;
+        F h = mul_of(next_h, all_of<V>(-1.0f));                      // negated, as all states are
+        if (!CLUSTER) carry = next_carry;
         more = item.next();
         if (more) {
             item.follow(line_z, a.gate);
             item.follow(line_x, a.x);
             item.follow(line_g, a.dout);
             fetch(turn ^ 1);
+            next_h = state_before(item.place);
+            if (!CLUSTER) next_carry = load_state<V>(a.dfinal, item.place.b, a.channels, item.place, seat.lane);
         }
         fetches_end();
-        F h;                                                         // the state before the block's span, negated
-        if (p.k == 0) h = load_state<V>(a.h0, p.b, a.channels, p, seat.lane);
-        else h = load_state<V>(p.k < a.spans ? a.states : nullptr, p.b * (a.spans - 1) + p.k - 1, a.channels, p, seat.lane);
-        if (!CLUSTER) carry = load_state<V>(a.dfinal, p.b, a.channels, p, seat.lane, 1.0f);
         fetches_wait<1>();
         char *const at = stages + turn * 3 * S::BYTES;
         const S z = {at, seat.lane}, x = {at + S::BYTES, seat.lane}, g = {at + 2 * S::BYTES, seat.lane};
@@ -576,7 +588,7 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
         Affine<V> own = {all_of<V>(1.0f), all_of<V>(0.0f)};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            const F e = exp_of<T, true>(L::get(z[s]));
+            const F e = exp_of<T>(L::get(L::at_most_88(z[s])));
             n[s] = minus_shut(e);
             d[s] = mul_of(mul_of(e, n[s]), n[s]);                    // -a times -(1 - a)
             hb = advance(n[s], hb, L::get(x[s]));
@@ -604,7 +616,7 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
         z.write(line_dz, S::round(a.dgate), in, p);
         item.follow(line_dx, a.dx);
         item.follow(line_dz, a.dgate);
-        if (p.k == 0 && seat.warp == 0) store_state<V>(a.dh0, p.b, a.channels, p, seat.lane, into, 1.0f);
+        if (p.k == 0 && seat.warp == 0) store_state<V>(a.dh0, p.b, a.channels, p, seat.lane, into);
         __syncwarp();                                                // before the stage is filled again
     } while (more);
     joins.close(a.stalls);
@@ -632,7 +644,6 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
         const int windows = (a.spans + MOST_BLOCKS - 1) / MOST_BLOCKS;
         a.blocks = (a.spans + windows - 1) / windows;
         a.stretches = WARPS;
-        a.steps = STEPS;
         grid = a.chains * a.blocks;
         cfg.blockDim = dim3(32 * WARPS);
         attr.id = cudaLaunchAttributeClusterDimension;
@@ -644,7 +655,6 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
         // several chains a block where one needs few warps
         a.blocks = 1;
         a.stretches = a.length > STEPS ? (a.length + STEPS - 1) / STEPS : 1;
-        a.steps = (a.length + a.stretches - 1) / a.stretches;
         const int groups = WARPS / a.stretches > 0 ? WARPS / a.stretches : 1;
         cfg.blockDim = dim3(32 * groups * a.stretches);
         const int64_t most = (int64_t)sm_count() * (backward ? BACKWARD_BLOCKS : FORWARD_BLOCKS);
