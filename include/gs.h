@@ -534,12 +534,13 @@ GS_API gs_status gs_sgns_epoch(const gs_graph *g, const uint64_t *d_alias,
 GS_API gs_status gs_refused_ids(uint64_t *h_count, int32_t clear, void *stream);
 
 /*
- * Sticky per-device count of thread blocks of the tensor-core attention kernels that gave up a wait inside
+ * Sticky per-device count of thread blocks of the tensor-core attention kernels, and of the recurrence's over more
+ * than 128 positions (whose blocks hand states to one another), that gave up a wait inside
  * the kernel (about twenty seconds without progress; the results of that call are then not valid).
  * No finite input causes it (a row of gradients that has to be computed a second time, below, over some 10^6 positions
  * and query heads takes that long); it is there so that a fault of the hardware or of the library ends as an error and not
- * as a hang.  While the count is not zero, gs_attention_forward and gs_attention_backward on that device
- * return GS_ERR_CUDA: the call after the one that failed reports it, as the runtime does with errors of kernels.
+ * as a hang.  While the count is not zero, gs_attention_forward, gs_attention_backward and the recurrence's calls over more than 128
+ * positions return GS_ERR_CUDA on that device: the call after the one that failed reports it, as the runtime does with errors of kernels.
  * Reads the count of the current device after the work queued on `stream`, clears it if clear != 0, and WAITS.
  * gs_stall_drill queues one block whose wait nothing ends (it gives up within about two seconds), so that an application
  * can see what it does with the error; the count goes up by one, no data is touched.  Errors: GS_ERR_OOM, GS_ERR_CUDA.
