@@ -19,7 +19,7 @@ struct PackArgs {
 
 // Lanes that hold a block of columns, and values of a lane's access
 template <typename T, bool ALIGNED> struct Holders {
-    static constexpr int VEC = ALIGNED ? Wide<T>::N : 1, LANES = ALIGNED ? KEPT_BLOCK / VEC : 32, PIECES = KEPT_BLOCK / VEC / LANES;
+    static constexpr int VEC = ALIGNED ? Wide<T>::N : 1, LANES = ALIGNED ? KEPT_BLOCK / VEC : 32, PIECES = KEPT_BLOCK / VEC / LANES, N = VEC % 2 ? VEC : VEC / 2;
     static constexpr int AT_ONCE = ALIGNED ? 4 : 1;                    // blocks that a group of lanes has under way
 };
 
@@ -62,22 +62,21 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const __grid_constan
         }
 #pragma unroll
         for (int u = 0; u < H::AT_ONCE; ++u) {
-            float f[H::PIECES][H::VEC];
+            typename P::F f[H::PIECES][H::N];
             uint32_t top = 0;
 #pragma unroll
             for (int k = 0; k < H::PIECES; ++k) {
                 P::get(r[u][k], f[k]);
 #pragma unroll
-                for (int e = 0; e < H::VEC; ++e) top = max(top, magnitude(f[k][e]));
+                for (int e = 0; e < H::N; ++e) top = max(top, magnitude(f[k][e]));
             }
             const KeptScale scale(largest<H::LANES>(top));
             if (!at[u].there) continue;
 #pragma unroll
             for (int k = 0; k < H::PIECES; ++k) {
                 const int64_t c = at[u].first + (k * H::LANES + member) * H::VEC;
-                int q[H::VEC];
-#pragma unroll
-                for (int e = 0; e < H::VEC; ++e) q[e] = scale.of(f[k][e]);
+                uint32_t q[H::VEC];
+                scale.of(f[k], q);
                 if (c < a.columns)
                     *reinterpret_cast<typename Kept<H::VEC>::raw *>(a.packed + at[u].row * a.columns + c) = Kept<H::VEC>::put(q);
             }
@@ -116,11 +115,8 @@ __global__ void __launch_bounds__(PACK_THREADS) unpack_kernel(const __grid_const
 #pragma unroll
             for (int k = 0; k < H::PIECES; ++k) {
                 const int64_t c = at[u].first + (k * H::LANES + member) * H::VEC;
-                int q[H::VEC];
-                float f[H::VEC];
-                Kept<H::VEC>::get(r[u][k], q);
-#pragma unroll
-                for (int e = 0; e < H::VEC; ++e) f[e] = kept_value(q[e], s[u]);
+                typename P::F f[H::N];
+                Kept<H::VEC>::get(r[u][k], s[u], f);
                 if (c < a.columns) *reinterpret_cast<typename P::raw *>(row + c) = P::put(f);
             }
         }

@@ -5,7 +5,10 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "gs_common.cuh"
+#include "gs_tc.cuh"
 
 namespace gs {
 
@@ -50,34 +53,60 @@ template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, fl
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// N neighbouring elements as one access moves them: 16 bytes, or one element where rows are not aligned to that
+// One value, or two neighbours that one instruction works on
+template <int V> struct Vec;
+template <> struct Vec<1> { typedef float type; };
+template <> struct Vec<2> { typedef float2 type; };
+__device__ __forceinline__ float fma_of(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float2 fma_of(float2 a, float2 b, float2 c) { return tc::fma2(a, b, c); }
+__device__ __forceinline__ float mul_of(float a, float b) { return a * b; }
+__device__ __forceinline__ float2 mul_of(float2 a, float2 b) { return tc::mul2(a, b); }
+__device__ __forceinline__ float add_of(float a, float b) { return a + b; }
+__device__ __forceinline__ float2 add_of(float2 a, float2 b) { return tc::add2(a, b); }
+__device__ __forceinline__ float sum_of(float a) { return a; }
+__device__ __forceinline__ float sum_of(float2 a) { return a.x + a.y; }
+template <int V> __device__ __forceinline__ typename Vec<V>::type all_of(float x)
+{
+    if constexpr (V == 1) return x;
+    else return make_float2(x, x);
+}
+
+// N neighbouring elements as one access moves them, 16 bytes, or one element where rows are not aligned to that; in fp32 they are N / V
+// pairs (or one value)
 template <typename T, int N> struct Piece;
 template <> struct Piece<float, 4> {
     typedef float4 raw;
+    typedef float2 F;
     static __device__ __forceinline__ raw none() { return make_float4(0.f, 0.f, 0.f, 0.f); }
-    static __device__ __forceinline__ void get(raw r, float (&f)[4]) { f[0] = r.x; f[1] = r.y; f[2] = r.z; f[3] = r.w; }
-    static __device__ __forceinline__ raw put(const float (&f)[4]) { return make_float4(f[0], f[1], f[2], f[3]); }
+    static __device__ __forceinline__ void get(raw r, F (&f)[2])
+    {
+        f[0] = make_float2(r.x, r.y);
+        f[1] = make_float2(r.z, r.w);
+    }
+    static __device__ __forceinline__ raw put(const F (&f)[2]) { return make_float4(f[0].x, f[0].y, f[1].x, f[1].y); }
 };
 template <typename T> struct Piece<T, 8> {
     typedef uint4 raw;
+    typedef float2 F;
     static __device__ __forceinline__ raw none() { return make_uint4(0u, 0u, 0u, 0u); }
-    static __device__ __forceinline__ void get(raw r, float (&f)[8])
+    static __device__ __forceinline__ void get(raw r, F (&f)[4])
     {
-        unpack2<T>(r.x, f[0], f[1]);
-        unpack2<T>(r.y, f[2], f[3]);
-        unpack2<T>(r.z, f[4], f[5]);
-        unpack2<T>(r.w, f[6], f[7]);
+        unpack2<T>(r.x, f[0].x, f[0].y);
+        unpack2<T>(r.y, f[1].x, f[1].y);
+        unpack2<T>(r.z, f[2].x, f[2].y);
+        unpack2<T>(r.w, f[3].x, f[3].y);
     }
-    static __device__ __forceinline__ raw put(const float (&f)[8])
+    static __device__ __forceinline__ raw put(const F (&f)[4])
     {
-        return make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
+        return make_uint4(pack2<T>(f[0].x, f[0].y), pack2<T>(f[1].x, f[1].y), pack2<T>(f[2].x, f[2].y), pack2<T>(f[3].x, f[3].y));
     }
 };
 template <typename T> struct Piece<T, 1> {
     typedef T raw;
+    typedef float F;
     static __device__ __forceinline__ raw none() { return from_float<T>(0.f); }
-    static __device__ __forceinline__ void get(raw r, float (&f)[1]) { f[0] = to_float(r); }
-    static __device__ __forceinline__ raw put(const float (&f)[1]) { return from_float<T>(f[0]); }
+    static __device__ __forceinline__ void get(raw r, F (&f)[1]) { f[0] = to_float(r); }
+    static __device__ __forceinline__ raw put(const F (&f)[1]) { return from_float<T>(f[0]); }
 };
 template <typename T> struct Wide;                    // elements of a 16-byte access
 template <> struct Wide<float> { static constexpr int N = 4; };
@@ -120,6 +149,7 @@ static constexpr int KEPT_BLOCK = 128;                // columns that share a sc
 // Largest magnitude of a block as bits of |x|: as whole numbers these order finite values like the values, and infinities and
 // NaN above all of them, which a maximum of floats would let go.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+__device__ __forceinline__ uint32_t magnitude(float2 x) { return max(magnitude(x.x), magnitude(x.y)); }
 template <int LANES>
 __device__ __forceinline__ uint32_t largest(uint32_t m)
 {
@@ -128,75 +158,109 @@ __device__ __forceinline__ uint32_t largest(uint32_t m)
     return m;
 }
 
-// The whole number nearest to x / s.  The quotient by a rounded reciprocal is at most one off; what remains, x - q s, is a
-// multiple of the smaller operand's last place below s in magnitude and so exact in one multiply-add, and its comparison with s / 2
-// decides, ties to even.  Blocks of small values are scaled up by a power of two first, so that the reciprocal is finite.
+// The whole number nearest to x / s, as the low byte of its sum with WHOLE (a sum in which the last place is one).  x times a rounded reciprocal,
+// rounded to a whole number q, is at most one off; what remains, x - q s, is a multiple of the smaller operand's last place below s in magnitude
+// and so exact in one multiply-add, and where it is not below s / 2 the slow way decides, ties to even: hardly ever.  The same way
+// go blocks of magnitudes whose reciprocal is not finite or whose scale is subnormal (and q possibly beyond 127), scaled up by a power of two.
+static constexpr float WHOLE = 12582912.0f;           // 1.5 * 2^23
 struct KeptScale {
-    float s, up, scaled, inverse;
+    float s, inverse, half;                           // inverse 0: everything becomes 0
+    bool slow;
     __device__ __forceinline__ explicit KeptScale(uint32_t top)
     {
         const float t = __uint_as_float(top);
         s = top >= 0x7F800000u ? __uint_as_float(0x7FFFFFFFu) : __fdiv_rd(t, 127.0f);
-        up = t < 8.67361738e-19f ? 1.20892582e24f : 1.0f;             // 2^-60: 2^80
-        scaled = s * up;
-        inverse = s > 0.0f ? __frcp_rn(scaled) : 0.0f;                // s NaN: 0 as well
+        slow = t < 8.67361738e-19f;                   // 2^-60
+        inverse = slow || !(s > 0.0f) ? 0.0f : __frcp_rn(s);
+        half = 0.5f * s;
     }
-    __device__ __forceinline__ int of(float x) const
+    __device__ __forceinline__ uint32_t slowly(float x) const
     {
-        const float v = x * up;
-        float q = rintf(v * inverse);
-        const float left = fmaf(-q, scaled, v), over = fabsf(left) - 0.5f * scaled;
-        if (over >= 0.0f && inverse > 0.0f && (over > 0.0f || ((int)q & 1))) q += copysignf(1.0f, left);
-        return inverse > 0.0f ? (int)fminf(fmaxf(q, -127.0f), 127.0f) : 0;
+        if (!(s > 0.0f)) return 0u;
+        const float up = slow ? 1.20892582e24f : 1.0f, v = x * up, step = s * up;                  // 2^80
+        float q = rintf(v * __frcp_rn(step));
+        const float left = fmaf(-q, step, v), over = fabsf(left) - 0.5f * step;
+        if (over > 0.0f || (over == 0.0f && ((int)q & 1))) q += copysignf(1.0f, left);
+        return (uint32_t)(int)fminf(fmaxf(q, -127.0f), 127.0f);
+    }
+    // words whose low bytes are the numbers; returns the largest |x - q s|
+    __device__ __forceinline__ float fast(float x, uint32_t (&q)[1]) const
+    {
+        const float t = fmaf(x, inverse, WHOLE);
+        q[0] = __float_as_uint(t);
+        return fabsf(fmaf(WHOLE - t, s, x));
+    }
+    __device__ __forceinline__ float fast(float2 x, uint32_t (&q)[2]) const
+    {
+        const float2 t = tc::fma2(x, make_float2(inverse, inverse), make_float2(WHOLE, WHOLE));
+        q[0] = __float_as_uint(t.x);
+        q[1] = __float_as_uint(t.y);
+        const float2 minus = make_float2(WHOLE - t.x, WHOLE - t.y), left = tc::fma2(minus, make_float2(s, s), x);
+        return fmaxf(fabsf(left.x), fabsf(left.y));
+    }
+    template <typename F, int N, int M>
+    __device__ __forceinline__ void of(const F (&x)[N], uint32_t (&q)[M]) const
+    {
+        constexpr int V = M / N;
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t w[V];
+            most = fmaxf(most, fast(x[i], w));
+#pragma unroll
+            for (int v = 0; v < V; ++v) q[i * V + v] = w[v];
+        }
+        if (inverse > 0.0f && most < half) return;
+        const float *one = reinterpret_cast<const float *>(x);
+#pragma unroll
+        for (int e = 0; e < M; ++e) q[e] = slowly(one[e]);
     }
 };
-__device__ __forceinline__ float kept_value(int q, float s) { return (float)q * s; }
 
-// N neighbouring 8-bit values
+// N neighbouring 8-bit values, and what they stand for
 template <int N> struct Kept;
-template <> struct Kept<8> {
-    typedef uint2 raw;
-    static __device__ __forceinline__ raw none() { return make_uint2(0u, 0u); }
-    static __device__ __forceinline__ void get(raw r, int (&q)[8])
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            q[i] = (int)(r.x << (24 - 8 * i)) >> 24;
-            q[4 + i] = (int)(r.y << (24 - 8 * i)) >> 24;
-        }
-    }
-    static __device__ __forceinline__ raw put(const int (&q)[8])
-    {
-        uint2 r = make_uint2(0u, 0u);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            r.x |= (uint32_t)(q[i] & 255) << (8 * i);
-            r.y |= (uint32_t)(q[4 + i] & 255) << (8 * i);
-        }
-        return r;
-    }
-};
 template <> struct Kept<4> {
     typedef uint32_t raw;
     static __device__ __forceinline__ raw none() { return 0u; }
-    static __device__ __forceinline__ void get(raw r, int (&q)[4])
+    static __device__ __forceinline__ raw put(const uint32_t (&q)[4])
     {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = (int)(r << (24 - 8 * i)) >> 24;
+        return __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
     }
-    static __device__ __forceinline__ raw put(const int (&q)[4])
+    // a byte b under the exponent of 2^23 is 2^23 + b, and b = q + 128
+    static __device__ __forceinline__ float2 two(uint32_t bytes, uint32_t first, float scale)
     {
-        uint32_t r = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r |= (uint32_t)(q[i] & 255) << (8 * i);
-        return r;
+        const float2 f = make_float2(__uint_as_float(__byte_perm(bytes, 0x4B000000u, 0x7440u | first)),
+                                     __uint_as_float(__byte_perm(bytes, 0x4B000000u, 0x7440u | (first + 1))));
+        return tc::mul2(tc::add2(f, make_float2(-8388736.0f, -8388736.0f)), make_float2(scale, scale));
+    }
+    static __device__ __forceinline__ void get(raw r, float scale, float2 (&f)[2])
+    {
+        const uint32_t bytes = r ^ 0x80808080u;
+        f[0] = two(bytes, 0, scale);
+        f[1] = two(bytes, 2, scale);
+    }
+};
+template <> struct Kept<8> {
+    typedef uint2 raw;
+    static __device__ __forceinline__ raw none() { return make_uint2(0u, 0u); }
+    static __device__ __forceinline__ raw put(const uint32_t (&q)[8])
+    {
+        return make_uint2(Kept<4>::put({q[0], q[1], q[2], q[3]}), Kept<4>::put({q[4], q[5], q[6], q[7]}));
+    }
+    static __device__ __forceinline__ void get(raw r, float scale, float2 (&f)[4])
+    {
+        const uint32_t a = r.x ^ 0x80808080u, b = r.y ^ 0x80808080u;
+        f[0] = Kept<4>::two(a, 0, scale);
+        f[1] = Kept<4>::two(a, 2, scale);
+        f[2] = Kept<4>::two(b, 0, scale);
+        f[3] = Kept<4>::two(b, 2, scale);
     }
 };
 template <> struct Kept<1> {
     typedef int8_t raw;
     static __device__ __forceinline__ raw none() { return 0; }
-    static __device__ __forceinline__ void get(raw r, int (&q)[1]) { q[0] = r; }
-    static __device__ __forceinline__ raw put(const int (&q)[1]) { return (int8_t)q[0]; }
+    static __device__ __forceinline__ raw put(const uint32_t (&q)[1]) { return (int8_t)q[0]; }
+    static __device__ __forceinline__ void get(raw r, float scale, float (&f)[1]) { f[0] = (float)r * scale; }
 };
 
 }  // namespace gs

@@ -27,40 +27,59 @@ struct NormArgs {
     const int32_t *lens;
     Divider by_length;
     int64_t rows, length;
+    int64_t step, step_b, step_t;                     // from a team's row to its next: rows, and the same in sequences and positions
     int32_t columns, kept_blocks;                     // kept_blocks = ceil(columns / KEPT_BLOCK)
     int32_t weight_f32;
     float eps;
 };
 
-// A row's place: `there`: it exists; `live`: its position is valid
+// A team's place among the rows, from one to the next without a division: `there`: the row exists; `live`: its position is valid
 struct RowAt {
     int64_t row, b, t;
     bool there, live;
+
+    __device__ __forceinline__ RowAt(const NormArgs &a, int64_t first) : row(first)
+    {
+        b = a.by_length.of(first);
+        t = first - b * a.length;
+        look(a);
+    }
+    __device__ __forceinline__ void look(const NormArgs &a)
+    {
+        there = row < a.rows;
+        live = there && (!a.lens || t < __ldg(a.lens + b));
+    }
+    __device__ __forceinline__ void next(const NormArgs &a)
+    {
+        row += a.step;
+        b += a.step_b;
+        t += a.step_t;
+        if (t >= a.length) {
+            t -= a.length;
+            ++b;
+        }
+        look(a);
+    }
+    template <typename T> __device__ __forceinline__ T *of(const NormRows &r) const { return static_cast<T *>(r.p) + b * r.sb + t * r.st; }
 };
-__device__ __forceinline__ RowAt row_at(const NormArgs &a, int64_t row)
+// the steps of a launch whose teams are `step` rows apart
+inline void set_step(NormArgs &a, int64_t step)
 {
-    RowAt r;
-    r.row = row;
-    r.there = row < a.rows;
-    r.b = r.there ? a.by_length.of(row) : 0;
-    r.t = r.there ? row - r.b * a.length : 0;
-    r.live = r.there && (!a.lens || r.t < __ldg(a.lens + r.b));
-    return r;
-}
-template <typename T>
-__device__ __forceinline__ T *row_of(const NormRows &t, const RowAt &r)
-{
-    return static_cast<T *>(t.p) + r.b * t.sb + r.t * t.st;
+    a.step = step;
+    a.step_b = step / a.length;
+    a.step_t = step % a.length;
 }
 
-// The shape of a team.  LANES 8, 16, 32: part of a warp; 0: the block, of up to 512 threads.  FAR: the rows' weights (and sums)
+// The shape of a team.  LANES 2 to 32: part of a warp; 0: the block, of up to 512 threads.  FAR: the rows' weights (and sums)
 // do not fit the threads' registers: weights are read again for every row, sums live in shared memory.
 template <int VEC_, int NV_, int LANES_, bool FAR_ = false>
 struct Team {
     static constexpr int VEC = VEC_, NV = NV_, LANES = LANES_;
+    static constexpr int V = VEC % 2 == 0 ? 2 : 1, N = VEC / V;       // a piece in fp32: N times V values
     static constexpr bool FAR = FAR_, BLOCK = LANES_ == 0;
     static constexpr int GROUP = BLOCK ? 32 : LANES;                  // lanes that reduce by shuffles
-    static constexpr int KEPT_LANES = GROUP < KEPT_BLOCK / VEC ? GROUP : KEPT_BLOCK / VEC;   // that hold a scale's columns
+    static constexpr int KEPT_LANES = GROUP < KEPT_BLOCK / VEC ? GROUP : KEPT_BLOCK / VEC;   // that hold a scale's columns,
+    static constexpr int KEPT_PIECES = KEPT_BLOCK / VEC / KEPT_LANES < NV ? KEPT_BLOCK / VEC / KEPT_LANES : NV;    // and their pieces
     static constexpr int THREADS = BLOCK ? 512 : NORM_THREADS;        // at most
     static __device__ __forceinline__ int size() { return BLOCK ? blockDim.x : LANES; }
     static __device__ __forceinline__ int member() { return BLOCK ? threadIdx.x : threadIdx.x % LANES; }
@@ -69,31 +88,40 @@ struct Team {
     static __device__ __forceinline__ int column(int v) { return (v * size() + member()) * VEC; }
 };
 
-// Sums over a team, two at a time.  The warps of a block leave theirs in one of two places in turn, so that one barrier a sum is enough:
+// Sums over a team, one or two at a time.  The warps of a block leave theirs in one of two places in turn, so that one barrier a sum is enough:
 // a place is written again two sums later, when every thread has met the barrier in between.
-struct PairSums {
+struct TeamSums {
     float2 (*place)[16];
     int turn;
 };
 template <typename S>
-__device__ __forceinline__ float2 team_sum(float2 v, PairSums &sums)
+__device__ __forceinline__ float team_sum(float v, TeamSums &sums)
 {
 #pragma unroll
-    for (int o = S::GROUP / 2; o; o >>= 1) {
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-    }
+    for (int o = S::GROUP / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (!S::BLOCK) return v;
+    float *place = reinterpret_cast<float *>(sums.place[sums.turn]);
+    sums.turn ^= 1;
+    if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = place[0];
+    for (int w = 1; w < (int)blockDim.x >> 5; ++w) v += place[w];
+    return v;
+}
+template <typename S>
+__device__ __forceinline__ float2 team_sum(float2 v, TeamSums &sums)
+{
+#pragma unroll
+    for (int o = S::GROUP / 2; o; o >>= 1)
+        v = add_of(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
     if (!S::BLOCK) return v;
     float2 *place = sums.place[sums.turn];
     sums.turn ^= 1;
     if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
     __syncthreads();
-    float2 all = place[0];
-    for (int w = 1; w < (int)blockDim.x >> 5; ++w) {
-        all.x += place[w].x;
-        all.y += place[w].y;
-    }
-    return all;
+    v = place[0];
+    for (int w = 1; w < (int)blockDim.x >> 5; ++w) v = add_of(v, place[w]);
+    return v;
 }
 
 // the columns [c, c + VEC) of a row; all of them lie in the row or none (VEC > 1 only where columns % VEC == 0)
@@ -103,31 +131,29 @@ __device__ __forceinline__ typename Piece<T, VEC>::raw load_piece(const T *row, 
     if (live && c < columns) return *reinterpret_cast<const typename Piece<T, VEC>::raw *>(row + c);
     return Piece<T, VEC>::none();
 }
-
-template <typename T> __device__ __forceinline__ float vector_at(const void *p, int32_t f32, int c)
+// the same of a weight or bias, `without` where there is none
+template <typename T, int VEC, typename F, int N>
+__device__ __forceinline__ void vector_piece(const void *p, int32_t f32, int c, int columns, float without, F (&f)[N])
 {
-    return f32 ? static_cast<const float *>(p)[c] : to_float(static_cast<const T *>(p)[c]);
-}
-template <typename T, int VEC>
-__device__ __forceinline__ void vector_piece(const void *p, int32_t f32, int c, int columns, float without, float (&f)[VEC])
-{
+    float *one = reinterpret_cast<float *>(f);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) f[e] = p && c < columns ? vector_at<T>(p, f32, c + e) : without;
+    for (int e = 0; e < VEC; ++e)
+        one[e] = !p || c >= columns ? without : f32 ? static_cast<const float *>(p)[c + e] : to_float(static_cast<const T *>(p)[c + e]);
 }
 
-// Calls launch(Team, threads, shared) with the team for rows of `columns` values.  Teams within a warp hold up to 16 columns a thread and up
-// to 512 in all (joins by shuffles alone); a block's 16 columns a thread up to 8192, 32 beyond.
+// Calls launch(Team, threads) with the team for rows of `columns` values: 16 columns a thread, as few threads as that takes up to a warp (fewer steps
+// to a sum: 128 columns of 16 bits by 8 threads XX, by 16 threads XX us), a block beyond; 32 a thread beyond 8192.
 template <typename T, typename F>
 static gs_status with_team(int columns, bool aligned, F &&launch)
 {
     constexpr int W = Wide<T>::N;
     auto block = [&](int per_thread) { return (columns + 32 * per_thread - 1) / (32 * per_thread) * 32; };
     if (aligned) {
-        if (columns <= 8 * W) return launch(Team<W, 1, 8>(), NORM_THREADS);
-        if (columns <= 16 * W) return launch(Team<W, 1, 16>(), NORM_THREADS);
-        if (columns <= 32 * W) return launch(Team<W, 1, 32>(), NORM_THREADS);
-        if (columns <= 64 * W) return launch(Team<W, 2, 32>(), NORM_THREADS);
-        if (W == 4 && columns <= 512) return launch(Team<W, W == 4 ? 4 : 2, 32>(), NORM_THREADS);
+        if (columns <= 32) return launch(Team<W, 16 / W, 2>(), NORM_THREADS);
+        if (columns <= 64) return launch(Team<W, 16 / W, 4>(), NORM_THREADS);
+        if (columns <= 128) return launch(Team<W, 16 / W, 8>(), NORM_THREADS);
+        if (columns <= 256) return launch(Team<W, 16 / W, 16>(), NORM_THREADS);
+        if (columns <= 512) return launch(Team<W, 16 / W, 32>(), NORM_THREADS);
         if (columns <= 8192) return launch(Team<W, 16 / W, 0>(), block(16));
         return launch(Team<W, 32 / W, 0, true>(), block(32));
     }

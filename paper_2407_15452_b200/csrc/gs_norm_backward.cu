@@ -11,147 +11,139 @@ namespace gs {
 // x of a row as it travels: T, or 8 bits and their scale
 template <typename T, int VEC, bool KEPT> struct Source {
     typename Piece<T, VEC>::raw r;
-    __device__ __forceinline__ void load(const NormArgs &a, const RowAt &at, int c)
+    __device__ __forceinline__ void load(const NormArgs &a, const RowAt &at, const T *row, int c)
     {
-        r = load_piece<T, VEC>(row_of<T>(a.x, at), c, a.columns, at.live);
+        r = load_piece<T, VEC>(row, c, a.columns, at.live);
     }
-    __device__ __forceinline__ void get(float (&f)[VEC]) const { Piece<T, VEC>::get(r, f); }
+    template <typename F, int N> __device__ __forceinline__ void get(F (&f)[N]) const { Piece<T, VEC>::get(r, f); }
 };
 template <typename T, int VEC> struct Source<T, VEC, true> {
     typename Kept<VEC>::raw r;
     float scale;
-    __device__ __forceinline__ void load(const NormArgs &a, const RowAt &at, int c)
+    __device__ __forceinline__ void load(const NormArgs &a, const RowAt &at, const T *, int c)
     {
         const bool on = at.live && c < a.columns;
         r = on ? *reinterpret_cast<const typename Kept<VEC>::raw *>(a.packed + at.row * a.columns + c) : Kept<VEC>::none();
         scale = on ? a.scales[at.row * a.kept_blocks + c / KEPT_BLOCK] : 0.0f;
     }
-    __device__ __forceinline__ void get(float (&f)[VEC]) const
-    {
-        int q[VEC];
-        Kept<VEC>::get(r, q);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) f[e] = kept_value(q[e], scale);
-    }
+    template <typename F, int N> __device__ __forceinline__ void get(F (&f)[N]) const { Kept<VEC>::get(r, scale, f); }
 };
 
 template <typename T, typename S, bool KEPT>
-__global__ void __launch_bounds__(S::THREADS) norm_backward_kernel(const __grid_constant__ NormArgs a)
+__global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_backward_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int VEC = S::VEC, NV = S::NV;
+    constexpr int VEC = S::VEC, NV = S::NV, N = S::N, V = S::V;
     typedef Piece<T, VEC> P;
+    typedef typename Vec<V>::type F;
     __shared__ float2 places[2][16];
-    extern __shared__ float2 shared_sums[];                        // FAR: [NV * VEC][threads]; teams in a warp: [team][column]
-    PairSums sums = {places, 0};
+    extern __shared__ float shared_sums[];                         // FAR: [dweight, dbias][column]; teams in a warp: [team][2][column]
+    TeamSums sums = {places, 0};
     const float inverse = 1.0f / (float)a.columns;
+    constexpr int WIDTH = (S::BLOCK ? 32 : S::LANES) * NV * VEC;   // of a warp's teams
 
-    float w[S::FAR ? 1 : NV][VEC];
-    float2 acc[S::FAR ? 1 : NV][VEC];                              // dweight, dbias
+    F w[S::FAR ? 1 : NV][N], dw[S::FAR ? 1 : NV][N], db[S::FAR ? 1 : NV][N];
+    F *const far_dw = reinterpret_cast<F *>(shared_sums) + threadIdx.x, *const far_db = far_dw + (S::FAR ? NV * N * blockDim.x : 0);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         if (!S::FAR) vector_piece<T, VEC>(a.weight, a.weight_f32, S::column(v), a.columns, 1.0f, w[S::FAR ? 0 : v]);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            if (S::FAR) shared_sums[(v * VEC + e) * blockDim.x + threadIdx.x] = make_float2(0.0f, 0.0f);
-            else acc[S::FAR ? 0 : v][e] = make_float2(0.0f, 0.0f);
+        for (int e = 0; e < N; ++e) {
+            if (S::FAR) far_dw[(v * N + e) * blockDim.x] = far_db[(v * N + e) * blockDim.x] = all_of<V>(0.0f);
+            else dw[S::FAR ? 0 : v][e] = db[S::FAR ? 0 : v][e] = all_of<V>(0.0f);
         }
     }
 
-    const int64_t step = (int64_t)gridDim.x * S::teams();
     int64_t base = (int64_t)blockIdx.x * S::teams();
-    RowAt next = row_at(a, base + S::index());
+    RowAt next(a, base + S::index());
     typename P::raw rdy[NV];
     Source<T, VEC, KEPT> rx[NV];
-    float2 stats = next.live ? reinterpret_cast<const float2 *>(a.stats)[next.row] : make_float2(0.0f, 0.0f);
+    float2 stats;
+    auto load = [&]() {
+        const T *row_x = next.of<const T>(a.x), *row_dy = next.of<const T>(a.dy);
+        stats = next.live ? reinterpret_cast<const float2 *>(a.stats)[next.row] : make_float2(0.0f, 0.0f);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        rx[v].load(a, next, S::column(v));
-        rdy[v] = load_piece<T, VEC>(row_of<T>(a.dy, next), S::column(v), a.columns, next.live);
-    }
-    for (; base < a.rows; base += step) {
+        for (int v = 0; v < NV; ++v) {
+            rx[v].load(a, next, row_x, S::column(v));
+            rdy[v] = load_piece<T, VEC>(row_dy, S::column(v), a.columns, next.live);
+        }
+    };
+    load();
+    for (; base < a.rows; base += a.step) {
         const RowAt at = next;
-        const float rstd = stats.y, mean = stats.x;
-        float xh[NV][VEC], g[NV][VEC];
-        float2 s = make_float2(0.0f, 0.0f);
+        const float rstd = stats.y;
+        const F by = all_of<V>(rstd), minus_mean = all_of<V>(-stats.x);
+        F xh[NV][N], g[NV][N], s1 = all_of<V>(0.0f), s2 = all_of<V>(0.0f);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             rx[v].get(xh[v]);
             P::get(rdy[v], g[v]);
             if (S::column(v) < a.columns) {
-                float wv[VEC];
+                F wv[N];
                 if (S::FAR) vector_piece<T, VEC>(a.weight, a.weight_f32, S::column(v), a.columns, 1.0f, wv);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float h = (xh[v][e] - mean) * rstd, d = g[v][e];
-                    if (S::FAR) {
-                        float2 &c = shared_sums[(v * VEC + e) * blockDim.x + threadIdx.x];
-                        c = make_float2(fmaf(d, h, c.x), c.y + d);
-                    } else {
-                        float2 &c = acc[S::FAR ? 0 : v][e];
-                        c.x = fmaf(d, h, c.x);
-                        c.y += d;
-                    }
+                for (int e = 0; e < N; ++e) {
+                    const F h = mul_of(add_of(xh[v][e], minus_mean), by), d = g[v][e];
+                    F &sum_w = S::FAR ? far_dw[(v * N + e) * blockDim.x] : dw[S::FAR ? 0 : v][e];
+                    F &sum_b = S::FAR ? far_db[(v * N + e) * blockDim.x] : db[S::FAR ? 0 : v][e];
+                    sum_w = fma_of(d, h, sum_w);
+                    sum_b = add_of(sum_b, d);
                     xh[v][e] = h;
-                    g[v][e] = d * (S::FAR ? wv[e] : w[S::FAR ? 0 : v][e]);
-                    s.x += g[v][e];
-                    s.y = fmaf(g[v][e], h, s.y);
+                    g[v][e] = mul_of(d, S::FAR ? wv[e] : w[S::FAR ? 0 : v][e]);
+                    s1 = add_of(s1, g[v][e]);
+                    s2 = fma_of(g[v][e], h, s2);
                 }
             }
         }
-        next = row_at(a, base + step + S::index());
-        stats = next.live ? reinterpret_cast<const float2 *>(a.stats)[next.row] : make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            rx[v].load(a, next, S::column(v));
-            rdy[v] = load_piece<T, VEC>(row_of<T>(a.dy, next), S::column(v), a.columns, next.live);
-        }
-        s = team_sum<S>(s, sums);
-        s.x *= inverse;
-        s.y *= inverse;
+        next.next(a);
+        load();
+        const float2 s = team_sum<S>(make_float2(sum_of(s1), sum_of(s2)), sums);
         if (at.there) {
-            T *to = row_of<T>(a.dx, at);
+            T *to = at.of<T>(a.dx);
+            const F less = all_of<V>(-s.x * inverse), along = all_of<V>(-s.y * inverse);
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int c = S::column(v);
                 if (c < a.columns) {
-                    float o[VEC];
+                    F o[N];
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) o[e] = at.live ? rstd * (g[v][e] - s.x - xh[v][e] * s.y) : 0.0f;
-                    *reinterpret_cast<typename P::raw *>(to + c) = P::put(o);
+                    for (int e = 0; e < N; ++e) o[e] = mul_of(by, fma_of(xh[v][e], along, add_of(g[v][e], less)));
+                    *reinterpret_cast<typename P::raw *>(to + c) = at.live ? P::put(o) : P::none();
                 }
             }
         }
     }
     if (!a.partial) return;
     // [block][2][columns]
-    float *dw = a.partial + (int64_t)blockIdx.x * 2 * a.columns, *db = dw + a.columns;
-    if (S::BLOCK) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c = S::column(v);
-            if (c < a.columns)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float2 t = S::FAR ? shared_sums[(v * VEC + e) * blockDim.x + threadIdx.x] : acc[S::FAR ? 0 : v][e];
-                    dw[c + e] = t.x;
-                    db[c + e] = t.y;
-                }
-        }
-    } else {
-        constexpr int WIDTH = (S::BLOCK ? 32 : S::LANES) * NV * VEC;
+    float *to_dw = a.partial + (int64_t)blockIdx.x * 2 * a.columns, *to_db = to_dw + a.columns;
+    if (!S::BLOCK) {
+        // the teams' sums, side by side
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) shared_sums[S::index() * WIDTH + S::column(v) + e] = acc[S::FAR ? 0 : v][e];
-        __syncthreads();
-        for (int c = threadIdx.x; c < a.columns; c += NORM_THREADS) {
-            float2 t = make_float2(0.0f, 0.0f);
-            for (int i = 0; i < S::teams(); ++i) {
-                t.x += shared_sums[i * WIDTH + c].x;
-                t.y += shared_sums[i * WIDTH + c].y;
+            for (int e = 0; e < VEC; ++e) {
+                float *team = shared_sums + S::index() * 2 * WIDTH + S::column(v) + e;
+                team[0] = reinterpret_cast<const float *>(dw[S::FAR ? 0 : v])[e];
+                team[WIDTH] = reinterpret_cast<const float *>(db[S::FAR ? 0 : v])[e];
             }
-            dw[c] = t.x;
-            db[c] = t.y;
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * a.columns; i += NORM_THREADS) {
+            const float *from = shared_sums + (i < a.columns ? i : WIDTH + i - a.columns);
+            float t = 0.0f;
+            for (int k = 0; k < S::teams(); ++k) t += from[k * 2 * WIDTH];
+            to_dw[i] = t;
+        }
+        return;
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int c = S::column(v);
+        if (c >= a.columns) continue;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const F sum_w = S::FAR ? far_dw[(v * N + e / V) * blockDim.x] : dw[S::FAR ? 0 : v][e / V];
+            const F sum_b = S::FAR ? far_db[(v * N + e / V) * blockDim.x] : db[S::FAR ? 0 : v][e / V];
+            to_dw[c + e] = reinterpret_cast<const float *>(&sum_w)[e % V];
+            to_db[c + e] = reinterpret_cast<const float *>(&sum_b)[e % V];
         }
     }
 }
@@ -189,6 +181,7 @@ static gs_status launch(const NormArgs &args, int threads, int32_t weight_type, 
     if (per_sm > NORM_PARTIALS) per_sm = NORM_PARTIALS;
     const int64_t blocks = (a.rows + teams - 1) / teams, most = (int64_t)sm_count() * per_sm;
     const int grid = (int)(blocks < most ? blocks : most);
+    set_step(a, (int64_t)grid * teams);
     const bool sums = dweight || dbias;
     if (!sums) a.partial = nullptr;
     const size_t shared = (S::FAR ? (size_t)S::NV * S::VEC * threads : S::BLOCK ? 0 : (size_t)NORM_THREADS * S::NV * S::VEC) * sizeof(float2);

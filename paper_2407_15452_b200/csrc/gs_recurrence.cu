@@ -15,7 +15,6 @@
 #include <type_traits>
 
 #include "gs_layers.cuh"
-#include "gs_tc.cuh"
 
 namespace gs {
 
@@ -41,21 +40,7 @@ struct ScanArgs {
     unsigned long long *stalls;           // where blocks whose waits ran out are counted
 };
 
-// V neighbouring channels of a lane: Lane<T, V>::raw as they travel, Vec<V>::type in fp32, two of them in one instruction each
-template <int V> struct Vec;
-template <> struct Vec<1> { typedef float type; };
-template <> struct Vec<2> { typedef float2 type; };
-__device__ __forceinline__ float fma_of(float a, float b, float c) { return fmaf(a, b, c); }
-__device__ __forceinline__ float2 fma_of(float2 a, float2 b, float2 c) { return tc::fma2(a, b, c); }
-__device__ __forceinline__ float mul_of(float a, float b) { return a * b; }
-__device__ __forceinline__ float2 mul_of(float2 a, float2 b) { return tc::mul2(a, b); }
-__device__ __forceinline__ float add_of(float a, float b) { return a + b; }
-__device__ __forceinline__ float2 add_of(float2 a, float2 b) { return tc::add2(a, b); }
-template <int V> __device__ __forceinline__ typename Vec<V>::type all_of(float x)
-{
-    if constexpr (V == 1) return x;
-    else return make_float2(x, x);
-}
+// V neighbouring channels of a lane as they travel, and in fp32
 template <typename T, int V> struct Lane;
 template <typename T> struct Lane<T, 1> {
     typedef T raw;
