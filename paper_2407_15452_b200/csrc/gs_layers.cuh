@@ -164,14 +164,18 @@ __device__ __forceinline__ uint32_t largest(uint32_t m)
 // go blocks of magnitudes whose reciprocal is not finite or whose scale is subnormal (and q possibly beyond 127), scaled up by a power of two.
 static constexpr float WHOLE = 12582912.0f;           // 1.5 * 2^23
 struct KeptScale {
-    float s, inverse, half;                           // inverse 0: everything becomes 0
+    float s, inverse, half;
     bool slow;
     __device__ __forceinline__ explicit KeptScale(uint32_t top)
     {
         const float t = __uint_as_float(top);
-        s = top >= 0x7F800000u ? __uint_as_float(0x7FFFFFFFu) : __fdiv_rd(t, 127.0f);
-        slow = t < 8.67361738e-19f;                   // 2^-60
-        inverse = slow || !(s > 0.0f) ? 0.0f : __frcp_rn(s);
+        // t / 127 towards zero: t times 1 / 127 as fp32 has it (2^-27 off) is one of the two neighbours of t / 127, and the exact sign of
+        // 127 s - t tells which
+        s = t * (1.0f / 127.0f);
+        if (fmaf(s, 127.0f, -t) > 0.0f) s = __uint_as_float(__float_as_uint(s) - 1u);
+        slow = top - 0x21800000u >= 0x5E000000u;      // below 2^-60, or not finite
+        if (slow) s = top >= 0x7F800000u ? __uint_as_float(0x7FFFFFFFu) : __fdiv_rd(t, 127.0f);
+        inverse = tc::rcp_fast(s);
         half = 0.5f * s;
     }
     __device__ __forceinline__ uint32_t slowly(float x) const
@@ -188,14 +192,14 @@ struct KeptScale {
     {
         const float t = fmaf(x, inverse, WHOLE);
         q[0] = __float_as_uint(t);
-        return fabsf(fmaf(WHOLE - t, s, x));
+        return fabsf(fmaf(t - WHOLE, -s, x));
     }
     __device__ __forceinline__ float fast(float2 x, uint32_t (&q)[2]) const
     {
         const float2 t = tc::fma2(x, make_float2(inverse, inverse), make_float2(WHOLE, WHOLE));
         q[0] = __float_as_uint(t.x);
         q[1] = __float_as_uint(t.y);
-        const float2 minus = make_float2(WHOLE - t.x, WHOLE - t.y), left = tc::fma2(minus, make_float2(s, s), x);
+        const float2 left = tc::fma2(tc::add2(t, make_float2(-WHOLE, -WHOLE)), make_float2(-s, -s), x);
         return fmaxf(fabsf(left.x), fabsf(left.y));
     }
     template <typename F, int N, int M>
@@ -210,7 +214,7 @@ struct KeptScale {
 #pragma unroll
             for (int v = 0; v < V; ++v) q[i * V + v] = w[v];
         }
-        if (inverse > 0.0f && most < half) return;
+        if (!slow && most < half) return;
         const float *one = reinterpret_cast<const float *>(x);
 #pragma unroll
         for (int e = 0; e < M; ++e) q[e] = slowly(one[e]);

@@ -32,7 +32,7 @@ static gs_status fill(const gs_layer_norm_config *c, NormArgs *a)
     return GS_OK;
 }
 
-static NormRows rows(const void *p, const int64_t (&stride)[2]) { return {const_cast<void *>(p), stride[0], stride[1]}; }
+static NormRows rows(const void *p, const int64_t (&stride)[2]) { return {const_cast<void *>(p), stride[0], stride[1], 0, 0}; }
 
 // Checks the tensors, the first `outputs` of which are written; tells whether 16-byte accesses fit all of them, and takes
 // the batch for one long sequence where that is the same.
@@ -49,6 +49,7 @@ static gs_status tensors(const gs_layer_norm_config *c, NormArgs *a, NormRows **
     }
     if (one) a->length = a->rows;
     a->by_length = Divider(a->length);
+    a->vectors_wide = (uintptr_t)a->weight % 16 == 0 && (uintptr_t)a->bias % 16 == 0;
     *aligned = wide;
     return GS_OK;
 }

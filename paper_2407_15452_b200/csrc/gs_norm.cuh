@@ -17,6 +17,7 @@ static constexpr int NORM_PARTIALS = 8;               // blocks of a backward la
 struct NormRows {
     void *p;
     int64_t sb, st;                                   // strides in elements: sequence, position
+    int64_t hop, wrap;                                // bytes from a team's row to its next, and more where that is another sequence's
 };
 
 struct NormArgs {
@@ -29,7 +30,7 @@ struct NormArgs {
     int64_t rows, length;
     int64_t step, step_b, step_t;                     // from a team's row to its next: rows, and the same in sequences and positions
     int32_t columns, kept_blocks;                     // kept_blocks = ceil(columns / KEPT_BLOCK)
-    int32_t weight_f32;
+    int32_t weight_f32, vectors_wide;                 // vectors_wide: weight and bias can be read 16 bytes at a time
     float eps;
 };
 
@@ -49,119 +50,166 @@ struct RowAt {
         there = row < a.rows;
         live = there && (!a.lens || t < __ldg(a.lens + b));
     }
-    __device__ __forceinline__ void next(const NormArgs &a)
+    // true if the next row is in another sequence than the steps have it
+    __device__ __forceinline__ bool next(const NormArgs &a)
     {
         row += a.step;
         b += a.step_b;
         t += a.step_t;
-        if (t >= a.length) {
+        const bool wrapped = t >= a.length;
+        if (wrapped) {
             t -= a.length;
             ++b;
         }
         look(a);
+        return wrapped;
     }
-    template <typename T> __device__ __forceinline__ T *of(const NormRows &r) const { return static_cast<T *>(r.p) + b * r.sb + t * r.st; }
+};
+// A team's place in a tensor, at the column of the thread's first piece
+template <typename T>
+struct Line {
+    char *p;
+    __device__ __forceinline__ Line(const NormRows &r, const RowAt &at, int column)
+        : p(reinterpret_cast<char *>(static_cast<T *>(r.p) + at.b * r.sb + at.t * r.st + column))
+    {
+    }
+    __device__ __forceinline__ void next(const NormRows &r, bool wrapped) { p += wrapped ? r.hop + r.wrap : r.hop; }
+    __device__ __forceinline__ T *at() const { return reinterpret_cast<T *>(p); }
 };
 // the steps of a launch whose teams are `step` rows apart
-inline void set_step(NormArgs &a, int64_t step)
+inline void set_step(NormArgs &a, int64_t step, int64_t element)
 {
     a.step = step;
     a.step_b = step / a.length;
     a.step_t = step % a.length;
+    for (NormRows *r : {&a.x, &a.y, &a.dy, &a.dx}) {
+        r->hop = (a.step_b * r->sb + a.step_t * r->st) * element;
+        r->wrap = (r->sb - a.length * r->st) * element;
+    }
 }
 
 // The shape of a team.  LANES 2 to 32: part of a warp; 0: the block, of up to 512 threads.  FAR: the rows' weights (and sums)
-// do not fit the threads' registers: weights are read again for every row, sums live in shared memory.
-template <int VEC_, int NV_, int LANES_, bool FAR_ = false>
+// do not fit the threads' registers: weights are read again for every row, sums live in shared memory.  FULL: every thread's every piece lies in
+// the row.
+template <int VEC_, int NV_, int LANES_, bool FULL_ = false, bool FAR_ = false>
 struct Team {
     static constexpr int VEC = VEC_, NV = NV_, LANES = LANES_;
     static constexpr int V = VEC % 2 == 0 ? 2 : 1, N = VEC / V;       // a piece in fp32: N times V values
-    static constexpr bool FAR = FAR_, BLOCK = LANES_ == 0;
+    static constexpr bool FULL = FULL_, FAR = FAR_, BLOCK = LANES_ == 0;
     static constexpr int GROUP = BLOCK ? 32 : LANES;                  // lanes that reduce by shuffles
     static constexpr int KEPT_LANES = GROUP < KEPT_BLOCK / VEC ? GROUP : KEPT_BLOCK / VEC;   // that hold a scale's columns,
     static constexpr int KEPT_PIECES = KEPT_BLOCK / VEC / KEPT_LANES < NV ? KEPT_BLOCK / VEC / KEPT_LANES : NV;    // and their pieces
     static constexpr int THREADS = BLOCK ? 512 : NORM_THREADS;        // at most
+    static constexpr int RESIDENT = BLOCK && NV * VEC > 8 ? 1 : 2;    // blocks of an SM that the registers have to allow
     static __device__ __forceinline__ int size() { return BLOCK ? blockDim.x : LANES; }
     static __device__ __forceinline__ int member() { return BLOCK ? threadIdx.x : threadIdx.x % LANES; }
     static __device__ __forceinline__ int teams() { return BLOCK ? 1 : NORM_THREADS / LANES; }
     static __device__ __forceinline__ int index() { return BLOCK ? 0 : threadIdx.x / LANES; }
     static __device__ __forceinline__ int column(int v) { return (v * size() + member()) * VEC; }
+    static __device__ __forceinline__ bool in(int v, int columns) { return FULL || column(v) < columns; }
+    // from a thread's first piece to its others, in elements
+    static __device__ __forceinline__ int apart(int v) { return v * size() * VEC; }
 };
 
-// Sums over a team, one or two at a time.  The warps of a block leave theirs in one of two places in turn, so that one barrier a sum is enough:
+// Sums over the lanes of a team that lie in one warp
+template <typename S>
+__device__ __forceinline__ float group_sum(float v)
+{
+#pragma unroll
+    for (int o = S::GROUP / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+template <typename S>
+__device__ __forceinline__ float2 group_sum(float2 v)
+{
+#pragma unroll
+    for (int o = S::GROUP / 2; o; o >>= 1)
+        v = add_of(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+    return v;
+}
+// Sums over a team, two at a time.  The warps of a block leave theirs in one of two places in turn, so that one barrier a sum is enough:
 // a place is written again two sums later, when every thread has met the barrier in between.
 struct TeamSums {
     float2 (*place)[16];
     int turn;
 };
 template <typename S>
-__device__ __forceinline__ float team_sum(float v, TeamSums &sums)
-{
-#pragma unroll
-    for (int o = S::GROUP / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (!S::BLOCK) return v;
-    float *place = reinterpret_cast<float *>(sums.place[sums.turn]);
-    sums.turn ^= 1;
-    if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = place[0];
-    for (int w = 1; w < (int)blockDim.x >> 5; ++w) v += place[w];
-    return v;
-}
-template <typename S>
 __device__ __forceinline__ float2 team_sum(float2 v, TeamSums &sums)
 {
-#pragma unroll
-    for (int o = S::GROUP / 2; o; o >>= 1)
-        v = add_of(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+    v = group_sum<S>(v);
     if (!S::BLOCK) return v;
     float2 *place = sums.place[sums.turn];
     sums.turn ^= 1;
     if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = place[0];
-    for (int w = 1; w < (int)blockDim.x >> 5; ++w) v = add_of(v, place[w]);
-    return v;
+    const int lane = threadIdx.x & 31;
+    v = lane < (int)blockDim.x >> 5 ? place[lane] : make_float2(0.0f, 0.0f);         // at most 16 warps
+#pragma unroll
+    for (int o = 8; o; o >>= 1)
+        v = add_of(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+    return make_float2(__shfl_sync(0xffffffffu, v.x, 0), __shfl_sync(0xffffffffu, v.y, 0));
 }
 
-// the columns [c, c + VEC) of a row; all of them lie in the row or none (VEC > 1 only where columns % VEC == 0)
+// a piece of a row, all of which lies in the row or nothing (VEC > 1 only where columns % VEC == 0)
 template <typename T, int VEC>
-__device__ __forceinline__ typename Piece<T, VEC>::raw load_piece(const T *row, int c, int columns, bool live)
+__device__ __forceinline__ typename Piece<T, VEC>::raw load_piece(const T *at, bool on)
 {
-    if (live && c < columns) return *reinterpret_cast<const typename Piece<T, VEC>::raw *>(row + c);
+    if (on) return *reinterpret_cast<const typename Piece<T, VEC>::raw *>(at);
     return Piece<T, VEC>::none();
 }
 // the same of a weight or bias, `without` where there is none
 template <typename T, int VEC, typename F, int N>
-__device__ __forceinline__ void vector_piece(const void *p, int32_t f32, int c, int columns, float without, F (&f)[N])
+__device__ __forceinline__ void vector_piece(const NormArgs &a, const void *p, int c, bool on, float without, F (&f)[N])
 {
     float *one = reinterpret_cast<float *>(f);
+    if (!p || !on) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e)
-        one[e] = !p || c >= columns ? without : f32 ? static_cast<const float *>(p)[c + e] : to_float(static_cast<const T *>(p)[c + e]);
+        for (int e = 0; e < VEC; ++e) one[e] = without;
+    } else if (VEC > 1 && a.vectors_wide) {
+        if (!a.weight_f32) {
+            if constexpr (VEC == 8) Piece<T, VEC>::get(*reinterpret_cast<const typename Piece<T, VEC>::raw *>(static_cast<const T *>(p) + c), f);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; e += 4) {
+                const float4 q = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + c + e);
+                one[e] = q.x;
+                if constexpr (VEC > 1) one[e + 1] = q.y, one[e + 2] = q.z, one[e + 3] = q.w;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) one[e] = a.weight_f32 ? static_cast<const float *>(p)[c + e] : to_float(static_cast<const T *>(p)[c + e]);
+    }
 }
 
 // Calls launch(Team, threads) with the team for rows of `columns` values: 16 columns a thread, as few threads as that takes up to a warp (fewer steps
-// to a sum: 128 columns of 16 bits by 8 threads XX, by 16 threads XX us), a block beyond; 32 a thread beyond 8192.
+// to a sum), a block beyond, with 8 columns a thread up to 4096 and 32 beyond 8192.
+template <int VEC, int PER_THREAD, int LANES, typename F>
+static gs_status full_or_not(int columns, int threads, F &&launch)
+{
+    if (columns == PER_THREAD * (LANES ? LANES : threads)) return launch(Team<VEC, PER_THREAD / VEC, LANES, true>(), threads);
+    return launch(Team<VEC, PER_THREAD / VEC, LANES, false>(), threads);
+}
 template <typename T, typename F>
 static gs_status with_team(int columns, bool aligned, F &&launch)
 {
     constexpr int W = Wide<T>::N;
     auto block = [&](int per_thread) { return (columns + 32 * per_thread - 1) / (32 * per_thread) * 32; };
     if (aligned) {
-        if (columns <= 32) return launch(Team<W, 16 / W, 2>(), NORM_THREADS);
-        if (columns <= 64) return launch(Team<W, 16 / W, 4>(), NORM_THREADS);
-        if (columns <= 128) return launch(Team<W, 16 / W, 8>(), NORM_THREADS);
-        if (columns <= 256) return launch(Team<W, 16 / W, 16>(), NORM_THREADS);
-        if (columns <= 512) return launch(Team<W, 16 / W, 32>(), NORM_THREADS);
-        if (columns <= 8192) return launch(Team<W, 16 / W, 0>(), block(16));
-        return launch(Team<W, 32 / W, 0, true>(), block(32));
+        if (columns <= 32) return full_or_not<W, 16, 2>(columns, NORM_THREADS, launch);
+        if (columns <= 64) return full_or_not<W, 16, 4>(columns, NORM_THREADS, launch);
+        if (columns <= 128) return full_or_not<W, 16, 8>(columns, NORM_THREADS, launch);
+        if (columns <= 256) return full_or_not<W, 16, 16>(columns, NORM_THREADS, launch);
+        if (columns <= 512) return full_or_not<W, 16, 32>(columns, NORM_THREADS, launch);
+        if (columns <= 4096) return full_or_not<W, 8, 0>(columns, block(8), launch);
+        if (columns <= 8192) return full_or_not<W, 16, 0>(columns, block(16), launch);
+        return launch(Team<W, 32 / W, 0, false, true>(), block(32));
     }
     if (columns <= 32) return launch(Team<1, 1, 32>(), NORM_THREADS);
     if (columns <= 128) return launch(Team<1, 4, 32>(), NORM_THREADS);
     if (columns <= 512) return launch(Team<1, 16, 32>(), NORM_THREADS);
     if (columns <= 8192) return launch(Team<1, 16, 0>(), block(16));
-    return launch(Team<1, 32, 0, true>(), block(32));
+    return launch(Team<1, 32, 0, false, true>(), block(32));
 }
 
 // gs_norm_forward.cu, gs_norm_backward.cu

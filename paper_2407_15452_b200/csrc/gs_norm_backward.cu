@@ -11,18 +11,14 @@ namespace gs {
 // x of a row as it travels: T, or 8 bits and their scale
 template <typename T, int VEC, bool KEPT> struct Source {
     typename Piece<T, VEC>::raw r;
-    __device__ __forceinline__ void load(const NormArgs &a, const RowAt &at, const T *row, int c)
-    {
-        r = load_piece<T, VEC>(row, c, a.columns, at.live);
-    }
+    __device__ __forceinline__ void load(const NormArgs &, const RowAt &, const T *at, int, bool on) { r = load_piece<T, VEC>(at, on); }
     template <typename F, int N> __device__ __forceinline__ void get(F (&f)[N]) const { Piece<T, VEC>::get(r, f); }
 };
 template <typename T, int VEC> struct Source<T, VEC, true> {
     typename Kept<VEC>::raw r;
     float scale;
-    __device__ __forceinline__ void load(const NormArgs &a, const RowAt &at, const T *, int c)
+    __device__ __forceinline__ void load(const NormArgs &a, const RowAt &at, const T *, int c, bool on)
     {
-        const bool on = at.live && c < a.columns;
         r = on ? *reinterpret_cast<const typename Kept<VEC>::raw *>(a.packed + at.row * a.columns + c) : Kept<VEC>::none();
         scale = on ? a.scales[at.row * a.kept_blocks + c / KEPT_BLOCK] : 0.0f;
     }
@@ -30,7 +26,7 @@ template <typename T, int VEC> struct Source<T, VEC, true> {
 };
 
 template <typename T, typename S, bool KEPT>
-__global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_backward_kernel(const __grid_constant__ NormArgs a)
+__global__ void __launch_bounds__(S::THREADS, S::RESIDENT) norm_backward_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr int VEC = S::VEC, NV = S::NV, N = S::N, V = S::V;
     typedef Piece<T, VEC> P;
@@ -45,7 +41,7 @@ __global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_backward_ke
     F *const far_dw = reinterpret_cast<F *>(shared_sums) + threadIdx.x, *const far_db = far_dw + (S::FAR ? NV * N * blockDim.x : 0);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        if (!S::FAR) vector_piece<T, VEC>(a.weight, a.weight_f32, S::column(v), a.columns, 1.0f, w[S::FAR ? 0 : v]);
+        if (!S::FAR) vector_piece<T, VEC>(a, a.weight, S::column(v), S::in(v, a.columns), 1.0f, w[S::FAR ? 0 : v]);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             if (S::FAR) far_dw[(v * N + e) * blockDim.x] = far_db[(v * N + e) * blockDim.x] = all_of<V>(0.0f);
@@ -58,13 +54,14 @@ __global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_backward_ke
     typename P::raw rdy[NV];
     Source<T, VEC, KEPT> rx[NV];
     float2 stats;
+    Line<T> x(a.x, next, S::column(0)), dy(a.dy, next, S::column(0)), dx(a.dx, next, S::column(0));
     auto load = [&]() {
-        const T *row_x = next.of<const T>(a.x), *row_dy = next.of<const T>(a.dy);
         stats = next.live ? reinterpret_cast<const float2 *>(a.stats)[next.row] : make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            rx[v].load(a, next, row_x, S::column(v));
-            rdy[v] = load_piece<T, VEC>(row_dy, S::column(v), a.columns, next.live);
+            const bool on = next.live && S::in(v, a.columns);
+            rx[v].load(a, next, x.at() + S::apart(v), S::column(v), on);
+            rdy[v] = load_piece<T, VEC>(dy.at() + S::apart(v), on);
         }
     };
     load();
@@ -77,9 +74,9 @@ __global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_backward_ke
         for (int v = 0; v < NV; ++v) {
             rx[v].get(xh[v]);
             P::get(rdy[v], g[v]);
-            if (S::column(v) < a.columns) {
+            if (S::in(v, a.columns)) {
                 F wv[N];
-                if (S::FAR) vector_piece<T, VEC>(a.weight, a.weight_f32, S::column(v), a.columns, 1.0f, wv);
+                if (S::FAR) vector_piece<T, VEC>(a, a.weight, S::column(v), true, 1.0f, wv);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const F h = mul_of(add_of(xh[v][e], minus_mean), by), d = g[v][e];
@@ -94,23 +91,24 @@ __global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_backward_ke
                 }
             }
         }
-        next.next(a);
+        const bool wrapped = next.next(a);
+        if (!KEPT) x.next(a.x, wrapped);
+        dy.next(a.dy, wrapped);
         load();
         const float2 s = team_sum<S>(make_float2(sum_of(s1), sum_of(s2)), sums);
         if (at.there) {
-            T *to = at.of<T>(a.dx);
             const F less = all_of<V>(-s.x * inverse), along = all_of<V>(-s.y * inverse);
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int c = S::column(v);
-                if (c < a.columns) {
+                if (S::in(v, a.columns)) {
                     F o[N];
 #pragma unroll
                     for (int e = 0; e < N; ++e) o[e] = mul_of(by, fma_of(xh[v][e], along, add_of(g[v][e], less)));
-                    *reinterpret_cast<typename P::raw *>(to + c) = at.live ? P::put(o) : P::none();
+                    *reinterpret_cast<typename P::raw *>(dx.at() + S::apart(v)) = at.live ? P::put(o) : P::none();
                 }
             }
         }
+        dx.next(a.dx, wrapped);
     }
     if (!a.partial) return;
     // [block][2][columns]
@@ -181,7 +179,7 @@ static gs_status launch(const NormArgs &args, int threads, int32_t weight_type, 
     if (per_sm > NORM_PARTIALS) per_sm = NORM_PARTIALS;
     const int64_t blocks = (a.rows + teams - 1) / teams, most = (int64_t)sm_count() * per_sm;
     const int grid = (int)(blocks < most ? blocks : most);
-    set_step(a, (int64_t)grid * teams);
+    set_step(a, (int64_t)grid * teams, sizeof(T));
     const bool sums = dweight || dbias;
     if (!sums) a.partial = nullptr;
     const size_t shared = (S::FAR ? (size_t)S::NV * S::VEC * threads : S::BLOCK ? 0 : (size_t)NORM_THREADS * S::NV * S::VEC) * sizeof(float2);

@@ -1,7 +1,8 @@
 // Layer norm, forward: y = (x - mean) rstd weight + bias, and on request x in 8 bits beside it.
 //
 // The mean is taken first and the squares of what differs from it second, both from registers; the differences' own mean, what rounding left
-// of the first, is taken with them, so that a mean far from zero costs no digits.  Bound: memory traffic, one read and one write of
+// of the first, is taken with them, so that a mean far from zero costs no digits.  A block's warps do so each for its own columns and
+// then join: the squares about their means, and the squares of the means about the row's.  Bound: memory traffic, one read and one write of
 // every value.
 #include "gs_norm.cuh"
 
@@ -9,28 +10,35 @@ namespace gs {
 
 // KEEP: x is kept in 8 bits as well
 template <typename T, typename S, bool KEEP>
-__global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_forward_kernel(const __grid_constant__ NormArgs a)
+__global__ void __launch_bounds__(S::THREADS, S::RESIDENT) norm_forward_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr int VEC = S::VEC, NV = S::NV, N = S::N, V = S::V;
     typedef Piece<T, VEC> P;
     typedef typename Vec<V>::type F;
-    __shared__ float2 places[2][16];
-    TeamSums sums = {places, 0};
+    __shared__ float4 places[2][16];                               // of a block's warps, in turn: mean, what it lacks, squares, columns
+    int turn = 0;
     const float inverse = 1.0f / (float)a.columns;
+    // columns of the lanes that reduce by shuffles, and 1 / that
+    float in_group = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) in_group += S::in(v, a.columns) ? (float)VEC : 0.0f;
+    in_group = group_sum<S>(in_group);
+    const float of_group = in_group > 0.0f ? 1.0f / in_group : 0.0f;
 
     F w[S::FAR ? 1 : NV][N], b[S::FAR ? 1 : NV][N];
     if (!S::FAR)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            vector_piece<T, VEC>(a.weight, a.weight_f32, S::column(v), a.columns, 1.0f, w[v]);
-            vector_piece<T, VEC>(a.bias, a.weight_f32, S::column(v), a.columns, 0.0f, b[v]);
+            vector_piece<T, VEC>(a, a.weight, S::column(v), S::in(v, a.columns), 1.0f, w[v]);
+            vector_piece<T, VEC>(a, a.bias, S::column(v), S::in(v, a.columns), 0.0f, b[v]);
         }
 
     int64_t base = (int64_t)blockIdx.x * S::teams();
     RowAt next(a, base + S::index());
+    Line<T> x(a.x, next, S::column(0)), y(a.y, next, S::column(0));
     typename P::raw raw[NV];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) raw[v] = load_piece<T, VEC>(next.of<const T>(a.x), S::column(v), a.columns, next.live);
+    for (int v = 0; v < NV; ++v) raw[v] = load_piece<T, VEC>(x.at() + S::apart(v), next.live && S::in(v, a.columns));
     for (; base < a.rows; base += a.step) {
         const RowAt at = next;
         F f[NV][N], s = all_of<V>(0.0f);
@@ -40,10 +48,10 @@ __global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_forward_ker
 #pragma unroll
             for (int e = 0; e < N; ++e) s = add_of(s, f[v][e]);
         }
-        next.next(a);
-        const T *row = next.of<const T>(a.x);
+        const bool wrapped = next.next(a);
+        x.next(a.x, wrapped);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) raw[v] = load_piece<T, VEC>(row, S::column(v), a.columns, next.live);
+        for (int v = 0; v < NV; ++v) raw[v] = load_piece<T, VEC>(x.at() + S::apart(v), next.live && S::in(v, a.columns));
 
         if constexpr (KEEP) {
 #pragma unroll
@@ -59,7 +67,7 @@ __global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_forward_ker
                     uint32_t q[VEC];
                     scale.of(f[v], q);
                     const int c = S::column(v);
-                    if (at.there && c < a.columns) {
+                    if (at.there && S::in(v, a.columns)) {
                         *reinterpret_cast<typename Kept<VEC>::raw *>(a.packed + at.row * a.columns + c) = Kept<VEC>::put(q);
                         if (c % KEPT_BLOCK == 0) a.scales[at.row * a.kept_blocks + c / KEPT_BLOCK] = scale.s;
                     }
@@ -67,66 +75,174 @@ __global__ void __launch_bounds__(S::THREADS, S::BLOCK ? 1 : 2) norm_forward_ker
             }
         }
 
-        const float mean = team_sum<S>(sum_of(s), sums) * inverse;
+        // a warp's own mean and squares about it, then the warps' together
+        const float mean = group_sum<S>(sum_of(s)) * of_group;
         F rest = all_of<V>(0.0f), squares = all_of<V>(0.0f);
         const F minus_mean = all_of<V>(-mean);
 #pragma unroll
         for (int v = 0; v < NV; ++v)
-            if (S::column(v) < a.columns)
+            if (S::in(v, a.columns))
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     f[v][e] = add_of(f[v][e], minus_mean);
                     rest = add_of(rest, f[v][e]);
                     squares = fma_of(f[v][e], f[v][e], squares);
                 }
-        float2 t = team_sum<S>(make_float2(sum_of(rest), sum_of(squares)), sums);
-        t.x *= inverse;
-        const float rstd = rsqrtf(fmaxf(fmaf(-t.x, t.x, t.y * inverse), 0.0f) + a.eps);
+        float2 t = group_sum<S>(make_float2(sum_of(rest), sum_of(squares)));
+        t.x *= of_group;                                             // the mean's own rounding
+        float less = t.x, m2 = t.y - in_group * t.x * t.x, whole = mean + t.x;
+        if (S::BLOCK) {
+            // means as what they differ by from the first warp's, which keeps their digits
+            float4 *place = places[turn];
+            turn ^= 1;
+            if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = make_float4(mean, t.x, m2, in_group);
+            __syncthreads();
+            const int other = threadIdx.x & 31;                      // at most 16 warps
+            const float first = place[0].x;
+            const float4 its = other < (int)blockDim.x >> 5 ? place[other] : make_float4(first, 0.0f, 0.0f, 0.0f);
+            float off = (its.x - first + its.y) * its.w;
+#pragma unroll
+            for (int o = 8; o; o >>= 1) off += __shfl_xor_sync(0xffffffffu, off, o);
+            off = __shfl_sync(0xffffffffu, off, 0) * inverse;
+            const float d = its.x - first + its.y - off;
+            m2 = fmaf(d * d, its.w, its.z);
+#pragma unroll
+            for (int o = 8; o; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+            m2 = __shfl_sync(0xffffffffu, m2, 0);
+            less = first - mean + off;
+            whole = first + off;
+        }
+        const float rstd = rsqrtf(fmaxf(m2 * inverse, 0.0f) + a.eps);
         if (at.there) {
-            T *to = at.of<T>(a.y);
-            const F by = all_of<V>(rstd), less = all_of<V>(-t.x);
+            const F by = all_of<V>(rstd), minus_less = all_of<V>(-less);
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int c = S::column(v);
-                if (c < a.columns) {
+                if (S::in(v, a.columns)) {
                     F wv[N], bv[N], o[N];
                     if (S::FAR) {
-                        vector_piece<T, VEC>(a.weight, a.weight_f32, c, a.columns, 1.0f, wv);
-                        vector_piece<T, VEC>(a.bias, a.weight_f32, c, a.columns, 0.0f, bv);
+                        vector_piece<T, VEC>(a, a.weight, S::column(v), true, 1.0f, wv);
+                        vector_piece<T, VEC>(a, a.bias, S::column(v), true, 0.0f, bv);
                     }
 #pragma unroll
                     for (int e = 0; e < N; ++e)
-                        o[e] = fma_of(mul_of(add_of(f[v][e], less), by), S::FAR ? wv[e] : w[S::FAR ? 0 : v][e],
+                        o[e] = fma_of(mul_of(add_of(f[v][e], minus_less), by), S::FAR ? wv[e] : w[S::FAR ? 0 : v][e],
                                       S::FAR ? bv[e] : b[S::FAR ? 0 : v][e]);
-                    *reinterpret_cast<typename P::raw *>(to + c) = at.live ? P::put(o) : P::none();
+                    *reinterpret_cast<typename P::raw *>(y.at() + S::apart(v)) = at.live ? P::put(o) : P::none();
                 }
             }
             if (a.stats && S::member() == 0)
-                reinterpret_cast<float2 *>(a.stats)[at.row] = at.live ? make_float2(mean + t.x, rstd) : make_float2(0.0f, 0.0f);
+                reinterpret_cast<float2 *>(a.stats)[at.row] = at.live ? make_float2(whole, rstd) : make_float2(0.0f, 0.0f);
         }
+        y.next(a.y, wrapped);
     }
+}
+
+// The values that `raw` stands for are not to be kept from one pass to the next: twice the registers
+__device__ __forceinline__ void taken_apart_again(uint4 &raw) { asm volatile("" : "+r"(raw.x), "+r"(raw.y), "+r"(raw.z), "+r"(raw.w)); }
+
+// Rows of 16 bits from 512 columns on, a warp each: the row stays in registers as it came, its values are taken apart once for each of
+// the three passes, weights come from the caches every time, and nothing waits at a barrier.
+template <typename T, int NV, bool KEEP>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_forward_rows_kernel(const __grid_constant__ NormArgs a)
+{
+    constexpr int VEC = 8, N = 4;
+    typedef Piece<T, VEC> P;
+    typedef Team<VEC, NV, 32> S;
+    const float inverse = 1.0f / (float)a.columns;
+    RowAt at(a, (int64_t)blockIdx.x * S::teams() + S::index());
+    Line<T> x(a.x, at, S::column(0)), y(a.y, at, S::column(0));
+    while (at.there) {
+        typename P::raw raw[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) raw[v] = load_piece<T, VEC>(x.at() + S::apart(v), at.live && S::in(v, a.columns));
+        float2 s = make_float2(0.0f, 0.0f), f[N];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            P::get(raw[v], f);
+#pragma unroll
+            for (int e = 0; e < N; ++e) s = add_of(s, f[e]);
+            if constexpr (KEEP) {
+                uint32_t top = 0, q[VEC];
+#pragma unroll
+                for (int e = 0; e < N; ++e) top = max(top, magnitude(f[e]));
+                const KeptScale scale(largest<KEPT_BLOCK / VEC>(top));
+                scale.of(f, q);
+                const int c = S::column(v);
+                if (c < a.columns) {
+                    *reinterpret_cast<uint2 *>(a.packed + at.row * a.columns + c) = Kept<VEC>::put(q);
+                    if (c % KEPT_BLOCK == 0) a.scales[at.row * a.kept_blocks + c / KEPT_BLOCK] = scale.s;
+                }
+            }
+        }
+        const float mean = group_sum<S>(sum_of(s)) * inverse;
+        const float2 minus_mean = make_float2(-mean, -mean);
+        float2 rest = make_float2(0.0f, 0.0f), squares = rest;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (S::in(v, a.columns)) {
+                taken_apart_again(raw[v]);
+                P::get(raw[v], f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float2 d = add_of(f[e], minus_mean);
+                    rest = add_of(rest, d);
+                    squares = fma_of(d, d, squares);
+                }
+            }
+        const float2 t = group_sum<S>(make_float2(sum_of(rest), sum_of(squares)));
+        const float less = t.x * inverse, rstd = rsqrtf(fmaxf(fmaf(-less, less, t.y * inverse), 0.0f) + a.eps);
+        const float2 by = make_float2(rstd, rstd), minus_less = make_float2(-less, -less);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (S::in(v, a.columns)) {
+                float2 w[N], b[N];
+                vector_piece<T, VEC>(a, a.weight, S::column(v), true, 1.0f, w);
+                vector_piece<T, VEC>(a, a.bias, S::column(v), true, 0.0f, b);
+                taken_apart_again(raw[v]);
+                P::get(raw[v], f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[e] = fma_of(mul_of(add_of(add_of(f[e], minus_mean), minus_less), by), w[e], b[e]);
+                *reinterpret_cast<typename P::raw *>(y.at() + S::apart(v)) = at.live ? P::put(f) : P::none();
+            }
+        if (a.stats && S::member() == 0)
+            reinterpret_cast<float2 *>(a.stats)[at.row] = at.live ? make_float2(mean + less, rstd) : make_float2(0.0f, 0.0f);
+        const bool wrapped = at.next(a);
+        x.next(a.x, wrapped);
+        y.next(a.y, wrapped);
+    }
+}
+
+template <typename K>
+static gs_status launch(K kernel, const NormArgs &args, int threads, int teams, int64_t most, int64_t element, cudaStream_t st)
+{
+    NormArgs a = args;
+    const int64_t blocks = (a.rows + teams - 1) / teams, grid = blocks < most ? blocks : most;
+    set_step(a, grid * teams, element);
+    kernel<<<(unsigned)grid, threads, 0, st>>>(a);
+    GS_CUDA_TRY(cudaGetLastError());
+    return GS_OK;
 }
 
 gs_status norm_forward(const NormArgs &a, int32_t dtype, bool aligned, cudaStream_t st)
 {
     return with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
+        const int64_t once = (int64_t)sm_count() * 2;                // blocks, which load their weights once
+        if constexpr (sizeof(T) == 2)
+            if (aligned && a.columns > 512 && a.columns <= 4096) {
+                const int teams = NORM_THREADS / 32;
+                if (a.columns <= 1024)
+                    return launch(a.packed ? norm_forward_rows_kernel<T, 4, true> : norm_forward_rows_kernel<T, 4, false>, a, NORM_THREADS, teams, 8 * once, 2, st);
+                if (a.columns <= 2048)
+                    return launch(a.packed ? norm_forward_rows_kernel<T, 8, true> : norm_forward_rows_kernel<T, 8, false>, a, NORM_THREADS, teams, 8 * once, 2, st);
+                return launch(a.packed ? norm_forward_rows_kernel<T, 16, true> : norm_forward_rows_kernel<T, 16, false>, a, NORM_THREADS, teams, 8 * once, 2, st);
+            }
         return with_team<T>(a.columns, aligned, [&](auto team, int threads) {
             typedef decltype(team) S;
-            const int teams = S::BLOCK ? 1 : NORM_THREADS / S::LANES;
-            const int64_t blocks = (a.rows + teams - 1) / teams, most = (int64_t)sm_count() * (2048 / threads) * 2;
-            const int64_t grid = blocks < most ? blocks : most;
-            NormArgs b = a;
-            set_step(b, grid * teams);
+            auto kernel = norm_forward_kernel<T, S, false>;
             if constexpr (S::VEC > 1)
-                if (a.packed) {
-                    norm_forward_kernel<T, S, true><<<(unsigned)grid, threads, 0, st>>>(b);
-                    GS_CUDA_TRY(cudaGetLastError());
-                    return GS_OK;
-                }
-            norm_forward_kernel<T, S, false><<<(unsigned)grid, threads, 0, st>>>(b);
-            GS_CUDA_TRY(cudaGetLastError());
-            return GS_OK;
+                if (a.packed) kernel = norm_forward_kernel<T, S, true>;
+            return launch(kernel, a, threads, S::BLOCK ? 1 : NORM_THREADS / S::LANES, once * (S::BLOCK ? 512 / threads > 0 ? 512 / threads : 1 : 1) , sizeof(T), st);
         });
     });
 }
