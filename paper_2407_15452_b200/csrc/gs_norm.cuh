@@ -88,20 +88,21 @@ inline void set_step(NormArgs &a, int64_t step, int64_t element)
     }
 }
 
-// The shape of a team.  LANES 2 to 32: part of a warp; 0: the block, of up to 512 threads.  FAR: the rows' weights (and sums)
+// The shape of a team.  LANES 2 to 32: part of a warp; more: the block; 0: the block, of up to 512 threads.  FAR: the rows' weights (and sums)
 // do not fit the threads' registers: weights are read again for every row, sums live in shared memory.  FULL: every thread's every piece lies in
 // the row.
 template <int VEC_, int NV_, int LANES_, bool FULL_ = false, bool FAR_ = false>
 struct Team {
     static constexpr int VEC = VEC_, NV = NV_, LANES = LANES_;
     static constexpr int V = VEC % 2 == 0 ? 2 : 1, N = VEC / V;       // a piece in fp32: N times V values
-    static constexpr bool FULL = FULL_, FAR = FAR_, BLOCK = LANES_ == 0;
+    static constexpr bool FULL = FULL_, FAR = FAR_, BLOCK = LANES_ == 0 || LANES_ > 32;
     static constexpr int GROUP = BLOCK ? 32 : LANES;                  // lanes that reduce by shuffles
     static constexpr int KEPT_LANES = GROUP < KEPT_BLOCK / VEC ? GROUP : KEPT_BLOCK / VEC;   // that hold a scale's columns,
     static constexpr int KEPT_PIECES = KEPT_BLOCK / VEC / KEPT_LANES < NV ? KEPT_BLOCK / VEC / KEPT_LANES : NV;    // and their pieces
-    static constexpr int THREADS = BLOCK ? 512 : NORM_THREADS;        // at most
-    static constexpr int RESIDENT = BLOCK && NV * VEC > 8 ? 1 : 2;    // blocks of an SM that the registers have to allow
-    static __device__ __forceinline__ int size() { return BLOCK ? blockDim.x : LANES; }
+    static constexpr int THREADS = !BLOCK ? NORM_THREADS : LANES ? LANES : 512;       // at most
+    // threads of an SM that the registers have to allow, and blocks of these
+    static constexpr int ON_SM = BLOCK && NV * VEC <= 8 ? 1024 : 512, RESIDENT = ON_SM / THREADS;
+    static __device__ __forceinline__ int size() { return LANES ? LANES : blockDim.x; }
     static __device__ __forceinline__ int member() { return BLOCK ? threadIdx.x : threadIdx.x % LANES; }
     static __device__ __forceinline__ int teams() { return BLOCK ? 1 : NORM_THREADS / LANES; }
     static __device__ __forceinline__ int index() { return BLOCK ? 0 : threadIdx.x / LANES; }
@@ -205,11 +206,16 @@ static gs_status with_team(int columns, bool aligned, F &&launch)
         if (columns <= 8192) return full_or_not<W, 16, 0>(columns, block(16), launch);
         return launch(Team<W, 32 / W, 0, false, true>(), block(32));
     }
-    if (columns <= 32) return launch(Team<1, 1, 32>(), NORM_THREADS);
-    if (columns <= 128) return launch(Team<1, 4, 32>(), NORM_THREADS);
+    if (columns <= 32) return launch(Team<1, 2, 16>(), NORM_THREADS);
+    if (columns <= 64) return launch(Team<1, 4, 16>(), NORM_THREADS);
+    if (columns <= 128) return launch(Team<1, 8, 16>(), NORM_THREADS);
+    if (columns <= 256) return launch(Team<1, 8, 32>(), NORM_THREADS);
     if (columns <= 512) return launch(Team<1, 16, 32>(), NORM_THREADS);
-    if (columns <= 8192) return launch(Team<1, 16, 0>(), block(16));
-    return launch(Team<1, 32, 0, false, true>(), block(32));
+    if (columns <= 1024) return launch(Team<1, 16, 64>(), 64);
+    if (columns <= 2048) return launch(Team<1, 16, 128>(), 128);
+    if (columns <= 4096) return launch(Team<1, 16, 256>(), 256);
+    if (columns <= 8192) return launch(Team<1, 16, 512>(), 512);
+    return launch(Team<1, 32, 512, false, true>(), 512);
 }
 
 // gs_norm_forward.cu, gs_norm_backward.cu

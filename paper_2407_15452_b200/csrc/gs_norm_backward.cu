@@ -174,8 +174,7 @@ static gs_status launch(const NormArgs &args, int threads, int32_t weight_type, 
 {
     NormArgs a = args;
     const int teams = S::BLOCK ? 1 : NORM_THREADS / S::LANES;
-    int per_sm = 1024 / threads;
-    if (per_sm < 1) per_sm = 1;
+    int per_sm = S::ON_SM / threads;
     if (per_sm > NORM_PARTIALS) per_sm = NORM_PARTIALS;
     const int64_t blocks = (a.rows + teams - 1) / teams, most = (int64_t)sm_count() * per_sm;
     const int grid = (int)(blocks < most ? blocks : most);

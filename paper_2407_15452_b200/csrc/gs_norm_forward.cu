@@ -137,81 +137,6 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) norm_forward_kernel(c
     }
 }
 
-// The values that `raw` stands for are not to be kept from one pass to the next: twice the registers
-__device__ __forceinline__ void taken_apart_again(uint4 &raw) { asm volatile("" : "+r"(raw.x), "+r"(raw.y), "+r"(raw.z), "+r"(raw.w)); }
-
-// Rows of 16 bits from 512 columns on, a warp each: the row stays in registers as it came, its values are taken apart once for each of
-// the three passes, weights come from the caches every time, and nothing waits at a barrier.
-template <typename T, int NV, bool KEEP>
-__global__ void __launch_bounds__(NORM_THREADS, 2) norm_forward_rows_kernel(const __grid_constant__ NormArgs a)
-{
-    constexpr int VEC = 8, N = 4;
-    typedef Piece<T, VEC> P;
-    typedef Team<VEC, NV, 32> S;
-    const float inverse = 1.0f / (float)a.columns;
-    RowAt at(a, (int64_t)blockIdx.x * S::teams() + S::index());
-    Line<T> x(a.x, at, S::column(0)), y(a.y, at, S::column(0));
-    while (at.there) {
-        typename P::raw raw[NV];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) raw[v] = load_piece<T, VEC>(x.at() + S::apart(v), at.live && S::in(v, a.columns));
-        float2 s = make_float2(0.0f, 0.0f), f[N];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            P::get(raw[v], f);
-#pragma unroll
-            for (int e = 0; e < N; ++e) s = add_of(s, f[e]);
-            if constexpr (KEEP) {
-                uint32_t top = 0, q[VEC];
-#pragma unroll
-                for (int e = 0; e < N; ++e) top = max(top, magnitude(f[e]));
-                const KeptScale scale(largest<KEPT_BLOCK / VEC>(top));
-                scale.of(f, q);
-                const int c = S::column(v);
-                if (c < a.columns) {
-                    *reinterpret_cast<uint2 *>(a.packed + at.row * a.columns + c) = Kept<VEC>::put(q);
-                    if (c % KEPT_BLOCK == 0) a.scales[at.row * a.kept_blocks + c / KEPT_BLOCK] = scale.s;
-                }
-            }
-        }
-        const float mean = group_sum<S>(sum_of(s)) * inverse;
-        const float2 minus_mean = make_float2(-mean, -mean);
-        float2 rest = make_float2(0.0f, 0.0f), squares = rest;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-            if (S::in(v, a.columns)) {
-                taken_apart_again(raw[v]);
-                P::get(raw[v], f);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float2 d = add_of(f[e], minus_mean);
-                    rest = add_of(rest, d);
-                    squares = fma_of(d, d, squares);
-                }
-            }
-        const float2 t = group_sum<S>(make_float2(sum_of(rest), sum_of(squares)));
-        const float less = t.x * inverse, rstd = rsqrtf(fmaxf(fmaf(-less, less, t.y * inverse), 0.0f) + a.eps);
-        const float2 by = make_float2(rstd, rstd), minus_less = make_float2(-less, -less);
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-            if (S::in(v, a.columns)) {
-                float2 w[N], b[N];
-                vector_piece<T, VEC>(a, a.weight, S::column(v), true, 1.0f, w);
-                vector_piece<T, VEC>(a, a.bias, S::column(v), true, 0.0f, b);
-                taken_apart_again(raw[v]);
-                P::get(raw[v], f);
-#pragma unroll
-                for (int e = 0; e < N; ++e) f[e] = fma_of(mul_of(add_of(add_of(f[e], minus_mean), minus_less), by), w[e], b[e]);
-                *reinterpret_cast<typename P::raw *>(y.at() + S::apart(v)) = at.live ? P::put(f) : P::none();
-            }
-        if (a.stats && S::member() == 0)
-            reinterpret_cast<float2 *>(a.stats)[at.row] = at.live ? make_float2(mean + less, rstd) : make_float2(0.0f, 0.0f);
-        const bool wrapped = at.next(a);
-        x.next(a.x, wrapped);
-        y.next(a.y, wrapped);
-    }
-}
-
 template <typename K>
 static gs_status launch(K kernel, const NormArgs &args, int threads, int teams, int64_t most, int64_t element, cudaStream_t st)
 {
@@ -227,22 +152,12 @@ gs_status norm_forward(const NormArgs &a, int32_t dtype, bool aligned, cudaStrea
 {
     return with_type(dtype, [&](auto t) {
         typedef decltype(t) T;
-        const int64_t once = (int64_t)sm_count() * 2;                // blocks, which load their weights once
-        if constexpr (sizeof(T) == 2)
-            if (aligned && a.columns > 512 && a.columns <= 4096) {
-                const int teams = NORM_THREADS / 32;
-                if (a.columns <= 1024)
-                    return launch(a.packed ? norm_forward_rows_kernel<T, 4, true> : norm_forward_rows_kernel<T, 4, false>, a, NORM_THREADS, teams, 8 * once, 2, st);
-                if (a.columns <= 2048)
-                    return launch(a.packed ? norm_forward_rows_kernel<T, 8, true> : norm_forward_rows_kernel<T, 8, false>, a, NORM_THREADS, teams, 8 * once, 2, st);
-                return launch(a.packed ? norm_forward_rows_kernel<T, 16, true> : norm_forward_rows_kernel<T, 16, false>, a, NORM_THREADS, teams, 8 * once, 2, st);
-            }
         return with_team<T>(a.columns, aligned, [&](auto team, int threads) {
             typedef decltype(team) S;
             auto kernel = norm_forward_kernel<T, S, false>;
             if constexpr (S::VEC > 1)
                 if (a.packed) kernel = norm_forward_kernel<T, S, true>;
-            return launch(kernel, a, threads, S::BLOCK ? 1 : NORM_THREADS / S::LANES, once * (S::BLOCK ? 512 / threads > 0 ? 512 / threads : 1 : 1) , sizeof(T), st);
+            return launch(kernel, a, threads, S::BLOCK ? 1 : NORM_THREADS / S::LANES, (int64_t)sm_count() * (S::ON_SM / threads), sizeof(T), st);
         });
     });
 }
