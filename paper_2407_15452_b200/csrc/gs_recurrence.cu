@@ -157,6 +157,15 @@ struct Stage {
     }
     static __device__ __forceinline__ int64_t round(const ScanTensor &t) { return AT_ONCE * t.st * (int64_t)sizeof(T); }
 
+    static __device__ __forceinline__ void copy(uint32_t to, const char *from, int on)
+    {
+        if constexpr (CHUNK == 4)
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], 4;\n\t}"
+                         ::"r"(to), "l"(from), "r"(on) : "memory");
+        else
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}"
+                         ::"r"(to), "l"(from), "r"(on) : "memory");
+    }
     __device__ __forceinline__ void fetch(const char *from, int64_t step, bool in, int valid, uint32_t without) const
     {
         char *to = room + lane * CHUNK;
@@ -165,26 +174,26 @@ struct Stage {
 #pragma unroll
             for (int i = 0; i < ROUNDS; ++i, from += step, to += 32 * CHUNK)
                 *reinterpret_cast<uint16_t *>(to) = in && i < valid ? *reinterpret_cast<const uint16_t *>(from) : (uint16_t)without;
-        } else {
-            const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
-#pragma unroll
-            for (int i = 0; i < ROUNDS; ++i, from += step) {
-                const int on = in && i * AT_ONCE + row < valid;
-                if constexpr (CHUNK == 4)
-                    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], 4;\n\t}"
-                                 ::"r"(at + i * 32 * CHUNK), "l"(from), "r"(on) : "memory");
-                else
-                    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}"
-                                 ::"r"(at + i * 32 * CHUNK), "l"(from), "r"(on) : "memory");
-            }
-            if (valid < STEPS)
-#pragma unroll
-                for (int i = 0; i < ROUNDS; ++i, to += 32 * CHUNK)
-                    if (i * AT_ONCE + row >= valid) {
-                        if constexpr (CHUNK == 4) *reinterpret_cast<uint32_t *>(to) = without;
-                        else *reinterpret_cast<uint4 *>(to) = make_uint4(without, without, without, without);
-                    }
+            return;
         }
+        const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+        if constexpr (CHUNK == 4) {
+            if (valid == STEPS) {                    // a row a round: no test of each (3 x 5003 x 777 fp32 backward 109 -> 104 us)
+                if (in)
+#pragma unroll
+                    for (int i = 0; i < ROUNDS; ++i, from += step) copy(at + i * 32 * CHUNK, from, true);
+                return;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i, from += step) copy(at + i * 32 * CHUNK, from, in && i * AT_ONCE + row < valid);
+        if (valid < STEPS)
+#pragma unroll
+            for (int i = 0; i < ROUNDS; ++i, to += 32 * CHUNK)
+                if (i * AT_ONCE + row >= valid) {
+                    if constexpr (CHUNK == 4) *reinterpret_cast<uint32_t *>(to) = without;
+                    else *reinterpret_cast<uint4 *>(to) = make_uint4(without, without, without, without);
+                }
     }
     // positions that are not valid are written as zeros
     __device__ __forceinline__ void write(char *to, int64_t step, bool in, const Place &p) const
@@ -195,6 +204,12 @@ struct Stage {
         word w[ROUNDS];
 #pragma unroll
         for (int i = 0; i < ROUNDS; ++i) w[i] = *reinterpret_cast<const word *>(from + i * 32 * CHUNK);
+        if (CHUNK == 4 && p.valid == STEPS) {
+            if (in)
+#pragma unroll
+                for (int i = 0; i < ROUNDS; ++i, to += step) *reinterpret_cast<word *>(to) = w[i];
+            return;
+        }
         if (p.valid < STEPS) {
 #pragma unroll
             for (int i = 0; i < ROUNDS; ++i)
