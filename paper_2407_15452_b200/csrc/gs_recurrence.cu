@@ -35,7 +35,7 @@ struct ScanArgs {
     Divider by_slabs;
     int64_t batch, channels, chains;      // chains = batch * slabs
     int32_t length, slabs, spans;         // slabs of 32 * V channels; spans = ceil(length / SPAN)
-    int32_t stretches;                    // warps that share a span
+    int32_t stretches;                    // warps that share a span; a block has as many chains as that leaves room for
     int32_t blocks;                       // blocks of a cluster
     unsigned long long *stalls;           // where blocks whose waits ran out are counted
 };
@@ -643,10 +643,17 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
     auto kernel = backward ? cluster ? scan_backward_kernel<T, V, CHUNK, true> : scan_backward_kernel<T, V, CHUNK, false>
                            : cluster ? scan_forward_kernel<T, V, CHUNK, true> : scan_forward_kernel<T, V, CHUNK, false>;
     SharedRecord &record = records[2 * backward + cluster];
-    const size_t shared = (size_t)(backward ? 6 : 3) * WARPS * Stage<T, V, CHUNK>::BYTES;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr = {};
-    const int64_t slots = (int64_t)sm_count() * (backward ? BACKWARD_BLOCKS : FORWARD_BLOCKS);     // blocks that the device holds at once
+    // a block's warps, and how many such blocks the device holds at once by registers and shared memory
+    a.stretches = a.length >= SPAN ? WARPS : a.length > STEPS ? (a.length + STEPS - 1) / STEPS : 1;
+    const int groups = WARPS / a.stretches, warps = groups * a.stretches;
+    const size_t shared = (size_t)(backward ? 6 : 3) * warps * Stage<T, V, CHUNK>::BYTES;
+    const size_t board = backward ? cluster ? sizeof(Board<V, true, true>) : sizeof(Board<V, false, true>)
+                                  : cluster ? sizeof(Board<V, true, false>) : sizeof(Board<V, false, false>);
+    const int by_registers = (backward ? BACKWARD_BLOCKS : FORWARD_BLOCKS) * WARPS / warps, by_shared = (int)((size_t)228 * 1024 / (shared + board + 1024));
+    const int64_t slots = (int64_t)sm_count() * (by_registers < by_shared ? by_registers : by_shared);
+    cfg.blockDim = dim3(32 * warps);
     int64_t grid;
     if (cluster) {
         a.stalls = stall_counter();
@@ -657,20 +664,14 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
         // 165, 118, 106, 97.  Sizes between lie between, or above: 3 blocks backward 157 and 101, 7 blocks fp32 107.
         a.blocks = 1;
         while (a.blocks < MOST_BLOCKS && a.blocks < a.spans && a.chains * a.blocks < slots) a.blocks *= 2;
-        a.stretches = WARPS;
         grid = a.chains * a.blocks;
-        cfg.blockDim = dim3(32 * WARPS);
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = (unsigned)a.blocks;
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
     } else {
-        // several chains a block where one needs few warps
         a.blocks = 1;
-        a.stretches = a.length > STEPS ? (a.length + STEPS - 1) / STEPS : 1;
-        const int groups = WARPS / a.stretches > 0 ? WARPS / a.stretches : 1;
-        cfg.blockDim = dim3(32 * groups * a.stretches);
         grid = (a.chains + groups - 1) / groups;
         if (grid > slots) grid = slots;
     }
