@@ -660,7 +660,7 @@ GS_API gs_status gs_clip_gradients(const gs_tensor *h_grads, const gs_tensor *h_
  * (they may hold anything, NaN included), their y, stats and dx are written as zeros and they add nothing to the sums.
  * x, y, dy, dx have type dtype, any strides (in elements) over batch and position and contiguous columns; d_weight,
  * d_bias and their gradients have type weight_dtype (GS_TABLE_F32 or dtype) and may be NULL (weight 1, bias 0; a
- * gradient that is NULL is not computed).  d_stats is float [batch][length][2]: mean and rstd, contiguous (NULL in
+ * gradient that is NULL is not computed).  d_stats is float [batch][length][2]: mean and rstd, contiguous, aligned to 8 bytes (NULL in
  * the forward call if no gradient will be asked for).  Inputs may have zero strides, outputs may not; no
  * output may overlap an input or another output.  Sums are fp32 in an order that the shapes, the types, the alignment and the device
  * fix: results are bitwise repeatable.
@@ -702,6 +702,9 @@ GS_API gs_status gs_layer_norm_backward(const gs_layer_norm_config *cfg, const v
  * d_states (NULL if no gradient will be asked for): gs_recurrence_states(cfg) floats, [batch][(length - 1) / 128][channels], the state
  * after every 128 positions but the last, from which the backward call computes the states in between again.
  * d_dout, d_dfinal NULL: zeros; d_dh0 NULL: not wanted.
+ * d_work: gs_recurrence_work(cfg) floats of the caller's, aligned to 16 bytes, written by the call; NULL is allowed, and long sequences of few channels then take
+ * longer (and may differ in their last bits: their sums are cut elsewhere).  gs_recurrence_states and gs_recurrence_work return -1
+ * for a configuration that the calls refuse.
  * Tensors have type dtype, any strides (in elements) over batch and position, contiguous channels; zero strides of inputs, overlaps
  * and repeatability as above (but for d_final = d_h0).  Products and sums are fp32.  What follows an infinity in x or a state is infinite or NaN.
  * Supported: lengths and channels up to 2^30, 2^40 states (batch x channels).  Errors: as above.
@@ -716,11 +719,13 @@ typedef struct gs_recurrence_config {
 } gs_recurrence_config;
 
 GS_API int64_t gs_recurrence_states(const gs_recurrence_config *cfg);
+GS_API int64_t gs_recurrence_work(const gs_recurrence_config *cfg);
 GS_API gs_status gs_recurrence_forward(const gs_recurrence_config *cfg, const void *d_gate, const void *d_x,
-                                const float *d_h0, void *d_out, float *d_final, float *d_states, void *stream);
+                                const float *d_h0, void *d_out, float *d_final, float *d_states, float *d_work,
+                                void *stream);
 GS_API gs_status gs_recurrence_backward(const gs_recurrence_config *cfg, const void *d_dout, const float *d_dfinal,
                                  const void *d_gate, const void *d_x, const float *d_h0, const float *d_states,
-                                 void *d_dgate, void *d_dx, float *d_dh0, void *stream);
+                                 void *d_dgate, void *d_dx, float *d_dh0, float *d_work, void *stream);
 
 /*
  * Activations kept in 8 bits between the forward and the backward pass: rows of `columns` values (row_stride elements

@@ -40,7 +40,7 @@ EXPORTS = [
     "gs_attention_forward", "gs_attention_backward", "gs_attention_backward_work",
     "gs_stalled_kernels", "gs_stall_drill", "gs_gradient_norm_work", "gs_gradient_norm", "gs_clip_gradients",
     "gs_layer_norm_forward", "gs_layer_norm_backward", "gs_layer_norm_backward_work",
-    "gs_recurrence_states", "gs_recurrence_forward", "gs_recurrence_backward",
+    "gs_recurrence_states", "gs_recurrence_work", "gs_recurrence_forward", "gs_recurrence_backward",
     "gs_checkpoint_pack", "gs_checkpoint_unpack",
 ]
 
@@ -135,8 +135,9 @@ def lib():
         L.gs_layer_norm_backward_work.argtypes, L.gs_layer_norm_backward_work.restype = [p], i64
         L.gs_layer_norm_backward.argtypes = [p] * 12
         L.gs_recurrence_states.argtypes, L.gs_recurrence_states.restype = [p], i64
-        L.gs_recurrence_forward.argtypes = [p] * 8
-        L.gs_recurrence_backward.argtypes = [p] * 11
+        L.gs_recurrence_work.argtypes, L.gs_recurrence_work.restype = [p], i64
+        L.gs_recurrence_forward.argtypes = [p] * 9
+        L.gs_recurrence_backward.argtypes = [p] * 12
         L.gs_checkpoint_pack.argtypes = [i32, p, i64, i64, i64, p, p, p]
         L.gs_checkpoint_unpack.argtypes = [i32, p, p, i64, i64, i64, p, p]
         _lib = L
@@ -751,6 +752,12 @@ def _state(t, device, shape, name):
     return 0 if t is None else _exactly(t, torch.float32, device, shape, name)
 
 
+@functools.lru_cache(maxsize=64)
+def _recurrence_work(length, device):
+    """Floats of scratch, which depend on the length (and the device) only."""
+    return max(0, lib().gs_recurrence_work(_pack_recurrence(0, length, 1, 1, 0, *(_NO_STRIDE2 * 6))))
+
+
 def gs_recurrence_forward(gate, x, h0=None, lens=None, keep=True, out=None, final=None):
     """Gated linear recurrence along the positions of x[batch, length, channels] (see gs.h) from the state h0 float32[batch, channels]
     (zeros if None).  Returns (out like x, final float32[batch, channels], states): states is what gs_recurrence_backward needs,
@@ -764,9 +771,10 @@ def gs_recurrence_forward(gate, x, h0=None, lens=None, keep=True, out=None, fina
     cfg = _pack_recurrence(_TABLE_DTYPE[dtype], n, b, c, _lens(lens, b, device, "lens"),
                            *_positions(gate, dtype, device, shape, "gate"), *_positions(x, dtype, device, shape, "x"),
                            *_positions(out, dtype, device, shape, "out"), *(_NO_STRIDE2 * 3))
+    work = final.new_empty(words) if (words := _recurrence_work(n, device)) else None
     _check(lib().gs_recurrence_forward(cfg, gate.data_ptr(), x.data_ptr(), _state(h0, device, (b, c), "h0"), out.data_ptr(),
                                        _state(final, device, (b, c), "final"), states.data_ptr() if keep else 0,
-                                       _raw_stream(device)))
+                                       0 if work is None else work.data_ptr(), _raw_stream(device)))
     return out, final, states
 
 
@@ -784,10 +792,12 @@ def gs_recurrence_backward(dout, gate, x, h0=None, states=None, dfinal=None, len
                            *_positions(gate, dtype, device, shape, "gate"), *_positions(x, dtype, device, shape, "x"), *_NO_STRIDE2,
                            *(_NO_STRIDE2 if dout is None else _positions(dout, dtype, device, shape, "dout")),
                            *_positions(dgate, dtype, device, shape, "dgate"), *_positions(dx, dtype, device, shape, "dx"))
+    work = dh0.new_empty(words) if (words := _recurrence_work(n, device)) else None
     at_states = _exactly(states, torch.float32, device, (b, kept, c), "states") if kept else 0
     _check(lib().gs_recurrence_backward(cfg, 0 if dout is None else dout.data_ptr(), _state(dfinal, device, (b, c), "dfinal"),
                                         gate.data_ptr(), x.data_ptr(), _state(h0, device, (b, c), "h0"), at_states,
-                                        dgate.data_ptr(), dx.data_ptr(), dh0.data_ptr(), _raw_stream(device)))
+                                        dgate.data_ptr(), dx.data_ptr(), dh0.data_ptr(), 0 if work is None else work.data_ptr(),
+                                        _raw_stream(device)))
     return dgate, dx, dh0
 
 

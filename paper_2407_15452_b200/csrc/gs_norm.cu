@@ -39,6 +39,9 @@ static NormRows rows(const void *p, const int64_t (&stride)[2]) { return {const_
 static gs_status tensors(const gs_layer_norm_config *c, NormArgs *a, NormRows **t, int n, int outputs, bool *aligned)
 {
     const int64_t es = (int64_t)size_of(c->dtype);
+    const uintptr_t vector = size_of(c->weight_dtype);
+    if ((uintptr_t)a->weight % vector || (uintptr_t)a->bias % vector) return bad("weight or bias not aligned to its element size");
+    if ((uintptr_t)a->stats % 8) return bad("d_stats must be aligned to 8 bytes");
     bool wide = c->columns * es % 16 == 0, one = !c->d_lens;
     for (int i = 0; i < n; ++i) {
         if (!t[i]->p) return bad("null pointer");

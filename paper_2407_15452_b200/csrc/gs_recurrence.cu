@@ -19,6 +19,9 @@
 namespace gs {
 
 static constexpr int STEPS = 16, WARPS = 8, SPAN = STEPS * WARPS, MOST_BLOCKS = 8;
+// Windows of a chain from which on clusters may share it: 8192 positions of 64 channels bf16 alone | shared forward 21 | 20 us, backward 29 | 20; 4096
+// positions 18 | 20 and 18 | 20
+static constexpr int LEAST_WINDOWS = 8;
 // Blocks of an SM: what their registers and the shared memory that the next inputs wait in allow
 static constexpr int FORWARD_BLOCKS = 3, BACKWARD_BLOCKS = 2;
 
@@ -37,6 +40,8 @@ struct ScanArgs {
     int32_t length, slabs, spans;         // slabs of 32 * V channels; spans = ceil(length / SPAN)
     int32_t stretches;                    // warps that share a span; a block has as many chains as that leaves room for
     int32_t blocks;                       // blocks of a cluster
+    int32_t parts, windows_of_part;       // clusters that share a chain, and windows that each of them has
+    float *sums;                          // where there are several: what each chain's parts amount to, see scan_sums_kernel
     unsigned long long *stalls;           // where blocks whose waits ran out are counted
 };
 
@@ -418,13 +423,25 @@ struct Items {
     Place place;
     bool in;                                         // the lane's chunks lie in the tensors
     int64_t chain;
-    int window, windows;
+    int part, window, first, last;                   // windows: the present one, and the part's
 
     __device__ __forceinline__ Items(const ScanArgs &args, const Seat<CLUSTER> &s) : a(args), seat(s)
     {
-        windows = CLUSTER ? (a.spans + a.blocks - 1) / a.blocks : 1;
-        window = CLUSTER && BACK ? windows - 1 : 0;
-        chain = CLUSTER ? blockIdx.x / a.blocks : (int64_t)blockIdx.x * seat.groups + seat.group;
+        part = first = last = 0;
+        if (CLUSTER) {
+            chain = blockIdx.x / a.blocks;
+            if (a.parts > 1) {
+                const int64_t whole = chain / a.parts;
+                part = (int)(chain - whole * a.parts);
+                chain = whole;
+            }
+            const int windows = (a.spans + a.blocks - 1) / a.blocks;
+            first = part * a.windows_of_part;
+            last = min(first + a.windows_of_part, windows) - 1;
+        } else {
+            chain = (int64_t)blockIdx.x * seat.groups + seat.group;
+        }
+        window = CLUSTER && BACK ? last : first;
         settle();
     }
     __device__ __forceinline__ void settle()
@@ -437,7 +454,7 @@ struct Items {
     {
         if (CLUSTER) {
             window += BACK ? -1 : 1;
-            if (BACK ? window < 0 : window >= windows) return false;
+            if (BACK ? window < first : window > last) return false;
             place.stretch(a, window * a.blocks + seat.rank, seat.warp);
         } else {
             chain += (int64_t)gridDim.x * seat.groups;
@@ -453,6 +470,70 @@ struct Items {
         else line = S::chunk(t, place, seat.lane);
     }
 };
+
+// Few chains, long ones: several clusters share a chain, each with a part of its windows, and a kernel ahead of theirs sums the parts up: a block for every `windows_of_part` spans, with as
+// many stretches one after another in each of its warps, leaves the function of its positions.  Entry 0 of a chain is its state before everything (a
+// function that takes no notice of what comes before), which the clusters read here and not from h0: one of them may have written the final state there.
+// BACK: of r, and entry 0 is what comes from behind the end.
+template <typename T, int V, bool BACK>
+__global__ void __launch_bounds__(32 * WARPS) scan_sums_kernel(const __grid_constant__ ScanArgs a)
+{
+    typedef Lane<T, V> L;
+    typedef typename Vec<V>::type F;
+    __shared__ Affine<V> stretch[WARPS][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, each = a.parts * a.blocks;
+    const int64_t chain = blockIdx.x / each;
+    const int entry = (int)(blockIdx.x - chain * each);
+    Place p = place_of<V>(a, chain, lane);
+    Affine<V> own = {all_of<V>(1.0f), all_of<V>(0.0f)};
+    const ScanTensor &other = BACK ? a.dout : a.x;
+    for (int j = 0; j < a.windows_of_part; ++j) {
+        // this warp's positions follow one another, so that the order of the sums is the order of the positions
+        const int64_t t0 = ((int64_t)entry * WARPS + warp) * a.windows_of_part * STEPS + j * STEPS;
+        const int valid = (int)min((int64_t)STEPS, max((int64_t)p.len - t0, (int64_t)0));
+        if (valid == 0) break;
+        const int64_t at = p.c + (p.on ? lane * V : 0);
+        const char *gate = static_cast<const char *>(a.gate.p) + (p.b * a.gate.sb + t0 * a.gate.st + at) * (int64_t)sizeof(T);
+        const char *from = static_cast<const char *>(other.p) + (p.b * other.sb + t0 * other.st + at) * (int64_t)sizeof(T);
+        typename L::raw z[STEPS], x[STEPS];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (s < valid) {
+                z[s] = *reinterpret_cast<const typename L::raw *>(gate + s * a.gate.st * (int64_t)sizeof(T));
+                x[s] = other.p ? *reinterpret_cast<const typename L::raw *>(from + s * other.st * (int64_t)sizeof(T)) : L::put(all_of<V>(0.0f));
+            }
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (s < valid) {
+                const F n = minus_shut(exp_of<T>(L::get(z[s])));
+                if (!BACK) own.b = advance(n, own.b, L::get(x[s]));
+                own.p = fma_of(n, own.p, own.p);
+                if (BACK) own.b = fma_of(own.p, L::get(x[s]), own.b);
+            }
+    }
+    stretch[warp][lane] = own;
+    __syncthreads();
+    if (warp) return;
+    Affine<V> all = stretch[BACK ? WARPS - 1 : 0][lane];
+    for (int i = 1; i < WARPS; ++i) all.before(stretch[BACK ? WARPS - 1 - i : i][lane]);
+    Affine<V> *to = reinterpret_cast<Affine<V> *>(a.sums) + chain * (each + 1) * 32 + lane;
+    to[(BACK ? each - entry : 1 + entry) * 32] = all;
+    if (entry == 0) {
+        const F h = load_state<V>(BACK ? a.dfinal : a.h0, p.b, a.channels, p, lane);
+        to[0] = {all_of<V>(0.0f), BACK ? h : mul_of(h, all_of<V>(-1.0f))};
+    }
+}
+// the state before a part (BACK: r behind it), from the sums of those before
+template <int V, bool BACK>
+__device__ __forceinline__ typename Vec<V>::type part_start(const ScanArgs &a, int64_t chain, int part, int lane)
+{
+    const int each = a.parts * a.blocks, entries = 1 + (BACK ? a.parts - 1 - part : part) * a.blocks;
+    const Affine<V> *from = reinterpret_cast<const Affine<V> *>(a.sums) + chain * (each + 1) * 32 + lane;
+    typename Vec<V>::type carry = all_of<V>(0.0f);
+#pragma unroll 8
+    for (int i = 0; i < entries; ++i) carry = from[(int64_t)i * 32].of(carry);
+    return carry;
+}
 
 template <typename T, int V, int CHUNK, bool CLUSTER>
 __global__ void __launch_bounds__(32 * WARPS, FORWARD_BLOCKS) scan_forward_kernel(const __grid_constant__ ScanArgs a)
@@ -477,7 +558,9 @@ __global__ void __launch_bounds__(32 * WARPS, FORWARD_BLOCKS) scan_forward_kerne
     fetches_end();
 
     const F minus = all_of<V>(-1.0f);
-    F next_h = load_state<V>(a.h0, item.place.b, a.channels, item.place, seat.lane), carry = mul_of(next_h, minus);
+    F next_h = load_state<V>(CLUSTER && a.parts > 1 ? nullptr : a.h0, item.place.b, a.channels, item.place, seat.lane);
+    F carry = mul_of(next_h, minus);
+    if (CLUSTER && a.parts > 1) carry = part_start<V, false>(a, item.chain, item.part, seat.lane);
     if (CLUSTER) cluster_wait();
     bool more;
     do {
@@ -564,6 +647,7 @@ __global__ void __launch_bounds__(32 * WARPS, BACKWARD_BLOCKS) scan_backward_ker
         return load_state<V>(p.k < a.spans ? a.states : nullptr, p.b * (a.spans - 1) + p.k - 1, a.channels, p, seat.lane);
     };
     F next_h = state_before(item.place), carry = load_state<V>(a.dfinal, item.place.b, a.channels, item.place, seat.lane), next_carry = carry;
+    if (CLUSTER && a.parts > 1) carry = part_start<V, true>(a, item.chain, item.part, seat.lane);
     if (CLUSTER) cluster_wait();
     bool more;
     int turn = 0;
@@ -664,7 +748,24 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
         // 165, 118, 106, 97.  Sizes between lie between, or above: 3 blocks backward 157 and 101, 7 blocks fp32 107.
         a.blocks = 1;
         while (a.blocks < MOST_BLOCKS && a.blocks < a.spans && a.chains * a.blocks < slots) a.blocks *= 2;
-        grid = a.chains * a.blocks;
+        // Parts of a chain, where its clusters alone leave most of the device idle: each part's windows come one after another, the parts'
+        // side by side, for a second reading of two inputs.  Alone | shared, bf16: 32768 x 64 forward 71 | 30 us, backward 98 | 30; 200000 x 64
+        // 409 | 76 and 572 | 67; 32768 x 512 73 | 65 (6 parts) and 100 | 73 (4); 32768 x 1024 96 | 108 (3) and 149 | 131 (2); fp32 2 x 16384 x
+        // 256 42 | 56 (3) and 64 | 63 (2)
+        const int windows = (a.spans + a.blocks - 1) / a.blocks;
+        a.parts = 1;
+        a.windows_of_part = windows;
+        const int64_t most = slots / (a.chains * a.blocks);
+        if (a.sums && a.blocks == MOST_BLOCKS && windows >= LEAST_WINDOWS && most >= (backward ? 2 : 4)) {
+            a.windows_of_part = (int)((windows + most - 1) / most);
+            a.parts = (windows + a.windows_of_part - 1) / a.windows_of_part;
+        }
+        grid = a.chains * a.parts * a.blocks;
+        if (a.parts > 1) {
+            if (backward) scan_sums_kernel<T, V, true><<<(unsigned)grid, 32 * WARPS, 0, st>>>(a);
+            else scan_sums_kernel<T, V, false><<<(unsigned)grid, 32 * WARPS, 0, st>>>(a);
+            GS_CUDA_TRY(cudaGetLastError());
+        }
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = (unsigned)a.blocks;
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
@@ -722,6 +823,9 @@ static ScanTensor tensor(const void *p, const int64_t (&stride)[2])
 static gs_status run(ScanArgs &a, int32_t dtype, const ScanTensor *const *t, int n, int outputs, bool backward, cudaStream_t st)
 {
     const int64_t es = (int64_t)size_of(dtype);
+    if ((uintptr_t)a.sums % 16) return bad("d_work must be aligned to 16 bytes");
+    for (const void *p : {(const void *)a.h0, (const void *)a.dfinal, (const void *)a.final_state, (const void *)a.dh0, (const void *)a.states})
+        if ((uintptr_t)p % 4) return bad("a state is not aligned to its element size");
     bool pairs = es == 2 && a.channels % 2 == 0, wide = a.channels * es % 16 == 0;
     for (int i = 0; i < n; ++i) {
         if (!t[i]->p) return bad("null pointer");
@@ -748,6 +852,15 @@ using namespace gs;
 
 extern "C" {
 
+int64_t gs_recurrence_work(const gs_recurrence_config *cfg)
+{
+    ScanArgs a;
+    if (check(cfg, &a) != GS_OK) return -1;
+    if (a.length <= (LEAST_WINDOWS - 1) * MOST_BLOCKS * SPAN) return 0;
+    // a block's function for each of the blocks that the device holds at once, and one more a chain, of which there are fewer: 64 channels of two numbers
+    return (int64_t)sm_count() * FORWARD_BLOCKS * 2 * 64 * 2;
+}
+
 int64_t gs_recurrence_states(const gs_recurrence_config *cfg)
 {
     ScanArgs a;
@@ -756,7 +869,7 @@ int64_t gs_recurrence_states(const gs_recurrence_config *cfg)
 }
 
 gs_status gs_recurrence_forward(const gs_recurrence_config *cfg, const void *d_gate, const void *d_x, const float *d_h0,
-                                void *d_out, float *d_final, float *d_states, void *stream)
+                                void *d_out, float *d_final, float *d_states, float *d_work, void *stream)
 {
     ScanArgs a;
     gs_status s = check(cfg, &a);
@@ -764,6 +877,7 @@ gs_status gs_recurrence_forward(const gs_recurrence_config *cfg, const void *d_g
     a.h0 = d_h0;
     a.final_state = d_final;
     a.states = d_states;
+    a.sums = d_work;
     if (a.length == 0) return copy_states(d_h0, d_final, a.batch * a.channels, (cudaStream_t)stream);
     a.gate = tensor(d_gate, cfg->gate_stride);
     a.x = tensor(d_x, cfg->x_stride);
@@ -774,7 +888,7 @@ gs_status gs_recurrence_forward(const gs_recurrence_config *cfg, const void *d_g
 
 gs_status gs_recurrence_backward(const gs_recurrence_config *cfg, const void *d_dout, const float *d_dfinal,
                                  const void *d_gate, const void *d_x, const float *d_h0, const float *d_states,
-                                 void *d_dgate, void *d_dx, float *d_dh0, void *stream)
+                                 void *d_dgate, void *d_dx, float *d_dh0, float *d_work, void *stream)
 {
     ScanArgs a;
     gs_status s = check(cfg, &a);
@@ -782,6 +896,7 @@ gs_status gs_recurrence_backward(const gs_recurrence_config *cfg, const void *d_
     a.h0 = d_h0;
     a.dfinal = d_dfinal;
     a.dh0 = d_dh0;
+    a.sums = d_work;
     a.states = const_cast<float *>(d_states);
     if (a.length == 0) return copy_states(d_dfinal, d_dh0, a.batch * a.channels, (cudaStream_t)stream);
     if (a.length > SPAN && !d_states) return bad("d_states is NULL");

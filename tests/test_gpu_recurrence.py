@@ -62,6 +62,17 @@ def test_long():
     check(*tensors(2, 6000, 64, BF16, 2))
 
 
+@pytest.mark.parametrize("b,n,c,dtype", [(1, 8193, 64, BF16), (1, 9300, 33, F32), (2, 8500, 16, F16), (1, 12300, 130, F32)])
+def test_chains_that_several_clusters_share(b, n, c, dtype):
+    args = gate, x, dout, h0, dfinal, lens = tensors(b, n, c, dtype, n, ragged=b > 1)
+    out, final, _, _ = check(*args)
+    state = h0.clone()                                                             # the final state in the place of the first
+    again, _, _ = B.gs_recurrence_forward(gate, x, state, lens, final=state)
+    assert torch.equal(again, out) and torch.equal(state, final)
+    if n == 8193:
+        check(gate, x, dout, None, None, torch.full((b,), n - 5000, dtype=torch.int32, device="cuda"))
+
+
 def test_no_incoming_gradient():
     gate, x, dout, h0, dfinal, lens = tensors(3, 200, 40, F32, 6)
     _, _, states = B.gs_recurrence_forward(gate, x, h0, lens)

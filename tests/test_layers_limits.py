@@ -60,6 +60,8 @@ def test_layer_norm_pointers(lib):
     refused(lib, forward(norm(), P, P, P, P, P, None, P, None), INVALID, "together")
     refused(lib, forward(norm(strides={"y": (0, 64)}), P, P, P, P, P, None, None, None), INVALID, "zero stride")
     refused(lib, forward(norm(strides={"y": (64, 0)}), P, P, P, P, P, None, None, None), INVALID, "zero stride")
+    refused(lib, forward(norm(), P, ctypes.c_void_p(4098), P, P, P, None, None, None), INVALID, "aligned")
+    refused(lib, forward(norm(), P, P, P, P, ctypes.c_void_p(4100), None, None, None), INVALID, "8 bytes")
     refused(lib, backward(norm(), P, P, P, P, P, P, P, P, P, P, None), INVALID, "either")
     refused(lib, backward(norm(), P, None, None, None, P, P, P, P, P, P, None), INVALID, "either")
     refused(lib, backward(norm(), P, None, P, None, P, P, P, P, P, P, None), INVALID, "either")
@@ -76,23 +78,26 @@ def test_layer_norm_pointers(lib):
     (dict(batch=1 << 62, channels=1 << 31), UNSUPPORTED, "states"), (dict(batch=1 << 32, channels=64), UNSUPPORTED, "one launch"),
 ])
 def test_recurrence_configurations(lib, kw, want, word):
-    refused(lib, lib.gs_recurrence_forward(scan(**kw), *(P,) * 6, None), want, word)
-    refused(lib, lib.gs_recurrence_backward(scan(**kw), *(P,) * 9, None), want, word)
+    refused(lib, lib.gs_recurrence_forward(scan(**kw), *(P,) * 6, None, None), want, word)
+    refused(lib, lib.gs_recurrence_backward(scan(**kw), *(P,) * 9, None, None), want, word)
     if word != "one launch":
-        assert lib.gs_recurrence_states(scan(**kw)) == -1
+        assert lib.gs_recurrence_states(scan(**kw)) == -1 and lib.gs_recurrence_work(scan(**kw)) == -1
 
 
 def test_recurrence_pointers(lib):
     forward, backward = lib.gs_recurrence_forward, lib.gs_recurrence_backward
-    refused(lib, forward(None, *(P,) * 6, None), INVALID, "NULL")
+    refused(lib, forward(None, *(P,) * 6, None, None), INVALID, "NULL")
     for missing in (0, 1, 3):
-        refused(lib, forward(scan(), *(None if i == missing else P for i in range(6)), None), INVALID, "null")
-    refused(lib, forward(scan(), P, ctypes.c_void_p(4099), P, P, P, P, None), INVALID, "aligned")
-    refused(lib, forward(scan(strides={"out": (0, 64)}), *(P,) * 6, None), INVALID, "zero stride")
+        refused(lib, forward(scan(), *(None if i == missing else P for i in range(6)), None, None), INVALID, "null")
+    refused(lib, forward(scan(), P, ctypes.c_void_p(4099), P, P, P, P, None, None), INVALID, "aligned")
+    refused(lib, forward(scan(strides={"out": (0, 64)}), *(P,) * 6, None, None), INVALID, "zero stride")
     for missing, word in ((2, "null"), (3, "null"), (5, "d_states"), (6, "null"), (7, "null")):
-        refused(lib, backward(scan(), *(None if i == missing else P for i in range(9)), None), INVALID, word)
-    refused(lib, backward(scan(strides={"dgate": (19200, 0)}), *(P,) * 9, None), INVALID, "zero stride")
+        refused(lib, backward(scan(), *(None if i == missing else P for i in range(9)), None, None), INVALID, word)
+    refused(lib, backward(scan(strides={"dgate": (19200, 0)}), *(P,) * 9, None, None), INVALID, "zero stride")
     assert lib.gs_recurrence_states(scan()) == 2 * 2 * 64
+    refused(lib, forward(scan(), *(P,) * 6, ctypes.c_void_p(4104), None), INVALID, "16 bytes")
+    refused(lib, backward(scan(), *(P,) * 9, ctypes.c_void_p(4104), None), INVALID, "16 bytes")
+    refused(lib, forward(scan(), P, P, ctypes.c_void_p(4098), P, P, P, None, None), INVALID, "aligned")
     for length, kept in ((0, 0), (1, 0), (128, 0), (129, 1), (256, 1), (257, 2)):
         assert lib.gs_recurrence_states(scan(length=length)) == 2 * 64 * kept
 
