@@ -42,6 +42,7 @@ static gs_status tensors(const gs_layer_norm_config *c, NormArgs *a, NormRows **
     const uintptr_t vector = size_of(c->weight_dtype);
     if ((uintptr_t)a->weight % vector || (uintptr_t)a->bias % vector) return bad("weight or bias not aligned to its element size");
     if ((uintptr_t)a->stats % 8) return bad("d_stats must be aligned to 8 bytes");
+    if ((uintptr_t)a->partial % 4 || (uintptr_t)a->scales % 4) return bad("d_work or d_scales not aligned to its element size");
     bool wide = c->columns * es % 16 == 0, one = !c->d_lens;
     for (int i = 0; i < n; ++i) {
         if (!t[i]->p) return bad("null pointer");
@@ -75,13 +76,13 @@ gs_status gs_layer_norm_forward(const gs_layer_norm_config *cfg, const void *d_x
     a.weight = d_weight;
     a.bias = d_bias;
     a.stats = d_stats;
+    a.scales = d_scales;
     NormRows *all[2] = {&a.y, &a.x};
     bool aligned;
     if ((s = tensors(cfg, &a, all, 2, 1, &aligned)) != GS_OK) return s;
     cudaStream_t st = (cudaStream_t)stream;
     if (d_packed && aligned && (uintptr_t)d_packed % 8 == 0) {
         a.packed = d_packed;
-        a.scales = d_scales;
     } else if (d_packed) {
         s = checkpoint_pack(cfg->dtype, a.x, cfg->d_lens, cfg->batch, cfg->length, cfg->columns, d_packed, d_scales, st);
         if (s != GS_OK) return s;

@@ -2,8 +2,10 @@
 // dy xh and dy over all rows.
 //
 // x (or its 8-bit form) and dy are read once.  A thread adds up the weights' gradients of its columns over the rows of its team;
-// the teams of a block are joined through shared memory, the blocks' sums by a second kernel, always in the same order.  Bound:
-// memory traffic.
+// the teams of a block are joined through shared memory, the blocks' sums by a second kernel, always in the same order.
+//
+// Bound: memory traffic in fp32 (400000 x 128 108 us, 5.7 TB/s), and nearly so in bf16 (61 us, 5.1 TB/s; 16384 x 4096 91 us, 4.4 TB/s: a thread
+// has 8 columns there, since their sums and weights are 24 registers and two blocks of 512 threads have to fit; with 16 columns 107 us).
 #include "gs_norm.cuh"
 
 namespace gs {

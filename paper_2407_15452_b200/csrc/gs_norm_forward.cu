@@ -2,8 +2,11 @@
 //
 // The mean is taken first and the squares of what differs from it second, both from registers; the differences' own mean, what rounding left
 // of the first, is taken with them, so that a mean far from zero costs no digits.  A block's warps do so each for its own columns and
-// then join: the squares about their means, and the squares of the means about the row's.  Bound: memory traffic, one read and one write of
-// every value.
+// then join: the squares about their means, and the squares of the means about the row's.
+//
+// Every value is read and written once, and memory traffic is the bound of fp32 rows and of short ones: 400000 x 128 take 67 us in fp32 (6.1 TB/s)
+// and 44 in bf16 (4.7).  Wide 16-bit rows are bound by the steps of a block's sums, shuffles and a barrier with few rows under way at once:
+// 16384 x 4096 bf16 73 us (3.7 TB/s), issue slots 68 % busy; with 32 columns a thread and the weights in shared memory 84, a warp for every row 95.
 #include "gs_norm.cuh"
 
 namespace gs {

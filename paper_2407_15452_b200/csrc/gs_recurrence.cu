@@ -5,11 +5,17 @@
 //
 // Over a stretch of positions the state is an affine function of the state before it, h_end = P h_start + B with
 // P the product of the a_t, and r_start = P r_end + R with the same P, so stretches can be computed side by side and joined.
-// A warp has a stretch of up to 16 positions of 32 (or 64) channels, a block 8 stretches one after another, SPAN positions,
-// and sequences longer than that are a cluster's: its blocks take neighbouring spans, exchange the (P, B) of theirs through
-// distributed shared memory and go on to the next window of spans with the state that all of them know.  Every input is read once and every
-// output written once; the joins are made in a fixed order.  The backward pass reads the state before each span, which the
-// forward pass left, computes h again (one stream fewer than reading it, and in fp32) and joins only r.
+// A warp has a stretch of up to 16 positions of 32 channels (64 of 16-bit tensors, two an instruction), a block 8 stretches one after
+// another, SPAN positions; sequences no longer than that share blocks, which go from one group of them to the next.  A longer sequence is a cluster's: its blocks take neighbouring
+// spans, send each other the (P, B) of theirs through distributed shared memory and go on to the next window of spans with the state that all of them
+// know by then.  Where that leaves the device idle, several clusters share a sequence.  A stretch is gone through twice, for its function and for its results, from gates held
+// in registers; the next one's inputs arrive in shared memory meanwhile.  Every input is read once and every output written once; the joins are made in
+// a fixed order.  The backward pass reads the state before each span, which the forward pass left, computes h again (one stream fewer than reading it,
+// and in fp32) and joins only r.
+//
+// Bound: memory traffic and, for 16 bits, the time that the dozen instructions of an element and the joins take beside it.  Long sequences, 4 x 8192 x 2048
+// bf16: forward 88 us (4.6 TB/s; without the joins 76, with loads and stores alone 66), backward 146 (4.6).  Walks of 40 x 128 bf16, 16384 of them: 101 us
+// (4.6 TB/s), 8192 of 80 f16 backward 152 (5.2); fp32 walks of 100 x 256 forward 213 us (5.9 TB/s), backward 345 (6.1).
 #include <math.h>
 
 #include <type_traits>

@@ -241,6 +241,18 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(dx, B.gs_recurrence_backward(dout, gate, x, h0, want[2], dfinal)[1])
 
 
+def test_a_wait_that_ran_out_fails_the_next_long_call():
+    gate, x, _, h0, _, _ = tensors(1, 300, 16, F32, 17)
+    B.gs_stall_drill()
+    torch.cuda.synchronize()
+    with pytest.raises(B.GsError, match="gave up a wait"):
+        B.gs_recurrence_forward(gate, x, h0)
+    B.gs_recurrence_forward(gate[:, :128], x[:, :128], h0)                         # short ones wait for nobody
+    assert B.gs_stalled_kernels(clear=True) == 1
+    B.gs_recurrence_forward(gate, x, h0)
+    assert B.gs_stalled_kernels() == 0
+
+
 def test_empty():
     for b, n in ((0, 5), (3, 0), (0, 0)):
         x = torch.empty((b, n, 16), device="cuda")

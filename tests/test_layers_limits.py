@@ -62,6 +62,8 @@ def test_layer_norm_pointers(lib):
     refused(lib, forward(norm(strides={"y": (64, 0)}), P, P, P, P, P, None, None, None), INVALID, "zero stride")
     refused(lib, forward(norm(), P, ctypes.c_void_p(4098), P, P, P, None, None, None), INVALID, "aligned")
     refused(lib, forward(norm(), P, P, P, P, ctypes.c_void_p(4100), None, None, None), INVALID, "8 bytes")
+    refused(lib, forward(norm(), P, P, P, P, P, P, ctypes.c_void_p(4098), None), INVALID, "aligned")
+    refused(lib, backward(norm(), P, P, None, None, P, P, ctypes.c_void_p(4098), P, P, P, None), INVALID, "aligned")
     refused(lib, backward(norm(), P, P, P, P, P, P, P, P, P, P, None), INVALID, "either")
     refused(lib, backward(norm(), P, None, None, None, P, P, P, P, P, P, None), INVALID, "either")
     refused(lib, backward(norm(), P, None, P, None, P, P, P, P, P, P, None), INVALID, "either")
