@@ -143,12 +143,12 @@ __device__ __forceinline__ float2 team_sum(float2 v, TeamSums &sums)
     sums.turn ^= 1;
     if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
     __syncthreads();
-    const int lane = threadIdx.x & 31;
-    v = lane < (int)blockDim.x >> 5 ? place[lane] : make_float2(0.0f, 0.0f);         // at most 16 warps
+    const int w = threadIdx.x & 15;                                // at most 16 warps
+    v = w < (int)blockDim.x >> 5 ? place[w] : make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int o = 8; o; o >>= 1)
         v = add_of(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
-    return make_float2(__shfl_sync(0xffffffffu, v.x, 0), __shfl_sync(0xffffffffu, v.y, 0));
+    return v;
 }
 
 // a piece of a row, all of which lies in the row or nothing (VEC > 1 only where columns % VEC == 0)

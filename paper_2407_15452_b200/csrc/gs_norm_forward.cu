@@ -6,7 +6,7 @@
 //
 // Every value is read and written once, and memory traffic is the bound of fp32 rows and of short ones: 400000 x 128 take 67 us in fp32 (6.1 TB/s)
 // and 44 in bf16 (4.7).  Wide 16-bit rows are bound by the steps of a block's sums, shuffles and a barrier with few rows under way at once:
-// 16384 x 4096 bf16 73 us (3.7 TB/s), issue slots 68 % busy; with 32 columns a thread and the weights in shared memory 84, a warp for every row 95.
+// 16384 x 4096 bf16 71 us (3.8 TB/s); with 32 columns a thread and the weights in shared memory 84, a warp for every row 95.
 #include "gs_norm.cuh"
 
 namespace gs {
@@ -100,18 +100,16 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) norm_forward_kernel(c
             turn ^= 1;
             if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = make_float4(mean, t.x, m2, in_group);
             __syncthreads();
-            const int other = threadIdx.x & 31;                      // at most 16 warps
+            const int other = threadIdx.x & 15;                      // at most 16 warps
             const float first = place[0].x;
             const float4 its = other < (int)blockDim.x >> 5 ? place[other] : make_float4(first, 0.0f, 0.0f, 0.0f);
-            float off = (its.x - first + its.y) * its.w;
+            const float d = its.x - first + its.y;
+            float2 all = make_float2(d * its.w, fmaf(d * d, its.w, its.z));
 #pragma unroll
-            for (int o = 8; o; o >>= 1) off += __shfl_xor_sync(0xffffffffu, off, o);
-            off = __shfl_sync(0xffffffffu, off, 0) * inverse;
-            const float d = its.x - first + its.y - off;
-            m2 = fmaf(d * d, its.w, its.z);
-#pragma unroll
-            for (int o = 8; o; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
-            m2 = __shfl_sync(0xffffffffu, m2, 0);
+            for (int o = 8; o; o >>= 1)
+                all = add_of(all, make_float2(__shfl_xor_sync(0xffffffffu, all.x, o), __shfl_xor_sync(0xffffffffu, all.y, o)));
+            const float off = all.x * inverse;
+            m2 = fmaf(-off, all.x, all.y);
             less = first - mean + off;
             whole = first + off;
         }

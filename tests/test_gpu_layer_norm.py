@@ -73,6 +73,16 @@ def test_a_mean_far_from_zero(columns):
     check(x, torch.randn_like(x), None, None, None)
 
 
+@pytest.mark.parametrize("dtype", [F16, F32])
+@pytest.mark.parametrize("columns", [520, 1024, 4096, 8192])
+def test_a_few_columns_far_from_the_rest(columns, dtype):
+    gen = torch.Generator("cuda").manual_seed(6)
+    for first, count, value in ((0, 1, 1e4), (0, 8, 1e4), (256, 8, -3e4), (columns - 8, 8, 2e3), (0, 200, 500.0)):
+        x = torch.randn((1, 20, columns), generator=gen, device="cuda")
+        x[..., first:first + count] += value
+        check(x.to(dtype), torch.randn_like(x).to(dtype), None, None, None)
+
+
 def test_constant_rows_and_zero_eps():
     x = torch.full((1, 4, 40), 3.0, device="cuda")
     y, stats = B.gs_layer_norm_forward(x, None, torch.full((40,), 0.5, device="cuda"))
