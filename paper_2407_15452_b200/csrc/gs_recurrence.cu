@@ -355,38 +355,6 @@ struct Joins {
         for (int i = 0; i < count; ++i) ahead.before(board.stretch[place][BACK ? edge - i : edge + i][lane]);
         if (!CLUSTER) return;
         __syncwarp();
-        cluster_arrive();
-        cluster_wait();
-        if (threadIdx.x == 0 && stalls && *(volatile int *)&board.stalled) atomicAdd_system(stalls, 1ull);
-    }
-
-    // Gives away the function of this warp's stretch and hb, the b of h over it; h moves from the state before the block's first stretch to
-    // that before this one.
-    __device__ __forceinline__ void give(const Affine<V> &own, F hb, F &h)
-    {
-        const int place = CLUSTER ? 0 : window & 1;
-        if (CLUSTER && window > 0) tc::bar_wait(address(&board.read), (window - 1) & 1, &board.stalled);
-        board.stretch[place][first + warp][lane] = own;
-        if (BACK) board.ahead[BACK ? place : 0][BACK ? first + warp : 0][lane] = hb;
-        __syncthreads();
-        if (BACK)
-#pragma unroll 1
-            for (int i = 0; i < warp; ++i)
-                h = fma_of(board.stretch[place][first + i][lane].p, h, board.ahead[BACK ? place : 0][BACK ? first + i : 0][lane]);
-        ahead.p = all_of<V>(1.0f);
-        ahead.b = all_of<V>(0.0f);
-        const int count = BACK ? stretches - 1 - warp : warp, edge = BACK ? first + stretches - 1 : first;
-        if (CLUSTER && !BACK) {                      // all turns of the loop at once | one after another: 4 x 8192 x 2048
-            // bf16 forward 91 | 92 us, backward 146 | 144, walks of 40 101 | 97
-#pragma unroll
-            for (int i = 0; i < WARPS - 1; ++i)
-                if (i < count) ahead.before(board.stretch[place][edge + i][lane]);
-        } else {
-#pragma unroll 1
-            for (int i = 0; i < count; ++i) ahead.before(board.stretch[place][BACK ? edge - i : edge + i][lane]);
-        }
-        if (!CLUSTER) return;
-        __syncwarp();
         if (lane == 0) tc::bar_arrive(address(&board.read));
         const uint32_t bar = address(&board.come[window & 1]);
         if (count == WARPS - 1) {                    // this stretch ends the block's span
