@@ -148,21 +148,23 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) norm_backward_kernel(
     }
 }
 
-// Sums of the blocks' partial sums: a block has 32 neighbouring values of [2][columns], warp w adds up every eighth block's
-__global__ void __launch_bounds__(256) norm_join_kernel(const float *partial, int blocks, int columns, void *dweight, void *dbias, int type)
+// Sums of the blocks' partial sums: a block has 32 neighbouring values of [2][columns], warp w adds up every 32nd block's (of 8 warps each
+// takes four times as many, one after another: 20000 x 1001 f16 backward 58 us in all, 53 with 32)
+static constexpr int JOIN_WARPS = 32;
+__global__ void __launch_bounds__(32 * JOIN_WARPS) norm_join_kernel(const float *partial, int blocks, int columns, void *dweight, void *dbias, int type)
 {
-    __shared__ float part[8][32];
+    __shared__ float part[JOIN_WARPS][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
     cudaGridDependencySynchronize();
     float s = 0.0f;
     if (i < 2 * columns)
 #pragma unroll 8
-        for (int k = warp; k < blocks; k += 8) s += partial[(int64_t)k * 2 * columns + i];
+        for (int k = warp; k < blocks; k += JOIN_WARPS) s += partial[(int64_t)k * 2 * columns + i];
     part[warp][lane] = s;
     __syncthreads();
     if (warp || i >= 2 * columns) return;
 #pragma unroll
-    for (int w = 1; w < 8; ++w) s += part[w][lane];
+    for (int w = 1; w < JOIN_WARPS; ++w) s += part[w][lane];
     void *to = i < columns ? dweight : dbias;
     const int c = i < columns ? i : i - columns;
     if (!to) return;
@@ -190,7 +192,7 @@ static gs_status launch(const NormArgs &args, int threads, int32_t weight_type, 
     norm_backward_kernel<T, S, KEPT><<<grid, threads, shared, st>>>(a);
     GS_CUDA_TRY(cudaGetLastError());
     if (sums)
-        GS_CUDA_TRY(launch_after(norm_join_kernel, (2 * a.columns + 31) / 32, 256, 0, st, a.partial, grid, a.columns, dweight, dbias,
+        GS_CUDA_TRY(launch_after(norm_join_kernel, (2 * a.columns + 31) / 32, 32 * JOIN_WARPS, 0, st, a.partial, grid, a.columns, dweight, dbias,
                                  weight_type));
     return GS_OK;
 }
