@@ -7,6 +7,7 @@ import torch
 
 from paper_2407_15452_b200 import binding as B
 from paper_2407_15452_b200 import workloads as WL
+from paper_2407_15452_b200.layers import gated_recurrence, kept_in_8_bits, layer_norm
 from tests.test_gpu_walk_encoder import _example
 
 pytestmark = pytest.mark.gpu
@@ -93,6 +94,63 @@ def test_walks_carried_on_one_node_at_a_time(dtype):
         on = (walks >= 0)[..., None]
         assert ((torch.cat(parts, 1) - whole) * on).abs().max() <= size * whole.abs().max()
         assert (state - final).abs().max() <= size * final.abs().max()
+
+
+def test_a_training_step_captured_into_a_graph():
+    # layer norm from 8 bits, the recurrence and a function whose input is kept, forward and backward, replayed on other inputs
+    gen = torch.Generator("cuda").manual_seed(4)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda")                   # noqa: E731
+    x, m, w, b = rand(4, 150, 64), rand(64, 128) / 8, 1 + 0.1 * rand(64), 0.1 * rand(64)
+    lens = torch.tensor([150, 0, 77, 149], dtype=torch.int32, device="cuda")
+    wanted = [t.requires_grad_(True) for t in (x, m, w, b)]
+
+    def block(x, m, w, b):
+        gate, value = (layer_norm(x, w, b, lens=lens, checkpoint=True) @ m).chunk(2, -1)
+        return gated_recurrence(gate, value, None, lens)[0]
+
+    def step():
+        y = x + block(x, m, w, b)
+        y = y + kept_in_8_bits(block, y, m, w, b)
+        return [y.detach(), *torch.autograd.grad(y.square().sum(), wanted)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        eager = step()                                       # also allocates what libraries need; its results stay alive
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for seed in range(2):
+        with torch.no_grad():
+            x.copy_(rand(4, 150, 64))
+            lens.copy_(torch.tensor([[20, 150, 0, 128], [129, 1, 150, 5]][seed], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, c in zip(got, step()):
+            assert torch.equal(a, c)
+    assert len(eager) == len(got)
+
+
+def test_two_streams_at_once():
+    gen = torch.Generator("cuda").manual_seed(5)
+    make = lambda: [torch.randn((2, 9000, 64), generator=gen, device="cuda").bfloat16() for _ in range(3)]      # noqa: E731
+    sets, streams = [make(), make()], [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def both(gate, x, dout):
+        out, final, states = B.gs_recurrence_forward(gate, x)
+        y, stats = B.gs_layer_norm_forward(out)
+        return [out, final, y, *B.gs_recurrence_backward(dout, gate, x, None, states), *B.gs_checkpoint_pack(y),
+                B.gs_layer_norm_backward(dout, out, None, None, stats)[0]]
+    want = [both(*s) for s in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i] = both(*sets[i])
+    torch.cuda.synchronize()
+    for g, r in zip(got, want):
+        assert all(torch.equal(a, c) for a, c in zip(g, r))
 
 
 @pytest.mark.parametrize("kw", [dict(mixer="recurrence"), dict(mixer="recurrence", norm=True), dict(norm=True, kept=True),
