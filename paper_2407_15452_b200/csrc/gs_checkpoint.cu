@@ -2,7 +2,7 @@
 //
 // A block of 128 columns is held by 16 or 32 lanes, 16 bytes of values each (or, where rows are not aligned to that, by a warp,
 // one value at a time), so that its largest magnitude is a few shuffles and every value is read once.  Bound: memory traffic; 16384 x 4096
-// there and back take 112 us in fp32 (6.0 TB/s) and 75 in bf16 (5.4 TB/s; packing is the slower half, its issue slots 70 % busy).
+// there and back take 110 us in fp32 (6.1 TB/s) and 75 in bf16 (5.4 TB/s; packing is the slower half, its issue slots 70 % busy).
 #include "gs_norm.cuh"
 
 namespace gs {
