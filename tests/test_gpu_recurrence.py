@@ -62,6 +62,12 @@ def test_long():
     check(*tensors(2, 6000, 64, BF16, 2))
 
 
+@pytest.mark.parametrize("b,n,c,dtype", [(460, 140, 64, BF16), (310, 300, 32, F32), (230, 300, 40, F16), (120, 600, 50, BF16), (60, 700, 96, F32)])
+def test_clusters_of_every_size(b, n, c, dtype):
+    # as many chains as leave 1, 2, 4 and 8 blocks to each of them
+    check(*tensors(b, n, c, dtype, b))
+
+
 @pytest.mark.parametrize("b,n,c,dtype", [(1, 8193, 64, BF16), (1, 9300, 33, F32), (2, 8500, 16, F16), (1, 12300, 130, F32)])
 def test_chains_that_several_clusters_share(b, n, c, dtype):
     args = gate, x, dout, h0, dfinal, lens = tensors(b, n, c, dtype, n, ragged=b > 1)
