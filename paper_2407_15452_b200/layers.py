@@ -111,9 +111,7 @@ class _Kept(torch.autograd.Function):
     @staticmethod
     def forward(ctx, function, x, *others):
         with torch.no_grad():
-            out = function(x, *others)
-        if not isinstance(out, torch.Tensor):
-            raise TypeError("the function must return one tensor")
+            out = _one_tensor(function(x, *others))
         tensors = [o for o in others if isinstance(o, torch.Tensor)]
         ctx.function, ctx.dtype = function, x.dtype
         ctx.plain = [None if isinstance(o, torch.Tensor) else o for o in others]
@@ -145,6 +143,15 @@ class _Kept(torch.autograd.Function):
         return None, dx, *rest
 
 
+_HIDDEN = "the function uses a tensor that requires a gradient and is not one of its arguments"
+
+
+def _one_tensor(out):
+    if not isinstance(out, torch.Tensor):
+        raise TypeError("the function must return one tensor")
+    return out
+
+
 def _only_from(out, leaves):
     """Raises if `out` was computed from tensors that ask for gradients and are not among `leaves`."""
     known, seen, todo = {id(t) for t in leaves}, set(), [out.grad_fn]
@@ -155,7 +162,7 @@ def _only_from(out, leaves):
         seen.add(node)
         variable = getattr(node, "variable", None)
         if variable is not None and id(variable) not in known:
-            raise RuntimeError("the function uses a tensor that requires a gradient and is not one of its arguments")
+            raise RuntimeError(_HIDDEN)
         todo += [n for n, _ in node.next_functions]
 
 
@@ -163,5 +170,11 @@ def kept_in_8_bits(function, x, *others):
     """function(x, *others), of which nothing but x in 8 bits (and the tensors among `others`: weights, lengths) is kept for the
     backward pass; that calls the function again, on x as the 8 bits have it, and differentiates it.  The result is exact, the
     gradients are those at the kept x.  The function must return one tensor, give the same result when it
-    is called again, and take every tensor that requires a gradient as an argument (it raises otherwise)."""
+    is called again, and take every tensor that requires a gradient as an argument itself (not in a list, a module or a closure): otherwise
+    the backward pass raises, and this call does where no argument requires a gradient, so that there would be no backward pass."""
+    if torch.is_grad_enabled() and not any(isinstance(t, torch.Tensor) and t.requires_grad for t in (x, *others)):
+        out = _one_tensor(function(x, *others))
+        if out.requires_grad:
+            raise RuntimeError(_HIDDEN)
+        return out
     return _Kept.apply(function, x, *others)

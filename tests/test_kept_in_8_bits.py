@@ -1,0 +1,36 @@
+"""Functions whose input is kept in 8 bits: parameters that are not arguments, arguments written into, and the second call of the
+function, which has to be the first one's.  On the CPU the library calls are stood in for by their definitions."""
+import pytest
+import torch
+
+from paper_2407_15452_b200 import layers as L
+from tests.test_layers_autograd import _inputs, device  # noqa: F401
+
+
+def _hidden(how, m):
+    """A function of one tensor that uses the parameter m without taking it as an argument, and what else to hand it."""
+    if how == "module":
+        linear = torch.nn.Linear(24, 24, device=m.device)
+        return linear, ()
+    if how == "closure":
+        return (lambda t: t @ m), ()
+    return (lambda t, ms: t @ ms[0]), ([m],)
+
+
+@pytest.mark.parametrize("how", ["module", "closure", "list"])
+def test_a_hidden_parameter_behind_an_input_without_gradient_raises(device, how):  # noqa: F811
+    x, m, w, b, lens = _inputs(device)
+    f, rest = _hidden(how, m)
+    with pytest.raises(RuntimeError, match="not one of its arguments"):
+        L.kept_in_8_bits(f, x.detach(), *rest)
+    with torch.no_grad():                                   # nothing to lose
+        assert torch.equal(L.kept_in_8_bits(f, x.detach(), *rest), f(x.detach(), *rest))
+    m.requires_grad_(False)
+    if how != "module":
+        y = L.kept_in_8_bits(f, x.detach(), *rest)
+        assert not y.requires_grad and torch.equal(y, f(x.detach(), *rest))
+    # beside an argument that asks for a gradient the backward pass raises
+    f, rest = _hidden(how, m.requires_grad_(True))
+    y = L.kept_in_8_bits(lambda t, scale, *r: f(t, *r) * scale, x.detach(), w.detach()[:1].requires_grad_(True), *rest)
+    with pytest.raises(RuntimeError, match="not one of its arguments"):
+        y.sum().backward()
