@@ -110,14 +110,18 @@ def gated_recurrence(gate, x, h0=None, lens=None):
 class _Kept(torch.autograd.Function):
     @staticmethod
     def forward(ctx, function, x, *others):
+        tensors = [o for o in others if isinstance(o, torch.Tensor)]
+        if any(ctx.needs_input_grad):                   # x as the function finds it
+            kept, versions = B.gs_checkpoint_pack(x if x.is_contiguous() else x.contiguous()), [t._version for t in (x, *tensors)]
         with torch.no_grad():
             out = _one_tensor(function(x, *others))
-        tensors = [o for o in others if isinstance(o, torch.Tensor)]
         ctx.function, ctx.dtype = function, x.dtype
         ctx.plain = [None if isinstance(o, torch.Tensor) else o for o in others]
         ctx.is_tensor = [isinstance(o, torch.Tensor) for o in others]
         if any(ctx.needs_input_grad):
-            ctx.save_for_backward(*B.gs_checkpoint_pack(x if x.is_contiguous() else x.contiguous()), *tensors)
+            if versions != [t._version for t in (x, *tensors)]:
+                raise RuntimeError("the function wrote into one of its arguments: it would do so again in the backward pass")
+            ctx.save_for_backward(*kept, *tensors)
         return out
 
     @staticmethod
@@ -169,9 +173,10 @@ def _only_from(out, leaves):
 def kept_in_8_bits(function, x, *others):
     """function(x, *others), of which nothing but x in 8 bits (and the tensors among `others`: weights, lengths) is kept for the
     backward pass; that calls the function again, on x as the 8 bits have it, and differentiates it.  The result is exact, the
-    gradients are those at the kept x.  The function must return one tensor, give the same result when it
-    is called again, and take every tensor that requires a gradient as an argument itself (not in a list, a module or a closure): otherwise
-    the backward pass raises, and this call does where no argument requires a gradient, so that there would be no backward pass."""
+    gradients are those at the kept x.  The function must return one tensor, give the same result when it is called again, leave
+    its arguments as they are (this call raises if they changed) and take every tensor that requires a gradient as an argument itself, not
+    in a list, a module or a closure: otherwise the backward pass raises, and this call does where no argument requires a gradient, so
+    that there would be no backward pass."""
     if torch.is_grad_enabled() and not any(isinstance(t, torch.Tensor) and t.requires_grad for t in (x, *others)):
         out = _one_tensor(function(x, *others))
         if out.requires_grad:

@@ -34,3 +34,15 @@ def test_a_hidden_parameter_behind_an_input_without_gradient_raises(device, how)
     y = L.kept_in_8_bits(lambda t, scale, *r: f(t, *r) * scale, x.detach(), w.detach()[:1].requires_grad_(True), *rest)
     with pytest.raises(RuntimeError, match="not one of its arguments"):
         y.sum().backward()
+
+
+def test_a_function_that_writes_into_its_arguments_raises(device):  # noqa: F811
+    x, m, w, b, lens = _inputs(device)
+    for f, args in ((lambda t, m: t.add_(1.0) @ m, (x.detach().clone(), m)),
+                    (lambda t, m: t[0].mul_(2.0) @ m, (x * 1.0, m.detach())),
+                    (lambda t, w: w.add_(1.0) * t, (x, w.detach().clone()))):
+        with pytest.raises(RuntimeError, match="wrote into"):
+            L.kept_in_8_bits(f, *args)
+    y = L.kept_in_8_bits(lambda t, m: (t + 0).add_(1.0) @ m, x.detach(), m)       # its own tensors it may change
+    y.sum().backward()
+    assert m.grad is not None
