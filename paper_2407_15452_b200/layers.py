@@ -4,6 +4,8 @@ derivative through it raises.
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import binding as B
@@ -107,6 +109,23 @@ def gated_recurrence(gate, x, h0=None, lens=None):
 
 
 # ---------------------------------------------------------------- activations in 8 bits
+def _autocast():
+    """The state of autocast: (device type, enabled, dtype, cache) of the types that tensors here may have."""
+    cache = torch.is_autocast_cache_enabled()
+    return [(k, torch.is_autocast_enabled(k), torch.get_autocast_dtype(k), cache) for k in ("cuda", "cpu")]
+
+
+@contextlib.contextmanager
+def _under(states):
+    """Autocast as _autocast found it then."""
+    with contextlib.ExitStack() as stack:
+        for then, now in zip(states, _autocast()):
+            if then != now and (then[1] or now[1]):
+                kind, enabled, dtype, cache = then
+                stack.enter_context(torch.autocast(kind, dtype, enabled, cache))
+        yield
+
+
 class _Kept(torch.autograd.Function):
     @staticmethod
     def forward(ctx, function, x, *others):
@@ -115,7 +134,7 @@ class _Kept(torch.autograd.Function):
             kept, versions = B.gs_checkpoint_pack(x if x.is_contiguous() else x.contiguous()), [t._version for t in (x, *tensors)]
         with torch.no_grad():
             out = _one_tensor(function(x, *others))
-        ctx.function, ctx.dtype = function, x.dtype
+        ctx.function, ctx.dtype, ctx.autocast = function, x.dtype, _autocast()
         ctx.plain = [None if isinstance(o, torch.Tensor) else o for o in others]
         ctx.is_tensor = [isinstance(o, torch.Tensor) for o in others]
         if any(ctx.needs_input_grad):
@@ -135,7 +154,8 @@ class _Kept(torch.autograd.Function):
         with torch.enable_grad():
             it = iter(tensors)
             others = [next(it) if is_tensor else p for is_tensor, p in zip(ctx.is_tensor, ctx.plain)]
-            out = ctx.function(x, *others)
+            with _under(ctx.autocast):
+                out = ctx.function(x, *others)
         asked = [t for t in (x, *tensors) if t.requires_grad]
         _only_from(out, asked)
         grads = iter(torch.autograd.grad(out, asked, dout, allow_unused=True) if out.requires_grad else [None] * len(asked))

@@ -46,3 +46,25 @@ def test_a_function_that_writes_into_its_arguments_raises(device):  # noqa: F811
     y = L.kept_in_8_bits(lambda t, m: (t + 0).add_(1.0) @ m, x.detach(), m)       # its own tensors it may change
     y.sum().backward()
     assert m.grad is not None
+
+
+@pytest.mark.parametrize("then,later", [(True, False), (False, True), (True, True)])
+def test_the_second_call_runs_under_the_first_ones_autocast(device, then, later):  # noqa: F811
+    x, m, w, b, lens = _inputs(device)
+    seen = []
+
+    def f(t, m):
+        y = t @ m
+        seen.append(y.dtype)
+        return y.float()
+    with torch.autocast(device, torch.bfloat16, enabled=then):
+        y = L.kept_in_8_bits(f, x, m)
+    with torch.autocast(device, torch.bfloat16, enabled=later):
+        y.sum().backward()
+    assert seen == [torch.bfloat16 if then else torch.float32] * 2
+    kept = L.B.gs_checkpoint_unpack(*L.B.gs_checkpoint_pack(x.detach())).requires_grad_(True)
+    with torch.autocast(device, torch.bfloat16, enabled=then):
+        again = (kept @ m).float()
+    with torch.autocast(device, torch.bfloat16, enabled=later):        # as the backward pass of anything else
+        want = torch.autograd.grad(again.sum(), [kept, m])
+    assert torch.equal(x.grad, want[0]) and torch.equal(m.grad, want[1])
