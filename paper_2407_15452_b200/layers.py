@@ -7,6 +7,7 @@ from __future__ import annotations
 import contextlib
 
 import torch
+from torch.utils._python_dispatch import TorchDispatchMode
 
 from . import binding as B
 
@@ -126,15 +127,55 @@ def _under(states):
         yield
 
 
+class _NoDraws(TorchDispatchMode):
+    """Refuses operations that draw random numbers."""
+
+    def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+        if torch.Tag.nondeterministic_seeded in func.tags:
+            raise RuntimeError("a function that draws random numbers cannot be captured into a CUDA graph by kept_in_8_bits: "
+                               "the call in the backward pass would draw others")
+        return func(*args, **(kwargs or {}))
+
+
+def _capturing(x):
+    return x.is_cuda and torch.cuda.is_current_stream_capturing()
+
+
+def _generators(x, others):
+    """What a function of these arguments may draw from, with the present states."""
+    gens = [torch.default_generator, *(o for o in others if isinstance(o, torch.Generator))]
+    if x.is_cuda:
+        gens.append(torch.cuda.default_generators[x.device.index])
+    return [(g, g.get_state()) for g in gens]
+
+
+@contextlib.contextmanager
+def _drawing_from(states):
+    """The generators as they were in `states`; afterwards as they are now."""
+    now = [(g, g.get_state()) for g, _ in states]
+    try:
+        for g, state in states:
+            g.set_state(state)
+        yield
+    finally:
+        for g, state in now:
+            g.set_state(state)
+
+
 class _Kept(torch.autograd.Function):
     @staticmethod
     def forward(ctx, function, x, *others):
         tensors = [o for o in others if isinstance(o, torch.Tensor)]
-        if any(ctx.needs_input_grad):                   # x as the function finds it
+        # x and the generators as the function finds them (states of generators cannot be had while a graph is captured)
+        random, capturing = [], _capturing(x)
+        if any(ctx.needs_input_grad):
             kept, versions = B.gs_checkpoint_pack(x if x.is_contiguous() else x.contiguous()), [t._version for t in (x, *tensors)]
-        with torch.no_grad():
+            if not capturing:
+                random = _generators(x, others)
+        with torch.no_grad(), _NoDraws() if capturing else contextlib.nullcontext():
             out = _one_tensor(function(x, *others))
         ctx.function, ctx.dtype, ctx.autocast = function, x.dtype, _autocast()
+        ctx.random = random if any(not torch.equal(state, g.get_state()) for g, state in random) else []
         ctx.plain = [None if isinstance(o, torch.Tensor) else o for o in others]
         ctx.is_tensor = [isinstance(o, torch.Tensor) for o in others]
         if any(ctx.needs_input_grad):
@@ -154,7 +195,7 @@ class _Kept(torch.autograd.Function):
         with torch.enable_grad():
             it = iter(tensors)
             others = [next(it) if is_tensor else p for is_tensor, p in zip(ctx.is_tensor, ctx.plain)]
-            with _under(ctx.autocast):
+            with _under(ctx.autocast), _drawing_from(ctx.random):
                 out = ctx.function(x, *others)
         asked = [t for t in (x, *tensors) if t.requires_grad]
         _only_from(out, asked)
@@ -193,7 +234,9 @@ def _only_from(out, leaves):
 def kept_in_8_bits(function, x, *others):
     """function(x, *others), of which nothing but x in 8 bits (and the tensors among `others`: weights, lengths) is kept for the
     backward pass; that calls the function again, on x as the 8 bits have it, and differentiates it.  The result is exact, the
-    gradients are those at the kept x.  The function must return one tensor, give the same result when it is called again, leave
+    gradients are those at the kept x.  The second call runs under the first one's autocast and draws the same random numbers (from
+    torch's own generators and from arguments that are generators; while a CUDA graph is captured, a function that draws raises).  The
+    function must return one tensor, give the same result when it is called again otherwise, leave
     its arguments as they are (this call raises if they changed) and take every tensor that requires a gradient as an argument itself, not
     in a list, a module or a closure: otherwise the backward pass raises, and this call does where no argument requires a gradient, so
     that there would be no backward pass."""

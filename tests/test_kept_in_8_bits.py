@@ -68,3 +68,53 @@ def test_the_second_call_runs_under_the_first_ones_autocast(device, then, later)
     with torch.autocast(device, torch.bfloat16, enabled=later):        # as the backward pass of anything else
         want = torch.autograd.grad(again.sum(), [kept, m])
     assert torch.equal(x.grad, want[0]) and torch.equal(m.grad, want[1])
+
+
+@pytest.mark.parametrize("source", ["default", "argument", "cpu"])
+def test_the_second_call_draws_the_first_ones_random_numbers(device, source):  # noqa: F811
+    x, m, w, b, lens = _inputs(device)
+    gen = torch.Generator(device).manual_seed(5)
+    seen = []
+
+    def f(t, m, gen):
+        shape, where = t.shape, "cpu" if source == "cpu" else t.device
+        mask = torch.rand(shape, device=where, generator=gen if source == "argument" else None).to(t.device) < 0.5
+        seen.append(mask)
+        return t * mask @ m
+    y = L.kept_in_8_bits(f, x, m, gen)
+    draw = lambda: torch.rand(8, device=device, generator=gen if source == "argument" else None)      # noqa: E731
+    states = [g.get_state() for g in (gen, torch.default_generator)]
+    if device == "cuda":
+        states.append(torch.cuda.get_rng_state())
+    y.sum().backward()
+    assert len(seen) == 2 and torch.equal(seen[0], seen[1])
+    # and what is drawn afterwards is what would have been drawn
+    after = [g.get_state() for g in (gen, torch.default_generator)] + ([torch.cuda.get_rng_state()] if device == "cuda" else [])
+    assert all(torch.equal(a, c) for a, c in zip(states, after))
+    assert not torch.equal(draw(), draw())
+    kept = L.B.gs_checkpoint_unpack(*L.B.gs_checkpoint_pack(x.detach())).requires_grad_(True)
+    want = torch.autograd.grad((kept * seen[0] @ m).sum(), [kept, m])
+    assert torch.equal(x.grad, want[0]) and torch.equal(m.grad, want[1])
+
+
+@pytest.mark.gpu
+def test_random_numbers_in_a_captured_function_are_refused():
+    gen = torch.Generator("cuda").manual_seed(4)
+    x, m = (torch.randn(s, generator=gen, device="cuda").requires_grad_(True) for s in ((2, 6, 24), (24, 48)))
+
+    def step(p):
+        y = L.kept_in_8_bits(lambda t, m: torch.nn.functional.dropout(t, p, training=p > 0) @ m, x, m)
+        return torch.autograd.grad(y.sum(), [x, m])
+    want = step(0.0)
+    step(0.5)                                               # eager calls may
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="random numbers"):
+        with torch.cuda.graph(graph):
+            step(0.5)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(0.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
