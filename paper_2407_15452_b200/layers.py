@@ -31,6 +31,11 @@ def _once(what):
     return gradient
 
 
+def _asks(*tensors):
+    """True if a gradient can be asked for; a function's needs_input_grad does not know of torch.no_grad()."""
+    return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
+
+
 def _rows_of_columns(t):
     return t if t is None or t.shape[-1] <= 1 or t.stride(-1) == 1 else t.contiguous()
 
@@ -42,8 +47,7 @@ _norm_gradient = _once("layer_norm")
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps, lens, checkpoint):
-        wanted = any(ctx.needs_input_grad)
-        if checkpoint and wanted:
+        if checkpoint:
             y, stats, packed, scales = B.gs_layer_norm_forward(x, weight, bias, eps, lens, checkpoint=True)
             ctx.save_for_backward(packed, weight, bias, stats, lens, scales)
         else:
@@ -74,7 +78,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, lens=None, checkpoint=False)
         if x.dim() == 0:
             raise ValueError("x must have at least one dimension")
         x = x.reshape(1, -1, shape[-1]) if shape[-1] else x.reshape(1, 0, 0)
-    return _LayerNorm.apply(x, weight, bias, eps, lens, checkpoint).view(shape)
+    return _LayerNorm.apply(x, weight, bias, eps, lens, checkpoint and _asks(x, weight, bias)).view(shape)
 
 
 # ---------------------------------------------------------------- gated linear recurrence
@@ -83,9 +87,9 @@ _recurrence_gradient = _once("gated_recurrence")
 
 class _Recurrence(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, gate, x, h0, lens):
+    def forward(ctx, gate, x, h0, lens, keep):
         ctx.set_materialize_grads(False)
-        out, final, states = B.gs_recurrence_forward(gate, x, h0, lens, keep=any(ctx.needs_input_grad))
+        out, final, states = B.gs_recurrence_forward(gate, x, h0, lens, keep=keep)
         ctx.save_for_backward(gate, x, h0, lens, states)
         return out, final
 
@@ -93,20 +97,20 @@ class _Recurrence(torch.autograd.Function):
     def backward(ctx, dout, dfinal):
         gate, x, h0, lens, states = ctx.saved_tensors
         if dout is None and dfinal is None:
-            return None, None, None, None
+            return None, None, None, None, None
 
         def call(dout, dfinal, gate, x, h0):
             return B.gs_recurrence_backward(_rows_of_columns(dout), gate, x, h0, states,
                                             None if dfinal is None else dfinal.contiguous(), lens)
         dgate, dx, dh0 = _recurrence_gradient(call, dout, dfinal, gate, x, h0)
-        return dgate, dx, None if h0 is None else dh0, None
+        return dgate, dx, None if h0 is None else dh0, None, None
 
 
 def gated_recurrence(gate, x, h0=None, lens=None):
     """h_t = a_t h_(t-1) + (1 - a_t) x_t with a_t = sigmoid(gate_t), along the positions of gate, x[batch, length, channels] from
     h0 float32[batch, channels] (zeros if None).  Returns (h like x, the state after each sequence's last valid
     position, float32[batch, channels]); the state, handed in as h0, continues the sequences."""
-    return _Recurrence.apply(gate, x, h0, lens)
+    return _Recurrence.apply(gate, x, h0, lens, _asks(gate, x, h0))
 
 
 # ---------------------------------------------------------------- activations in 8 bits
@@ -137,10 +141,6 @@ class _NoDraws(TorchDispatchMode):
         return func(*args, **(kwargs or {}))
 
 
-def _capturing(x):
-    return x.is_cuda and torch.cuda.is_current_stream_capturing()
-
-
 def _generators(x, others):
     """What a function of these arguments may draw from, with the present states."""
     gens = [torch.default_generator, *(o for o in others if isinstance(o, torch.Generator))]
@@ -167,21 +167,18 @@ class _Kept(torch.autograd.Function):
     def forward(ctx, function, x, *others):
         tensors = [o for o in others if isinstance(o, torch.Tensor)]
         # x and the generators as the function finds them (states of generators cannot be had while a graph is captured)
-        random, capturing = [], _capturing(x)
-        if any(ctx.needs_input_grad):
-            kept, versions = B.gs_checkpoint_pack(x if x.is_contiguous() else x.contiguous()), [t._version for t in (x, *tensors)]
-            if not capturing:
-                random = _generators(x, others)
+        kept, versions = B.gs_checkpoint_pack(x if x.is_contiguous() else x.contiguous()), [t._version for t in (x, *tensors)]
+        capturing = x.is_cuda and torch.cuda.is_current_stream_capturing()
+        random = [] if capturing else _generators(x, others)
         with torch.no_grad(), _NoDraws() if capturing else contextlib.nullcontext():
             out = _one_tensor(function(x, *others))
+        if versions != [t._version for t in (x, *tensors)]:
+            raise RuntimeError("the function wrote into one of its arguments: it would do so again in the backward pass")
         ctx.function, ctx.dtype, ctx.autocast = function, x.dtype, _autocast()
         ctx.random = random if any(not torch.equal(state, g.get_state()) for g, state in random) else []
         ctx.plain = [None if isinstance(o, torch.Tensor) else o for o in others]
         ctx.is_tensor = [isinstance(o, torch.Tensor) for o in others]
-        if any(ctx.needs_input_grad):
-            if versions != [t._version for t in (x, *tensors)]:
-                raise RuntimeError("the function wrote into one of its arguments: it would do so again in the backward pass")
-            ctx.save_for_backward(*kept, *tensors)
+        ctx.save_for_backward(*kept, *tensors)
         return out
 
     @staticmethod
@@ -240,9 +237,9 @@ def kept_in_8_bits(function, x, *others):
     its arguments as they are (this call raises if they changed) and take every tensor that requires a gradient as an argument itself, not
     in a list, a module or a closure: otherwise the backward pass raises, and this call does where no argument requires a gradient, so
     that there would be no backward pass."""
-    if torch.is_grad_enabled() and not any(isinstance(t, torch.Tensor) and t.requires_grad for t in (x, *others)):
-        out = _one_tensor(function(x, *others))
-        if out.requires_grad:
-            raise RuntimeError(_HIDDEN)
-        return out
-    return _Kept.apply(function, x, *others)
+    if _asks(x, *others):
+        return _Kept.apply(function, x, *others)
+    out = _one_tensor(function(x, *others))
+    if torch.is_grad_enabled() and out.requires_grad:
+        raise RuntimeError(_HIDDEN)
+    return out
