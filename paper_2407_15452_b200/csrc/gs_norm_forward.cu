@@ -113,7 +113,8 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) norm_forward_kernel(c
             less = first - mean + off;
             whole = first + off;
         }
-        const float rstd = rsqrtf(fmaxf(m2 * inverse, 0.0f) + a.eps);
+        const float variance = m2 * inverse;
+        const float rstd = rsqrtf((variance < 0.0f ? 0.0f : variance) + a.eps);     // a NaN stays one, which a maximum would let go
         if (at.there) {
             const F by = all_of<V>(rstd), minus_less = all_of<V>(-less);
 #pragma unroll
