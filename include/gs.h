@@ -667,8 +667,8 @@ GS_API gs_status gs_clip_gradients(const gs_tensor *h_grads, const gs_tensor *h_
  * With d_packed and d_scales the forward call also keeps x as gs_checkpoint_pack does (rows = batch * length), zeros
  * and a scale of zero at positions that are not valid; the backward call then takes them in place of x (d_x NULL): the gradients of
  * the formulas above with mean and rstd of the original and x as the checkpoint has it.
- * d_work: gs_layer_norm_backward_work(cfg) floats of the caller's, written by the call (-1 for a configuration that
- * the calls refuse).  Supported: 1 to 16384 columns, 2^40 rows.  Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED, GS_ERR_CUDA.
+ * d_work: gs_layer_norm_backward_work(cfg) floats of the caller's, written by the call: two rows of columns for each thread block, so they grow with the
+ * number of rows up to what fills the device (-1 for a configuration that the calls refuse); not used, and may be NULL, where neither gradient is asked for.  Supported: 1 to 16384 columns, 2^40 rows.  Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED, GS_ERR_CUDA.
  */
 typedef struct gs_layer_norm_config {
     int32_t dtype;

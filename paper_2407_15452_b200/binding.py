@@ -713,8 +713,9 @@ def gs_layer_norm_forward(x, weight=None, bias=None, eps=1e-5, lens=None, checkp
 
 
 @functools.lru_cache(maxsize=256)
-def _norm_backward_work(dtype, columns, device):
-    return max(0, lib().gs_layer_norm_backward_work(_pack_norm(dtype, dtype, 0, 0, columns, 0.0, 0, *(_NO_STRIDE2 * 4))))
+def _norm_backward_work(dtype, rows, columns, device):
+    """Floats of scratch, which follow the number of blocks."""
+    return max(0, lib().gs_layer_norm_backward_work(_pack_norm(dtype, dtype, 1, rows, columns, 0.0, 0, *(_NO_STRIDE2 * 4))))
 
 
 def gs_layer_norm_backward(dy, x, weight, bias, stats, lens=None, scales=None, dx=None):
@@ -738,7 +739,7 @@ def gs_layer_norm_backward(dy, x, weight, bias, stats, lens=None, scales=None, d
     _vector(bias, wt, device, c, "bias")
     dweight = None if weight is None else torch.empty_like(weight)
     dbias = None if bias is None else torch.empty_like(bias)
-    work = stats.new_empty(_norm_backward_work(_TABLE_DTYPE[dtype], c, device))
+    work = stats.new_empty(_norm_backward_work(_TABLE_DTYPE[dtype], b * n, c, device))
     _check(lib().gs_layer_norm_backward(cfg, dy.data_ptr(), at_x, packed, at_scales, at_weight, at_stats, work.data_ptr(),
                                         dx.data_ptr(), 0 if dweight is None else dweight.data_ptr(),
                                         0 if dbias is None else dbias.data_ptr(), _raw_stream(device)))

@@ -94,7 +94,7 @@ int64_t gs_layer_norm_backward_work(const gs_layer_norm_config *cfg)
 {
     NormArgs a;
     if (fill(cfg, &a) != GS_OK) return -1;
-    return (int64_t)sm_count() * NORM_PARTIALS * 2 * a.columns;
+    return norm_backward_partials(a.rows, a.columns, cfg->dtype) * 2 * a.columns;
 }
 
 gs_status gs_layer_norm_backward(const gs_layer_norm_config *cfg, const void *d_dy, const void *d_x, const int8_t *d_packed,

@@ -223,6 +223,8 @@ static gs_status with_team(int columns, bool aligned, F &&launch)
 // gs_norm_forward.cu, gs_norm_backward.cu
 gs_status norm_forward(const NormArgs &a, int32_t dtype, bool aligned, cudaStream_t st);
 gs_status norm_backward(const NormArgs &a, int32_t dtype, bool aligned, void *dweight, void *dbias, cudaStream_t st);
+// blocks that leave sums of their rows for another kernel: as many as any alignment of the tensors takes
+int64_t norm_backward_partials(int64_t rows, int32_t columns, int32_t dtype);
 // gs_checkpoint.cu
 gs_status checkpoint_pack(int32_t dtype, const NormRows &x, const int32_t *lens, int64_t batch, int64_t length, int64_t columns,
                           int8_t *packed, float *scales, cudaStream_t st);

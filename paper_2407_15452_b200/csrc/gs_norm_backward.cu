@@ -173,16 +173,23 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) norm_join_kernel(const float 
     else static_cast<__nv_bfloat16 *>(to)[c] = from_float<__nv_bfloat16>(s);
 }
 
+// Blocks of a launch: one for every so many rows, at most what the device holds at once
+template <typename S>
+static int grid_of(int64_t rows, int threads)
+{
+    const int teams = S::BLOCK ? 1 : NORM_THREADS / S::LANES;
+    int per_sm = S::ON_SM / threads;
+    if (per_sm > NORM_PARTIALS) per_sm = NORM_PARTIALS;
+    const int64_t blocks = (rows + teams - 1) / teams, most = (int64_t)sm_count() * per_sm;
+    return (int)(blocks < most ? blocks : most);
+}
+
 template <typename T, typename S, bool KEPT>
 static gs_status launch(const NormArgs &args, int threads, int32_t weight_type, void *dweight, void *dbias, cudaStream_t st)
 {
     NormArgs a = args;
-    const int teams = S::BLOCK ? 1 : NORM_THREADS / S::LANES;
-    int per_sm = S::ON_SM / threads;
-    if (per_sm > NORM_PARTIALS) per_sm = NORM_PARTIALS;
-    const int64_t blocks = (a.rows + teams - 1) / teams, most = (int64_t)sm_count() * per_sm;
-    const int grid = (int)(blocks < most ? blocks : most);
-    set_step(a, (int64_t)grid * teams, sizeof(T));
+    const int grid = grid_of<S>(a.rows, threads);
+    set_step(a, (int64_t)grid * (S::BLOCK ? 1 : NORM_THREADS / S::LANES), sizeof(T));
     const bool sums = dweight || dbias;
     if (!sums) a.partial = nullptr;
     const size_t shared = (S::FAR ? (size_t)S::NV * S::VEC * threads : S::BLOCK ? 0 : (size_t)NORM_THREADS * S::NV * S::VEC) * sizeof(float2);
@@ -195,6 +202,22 @@ static gs_status launch(const NormArgs &args, int threads, int32_t weight_type, 
         GS_CUDA_TRY(launch_after(norm_join_kernel, (2 * a.columns + 31) / 32, 32 * JOIN_WARPS, 0, st, a.partial, grid, a.columns, dweight, dbias,
                                  weight_type));
     return GS_OK;
+}
+
+int64_t norm_backward_partials(int64_t rows, int32_t columns, int32_t dtype)
+{
+    int most = 0;
+    with_type(dtype, [&](auto t) {
+        typedef decltype(t) T;
+        auto count = [&](auto team, int threads) {
+            const int grid = grid_of<decltype(team)>(rows, threads);
+            if (grid > most) most = grid;
+            return GS_OK;
+        };
+        if (columns % Wide<T>::N == 0) with_team<T>(columns, true, count);
+        return with_team<T>(columns, false, count);
+    });
+    return most;
 }
 
 gs_status norm_backward(const NormArgs &a, int32_t dtype, bool aligned, void *dweight, void *dbias, cudaStream_t st)
