@@ -718,9 +718,9 @@ def _norm_backward_work(dtype, rows, columns, device):
     return max(0, lib().gs_layer_norm_backward_work(_pack_norm(dtype, dtype, 1, rows, columns, 0.0, 0, *(_NO_STRIDE2 * 4))))
 
 
-def gs_layer_norm_backward(dy, x, weight, bias, stats, lens=None, scales=None, dx=None):
-    """Gradients of gs_layer_norm_forward: returns (dx like dy, dweight, dbias), None for a weight or bias that is None.
-    x: the forward call's, or its `packed` together with its `scales`."""
+def gs_layer_norm_backward(dy, x, weight, bias, stats, lens=None, scales=None, dx=None, sums=True):
+    """Gradients of gs_layer_norm_forward: returns (dx like dy, dweight, dbias), None for a weight or bias that is None, and for both
+    with sums=False (frozen ones).  x: the forward call's, or its `packed` together with its `scales`."""
     device = _leading(dy, "dy", _TABLE_DTYPE)
     shape, dtype = dy.shape, dy.dtype
     b, n, c = shape
@@ -737,10 +737,10 @@ def gs_layer_norm_backward(dy, x, weight, bias, stats, lens=None, scales=None, d
                      *_positions(dy, dtype, device, shape, "dy"), *_positions(dx, dtype, device, shape, "dx"))
     at_weight = _vector(weight, wt, device, c, "weight")
     _vector(bias, wt, device, c, "bias")
-    dweight = None if weight is None else torch.empty_like(weight)
-    dbias = None if bias is None else torch.empty_like(bias)
-    work = stats.new_empty(_norm_backward_work(_TABLE_DTYPE[dtype], b * n, c, device))
-    _check(lib().gs_layer_norm_backward(cfg, dy.data_ptr(), at_x, packed, at_scales, at_weight, at_stats, work.data_ptr(),
+    dweight = torch.empty_like(weight) if sums and weight is not None else None
+    dbias = torch.empty_like(bias) if sums and bias is not None else None
+    work = None if dweight is None and dbias is None else stats.new_empty(_norm_backward_work(_TABLE_DTYPE[dtype], b * n, c, device))
+    _check(lib().gs_layer_norm_backward(cfg, dy.data_ptr(), at_x, packed, at_scales, at_weight, at_stats, 0 if work is None else work.data_ptr(),
                                         dx.data_ptr(), 0 if dweight is None else dweight.data_ptr(),
                                         0 if dbias is None else dbias.data_ptr(), _raw_stream(device)))
     return dx, dweight, dbias

@@ -61,10 +61,13 @@ class _LayerNorm(torch.autograd.Function):
         if scales is not None and torch.is_grad_enabled():
             raise RuntimeError("layer_norm with checkpoint=True is differentiable once: call backward without create_graph")
 
+        frozen = not any(ctx.needs_input_grad[1:3]) and (weight is not None or bias is not None)
+
         def call(dy, weight, x, bias):
-            return tuple(g for g in B.gs_layer_norm_backward(_rows_of_columns(dy), x, weight, bias, stats, lens, scales) if g is not None)
+            kw = dict(sums=False) if frozen else {}
+            return tuple(g for g in B.gs_layer_norm_backward(_rows_of_columns(dy), x, weight, bias, stats, lens, scales, **kw) if g is not None)
         grads = iter(_norm_gradient(call, dy, weight, x, bias))
-        return next(grads), None if weight is None else next(grads), None if bias is None else next(grads), None, None, None
+        return next(grads), None if frozen or weight is None else next(grads), None if frozen or bias is None else next(grads), None, None, None
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, lens=None, checkpoint=False):
