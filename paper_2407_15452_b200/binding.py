@@ -653,6 +653,13 @@ def _positions(t, dtype, device, shape, name):
     return st[:2]
 
 
+def _like(t):
+    """A result beside t[batch, position, column]: its layout where that is dense, contiguous columns always (torch may put another
+    dimension inmost where positions of t share memory)."""
+    r = torch.empty_like(t)
+    return r if r.dim() != 3 or r.stride(2) == 1 else t.new_empty(t.shape)
+
+
 def _leading(t, name, dtypes):
     """Device and dtype code of the tensor that a call's other tensors are measured by."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in dtypes):
@@ -697,7 +704,7 @@ def gs_layer_norm_forward(x, weight=None, bias=None, eps=1e-5, lens=None, checkp
     shape, dtype = x.shape, x.dtype
     b, n, c = shape
     wt = _vector_dtype(weight, bias, dtype)
-    y = torch.empty_like(x) if y is None else y
+    y = _like(x) if y is None else y
     stats = x.new_empty((b, n, 2), dtype=torch.float32)
     packed = scales = None
     if checkpoint:
@@ -725,7 +732,7 @@ def gs_layer_norm_backward(dy, x, weight, bias, stats, lens=None, scales=None, d
     shape, dtype = dy.shape, dy.dtype
     b, n, c = shape
     wt = _vector_dtype(weight, bias, dtype)
-    dx = torch.empty_like(dy) if dx is None else dx
+    dx = _like(dy) if dx is None else dx
     if scales is None:
         at_x, strides, packed, at_scales = None, _positions(x, dtype, device, shape, "x"), 0, 0
         at_x = x.data_ptr()
@@ -766,7 +773,7 @@ def gs_recurrence_forward(gate, x, h0=None, lens=None, keep=True, out=None, fina
     device = _leading(x, "x", _TABLE_DTYPE)
     shape, dtype = x.shape, x.dtype
     b, n, c = shape
-    out = torch.empty_like(x) if out is None else out
+    out = _like(x) if out is None else out
     final = x.new_empty((b, c), dtype=torch.float32) if final is None else final
     states = x.new_empty((b, max(0, n - 1) // GS_RECURRENCE_SPAN, c), dtype=torch.float32) if keep else None
     cfg = _pack_recurrence(_TABLE_DTYPE[dtype], n, b, c, _lens(lens, b, device, "lens"),
@@ -785,8 +792,8 @@ def gs_recurrence_backward(dout, gate, x, h0=None, states=None, dfinal=None, len
     device = _leading(x, "x", _TABLE_DTYPE)
     shape, dtype = x.shape, x.dtype
     b, n, c = shape
-    dgate = torch.empty_like(gate) if dgate is None else dgate
-    dx = torch.empty_like(x) if dx is None else dx
+    dgate = _like(gate) if dgate is None else dgate
+    dx = _like(x) if dx is None else dx
     dh0 = x.new_empty((b, c), dtype=torch.float32)
     kept = max(0, n - 1) // GS_RECURRENCE_SPAN
     cfg = _pack_recurrence(_TABLE_DTYPE[dtype], n, b, c, _lens(lens, b, device, "lens"),
