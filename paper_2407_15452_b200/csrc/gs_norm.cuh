@@ -184,8 +184,9 @@ __device__ __forceinline__ void vector_piece(const NormArgs &a, const void *p, i
 }
 
 // Calls launch(Team, threads) with the team for rows of `columns` values: 16 columns a thread, as few threads as that takes up to a warp (fewer steps
-// to a sum; 400000 x 128 bf16 forward by 8 threads 51 us, by 16 68), a block beyond, with 8 columns a thread up to 4096 (backward 91 us against 107 with
-// 16) and 32 beyond 8192.  Rows that 16-byte accesses do not fit go one value at a time, by blocks whose size the compiler knows (20000 x 1001
+// to a sum; 400000 x 128 bf16 forward by 8 threads 51 us, by 16 68), a block beyond, with 8 columns a thread up to 4096 (16384 x 4096 bf16 backward 91 us
+// against 107 with 16; forward, which takes the same teams, 70 against 67, and keeping 8 bits with the backward pass from them 215 against 208, 65536 x 768 159
+// against 184) and 32 beyond 8192.  Rows that 16-byte accesses do not fit go one value at a time, by blocks whose size the compiler knows (20000 x 1001
 // bf16 backward 55 us, by blocks of any size 75).
 template <int VEC, int PER_THREAD, int LANES, typename F>
 static gs_status full_or_not(int columns, int threads, F &&launch)

@@ -4,9 +4,9 @@
 // of the first, is taken with them, so that a mean far from zero costs no digits.  A block's warps do so each for its own columns and
 // then join: the squares about their means, and the squares of the means about the row's.
 //
-// Every value is read and written once, and memory traffic is the bound of fp32 rows and of short ones: 400000 x 128 take 67 us in fp32 (6.1 TB/s)
-// and 44 in bf16 (4.7).  Wide 16-bit rows are bound by the steps of a block's sums, shuffles and a barrier with few rows under way at once:
-// 16384 x 4096 bf16 71 us (3.8 TB/s); with 32 columns a thread and the weights in shared memory 84, a warp for every row 95.
+// Every value is read and written once, and memory traffic is the bound of fp32 rows and of short ones: 400000 x 128 take 68 us in fp32 (6.0 TB/s)
+// and 44 in bf16 (4.7).  Wide 16-bit rows take 25 instructions a value, which keep the issue slots busy for two thirds of the time; the rest are the steps of a block's sums,
+// shuffles and a barrier with few rows under way at once: 16384 x 4096 bf16 71 us (3.8 TB/s), fp32 96 (5.6), keeping 8 bits and the backward pass from them 215 and 271; with 32 columns a thread and the weights in shared memory 84, a warp for every row 95.
 #include "gs_norm.cuh"
 
 namespace gs {

@@ -9,13 +9,16 @@
 // another, SPAN positions; sequences no longer than that share blocks, which go from one group of them to the next.  A longer sequence is a cluster's: its blocks take neighbouring
 // spans, send each other the (P, B) of theirs through distributed shared memory and go on to the next window of spans with the state that all of them
 // know by then.  Where that leaves the device idle, several clusters share a sequence.  A stretch is gone through twice, for its function and for its results, from gates held
-// in registers; the next one's inputs arrive in shared memory meanwhile.  Every input is read once and every output written once; the joins are made in
+// in registers; the next one's inputs arrive in shared memory meanwhile (rows of 16 bits that are
+// aligned to two bytes only come through registers, before the joins).  Every input is read once and every output written once; the joins are made in
 // a fixed order.  The backward pass reads the state before each span, which the forward pass left, computes h again (one stream fewer than reading it,
 // and in fp32) and joins only r.
 //
 // Bound: memory traffic and, for 16 bits, the time that the dozen instructions of an element and the joins take beside it.  Long sequences, 4 x 8192 x 2048
-// bf16: forward 92 us (4.4 TB/s; without the joins 76, with loads and stores alone 66), backward 144 (4.7).  Walks of 40 x 128 bf16, 16384 of them: 97 us
-// (4.8 TB/s), 8192 of 80 f16 backward 151 (5.2); fp32 walks of 100 x 256 forward 213 us (5.9 TB/s), backward 345 (6.1).
+// bf16: forward 93 us (4.3 TB/s; without the joins 76, with loads and stores alone 66), backward 145 to 155 (4.3 to 4.6).  Walks of 40 x 128 bf16, 16384 of
+// them: 97 to 105 us (4.6 to 4.9 TB/s), 8192 of 80 f16 backward 151 to 169 (4.7 to 5.3); fp32 walks of 100 x 256, 4096 of them, forward 211 us (6.0 TB/s), backward 353
+// (6.0).  (Ranges: several devices and runs.)  Rows aligned to four bytes only: 3 x 5003 x 777 fp32 backward 117 us (3 x 5000 x 776: 69); to two: 4 x 8192 x
+// 2047 bf16 254 us forward and 337 backward (2046 channels 126 and 264), 16384 walks of 40 x 127 223 and 434 (128 channels 99 and 171).
 #include <math.h>
 
 #include <type_traits>
@@ -25,7 +28,7 @@
 namespace gs {
 
 static constexpr int STEPS = 16, WARPS = 8, SPAN = STEPS * WARPS, MOST_BLOCKS = 8;
-// Windows of a chain from which on clusters may share it: 8192 positions of 64 channels bf16 alone | shared forward 21 | 20 us, backward 29 | 20; 4096
+// Windows of a chain from which on clusters may share it: 8192 positions of 64 channels bf16 alone | shared forward 22 | 19 us, backward 29 | 20; 4096
 // positions 18 | 20 and 18 | 20
 static constexpr int LEAST_WINDOWS = 8;
 // Blocks of an SM: what their registers and the shared memory that the next inputs wait in allow
@@ -145,8 +148,8 @@ __device__ __forceinline__ Place place_of(const ScanArgs &a, int64_t chain, int 
 }
 
 // A warp's stretch of one tensor in shared memory, [step][lane].  Lanes bring (and take away) CHUNK bytes each, 16 where the tensors' rows are
-// aligned to that, so that a stretch is four copies of a warp; each lane computes with its own channels of every position.  No registers
-// are held while inputs are on their way.  In the places of positions that are not valid stands `without`, a gate that is open (a = 1) or a zero, so that
+// aligned to that, so that a stretch is four copies of a warp; each lane computes with its own channels of every position.  Copies of 4 and 16
+// bytes hold no registers while they are on their way; there are none of 2, so those are loads that the warp waits for before it goes on.  In the places of positions that are not valid stands `without`, a gate that is open (a = 1) or a zero, so that
 // what is computed from them changes nothing and needs no test.
 template <typename T, int V, int CHUNK>
 struct Stage {
@@ -755,14 +758,14 @@ static gs_status launch(const ScanArgs &args, bool backward, cudaStream_t st)
         gs_status s = stalled_before();
         if (s != GS_OK) return s;
         // Clusters as small as fill the device: their blocks wait for one another in every window.  Measured with 1, 2, 4, 8 blocks:
-        // 4 x 8192 x 2048 bf16 forward (rule: 4) 117, 88, 88, 98 us, backward (4) 168, 142, 147, 165; 3 x 5003 x 777 fp32 backward (4)
-        // 165, 118, 106, 97.  Sizes between lie between, or above: 3 blocks backward 157 and 101, 7 blocks fp32 107.
+        // 4 x 8192 x 2048 bf16 forward (rule: 4) 127, 91, 93, 100 us, backward (4) 179, 139, 144, 160; 3 x 5003 x 777 fp32 backward (4)
+        // 164, 109, 117, 109.  Counts between (3, 7) lay between these or above.
         a.blocks = 1;
         while (a.blocks < MOST_BLOCKS && a.blocks < a.spans && a.chains * a.blocks < slots) a.blocks *= 2;
         // Parts of a chain, where its clusters alone leave most of the device idle: each part's windows come one after another, the parts'
-        // side by side, for a second reading of two inputs.  Alone | shared, bf16: 32768 x 64 forward 71 | 30 us, backward 98 | 30; 200000 x 64
-        // 409 | 76 and 572 | 67; 32768 x 512 73 | 65 (6 parts) and 100 | 73 (4); 32768 x 1024 96 | 108 (3) and 149 | 131 (2); fp32 2 x 16384 x
-        // 256 42 | 56 (3) and 64 | 63 (2)
+        // side by side, for a second reading of two inputs.  Alone | shared, bf16: 32768 x 64 forward 74 | 29 us, backward 99 | 29; 200000 x 64
+        // 427 | 77 and 582 | 64; 32768 x 512 74 | 64 (6 parts) and 101 | 72 (4); 32768 x 1024 97 | 108 (3) and 146 | 127 (2); fp32 2 x 16384 x
+        // 256 41 | 56 (3) and 64 | 62 (2)
         const int windows = (a.spans + a.blocks - 1) / a.blocks;
         a.parts = 1;
         a.windows_of_part = windows;
