@@ -165,17 +165,22 @@ def _drawing_from(states):
             g.set_state(state)
 
 
+def _versions(tensors):
+    """What changes when a tensor is written into (tensors of inference mode count nothing, and cannot be written into outside)."""
+    return [None if t.is_inference() else t._version for t in tensors]
+
+
 class _Kept(torch.autograd.Function):
     @staticmethod
     def forward(ctx, function, x, *others):
         tensors = [o for o in others if isinstance(o, torch.Tensor)]
         # x and the generators as the function finds them (states of generators cannot be had while a graph is captured)
-        kept, versions = B.gs_checkpoint_pack(x if x.is_contiguous() else x.contiguous()), [t._version for t in (x, *tensors)]
+        kept, versions = B.gs_checkpoint_pack(x if x.is_contiguous() else x.contiguous()), _versions((x, *tensors))
         capturing = x.is_cuda and torch.cuda.is_current_stream_capturing()
         random = [] if capturing else _generators(x, others)
         with torch.no_grad(), _NoDraws() if capturing else contextlib.nullcontext():
             out = _one_tensor(function(x, *others))
-        if versions != [t._version for t in (x, *tensors)]:
+        if versions != _versions((x, *tensors)):
             raise RuntimeError("the function wrote into one of its arguments: it would do so again in the backward pass")
         ctx.function, ctx.dtype, ctx.autocast = function, x.dtype, _autocast()
         ctx.random = random if any(not torch.equal(state, g.get_state()) for g, state in random) else []

@@ -118,3 +118,13 @@ def test_random_numbers_in_a_captured_function_are_refused():
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, c) for a, c in zip(got, want))
+
+
+def test_an_input_computed_in_inference_mode(device):  # noqa: F811
+    x, m, w, b, lens = _inputs(device)
+    with torch.inference_mode():
+        features = x * 2.0
+    L.kept_in_8_bits(lambda t, m: t @ m, features, m).sum().backward()
+    kept = L.B.gs_checkpoint_unpack(*L.B.gs_checkpoint_pack(features.clone()))
+    (want,) = torch.autograd.grad((kept @ m).sum(), m)
+    assert torch.equal(m.grad, want)
